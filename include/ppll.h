@@ -254,6 +254,83 @@ int ppll_block_phase_times(ppll_block_t* block, float* ms);
  * what the hardware byte counters of a profiler run are scaled against. */
 int ppll_probe_copy(const void* src_dev, void* dst_dev, size_t bytes, void* hip_stream);
 
+/* ------------------------------------------------------------------ orthogonalised updates
+ * Equal matrices in a flat blob of elements (parameters, gradients, momenta: a block's tables, or a caller's own).  Element (r, c) of
+ * matrix i is blob[offset + i * stride + r * ld + c].  The matrices of a group lie one behind the other (stride >= (rows - 1) * ld + cols)
+ * or side by side (stride >= cols, (count - 1) * stride + cols <= ld: the query, key and value parts of a [dim, 3 dim] weight).  No element
+ * belongs to two matrices of a call: groups whose extents overlap need one ld and different columns of it, else PPLL_ERR_SHAPE.
+ * rows, cols: 1..8192; count: 0..65535; offset and stride >= 0. */
+typedef struct {
+  int64_t offset, stride, ld;
+  int32_t rows, cols, count, reserved;   /* reserved: 0 */
+} ppll_matrix_group;
+
+/* Newton-Schulz orthogonalisation of every matrix G of up to 16 groups:
+ *   X = G / (|G|_F + 1e-7);  `steps` times  A = X X^T,  X = a X + (b A + c A A) X,  (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * (X^T X on the other side where rows > cols, which is the same), the published polynomial of the Muon optimizer: after 5 steps the
+ * singular values that are not tiny beside the largest lie around 1 (0.7 to 1.2).  in_dev and out_dev are blobs of `precision`'s type (PPLL_FP32, PPLL_BF16)
+ * with the groups' layout; out_dev may be in_dev; elements of out_dev outside the matrices are left as they are.  steps: 1..16.
+ * All arithmetic is at fp32 precision whichever the type (operands of the products as two fp16 terms each).  A matrix of zeros gives
+ * zeros; one with a NaN or an infinity gives NaN in all its elements and leaves the others alone.
+ * Workspace: ppll_orthogonalize_workspace_bytes(the same groups) bytes, used by nothing else until the stream has passed the call; its
+ * contents need not survive between calls, and calls that may run at the same time need one each.  Asynchronous on hip_stream; may be
+ * captured into a graph.  n_groups = 0 and groups of count 0 are allowed. */
+int ppll_orthogonalize_workspace_bytes(const ppll_matrix_group* groups, int32_t n_groups, size_t* bytes);
+int ppll_orthogonalize(const ppll_matrix_group* groups, int32_t n_groups, int32_t precision, int32_t steps, const void* in_dev,
+                       void* out_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* One step of the Muon optimizer on every matrix of the groups, in fp32 blobs of one layout:
+ *   m <- momentum * m + g;  u = g + momentum * m (nesterov) or m;  O = orthogonalised u (as above)
+ *   p <- p * (1 - lr * weight_decay) - lr * 0.2 * sqrt(max(rows, cols)) * O
+ * The last factor gives the update the root mean square of an AdamW update (0.2), so that one learning rate serves both.  shadow_dev
+ * (nullable): a bf16 blob of the same layout that receives the new p.  Workspace, steps, stream as above; the four blobs must not overlap.
+ * ppll_block_step with optimizer = PPLL_MUON makes this call for its weight matrices. */
+int ppll_muon_step(const ppll_matrix_group* groups, int32_t n_groups, int32_t steps, const float* grads_dev, float* momentum_dev,
+                   float* params_dev, void* shadow_dev, float lr, float momentum, int32_t nesterov, float weight_decay,
+                   void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------ queries and keys: norm and rotary positions
+ * Queries and keys of `rows` token rows as a projection leaves them: element d of head h of row r at q[r * q_ld + h * head_dim + d].  Either
+ * pointer may be null where its number of heads is 0.  Row strides in elements, at least heads * head_dim. */
+typedef struct {
+  void *q, *k;            /* device memory */
+  int64_t q_ld, k_ld;
+} ppll_queries_keys;
+
+/* The rotation: `axes` axes of positions (1..3: a sequence; height, width; time, height, width), pairs[a] pairs of each head turn with axis a,
+ * sum(pairs) <= head_dim / 2 = all pairs.  Pair p of P = sum(pairs) is elements (p, P + p) of the head, or with `neighbours` (2p, 2p + 1);
+ * elements from 2 P on do not turn.  Pair i of the n that belong to axis a turns by positions[token][a] * base^(-i / n) radians (the angle
+ * is reduced in 64 bits, so far positions lose nothing).  Row r holds token r % tokens: a batch of sequences with the same positions, or
+ * with tokens = rows one row of positions each. */
+typedef struct {
+  uint32_t struct_size;   /* = sizeof(ppll_rotary_config)                        */
+  int32_t precision;      /* element type of queries, keys and their gradients   */
+  int32_t rows, tokens;   /* rows >= 0 a multiple of tokens >= 1                 */
+  int32_t q_heads, k_heads;   /* each 0..65536, not both 0; they may differ      */
+  int32_t head_dim;       /* 2..256, even                                        */
+  int32_t axes;
+  int32_t pairs[3];
+  int32_t neighbours;
+  float base;             /* > 0 and finite                                      */
+  float norm_eps;         /* of the RMS norm, > 0; ignored without scales        */
+} ppll_rotary_config;
+
+/* Forward: y = R(position) z with z = x, or with scales z = x / sqrt(mean over the head of x^2 + norm_eps) * scale (the RMS norm of each
+ * head; the head_dim scales are shared by all heads).  positions_dev: int32 [tokens][axes]; q_scale_dev / k_scale_dev: fp32 [head_dim], both or
+ * neither (one is enough where the other side has no heads).  in, out, keep: keep (nullable) receives x as it is, for a backward pass when out
+ * is in.  out may be in (same pointers and strides); otherwise the buffers must not overlap.  Asynchronous on hip_stream. */
+int ppll_qk_rotary_forward(const ppll_rotary_config* cfg, const int32_t* positions_dev, const float* q_scale_dev, const float* k_scale_dev,
+                           const ppll_queries_keys* in, const ppll_queries_keys* out, const ppll_queries_keys* keep, void* hip_stream);
+
+/* Backward: from dy the gradient dx at the forward's input x, and with scales d_q_scale_dev / d_k_scale_dev, fp32 [head_dim], overwritten
+ * (zeros where rows = 0).  x: the forward's input, needed with scales only (else null).  dx may be dy.  Without scales no workspace is
+ * needed (null, 0), else ppll_qk_rotary_workspace_bytes(cfg) bytes that nothing else uses until the stream has passed the call.  The sums
+ * over rows and heads run in a fixed order. */
+int ppll_qk_rotary_workspace_bytes(const ppll_rotary_config* cfg, size_t* bytes);
+int ppll_qk_rotary_backward(const ppll_rotary_config* cfg, const int32_t* positions_dev, const float* q_scale_dev, const float* k_scale_dev,
+                            const ppll_queries_keys* x, const ppll_queries_keys* dy, const ppll_queries_keys* dx, float* d_q_scale_dev,
+                            float* d_k_scale_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -395,6 +395,56 @@ def adamw_update(p, g, m, v, t, lr, beta1, beta2, eps, weight_decay):
     return p - lr * mhat / (np.sqrt(vhat) + eps), m, v
 
 
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+
+
+def orthogonalize(g, steps=5):
+    """Newton-Schulz iteration on g / (|g| + 1e-7): every singular value s becomes a s + b s^3 + c s^5, `steps` times."""
+    if g.shape[0] > g.shape[1]:          # the same with X^T X on the other side, which is the smaller product
+        return orthogonalize(g.T, steps).T
+    a, b, c = NEWTON_SCHULZ
+    x = g / (np.sqrt((g * g).sum()) + 1e-7)
+    for _ in range(steps):
+        gram = x @ x.T
+        x = a * x + (b * gram + c * gram @ gram) @ x
+    return x
+
+
+def muon_update(p, g, m, lr, momentum, nesterov, weight_decay, steps=5):
+    """Momentum, orthogonalised update scaled to a root mean square of 0.2, decoupled weight decay."""
+    m = momentum * m + g
+    o = orthogonalize(g + momentum * m if nesterov else m, steps)
+    return p * (1.0 - lr * weight_decay) - lr * 0.2 * math.sqrt(max(p.shape)) * o, m
+
+
+def rotary_angles(positions, pairs, base):
+    """Angles [tokens, sum(pairs)]: pair i of the n of axis a turns by positions[:, a] * base^(-i / n)."""
+    return np.concatenate([positions[:, a:a + 1].astype(np.float64) * float(base) ** (-np.arange(n) / n)
+                           for a, n in enumerate(pairs)], axis=1)
+
+
+def rotate(x, angles, neighbours=False):
+    """x [..., tokens, heads, head_dim]: pair p is elements (p, P + p) or, as neighbours, (2p, 2p + 1); the rest does not turn."""
+    P = angles.shape[1]
+    first, second = (np.arange(P) * 2, np.arange(P) * 2 + 1) if neighbours else (np.arange(P), np.arange(P) + P)
+    c, s = np.cos(angles)[:, None, :], np.sin(angles)[:, None, :]
+    y = x.copy()
+    y[..., first] = x[..., first] * c - x[..., second] * s
+    y[..., second] = x[..., second] * c + x[..., first] * s
+    return y
+
+
+def rms_norm_fwd(x, g, eps):
+    r = 1.0 / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps)
+    return x * r * g, (x * r, r)
+
+
+def rms_norm_bwd(dy, cache, g):
+    xhat, r = cache
+    dh = dy * g
+    return r * (dh - xhat * (dh * xhat).mean(axis=-1, keepdims=True)), (dy * xhat).sum(axis=tuple(range(dy.ndim - 1)))
+
+
 # --------------------------------------------------------------------------
 # block = module M_j + auxiliary network A_j
 # --------------------------------------------------------------------------

@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libppll.so")
 PPLL_OK = 0
 ERR_NAMES = {1: "PPLL_ERR_NULL", 2: "PPLL_ERR_CONFIG", 3: "PPLL_ERR_SHAPE", 4: "PPLL_ERR_WORKSPACE",
              5: "PPLL_ERR_HIP", 6: "PPLL_ERR_LABEL", 7: "PPLL_ERR_STATE"}
+FP32, BF16 = 0, 1
 T_PARAM, T_GRAD, T_MOMENT1, T_MOMENT2, T_BN_MEAN, T_BN_VAR = range(6)
 
 
@@ -50,6 +51,48 @@ def make_config(wl: dict) -> BlockConfig:
             setattr(cfg, k, v)
     cfg.struct_size = C.sizeof(BlockConfig)
     return cfg
+
+
+class MatrixGroup(C.Structure):
+    """Mirror of ppll_matrix_group."""
+    _fields_ = [("offset", C.c_int64), ("stride", C.c_int64), ("ld", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32),
+                ("count", C.c_int32), ("reserved", C.c_int32)]
+
+
+def matrix_group(offset: int, rows: int, cols: int, ld: Optional[int] = None, count: int = 1, stride: Optional[int] = None) -> MatrixGroup:
+    """`count` matrices of rows x cols, one behind the other unless ld and stride say otherwise."""
+    ld = cols if ld is None else ld
+    return MatrixGroup(offset, rows * ld if stride is None else stride, ld, rows, cols, count, 0)
+
+
+class QueriesKeys(C.Structure):
+    """Mirror of ppll_queries_keys."""
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("q_ld", C.c_int64), ("k_ld", C.c_int64)]
+
+
+def queries_keys(q, k) -> QueriesKeys:
+    """2-d tensors [rows, heads * head_dim] whose last axis is contiguous, or None."""
+    for t in (q, k):
+        if t is not None and (t.dim() != 2 or t.stride(1) != 1 and t.shape[1] > 1):
+            raise PpllError(3, "queries and keys are 2-d tensors with a contiguous last axis")
+    ld = [0 if t is None else t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]) for t in (q, k)]
+    return QueriesKeys(_ptr(q), _ptr(k), *ld)
+
+
+class RotaryConfig(C.Structure):
+    """Mirror of ppll_rotary_config."""
+    _fields_ = [("struct_size", C.c_uint32), ("precision", C.c_int32), ("rows", C.c_int32), ("tokens", C.c_int32), ("q_heads", C.c_int32),
+                ("k_heads", C.c_int32), ("head_dim", C.c_int32), ("axes", C.c_int32), ("pairs", C.c_int32 * 3), ("neighbours", C.c_int32),
+                ("base", C.c_float), ("norm_eps", C.c_float)]
+
+
+def rotary_config(precision: int, rows: int, tokens: int, q_heads: int, k_heads: int, head_dim: int, pairs: Sequence[int], base: float,
+                  neighbours: bool = False, norm_eps: float = 1e-6) -> RotaryConfig:
+    """`pairs`: of each axis, one to three of them."""
+    if not 1 <= len(pairs) <= 3:
+        raise PpllError(2, f"{len(pairs)} axes: one to three are possible")
+    return RotaryConfig(C.sizeof(RotaryConfig), precision, rows, tokens, q_heads, k_heads, head_dim, len(pairs),
+                        (C.c_int32 * 3)(*pairs), 1 if neighbours else 0, base, norm_eps)
 
 
 _lib = None
@@ -87,6 +130,17 @@ _SIGS = {
     "ppll_block_profile_enable": (C.c_int, [C.c_void_p, C.c_int32]),
     "ppll_block_profile_read": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
     "ppll_block_profile_read_conv": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
+    "ppll_orthogonalize_workspace_bytes": (C.c_int, [C.POINTER(MatrixGroup), C.c_int32, C.POINTER(C.c_size_t)]),
+    "ppll_orthogonalize": (C.c_int, [C.POINTER(MatrixGroup), C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                     C.c_void_p]),
+    "ppll_muon_step": (C.c_int, [C.POINTER(MatrixGroup), C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+                                 C.c_float, C.c_int32, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ppll_qk_rotary_forward": (C.c_int, [C.POINTER(RotaryConfig), C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(QueriesKeys),
+                                         C.POINTER(QueriesKeys), C.POINTER(QueriesKeys), C.c_void_p]),
+    "ppll_qk_rotary_workspace_bytes": (C.c_int, [C.POINTER(RotaryConfig), C.POINTER(C.c_size_t)]),
+    "ppll_qk_rotary_backward": (C.c_int, [C.POINTER(RotaryConfig), C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(QueriesKeys),
+                                          C.POINTER(QueriesKeys), C.POINTER(QueriesKeys), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                          C.c_void_p]),
     "ppll_block_profile_read_small": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
 }
 EXPORTS = tuple(_SIGS)
@@ -299,3 +353,45 @@ def ppll_block_profile_read_small(block):
 
 def ppll_probe_copy(src, dst, nbytes: int, stream=None) -> None:
     _check(lib().ppll_probe_copy(_ptr(src), _ptr(dst), nbytes, _ptr(stream)))
+
+
+def _groups(groups: Sequence[MatrixGroup]):
+    return (MatrixGroup * max(len(groups), 1))(*groups)
+
+
+def ppll_orthogonalize_workspace_bytes(groups: Sequence[MatrixGroup]) -> int:
+    out = C.c_size_t(0)
+    _check(lib().ppll_orthogonalize_workspace_bytes(_groups(groups), len(groups), C.byref(out)))
+    return out.value
+
+
+def ppll_orthogonalize(groups: Sequence[MatrixGroup], precision: int, steps: int, x, out, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib().ppll_orthogonalize(_groups(groups), len(groups), precision, steps, _ptr(x), _ptr(out), _ptr(workspace), workspace_bytes,
+                                    _ptr(stream)))
+
+
+def ppll_muon_step(groups: Sequence[MatrixGroup], steps: int, grads, momentum_buffer, params, shadow, lr: float, momentum: float, nesterov: bool,
+                   weight_decay: float, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(lib().ppll_muon_step(_groups(groups), len(groups), steps, _ptr(grads), _ptr(momentum_buffer), _ptr(params), _ptr(shadow), lr, momentum,
+                                1 if nesterov else 0, weight_decay, _ptr(workspace), workspace_bytes, _ptr(stream)))
+
+
+def _ref(s):
+    return None if s is None else C.byref(s)
+
+
+def ppll_qk_rotary_forward(cfg: RotaryConfig, positions, q_scale, k_scale, x: QueriesKeys, y: QueriesKeys, keep: Optional[QueriesKeys] = None,
+                           stream=None) -> None:
+    _check(lib().ppll_qk_rotary_forward(_ref(cfg), _ptr(positions), _ptr(q_scale), _ptr(k_scale), _ref(x), _ref(y), _ref(keep), _ptr(stream)))
+
+
+def ppll_qk_rotary_workspace_bytes(cfg: RotaryConfig) -> int:
+    out = C.c_size_t(0)
+    _check(lib().ppll_qk_rotary_workspace_bytes(_ref(cfg), C.byref(out)))
+    return out.value
+
+
+def ppll_qk_rotary_backward(cfg: RotaryConfig, positions, q_scale, k_scale, x: Optional[QueriesKeys], dy: QueriesKeys, dx: QueriesKeys,
+                            d_q_scale=None, d_k_scale=None, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().ppll_qk_rotary_backward(_ref(cfg), _ptr(positions), _ptr(q_scale), _ptr(k_scale), _ref(x), _ref(dy), _ref(dx), _ptr(d_q_scale),
+                                         _ptr(d_k_scale), _ptr(workspace), workspace_bytes, _ptr(stream)))

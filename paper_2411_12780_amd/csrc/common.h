@@ -357,6 +357,21 @@ int launch_refresh_shadow(hipStream_t s, const float* p, uint16_t* shadow, size_
 int launch_fill_zero(hipStream_t s, void* p, size_t bytes);
 int launch_copy_probe(hipStream_t s, const void* src, void* dst, size_t bytes);
 
+// Orthogonalised updates (k_ortho.hip): ws is the workspace that the plan lays out
+struct OrthoPlan;
+int launch_orthogonalize(hipStream_t s, const OrthoPlan& p, int dt, int steps, const void* in, void* out, char* ws);
+int launch_muon(hipStream_t s, const OrthoPlan& p, int steps, const float* g, float* m, float* w, uint16_t* shadow, float lr, float momentum,
+                int nesterov, float weight_decay, char* ws);
+
+// ---------------------------------------------------------------- queries and keys (k_rotary.hip)
+struct RotaryPlan;
+struct RotarySide;
+int launch_rotary_fwd(hipStream_t s, const RotaryPlan& p, int dt, const int32_t* positions, const RotarySide& q, const RotarySide& k);
+// partials (null without scales): rotary_partial_floats() floats; *rows receives the rows of [2][head_dim] sums left there
+int launch_rotary_bwd(hipStream_t s, const RotaryPlan& p, int dt, const int32_t* positions, const RotarySide& q, const RotarySide& k, float* partials,
+                      int* rows);
+int launch_rotary_scales(hipStream_t s, const float* partials, int rows, int hd, float* dq, float* dk);   // their sums; dq, dk nullable
+
 // ---------------------------------------------------------------- ResNet pieces
 // stat / stat_blocks (nullable): room for the sums a BatchNorm over y needs (bn_partial_floats of y's shape); on
 // return *stat_blocks is the number of partial rows the convolution wrote there itself (0: none, the BatchNorm

@@ -1,0 +1,41 @@
+// Orthogonalised updates: what a call's matrices are, where their intermediates lie in the workspace.  Host arithmetic only.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/ppll.h"
+
+namespace ppll {
+
+constexpr int ORTHO_GROUPS = 16;       // groups of a call
+constexpr int ORTHO_SIDE = 8192;       // rows and columns of a matrix, at most
+constexpr int ORTHO_STEPS = 16;        // Newton-Schulz steps, at most
+constexpr int NORM_ROWS = 32, NORM_COLS = 256;   // piece of a matrix whose squares one workgroup adds up
+
+// A group as the kernels see it.  A matrix is worked on as X [m][n] with m <= n (transposed where rows > cols), padded with zeros to
+// mp x np: zero rows and columns stay zero through every product, so no product has a border.  Each intermediate is two planes of fp16,
+// one behind the other; offsets in bytes from the start of the workspace, those of matrix i of the group i times its size further.
+struct OrthoGroup {
+  int64_t offset, stride, ld;          // elements, in the caller's blobs
+  int32_t rows, cols, count;
+  int32_t m, n, mp, np, tall;
+  int32_t first;                       // place of the group's first matrix among all of the call
+  int32_t first_piece;                 // of its pieces among those of all groups
+  int64_t x, xt[2], a, b;
+  __host__ __device__ int64_t plane_x() const { return (int64_t)mp * np; }      // elements
+  __host__ __device__ int64_t plane_a() const { return (int64_t)mp * mp; }
+  __host__ __device__ int pieces() const { return ((rows + NORM_ROWS - 1) / NORM_ROWS) * ((cols + NORM_COLS - 1) / NORM_COLS); }
+};
+struct OrthoPlan {
+  OrthoGroup g[ORTHO_GROUPS];
+  int32_t n;                           // groups with a matrix in them
+  int32_t tile;                        // 64 or 128
+  int64_t partials;                    // byte offset of the partial sums of squares, one double a piece
+  int64_t shrink;                      // and of a float for each matrix (see k_ortho.hip)
+  int64_t bytes;
+};
+
+// Checks the groups and lays the workspace out.  PPLL_OK, or an error with its text set.
+int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* plan);
+
+}  // namespace ppll
