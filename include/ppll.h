@@ -55,7 +55,7 @@ enum {
 enum { PPLL_VIT = 0, PPLL_RESNET = 1 };
 enum { PPLL_FP32 = 0, PPLL_BF16 = 1 };
 enum { PPLL_IN_IMAGE = 0, PPLL_IN_ACTIVATION = 1 };
-enum { PPLL_SGD = 0, PPLL_ADAMW = 1 };
+enum { PPLL_SGD = 0, PPLL_ADAMW = 1, PPLL_MUON = 2 };
 /* tensor kinds for ppll_block_read_tensor / write_tensor */
 enum { PPLL_T_PARAM = 0, PPLL_T_GRAD = 1, PPLL_T_MOMENT1 = 2, PPLL_T_MOMENT2 = 3,
        PPLL_T_BN_MEAN = 4, PPLL_T_BN_VAR = 5 };
@@ -74,7 +74,7 @@ enum { PPLL_T_PARAM = 0, PPLL_T_GRAD = 1, PPLL_T_MOMENT1 = 2, PPLL_T_MOMENT2 = 3
  * zero channels, the blocks before it work on [2*height, 2*width, channels/2]
  * and that is also the shape of x_in (of the stem's output with a stem). */
 typedef struct {
-  uint32_t struct_size;   /* = sizeof(ppll_block_config)                         */
+  uint32_t struct_size;   /* = sizeof(ppll_block_config), or of its part that ends with `seed`: the fields behind are then 0 */
   int32_t arch;           /* PPLL_VIT | PPLL_RESNET                              */
   int32_t precision;      /* PPLL_FP32 | PPLL_BF16 (fp32 master weights always)  */
   int32_t input_kind;     /* PPLL_IN_IMAGE (ViT patches, ResNet stem) | PPLL_IN_ACTIVATION */
@@ -83,13 +83,23 @@ typedef struct {
   int32_t tokens, dim, heads, mlp_dim, depth, aux_depth; /* ViT                  */
   int32_t channels, height, width, n_basic_blocks, aux_channels; /* ResNet       */
   int32_t transition_block; /* ResNet: 0 = none, i+1 = basic block i downsamples */
-  int32_t optimizer;      /* PPLL_SGD | PPLL_ADAMW                               */
-  float momentum;         /* SGD                                                 */
-  int32_t nesterov;       /* SGD                                                 */
-  float weight_decay;     /* SGD: coupled L2; AdamW: decoupled                   */
+  /* PPLL_MUON: ppll_muon_step (5 Newton-Schulz steps) for the weight matrices of the encoder layers (query, key and value parts each
+   * for itself) and the 3x3 filters behind the stem as [9 Cin, Cout] matrices; AdamW for the rest (embeddings, vectors, stem, head) */
+  int32_t optimizer;      /* PPLL_SGD | PPLL_ADAMW | PPLL_MUON                   */
+  float momentum;         /* SGD, Muon                                           */
+  int32_t nesterov;       /* SGD, Muon                                           */
+  float weight_decay;     /* SGD: coupled L2; AdamW, Muon: decoupled             */
   float beta1, beta2, adam_eps;
   float ln_eps, bn_eps, bn_momentum;
   uint64_t seed;          /* used only when no initial parameters are supplied   */
+  /* ViT, all layers (0: none).  rotary: queries and keys turn by the patch's place, token 1 + y * grid_w + x by y on the first half of the
+   * pairs and by x on the others (ppll_qk_rotary_forward with pairs {P - P / 2, P / 2}, P = dim / heads / 2); the class token does not
+   * turn.  qk_norm: RMS norm of each head of queries and keys before that, with learned scales [dim / heads] for each layer (tensors
+   * qn.g and kn.g behind qkv.b). */
+  int32_t rotary, grid_h, grid_w;   /* rotary = 1: tokens = grid_h * grid_w + 1; with PPLL_IN_IMAGE the grid of patches */
+  float rotary_base;                /* > 0                                       */
+  int32_t qk_norm;
+  float qk_norm_eps;                /* > 0                                       */
 } ppll_block_config;
 
 typedef struct ppll_block ppll_block_t;
@@ -298,7 +308,7 @@ typedef struct {
 } ppll_queries_keys;
 
 /* The rotation: `axes` axes of positions (1..3: a sequence; height, width; time, height, width), pairs[a] pairs of each head turn with axis a,
- * sum(pairs) <= head_dim / 2 = all pairs.  Pair p of P = sum(pairs) is elements (p, P + p) of the head, or with `neighbours` (2p, 2p + 1);
+ * sum(pairs) <= head_dim / 2 (0: the norm alone).  Pair p of P = sum(pairs) is elements (p, P + p) of the head, or with `neighbours` (2p, 2p + 1);
  * elements from 2 P on do not turn.  Pair i of the n that belong to axis a turns by positions[token][a] * base^(-i / n) radians (the angle
  * is reduced in 64 bits, so far positions lose nothing).  Row r holds token r % tokens: a batch of sequences with the same positions, or
  * with tokens = rows one row of positions each. */

@@ -48,6 +48,7 @@ IN_IMAGE = 0
 IN_ACTIVATION = 1
 OPT_SGD = 0
 OPT_ADAMW = 1
+OPT_MUON = 2
 
 
 @dataclass
@@ -90,16 +91,24 @@ class BlockConfig:
     ln_eps: float = 1e-6
     bn_eps: float = 1e-5
     bn_momentum: float = 0.1
+    # ViT: rotary positions of the patches (grid_h x grid_w) and RMS norm of each head of queries and keys, in every layer
+    rotary: int = 0
+    grid_h: int = 0
+    grid_w: int = 0
+    rotary_base: float = 100.0
+    qk_norm: int = 0
+    qk_norm_eps: float = 1e-6
 
 
 # --------------------------------------------------------------------------
 # parameter tables
 # --------------------------------------------------------------------------
 
-def _encoder_layer_spec(prefix: str, D: int, F: int) -> List[Tuple[str, Tuple[int, ...]]]:
+def _encoder_layer_spec(prefix: str, D: int, F: int, qk_norm: int = 0) -> List[Tuple[str, Tuple[int, ...]]]:
     return [
         (f"{prefix}.ln1.g", (D,)), (f"{prefix}.ln1.b", (D,)),
         (f"{prefix}.qkv.w", (D, 3 * D)), (f"{prefix}.qkv.b", (3 * D,)),
+        *([(f"{prefix}.qn.g", (qk_norm,)), (f"{prefix}.kn.g", (qk_norm,))] if qk_norm else []),
         (f"{prefix}.proj.w", (D, D)), (f"{prefix}.proj.b", (D,)),
         (f"{prefix}.ln2.g", (D,)), (f"{prefix}.ln2.b", (D,)),
         (f"{prefix}.fc1.w", (D, F)), (f"{prefix}.fc1.b", (F,)),
@@ -136,10 +145,11 @@ def param_spec(cfg: BlockConfig) -> List[Tuple[str, Tuple[int, ...]]]:
         if cfg.input_kind == IN_IMAGE:
             spec += [("pe.w", (cfg.patch * cfg.patch * cfg.img_c, D)), ("pe.b", (D,)),
                      ("cls", (D,)), ("pos", (cfg.tokens, D))]
+        head = D // cfg.heads if cfg.qk_norm else 0
         for l in range(cfg.depth):
-            spec += _encoder_layer_spec(f"blk{l}", D, F)
+            spec += _encoder_layer_spec(f"blk{l}", D, F, head)
         for a in range(cfg.aux_depth):
-            spec += _encoder_layer_spec(f"aux{a}", D, F)
+            spec += _encoder_layer_spec(f"aux{a}", D, F, head)
         spec += [("head.ln.g", (D,)), ("head.ln.b", (D,)),
                  ("head.w", (D, cfg.num_classes)), ("head.b", (cfg.num_classes,))]
     elif cfg.arch == ARCH_RESNET:
@@ -508,28 +518,65 @@ def block_init(cfg: BlockConfig, flat_params: np.ndarray, dtype=np.float64,
     return st
 
 
+def _qk_angles(cfg):
+    """Angles [tokens, pairs] of the class token (none) and the patches, rows first."""
+    y, x = np.meshgrid(np.arange(cfg.grid_h), np.arange(cfg.grid_w), indexing="ij")
+    pos = np.concatenate([[[0, 0]], np.stack([y.reshape(-1), x.reshape(-1)], axis=1)])
+    pairs = cfg.dim // cfg.heads // 2
+    return rotary_angles(pos, [pairs - pairs // 2, pairs // 2], cfg.rotary_base)
+
+
+def _qk_fwd(qkv, p, pre, cfg):
+    """Norm and rotation of the query and key parts of qkv [B, T, 3D]."""
+    B, T, D3 = qkv.shape
+    D, cache, out = D3 // 3, [], qkv.copy()
+    for i, name in enumerate((".qn.g", ".kn.g")):
+        v = qkv[:, :, i * D:(i + 1) * D].reshape(B, T, cfg.heads, D // cfg.heads)
+        if cfg.qk_norm:
+            v, c = rms_norm_fwd(v, p[pre + name], cfg.qk_norm_eps)
+            cache.append(c)
+        if cfg.rotary:
+            v = rotate(v, _qk_angles(cfg))
+        out[:, :, i * D:(i + 1) * D] = v.reshape(B, T, D)
+    return out, cache
+
+
+def _qk_bwd(dqkv, cache, p, pre, grads, cfg):
+    B, T, D3 = dqkv.shape
+    D, out = D3 // 3, dqkv.copy()
+    for i, name in enumerate((".qn.g", ".kn.g")):
+        d = dqkv[:, :, i * D:(i + 1) * D].reshape(B, T, cfg.heads, D // cfg.heads)
+        if cfg.rotary:
+            d = rotate(d, -_qk_angles(cfg))
+        if cfg.qk_norm:
+            d, grads[pre + name] = rms_norm_bwd(d, cache[i], p[pre + name])
+        out[:, :, i * D:(i + 1) * D] = d.reshape(B, T, D)
+    return out
+
+
 def _encoder_fwd(x, p, pre, st):
     cfg = st.cfg
     u, c_ln1 = layernorm_fwd(x, p[pre + ".ln1.g"], p[pre + ".ln1.b"], cfg.ln_eps)
     qkv = linear_fwd(u, p[pre + ".qkv.w"], p[pre + ".qkv.b"])
+    qkv, c_qk = _qk_fwd(qkv, p, pre, cfg)
     o, c_att = attention_fwd(qkv, cfg.heads)
     x1 = x + linear_fwd(o, p[pre + ".proj.w"], p[pre + ".proj.b"])
     u2, c_ln2 = layernorm_fwd(x1, p[pre + ".ln2.g"], p[pre + ".ln2.b"], cfg.ln_eps)
     h = linear_fwd(u2, p[pre + ".fc1.w"], p[pre + ".fc1.b"])
     gl = gelu_fwd(h)
     x2 = x1 + linear_fwd(gl, p[pre + ".fc2.w"], p[pre + ".fc2.b"])
-    return x2, (c_ln1, u, c_att, o, c_ln2, u2, h, gl)
+    return x2, (c_ln1, u, c_qk, c_att, o, c_ln2, u2, h, gl)
 
 
 def _encoder_bwd(dx2, cache, p, pre, grads, st):
-    c_ln1, u, c_att, o, c_ln2, u2, h, gl = cache
+    c_ln1, u, c_qk, c_att, o, c_ln2, u2, h, gl = cache
     dgl, grads[pre + ".fc2.w"], grads[pre + ".fc2.b"] = linear_bwd(dx2, gl, p[pre + ".fc2.w"])
     dh = gelu_bwd(dgl, h)
     du2, grads[pre + ".fc1.w"], grads[pre + ".fc1.b"] = linear_bwd(dh, u2, p[pre + ".fc1.w"])
     d, grads[pre + ".ln2.g"], grads[pre + ".ln2.b"] = layernorm_bwd(du2, c_ln2, p[pre + ".ln2.g"])
     dx1 = dx2 + d
     do, grads[pre + ".proj.w"], grads[pre + ".proj.b"] = linear_bwd(dx1, o, p[pre + ".proj.w"])
-    dqkv = attention_bwd(do, c_att)
+    dqkv = _qk_bwd(attention_bwd(do, c_att), c_qk, p, pre, grads, st.cfg)
     du, grads[pre + ".qkv.w"], grads[pre + ".qkv.b"] = linear_bwd(dqkv, u, p[pre + ".qkv.w"])
     d, grads[pre + ".ln1.g"], grads[pre + ".ln1.b"] = layernorm_bwd(du, c_ln1, p[pre + ".ln1.g"])
     return dx1 + d
@@ -712,11 +759,23 @@ def local_loss(st: BlockState, x_in, labels) -> float:
     return float(cross_entropy(logits, np.asarray(labels))[0])
 
 
+def is_hidden_matrix(name):
+    """Weights that Muon updates: of the encoder layers, and the filters behind the stem."""
+    return name.endswith((".qkv.w", ".proj.w", ".fc1.w", ".fc2.w", ".conv1.w", ".conv2.w")) or name == "aux.conv.w"
+
+
 def apply_update(st: BlockState, grads: Dict[str, np.ndarray], lr: float) -> None:
     cfg = st.cfg
     st.steps += 1
     for name in st.params:
-        if cfg.optimizer == OPT_SGD:
+        if cfg.optimizer == OPT_MUON and is_hidden_matrix(name):
+            p = st.params[name]
+            parts = 3 if name.endswith(".qkv.w") else 1     # queries, keys and values are matrices of their own
+            split = lambda t: np.split(t.reshape(-1, t.shape[-1]), parts, axis=1)
+            new = [muon_update(*t, lr, cfg.momentum, bool(cfg.nesterov), cfg.weight_decay)
+                   for t in zip(split(p), split(grads[name]), split(st.mom1[name]))]
+            st.params[name], st.mom1[name] = (np.concatenate(t, axis=1).reshape(p.shape) for t in zip(*new))
+        elif cfg.optimizer == OPT_SGD:
             st.params[name], st.mom1[name] = sgd_update(
                 st.params[name], grads[name], st.mom1[name], lr, cfg.momentum,
                 bool(cfg.nesterov), cfg.weight_decay, st.steps == 1)

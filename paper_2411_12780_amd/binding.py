@@ -38,13 +38,15 @@ class BlockConfig(C.Structure):
                 ("optimizer", C.c_int32), ("momentum", C.c_float), ("nesterov", C.c_int32),
                 ("weight_decay", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float),
                 ("adam_eps", C.c_float), ("ln_eps", C.c_float), ("bn_eps", C.c_float),
-                ("bn_momentum", C.c_float), ("seed", C.c_uint64)]
+                ("bn_momentum", C.c_float), ("seed", C.c_uint64),
+                ("rotary", C.c_int32), ("grid_h", C.c_int32), ("grid_w", C.c_int32), ("rotary_base", C.c_float),
+                ("qk_norm", C.c_int32), ("qk_norm_eps", C.c_float)]
 
 
 def make_config(wl: dict) -> BlockConfig:
     """Workload dict (see synth.WORKLOADS) -> ppll_block_config; unknown keys are ignored."""
     cfg = BlockConfig()
-    defaults = dict(beta1=0.9, beta2=0.999, adam_eps=1e-8, ln_eps=1e-6, bn_eps=1e-5, bn_momentum=0.1)
+    defaults = dict(beta1=0.9, beta2=0.999, adam_eps=1e-8, ln_eps=1e-6, bn_eps=1e-5, bn_momentum=0.1, rotary_base=100.0, qk_norm_eps=1e-6)
     names = {f[0] for f in BlockConfig._fields_}
     for k, v in {**defaults, **wl}.items():
         if k in names:

@@ -2,6 +2,7 @@
 // the block engine / the K-stream pipeline.
 #include <cmath>
 #include <cstdarg>
+#include <cstddef>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
@@ -72,7 +73,8 @@ void seeded_params(const Block& b, std::vector<float>& out) {
   Rng rng{b.cfg.seed * 0x2545F4914F6CDD1Dull + 1};
   out.assign(b.P, 0.f);
   for (const TensorDesc& t : b.tensors) {
-    bool norm = t.name.find(".ln") != std::string::npos || t.name.find(".bn") != std::string::npos;
+    bool norm = false;
+    for (const char* part : {".ln", ".bn", ".qn", ".kn"}) norm |= t.name.find(part) != std::string::npos;
     bool conv = t.name.find("conv") != std::string::npos;
     double sd = 0.0, mean = 0.0;
     if (conv) sd = std::sqrt(2.0 / (double)t.rows);          // rows = 9 * Cin
@@ -139,6 +141,23 @@ int scratch_lookup(void** ptr_out, int* dev_out) {
   return PPLL_OK;
 }
 
+// A caller's configuration in full: one built before a field existed says so by its struct_size, and the field is 0.
+constexpr size_t CONFIG_TO_SEED = offsetof(ppll_block_config, rotary);
+int read_config(const ppll_block_config* c, ppll_block_config* full) {
+  if (!c) { set_error("config is null"); return PPLL_ERR_NULL; }
+  memset(full, 0, sizeof *full);
+  if (c->struct_size == CONFIG_TO_SEED) {
+    memcpy(full, c, CONFIG_TO_SEED);
+    full->struct_size = sizeof *full;
+  } else if (c->struct_size == sizeof *full) {
+    *full = *c;
+  } else {
+    set_error("config struct_size %u, library expects %zu", c->struct_size, sizeof *full);
+    return PPLL_ERR_CONFIG;
+  }
+  return validate_config(full);
+}
+
 int block_alive(ppll_block* h) {
   if (!h) { set_error("block handle is null"); return PPLL_ERR_NULL; }
   if (!h->b.alive) { set_error("block handle was destroyed"); return PPLL_ERR_STATE; }
@@ -157,45 +176,50 @@ int ppll_probe_copy(const void* src_dev, void* dst_dev, size_t bytes, void* hip_
 }
 
 int ppll_block_workspace_bytes(const ppll_block_config* cfg, size_t* bytes) {
-  PPLL_TRY(validate_config(cfg));
+  ppll_block_config full;
+  PPLL_TRY(read_config(cfg, &full));
   if (!bytes) { set_error("bytes is null"); return PPLL_ERR_NULL; }
   Block b;
-  b.cfg = *cfg;
+  b.cfg = full;
   *bytes = b.plan(nullptr);
   return PPLL_OK;
 }
 
 int ppll_block_param_bytes(const ppll_block_config* cfg, size_t* bytes) {
-  PPLL_TRY(validate_config(cfg));
+  ppll_block_config full;
+  PPLL_TRY(read_config(cfg, &full));
   if (!bytes) { set_error("bytes is null"); return PPLL_ERR_NULL; }
   Block b;
-  b.cfg = *cfg;
+  b.cfg = full;
   b.plan(nullptr);
   *bytes = b.P * sizeof(float);
   return PPLL_OK;
 }
 
 int ppll_block_in_bytes(const ppll_block_config* cfg, size_t* bytes) {
-  PPLL_TRY(validate_config(cfg));
+  ppll_block_config full;
+  PPLL_TRY(read_config(cfg, &full));
   if (!bytes) { set_error("bytes is null"); return PPLL_ERR_NULL; }
   Block b;
-  b.cfg = *cfg;
-  *bytes = (size_t)b.in_elems() * dtype_size(cfg->precision == PPLL_BF16 ? BF16 : F32);
+  b.cfg = full;
+  *bytes = (size_t)b.in_elems() * dtype_size(full.precision == PPLL_BF16 ? BF16 : F32);
   return PPLL_OK;
 }
 
 int ppll_block_out_bytes(const ppll_block_config* cfg, size_t* bytes) {
-  PPLL_TRY(validate_config(cfg));
+  ppll_block_config full;
+  PPLL_TRY(read_config(cfg, &full));
   if (!bytes) { set_error("bytes is null"); return PPLL_ERR_NULL; }
   Block b;
-  b.cfg = *cfg;
-  *bytes = (size_t)b.out_elems() * dtype_size(cfg->precision == PPLL_BF16 ? BF16 : F32);
+  b.cfg = full;
+  *bytes = (size_t)b.out_elems() * dtype_size(full.precision == PPLL_BF16 ? BF16 : F32);
   return PPLL_OK;
 }
 
 int ppll_block_init(const ppll_block_config* cfg, void* workspace_dev, size_t workspace_bytes,
                     const float* init_params_host, void* hip_stream, ppll_block_t** out) {
-  PPLL_TRY(validate_config(cfg));
+  ppll_block_config full;
+  PPLL_TRY(read_config(cfg, &full));
   if (!out) { set_error("out is null"); return PPLL_ERR_NULL; }
   PPLL_TRY(check_aligned(workspace_dev, "workspace_dev"));
   int device = -1;
@@ -203,7 +227,7 @@ int ppll_block_init(const ppll_block_config* cfg, void* workspace_dev, size_t wo
   ppll_block* h = new (std::nothrow) ppll_block();
   if (!h) { set_error("out of host memory"); return PPLL_ERR_STATE; }
   Block& b = h->b;
-  b.cfg = *cfg;
+  b.cfg = full;
   b.device = device;
   size_t need = b.plan((char*)workspace_dev);
   if (workspace_bytes < need) {
@@ -232,6 +256,11 @@ int ppll_block_init(const ppll_block_config* cfg, void* workspace_dev, size_t wo
   if (st == PPLL_OK) st = launch_fill_zero(s, b.loss_dev, sizeof(float));
   if (st == PPLL_OK) st = launch_fill_zero(s, b.flag_dev, sizeof(int));
   if (st != PPLL_OK) return fail(st);
+  std::vector<int32_t> positions;
+  if (b.rope_pos) {
+    b.rope_positions(positions);
+    if (!hip_ok(hipMemcpyAsync(b.rope_pos, positions.data(), positions.size() * sizeof(int32_t), hipMemcpyHostToDevice, s), "position upload")) return fail(PPLL_ERR_HIP);
+  }
   size_t bn_total = 0;
   for (int c : b.bn_channels) bn_total += c;
   if (bn_total) {
@@ -413,11 +442,17 @@ int ppll_block_destroy(ppll_block_t* h) {
 }
 
 // ------------------------------------------------------------------ pipeline
-static int pipeline_check(const ppll_block_config* cfgs, int32_t K, int32_t depth) {
-  if (!cfgs) { set_error("cfgs is null"); return PPLL_ERR_NULL; }
-  if (K < 1 || K > 64) { set_error("K = %d outside 1..64", K); return PPLL_ERR_CONFIG; }
+constexpr int MAX_BLOCKS = 64;
+// cfgs receives the K configurations in full; a caller's lie struct_size apart
+static int pipeline_check(const ppll_block_config* given, int32_t K, int32_t depth, ppll_block_config* cfgs) {
+  if (!given) { set_error("cfgs is null"); return PPLL_ERR_NULL; }
+  if (K < 1 || K > MAX_BLOCKS) { set_error("K = %d outside 1..%d", K, MAX_BLOCKS); return PPLL_ERR_CONFIG; }
   if (depth < 1 || depth > 16) { set_error("queue_depth = %d outside 1..16", depth); return PPLL_ERR_CONFIG; }
-  for (int j = 0; j < K; ++j) PPLL_TRY(validate_config(&cfgs[j]));
+  for (int j = 0; j < K; ++j) {
+    const ppll_block_config* c = (const ppll_block_config*)((const char*)given + (size_t)j * given->struct_size);
+    if (j > 0 && c->struct_size != given->struct_size) { set_error("configurations of one pipeline need one struct_size"); return PPLL_ERR_CONFIG; }
+    PPLL_TRY(read_config(c, &cfgs[j]));
+  }
   for (int j = 1; j < K; ++j) {
     size_t a, b;
     ppll_block_out_bytes(&cfgs[j - 1], &a);
@@ -433,8 +468,9 @@ static int pipeline_check(const ppll_block_config* cfgs, int32_t K, int32_t dept
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-int ppll_pipeline_workspace_bytes(const ppll_block_config* cfgs, int32_t K, int32_t depth, size_t* bytes) {
-  PPLL_TRY(pipeline_check(cfgs, K, depth));
+int ppll_pipeline_workspace_bytes(const ppll_block_config* given, int32_t K, int32_t depth, size_t* bytes) {
+  ppll_block_config cfgs[MAX_BLOCKS];
+  PPLL_TRY(pipeline_check(given, K, depth, cfgs));
   if (!bytes) { set_error("bytes is null"); return PPLL_ERR_NULL; }
   size_t total = 0, in_b, out_b, ws;
   const size_t lab = align256((size_t)cfgs[0].batch * sizeof(int32_t));
@@ -451,11 +487,13 @@ int ppll_pipeline_workspace_bytes(const ppll_block_config* cfgs, int32_t K, int3
   return PPLL_OK;
 }
 
-int ppll_pipeline_init(const ppll_block_config* cfgs, int32_t K, int32_t depth, void* workspace_dev,
+int ppll_pipeline_init(const ppll_block_config* given, int32_t K, int32_t depth, void* workspace_dev,
                        size_t workspace_bytes, void* const* hip_streams, const float* const* init_params_host,
                        ppll_pipeline_t** out) {
   size_t need;
-  PPLL_TRY(ppll_pipeline_workspace_bytes(cfgs, K, depth, &need));
+  ppll_block_config cfgs[MAX_BLOCKS];
+  PPLL_TRY(ppll_pipeline_workspace_bytes(given, K, depth, &need));
+  PPLL_TRY(pipeline_check(given, K, depth, cfgs));
   if (!out) { set_error("out is null"); return PPLL_ERR_NULL; }
   if (!hip_streams) { set_error("hip_streams is null"); return PPLL_ERR_NULL; }
   PPLL_TRY(check_aligned(workspace_dev, "workspace_dev"));

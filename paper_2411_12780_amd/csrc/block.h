@@ -7,6 +7,8 @@
 #include <vector>
 
 #include "common.h"
+#include "ortho.h"
+#include "rotary.h"
 
 namespace ppll {
 
@@ -18,15 +20,17 @@ struct TensorDesc {
 };
 
 struct EncoderParams {   // element offsets into the blob
-  size_t ln1_g, ln1_b, qkv_w, qkv_b, proj_w, proj_b, ln2_g, ln2_b, fc1_w, fc1_b, fc2_w, fc2_b;
+  size_t ln1_g, ln1_b, qkv_w, qkv_b, qn_g, kn_g, proj_w, proj_b, ln2_g, ln2_b, fc1_w, fc1_b, fc2_w, fc2_b;
 };
 struct EncoderActs {     // saved by the forward for the backward (h: gelu' at the MLP pre-activation, gl: its gelu)
   void *u1, *qkv, *att, *x1, *u2, *h, *gl, *x2;
+  void* qk = nullptr;      // queries and keys as projected [M, 2D], where they are normalised; null: nothing is kept
   float *mean1, *rstd1, *mean2, *rstd2, *lse;
 };
 // Compact buffers of the last auxiliary encoder layer, of which only the class-token row is computed behind the
 // key / value projection ([B, .] instead of [B*T, .]; see Block::encoder_fwd_cls).
 struct ClsActs {
+  void* q_raw = nullptr;                           // q as projected, where it is normalised
   void *q, *att, *x1, *u2, *h, *gl, *x2;          // forward (h: gelu' at the MLP pre-activation, gl: its gelu)
   void *d_h, *d_u2, *d_x1, *d_att, *d_q;          // backward
   float *mean2, *rstd2, *prob;                     // prob [B, H, T]
@@ -89,6 +93,16 @@ struct Block {
   size_t wgrad_ws_floats = 0;
 
   // ViT
+  // Rotary positions and norm of queries and keys, between the projection and attention of every layer
+  bool qk_prepared() const { return cfg.rotary || cfg.qk_norm; }
+  RotaryPlan rope{};                  // of one row a token: rows, tokens and heads are the call's
+  int32_t* rope_pos = nullptr;        // [T][2], rows and columns of the patches; the class token at 0
+  void rope_positions(std::vector<int32_t>& out) const;
+  // What Muon updates (groups of equal matrices), and the ranges of the blob that are left to AdamW
+  std::vector<ppll_matrix_group> muon_groups() const;
+  OrthoPlan ortho{};
+  char* ortho_ws = nullptr;
+  std::vector<BlobRange> adam_ranges;
   size_t pe_w = 0, pe_b = 0, cls = 0, pos = 0, head_ln_g = 0, head_ln_b = 0, head_w = 0, head_b = 0;
   std::vector<EncoderParams> enc_p;       // depth + aux_depth
   std::vector<EncoderActs> enc_a;
@@ -212,6 +226,11 @@ struct Block {
   int forward_eval_with(const EvalBuffers& e, const void* x_in, void* x_out, float* logits_out, hipStream_t s);
   size_t plan_eval_scratch(char* base, EvalBuffers* e) const;
   int encoder_bwd(int l, const void* x, const void* g_in, void* g_tmp, void* g_out, bool need_dx, hipStream_t s);
+  // queries and keys in place: q [q_rows, D] rows q_ld apart, k likewise (null: none), q_tokens / k_tokens of them a sequence
+  int qk_fwd(int l, void* q, long q_ld, int q_rows, int q_tokens, void* q_keep, long q_keep_ld, void* k, long k_ld, void* k_keep, long k_keep_ld,
+             hipStream_t s);
+  int qk_bwd(int l, void* dq, long q_ld, int q_rows, int q_tokens, const void* q_raw, long q_raw_ld, void* dk, long k_ld, const void* k_raw,
+             long k_raw_ld, hipStream_t s);
   int encoder_fwd_cls(int l, const EncoderActs& a, const ClsActs& c, const void* x, hipStream_t s);
   int encoder_bwd_cls(int l, const void* x, const void* d_x2, void* g_out, hipStream_t s);
   // dW[in, out] (row stride ldw) = X^T dY over K rows and db = column sums of dY; recorded for the grouped launch when

@@ -15,6 +15,7 @@ constexpr long SIDE_MIN_TILES = 256;
 // ... and only when their reduction runs over this many rows: short products end before the fork and join pay off
 // (640 rows at width 768: 4 % slower with the side stream)
 constexpr int SIDE_MIN_ROWS = 4096;
+constexpr int MUON_STEPS = 5;      // Newton-Schulz steps of an update
 
 
 namespace {
@@ -48,7 +49,7 @@ int validate_config(const ppll_block_config* c) {
   }
   auto bad = [](const char* what) { set_error("config: %s", what); return PPLL_ERR_CONFIG; };
   if (c->precision != PPLL_FP32 && c->precision != PPLL_BF16) return bad("precision must be PPLL_FP32 or PPLL_BF16");
-  if (c->optimizer != PPLL_SGD && c->optimizer != PPLL_ADAMW) return bad("optimizer must be PPLL_SGD or PPLL_ADAMW");
+  if (c->optimizer != PPLL_SGD && c->optimizer != PPLL_ADAMW && c->optimizer != PPLL_MUON) return bad("optimizer must be PPLL_SGD, PPLL_ADAMW or PPLL_MUON");
   if (c->batch < 1 || c->batch > 65536) return bad("batch outside 1..65536");
   if (c->num_classes < 2 || c->num_classes > 1024) return bad("num_classes outside 2..1024");
   if (c->arch == PPLL_VIT) {
@@ -64,6 +65,20 @@ int validate_config(const ppll_block_config* c) {
       if ((c->img_h / c->patch) * (c->img_w / c->patch) + 1 != c->tokens)
         return bad("tokens must equal (img_h/patch)*(img_w/patch) + 1");
     }
+    if ((c->rotary | c->qk_norm) & ~1) return bad("rotary and qk_norm must be 0 or 1");
+    if (c->rotary || c->qk_norm) {
+      const int dh = c->dim / c->heads;
+      if (dh % 2 || dh > 2 * ROTARY_PAIRS) return bad("rotary positions and qk_norm need an even head width of 256 at most");
+      if (c->rotary) {
+        if (c->grid_h < 1 || c->grid_w < 1 || c->grid_h > 256 || c->grid_w > 256 || c->grid_h * c->grid_w + 1 != c->tokens)
+          return bad("rotary positions: tokens must equal grid_h * grid_w + 1");
+        if (c->input_kind == PPLL_IN_IMAGE && (c->grid_h != c->img_h / c->patch || c->grid_w != c->img_w / c->patch))
+          return bad("rotary positions: grid_h, grid_w must be the grid of patches");
+        if (!(c->rotary_base > 0.f) || !std::isfinite(c->rotary_base)) return bad("rotary_base must be positive and finite");
+      }
+      if (c->qk_norm && (!(c->qk_norm_eps > 0.f) || !std::isfinite(c->qk_norm_eps))) return bad("qk_norm_eps must be positive and finite");
+    }
+    if (c->optimizer == PPLL_MUON && c->mlp_dim > ORTHO_SIDE) return bad("mlp_dim above 8192 with the Muon optimizer");
     // every limit a kernel of the step would otherwise hit at launch time, when earlier kernels are already enqueued
     const size_t dh = (size_t)(c->dim / c->heads), T = (size_t)c->tokens;
     if (c->precision != PPLL_BF16 || dh != 64) {   // the run-time-typed attention kernels keep K, V (or Q, dO) of one head in LDS
@@ -86,6 +101,9 @@ int validate_config(const ppll_block_config* c) {
       if (c->img_c < 1 || c->img_h != m * c->height || c->img_w != m * c->width)
         return bad("the stem keeps the image size: img_h, img_w must equal the first basic block's input size");
     }
+    if (c->rotary || c->qk_norm) return bad("rotary positions and qk_norm belong to ViT blocks");
+    if (c->optimizer == PPLL_MUON && (9 * c->channels > ORTHO_SIDE || c->aux_channels > ORTHO_SIDE))
+      return bad("9 * channels or aux_channels above 8192 with the Muon optimizer");
     if (c->bn_eps <= 0.f || c->bn_momentum < 0.f || c->bn_momentum > 1.f) return bad("bn_eps > 0 and bn_momentum in [0,1] required");
     {
       const size_t m = c->transition_block > 0 ? 2 : 1, wide = c->channels > c->aux_channels ? c->channels : c->aux_channels;
@@ -109,6 +127,44 @@ size_t Block::in_elems() const {
 size_t Block::out_elems() const {
   if (cfg.arch == PPLL_VIT) return (size_t)cfg.batch * cfg.tokens * cfg.dim;
   return (size_t)cfg.batch * cfg.height * cfg.width * cfg.channels;
+}
+
+// Equal matrices of all layers (basic blocks of one shape) are a group: what lies between one layer's and the next is the same everywhere.
+std::vector<ppll_matrix_group> Block::muon_groups() const {
+  std::vector<ppll_matrix_group> groups;
+  auto add = [&](size_t off, size_t step, int rows, int cols, int ld, int count) {
+    groups.push_back({(int64_t)off, (int64_t)step, ld, rows, cols, count, 0});
+  };
+  if (cfg.arch == PPLL_VIT) {
+    const int D = cfg.dim, F = cfg.mlp_dim, layers = cfg.depth + cfg.aux_depth;
+    const EncoderParams& p = enc_p[0];
+    const size_t step = layers > 1 ? enc_p[1].qkv_w - p.qkv_w : 0;
+    for (int i = 0; i < 3; ++i) add(p.qkv_w + i * D, step, D, D, 3 * D, layers);
+    add(p.proj_w, step, D, D, D, layers);
+    add(p.fc1_w, step, D, F, F, layers);
+    add(p.fc2_w, step, F, D, D, layers);
+    return groups;
+  }
+  const int n = cfg.n_basic_blocks;
+  for (int i = 0; i < n;) {
+    const BasicBlockDims& d = rb_d[i];
+    int k = 1;
+    while (i + k < n && rb_d[i + k].Ci == d.Ci && rb_d[i + k].Co == d.Co) ++k;
+    const size_t step = k > 1 ? rb_p[i + 1].conv1_w - rb_p[i].conv1_w : 0;
+    add(rb_p[i].conv1_w, step, 9 * d.Ci, d.Co, d.Co, k);
+    add(rb_p[i].conv2_w, step, 9 * d.Co, d.Co, d.Co, k);
+    i += k;
+  }
+  add(aux_conv_w, 0, 9 * cfg.channels, cfg.aux_channels, cfg.aux_channels, 1);
+  return groups;
+}
+
+void Block::rope_positions(std::vector<int32_t>& out) const {
+  out.assign((size_t)cfg.tokens * 2, 0);
+  for (int t = 1; cfg.rotary && t < cfg.tokens; ++t) {
+    out[2 * t] = (t - 1) / cfg.grid_w;
+    out[2 * t + 1] = (t - 1) % cfg.grid_w;
+  }
 }
 
 size_t Block::plan(char* base) {
@@ -139,6 +195,7 @@ size_t Block::plan(char* base) {
       EncoderParams e;
       e.ln1_g = add(p + ".ln1.g", 1, D); e.ln1_b = add(p + ".ln1.b", 1, D);
       e.qkv_w = add(p + ".qkv.w", D, 3 * D); e.qkv_b = add(p + ".qkv.b", 1, 3 * D);
+      e.qn_g = cfg.qk_norm ? add(p + ".qn.g", 1, D / cfg.heads) : 0; e.kn_g = cfg.qk_norm ? add(p + ".kn.g", 1, D / cfg.heads) : 0;
       e.proj_w = add(p + ".proj.w", D, D); e.proj_b = add(p + ".proj.b", 1, D);
       e.ln2_g = add(p + ".ln2.g", 1, D); e.ln2_b = add(p + ".ln2.b", 1, D);
       e.fc1_w = add(p + ".fc1.w", D, F); e.fc1_b = add(p + ".fc1.b", 1, F);
@@ -179,8 +236,27 @@ size_t Block::plan(char* base) {
 
   Bump bump(base);
   params = bump.floats(P); grads = bump.floats(P); mom1 = bump.floats(P);
-  mom2 = cfg.optimizer == PPLL_ADAMW ? bump.floats(P) : nullptr;
+  mom2 = cfg.optimizer != PPLL_SGD ? bump.floats(P) : nullptr;
   shadow = dt == BF16 ? (uint16_t*)bump.take(P * sizeof(uint16_t)) : nullptr;
+  adam_ranges.clear();
+  ortho = OrthoPlan{};
+  ortho_ws = nullptr;
+  if (cfg.optimizer == PPLL_MUON) {
+    const std::vector<ppll_matrix_group> groups = muon_groups();
+    (void)ortho_plan(groups.data(), (int)groups.size(), &ortho);   // sizes that it refuses, validate_config has refused
+    ortho_ws = (char*)bump.take((size_t)ortho.bytes);
+    auto matrix = [&](size_t off) {
+      for (const ppll_matrix_group& g : groups)
+        for (int i = 0; i < g.count; ++i)
+          if ((int64_t)off == g.offset + i * g.stride) return true;
+      return false;
+    };
+    for (const TensorDesc& t : tensors) {
+      if (matrix(t.off)) continue;
+      if (!adam_ranges.empty() && adam_ranges.back().off + adam_ranges.back().n == t.off) adam_ranges.back().n += t.n;
+      else adam_ranges.push_back({t.off, t.n});
+    }
+  }
   size_t bn_total = 0;
   for (int c : bn_channels) { bn_off.push_back(bn_total); bn_total += c; }
   bn_mean_run = bump.floats(bn_total ? bn_total : 1);
@@ -206,7 +282,21 @@ size_t Block::plan(char* base) {
       a.x2 = bump.take(M * D * esz);
       a.mean1 = bump.floats(M); a.rstd1 = bump.floats(M); a.mean2 = bump.floats(M); a.rstd2 = bump.floats(M);
       a.lse = bump.floats((size_t)B * H * T);
+      a.qk = cfg.qk_norm ? bump.take(M * 2 * D * esz) : nullptr;
       enc_a.push_back(a);
+    }
+    rope = RotaryPlan{};
+    rope_pos = nullptr;
+    if (qk_prepared()) {
+      ppll_rotary_config c{};
+      c.struct_size = sizeof c; c.precision = cfg.precision;
+      c.rows = (int32_t)M; c.tokens = T; c.q_heads = c.k_heads = H; c.head_dim = D / H;
+      c.axes = 2;
+      const int pairs = cfg.rotary ? D / H / 2 : 0;
+      c.pairs[0] = pairs - pairs / 2; c.pairs[1] = pairs / 2;
+      c.base = cfg.rotary ? cfg.rotary_base : 1.f; c.norm_eps = cfg.qk_norm ? cfg.qk_norm_eps : 1.f;
+      (void)rotary_plan(&c, &rope);
+      rope_pos = (int32_t*)bump.take((size_t)T * 2 * sizeof(int32_t));
     }
     z = bump.take((size_t)B * D * esz); dz = bump.take((size_t)B * D * esz); dcls = bump.take((size_t)B * D * esz);
     prune_cls = cfg.aux_depth >= 1 && attention_cls_lds_bytes(T, D / H) <= 160 * 1024;
@@ -217,6 +307,7 @@ size_t Block::plan(char* base) {
       c.h = bump.take(bf); c.gl = bump.take(bf); c.d_h = bump.take(bf);
       c.d_u2 = bump.take(bd); c.d_x1 = bump.take(bd); c.d_att = bump.take(bd); c.d_q = bump.take(bd);
       c.mean2 = bump.floats(B); c.rstd2 = bump.floats(B); c.prob = bump.floats((size_t)B * H * T);
+      c.q_raw = cfg.qk_norm ? bump.take(bd) : nullptr;
     }
     head_mean = bump.floats(B); head_rstd = bump.floats(B);
     d_u = bump.take(M * D * esz);
@@ -243,6 +334,7 @@ size_t Block::plan(char* base) {
       if (eb > partial_floats) partial_floats = eb;
     }
     if (vit_head_partial_floats(B, D, C) > partial_floats) partial_floats = vit_head_partial_floats(B, D, C);
+    if (cfg.qk_norm && rotary_partial_floats(D / H) > partial_floats) partial_floats = rotary_partial_floats(D / H);
   } else {
     const int Ch = cfg.channels, A = cfg.aux_channels, Hh = cfg.height, W = cfg.width;
     const int Ho = (Hh - 1) / 2 + 1, Wo = (W - 1) / 2 + 1;
@@ -312,6 +404,7 @@ size_t Block::plan(char* base) {
     arena_floats = (size_t)(2 * (cfg.depth + cfg.aux_depth)) * (layernorm_bwd_partial_floats((int)M, D, dt) + 64) +
                    layernorm_bwd_partial_floats(B, D, dt) + (size_t)colsum_partial_floats(B, C) + 256 +
                    vit_head_partial_floats(B, D, C) + 64;
+    if (cfg.qk_norm) arena_floats += (size_t)(cfg.depth + cfg.aux_depth + 1) * (rotary_partial_floats(D / cfg.heads) + 64);
     if (cfg.input_kind == PPLL_IN_IMAGE)
       arena_floats += (size_t)embed_bwd_partial_floats(B, T, D) + (size_t)colsum_partial_floats((int)M, D) + 128;
     if (!(dt == BF16))   // the generic GEMM does not fold bias gradients: one column sum per Linear layer
@@ -344,6 +437,39 @@ int Block::first_norm(int l, const EncoderActs& a, const void* x, hipStream_t s)
   return launch_layernorm_fwd(s, x, dt, cfg.dim, cfg.batch * cfg.tokens, cfg.dim, n.g, n.b, n.eps, n.y, n.mean, n.rstd);
 }
 
+int Block::qk_fwd(int l, void* q, long q_ld, int q_rows, int q_tokens, void* q_keep, long q_keep_ld, void* k, long k_ld, void* k_keep, long k_keep_ld,
+                  hipStream_t s) {
+  RotaryPlan p = rope;
+  const EncoderParams& e = enc_p[l];
+  p.rows = q ? q_rows : cfg.batch * cfg.tokens;
+  p.tokens = q ? q_tokens : cfg.tokens;
+  p.heads[0] = q ? cfg.heads : 0; p.heads[1] = k ? cfg.heads : 0;
+  auto side = [&](void* x, long ld, void* keep, long keep_ld, size_t g) {
+    return RotarySide{x, nullptr, x, keep, ld, 0, ld, keep_ld, cfg.qk_norm ? params + g : nullptr};
+  };
+  return launch_rotary_fwd(s, p, dt, rope_pos, side(q, q_ld, q_keep, q_keep_ld, e.qn_g), side(k, k_ld, k_keep, k_keep_ld, e.kn_g));
+}
+
+int Block::qk_bwd(int l, void* dq, long q_ld, int q_rows, int q_tokens, const void* q_raw, long q_raw_ld, void* dk, long k_ld, const void* k_raw,
+                  long k_raw_ld, hipStream_t s) {
+  RotaryPlan p = rope;
+  const EncoderParams& e = enc_p[l];
+  p.rows = dq ? q_rows : cfg.batch * cfg.tokens;
+  p.tokens = dq ? q_tokens : cfg.tokens;
+  p.heads[0] = dq ? cfg.heads : 0; p.heads[1] = dk ? cfg.heads : 0;
+  auto side = [&](void* d, long ld, const void* raw, long raw_ld, size_t g) {
+    return RotarySide{raw, d, d, nullptr, raw_ld, ld, ld, 0, cfg.qk_norm ? params + g : nullptr};
+  };
+  bool queued = false;
+  float* partials = cfg.qk_norm ? rq.space((size_t)rotary_bwd_rows(p) * 2 * p.hd, &queued) : nullptr;
+  int rows = 0;
+  PPLL_TRY(launch_rotary_bwd(s, p, dt, rope_pos, side(dq, q_ld, q_raw, q_raw_ld, e.qn_g), side(dk, k_ld, k_raw, k_raw_ld, e.kn_g), partials, &rows));
+  if (!cfg.qk_norm) return PPLL_OK;
+  if (dq) PPLL_TRY(rq.reduce(s, queued, partials, rows, p.hd, 2 * p.hd, 1.f, grads + e.qn_g));
+  if (dk) PPLL_TRY(rq.reduce(s, queued, partials + p.hd, rows, p.hd, 2 * p.hd, 1.f, grads + e.kn_g));
+  return PPLL_OK;
+}
+
 int Block::encoder_fwd(int l, const EncoderActs& a, const void* x, void* x2_out, const EncoderActs* next, hipStream_t s,
                        const std::function<int()>& stored) {
   const int D = cfg.dim, F = cfg.mlp_dim, T = cfg.tokens, H = cfg.heads, M = cfg.batch * T;
@@ -353,6 +479,10 @@ int Block::encoder_fwd(int l, const EncoderActs& a, const void* x, void* x2_out,
   g.B = wptr(p.qkv_w); g.b_dt = wdt(); g.b_sk = 3 * D; g.b_sn = 1;
   g.C = a.qkv; g.c_dt = dt; g.ldc = 3 * D; g.M = M; g.N = 3 * D; g.K = D; g.bias = params + p.qkv_b;
   PPLL_TRY(launch_gemm(s, g));
+  if (qk_prepared()) {
+    char *q = (char*)a.qkv, *keep = (char*)a.qk;
+    PPLL_TRY(qk_fwd(l, q, 3 * D, M, T, keep, 2 * D, q + D * esz, 3 * D, keep ? keep + D * esz : nullptr, 2 * D, s));
+  }
   PPLL_TRY(launch_attention_fwd(s, a.qkv, dt, cfg.batch, T, H, D / H, a.att, a.lse));
   g = gemm_args();
   g.A = a.att; g.a_dt = dt; g.a_sm = D; g.a_sk = 1;
@@ -410,6 +540,10 @@ int Block::encoder_bwd(int l, const void* x, const void* g_in, void* g_tmp, void
   PPLL_TRY(launch_gemm(s, dgrad(g_tmp, D, p.proj_w, D, d_u)));
   PPLL_TRY(wgrad(a.att, D, g_tmp, D, p.proj_w, p.proj_b));
   PPLL_TRY(launch_attention_bwd(s, a.qkv, a.att, d_u, a.lse, dt, cfg.batch, T, H, D / H, d_qkv));
+  if (qk_prepared()) {
+    char *d = (char*)d_qkv, *raw = (char*)a.qk;
+    PPLL_TRY(qk_bwd(l, d, 3 * D, M, T, raw, 2 * D, d + D * esz, 3 * D, raw ? raw + D * esz : nullptr, 2 * D, s));
+  }
   PPLL_TRY(launch_gemm_then_norm_bwd(s, dgrad(d_qkv, 3 * D, p.qkv_w, D, d_u),
                                      {x, a.mean1, a.rstd1, params + p.ln1_g, g_tmp, need_dx ? g_out : nullptr, grads + p.ln1_g,
                                       grads + p.ln1_b}, rq));
@@ -487,6 +621,10 @@ int Block::encoder_fwd_cls(int l, const EncoderActs& a, const ClsActs& c, const 
   g.B = wptr(p.qkv_w); g.b_dt = wdt(); g.b_sk = 3 * D; g.b_sn = 1;
   g.C = c.q; g.c_dt = dt; g.ldc = D; g.M = B; g.N = D; g.K = D; g.bias = params + p.qkv_b;
   PPLL_TRY(launch_gemm(s, g));
+  if (qk_prepared()) {
+    PPLL_TRY(qk_fwd(l, nullptr, 0, 0, 0, nullptr, 0, a.qkv, 2 * D, a.qk, D, s));
+    if (cfg.qk_norm) PPLL_TRY(qk_fwd(l, c.q, D, B, 1, c.q_raw, D, nullptr, 0, nullptr, 0, s));     // the class token does not turn
+  }
   PPLL_TRY(launch_attention_cls_fwd(s, c.q, a.qkv, dt, B, T, H, D / H, c.att, c.prob));
   g = gemm_args();
   g.A = c.att; g.a_dt = dt; g.a_sm = D; g.a_sk = 1;
@@ -536,6 +674,10 @@ int Block::encoder_bwd_cls(int l, const void* x, const void* d_x2, void* g_out, 
   PPLL_TRY(launch_gemm(s, dgrad(c.d_x1, B, D, wptr(p.proj_w), D, D, c.d_att)));
   PPLL_TRY(wgrad_product(c.att, D, D, c.d_x1, D, D, B, grads + p.proj_w, D, grads + p.proj_b, s));
   PPLL_TRY(launch_attention_cls_bwd(s, c.q, a.qkv, c.prob, c.d_att, dt, B, T, H, D / H, c.d_q, d_kv));
+  if (qk_prepared()) {
+    PPLL_TRY(qk_bwd(l, nullptr, 0, 0, 0, nullptr, 0, d_kv, 2 * D, a.qk, D, s));
+    if (cfg.qk_norm) PPLL_TRY(qk_bwd(l, c.d_q, D, B, 1, c.q_raw, D, nullptr, 0, nullptr, 0, s));
+  }
   // gradient at LayerNorm 1's output: keys and values of all rows, plus the query's share on the class-token rows
   PPLL_TRY(launch_gemm(s, dgrad(d_kv, M, 2 * D, (const char*)wptr(p.qkv_w) + (size_t)D * wsz, 3 * D, D, d_u)));
   g = dgrad(c.d_q, B, D, wptr(p.qkv_w), 3 * D, D, d_u);
@@ -900,6 +1042,11 @@ int Block::update(float lr, hipStream_t s) {
     return launch_sgd(s, params, grads, mom1, shadow, P, lr, cfg.momentum, cfg.nesterov, cfg.weight_decay, steps == 1);
   float bc1 = (float)(1.0 - std::pow((double)cfg.beta1, (double)steps));
   float bc2 = (float)(1.0 - std::pow((double)cfg.beta2, (double)steps));
+  if (cfg.optimizer == PPLL_MUON) {
+    PPLL_TRY(launch_adamw_ranges(s, adam_ranges.data(), (int)adam_ranges.size(), params, grads, mom1, mom2, shadow, lr, cfg.beta1, cfg.beta2,
+                                 cfg.adam_eps, cfg.weight_decay, bc1, bc2));
+    return launch_muon(s, ortho, MUON_STEPS, grads, mom1, params, shadow, lr, cfg.momentum, cfg.nesterov, cfg.weight_decay, ortho_ws);
+  }
   return launch_adamw(s, params, grads, mom1, mom2, shadow, P, lr, cfg.beta1, cfg.beta2, cfg.adam_eps, cfg.weight_decay, bc1, bc2);
 }
 
@@ -930,7 +1077,7 @@ size_t Block::plan_eval_scratch(char* base, EvalBuffers* e) const {
     a.h = bump.take(M * F * esz); a.gl = bump.take(M * F * esz);
     a.mean1 = bump.floats(M); a.rstd1 = bump.floats(M); a.mean2 = bump.floats(M); a.rstd2 = bump.floats(M);
     a.lse = bump.floats(B * H * T);
-    e->shared_enc[0] = a; e->shared_enc[1] = a;
+    e->shared_enc[0] = a; e->shared_enc[1] = a;      // (qk null: an evaluation keeps no queries and keys)
     e->shared_enc[0].x2 = bump.take(M * D * esz);
     e->shared_enc[1].x2 = bump.take(M * D * esz);
     e->z = bump.take(B * D * esz);

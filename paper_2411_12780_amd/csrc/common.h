@@ -353,6 +353,10 @@ int launch_sgd(hipStream_t s, float* p, const float* g, float* buf, uint16_t* sh
                float momentum, int nesterov, float wd, int first);
 int launch_adamw(hipStream_t s, float* p, const float* g, float* m, float* v, uint16_t* shadow, size_t n, float lr,
                  float b1, float b2, float eps, float wd, float bias_corr1, float bias_corr2);
+// AdamW on ranges of the blob (offsets from p, g, m, v, shadow)
+struct BlobRange { size_t off, n; };
+int launch_adamw_ranges(hipStream_t s, const BlobRange* ranges, int n, float* p, const float* g, float* m, float* v, uint16_t* shadow, float lr,
+                        float b1, float b2, float eps, float wd, float bias_corr1, float bias_corr2);
 int launch_refresh_shadow(hipStream_t s, const float* p, uint16_t* shadow, size_t n);
 int launch_fill_zero(hipStream_t s, void* p, size_t bytes);
 int launch_copy_probe(hipStream_t s, const void* src, void* dst, size_t bytes);
@@ -370,6 +374,7 @@ int launch_rotary_fwd(hipStream_t s, const RotaryPlan& p, int dt, const int32_t*
 // partials (null without scales): rotary_partial_floats() floats; *rows receives the rows of [2][head_dim] sums left there
 int launch_rotary_bwd(hipStream_t s, const RotaryPlan& p, int dt, const int32_t* positions, const RotarySide& q, const RotarySide& k, float* partials,
                       int* rows);
+int rotary_bwd_rows(const RotaryPlan& p);      // rows of sums that a backward pass leaves
 int launch_rotary_scales(hipStream_t s, const float* partials, int rows, int hd, float* dq, float* dk);   // their sums; dq, dk nullable
 
 // ---------------------------------------------------------------- ResNet pieces

@@ -1453,6 +1453,22 @@ __global__ __launch_bounds__(256) void adamw_kernel(float* p, const float* g, fl
   }
 }
 
+// The same on ranges of the blob: what the Muon optimizer leaves, vectors between the weight matrices.  1024 elements a workgroup.
+constexpr int ADAM_RANGES = 120;    // of a launch: the table stays below the 4 KB of a kernel's arguments
+struct AdamRanges { int n; int first[ADAM_RANGES + 1]; BlobRange range[ADAM_RANGES]; };
+__global__ __launch_bounds__(256) void adamw_ranges_kernel(AdamRanges r, float* p, const float* g, float* m, float* v, uint16_t* shadow, AdamArgs a) {
+  int j = 0;
+  while (j + 1 < r.n && (int)blockIdx.x >= r.first[j + 1]) ++j;
+  const size_t from = (size_t)((int)blockIdx.x - r.first[j]) * 1024, end = min(from + 1024, r.range[j].n);
+  for (size_t k = from + threadIdx.x; k < end; k += 256) {
+    const size_t i = r.range[j].off + k;
+    float mi = m[i], vi = v[i];
+    const float o = adamw_one(p[i], g[i], mi, vi, a);
+    m[i] = mi; v[i] = vi; p[i] = o;
+    if (shadow) shadow[i] = f32_to_bf16(o);
+  }
+}
+
 __global__ __launch_bounds__(256) void refresh_shadow_kernel(const float* p, uint16_t* shadow, size_t n) {
   size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
   if (i < n) shadow[i] = f32_to_bf16(p[i]);
@@ -1474,6 +1490,20 @@ int launch_adamw(hipStream_t s, float* p, const float* g, float* m, float* v, ui
                  float b1, float b2, float eps, float wd, float bc1, float bc2) {
   hipLaunchKernelGGL(adamw_kernel, dim3((n + 1023) / 1024), dim3(256), 0, s, p, g, m, v, shadow, n, AdamArgs{lr, b1, b2, eps, wd, bc1, bc2});
   PPLL_HIP(hipGetLastError());
+  return PPLL_OK;
+}
+int launch_adamw_ranges(hipStream_t s, const BlobRange* ranges, int n, float* p, const float* g, float* m, float* v, uint16_t* shadow, float lr,
+                        float b1, float b2, float eps, float wd, float bc1, float bc2) {
+  for (int j0 = 0; j0 < n; j0 += ADAM_RANGES) {
+    AdamRanges r{};
+    r.n = n - j0 < ADAM_RANGES ? n - j0 : ADAM_RANGES;
+    for (int j = 0; j < r.n; ++j) {
+      r.range[j] = ranges[j0 + j];
+      r.first[j + 1] = r.first[j] + (int)((ranges[j0 + j].n + 1023) / 1024);
+    }
+    hipLaunchKernelGGL(adamw_ranges_kernel, dim3(r.first[r.n]), dim3(256), 0, s, r, p, g, m, v, shadow, AdamArgs{lr, b1, b2, eps, wd, bc1, bc2});
+    PPLL_HIP(hipGetLastError());
+  }
   return PPLL_OK;
 }
 int launch_refresh_shadow(hipStream_t s, const float* p, uint16_t* shadow, size_t n) {

@@ -176,7 +176,7 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
   const int64_t plane_p = MODE == GRAM ? px : pa, plane_q = MODE == POLY ? pa : px;
   const int K = MODE == GRAM ? g.np : g.mp;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wi = wave >> 1, wj = wave & 1;
-  f32x16 acc[IM][IM] = {};
+  f32x16 acc[IM][IM] = {}, cross[IM][IM] = {};
   // rows of 32 k, 64 bytes; the 16-byte granule q of row r sits at q ^ (r / 4 % 4)
   for (int k0 = 0; k0 < K; k0 += BK) {
     __syncthreads();
@@ -200,8 +200,8 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
       for (int i = 0; i < IM; ++i)
         for (int j = 0; j < IM; ++j) {
           acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[j], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], acc[i][j], 0, 0, 0);
+          cross[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], cross[i][j], 0, 0, 0);
+          cross[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], cross[i][j], 0, 0, 0);
         }
     }
   }
@@ -211,7 +211,7 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
       for (int r4 = 0; r4 < 4; ++r4) {
         const int i = bi * TILE + (wi * IM + ii) * 32 + r4 * 8 + 4 * (lane >> 5), j = bj * TILE + (wj * IM + jj) * 32 + (lane & 31);
         float v[4];
-        for (int k = 0; k < 4; ++k) v[k] = acc[ii][jj][r4 * 4 + k] * UNSCALE;
+        for (int k = 0; k < 4; ++k) v[k] = (acc[ii][jj][r4 * 4 + k] + cross[ii][jj][r4 * 4 + k]) * UNSCALE;
         if (MODE != GRAM) {
           // A is symmetric, X^T holds X: four neighbours of a column are four of a row there
           const _Float16* add = (MODE == POLY ? A : XT) + (int64_t)j * g.mp + i;

@@ -131,10 +131,14 @@ __global__ __launch_bounds__(256) void rotary_scale_kernel(const float* partials
   out[e] = t;
 }
 
+constexpr int ROWS_WG = 8;
+int workgroups_of(const RotaryPlan& p, bool bwd) {
+  const int64_t blocks = ((int64_t)p.rows + ROWS_WG - 1) / ROWS_WG, most = bwd ? ROTARY_PARTIALS : 65536;
+  return (int)(blocks < most ? blocks : most);
+}
 int launch(hipStream_t s, RotaryArgs& a, int dt, bool bwd, int* workgroups) {
-  a.rows_wg = 8;
-  const int64_t blocks = ((int64_t)a.p.rows + a.rows_wg - 1) / a.rows_wg;
-  const int wgs = (int)(bwd ? (blocks < ROTARY_PARTIALS ? blocks : ROTARY_PARTIALS) : (blocks < 65536 ? blocks : 65536));
+  a.rows_wg = ROWS_WG;
+  const int wgs = workgroups_of(a.p, bwd);
   const size_t lds = (size_t)a.rows_wg * a.p.pairs * sizeof(float2);
   *workgroups = wgs;
   if (!wgs) return PPLL_OK;
@@ -155,6 +159,7 @@ int launch_rotary_bwd(hipStream_t s, const RotaryPlan& p, int dt, const int32_t*
   RotaryArgs a{p, {q, k}, positions, partials, 0};
   return launch(s, a, dt, true, rows);
 }
+int rotary_bwd_rows(const RotaryPlan& p) { return workgroups_of(p, true); }
 int launch_rotary_scales(hipStream_t s, const float* partials, int rows, int hd, float* dq, float* dk) {
   hipLaunchKernelGGL(rotary_scale_kernel, dim3(2 * ((hd + 15) / 16)), dim3(256), 0, s, partials, rows, hd, dq, dk);
   PPLL_HIP(hipGetLastError());

@@ -116,7 +116,6 @@ int rotary_plan(const ppll_rotary_config* c, RotaryPlan* p) {
     pairs += n;
     p->end[a] = pairs;
   }
-  if (pairs < 1) return bad("no pair turns");
   p->pairs = pairs;
   return PPLL_OK;
 }

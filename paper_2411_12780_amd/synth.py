@@ -15,7 +15,7 @@ import numpy as np
 # arch / input_kind / optimizer / precision codes are the ones of include/ppll.h
 VIT, RESNET = 0, 1
 IMAGE, ACTIVATION = 0, 1
-SGD, ADAMW = 0, 1
+SGD, ADAMW, MUON = 0, 1, 2
 FP32, BF16 = 0, 1
 
 _VIT_STAGE = dict(arch=VIT, precision=BF16, input_kind=IMAGE, batch=128, num_classes=10,
@@ -69,6 +69,9 @@ WORKLOADS = {
                                  num_classes=10, channels=64, height=8, width=8, transition_block=1,
                                  n_basic_blocks=5, aux_channels=64, optimizer=SGD, momentum=0.9,
                                  nesterov=1, weight_decay=1e-4, bn_eps=1e-5, bn_momentum=0.1, lr=0.01),
+    # the ViT stage trained by Muon, with rotary positions of the 8 x 8 patches and normalised queries and keys
+    "vit_stage_muon_bf16": dict(_VIT_STAGE, optimizer=MUON, momentum=0.95, nesterov=1, rotary=1, grid_h=8, grid_w=8, rotary_base=100.0,
+                                qk_norm=1, qk_norm_eps=1e-6),
     # STL-10-shaped ViT stage (96 x 96 images)
     "vit_large_image_bf16": dict(_VIT_STAGE, batch=64, img_h=96, img_w=96, patch=8, tokens=145),
 }
@@ -189,7 +192,7 @@ def make_params(spec, seed: int = 0, jitter: bool = False) -> np.ndarray:
     for name, shape in spec:
         n = int(np.prod(shape))
         leaf = name.split(".")[-1]
-        is_norm = ".ln" in name or ".bn" in name
+        is_norm = any(n in name for n in (".ln", ".bn", ".qn", ".kn"))
         if len(shape) == 4:
             v = rng.standard_normal(n) * np.sqrt(2.0 / (9.0 * shape[2]))
         elif is_norm and leaf == "g":
