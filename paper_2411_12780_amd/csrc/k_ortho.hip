@@ -38,10 +38,13 @@ struct Source { const void* in; int dt; const float* g; float* m; float momentum
 // Where the result goes: out (orthogonalize), or null: the parameters
 struct Target { void* out; int dt; float* p; uint16_t* shadow; float lr, decay; };
 
-__device__ __forceinline__ float split_hi(float v, _Float16& hi, _Float16& lo) {
+// v is pinned to its fp32 value first: the compiler may fold the arithmetic that gives it into one of the two conversions (a fused operation
+// that rounds to fp16 once) and not into the other, and at a tie hi and what lo is counted from are then two neighbours (one element in some
+// 20000 was off by a whole step of hi, 2^-11 of it).
+__device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
+  asm("" : "+v"(v));
   hi = (_Float16)v;
   lo = (_Float16)(v - (float)hi);
-  return v;
 }
 __device__ __forceinline__ int64_t element(const OrthoGroup& g, int matrix, int r, int c) {
   return g.offset + (int64_t)matrix * g.stride + (int64_t)r * g.ld + c;
@@ -124,14 +127,14 @@ __global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, c
   f16x8 h[2], l[2];
   for (int k = 0; k < 16; ++k) {
     _Float16 a, b;
-    split_hi(tile[y][q + k], a, b);
+    split(tile[y][q + k], a, b);
     h[k / 8][k % 8] = a; l[k / 8][k % 8] = b;
   }
   _Float16* to = x + (int64_t)(i0 + y) * g.np + j0 + q;
   for (int k = 0; k < 2; ++k) { *(f16x8*)(to + 8 * k) = h[k]; *(f16x8*)(to + plane + 8 * k) = l[k]; }
   for (int k = 0; k < 16; ++k) {
     _Float16 a, b;
-    split_hi(tile[q + k][y], a, b);
+    split(tile[q + k][y], a, b);
     h[k / 8][k % 8] = a; l[k / 8][k % 8] = b;
   }
   to = xt + (int64_t)(j0 + y) * g.mp + i0 + q;
@@ -239,7 +242,7 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
         f16x4 h, l;
         for (int k = 0; k < 4; ++k) {
           _Float16 a, b;
-          split_hi(v[k], a, b);
+          split(v[k], a, b);
           h[k] = a; l[k] = b;
         }
         _Float16* D = MODE == GRAM ? A : MODE == POLY ? B : X;

@@ -13,6 +13,7 @@ struct RotaryArgs {
   const int32_t* positions;
   float* partials;         // [workgroups][2][head_dim], backward with scales
   int rows_wg;             // rows that a workgroup takes at a time
+  int lanes;               // of a head, in rotary_kernel: a power of two
 };
 
 // cos and sin of every pair of the rows from row0 on, once for all heads: the angle in turns and its nearest whole number in 64 bits (a
@@ -114,6 +115,124 @@ template <bool BWD> __global__ __launch_bounds__(256) void rotary_plain_kernel(R
   }
 }
 
+// V elements in memory, 8 or 16 bytes, as fp32
+template <class T, int V> struct Piece {
+  static constexpr int WORDS = V * (int)sizeof(T) / 4;
+  typedef __attribute__((ext_vector_type(WORDS))) uint32_t words;
+  words w;
+  __device__ __forceinline__ void load(const void* p, int64_t at) { w = *(const words*)((const T*)p + at); }
+  __device__ __forceinline__ void store(void* p, int64_t at) const { *(words*)((T*)p + at) = w; }
+  __device__ __forceinline__ float get(int i) const {
+    if (sizeof(T) == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+  __device__ __forceinline__ void set(const float* v) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = sizeof(T) == 4 ? __float_as_uint(v[i]) : f32x2_to_bf16x2(v[2 * i], v[2 * i + 1]);
+  }
+};
+__device__ __forceinline__ float head_sum(float v, int lanes) {
+  for (int o = lanes >> 1; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// Heads that turn whole, V pairs a lane in two pieces of V elements (of either half of the head, or neighbours), the head's P / V lanes
+// rounded up to a power of two.  Bound by memory: each element is read and written once, cos and sin come from LDS.
+template <class T, int V, bool NEXT, bool NORM, bool BWD> __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
+  extern __shared__ float2 table[];
+  const int P = a.p.pairs, hd = a.p.hd, lanes = a.lanes, c = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = 256 / lanes;
+  const bool on = c * V < P;
+  const int e0 = !on ? 0 : NEXT ? 2 * V * c : V * c, e1 = !on ? 0 : NEXT ? e0 + V : P + e0;
+  const float per = 1.f / hd;
+  float sums[2][2 * V] = {};
+  for (int64_t row0 = (int64_t)blockIdx.x * a.rows_wg; row0 < a.p.rows; row0 += (int64_t)gridDim.x * a.rows_wg) {
+    const int rows = (int)min((int64_t)a.rows_wg, a.p.rows - row0);
+    if (row0 != (int64_t)blockIdx.x * a.rows_wg) __syncthreads();
+    fill_table(a, (int)row0, rows, table);
+    __syncthreads();
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      const RotarySide& s = a.side[side];
+      const int heads = a.p.heads[side];
+      if (!heads) continue;
+      float g[2 * V];
+      if (NORM) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) { g[i] = s.scale[e0 + i]; g[V + i] = s.scale[e1 + i]; }
+      }
+      const int dr = groups / heads, dh = groups - dr * heads;
+      int r = group / heads, h = group - r * heads;
+      for (; r < rows; r += dr, h += dh) {
+        if (h >= heads) { h -= heads; if (++r >= rows) break; }
+        const int64_t row = row0 + r;
+        Piece<T, V> x0{}, x1{}, d0{}, d1{};
+        if (on) {
+          if (!BWD || NORM) { x0.load(s.x, row * s.x_ld + h * hd + e0); x1.load(s.x, row * s.x_ld + h * hd + e1); }
+          if (BWD) { d0.load(s.dy, row * s.dy_ld + h * hd + e0); d1.load(s.dy, row * s.dy_ld + h * hd + e1); }
+          if (!BWD && s.keep) { x0.store(s.keep, row * s.keep_ld + h * hd + e0); x1.store(s.keep, row * s.keep_ld + h * hd + e1); }
+        }
+        float v[2 * V], z[2 * V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) { v[i] = x0.get(i); v[V + i] = x1.get(i); }
+        float rs = 1.f;
+        if (NORM) {
+          float q = 0.f;
+#pragma unroll
+          for (int i = 0; i < 2 * V; ++i) q = fmaf(v[i], v[i], q);
+          rs = 1.f / sqrtf(fmaf(head_sum(q, lanes), per, a.p.eps));
+#pragma unroll
+          for (int i = 0; i < 2 * V; ++i) v[i] *= rs;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          z[i] = BWD ? d0.get(i) : NORM ? v[i] * g[i] : v[i];
+          z[V + i] = BWD ? d1.get(i) : NORM ? v[V + i] * g[V + i] : v[V + i];
+        }
+        const float2* cs = table + r * P + (on ? c * V : 0);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          float &u = NEXT ? z[2 * i] : z[i], &w = NEXT ? z[2 * i + 1] : z[V + i];
+          const float sn = BWD ? -cs[i].y : cs[i].y, t = u;
+          u = fmaf(t, cs[i].x, -w * sn);
+          w = fmaf(w, cs[i].x, t * sn);
+        }
+        if (BWD && NORM) {
+          float along = 0.f;
+#pragma unroll
+          for (int i = 0; i < 2 * V; ++i) {
+            sums[side][i] = fmaf(z[i], v[i], sums[side][i]);
+            z[i] *= g[i];
+            along = fmaf(z[i], v[i], along);
+          }
+          along = head_sum(along, lanes) * per;
+#pragma unroll
+          for (int i = 0; i < 2 * V; ++i) z[i] = rs * fmaf(-v[i], along, z[i]);
+        }
+        if (on) {
+          d0.set(z); d1.set(z + V);
+          d0.store(s.y, row * s.y_ld + h * hd + e0); d1.store(s.y, row * s.y_ld + h * hd + e1);
+        }
+      }
+    }
+  }
+  if (!BWD || !NORM) return;
+  // the sums of a head's lanes over the wave's groups, then over the four waves, in this order always
+  __shared__ float part[4][256];
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) {
+      float v = sums[side][i];
+      for (int o = 32; o >= lanes; o >>= 1) v += __shfl_xor(v, o);
+      if (on && (threadIdx.x & 63) < lanes) part[threadIdx.x >> 6][(i < V ? e0 : e1 - V) + i] = v;
+    }
+    __syncthreads();
+    const int e = threadIdx.x;
+    if (e < hd) a.partials[((int64_t)blockIdx.x * 2 + side) * hd + e] = part[0][e] + part[1][e] + part[2][e] + part[3][e];
+  }
+}
+
 // d scale from the workgroups' partial sums, 16 elements a workgroup; queries first, then keys
 __global__ __launch_bounds__(256) void rotary_scale_kernel(const float* partials, int chunks, int hd, float* dq, float* dk) {
   __shared__ float red[16][17];
@@ -131,33 +250,67 @@ __global__ __launch_bounds__(256) void rotary_scale_kernel(const float* partials
   out[e] = t;
 }
 
-constexpr int ROWS_WG = 8;
+// Rows that a workgroup takes at a time: as many as fill the chip's 256 units twice over, up to 8, whose table of 32 pairs a row takes each
+// thread one sine and cosine.
+int rows_wg(const RotaryPlan& p) {
+  const int r = p.rows / 512;
+  return r < 1 ? 1 : r > 8 ? 8 : r;
+}
 int workgroups_of(const RotaryPlan& p, bool bwd) {
-  const int64_t blocks = ((int64_t)p.rows + ROWS_WG - 1) / ROWS_WG, most = bwd ? ROTARY_PARTIALS : 65536;
+  const int64_t blocks = ((int64_t)p.rows + rows_wg(p) - 1) / rows_wg(p), most = bwd ? ROTARY_PARTIALS : (int64_t)1 << 30;
   return (int)(blocks < most ? blocks : most);
 }
-int launch(hipStream_t s, RotaryArgs& a, int dt, bool bwd, int* workgroups) {
-  a.rows_wg = ROWS_WG;
-  const int wgs = workgroups_of(a.p, bwd);
+// Elements of a lane's piece: 16 bytes, or 8 where half a head or a buffer has no more in common with them; 0: no pieces.
+int piece_of(const RotaryArgs& a, int dt) {
+  const int P = a.p.pairs, esz = (int)dtype_size(dt);
+  if (2 * P != a.p.hd) return 0;
+  for (int v = 16 / esz; v >= 4; v /= 2) {
+    bool ok = P % v == 0;
+    for (const RotarySide& s : a.side)
+      for (const void* p : {s.x, s.dy, (const void*)s.y, (const void*)s.keep}) ok = ok && !((uintptr_t)p & (v * esz - 1));
+    for (const RotarySide& s : a.side)
+      for (int64_t ld : {s.x_ld, s.dy_ld, s.y_ld, s.keep_ld}) ok = ok && ld % v == 0;
+    if (ok) return v;
+  }
+  return 0;
+}
+template <class T, int V, bool BWD> void launch_pieces(hipStream_t s, const RotaryArgs& a, int wgs, size_t lds) {
+  const bool norm = a.side[0].scale || a.side[1].scale;
+  if (a.p.neighbours) {
+    if (norm) hipLaunchKernelGGL((rotary_kernel<T, V, true, true, BWD>), dim3(wgs), dim3(256), lds, s, a);
+    else hipLaunchKernelGGL((rotary_kernel<T, V, true, false, BWD>), dim3(wgs), dim3(256), lds, s, a);
+  } else {
+    if (norm) hipLaunchKernelGGL((rotary_kernel<T, V, false, true, BWD>), dim3(wgs), dim3(256), lds, s, a);
+    else hipLaunchKernelGGL((rotary_kernel<T, V, false, false, BWD>), dim3(wgs), dim3(256), lds, s, a);
+  }
+}
+template <bool BWD> int launch(hipStream_t s, RotaryArgs& a, int dt, int* workgroups) {
+  a.rows_wg = rows_wg(a.p);
+  const int wgs = workgroups_of(a.p, BWD);
   const size_t lds = (size_t)a.rows_wg * a.p.pairs * sizeof(float2);
   *workgroups = wgs;
   if (!wgs) return PPLL_OK;
-  if (bwd) hipLaunchKernelGGL((rotary_plain_kernel<true>), dim3(wgs), dim3(256), lds, s, a, dt);
-  else hipLaunchKernelGGL((rotary_plain_kernel<false>), dim3(wgs), dim3(256), lds, s, a, dt);
+  const int piece = piece_of(a, dt);
+  if (piece)
+    for (a.lanes = 1; a.lanes * piece < a.p.pairs;) a.lanes *= 2;
+  if (!piece) hipLaunchKernelGGL((rotary_plain_kernel<BWD>), dim3(wgs), dim3(256), lds, s, a, dt);
+  else if (dt == F32) launch_pieces<float, 4, BWD>(s, a, wgs, lds);
+  else if (piece == 8) launch_pieces<uint16_t, 8, BWD>(s, a, wgs, lds);
+  else launch_pieces<uint16_t, 4, BWD>(s, a, wgs, lds);
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }
 }  // namespace
 
 int launch_rotary_fwd(hipStream_t s, const RotaryPlan& p, int dt, const int32_t* positions, const RotarySide& q, const RotarySide& k) {
-  RotaryArgs a{p, {q, k}, positions, nullptr, 0};
+  RotaryArgs a{p, {q, k}, positions, nullptr, 0, 0};
   int wgs;
-  return launch(s, a, dt, false, &wgs);
+  return launch<false>(s, a, dt, &wgs);
 }
 int launch_rotary_bwd(hipStream_t s, const RotaryPlan& p, int dt, const int32_t* positions, const RotarySide& q, const RotarySide& k, float* partials,
                       int* rows) {
-  RotaryArgs a{p, {q, k}, positions, partials, 0};
-  return launch(s, a, dt, true, rows);
+  RotaryArgs a{p, {q, k}, positions, partials, 0, 0};
+  return launch<true>(s, a, dt, rows);
 }
 int rotary_bwd_rows(const RotaryPlan& p) { return workgroups_of(p, true); }
 int launch_rotary_scales(hipStream_t s, const float* partials, int rows, int hd, float* dq, float* dk) {
