@@ -72,13 +72,20 @@ class QueriesKeys(C.Structure):
     _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("q_ld", C.c_int64), ("k_ld", C.c_int64)]
 
 
+def _rows(t):
+    """Address and row stride of a 2-d tensor whose last axis is contiguous."""
+    if t is None:
+        return None, 0
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise PpllError(3, "queries and keys are 2-d tensors with a contiguous last axis")
+    return t.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], shape[1])
+
+
 def queries_keys(q, k) -> QueriesKeys:
     """2-d tensors [rows, heads * head_dim] whose last axis is contiguous, or None."""
-    for t in (q, k):
-        if t is not None and (t.dim() != 2 or t.stride(1) != 1 and t.shape[1] > 1):
-            raise PpllError(3, "queries and keys are 2-d tensors with a contiguous last axis")
-    ld = [0 if t is None else t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]) for t in (q, k)]
-    return QueriesKeys(_ptr(q), _ptr(k), *ld)
+    (qp, ql), (kp, kl) = _rows(q), _rows(k)
+    return QueriesKeys(qp, kp, ql, kl)
 
 
 class RotaryConfig(C.Structure):
@@ -173,9 +180,7 @@ def _check(status: int) -> None:
 
 def _ptr(t) -> Optional[int]:
     """Device/host address of a torch tensor, numpy array, int or None."""
-    if t is None:
-        return None
-    if isinstance(t, int):
+    if t is None or isinstance(t, int):
         return t
     if isinstance(t, np.ndarray):
         return t.ctypes.data

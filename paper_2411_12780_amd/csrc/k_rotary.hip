@@ -137,81 +137,83 @@ __device__ __forceinline__ float head_sum(float v, int lanes) {
 }
 
 // Heads that turn whole, V pairs a lane in two pieces of V elements (of either half of the head, or neighbours), the head's P / V lanes
-// rounded up to a power of two.  Bound by memory: each element is read and written once, cos and sin come from LDS.
-template <class T, int V, bool NEXT, bool NORM, bool BWD> __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
+// rounded up to a power of two; queries and keys in workgroups of their own (blockIdx.y), which leaves registers for the sums of one side
+// and the next head's elements on their way.  Bound by memory: each element is read and written once, cos and sin come from LDS.
+template <class T, int V, bool NEXT, bool NORM, bool BWD> __global__ __launch_bounds__(256, 4) void rotary_kernel(RotaryArgs a) {
   extern __shared__ float2 table[];
+  const int side = a.p.heads[0] ? blockIdx.y : 1;
+  const RotarySide& s = a.side[side];
   const int P = a.p.pairs, hd = a.p.hd, lanes = a.lanes, c = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = 256 / lanes;
+  const int heads = a.p.heads[side], dr = groups / heads, dh = groups - dr * heads;
   const bool on = c * V < P;
   const int e0 = !on ? 0 : NEXT ? 2 * V * c : V * c, e1 = !on ? 0 : NEXT ? e0 + V : P + e0;
   const float per = 1.f / hd;
-  float sums[2][2 * V] = {};
+  float g[2 * V], sums[2 * V] = {};
+#pragma unroll
+  for (int i = 0; i < V; ++i) { g[i] = NORM ? s.scale[e0 + i] : 1.f; g[V + i] = NORM ? s.scale[e1 + i] : 1.f; }
   for (int64_t row0 = (int64_t)blockIdx.x * a.rows_wg; row0 < a.p.rows; row0 += (int64_t)gridDim.x * a.rows_wg) {
     const int rows = (int)min((int64_t)a.rows_wg, a.p.rows - row0);
+    int r = group / heads, h = group - r * heads;
+    Piece<T, V> x0{}, x1{}, d0{}, d1{};
+    auto load = [&]() {
+      if (!on || r >= rows) return;
+      const int64_t row = row0 + r;
+      if (!BWD || NORM) { x0.load(s.x, row * s.x_ld + h * hd + e0); x1.load(s.x, row * s.x_ld + h * hd + e1); }
+      if (BWD) { d0.load(s.dy, row * s.dy_ld + h * hd + e0); d1.load(s.dy, row * s.dy_ld + h * hd + e1); }
+    };
+    load();
     if (row0 != (int64_t)blockIdx.x * a.rows_wg) __syncthreads();
     fill_table(a, (int)row0, rows, table);
     __syncthreads();
+    while (r < rows) {
+      const int64_t row = row0 + r;
+      const float2* cs = table + r * P + (on ? c * V : 0);
+      const int at = h * hd;
+      Piece<T, V> u0 = x0, u1 = x1;
+      float z[2 * V], v[2 * V];
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-      const RotarySide& s = a.side[side];
-      const int heads = a.p.heads[side];
-      if (!heads) continue;
-      float g[2 * V];
-      if (NORM) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) { g[i] = s.scale[e0 + i]; g[V + i] = s.scale[e1 + i]; }
+      for (int i = 0; i < V; ++i) {
+        v[i] = x0.get(i); v[V + i] = x1.get(i);
+        z[i] = BWD ? d0.get(i) : v[i]; z[V + i] = BWD ? d1.get(i) : v[V + i];
       }
-      const int dr = groups / heads, dh = groups - dr * heads;
-      int r = group / heads, h = group - r * heads;
-      for (; r < rows; r += dr, h += dh) {
-        if (h >= heads) { h -= heads; if (++r >= rows) break; }
-        const int64_t row = row0 + r;
-        Piece<T, V> x0{}, x1{}, d0{}, d1{};
-        if (on) {
-          if (!BWD || NORM) { x0.load(s.x, row * s.x_ld + h * hd + e0); x1.load(s.x, row * s.x_ld + h * hd + e1); }
-          if (BWD) { d0.load(s.dy, row * s.dy_ld + h * hd + e0); d1.load(s.dy, row * s.dy_ld + h * hd + e1); }
-          if (!BWD && s.keep) { x0.store(s.keep, row * s.keep_ld + h * hd + e0); x1.store(s.keep, row * s.keep_ld + h * hd + e1); }
+      r += dr; h += dh;
+      if (h >= heads) { h -= heads; ++r; }
+      load();
+      float rs = 1.f;
+      if (NORM) {
+        float q = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) q = fmaf(v[i], v[i], q);
+        rs = 1.f / sqrtf(fmaf(head_sum(q, lanes), per, a.p.eps));
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) {
+          v[i] *= rs;
+          if (!BWD) z[i] = v[i] * g[i];
         }
-        float v[2 * V], z[2 * V];
+      }
 #pragma unroll
-        for (int i = 0; i < V; ++i) { v[i] = x0.get(i); v[V + i] = x1.get(i); }
-        float rs = 1.f;
-        if (NORM) {
-          float q = 0.f;
+      for (int i = 0; i < V; ++i) {
+        float &u = NEXT ? z[2 * i] : z[i], &w = NEXT ? z[2 * i + 1] : z[V + i];
+        const float sn = BWD ? -cs[i].y : cs[i].y, t = u;
+        u = fmaf(t, cs[i].x, -w * sn);
+        w = fmaf(w, cs[i].x, t * sn);
+      }
+      if (BWD && NORM) {
+        float along = 0.f;
 #pragma unroll
-          for (int i = 0; i < 2 * V; ++i) q = fmaf(v[i], v[i], q);
-          rs = 1.f / sqrtf(fmaf(head_sum(q, lanes), per, a.p.eps));
-#pragma unroll
-          for (int i = 0; i < 2 * V; ++i) v[i] *= rs;
+        for (int i = 0; i < 2 * V; ++i) {
+          sums[i] = fmaf(z[i], v[i], sums[i]);
+          z[i] *= g[i];
+          along = fmaf(z[i], v[i], along);
         }
+        along = head_sum(along, lanes) * per;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          z[i] = BWD ? d0.get(i) : NORM ? v[i] * g[i] : v[i];
-          z[V + i] = BWD ? d1.get(i) : NORM ? v[V + i] * g[V + i] : v[V + i];
-        }
-        const float2* cs = table + r * P + (on ? c * V : 0);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          float &u = NEXT ? z[2 * i] : z[i], &w = NEXT ? z[2 * i + 1] : z[V + i];
-          const float sn = BWD ? -cs[i].y : cs[i].y, t = u;
-          u = fmaf(t, cs[i].x, -w * sn);
-          w = fmaf(w, cs[i].x, t * sn);
-        }
-        if (BWD && NORM) {
-          float along = 0.f;
-#pragma unroll
-          for (int i = 0; i < 2 * V; ++i) {
-            sums[side][i] = fmaf(z[i], v[i], sums[side][i]);
-            z[i] *= g[i];
-            along = fmaf(z[i], v[i], along);
-          }
-          along = head_sum(along, lanes) * per;
-#pragma unroll
-          for (int i = 0; i < 2 * V; ++i) z[i] = rs * fmaf(-v[i], along, z[i]);
-        }
-        if (on) {
-          d0.set(z); d1.set(z + V);
-          d0.store(s.y, row * s.y_ld + h * hd + e0); d1.store(s.y, row * s.y_ld + h * hd + e1);
-        }
+        for (int i = 0; i < 2 * V; ++i) z[i] = rs * fmaf(-v[i], along, z[i]);
+      }
+      if (on) {
+        if (!BWD && s.keep) { u0.store(s.keep, row * s.keep_ld + at + e0); u1.store(s.keep, row * s.keep_ld + at + e1); }
+        u0.set(z); u1.set(z + V);
+        u0.store(s.y, row * s.y_ld + at + e0); u1.store(s.y, row * s.y_ld + at + e1);
       }
     }
   }
@@ -219,45 +221,53 @@ template <class T, int V, bool NEXT, bool NORM, bool BWD> __global__ __launch_bo
   // the sums of a head's lanes over the wave's groups, then over the four waves, in this order always
   __shared__ float part[4][256];
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2 * V; ++i) {
-      float v = sums[side][i];
-      for (int o = 32; o >= lanes; o >>= 1) v += __shfl_xor(v, o);
-      if (on && (threadIdx.x & 63) < lanes) part[threadIdx.x >> 6][(i < V ? e0 : e1 - V) + i] = v;
-    }
-    __syncthreads();
-    const int e = threadIdx.x;
-    if (e < hd) a.partials[((int64_t)blockIdx.x * 2 + side) * hd + e] = part[0][e] + part[1][e] + part[2][e] + part[3][e];
+  for (int i = 0; i < 2 * V; ++i) {
+    float v = sums[i];
+    for (int o = 32; o >= lanes; o >>= 1) v += __shfl_xor(v, o);
+    if (on && (threadIdx.x & 63) < lanes) part[threadIdx.x >> 6][(i < V ? e0 : e1 - V) + i] = v;
   }
+  __syncthreads();
+  const int e = threadIdx.x;
+  if (e < hd) a.partials[((int64_t)blockIdx.x * 2 + side) * hd + e] = part[0][e] + part[1][e] + part[2][e] + part[3][e];
 }
 
 // d scale from the workgroups' partial sums, 16 elements a workgroup; queries first, then keys
-__global__ __launch_bounds__(256) void rotary_scale_kernel(const float* partials, int chunks, int hd, float* dq, float* dk) {
-  __shared__ float red[16][17];
+__global__ __launch_bounds__(1024) void rotary_scale_kernel(const float* partials, int chunks, int hd, float* dq, float* dk) {
+  __shared__ float red[64][17];
   const int col = threadIdx.x & 15, grp = threadIdx.x >> 4, across = (hd + 15) / 16;
   const int side = blockIdx.x / across, e = blockIdx.x % across * 16 + col;
-  float acc = 0.f;
-  if (e < hd)
-    for (int c = grp; c < chunks; c += 16) acc += partials[((int64_t)c * 2 + side) * hd + e];
-  red[grp][col] = acc;
-  __syncthreads();
   float* out = side ? dk : dq;
-  if (grp || e >= hd || !out) return;
-  float t = 0.f;
-  for (int g = 0; g < 16; ++g) t += red[g][col];
-  out[e] = t;
+  if (!out) return;
+  float acc = 0.f;
+  if (e < hd) {
+#pragma unroll 8
+    for (int c = grp; c < chunks; c += 64) acc += partials[((int64_t)c * 2 + side) * hd + e];
+  }
+  red[grp][col] = acc;
+  for (int w = 32; w > 0; w >>= 1) {
+    __syncthreads();
+    if (grp < w) red[grp][col] += red[grp + w][col];
+  }
+  if (grp == 0 && e < hd) out[e] = red[0][col];
 }
 
-// Rows that a workgroup takes at a time: as many as fill the chip's 256 units twice over, up to 8, whose table of 32 pairs a row takes each
-// thread one sine and cosine.
-int rows_wg(const RotaryPlan& p) {
-  const int r = p.rows / 512;
-  return r < 1 ? 1 : r > 8 ? 8 : r;
+// Rows that a workgroup takes at a time.  Forward: enough for each thread to have two or three heads, whose reads then overlap, unless that
+// leaves the 256 units fewer than four workgroups.  Backward: the partial sums hold 512 workgroups a side, which share the rows evenly; the
+// table of a turn is 32 KB at most.
+int rows_wg(const RotaryPlan& p, bool bwd) {
+  const int most = p.pairs > 64 ? 32 : 64;
+  if (bwd) {
+    const int64_t each = ((int64_t)p.rows + ROTARY_PARTIALS - 1) / ROTARY_PARTIALS, turns = (each + most - 1) / most;
+    return (int)((each + turns - 1) / (turns > 0 ? turns : 1));
+  }
+  const int heads = p.heads[0] > p.heads[1] ? p.heads[0] : p.heads[1], sides = p.heads[0] && p.heads[1] ? 2 : 1;
+  const int64_t few = (int64_t)p.rows * sides / 2048, busy = 10240 / ((int64_t)heads * p.hd) + 1;
+  const int64_t r = few < busy ? few : busy;
+  return (int)(r < 1 ? 1 : r > most ? most : r);
 }
 int workgroups_of(const RotaryPlan& p, bool bwd) {
-  const int64_t blocks = ((int64_t)p.rows + rows_wg(p) - 1) / rows_wg(p), most = bwd ? ROTARY_PARTIALS : (int64_t)1 << 30;
+  const int each = rows_wg(p, bwd) > 0 ? rows_wg(p, bwd) : 1;
+  const int64_t blocks = ((int64_t)p.rows + each - 1) / each, most = bwd ? ROTARY_PARTIALS : (int64_t)1 << 30;
   return (int)(blocks < most ? blocks : most);
 }
 // Elements of a lane's piece: 16 bytes, or 8 where half a head or a buffer has no more in common with them; 0: no pieces.
@@ -275,17 +285,18 @@ int piece_of(const RotaryArgs& a, int dt) {
   return 0;
 }
 template <class T, int V, bool BWD> void launch_pieces(hipStream_t s, const RotaryArgs& a, int wgs, size_t lds) {
+  const dim3 grid(wgs, a.p.heads[0] && a.p.heads[1] ? 2 : 1);
   const bool norm = a.side[0].scale || a.side[1].scale;
   if (a.p.neighbours) {
-    if (norm) hipLaunchKernelGGL((rotary_kernel<T, V, true, true, BWD>), dim3(wgs), dim3(256), lds, s, a);
-    else hipLaunchKernelGGL((rotary_kernel<T, V, true, false, BWD>), dim3(wgs), dim3(256), lds, s, a);
+    if (norm) hipLaunchKernelGGL((rotary_kernel<T, V, true, true, BWD>), grid, dim3(256), lds, s, a);
+    else hipLaunchKernelGGL((rotary_kernel<T, V, true, false, BWD>), grid, dim3(256), lds, s, a);
   } else {
-    if (norm) hipLaunchKernelGGL((rotary_kernel<T, V, false, true, BWD>), dim3(wgs), dim3(256), lds, s, a);
-    else hipLaunchKernelGGL((rotary_kernel<T, V, false, false, BWD>), dim3(wgs), dim3(256), lds, s, a);
+    if (norm) hipLaunchKernelGGL((rotary_kernel<T, V, false, true, BWD>), grid, dim3(256), lds, s, a);
+    else hipLaunchKernelGGL((rotary_kernel<T, V, false, false, BWD>), grid, dim3(256), lds, s, a);
   }
 }
 template <bool BWD> int launch(hipStream_t s, RotaryArgs& a, int dt, int* workgroups) {
-  a.rows_wg = rows_wg(a.p);
+  a.rows_wg = rows_wg(a.p, BWD);
   const int wgs = workgroups_of(a.p, BWD);
   const size_t lds = (size_t)a.rows_wg * a.p.pairs * sizeof(float2);
   *workgroups = wgs;
@@ -314,7 +325,7 @@ int launch_rotary_bwd(hipStream_t s, const RotaryPlan& p, int dt, const int32_t*
 }
 int rotary_bwd_rows(const RotaryPlan& p) { return workgroups_of(p, true); }
 int launch_rotary_scales(hipStream_t s, const float* partials, int rows, int hd, float* dq, float* dk) {
-  hipLaunchKernelGGL(rotary_scale_kernel, dim3(2 * ((hd + 15) / 16)), dim3(256), 0, s, partials, rows, hd, dq, dk);
+  hipLaunchKernelGGL(rotary_scale_kernel, dim3(2 * ((hd + 15) / 16)), dim3(1024), 0, s, partials, rows, hd, dq, dk);
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }

@@ -108,11 +108,14 @@ int rotary_plan(const ppll_rotary_config* c, RotaryPlan* p) {
   if (!(c->base > 0.f) || !std::isfinite(c->base)) return bad("base must be positive and finite");
   p->rows = c->rows; p->tokens = c->tokens; p->heads[0] = c->q_heads; p->heads[1] = c->k_heads;
   p->hd = c->head_dim; p->axes = c->axes; p->neighbours = c->neighbours != 0; p->eps = c->norm_eps;
+  // (exp2 takes a third of pow's time, of the 0.7 us of a call with 32 pairs; the exponent's rounding is a relative 1e-16 for each octave,
+  // which a pair that turns less feels less)
+  const double octaves = std::log2((double)c->base);
   int pairs = 0;
   for (int a = 0; a < 3; ++a) {
     const int n = a < c->axes ? c->pairs[a] : 0;
     if (n < 0 || n > c->head_dim / 2 - pairs) return bad("pairs of the axes: none negative, together head_dim / 2 at most");
-    for (int i = 0; i < n; ++i) p->turns[pairs + i] = std::pow((double)c->base, -(double)i / n) / 6.283185307179586476925;
+    for (int i = 0; i < n; ++i) p->turns[pairs + i] = std::exp2(-octaves * i / n) / 6.283185307179586476925;
     pairs += n;
     p->end[a] = pairs;
   }

@@ -8,7 +8,7 @@
 namespace ppll {
 
 constexpr int ROTARY_PAIRS = 128;          // pairs of a head, at most
-constexpr int ROTARY_PARTIALS = 1024;      // workgroups of a backward pass, each leaving a row of 2 x head_dim partial sums
+constexpr int ROTARY_PARTIALS = 512;       // workgroups of a backward pass (a side), each leaving a row of partial sums in [.][2][head_dim]
 
 struct RotaryPlan {
   int32_t rows, tokens, heads[2], hd, axes, pairs, neighbours;
