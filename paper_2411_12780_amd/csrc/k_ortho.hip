@@ -1,5 +1,6 @@
 // Newton-Schulz orthogonalisation of batches of matrices and the Muon step around it.
 #include "common.h"
+#include "gemm_pipe.h"
 #include "ortho.h"
 
 #include <math.h>
@@ -7,7 +8,12 @@
 namespace ppll {
 
 namespace {
-typedef __attribute__((ext_vector_type(16))) float f32x16;
+using pipe::barrier;
+using pipe::f32x16;
+using pipe::lds_char;
+using pipe::u32x2;
+using pipe::u32x4;
+using pipe::wait_vm;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 
@@ -93,7 +99,7 @@ __global__ __launch_bounds__(256) void squares_kernel(OrthoPlan p, Source s, cha
   if (threadIdx.x == 0) ((double*)(ws + p.partials))[g.first_piece + at.matrix * g.pieces() + id] = sums[0];
 }
 
-// Y = u / |u| and its transpose, in tiles of 64 x 64.
+// Y = u / |u|, in tiles of 64 x 64.
 __global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, char* ws) {
   int id = blockIdx.x;
   const Place at = place_of(p, id, [](const OrthoGroup& g) { return (g.mp / 64) * (g.np / 64); });
@@ -121,8 +127,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, c
   }
   __syncthreads();
   const int64_t plane = g.plane_x();
-  _Float16* x = (_Float16*)(ws + g.x) + at.matrix * 2 * plane;
-  _Float16* xt = (_Float16*)(ws + g.xt[0]) + at.matrix * 2 * plane;
+  _Float16* x = (_Float16*)(ws + g.x[0]) + at.matrix * 2 * plane;
   const int y = t / 4, q = t % 4 * 16;
   f16x8 h[2], l[2];
   for (int k = 0; k < 16; ++k) {
@@ -132,23 +137,77 @@ __global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, c
   }
   _Float16* to = x + (int64_t)(i0 + y) * g.np + j0 + q;
   for (int k = 0; k < 2; ++k) { *(f16x8*)(to + 8 * k) = h[k]; *(f16x8*)(to + plane + 8 * k) = l[k]; }
-  for (int k = 0; k < 16; ++k) {
-    _Float16 a, b;
-    split(tile[q + k][y], a, b);
-    h[k / 8][k % 8] = a; l[k / 8][k % 8] = b;
-  }
-  to = xt + (int64_t)(j0 + y) * g.mp + i0 + q;
-  for (int k = 0; k < 2; ++k) { *(f16x8*)(to + 8 * k) = h[k]; *(f16x8*)(to + plane + 8 * k) = l[k]; }
 }
 
-// C[i][j] = sum over k of P[i][k] Q[j][k]:
-//  GRAM   P = Q = X        A = C                        symmetric: tiles on and under the diagonal, each stored twice
-//  POLY   P = Q = A        B = b A + c C                likewise
-//  APPLY  P = B, Q = X^T   X = a X + C and X^T          (X^T in two buffers in turn: other tiles still read the old one)
+// ------------------------------------------------------------------ products
+// C[i][j] = sum over k of P[i][k] Q(k, j), a tile of TILE x TILE a workgroup of four waves:
+//  GRAM   P = X, Q = X'        A = C                    symmetric: tiles on and under the diagonal, each stored twice
+//  POLY   P = A, Q = A'        B = b A + c C            likewise
+//  APPLY  P = B, Q = X         X = a X + C              (X in two buffers in turn: other tiles still read the old one)
 //  LAST   the same, to where the result goes
+// A stage of the pipeline is KT k of the four planes (hi and lo of P and of Q), 8 KB each and each copied by one wave straight from memory to
+// LDS; there are two stages.  A wave multiplies 64 x 64: three products of 32 x 32 x 16 for each pair of fragments, 12 for eight fragments read.
+//  TILE 128: a wave has a quarter of the tile and all k.  TILE 64: it has all of the tile and a quarter of the k, and the four sums are added up
+//  at the end: fragments are read once for 12 products all the same, where quarters of 32 x 32 would read twice as much for each.
+// Layouts in LDS, as in gemm_pipe.h: k contiguous (P, and Q of GRAM and POLY): rows of KT k, their 16-byte granules permuted; k rows (X of APPLY):
+// rows of TILE columns whose 64-byte windows are permuted, for the transposing read.
+template <int TILE> struct Tile {
+  static constexpr int KT = TILE == 128 ? 32 : 64, PLANE = TILE * KT * 2, STAGE = 4 * PLANE, LDS = 2 * STAGE;
+  static constexpr int PITCH = TILE * 2;                     // of a k row
+  static constexpr int R32 = 32 * KT * 2;                    // 32 rows with k contiguous
+};
+struct Planes { u32x4 p[2], pl[2], q[2], ql[2]; };           // fragments: hi and lo of two 32-row tiles of P and of Q
+
+#define NS_MMA(C, Q, P) "v_mfma_f32_32x32x16_f16 %[" C "], %[" Q "], %[" P "], %[" C "]\n"
+#define NS_ACC [h00] "+v"(hh[0][0]), [h01] "+v"(hh[0][1]), [h10] "+v"(hh[1][0]), [h11] "+v"(hh[1][1]), [x00] "+v"(xx[0][0]), \
+               [x01] "+v"(xx[0][1]), [x10] "+v"(xx[1][0]), [x11] "+v"(xx[1][1])
+#define NS_CUR [p0] "v"(f.p[0]), [p1] "v"(f.p[1]), [a0] "v"(f.pl[0]), [a1] "v"(f.pl[1]), [q0] "v"(f.q[0]), [q1] "v"(f.q[1]), [b0] "v"(f.ql[0]), \
+               [b1] "v"(f.ql[1])
+#define NS_CROSS NS_MMA("x00", "b0", "p0") NS_MMA("x01", "b0", "p1") NS_MMA("x10", "b1", "p0") NS_MMA("x11", "b1", "p1") \
+                 NS_MMA("x00", "q0", "a0") NS_MMA("x01", "q0", "a1") NS_MMA("x10", "q1", "a0") NS_MMA("x11", "q1", "a1")
+// The 12 products of the fragments at hand (into hh: hi hi, into xx the cross terms: small terms summed apart keep their digits, error of
+// 1536 x 6144 1.8e-6 instead of 3.2e-6), and under them the reads of the next ones, at rp and rq, which have arrived when the block ends.  One
+// assembly block, as in gemm_pipe.h: the compiler would wait for all copies into LDS before a read that it knows of.
+template <int TILE, bool TR>
+__device__ __forceinline__ void k_step(f32x16 (&hh)[2][2], f32x16 (&xx)[2][2], const Planes& f, Planes& n, int rp, int rq) {
+  using S = Tile<TILE>;
+  if constexpr (!TR) {
+    asm volatile("s_nop 1\n" NS_MMA("h00", "q0", "p0") "ds_read_b128 %[s0], %[rp]\n ds_read_b128 %[s1], %[rp] offset:%[r1]\n"
+                 NS_MMA("h01", "q0", "p1") "ds_read_b128 %[t0], %[rq]\n ds_read_b128 %[t1], %[rq] offset:%[r1]\n"
+                 NS_MMA("h10", "q1", "p0") "ds_read_b128 %[u0], %[rq] offset:%[l0]\n ds_read_b128 %[u1], %[rq] offset:%[l1]\n"
+                 NS_MMA("h11", "q1", "p1") "ds_read_b128 %[v0], %[rp] offset:%[l0]\n ds_read_b128 %[v1], %[rp] offset:%[l1]\n"
+                 NS_CROSS "s_waitcnt lgkmcnt(0)"
+                 : NS_ACC, [s0] "=&v"(n.p[0]), [s1] "=&v"(n.p[1]), [v0] "=&v"(n.pl[0]), [v1] "=&v"(n.pl[1]), [t0] "=&v"(n.q[0]),
+                   [t1] "=&v"(n.q[1]), [u0] "=&v"(n.ql[0]), [u1] "=&v"(n.ql[1])
+                 : NS_CUR, [rp] "v"(rp), [rq] "v"(rq), [r1] "n"(S::R32), [l0] "n"(S::PLANE), [l1] "n"(S::PLANE + S::R32)
+                 : "memory");
+  } else {
+    u32x2 t[2][2], u[2][2];
+    asm volatile("s_nop 1\n" NS_MMA("h00", "q0", "p0") "ds_read_b128 %[s0], %[rp]\n ds_read_b128 %[s1], %[rp] offset:%[r1]\n"
+                 "ds_read_b64_tr_b16 %[t00], %[rq]\n ds_read_b64_tr_b16 %[t01], %[rq] offset:%[f]\n"
+                 NS_MMA("h01", "q0", "p1") "ds_read_b64_tr_b16 %[t10], %[rx]\n ds_read_b64_tr_b16 %[t11], %[rx] offset:%[f]\n"
+                 "ds_read_b64_tr_b16 %[u00], %[rq] offset:%[l0]\n ds_read_b64_tr_b16 %[u01], %[rq] offset:%[lf]\n"
+                 NS_MMA("h10", "q1", "p0") "ds_read_b64_tr_b16 %[u10], %[rx] offset:%[l0]\n ds_read_b64_tr_b16 %[u11], %[rx] offset:%[lf]\n"
+                 NS_MMA("h11", "q1", "p1") "ds_read_b128 %[v0], %[rp] offset:%[l0]\n ds_read_b128 %[v1], %[rp] offset:%[l1]\n"
+                 NS_CROSS "s_waitcnt lgkmcnt(0)"
+                 : NS_ACC, [s0] "=&v"(n.p[0]), [s1] "=&v"(n.p[1]), [v0] "=&v"(n.pl[0]), [v1] "=&v"(n.pl[1]), [t00] "=&v"(t[0][0]),
+                   [t01] "=&v"(t[0][1]), [t10] "=&v"(t[1][0]), [t11] "=&v"(t[1][1]), [u00] "=&v"(u[0][0]), [u01] "=&v"(u[0][1]),
+                   [u10] "=&v"(u[1][0]), [u11] "=&v"(u[1][1])
+                 : NS_CUR, [rp] "v"(rp), [rq] "v"(rq), [rx] "v"(rq ^ 64), [r1] "n"(S::R32), [l0] "n"(S::PLANE), [l1] "n"(S::PLANE + S::R32),
+                   [f] "n"(4 * S::PITCH), [lf] "n"(S::PLANE + 4 * S::PITCH)
+                 : "memory");
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      n.q[j] = (u32x4){t[j][0].x, t[j][0].y, t[j][1].x, t[j][1].y};
+      n.ql[j] = (u32x4){u[j][0].x, u[j][0].y, u[j][1].x, u[j][1].y};
+    }
+  }
+}
+
 template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_kernel(OrthoPlan p, Target t, char* ws, int step) {
-  constexpr int BK = 32, IM = TILE / 64, OPERAND = TILE * BK * 2;      // bytes of a plane's rows
-  __shared__ __align__(16) char lds[4 * OPERAND];
+  using S = Tile<TILE>;
+  constexpr bool TR = MODE >= APPLY;
+  extern __shared__ __align__(16) char stages[];
   int id = blockIdx.x;
   const Place at = place_of(p, id, [](const OrthoGroup& g) {
     const int a = g.mp / TILE;
@@ -167,98 +226,200 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
   }
   const int64_t px = g.plane_x(), pa = g.plane_a();
   const int from = step & 1;
-  const Shrink shrink = shrink_of(((const float*)(ws + p.shrink))[g.first + at.matrix], step);
-  const float poly_b = NS_B * shrink.now * shrink.now, poly_c = NS_C * shrink.now * shrink.now * shrink.now * shrink.now;
-  _Float16* X = (_Float16*)(ws + g.x) + at.matrix * 2 * px;
-  _Float16* XT = (_Float16*)(ws + g.xt[from]) + at.matrix * 2 * px;
-  _Float16* XN = (_Float16*)(ws + g.xt[from ^ 1]) + at.matrix * 2 * px;
+  _Float16* X = (_Float16*)(ws + g.x[from]) + at.matrix * 2 * px;
   _Float16* A = (_Float16*)(ws + g.a) + at.matrix * 2 * pa;
   _Float16* B = (_Float16*)(ws + g.b) + at.matrix * 2 * pa;
-  const _Float16* P = MODE == GRAM ? X : MODE == POLY ? A : B;
-  const _Float16* Q = MODE == GRAM ? X : MODE == POLY ? A : XT;
-  const int64_t plane_p = MODE == GRAM ? px : pa, plane_q = MODE == POLY ? pa : px;
-  const int K = MODE == GRAM ? g.np : g.mp;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wi = wave >> 1, wj = wave & 1;
-  f32x16 acc[IM][IM] = {}, cross[IM][IM] = {};
-  // rows of 32 k, 64 bytes; the 16-byte granule q of row r sits at q ^ (r / 4 % 4)
-  for (int k0 = 0; k0 < K; k0 += BK) {
-    __syncthreads();
-    for (int c = tid; c < TILE * 4; c += 256) {
-      const int r = c >> 2, q = c & 3, to = r * 64 + ((q ^ (r >> 2 & 3)) << 4);
-      const int64_t fp = (int64_t)(bi * TILE + r) * K + k0 + q * 8, fq = (int64_t)(bj * TILE + r) * K + k0 + q * 8;
-      *(f16x8*)(lds + to) = *(const f16x8*)(P + fp);
-      *(f16x8*)(lds + OPERAND + to) = *(const f16x8*)(P + plane_p + fp);
-      *(f16x8*)(lds + 2 * OPERAND + to) = *(const f16x8*)(Q + fq);
-      *(f16x8*)(lds + 3 * OPERAND + to) = *(const f16x8*)(Q + plane_q + fq);
+  const int K = MODE == GRAM ? g.np : g.mp, nk = K / S::KT;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  // ---- what this wave copies: plane `wave` of P hi, P lo, Q hi, Q lo
+  const bool is_q = wave >= 2;
+  const int64_t plane = (MODE == GRAM || (TR && is_q)) ? px : pa;
+  const _Float16* src = (MODE == GRAM ? X : MODE == POLY ? A : is_q ? X : B) + (wave & 1 ? plane : 0);
+  const __amdgpu_buffer_rsrc_t rs = pipe::make_rsrc(src, (uint32_t)(plane * 2));
+  lds_char* const lds = (lds_char*)stages;
+  int off[2], every, step_k;         // bytes: this lane's of even and odd copies at stage 0, from copy to copy, from stage to stage
+  if (TR && is_q) {
+    const int ld2 = g.np * 2;
+    const int kr = TILE == 128 ? lane >> 4 : lane >> 3, slot = TILE == 128 ? lane & 15 : lane & 7;
+    const int win = (slot >> 2) ^ (TILE == 128 ? kr & 3 : kr >> 1 & 1);
+    off[0] = off[1] = kr * ld2 + (bj * TILE + (win * 4 + (slot & 3)) * 8) * 2;
+    every = (TILE == 128 ? 4 : 8) * ld2;
+    step_k = S::KT * ld2;
+  } else {
+    const int ld2 = K * 2, row0 = (is_q ? bj : bi) * TILE;
+    if (TILE == 128) {
+      off[0] = off[1] = (row0 + (lane >> 2)) * ld2 + ((lane & 3) ^ (lane >> 4 & 3)) * 16;
+      every = 16 * ld2;
+    } else {
+      for (int odd = 0; odd < 2; ++odd) off[odd] = (row0 + (lane >> 3)) * ld2 + ((lane & 7) ^ ((4 * odd + (lane >> 4)) & 7)) * 16;
+      every = 8 * ld2;
     }
-    __syncthreads();
-    for (int kk = 0; kk < 2; ++kk) {
-      f16x8 ph[IM], pl[IM], qh[IM], ql[IM];
-      for (int i = 0; i < IM; ++i) {
-        const int q = kk * 2 + (lane >> 5), rp = (wi * IM + i) * 32 + (lane & 31), rq = (wj * IM + i) * 32 + (lane & 31);
-        const int fp = rp * 64 + ((q ^ (rp >> 2 & 3)) << 4), fq = rq * 64 + ((q ^ (rq >> 2 & 3)) << 4);
-        ph[i] = *(const f16x8*)(lds + fp); pl[i] = *(const f16x8*)(lds + OPERAND + fp);
-        qh[i] = *(const f16x8*)(lds + 2 * OPERAND + fq); ql[i] = *(const f16x8*)(lds + 3 * OPERAND + fq);
-      }
-      for (int i = 0; i < IM; ++i)
-        for (int j = 0; j < IM; ++j) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[j], acc[i][j], 0, 0, 0);
-          cross[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], cross[i][j], 0, 0, 0);
-          cross[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], cross[i][j], 0, 0, 0);
-        }
+    step_k = S::KT * 2;
+  }
+  auto issue = [&](int i) {
+    if (i >= nk) return;
+    lds_char* to = lds + (i & 1) * S::STAGE + wave * S::PLANE;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) pipe::load_to_lds(rs, to + c * 1024, off[c & 1] + c * every + i * step_k);
+  };
+
+  // ---- where this wave reads its fragments, in stage 0
+  const int base = (int)(uintptr_t)lds, wi = TILE == 128 ? wave >> 1 : 0, wj = TILE == 128 ? wave & 1 : 0, kk = TILE == 128 ? 0 : wave;
+  auto rows_at = [&](int region, int row0) {       // k contiguous
+    const int r = lane & 31;
+    if (TILE == 128) return region + (row0 + r) * 64 + (((lane >> 5) ^ (r >> 2 & 3)) << 4);
+    return region + (row0 + r) * 128 + (((2 * kk + (lane >> 5)) ^ (r >> 1 & 7)) << 4);
+  };
+  const int rp = rows_at(base, wi * 64);
+  int rq;
+  if (TR) {
+    const int kr = 8 * (lane >> 5) + ((lane & 15) >> 2), perm = TILE == 128 ? kr & 3 : kr >> 1 & 1;
+    rq = base + 2 * S::PLANE + (kr + 16 * kk) * S::PITCH + (((wj * 2) ^ perm) << 6) + (16 * (lane >> 4 & 1) + 4 * (lane & 3)) * 2;
+  } else {
+    rq = rows_at(base + 2 * S::PLANE, wj * 64);
+  }
+  constexpr int NEXT_Q = TR ? 16 * S::PITCH : 0;    // the second k step of a stage (TILE 128)
+
+  // ---- main loop: a stage is filled again from the moment that everyone has read it
+  f32x16 hh[2][2] = {}, xx[2][2] = {};
+  Planes f0, f1;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) f1.p[i] = f1.pl[i] = f1.q[i] = f1.ql[i] = (u32x4){0, 0, 0, 0};
+  issue(0);
+  issue(1);
+  if (nk > 1) wait_vm<8>();
+  else wait_vm<0>();
+  barrier();
+  k_step<TILE, TR>(hh, xx, f1, f0, rp, rq);         // the first fragments: products with zeros under the reads
+  if constexpr (TILE == 128) {
+    for (int i = 0; i < nk; ++i) {
+      const int st = (i & 1) * S::STAGE, nx = S::STAGE - st;
+      k_step<TILE, TR>(hh, xx, f0, f1, TILE == 128 ? (rp ^ 32) + st : 0, (TR ? rq + NEXT_Q : rq ^ 32) + st);
+      wait_vm<0>();         // this wave's part of stage i + 1 is in LDS
+      barrier();            // and everyone's; nobody reads stage i any more
+      issue(i + 2);
+      k_step<TILE, TR>(hh, xx, f1, f0, rp + nx, rq + nx);
+    }
+  } else {
+    for (int i = 0; i < nk; i += 2) {
+      wait_vm<0>();
+      barrier();
+      issue(i + 2);
+      k_step<TILE, TR>(hh, xx, f0, f1, rp + S::STAGE, rq + S::STAGE);
+      if (i + 1 >= nk) break;
+      wait_vm<0>();
+      barrier();
+      issue(i + 3);
+      k_step<TILE, TR>(hh, xx, f1, f0, rp, rq);
     }
   }
-  // lane: column j, rows 8 (r / 4) + 4 (lane / 32) + r % 4 of a 32 x 32 tile
-  for (int ii = 0; ii < IM; ++ii)
-    for (int jj = 0; jj < IM; ++jj)
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const int i = bi * TILE + (wi * IM + ii) * 32 + r4 * 8 + 4 * (lane >> 5), j = bj * TILE + (wj * IM + jj) * 32 + (lane & 31);
-        float v[4];
-        for (int k = 0; k < 4; ++k) v[k] = (acc[ii][jj][r4 * 4 + k] + cross[ii][jj][r4 * 4 + k]) * UNSCALE;
-        if (MODE != GRAM) {
-          // A is symmetric, X^T holds X: four neighbours of a column are four of a row there
-          const _Float16* add = (MODE == POLY ? A : XT) + (int64_t)j * g.mp + i;
-          const f16x4 h = *(const f16x4*)add, l = *(const f16x4*)(add + (MODE == POLY ? pa : px));
-          for (int k = 0; k < 4; ++k) {
-            const float old = (float)h[k] + (float)l[k];
-            v[k] = MODE == POLY ? fmaf(poly_b, old, poly_c * v[k]) : fmaf(NS_A, old, v[k]) * shrink.ratio;
-          }
-        }
-        if (MODE == LAST) {
-          const float scale = UNSCALE * shrink.next * (t.out ? 1.f : 0.2f * t.lr * sqrtf((float)g.n));
-          for (int k = 0; k < 4; ++k) {
-            if (i + k >= g.m || j >= g.n) continue;
-            const int64_t e = g.tall ? element(g, at.matrix, j, i + k) : element(g, at.matrix, i + k, j);
-            if (t.out) {
-              st_f(t.out, (size_t)e, v[k] * scale, t.dt);
-            } else {
-              const float w = t.p[e] * t.decay - v[k] * scale;
-              t.p[e] = w;
-              if (t.shadow) t.shadow[e] = f32_to_bf16(w);
-            }
-          }
-          continue;
-        }
-        f16x4 h, l;
+  asm volatile("s_nop 15\n s_nop 3" ::: "memory");    // the last products are through before a vector instruction reads the accumulators
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) asm volatile("" : "+v"(hh[j][i]), "+v"(xx[j][i]));
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) hh[j][i] += xx[j][i];
+
+  const Shrink shrink = shrink_of(((const float*)(ws + p.shrink))[g.first + at.matrix], step);
+  const float poly_b = NS_B * shrink.now * shrink.now, poly_c = NS_C * shrink.now * shrink.now * shrink.now * shrink.now;
+  // a 32 x 32 tile: lane l holds row l % 32, columns 8 q + 4 (l / 32) + e in element 4 q + e
+  auto finish = [&](const f32x16& acc, int i0, int j0) {
+    const int i = i0 + (lane & 31);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int j = j0 + 8 * q + 4 * (lane >> 5);
+      float v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = acc[q * 4 + k] * UNSCALE;
+      if (MODE != GRAM) {
+        const _Float16* add = MODE == POLY ? A + (int64_t)i * g.mp + j : X + (int64_t)i * g.np + j;
+        const f16x4 h = *(const f16x4*)add, l = *(const f16x4*)(add + (MODE == POLY ? pa : px));
+#pragma unroll
         for (int k = 0; k < 4; ++k) {
-          _Float16 a, b;
-          split(v[k], a, b);
-          h[k] = a; l[k] = b;
-        }
-        _Float16* D = MODE == GRAM ? A : MODE == POLY ? B : X;
-        _Float16* DT = MODE == GRAM ? A : MODE == POLY ? B : XN;
-        const int64_t plane = MODE <= POLY ? pa : px;
-        const int ld = MODE <= POLY ? g.mp : g.np;
-        for (int k = 0; k < 4; ++k) {
-          D[(int64_t)(i + k) * ld + j] = h[k];
-          D[plane + (int64_t)(i + k) * ld + j] = l[k];
-        }
-        if (MODE == APPLY || bi != bj) {
-          *(f16x4*)(DT + (int64_t)j * g.mp + i) = h;
-          *(f16x4*)(DT + plane + (int64_t)j * g.mp + i) = l;
+          const float old = (float)h[k] + (float)l[k];
+          v[k] = MODE == POLY ? fmaf(poly_b, old, poly_c * v[k]) : fmaf(NS_A, old, v[k]) * shrink.ratio;
         }
       }
+      if (MODE == LAST) {
+        const float scale = UNSCALE * shrink.next * (t.out ? 1.f : 0.2f * t.lr * sqrtf((float)g.n));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (i >= g.m || j + k >= g.n) continue;
+          const int64_t e = g.tall ? element(g, at.matrix, j + k, i) : element(g, at.matrix, i, j + k);
+          if (t.out) {
+            st_f(t.out, (size_t)e, v[k] * scale, t.dt);
+          } else {
+            const float w = t.p[e] * t.decay - v[k] * scale;
+            t.p[e] = w;
+            if (t.shadow) t.shadow[e] = f32_to_bf16(w);
+          }
+        }
+        continue;
+      }
+      f16x4 h, l;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        _Float16 a, b;
+        split(v[k], a, b);
+        h[k] = a; l[k] = b;
+      }
+      if (MODE == APPLY) {
+        _Float16* to = (_Float16*)(ws + g.x[from ^ 1]) + at.matrix * 2 * px + (int64_t)i * g.np + j;
+        *(f16x4*)to = h;
+        *(f16x4*)(to + px) = l;
+      } else {
+        _Float16* D = MODE == GRAM ? A : B;
+        *(f16x4*)(D + (int64_t)i * g.mp + j) = h;
+        *(f16x4*)(D + pa + (int64_t)i * g.mp + j) = l;
+        if (bi != bj) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            D[(int64_t)(j + k) * g.mp + i] = h[k];
+            D[pa + (int64_t)(j + k) * g.mp + i] = l[k];
+          }
+        }
+      }
+    }
+  };
+  if constexpr (TILE == 128) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) finish(hh[j][i], bi * 128 + wi * 64 + i * 32, bj * 128 + wj * 64 + j * 32);
+  } else {
+    // the four waves' sums: each has the 32 x 32 tile of its number
+    float4* sums = (float4*)stages;                   // [wave][tile][q][lane]
+    barrier();                                        // nobody reads a stage any more
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x16& v = hh[k >> 1][k & 1];
+        sums[((wave * 4 + k) * 4 + q) * 64 + lane] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+      }
+    __syncthreads();
+    f32x16 acc;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float4 a = sums[(wave * 4 + q) * 64 + lane];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) {
+        const float4 b = sums[((w * 4 + wave) * 4 + q) * 64 + lane];
+        a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+      }
+      acc[4 * q] = a.x; acc[4 * q + 1] = a.y; acc[4 * q + 2] = a.z; acc[4 * q + 3] = a.w;
+    }
+    finish(acc, bi * 64 + (wave & 1) * 32, bj * 64 + (wave >> 1) * 32);
+  }
 }
+#undef NS_MMA
+#undef NS_ACC
+#undef NS_CUR
+#undef NS_CROSS
 
 int64_t tiles(const OrthoPlan& p, int mode) {
   int64_t n = 0;
@@ -270,8 +431,8 @@ int64_t tiles(const OrthoPlan& p, int mode) {
 }
 template <int MODE> int launch_product(hipStream_t s, const OrthoPlan& p, const Target& t, char* ws, int step) {
   const dim3 grid((unsigned)tiles(p, MODE));
-  if (p.tile == 128) hipLaunchKernelGGL((product_kernel<128, MODE>), grid, dim3(256), 0, s, p, t, ws, step);
-  else hipLaunchKernelGGL((product_kernel<64, MODE>), grid, dim3(256), 0, s, p, t, ws, step);
+  if (p.tile == 128) hipLaunchKernelGGL((product_kernel<128, MODE>), grid, dim3(256), Tile<128>::LDS, s, p, t, ws, step);
+  else hipLaunchKernelGGL((product_kernel<64, MODE>), grid, dim3(256), Tile<64>::LDS, s, p, t, ws, step);
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }

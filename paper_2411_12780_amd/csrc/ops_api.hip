@@ -82,9 +82,8 @@ int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* pla
     matrices += o.count; pieces += (int64_t)o.count * o.pieces();
     squares += (int64_t)o.count * (o.mp / 64) * (o.np / 64);
     tiles += (int64_t)o.count * (o.mp / plan->tile) * (o.np / plan->tile);
-    o.x = take(o.count * 2 * 2 * o.plane_x());
-    o.xt[0] = take(o.count * 2 * 2 * o.plane_x());
-    o.xt[1] = take(o.count * 2 * 2 * o.plane_x());
+    o.x[0] = take(o.count * 2 * 2 * o.plane_x());
+    o.x[1] = take(o.count * 2 * 2 * o.plane_x());
     o.a = take(o.count * 2 * 2 * o.plane_a());
     o.b = take(o.count * 2 * 2 * o.plane_a());
     if (pieces > MOST_ITEMS || squares > MOST_ITEMS || tiles > MOST_ITEMS) { set_error("too many matrices for one call"); return PPLL_ERR_SHAPE; }

@@ -21,7 +21,7 @@ struct OrthoGroup {
   int32_t m, n, mp, np, tall;
   int32_t first;                       // place of the group's first matrix among all of the call
   int32_t first_piece;                 // of its pieces among those of all groups
-  int64_t x, xt[2], a, b;
+  int64_t x[2], a, b;
   __host__ __device__ int64_t plane_x() const { return (int64_t)mp * np; }      // elements
   __host__ __device__ int64_t plane_a() const { return (int64_t)mp * mp; }
   __host__ __device__ int pieces() const { return ((rows + NORM_ROWS - 1) / NORM_ROWS) * ((cols + NORM_COLS - 1) / NORM_COLS); }
