@@ -37,7 +37,7 @@ __device__ __forceinline__ Shrink shrink_of(float t0, int step) {
   return {t, next, t0 > 0.f ? t / next : 1.f};
 }
 
-enum { GRAM = 0, POLY = 1, APPLY = 2, LAST = 3 };
+constexpr int GRAM = ORTHO_GRAM, POLY = ORTHO_POLY, APPLY = ORTHO_APPLY, LAST = ORTHO_APPLY + 1;
 
 // What a call works on.  in: blob of the matrices (orthogonalize), or null: u from g and the momentum (Muon step)
 struct Source { const void* in; int dt; const float* g; float* m; float momentum; int nesterov; };
@@ -82,13 +82,27 @@ __global__ __launch_bounds__(256) void squares_kernel(OrthoPlan p, Source s, cha
   const OrthoGroup& g = p.g[at.group];
   const int across = (g.cols + NORM_COLS - 1) / NORM_COLS, r0 = id / across * NORM_ROWS, c = id % across * NORM_COLS + threadIdx.x;
   double sum = 0;
-  if (c < g.cols)
-    for (int r = r0; r < min(r0 + NORM_ROWS, g.rows); ++r) {
-      const int64_t e = element(g, at.matrix, r, c);
-      if (!s.in) s.m[e] = fmaf(s.momentum, s.m[e], s.g[e]);
-      const double u = read_u(s, e);
-      sum += u * u;
+  const int64_t first = element(g, at.matrix, r0, c);
+  const int rows = c < g.cols ? min(NORM_ROWS, g.rows - r0) : 0;
+  for (int r = 0; r < rows; r += 8) {        // eight rows on their way at a time
+    float u[8], m[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int64_t e = first + (int64_t)(r + k) * g.ld;
+      const bool on = r + k < rows;
+      u[k] = !on ? 0.f : s.in ? ld_f(s.in, (size_t)e, s.dt) : s.g[e];
+      m[k] = on && !s.in ? s.m[e] : 0.f;
     }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (!s.in) {
+        m[k] = fmaf(s.momentum, m[k], u[k]);
+        if (r + k < rows) s.m[first + (int64_t)(r + k) * g.ld] = m[k];
+        u[k] = s.nesterov ? fmaf(s.momentum, m[k], u[k]) : m[k];
+      }
+      sum += (double)u[k] * u[k];
+    }
+  }
   __shared__ double sums[256];
   sums[threadIdx.x] = sum;
   __syncthreads();
@@ -204,15 +218,14 @@ __device__ __forceinline__ void k_step(f32x16 (&hh)[2][2], f32x16 (&xx)[2][2], c
   }
 }
 
-template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_kernel(OrthoPlan p, Target t, char* ws, int step) {
+template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_kernel(OrthoPlan p, XcdShares shares, Target t, char* ws, int step) {
   using S = Tile<TILE>;
   constexpr bool TR = MODE >= APPLY;
   extern __shared__ __align__(16) char stages[];
-  int id = blockIdx.x;
-  const Place at = place_of(p, id, [](const OrthoGroup& g) {
-    const int a = g.mp / TILE;
-    return MODE <= POLY ? a * (a + 1) / 2 : a * (g.np / TILE);
-  });
+  const int xcd = blockIdx.x & 7;
+  int id = shares.first[xcd] + (int)(blockIdx.x >> 3);
+  if (id >= shares.first[xcd + 1]) return;
+  const Place at = place_of(p, id, [](const OrthoGroup& g) { return tiles_of_matrix(g, TILE, MODE); });
   const OrthoGroup& g = p.g[at.group];
   int bi, bj;
   if (MODE <= POLY) {
@@ -221,8 +234,8 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
     while (bi * (bi + 1) / 2 > id) --bi;
     bj = id - bi * (bi + 1) / 2;
   } else {
-    const int across = g.np / TILE;
-    bi = id / across; bj = id % across;
+    const int down = (g.mp + TILE - 1) / TILE;         // tiles that read the same columns of X follow one another
+    bj = id / down; bi = id - bj * down;
   }
   const int64_t px = g.plane_x(), pa = g.plane_a();
   const int from = step & 1;
@@ -324,96 +337,158 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
 #pragma unroll
     for (int i = 0; i < 2; ++i) hh[j][i] += xx[j][i];
 
+  // ---- epilogue: through LDS, so that a wave reads and writes whole 16-byte pieces of whole cache lines
   const Shrink shrink = shrink_of(((const float*)(ws + p.shrink))[g.first + at.matrix], step);
   const float poly_b = NS_B * shrink.now * shrink.now, poly_c = NS_C * shrink.now * shrink.now * shrink.now * shrink.now;
-  // a 32 x 32 tile: lane l holds row l % 32, columns 8 q + 4 (l / 32) + e in element 4 q + e
-  auto finish = [&](const f32x16& acc, int i0, int j0) {
-    const int i = i0 + (lane & 31);
+  constexpr int PITCH = 68;                             // floats of a row of 64 and room: rows 4 banks apart
+  // rows r0 .. of `sums`, which holds the products of rows i0 .. and columns j0 .. j0 + 63: finished and stored; `again`: the finished values
+  // go back to `sums`, for the mirrored tile
+  auto store_rows = [&](float* sums, int rows, int i0, int j0, bool again) {
+    const int seg = (lane & 7) * 8;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int j = j0 + 8 * q + 4 * (lane >> 5);
-      float v[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = acc[q * 4 + k] * UNSCALE;
+    for (int r = lane >> 3; r < rows; r += 8) {
+      float* from_lds = sums + r * PITCH + seg;
+      const float4 lo4 = *(const float4*)from_lds, hi4 = *(const float4*)(from_lds + 4);
+      float v[8] = {lo4.x, lo4.y, lo4.z, lo4.w, hi4.x, hi4.y, hi4.z, hi4.w};
+      const int ld = MODE == APPLY ? g.np : g.mp;
+      const int64_t at_e = (int64_t)(i0 + r) * ld + j0 + seg, pl = MODE == APPLY ? px : pa;
       if (MODE != GRAM) {
-        const _Float16* add = MODE == POLY ? A + (int64_t)i * g.mp + j : X + (int64_t)i * g.np + j;
-        const f16x4 h = *(const f16x4*)add, l = *(const f16x4*)(add + (MODE == POLY ? pa : px));
+        const _Float16* add = (MODE == POLY ? A : X) + at_e;
+        const f16x8 h = *(const f16x8*)add, l = *(const f16x8*)(add + pl);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 8; ++k) {
           const float old = (float)h[k] + (float)l[k];
-          v[k] = MODE == POLY ? fmaf(poly_b, old, poly_c * v[k]) : fmaf(NS_A, old, v[k]) * shrink.ratio;
+          v[k] = MODE == POLY ? fmaf(poly_b, old, poly_c * (v[k] * UNSCALE)) : fmaf(NS_A, old, v[k] * UNSCALE) * shrink.ratio;
         }
-      }
-      if (MODE == LAST) {
-        const float scale = UNSCALE * shrink.next * (t.out ? 1.f : 0.2f * t.lr * sqrtf((float)g.n));
+      } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (i >= g.m || j + k >= g.n) continue;
-          const int64_t e = g.tall ? element(g, at.matrix, j + k, i) : element(g, at.matrix, i, j + k);
-          if (t.out) {
-            st_f(t.out, (size_t)e, v[k] * scale, t.dt);
-          } else {
-            const float w = t.p[e] * t.decay - v[k] * scale;
-            t.p[e] = w;
-            if (t.shadow) t.shadow[e] = f32_to_bf16(w);
-          }
-        }
-        continue;
+        for (int k = 0; k < 8; ++k) v[k] *= UNSCALE;
       }
-      f16x4 h, l;
+      if (again) {
+        *(float4*)from_lds = make_float4(v[0], v[1], v[2], v[3]);
+        *(float4*)(from_lds + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      }
+      f16x8 h, l;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < 8; ++k) {
         _Float16 a, b;
         split(v[k], a, b);
         h[k] = a; l[k] = b;
       }
-      if (MODE == APPLY) {
-        _Float16* to = (_Float16*)(ws + g.x[from ^ 1]) + at.matrix * 2 * px + (int64_t)i * g.np + j;
-        *(f16x4*)to = h;
-        *(f16x4*)(to + px) = l;
-      } else {
-        _Float16* D = MODE == GRAM ? A : B;
-        *(f16x4*)(D + (int64_t)i * g.mp + j) = h;
-        *(f16x4*)(D + pa + (int64_t)i * g.mp + j) = l;
-        if (bi != bj) {
+      _Float16* to = (MODE == GRAM ? A : MODE == POLY ? B : (_Float16*)(ws + g.x[from ^ 1]) + at.matrix * 2 * px) + at_e;
+      *(f16x8*)to = h;
+      *(f16x8*)(to + pl) = l;
+    }
+  };
+  // columns c0 .. c0 + cols - 1 of `rows` (a multiple of 8) finished rows, as rows of the mirrored tile
+  auto store_mirrored = [&](const float* sums, int rows, int i0, int c0, int cols, int j0) {
+    const int segs = rows / 8, seg = lane % segs * 8;
+    _Float16* D = MODE == GRAM ? A : B;
+    for (int c = c0 + lane / segs; c < c0 + cols; c += 64 / segs) {
+      f16x8 h, l;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            D[(int64_t)(j + k) * g.mp + i] = h[k];
-            D[pa + (int64_t)(j + k) * g.mp + i] = l[k];
-          }
+      for (int k = 0; k < 8; ++k) {
+        _Float16 a, b;
+        split(sums[(seg + k) * PITCH + c], a, b);
+        h[k] = a; l[k] = b;
+      }
+      _Float16* to = D + (int64_t)(j0 + c) * g.mp + i0 + seg;
+      *(f16x8*)to = h;
+      *(f16x8*)(to + pa) = l;
+    }
+  };
+  // the result, from the same place; the caller's rows are columns of `sums` where the matrix is tall.  A wave takes 64 elements at a time
+  // that lie side by side (tall: `rows` of them), whatever the alignment, and has eight times as many on their way.
+  auto store_result = [&](const float* sums, int r0, int rows, int i0, int j0) {
+    const float scale = UNSCALE * shrink.next * (t.out ? 1.f : 0.2f * t.lr * sqrtf((float)g.n));
+    for (int k0 = 0; k0 < rows; k0 += 8) {
+      float v[8], w[8];
+      int64_t e[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int r = r0 + (g.tall ? lane % rows : k0 + k), c = g.tall ? lane / rows + (k0 + k) * (64 / rows) : lane, i = i0 + r, j = j0 + c;
+        e[k] = i >= g.m || j >= g.n ? -1 : g.tall ? element(g, at.matrix, j, i) : element(g, at.matrix, i, j);
+        const _Float16* add = X + (int64_t)i * g.np + j;
+        w[k] = !t.out && e[k] >= 0 ? t.p[e[k]] : 0.f;
+        v[k] = fmaf(NS_A, (float)add[0] + (float)add[px], sums[r * PITCH + c] * UNSCALE) * shrink.ratio * scale;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (e[k] < 0) continue;
+        if (t.out) {
+          st_f(t.out, (size_t)e[k], v[k], t.dt);
+        } else {
+          w[k] = w[k] * t.decay - v[k];
+          t.p[e[k]] = w[k];
+          if (t.shadow) t.shadow[e[k]] = f32_to_bf16(w[k]);
         }
       }
     }
   };
+  // a 32 x 32 tile of sums: lane l holds row l % 32, columns 8 q + 4 (l / 32) + e in element 4 q + e
+  auto put = [&](float* sums, const f32x16& acc, int r0, int c0) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *(float4*)(sums + (r0 + (lane & 31)) * PITCH + c0 + 8 * q + 4 * (lane >> 5)) =
+          make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+  };
+  barrier();                                            // nobody reads a stage any more
   if constexpr (TILE == 128) {
+    // 32 rows at a time, in a part of LDS of the wave's own; what lies past the padded size (a multiple of 64) is not stored
+    float* sums = (float*)stages + wave * 32 * PITCH;
+    const int i0 = bi * 128 + wi * 64, j0 = bj * 128 + wj * 64;
+    if (i0 >= g.mp || j0 >= (MODE <= POLY ? g.mp : g.np)) return;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) finish(hh[j][i], bi * 128 + wi * 64 + i * 32, bj * 128 + wj * 64 + j * 32);
+    for (int i = 0; i < 2; ++i) {
+      wave_sync();
+      put(sums, hh[0][i], 0, 0);
+      put(sums, hh[1][i], 0, 32);
+      wave_sync();
+      if (MODE == LAST) {
+        store_result(sums, 0, 32, i0 + 32 * i, j0);
+      } else {
+        store_rows(sums, 32, i0 + 32 * i, j0, MODE <= POLY && bi != bj);
+        if (MODE <= POLY && bi != bj) {
+          wave_sync();
+          store_mirrored(sums, 32, i0 + 32 * i, 0, 64, j0);
+        }
+      }
+    }
   } else {
-    // the four waves' sums: each has the 32 x 32 tile of its number
-    float4* sums = (float4*)stages;                   // [wave][tile][q][lane]
-    barrier();                                        // nobody reads a stage any more
+    // the four waves' sums: each adds up the 32 x 32 tile of its number and finishes 16 rows of the whole
+    float4* quarters = (float4*)stages;                 // [wave][tile][q][lane]
+    float* sums = (float*)stages;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const f32x16& v = hh[k >> 1][k & 1];
-        sums[((wave * 4 + k) * 4 + q) * 64 + lane] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        quarters[((wave * 4 + k) * 4 + q) * 64 + lane] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
       }
     __syncthreads();
     f32x16 acc;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      float4 a = sums[(wave * 4 + q) * 64 + lane];
+      float4 a = quarters[(wave * 4 + q) * 64 + lane];
 #pragma unroll
       for (int w = 1; w < 4; ++w) {
-        const float4 b = sums[((w * 4 + wave) * 4 + q) * 64 + lane];
+        const float4 b = quarters[((w * 4 + wave) * 4 + q) * 64 + lane];
         a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
       }
       acc[4 * q] = a.x; acc[4 * q + 1] = a.y; acc[4 * q + 2] = a.z; acc[4 * q + 3] = a.w;
     }
-    finish(acc, bi * 64 + (wave & 1) * 32, bj * 64 + (wave >> 1) * 32);
+    __syncthreads();
+    put(sums, acc, (wave & 1) * 32, (wave >> 1) * 32);
+    __syncthreads();
+    if (MODE == LAST) {
+      store_result(sums, wave * 16, 16, bi * 64, bj * 64);
+    } else {
+      store_rows(sums + wave * 16 * PITCH, 16, bi * 64 + wave * 16, bj * 64, MODE <= POLY && bi != bj);
+      if (MODE <= POLY && bi != bj) {
+        __syncthreads();
+        store_mirrored(sums, 64, bi * 64, wave * 16, 16, bj * 64);
+      }
+    }
   }
 }
 #undef NS_MMA
@@ -421,18 +496,14 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
 #undef NS_CUR
 #undef NS_CROSS
 
-int64_t tiles(const OrthoPlan& p, int mode) {
-  int64_t n = 0;
-  for (int k = 0; k < p.n; ++k) {
-    const int64_t a = p.g[k].mp / p.tile, b = p.g[k].np / p.tile;
-    n += p.g[k].count * (mode <= POLY ? a * (a + 1) / 2 : a * b);
-  }
-  return n;
-}
 template <int MODE> int launch_product(hipStream_t s, const OrthoPlan& p, const Target& t, char* ws, int step) {
-  const dim3 grid((unsigned)tiles(p, MODE));
-  if (p.tile == 128) hipLaunchKernelGGL((product_kernel<128, MODE>), grid, dim3(256), Tile<128>::LDS, s, p, t, ws, step);
-  else hipLaunchKernelGGL((product_kernel<64, MODE>), grid, dim3(256), Tile<64>::LDS, s, p, t, ws, step);
+  const int phase = MODE < APPLY ? MODE : APPLY, tile = p.tile[phase];
+  const XcdShares& shares = p.shares[phase];
+  int longest = 0;
+  for (int x = 0; x < 8; ++x) longest = shares.first[x + 1] - shares.first[x] > longest ? shares.first[x + 1] - shares.first[x] : longest;
+  const dim3 grid(8 * (unsigned)longest);
+  if (tile == 128) hipLaunchKernelGGL((product_kernel<128, MODE>), grid, dim3(256), Tile<128>::LDS, s, p, shares, t, ws, step);
+  else hipLaunchKernelGGL((product_kernel<64, MODE>), grid, dim3(256), Tile<64>::LDS, s, p, shares, t, ws, step);
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }

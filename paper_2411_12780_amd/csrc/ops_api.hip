@@ -1,5 +1,6 @@
 // C entry points of the operators that work on a caller's own buffers (include/ppll.h): argument checks on the host, the layout of the
 // workspace, then the launches.
+#include <algorithm>
 #include <cmath>
 
 #include "common.h"
@@ -34,6 +35,40 @@ bool overlap(const Run& a, const Run& b) {
   }
   return false;
 }
+// Tiles of one of the products, and how the XCDs share them.
+// A unit gets through 32 k of a 128 x 128 tile in about 0.4 us and of a 64 x 64 one in 0.17; the larger ones are ahead where there are enough of
+// them for the units, or where one is no longer than all of the smaller ones' turns.
+void plan_product(OrthoPlan* p, int phase) {
+  double best = 0;
+  for (int tile : {128, 64}) {
+    double all = 0, longest = 0;
+    for (int k = 0; k < p->n; ++k) {
+      const OrthoGroup& o = p->g[k];
+      const double len = (phase == ORTHO_GRAM ? o.np : o.mp) * (tile == 128 ? 0.4 : 0.17);
+      all += (double)o.count * tiles_of_matrix(o, tile, phase) * len;
+      if (len > longest) longest = len;
+    }
+    const double time = std::max(all / 256, longest);
+    if (tile == 128 || time < best) { best = time; p->tile[phase] = tile; }
+  }
+  // shares of equal work, in whole tiles
+  const int tile = p->tile[phase];
+  double all = 0, before = 0;
+  int32_t tiles = 0, x = 0;
+  auto len = [&](const OrthoGroup& o) { return (double)(phase == ORTHO_GRAM ? o.np : o.mp); };
+  for (int k = 0; k < p->n; ++k) all += (double)p->g[k].count * tiles_of_matrix(p->g[k], tile, phase) * len(p->g[k]);
+  int32_t* first = p->shares[phase].first;
+  first[0] = 0;
+  for (int k = 0; k < p->n; ++k) {
+    const int32_t n = p->g[k].count * tiles_of_matrix(p->g[k], tile, phase);
+    const double one = len(p->g[k]);
+    // the boundaries that fall into this group
+    while (x < 7 && before + n * one >= all * (x + 1) / 8) first[++x] = tiles + (int32_t)std::min<double>(n, std::ceil((all * (x + 1) / 8 - before) / one));
+    before += n * one;
+    tiles += n;
+  }
+  while (x < 8) first[++x] = tiles;
+}
 int64_t pad(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 }  // namespace
@@ -43,7 +78,6 @@ int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* pla
   if (n_groups > 0 && !groups) { set_error("groups is null"); return PPLL_ERR_NULL; }
   *plan = OrthoPlan{};
   Run runs[ORTHO_GROUPS];
-  int64_t wide = 0;                                // tiles of 128 x 128 of the smallest product
   for (int k = 0; k < n_groups; ++k) {
     const ppll_matrix_group& g = groups[k];
     if (g.rows < 1 || g.cols < 1 || g.rows > ORTHO_SIDE || g.cols > ORTHO_SIDE) {
@@ -69,25 +103,23 @@ int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* pla
     o.rows = g.rows; o.cols = g.cols; o.count = g.count;
     o.tall = g.rows > g.cols;
     o.m = o.tall ? g.cols : g.rows; o.n = o.tall ? g.rows : g.cols;
-    const int64_t t = (o.m + 127) / 128;
-    wide += o.count * t * (t + 1) / 2;
+    o.mp = (int32_t)pad(o.m, 64); o.np = (int32_t)pad(o.n, 64);
   }
-  plan->tile = wide >= 256 ? 128 : 64;
-  int64_t at = 0, pieces = 0, matrices = 0, squares = 0, tiles = 0;
+  std::stable_sort(plan->g, plan->g + plan->n, [](const OrthoGroup& a, const OrthoGroup& b) { return a.np > b.np; });
+  int64_t at = 0, pieces = 0, matrices = 0, squares = 0;
   auto take = [&](int64_t bytes) { const int64_t p = at; at = pad(at + bytes, 256); return p; };
   for (int k = 0; k < plan->n; ++k) {
     OrthoGroup& o = plan->g[k];
-    o.mp = (int32_t)pad(o.m, plan->tile); o.np = (int32_t)pad(o.n, plan->tile);
     o.first = (int32_t)matrices; o.first_piece = (int32_t)pieces;
     matrices += o.count; pieces += (int64_t)o.count * o.pieces();
     squares += (int64_t)o.count * (o.mp / 64) * (o.np / 64);
-    tiles += (int64_t)o.count * (o.mp / plan->tile) * (o.np / plan->tile);
     o.x[0] = take(o.count * 2 * 2 * o.plane_x());
     o.x[1] = take(o.count * 2 * 2 * o.plane_x());
     o.a = take(o.count * 2 * 2 * o.plane_a());
     o.b = take(o.count * 2 * 2 * o.plane_a());
-    if (pieces > MOST_ITEMS || squares > MOST_ITEMS || tiles > MOST_ITEMS) { set_error("too many matrices for one call"); return PPLL_ERR_SHAPE; }
+    if (pieces > MOST_ITEMS || 8 * squares > MOST_ITEMS) { set_error("too many matrices for one call"); return PPLL_ERR_SHAPE; }
   }
+  for (int phase = 0; phase < 3; ++phase) plan_product(plan, phase);
   plan->partials = take(pieces * (int64_t)sizeof(double));
   plan->shrink = take(matrices * (int64_t)sizeof(float));
   plan->bytes = at;
