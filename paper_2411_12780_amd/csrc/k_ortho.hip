@@ -397,32 +397,74 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
       *(f16x8*)(to + pa) = l;
     }
   };
-  // the result, from the same place; the caller's rows are columns of `sums` where the matrix is tall.  A wave takes 64 elements at a time
-  // that lie side by side (tall: `rows` of them), whatever the alignment, and has eight times as many on their way.
-  auto store_result = [&](const float* sums, int r0, int rows, int i0, int j0) {
+  // n of eight elements side by side in the caller's blob, from element e on
+  const bool quads = ((g.offset | g.stride | g.ld) & 3) == 0;
+  auto store_eight = [&](int64_t e, int n, const float* v) {
+    if (quads && n == 8) {
+      float w[8];
+      if (!t.out) {
+        const float4 a = *(const float4*)(t.p + e), b = *(const float4*)(t.p + e + 4);
+        const float old[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = old[k] * t.decay - v[k];
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = v[k];
+      }
+      if (!t.out || t.dt == F32) {
+        float* to = (t.out ? (float*)t.out : t.p) + e;
+        *(float4*)to = make_float4(w[0], w[1], w[2], w[3]);
+        *(float4*)(to + 4) = make_float4(w[4], w[5], w[6], w[7]);
+      }
+      uint16_t* half = t.out ? t.dt == BF16 ? (uint16_t*)t.out : nullptr : t.shadow;
+      if (half) {
+        *(uint2*)(half + e) = make_uint2(f32x2_to_bf16x2(w[0], w[1]), f32x2_to_bf16x2(w[2], w[3]));
+        *(uint2*)(half + e + 4) = make_uint2(f32x2_to_bf16x2(w[4], w[5]), f32x2_to_bf16x2(w[6], w[7]));
+      }
+      return;
+    }
+    float w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = !t.out && k < n ? t.p[e + k] : 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (k >= n) continue;
+      if (t.out) {
+        st_f(t.out, (size_t)(e + k), v[k], t.dt);
+      } else {
+        w[k] = w[k] * t.decay - v[k];
+        t.p[e + k] = w[k];
+        if (t.shadow) t.shadow[e + k] = f32_to_bf16(w[k]);
+      }
+    }
+  };
+  // the result: rows r0 .. of `sums`; where the matrix is tall the caller's rows are columns of `sums`
+  auto store_result = [&](float* sums, int r0, int rows, int i0, int j0) {
     const float scale = UNSCALE * shrink.next * (t.out ? 1.f : 0.2f * t.lr * sqrtf((float)g.n));
-    for (int k0 = 0; k0 < rows; k0 += 8) {
-      float v[8], w[8];
-      int64_t e[8];
+    const int seg = (lane & 7) * 8;
+    for (int r = r0 + (lane >> 3); r < r0 + rows; r += 8) {
+      float* from_lds = sums + r * PITCH + seg;
+      const float4 lo4 = *(const float4*)from_lds, hi4 = *(const float4*)(from_lds + 4);
+      float v[8] = {lo4.x, lo4.y, lo4.z, lo4.w, hi4.x, hi4.y, hi4.z, hi4.w};
+      const _Float16* add = X + (int64_t)(i0 + r) * g.np + j0 + seg;
+      const f16x8 h = *(const f16x8*)add, l = *(const f16x8*)(add + px);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int r = r0 + (g.tall ? lane % rows : k0 + k), c = g.tall ? lane / rows + (k0 + k) * (64 / rows) : lane, i = i0 + r, j = j0 + c;
-        e[k] = i >= g.m || j >= g.n ? -1 : g.tall ? element(g, at.matrix, j, i) : element(g, at.matrix, i, j);
-        const _Float16* add = X + (int64_t)i * g.np + j;
-        w[k] = !t.out && e[k] >= 0 ? t.p[e[k]] : 0.f;
-        v[k] = fmaf(NS_A, (float)add[0] + (float)add[px], sums[r * PITCH + c] * UNSCALE) * shrink.ratio * scale;
+      for (int k = 0; k < 8; ++k) v[k] = fmaf(NS_A, (float)h[k] + (float)l[k], v[k] * UNSCALE) * shrink.ratio * scale;
+      if (!g.tall) {
+        if (i0 + r < g.m && j0 + seg < g.n) store_eight(element(g, at.matrix, i0 + r, j0 + seg), min(8, g.n - j0 - seg), v);
+      } else {
+        *(float4*)from_lds = make_float4(v[0], v[1], v[2], v[3]);
+        *(float4*)(from_lds + 4) = make_float4(v[4], v[5], v[6], v[7]);
       }
+    }
+    if (!g.tall) return;
+    wave_sync();
+    const int segs = rows / 8, i = i0 + r0 + lane % segs * 8;
+    for (int c = lane / segs; c < 64; c += 64 / segs) {
+      float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if (e[k] < 0) continue;
-        if (t.out) {
-          st_f(t.out, (size_t)e[k], v[k], t.dt);
-        } else {
-          w[k] = w[k] * t.decay - v[k];
-          t.p[e[k]] = w[k];
-          if (t.shadow) t.shadow[e[k]] = f32_to_bf16(w[k]);
-        }
-      }
+      for (int k = 0; k < 8; ++k) v[k] = sums[(r0 + lane % segs * 8 + k) * PITCH + c];
+      if (i < g.m && j0 + c < g.n) store_eight(element(g, at.matrix, j0 + c, i), min(8, g.m - i), v);
     }
   };
   // a 32 x 32 tile of sums: lane l holds row l % 32, columns 8 q + 4 (l / 32) + e in element 4 q + e
