@@ -59,7 +59,7 @@ __device__ __forceinline__ int64_t element(const OrthoGroup& g, int matrix, int 
 struct Place { int group, matrix; };
 template <class EACH> __device__ __forceinline__ Place place_of(const OrthoPlan& p, int& id, EACH each) {
   for (int k = 0; k < p.n; ++k) {
-    const int e = each(p.g[k]), all = e * p.g[k].count;
+    const int e = each(p.g[k]), all = e * p.g[k].count;      // (none: no items of this kind)
     if (id < all) {
       const int i = id / e;
       id -= i * e;
@@ -78,7 +78,7 @@ __device__ __forceinline__ float read_u(const Source& s, int64_t at) {
 // The momentum, and the sums of squares of pieces of 32 x 256 (in 64 bits: gradients of 1e-25 or 1e25 have a norm as well).
 __global__ __launch_bounds__(256) void squares_kernel(OrthoPlan p, Source s, char* ws) {
   int id = blockIdx.x;
-  const Place at = place_of(p, id, [](const OrthoGroup& g) { return g.pieces(); });
+  const Place at = place_of(p, id, [](const OrthoGroup& g) { return g.small ? 0 : g.pieces(); });
   const OrthoGroup& g = p.g[at.group];
   const int across = (g.cols + NORM_COLS - 1) / NORM_COLS, r0 = id / across * NORM_ROWS, c = id % across * NORM_COLS + threadIdx.x;
   double sum = 0;
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(256) void squares_kernel(OrthoPlan p, Source s, cha
 // Y = u / |u|, in tiles of 64 x 64.
 __global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, char* ws) {
   int id = blockIdx.x;
-  const Place at = place_of(p, id, [](const OrthoGroup& g) { return (g.mp / 64) * (g.np / 64); });
+  const Place at = place_of(p, id, [](const OrthoGroup& g) { return g.small ? 0 : (g.mp / 64) * (g.np / 64); });
   const OrthoGroup& g = p.g[at.group];
   const int t = threadIdx.x, i0 = id / (g.np / 64) * 64, j0 = id % (g.np / 64) * 64;
   __shared__ double sums[256];
@@ -538,6 +538,195 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
 #undef NS_CUR
 #undef NS_CROSS
 
+// ------------------------------------------------------------------ small matrices
+// All steps of one matrix in one workgroup of 16 waves: X and A (then B in its place) stay in LDS as planes, rows 16 bytes longer than their
+// elements so that 16 rows' pieces meet no bank twice.  A wave multiplies 16 x 16 tiles (v_mfma_f32_16x16x32_f16) of up to NT turns; results
+// wait in registers until everyone has read what they replace.  Bound by the chain of barriers and LDS reads: 64 x 64 takes some 2 us a step, where
+// the three launches of the tiled kernels take 15.
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+constexpr int SMALL_TURNS = (ORTHO_SMALL_ELEMENTS / 256 + 15) / 16;      // tiles of the largest X for each wave
+constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64;
+typedef __attribute__((ext_vector_type(4))) short i16x4;
+// Four rows of 16 elements, an 8-byte piece from each of 16 lanes: each lane receives the four elements of its column.
+__device__ __forceinline__ f16x4 read_columns(const _Float16* from) {
+  return __builtin_bit_cast(f16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)from));
+}
+template <int NT> __global__ __launch_bounds__(SMALL_THREADS) void small_kernel(OrthoPlan p, Source src, Target t, int steps) {
+  extern __shared__ __align__(16) char stages[];
+  __shared__ double sums[SMALL_WAVES];
+  int id = blockIdx.x;
+  const Place at = place_of(p, id, [](const OrthoGroup& g) { return g.small ? 1 : 0; });
+  const OrthoGroup& g = p.g[at.group];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lx = g.np + 8, la = g.mp + 8, px = g.mp * lx, pa = g.mp * la;      // row lengths and planes, in halves
+  _Float16 *X = (_Float16*)stages, *A = X + 2 * px;
+  for (int k = tid; k < (2 * px + 2 * pa) / 8; k += SMALL_THREADS) ((f16x8*)stages)[k] = f16x8{};
+  // ---- momentum, norm, X
+  const int all = g.rows * g.cols;
+  const float per = 1.f / g.cols;
+  auto place = [&](int e, int& r, int& c) { r = (int)(((float)e + 0.5f) * per); c = e - r * g.cols; };     // exact: e < 2^16
+  double sum = 0;
+  for (int e0 = tid; e0 < all; e0 += 4 * SMALL_THREADS) {
+    float u[4], m[4];
+    int64_t el[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e = e0 + k * SMALL_THREADS;
+      int r, c;
+      place(e, r, c);
+      el[k] = e < all ? element(g, at.matrix, r, c) : -1;
+      u[k] = el[k] < 0 ? 0.f : src.in ? ld_f(src.in, (size_t)el[k], src.dt) : src.g[el[k]];
+      m[k] = el[k] >= 0 && !src.in ? src.m[el[k]] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (!src.in) {
+        m[k] = fmaf(src.momentum, m[k], u[k]);
+        if (el[k] >= 0) src.m[el[k]] = m[k];
+        u[k] = src.nesterov ? fmaf(src.momentum, m[k], u[k]) : m[k];
+      }
+      sum += (double)u[k] * u[k];
+    }
+  }
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  sum = 0;
+  for (int w = 0; w < SMALL_WAVES; ++w) sum += sums[w];
+  const double norm = sqrt(sum), inv = norm > 0 ? SCALE / norm : norm;
+  const float t0 = (float)(norm / (norm + NORM_EPS));
+  for (int e0 = tid; e0 < all; e0 += 4 * SMALL_THREADS) {
+    float u[4];
+    int r[4], c[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e = e0 + k * SMALL_THREADS;
+      place(e, r[k], c[k]);
+      u[k] = e < all ? read_u(src, element(g, at.matrix, r[k], c[k])) : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (e0 + k * SMALL_THREADS >= all) continue;
+      _Float16* to = X + (g.tall ? c[k] * lx + r[k] : r[k] * lx + c[k]);
+      split((float)(u[k] * inv), to[0], to[px]);
+    }
+  }
+  __syncthreads();
+
+  // ---- tile `n` of a product of `across` tiles a row: P rows i0 .., Q rows j0 .. (or columns of X) over K; lane l: row l % 16, columns
+  // 4 (l / 16) + e of the tile in element e
+  const int row = lane & 15, kpart = 8 * (lane >> 4);
+  auto rows_product = [&](const _Float16* P, int ld, int plane, int i0, int j0, int K) {
+    f32x4 hh = {}, xx = {};
+    const _Float16 *pr = P + (i0 + row) * ld + kpart, *qr = P + (j0 + row) * ld + kpart;
+    for (int k = 0; k < K; k += 32) {
+      const f16x8 ph = *(const f16x8*)(pr + k), pl = *(const f16x8*)(pr + plane + k), qh = *(const f16x8*)(qr + k), ql = *(const f16x8*)(qr + plane + k);
+      hh = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh, ph, hh, 0, 0, 0);
+      xx = __builtin_amdgcn_mfma_f32_16x16x32_f16(ql, ph, xx, 0, 0, 0);
+      xx = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh, pl, xx, 0, 0, 0);
+    }
+    return hh + xx;
+  };
+  auto columns_product = [&](const _Float16* B, int i0, int j0) {
+    f32x4 hh = {}, xx = {};
+    const _Float16 *pr = B + (i0 + row) * la + kpart, *qr = X + (kpart + (row >> 2)) * lx + j0 + 4 * (row & 3);
+    for (int k = 0; k < g.mp; k += 32) {
+      const f16x8 ph = *(const f16x8*)(pr + k), pl = *(const f16x8*)(pr + pa + k);
+      f16x8 q[2];
+#pragma unroll
+      for (int pl2 = 0; pl2 < 2; ++pl2) {
+        const _Float16* from = qr + pl2 * px + k * lx;
+        const f16x4 a = read_columns(from), b = read_columns(from + 4 * lx);
+        q[pl2] = f16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      }
+      hh = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[0], ph, hh, 0, 0, 0);
+      xx = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[1], ph, xx, 0, 0, 0);
+      xx = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[0], pl, xx, 0, 0, 0);
+    }
+    return hh + xx;
+  };
+  const int ta = g.mp / 16, tx = g.np / 16;
+  f32x4 held[NT];
+  // every tile of this wave: f(turn, i0, j0)
+  auto tiles = [&](int across, auto f) {
+    int first = wave;
+    if (NT > 3) asm volatile("" : "+s"(first));     // addresses of all turns, kept from step to step, would not fit into the registers
+#pragma unroll
+    for (int k = 0; k < NT; ++k) {
+      const int n = first + k * SMALL_WAVES;
+      if (n < ta * across) f(k, n / across * 16, n % across * 16);
+      if (NT > 3) __builtin_amdgcn_sched_barrier(0);     // the turns' fragments do not fit into the registers together
+    }
+  };
+  auto add_old = [&](const _Float16* from, int plane, f32x4 v, float old_by, float by, float ratio) {
+    const f16x4 h = *(const f16x4*)from, l = *(const f16x4*)(from + plane);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(old_by, (float)h[e] + (float)l[e], by * (v[e] * UNSCALE)) * ratio;
+    return v;
+  };
+  auto put = [&](_Float16* to, int plane, f32x4 v) {
+    f16x4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      _Float16 a, b;
+      split(v[e], a, b);
+      h[e] = a; l[e] = b;
+    }
+    *(f16x4*)to = h;
+    *(f16x4*)(to + plane) = l;
+  };
+  const int col = 4 * (lane >> 4);
+  for (int k = 0; k < steps; ++k) {
+    const Shrink shrink = shrink_of(t0, k);
+    const float t2 = shrink.now * shrink.now;
+    tiles(ta, [&](int, int i0, int j0) { put(A + (i0 + row) * la + j0 + col, pa, rows_product(X, lx, px, i0, j0, g.np) * UNSCALE); });
+    __syncthreads();
+    tiles(ta, [&](int n, int i0, int j0) {
+      held[n] = add_old(A + (i0 + row) * la + j0 + col, pa, rows_product(A, la, pa, i0, j0, g.mp), NS_B * t2, NS_C * t2 * t2, 1.f);
+    });
+    __syncthreads();
+    tiles(ta, [&](int n, int i0, int j0) { put(A + (i0 + row) * la + j0 + col, pa, held[n]); });
+    __syncthreads();
+    tiles(tx, [&](int n, int i0, int j0) {
+      held[n] = add_old(X + (i0 + row) * lx + j0 + col, px, columns_product(A, i0, j0), NS_A, 1.f, shrink.ratio);
+    });
+    if (k + 1 == steps) break;
+    __syncthreads();
+    tiles(tx, [&](int n, int i0, int j0) { put(X + (i0 + row) * lx + j0 + col, px, held[n]); });
+    __syncthreads();
+  }
+  const float scale = UNSCALE * shrink_of(t0, steps - 1).next * (t.out ? 1.f : 0.2f * t.lr * sqrtf((float)g.n));
+  tiles(tx, [&](int n, int i0, int j0) {
+    const int i = i0 + row;
+    int64_t el[4];
+    float w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = j0 + col + e;
+      el[e] = i >= g.m || j >= g.n ? -1 : g.tall ? element(g, at.matrix, j, i) : element(g, at.matrix, i, j);
+      w[e] = !t.out && el[e] >= 0 ? t.p[el[e]] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (el[e] < 0) continue;
+      if (t.out) {
+        st_f(t.out, (size_t)el[e], held[n][e] * scale, t.dt);
+      } else {
+        w[e] = w[e] * t.decay - held[n][e] * scale;
+        t.p[el[e]] = w[e];
+        if (t.shadow) t.shadow[el[e]] = f32_to_bf16(w[e]);
+      }
+    }
+  });
+}
+template <int NT> int launch_small(hipStream_t s, const OrthoPlan& p, const Source& src, const Target& dst, int steps, int matrices, int lds) {
+  static OncePerDevice once;
+  PPLL_TRY(raise_lds((const void*)small_kernel<NT>, ORTHO_SMALL_LDS, once));
+  hipLaunchKernelGGL((small_kernel<NT>), dim3(matrices), dim3(SMALL_THREADS), lds, s, p, src, dst, steps);
+  PPLL_HIP(hipGetLastError());
+  return PPLL_OK;
+}
+
 template <int MODE> int launch_product(hipStream_t s, const OrthoPlan& p, const Target& t, char* ws, int step) {
   const int phase = MODE < APPLY ? MODE : APPLY, tile = p.tile[phase];
   const XcdShares& shares = p.shares[phase];
@@ -551,12 +740,26 @@ template <int MODE> int launch_product(hipStream_t s, const OrthoPlan& p, const 
 }
 
 int run(hipStream_t s, const OrthoPlan& p, const Source& src, const Target& dst, int steps, char* ws) {
-  if (!p.n) return PPLL_OK;
   int64_t pieces = 0, squares = 0;
+  int small = 0, tiles = 0, lds = 0;
   for (int k = 0; k < p.n; ++k) {
-    pieces += (int64_t)p.g[k].count * p.g[k].pieces();
-    squares += (int64_t)p.g[k].count * (p.g[k].mp / 64) * (p.g[k].np / 64);
+    const OrthoGroup& g = p.g[k];
+    if (g.small) {
+      small += g.count;
+      tiles = g.mp / 16 * (g.np / 16) > tiles ? g.mp / 16 * (g.np / 16) : tiles;
+      lds = (int)g.small_lds() > lds ? (int)g.small_lds() : lds;
+    } else {
+      pieces += (int64_t)g.count * g.pieces();
+      squares += (int64_t)g.count * (g.mp / 64) * (g.np / 64);
+    }
   }
+  if (small) {
+    const int turns = (tiles + SMALL_WAVES - 1) / SMALL_WAVES;
+    if (turns <= 1) PPLL_TRY(launch_small<1>(s, p, src, dst, steps, small, lds));
+    else if (turns <= 3) PPLL_TRY(launch_small<3>(s, p, src, dst, steps, small, lds));
+    else PPLL_TRY(launch_small<SMALL_TURNS>(s, p, src, dst, steps, small, lds));
+  }
+  if (!pieces) return PPLL_OK;
   hipLaunchKernelGGL(squares_kernel, dim3((unsigned)pieces), dim3(256), 0, s, p, src, ws);
   PPLL_HIP(hipGetLastError());
   hipLaunchKernelGGL(normalise_kernel, dim3((unsigned)squares), dim3(256), 0, s, p, src, ws);

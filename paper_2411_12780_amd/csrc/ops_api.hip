@@ -44,6 +44,7 @@ void plan_product(OrthoPlan* p, int phase) {
     double all = 0, longest = 0;
     for (int k = 0; k < p->n; ++k) {
       const OrthoGroup& o = p->g[k];
+      if (o.small) continue;
       const double len = (phase == ORTHO_GRAM ? o.np : o.mp) * (tile == 128 ? 0.4 : 0.17);
       all += (double)o.count * tiles_of_matrix(o, tile, phase) * len;
       if (len > longest) longest = len;
@@ -103,13 +104,16 @@ int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* pla
     o.rows = g.rows; o.cols = g.cols; o.count = g.count;
     o.tall = g.rows > g.cols;
     o.m = o.tall ? g.cols : g.rows; o.n = o.tall ? g.rows : g.cols;
-    o.mp = (int32_t)pad(o.m, 64); o.np = (int32_t)pad(o.n, 64);
+    o.mp = (int32_t)pad(o.m, 32); o.np = (int32_t)pad(o.n, 32);
+    o.small = o.small_lds() <= ORTHO_SMALL_LDS;
+    if (!o.small) { o.mp = (int32_t)pad(o.m, 64); o.np = (int32_t)pad(o.n, 64); }
   }
   std::stable_sort(plan->g, plan->g + plan->n, [](const OrthoGroup& a, const OrthoGroup& b) { return a.np > b.np; });
   int64_t at = 0, pieces = 0, matrices = 0, squares = 0;
   auto take = [&](int64_t bytes) { const int64_t p = at; at = pad(at + bytes, 256); return p; };
   for (int k = 0; k < plan->n; ++k) {
     OrthoGroup& o = plan->g[k];
+    if (o.small) continue;
     o.first = (int32_t)matrices; o.first_piece = (int32_t)pieces;
     matrices += o.count; pieces += (int64_t)o.count * o.pieces();
     squares += (int64_t)o.count * (o.mp / 64) * (o.np / 64);

@@ -12,6 +12,9 @@ constexpr int ORTHO_SIDE = 8192;       // rows and columns of a matrix, at most
 constexpr int ORTHO_STEPS = 16;        // Newton-Schulz steps, at most
 constexpr int NORM_ROWS = 32, NORM_COLS = 256;   // piece of a matrix whose squares one workgroup adds up
 
+constexpr int ORTHO_SMALL_LDS = 160 * 1024 - 256;   // what a workgroup of the small kernel may have (256 bytes are its own)
+constexpr int ORTHO_SMALL_ELEMENTS = ORTHO_SMALL_LDS / 4;
+
 // A group as the kernels see it.  A matrix is worked on as X [m][n] with m <= n (transposed where rows > cols), padded with zeros to
 // mp x np: zero rows and columns stay zero through every product, so no product has a border.  Each intermediate is two planes of fp16,
 // one behind the other; offsets in bytes from the start of the workspace, those of matrix i of the group i times its size further.
@@ -19,16 +22,19 @@ struct OrthoGroup {
   int64_t offset, stride, ld;          // elements, in the caller's blobs
   int32_t rows, cols, count;
   int32_t m, n, mp, np, tall;
+  int32_t small;                       // all steps in one workgroup (then mp and np are multiples of 32, of 64 else)
   int32_t first;                       // place of the group's first matrix among all of the call
   int32_t first_piece;                 // of its pieces among those of all groups
   int64_t x[2], a, b;
   __host__ __device__ int64_t plane_x() const { return (int64_t)mp * np; }      // elements
   __host__ __device__ int64_t plane_a() const { return (int64_t)mp * mp; }
+  __host__ __device__ int64_t small_lds() const { return 4 * ((int64_t)mp * (np + 8) + (int64_t)mp * (mp + 8)); }   // bytes: X and A
   __host__ __device__ int pieces() const { return ((rows + NORM_ROWS - 1) / NORM_ROWS) * ((cols + NORM_COLS - 1) / NORM_COLS); }
 };
 // The products of a step: X X', then b A + c A A, then the product of that and X.
 enum { ORTHO_GRAM = 0, ORTHO_POLY = 1, ORTHO_APPLY = 2 };
 __host__ __device__ inline int tiles_of_matrix(const OrthoGroup& g, int tile, int phase) {
+  if (g.small) return 0;
   const int down = (g.mp + tile - 1) / tile, across = (g.np + tile - 1) / tile;
   return phase <= ORTHO_POLY ? down * (down + 1) / 2 : down * across;      // of a symmetric result those on and under the diagonal
 }

@@ -294,3 +294,12 @@ def test_no_element_of_many_loses_its_low_term():
     off = lambda v: ((v.double() - x).norm(dim=(1, 2)) / x.norm(dim=(1, 2))).max().item()  # noqa: E731
     own, fp32 = off(torch.from_numpy(got.reshape(400, 64, 64))), off(y)
     assert own <= 2 * fp32, (own, fp32)
+
+
+@pytest.mark.parametrize("rows,cols", [(64, 500), (33, 1000), (100, 250), (128, 144), (129, 129), (128, 160), (160, 96), (16, 2000), (32, 1264), (32, 1300), (64, 64)])
+def test_sizes_on_both_sides_of_what_one_workgroup_holds(rows, cols):
+    for shape in ((rows, cols), (cols, rows)):
+        groups = [P.matrix_group(3, *shape, ld=shape[1] + 1, count=2)]
+        values = np.random.default_rng(rows + cols).standard_normal(blob_size(groups)).astype(np.float32)
+        given, got = run(groups, values)
+        check(groups, given, got)

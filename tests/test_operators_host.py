@@ -20,9 +20,10 @@ def test_workspace_of_groups():
     size = P.ppll_orthogonalize_workspace_bytes
     assert size([]) == 0
     assert size([P.matrix_group(0, 8, 8, count=0)]) == 0
-    one = size([P.matrix_group(0, 8, 8)])
+    assert size([P.matrix_group(0, 8, 8, count=1000)]) == 0        # small ones never leave their workgroup
+    one = size([P.matrix_group(0, 300, 400)])
     assert one > 0 and one % 256 == 0
-    assert size([P.matrix_group(0, 8, 8), P.matrix_group(64, 8, 8)]) > one
+    assert size([P.matrix_group(0, 300, 400), P.matrix_group(120000, 300, 400)]) > one
     assert size([P.matrix_group(0, 8192, 8192)]) >= 8192 * 8192 * 4
 
 
@@ -41,23 +42,23 @@ def test_groups_that_are_refused(group):
 def test_groups_that_share_elements_are_refused():
     size, g = P.ppll_orthogonalize_workspace_bytes, P.matrix_group
     qkv = [g(i * 4, 4, 4, ld=12, count=3, stride=100) for i in range(3)]
-    assert size(qkv) > 0                                            # query, key and value parts of three layers
-    assert size([g(0, 4, 4, ld=12, count=3, stride=4), g(48, 4, 8)]) > 0
+    assert size(qkv) == 0                                           # query, key and value parts of three layers
+    assert size([g(0, 4, 4, ld=12, count=3, stride=4), g(48, 4, 8)]) == 0
     refused(SHAPE, size, [g(0, 4, 4), g(0, 4, 4)])                  # the same twice
     refused(SHAPE, size, [g(0, 4, 4), g(15, 2, 2)])
     refused(SHAPE, size, [g(0, 4, 5, ld=12), g(4, 4, 4, ld=12)])    # a common column
     refused(SHAPE, size, [g(0, 4, 4, ld=12), g(10, 4, 4, ld=12)])   # columns 10..13 are 10, 11 and 0, 1 of the next row
     refused(SHAPE, size, [g(0, 4, 4, ld=12), g(4, 4, 4, ld=11)])    # interleaved with another row length
     refused(SHAPE, size, [g(0, 4, 4, count=10, stride=100), g(715, 2, 2)])      # the eighth matrix is 700..715
-    assert size([g(0, 4, 4, count=10, stride=100), g(716, 2, 2)]) > 0
-    assert size([g(0, 4, 4, count=10, stride=100), g(715, 2, 2, count=0)]) > 0
-    assert size([g(0, 4, 4, count=10, stride=100), g(16, 4, 4, count=10, stride=100), g(32, 4, 4, count=5, stride=200)]) > 0
+    assert size([g(0, 4, 4, count=10, stride=100), g(716, 2, 2)]) == 0
+    assert size([g(0, 4, 4, count=10, stride=100), g(715, 2, 2, count=0)]) == 0
+    assert size([g(0, 4, 4, count=10, stride=100), g(16, 4, 4, count=10, stride=100), g(32, 4, 4, count=5, stride=200)]) == 0
 
 
 def test_more_groups_than_a_call_takes():
     groups = [P.matrix_group(16 * i, 4, 4) for i in range(17)]
     refused(SHAPE, P.ppll_orthogonalize_workspace_bytes, groups)
-    assert P.ppll_orthogonalize_workspace_bytes(groups[:16]) > 0
+    assert P.ppll_orthogonalize_workspace_bytes(groups[:16]) == 0
     g = P.MatrixGroup(0, 16, 4, 4, 4, 1, 1)                         # reserved
     refused(SHAPE, P.ppll_orthogonalize_workspace_bytes, [g])
     n = ctypes.c_size_t(0)
@@ -67,7 +68,7 @@ def test_more_groups_than_a_call_takes():
 
 
 def test_orthogonalize_refusals():
-    g = [P.matrix_group(0, 8, 8)]
+    g = [P.matrix_group(0, 300, 300)]
     ws = P.ppll_orthogonalize_workspace_bytes(g)
     call = P.ppll_orthogonalize
     refused(CONFIG, call, g, 2, 5, 16, 16, 16, ws)
@@ -84,7 +85,7 @@ def test_orthogonalize_refusals():
 
 
 def test_muon_refusals():
-    g = [P.matrix_group(0, 8, 8)]
+    g = [P.matrix_group(0, 300, 300)]
     ws = P.ppll_orthogonalize_workspace_bytes(g)
     def call(steps=5, grads=16, m=32, p=48, shadow=None, lr=0.1, momentum=0.9, decay=0.0, work=64, nbytes=ws):
         P.ppll_muon_step(g, steps, grads, m, p, shadow, lr, momentum, True, decay, work, nbytes)
