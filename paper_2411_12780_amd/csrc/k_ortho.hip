@@ -4,6 +4,7 @@
 #include "ortho.h"
 
 #include <math.h>
+#include <type_traits>
 
 namespace ppll {
 
@@ -44,13 +45,21 @@ struct Source { const void* in; int dt; const float* g; float* m; float momentum
 // Where the result goes: out (orthogonalize), or null: the parameters
 struct Target { void* out; int dt; float* p; uint16_t* shadow; float lr, decay; };
 
-// v is pinned to its fp32 value first: the compiler may fold the arithmetic that gives it into one of the two conversions (a fused operation
-// that rounds to fp16 once) and not into the other, and at a tie hi and what lo is counted from are then two neighbours (one element in some
-// 20000 was off by a whole step of hi, 2^-11 of it).
-__device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
-  asm("" : "+v"(v));
-  hi = (_Float16)v;
-  lo = (_Float16)(v - (float)hi);
+// hi and lo of n values.  Each is pinned to its fp32 value first: the compiler may fold the arithmetic that gives it into one of the conversions
+// (a fused operation that rounds to fp16 once) and not into the other, and at a tie hi and what lo is counted from are then two neighbours (one
+// element in some 20000 was off by a whole step of hi, 2^-11 of it).  Two values are converted by one instruction; lo is one fused operation.
+template <int N> struct Terms { _Float16 __attribute__((ext_vector_type(N))) hi, lo; };
+template <int N> __device__ __forceinline__ Terms<N> split_all(const float* v) {
+  Terms<N> r;
+#pragma unroll
+  for (int k = 0; k < N; k += 2) {
+    float a = v[k], b = v[k + 1];
+    asm("" : "+v"(a), "+v"(b));
+    const _Float16 ha = (_Float16)a, hb = (_Float16)b;
+    r.hi[k] = ha; r.hi[k + 1] = hb;
+    r.lo[k] = (_Float16)fmaf((float)ha, -1.f, a); r.lo[k + 1] = (_Float16)fmaf((float)hb, -1.f, b);
+  }
+  return r;
 }
 __device__ __forceinline__ int64_t element(const OrthoGroup& g, int matrix, int r, int c) {
   return g.offset + (int64_t)matrix * g.stride + (int64_t)r * g.ld + c;
@@ -73,6 +82,48 @@ __device__ __forceinline__ float read_u(const Source& s, int64_t at) {
   if (s.in) return ld_f(s.in, (size_t)at, s.dt);
   const float m = s.m[at];
   return s.nesterov ? fmaf(s.momentum, m, s.g[at]) : m;
+}
+
+__device__ __forceinline__ bool in_quads(const OrthoGroup& g) { return ((g.offset | g.stride | g.ld) & 3) == 0; }   // rows' pieces of four are aligned
+// The first n (at most eight) of eight values, to elements e .. of the result or as the update of the parameters there
+__device__ __forceinline__ void store_eight(const Target& t, bool quads, int64_t e, int n, const float* v) {
+  if (quads && n >= 8) {
+    float w[8];
+    if (!t.out) {
+      const float4 a = *(const float4*)(t.p + e), b = *(const float4*)(t.p + e + 4);
+      const float old[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = old[k] * t.decay - v[k];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = v[k];
+    }
+    if (!t.out || t.dt == F32) {
+      float* to = (t.out ? (float*)t.out : t.p) + e;
+      *(float4*)to = make_float4(w[0], w[1], w[2], w[3]);
+      *(float4*)(to + 4) = make_float4(w[4], w[5], w[6], w[7]);
+    }
+    uint16_t* half = t.out ? t.dt == BF16 ? (uint16_t*)t.out : nullptr : t.shadow;
+    if (half) {
+      *(uint2*)(half + e) = make_uint2(f32x2_to_bf16x2(w[0], w[1]), f32x2_to_bf16x2(w[2], w[3]));
+      *(uint2*)(half + e + 4) = make_uint2(f32x2_to_bf16x2(w[4], w[5]), f32x2_to_bf16x2(w[6], w[7]));
+    }
+    return;
+  }
+  float w[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) w[k] = !t.out && k < n ? t.p[e + k] : 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (k >= n) continue;
+    if (t.out) {
+      st_f(t.out, (size_t)(e + k), v[k], t.dt);
+    } else {
+      w[k] = w[k] * t.decay - v[k];
+      t.p[e + k] = w[k];
+      if (t.shadow) t.shadow[e + k] = f32_to_bf16(w[k]);
+    }
+  }
 }
 
 // The momentum, and the sums of squares of pieces of 32 x 256 (in 64 bits: gradients of 1e-25 or 1e25 have a norm as well).
@@ -143,14 +194,13 @@ __global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, c
   const int64_t plane = g.plane_x();
   _Float16* x = (_Float16*)(ws + g.x[0]) + at.matrix * 2 * plane;
   const int y = t / 4, q = t % 4 * 16;
-  f16x8 h[2], l[2];
-  for (int k = 0; k < 16; ++k) {
-    _Float16 a, b;
-    split(tile[y][q + k], a, b);
-    h[k / 8][k % 8] = a; l[k / 8][k % 8] = b;
-  }
   _Float16* to = x + (int64_t)(i0 + y) * g.np + j0 + q;
-  for (int k = 0; k < 2; ++k) { *(f16x8*)(to + 8 * k) = h[k]; *(f16x8*)(to + plane + 8 * k) = l[k]; }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const Terms<8> v = split_all<8>(&tile[y][q + 8 * k]);
+    *(f16x8*)(to + 8 * k) = v.hi;
+    *(f16x8*)(to + plane + 8 * k) = v.lo;
+  }
 }
 
 // ------------------------------------------------------------------ products
@@ -368,16 +418,10 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
         *(float4*)from_lds = make_float4(v[0], v[1], v[2], v[3]);
         *(float4*)(from_lds + 4) = make_float4(v[4], v[5], v[6], v[7]);
       }
-      f16x8 h, l;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        _Float16 a, b;
-        split(v[k], a, b);
-        h[k] = a; l[k] = b;
-      }
+      const Terms<8> v2 = split_all<8>(v);
       _Float16* to = (MODE == GRAM ? A : MODE == POLY ? B : (_Float16*)(ws + g.x[from ^ 1]) + at.matrix * 2 * px) + at_e;
-      *(f16x8*)to = h;
-      *(f16x8*)(to + pl) = l;
+      *(f16x8*)to = v2.hi;
+      *(f16x8*)(to + pl) = v2.lo;
     }
   };
   // columns c0 .. c0 + cols - 1 of `rows` (a multiple of 8) finished rows, as rows of the mirrored tile
@@ -385,63 +429,20 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
     const int segs = rows / 8, seg = lane % segs * 8;
     _Float16* D = MODE == GRAM ? A : B;
     for (int c = c0 + lane / segs; c < c0 + cols; c += 64 / segs) {
-      f16x8 h, l;
+      float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        _Float16 a, b;
-        split(sums[(seg + k) * PITCH + c], a, b);
-        h[k] = a; l[k] = b;
-      }
+      for (int k = 0; k < 8; ++k) v[k] = sums[(seg + k) * PITCH + c];
+      const Terms<8> v2 = split_all<8>(v);
       _Float16* to = D + (int64_t)(j0 + c) * g.mp + i0 + seg;
-      *(f16x8*)to = h;
-      *(f16x8*)(to + pa) = l;
-    }
-  };
-  // n of eight elements side by side in the caller's blob, from element e on
-  const bool quads = ((g.offset | g.stride | g.ld) & 3) == 0;
-  auto store_eight = [&](int64_t e, int n, const float* v) {
-    if (quads && n == 8) {
-      float w[8];
-      if (!t.out) {
-        const float4 a = *(const float4*)(t.p + e), b = *(const float4*)(t.p + e + 4);
-        const float old[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = old[k] * t.decay - v[k];
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = v[k];
-      }
-      if (!t.out || t.dt == F32) {
-        float* to = (t.out ? (float*)t.out : t.p) + e;
-        *(float4*)to = make_float4(w[0], w[1], w[2], w[3]);
-        *(float4*)(to + 4) = make_float4(w[4], w[5], w[6], w[7]);
-      }
-      uint16_t* half = t.out ? t.dt == BF16 ? (uint16_t*)t.out : nullptr : t.shadow;
-      if (half) {
-        *(uint2*)(half + e) = make_uint2(f32x2_to_bf16x2(w[0], w[1]), f32x2_to_bf16x2(w[2], w[3]));
-        *(uint2*)(half + e + 4) = make_uint2(f32x2_to_bf16x2(w[4], w[5]), f32x2_to_bf16x2(w[6], w[7]));
-      }
-      return;
-    }
-    float w[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = !t.out && k < n ? t.p[e + k] : 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (k >= n) continue;
-      if (t.out) {
-        st_f(t.out, (size_t)(e + k), v[k], t.dt);
-      } else {
-        w[k] = w[k] * t.decay - v[k];
-        t.p[e + k] = w[k];
-        if (t.shadow) t.shadow[e + k] = f32_to_bf16(w[k]);
-      }
+      *(f16x8*)to = v2.hi;
+      *(f16x8*)(to + pa) = v2.lo;
     }
   };
   // the result: rows r0 .. of `sums`; where the matrix is tall the caller's rows are columns of `sums`
   auto store_result = [&](float* sums, int r0, int rows, int i0, int j0) {
     const float scale = UNSCALE * shrink.next * (t.out ? 1.f : 0.2f * t.lr * sqrtf((float)g.n));
     const int seg = (lane & 7) * 8;
+    const bool quads = in_quads(g);
     for (int r = r0 + (lane >> 3); r < r0 + rows; r += 8) {
       float* from_lds = sums + r * PITCH + seg;
       const float4 lo4 = *(const float4*)from_lds, hi4 = *(const float4*)(from_lds + 4);
@@ -451,7 +452,7 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = fmaf(NS_A, (float)h[k] + (float)l[k], v[k] * UNSCALE) * shrink.ratio * scale;
       if (!g.tall) {
-        if (i0 + r < g.m && j0 + seg < g.n) store_eight(element(g, at.matrix, i0 + r, j0 + seg), min(8, g.n - j0 - seg), v);
+        if (i0 + r < g.m && j0 + seg < g.n) store_eight(t, quads, element(g, at.matrix, i0 + r, j0 + seg), g.n - j0 - seg, v);
       } else {
         *(float4*)from_lds = make_float4(v[0], v[1], v[2], v[3]);
         *(float4*)(from_lds + 4) = make_float4(v[4], v[5], v[6], v[7]);
@@ -464,7 +465,7 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
       float v[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = sums[(r0 + lane % segs * 8 + k) * PITCH + c];
-      if (i < g.m && j0 + c < g.n) store_eight(element(g, at.matrix, j0 + c, i), min(8, g.m - i), v);
+      if (i < g.m && j0 + c < g.n) store_eight(t, quads, element(g, at.matrix, j0 + c, i), g.m - i, v);
     }
   };
   // a 32 x 32 tile of sums: lane l holds row l % 32, columns 8 q + 4 (l / 32) + e in element 4 q + e
@@ -539,19 +540,21 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
 #undef NS_CROSS
 
 // ------------------------------------------------------------------ small matrices
-// All steps of one matrix in one workgroup of 16 waves: X and A (then B in its place) stay in LDS as planes, rows 16 bytes longer than their
-// elements so that 16 rows' pieces meet no bank twice.  A wave multiplies 16 x 16 tiles (v_mfma_f32_16x16x32_f16) of up to NT turns; results
-// wait in registers until everyone has read what they replace.  Bound by the chain of barriers and LDS reads: 64 x 64 takes some 2 us a step, where
-// the three launches of the tiled kernels take 15.
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-constexpr int SMALL_TURNS = (ORTHO_SMALL_ELEMENTS / 256 + 15) / 16;      // tiles of the largest X for each wave
-constexpr int SMALL_THREADS = 1024, SMALL_WAVES = SMALL_THREADS / 64;
+// All steps of one matrix in one workgroup of 8 waves: X and the symmetric matrices stay in LDS as planes, rows 16 bytes longer than their
+// elements, so that pieces of neighbouring rows meet no bank twice.  Bound by LDS reads and the barriers between the products: with tiles of
+// 16 x 16 on 16 waves, which read each element twice as often, a step of 64 x 64 took 2.7 us and one of 128 x 128 15.3.
+//  Gram and square: tiles of 32 x 32 on and under the diagonal, dealt out to the waves; where there are fewer (one, or three of long rows) the
+//  waves share the k and add up in LDS.
+//  The results of a product wait in registers until everyone has read what they replace, unless there is room for a second buffer.
 typedef __attribute__((ext_vector_type(4))) short i16x4;
 // Four rows of 16 elements, an 8-byte piece from each of 16 lanes: each lane receives the four elements of its column.
 __device__ __forceinline__ f16x4 read_columns(const _Float16* from) {
   return __builtin_bit_cast(f16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)from));
 }
-template <int NT> __global__ __launch_bounds__(SMALL_THREADS) void small_kernel(OrthoPlan p, Source src, Target t, int steps) {
+constexpr int SMALL_THREADS = 512, SMALL_WAVES = SMALL_THREADS / 64;
+constexpr int SMALL_TURNS = (ORTHO_SMALL_LDS / 4096 + SMALL_WAVES - 1) / SMALL_WAVES;      // tiles of the largest X for each wave
+// NT: tiles of X for a wave, at most; NG: of the symmetric matrices
+template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS) void small_kernel(OrthoPlan p, Source src, Target t, int steps) {
   extern __shared__ __align__(16) char stages[];
   __shared__ double sums[SMALL_WAVES];
   int id = blockIdx.x;
@@ -559,170 +562,289 @@ template <int NT> __global__ __launch_bounds__(SMALL_THREADS) void small_kernel(
   const OrthoGroup& g = p.g[at.group];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lx = g.np + 8, la = g.mp + 8, px = g.mp * lx, pa = g.mp * la;      // row lengths and planes, in halves
-  _Float16 *X = (_Float16*)stages, *A = X + 2 * px;
-  for (int k = tid; k < (2 * px + 2 * pa) / 8; k += SMALL_THREADS) ((f16x8*)stages)[k] = f16x8{};
-  // ---- momentum, norm, X
-  const int all = g.rows * g.cols;
-  const float per = 1.f / g.cols;
-  auto place = [&](int e, int& r, int& c) { r = (int)(((float)e + 0.5f) * per); c = e - r * g.cols; };     // exact: e < 2^16
+  const SmallRoom room = small_room(g);
+  _Float16 *X = (_Float16*)stages, *XN = room.two_x ? X + 2 * px : X, *A = XN + 2 * px, *B = room.two_a ? A + 2 * pa : A;
+  float4* parts = (float4*)(B + 2 * pa);                                       // [tile][share of k][q][lane]
+  // ---- momentum, norm, X: a thread takes pieces of eight elements of a row of X (tall: of a column of the caller's matrix, neighbours in
+  // neighbouring threads)
+  constexpr int PIECES = 2 * NT;
+  const int across = g.np / 8, all = g.mp * across;
+  auto piece_at = [&](int n, int& i, int& j) {
+    const int q = tid + n * SMALL_THREADS;
+    if (g.tall) { j = q / g.mp; i = q - j * g.mp; }
+    else { i = q / across; j = q - i * across; }
+    j *= 8;
+    return q < all;
+  };
+  const bool quads = in_quads(g);
+  float u[PIECES][8];
   double sum = 0;
-  for (int e0 = tid; e0 < all; e0 += 4 * SMALL_THREADS) {
-    float u[4], m[4];
-    int64_t el[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int e = e0 + k * SMALL_THREADS;
-      int r, c;
-      place(e, r, c);
-      el[k] = e < all ? element(g, at.matrix, r, c) : -1;
-      u[k] = el[k] < 0 ? 0.f : src.in ? ld_f(src.in, (size_t)el[k], src.dt) : src.g[el[k]];
-      m[k] = el[k] >= 0 && !src.in ? src.m[el[k]] : 0.f;
-    }
+  for (int n = 0; n < PIECES; ++n) {
+    int i, j;
+    const bool on = piece_at(n, i, j) && i < g.m;
+    const int count = on ? min(8, g.n - j) : 0;
+    const int64_t e = g.tall ? element(g, at.matrix, j, i) : element(g, at.matrix, i, j), one = g.tall ? g.ld : 1;
+    float m[8];
+    auto get = [&](const float* from, float* v) {
+      if (!g.tall && quads && count == 8) {
+        const float4 a = *(const float4*)(from + e), b = *(const float4*)(from + e + 4);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (!src.in) {
-        m[k] = fmaf(src.momentum, m[k], u[k]);
-        if (el[k] >= 0) src.m[el[k]] = m[k];
-        u[k] = src.nesterov ? fmaf(src.momentum, m[k], u[k]) : m[k];
+        for (int k = 0; k < 8; ++k) v[k] = k < count ? from[e + k * one] : 0.f;
       }
-      sum += (double)u[k] * u[k];
+    };
+    if (MUON) {
+      get(src.g, u[n]);
+      get(src.m, m);
+    } else if (src.dt == F32) {
+      get((const float*)src.in, u[n]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) u[n][k] = k < count ? bf16_to_f32(((const uint16_t*)src.in)[e + k * one]) : 0.f;
     }
+    if (MUON) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        m[k] = fmaf(src.momentum, m[k], u[n][k]);
+        u[n][k] = src.nesterov ? fmaf(src.momentum, m[k], u[n][k]) : m[k];
+      }
+      if (!g.tall && quads && count == 8) {
+        *(float4*)(src.m + e) = make_float4(m[0], m[1], m[2], m[3]);
+        *(float4*)(src.m + e + 4) = make_float4(m[4], m[5], m[6], m[7]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k < count) src.m[e + k * one] = m[k];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += (double)u[n][k] * u[n][k];
   }
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if (lane == 0) sums[wave] = sum;
   __syncthreads();
   sum = 0;
+#pragma unroll
   for (int w = 0; w < SMALL_WAVES; ++w) sum += sums[w];
   const double norm = sqrt(sum), inv = norm > 0 ? SCALE / norm : norm;
   const float t0 = (float)(norm / (norm + NORM_EPS));
-  for (int e0 = tid; e0 < all; e0 += 4 * SMALL_THREADS) {
-    float u[4];
-    int r[4], c[4];
+  // (a norm whose reciprocal fp32 cannot hold takes the products in 64 bits)
+  const float inv32 = (float)inv;
+  const bool far = !(inv32 > 1e-30f && inv32 < 1e30f);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int e = e0 + k * SMALL_THREADS;
-      place(e, r[k], c[k]);
-      u[k] = e < all ? read_u(src, element(g, at.matrix, r[k], c[k])) : 0.f;
-    }
+  for (int n = 0; n < PIECES; ++n) {
+    int i, j;
+    if (!piece_at(n, i, j)) break;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (e0 + k * SMALL_THREADS >= all) continue;
-      _Float16* to = X + (g.tall ? c[k] * lx + r[k] : r[k] * lx + c[k]);
-      split((float)(u[k] * inv), to[0], to[px]);
-    }
+    for (int k = 0; k < 8; ++k) u[n][k] = far ? (float)(u[n][k] * inv) : u[n][k] * inv32;
+    const Terms<8> v = split_all<8>(u[n]);
+    *(f16x8*)(X + i * lx + j) = v.hi;
+    *(f16x8*)(X + px + i * lx + j) = v.lo;
   }
   __syncthreads();
 
-  // ---- tile `n` of a product of `across` tiles a row: P rows i0 .., Q rows j0 .. (or columns of X) over K; lane l: row l % 16, columns
-  // 4 (l / 16) + e of the tile in element e
-  const int row = lane & 15, kpart = 8 * (lane >> 4);
-  auto rows_product = [&](const _Float16* P, int ld, int plane, int i0, int j0, int K) {
-    f32x4 hh = {}, xx = {};
-    const _Float16 *pr = P + (i0 + row) * ld + kpart, *qr = P + (j0 + row) * ld + kpart;
-    for (int k = 0; k < K; k += 32) {
-      const f16x8 ph = *(const f16x8*)(pr + k), pl = *(const f16x8*)(pr + plane + k), qh = *(const f16x8*)(qr + k), ql = *(const f16x8*)(qr + plane + k);
-      hh = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh, ph, hh, 0, 0, 0);
-      xx = __builtin_amdgcn_mfma_f32_16x16x32_f16(ql, ph, xx, 0, 0, 0);
-      xx = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh, pl, xx, 0, 0, 0);
-    }
+  // ---- products of 32 x 32: lane l holds row l % 32, columns 8 q + 4 (l / 32) + e in element 4 q + e
+  const int row = lane & 31, kpart = 8 * (lane >> 5);
+  // 64 k at a time, all fragments on their way before the first product: one wait for LDS instead of four.  32 where that many registers are taken.
+  struct Pair { f16x8 ph, pl, qh, ql; };
+  auto sum_up = [&](int from, int to, auto load) {
+    f32x16 hh = {}, xx = {};
+    auto piece = [&](int k, auto n) {
+      Pair f[decltype(n)::value];
+#pragma unroll
+      for (int i = 0; i < decltype(n)::value; ++i) f[i] = load(k + 16 * i);
+#pragma unroll
+      for (int i = 0; i < decltype(n)::value; ++i) {
+        hh = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i].qh, f[i].ph, hh, 0, 0, 0);
+        xx = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i].ql, f[i].ph, xx, 0, 0, 0);
+        xx = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i].qh, f[i].pl, xx, 0, 0, 0);
+      }
+    };
+    int k = from;
+    if (NT <= 2)
+      for (; k + 64 <= to; k += 64) piece(k, std::integral_constant<int, 4>());
+    for (; k < to; k += 32) piece(k, std::integral_constant<int, 2>());
     return hh + xx;
   };
-  auto columns_product = [&](const _Float16* B, int i0, int j0) {
-    f32x4 hh = {}, xx = {};
-    const _Float16 *pr = B + (i0 + row) * la + kpart, *qr = X + (kpart + (row >> 2)) * lx + j0 + 4 * (row & 3);
-    for (int k = 0; k < g.mp; k += 32) {
-      const f16x8 ph = *(const f16x8*)(pr + k), pl = *(const f16x8*)(pr + pa + k);
+  auto rows_product = [&](const _Float16* P, int ld, int plane, int i0, int j0, int from, int to) {
+    const _Float16 *pr = P + (i0 + row) * ld + kpart, *qr = P + (j0 + row) * ld + kpart;
+    return sum_up(from, to, [&](int k) {
+      return Pair{*(const f16x8*)(pr + k), *(const f16x8*)(pr + plane + k), *(const f16x8*)(qr + k), *(const f16x8*)(qr + plane + k)};
+    });
+  };
+  auto columns_product = [&](const _Float16* from, int i0, int j0) {
+    const _Float16 *pr = B + (i0 + row) * la + kpart;
+    const _Float16* qr = from + (kpart + ((lane & 15) >> 2)) * lx + j0 + 16 * (lane >> 4 & 1) + 4 * (lane & 3);
+    return sum_up(0, g.mp, [&](int k) {
       f16x8 q[2];
 #pragma unroll
-      for (int pl2 = 0; pl2 < 2; ++pl2) {
-        const _Float16* from = qr + pl2 * px + k * lx;
-        const f16x4 a = read_columns(from), b = read_columns(from + 4 * lx);
-        q[pl2] = f16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      for (int plane = 0; plane < 2; ++plane) {
+        const _Float16* at_k = qr + plane * px + k * lx;
+        const f16x4 a = read_columns(at_k), b = read_columns(at_k + 4 * lx);
+        q[plane] = f16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
       }
-      hh = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[0], ph, hh, 0, 0, 0);
-      xx = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[1], ph, xx, 0, 0, 0);
-      xx = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[0], pl, xx, 0, 0, 0);
-    }
-    return hh + xx;
+      return Pair{*(const f16x8*)(pr + k), *(const f16x8*)(pr + pa + k), q[0], q[1]};
+    });
   };
-  const int ta = g.mp / 16, tx = g.np / 16;
-  f32x4 held[NT];
-  // every tile of this wave: f(turn, i0, j0)
-  auto tiles = [&](int across, auto f) {
-    int first = wave;
-    if (NT > 3) asm volatile("" : "+s"(first));     // addresses of all turns, kept from step to step, would not fit into the registers
-#pragma unroll
-    for (int k = 0; k < NT; ++k) {
-      const int n = first + k * SMALL_WAVES;
-      if (n < ta * across) f(k, n / across * 16, n % across * 16);
-      if (NT > 3) __builtin_amdgcn_sched_barrier(0);     // the turns' fragments do not fit into the registers together
-    }
+  const int ta = g.mp / 32, tx = g.np / 32;
+  const bool whole = NT == 1 || ta <= 2;                          // as many waves as tiles: no mirroring
+  auto sym_tile = [&](int n, int& i0, int& j0) {       // of up to ten
+    if (whole) { i0 = n / ta * 32; j0 = n % ta * 32; return; }
+    const int i = n < 1 ? 0 : n < 3 ? 1 : n < 6 ? 2 : 3;
+    i0 = 32 * i; j0 = 32 * (n - i * (i + 1) / 2);
   };
-  auto add_old = [&](const _Float16* from, int plane, f32x4 v, float old_by, float by, float ratio) {
-    const f16x4 h = *(const f16x4*)from, l = *(const f16x4*)(from + plane);
+  const int ts = whole ? ta * ta : ta * (ta + 1) / 2, col = 4 * (lane >> 5);
+  auto add_old = [&](const _Float16* from, int plane, f32x16 v, float old_by, float by, float ratio) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaf(old_by, (float)h[e] + (float)l[e], by * (v[e] * UNSCALE)) * ratio;
+    for (int q = 0; q < 4; ++q) {
+      const f16x4 h = *(const f16x4*)(from + 8 * q), l = *(const f16x4*)(from + plane + 8 * q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * q + e] = fmaf(old_by, (float)h[e] + (float)l[e], by * (v[4 * q + e] * UNSCALE)) * ratio;
+    }
     return v;
   };
-  auto put = [&](_Float16* to, int plane, f32x4 v) {
-    f16x4 h, l;
+  auto put = [&](_Float16* to, int plane, f32x16 v, _Float16* mirrored) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      _Float16 a, b;
-      split(v[e], a, b);
-      h[e] = a; l[e] = b;
+    for (int q = 0; q < 4; ++q) {
+      const float four[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+      const Terms<4> r = split_all<4>(four);
+      *(f16x4*)(to + 8 * q) = r.hi;
+      *(f16x4*)(to + plane + 8 * q) = r.lo;
+      if (mirrored)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          mirrored[(8 * q + e) * la] = r.hi[e];
+          mirrored[(8 * q + e) * la + plane] = r.lo[e];
+        }
     }
-    *(f16x4*)to = h;
-    *(f16x4*)(to + plane) = l;
   };
-  const int col = 4 * (lane >> 4);
+  auto put_sym = [&](_Float16* D, f32x16 v, int i0, int j0) {
+    put(D + (i0 + row) * la + j0 + col, pa, v, !whole && i0 != j0 ? D + (j0 + col) * la + i0 + row : nullptr);
+  };
+  f32x16 held[NT > NG ? NT : NG];
+  // this wave's n-th tile; the addresses of several, kept from step to step, would not fit into the registers
+  auto nth = [&](int n) {
+    int first = wave;
+    if (NT > 1) {
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("" : "+s"(first));
+    }
+    return first + n * SMALL_WAVES;
+  };
   for (int k = 0; k < steps; ++k) {
     const Shrink shrink = shrink_of(t0, k);
     const float t2 = shrink.now * shrink.now;
-    tiles(ta, [&](int, int i0, int j0) { put(A + (i0 + row) * la + j0 + col, pa, rows_product(X, lx, px, i0, j0, g.np) * UNSCALE); });
-    __syncthreads();
-    tiles(ta, [&](int n, int i0, int j0) {
-      held[n] = add_old(A + (i0 + row) * la + j0 + col, pa, rows_product(A, la, pa, i0, j0, g.mp), NS_B * t2, NS_C * t2 * t2, 1.f);
-    });
-    __syncthreads();
-    tiles(ta, [&](int n, int i0, int j0) { put(A + (i0 + row) * la + j0 + col, pa, held[n]); });
-    __syncthreads();
-    tiles(tx, [&](int n, int i0, int j0) {
-      held[n] = add_old(X + (i0 + row) * lx + j0 + col, px, columns_product(A, i0, j0), NS_A, 1.f, shrink.ratio);
-    });
-    if (k + 1 == steps) break;
-    __syncthreads();
-    tiles(tx, [&](int n, int i0, int j0) { put(X + (i0 + row) * lx + j0 + col, px, held[n]); });
-    __syncthreads();
-  }
-  const float scale = UNSCALE * shrink_of(t0, steps - 1).next * (t.out ? 1.f : 0.2f * t.lr * sqrtf((float)g.n));
-  tiles(tx, [&](int n, int i0, int j0) {
-    const int i = i0 + row;
-    int64_t el[4];
-    float w[4];
+    // X X'
+    if (room.shares == 1) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = j0 + col + e;
-      el[e] = i >= g.m || j >= g.n ? -1 : g.tall ? element(g, at.matrix, j, i) : element(g, at.matrix, i, j);
-      w[e] = !t.out && el[e] >= 0 ? t.p[el[e]] : 0.f;
-    }
+      for (int n = 0; n < NG; ++n) {
+        const int tile = nth(n);
+        if (tile >= ts) break;
+        int i0, j0;
+        sym_tile(tile, i0, j0);
+        put_sym(A, rows_product(X, lx, px, i0, j0, 0, g.np) * UNSCALE, i0, j0);
+      }
+    } else {
+      const int n = wave / room.shares, share = wave % room.shares;
+      int i0, j0;
+      sym_tile(n, i0, j0);
+      const int each = (g.np / 32 + room.shares - 1) / room.shares * 32;
+      f32x16 v = {};
+      if (n < ts) v = rows_product(X, lx, px, i0, j0, min(share * each, g.np), min((share + 1) * each, g.np));
+      if (n < ts && share > 0)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (el[e] < 0) continue;
-      if (t.out) {
-        st_f(t.out, (size_t)el[e], held[n][e] * scale, t.dt);
-      } else {
-        w[e] = w[e] * t.decay - held[n][e] * scale;
-        t.p[el[e]] = w[e];
-        if (t.shadow) t.shadow[el[e]] = f32_to_bf16(w[e]);
+        for (int q = 0; q < 4; ++q)
+          parts[((n * room.shares + share) * 4 + q) * 64 + lane] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+      __syncthreads();
+      if (n < ts && share == 0) {
+        for (int o = 1; o < room.shares; ++o)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float4 b = parts[((n * room.shares + o) * 4 + q) * 64 + lane];
+            v[4 * q] += b.x; v[4 * q + 1] += b.y; v[4 * q + 2] += b.z; v[4 * q + 3] += b.w;
+          }
+        put_sym(A, v * UNSCALE, i0, j0);
       }
     }
-  });
+    __syncthreads();
+    // b A + c A A
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+      const int tile = nth(n);
+      if (tile >= ts) break;
+      int i0, j0;
+      sym_tile(tile, i0, j0);
+      held[n] = add_old(A + (i0 + row) * la + j0 + col, pa, rows_product(A, la, pa, i0, j0, 0, g.mp), NS_B * t2, NS_C * t2 * t2, 1.f);
+    }
+    if (!room.two_a) __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+      const int tile = nth(n);
+      if (tile >= ts) break;
+      int i0, j0;
+      sym_tile(tile, i0, j0);
+      put_sym(B, held[n], i0, j0);
+    }
+    __syncthreads();
+    // a X + (that) X
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int tile = nth(n), i0 = tile / tx * 32, j0 = tile % tx * 32;
+      if (tile >= ta * tx) break;
+      held[n] = add_old(X + (i0 + row) * lx + j0 + col, px, columns_product(X, i0, j0), NS_A, 1.f, shrink.ratio);
+    }
+    if (k + 1 == steps) break;
+    if (!room.two_x) __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int tile = nth(n), i0 = tile / tx * 32, j0 = tile % tx * 32;
+      if (tile >= ta * tx) break;
+      put(XN + (i0 + row) * lx + j0 + col, px, held[n], nullptr);
+    }
+    _Float16* const swap = X;
+    X = XN; XN = swap;
+    __syncthreads();
+  }
+  // ---- the result, from LDS in the same pieces
+  float* R = (float*)XN;                               // rows of lx floats, as large as the planes
+  const float scale = UNSCALE * shrink_of(t0, steps - 1).next * (MUON ? 0.2f * t.lr * sqrtf((float)g.n) : 1.f);
+  if (!room.two_x) __syncthreads();
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int tile = nth(n), i0 = tile / tx * 32, j0 = tile % tx * 32;
+    if (tile >= ta * tx) break;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *(float4*)(R + (i0 + row) * lx + j0 + col + 8 * q) =
+          make_float4(held[n][4 * q] * scale, held[n][4 * q + 1] * scale, held[n][4 * q + 2] * scale, held[n][4 * q + 3] * scale);
+  }
+  __syncthreads();
+  // eight of a row of the caller's
+  const int segs = g.tall ? (g.m + 7) / 8 : (g.n + 7) / 8, rows = g.tall ? g.n : g.m;
+  for (int q = tid; q < rows * segs; q += SMALL_THREADS) {
+    const int r = q / segs, c = (q - r * segs) * 8;
+    float v[8];
+    if (g.tall) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = R[(c + k) * lx + r];
+    } else {
+      const float4 a = *(const float4*)(R + r * lx + c), b = *(const float4*)(R + r * lx + c + 4);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+    store_eight(t, quads, element(g, at.matrix, r, c), (g.tall ? g.m : g.n) - c, v);
+  }
 }
-template <int NT> int launch_small(hipStream_t s, const OrthoPlan& p, const Source& src, const Target& dst, int steps, int matrices, int lds) {
-  static OncePerDevice once;
-  PPLL_TRY(raise_lds((const void*)small_kernel<NT>, ORTHO_SMALL_LDS, once));
-  hipLaunchKernelGGL((small_kernel<NT>), dim3(matrices), dim3(SMALL_THREADS), lds, s, p, src, dst, steps);
+template <int NT, int NG> int launch_small(hipStream_t s, const OrthoPlan& p, const Source& src, const Target& dst, int steps, int matrices, int lds) {
+  static OncePerDevice once, once_muon;
+  if (src.in) {
+    PPLL_TRY(raise_lds((const void*)small_kernel<NT, NG, false>, ORTHO_SMALL_LDS, once));
+    hipLaunchKernelGGL((small_kernel<NT, NG, false>), dim3(matrices), dim3(SMALL_THREADS), lds, s, p, src, dst, steps);
+  } else {
+    PPLL_TRY(raise_lds((const void*)small_kernel<NT, NG, true>, ORTHO_SMALL_LDS, once_muon));
+    hipLaunchKernelGGL((small_kernel<NT, NG, true>), dim3(matrices), dim3(SMALL_THREADS), lds, s, p, src, dst, steps);
+  }
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }
@@ -746,18 +868,18 @@ int run(hipStream_t s, const OrthoPlan& p, const Source& src, const Target& dst,
     const OrthoGroup& g = p.g[k];
     if (g.small) {
       small += g.count;
-      tiles = g.mp / 16 * (g.np / 16) > tiles ? g.mp / 16 * (g.np / 16) : tiles;
-      lds = (int)g.small_lds() > lds ? (int)g.small_lds() : lds;
+      tiles = g.mp / 32 * (g.np / 32) > tiles ? g.mp / 32 * (g.np / 32) : tiles;
+      lds = small_room(g).bytes > lds ? (int)small_room(g).bytes : lds;
     } else {
       pieces += (int64_t)g.count * g.pieces();
       squares += (int64_t)g.count * (g.mp / 64) * (g.np / 64);
     }
   }
   if (small) {
-    const int turns = (tiles + SMALL_WAVES - 1) / SMALL_WAVES;
-    if (turns <= 1) PPLL_TRY(launch_small<1>(s, p, src, dst, steps, small, lds));
-    else if (turns <= 3) PPLL_TRY(launch_small<3>(s, p, src, dst, steps, small, lds));
-    else PPLL_TRY(launch_small<SMALL_TURNS>(s, p, src, dst, steps, small, lds));
+    const int turns = (tiles + SMALL_WAVES - 1) / SMALL_WAVES;      // (eight tiles of X: three of the symmetric matrices at most; 16: ten)
+    if (turns <= 1) PPLL_TRY((launch_small<1, 1>(s, p, src, dst, steps, small, lds)));
+    else if (turns <= 2) PPLL_TRY((launch_small<2, 2>(s, p, src, dst, steps, small, lds)));
+    else PPLL_TRY((launch_small<SMALL_TURNS, 2>(s, p, src, dst, steps, small, lds)));
   }
   if (!pieces) return PPLL_OK;
   hipLaunchKernelGGL(squares_kernel, dim3((unsigned)pieces), dim3(256), 0, s, p, src, ws);

@@ -105,7 +105,7 @@ int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* pla
     o.tall = g.rows > g.cols;
     o.m = o.tall ? g.cols : g.rows; o.n = o.tall ? g.rows : g.cols;
     o.mp = (int32_t)pad(o.m, 32); o.np = (int32_t)pad(o.n, 32);
-    o.small = o.small_lds() <= ORTHO_SMALL_LDS;
+    o.small = small_room(o).bytes <= ORTHO_SMALL_LDS;
     if (!o.small) { o.mp = (int32_t)pad(o.m, 64); o.np = (int32_t)pad(o.n, 64); }
   }
   std::stable_sort(plan->g, plan->g + plan->n, [](const OrthoGroup& a, const OrthoGroup& b) { return a.np > b.np; });

@@ -13,7 +13,6 @@ constexpr int ORTHO_STEPS = 16;        // Newton-Schulz steps, at most
 constexpr int NORM_ROWS = 32, NORM_COLS = 256;   // piece of a matrix whose squares one workgroup adds up
 
 constexpr int ORTHO_SMALL_LDS = 160 * 1024 - 256;   // what a workgroup of the small kernel may have (256 bytes are its own)
-constexpr int ORTHO_SMALL_ELEMENTS = ORTHO_SMALL_LDS / 4;
 
 // A group as the kernels see it.  A matrix is worked on as X [m][n] with m <= n (transposed where rows > cols), padded with zeros to
 // mp x np: zero rows and columns stay zero through every product, so no product has a border.  Each intermediate is two planes of fp16,
@@ -28,9 +27,21 @@ struct OrthoGroup {
   int64_t x[2], a, b;
   __host__ __device__ int64_t plane_x() const { return (int64_t)mp * np; }      // elements
   __host__ __device__ int64_t plane_a() const { return (int64_t)mp * mp; }
-  __host__ __device__ int64_t small_lds() const { return 4 * ((int64_t)mp * (np + 8) + (int64_t)mp * (mp + 8)); }   // bytes: X and A
   __host__ __device__ int pieces() const { return ((rows + NORM_ROWS - 1) / NORM_ROWS) * ((cols + NORM_COLS - 1) / NORM_COLS); }
 };
+// The small kernel's LDS: X and A, in whole tiles of 32 x 32 and at most four of them a side for A; where there is room a second X and a second
+// A, and sums of shares of the k where A has few tiles.
+struct SmallRoom { int64_t bytes; int32_t two_x, two_a, shares; };
+__host__ __device__ inline SmallRoom small_room(const OrthoGroup& g) {
+  const int64_t x = 4 * (int64_t)g.mp * (g.np + 8), a = 4 * (int64_t)g.mp * (g.mp + 8);
+  SmallRoom r{x + a, 0, 0, 1};
+  if (g.mp > 128) { r.bytes = (int64_t)1 << 40; return r; }
+  const int shares = g.mp == 32 ? 8 : g.mp == 64 && g.np >= 192 ? 2 : 1, tiles = g.mp == 32 ? 1 : 4;
+  if (shares > 1 && r.bytes + shares * tiles * 4096 <= ORTHO_SMALL_LDS) { r.shares = shares; r.bytes += shares * tiles * 4096; }
+  if (r.bytes + a <= ORTHO_SMALL_LDS) { r.two_a = 1; r.bytes += a; }
+  if (r.bytes + x <= ORTHO_SMALL_LDS) { r.two_x = 1; r.bytes += x; }
+  return r;
+}
 // The products of a step: X X', then b A + c A A, then the product of that and X.
 enum { ORTHO_GRAM = 0, ORTHO_POLY = 1, ORTHO_APPLY = 2 };
 __host__ __device__ inline int tiles_of_matrix(const OrthoGroup& g, int tile, int phase) {
