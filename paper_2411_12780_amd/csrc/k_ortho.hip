@@ -61,6 +61,13 @@ template <int N> __device__ __forceinline__ Terms<N> split_all(const float* v) {
   }
   return r;
 }
+// a / b for a >= 0, b > 0 and a quotient under 2^21 (tiles of a side, matrices of a group): in fp32 it is off by less than one
+__device__ __forceinline__ int quotient(int a, int b) {
+  int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b));
+  const int r = a - q * b;
+  return r < 0 ? q - 1 : r >= b ? q + 1 : q;
+}
+__device__ __forceinline__ bool in_quads(const OrthoGroup& g) { return ((g.offset | g.stride | g.ld) & 3) == 0; }   // rows' pieces of four are aligned
 __device__ __forceinline__ int64_t element(const OrthoGroup& g, int matrix, int r, int c) {
   return g.offset + (int64_t)matrix * g.stride + (int64_t)r * g.ld + c;
 }
@@ -84,45 +91,39 @@ __device__ __forceinline__ float read_u(const Source& s, int64_t at) {
   return s.nesterov ? fmaf(s.momentum, m, s.g[at]) : m;
 }
 
-__device__ __forceinline__ bool in_quads(const OrthoGroup& g) { return ((g.offset | g.stride | g.ld) & 3) == 0; }   // rows' pieces of four are aligned
-// The first n (at most eight) of eight values, to elements e .. of the result or as the update of the parameters there
-__device__ __forceinline__ void store_eight(const Target& t, bool quads, int64_t e, int n, const float* v) {
+// What the update of the first n (at most eight) parameters from element e on starts from
+__device__ __forceinline__ void load_eight(const Target& t, bool quads, int64_t e, int n, float* w) {
   if (quads && n >= 8) {
-    float w[8];
-    if (!t.out) {
-      const float4 a = *(const float4*)(t.p + e), b = *(const float4*)(t.p + e + 4);
-      const float old[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    const float4 a = *(const float4*)(t.p + e), b = *(const float4*)(t.p + e + 4);
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+  } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = old[k] * t.decay - v[k];
-    } else {
+    for (int k = 0; k < 8; ++k) w[k] = k < n ? t.p[e + k] : 0.f;
+  }
+}
+// ... and the values themselves: as the result, or (MUON) as the update of the w that were there
+template <bool MUON> __device__ __forceinline__ void store_eight(const Target& t, bool quads, int64_t e, int n, const float* v, const float* w) {
+  float x[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = v[k];
+  for (int k = 0; k < 8; ++k) x[k] = MUON ? w[k] * t.decay - v[k] : v[k];
+  float* to = MUON ? t.p : t.dt == F32 ? (float*)t.out : nullptr;
+  uint16_t* half = MUON ? t.shadow : t.dt == BF16 ? (uint16_t*)t.out : nullptr;
+  if (quads && n >= 8) {
+    if (to) {
+      *(float4*)(to + e) = make_float4(x[0], x[1], x[2], x[3]);
+      *(float4*)(to + e + 4) = make_float4(x[4], x[5], x[6], x[7]);
     }
-    if (!t.out || t.dt == F32) {
-      float* to = (t.out ? (float*)t.out : t.p) + e;
-      *(float4*)to = make_float4(w[0], w[1], w[2], w[3]);
-      *(float4*)(to + 4) = make_float4(w[4], w[5], w[6], w[7]);
-    }
-    uint16_t* half = t.out ? t.dt == BF16 ? (uint16_t*)t.out : nullptr : t.shadow;
     if (half) {
-      *(uint2*)(half + e) = make_uint2(f32x2_to_bf16x2(w[0], w[1]), f32x2_to_bf16x2(w[2], w[3]));
-      *(uint2*)(half + e + 4) = make_uint2(f32x2_to_bf16x2(w[4], w[5]), f32x2_to_bf16x2(w[6], w[7]));
+      *(uint2*)(half + e) = make_uint2(f32x2_to_bf16x2(x[0], x[1]), f32x2_to_bf16x2(x[2], x[3]));
+      *(uint2*)(half + e + 4) = make_uint2(f32x2_to_bf16x2(x[4], x[5]), f32x2_to_bf16x2(x[6], x[7]));
     }
     return;
   }
-  float w[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) w[k] = !t.out && k < n ? t.p[e + k] : 0.f;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     if (k >= n) continue;
-    if (t.out) {
-      st_f(t.out, (size_t)(e + k), v[k], t.dt);
-    } else {
-      w[k] = w[k] * t.decay - v[k];
-      t.p[e + k] = w[k];
-      if (t.shadow) t.shadow[e + k] = f32_to_bf16(w[k]);
-    }
+    if (to) to[e + k] = x[k];
+    if (half) half[e + k] = f32_to_bf16(x[k]);
   }
 }
 
@@ -131,27 +132,53 @@ __global__ __launch_bounds__(256) void squares_kernel(OrthoPlan p, Source s, cha
   int id = blockIdx.x;
   const Place at = place_of(p, id, [](const OrthoGroup& g) { return g.small ? 0 : g.pieces(); });
   const OrthoGroup& g = p.g[at.group];
-  const int across = (g.cols + NORM_COLS - 1) / NORM_COLS, r0 = id / across * NORM_ROWS, c = id % across * NORM_COLS + threadIdx.x;
+  const int across = (g.cols + NORM_COLS - 1) / NORM_COLS, r0 = id / across * NORM_ROWS, c0 = id % across * NORM_COLS;
   double sum = 0;
-  const int64_t first = element(g, at.matrix, r0, c);
-  const int rows = c < g.cols ? min(NORM_ROWS, g.rows - r0) : 0;
-  for (int r = 0; r < rows; r += 8) {        // eight rows on their way at a time
-    float u[8], m[8];
+  if (in_quads(g) && r0 + NORM_ROWS <= g.rows && c0 + NORM_COLS <= g.cols && !(s.in && s.dt != F32)) {
+    // a wave's rows, 16 bytes a lane, all of them on their way at once
+    const int64_t first = element(g, at.matrix, r0 + (threadIdx.x >> 6) * (NORM_ROWS / 4), c0 + (threadIdx.x & 63) * 4);
+    float4 u[NORM_ROWS / 4], m[NORM_ROWS / 4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int64_t e = first + (int64_t)(r + k) * g.ld;
-      const bool on = r + k < rows;
-      u[k] = !on ? 0.f : s.in ? ld_f(s.in, (size_t)e, s.dt) : s.g[e];
-      m[k] = on && !s.in ? s.m[e] : 0.f;
+    for (int k = 0; k < NORM_ROWS / 4; ++k) {
+      u[k] = *(const float4*)((s.in ? (const float*)s.in : s.g) + first + k * g.ld);
+      if (!s.in) m[k] = *(const float4*)(s.m + first + k * g.ld);
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < NORM_ROWS / 4; ++k) {
+      float v[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
       if (!s.in) {
-        m[k] = fmaf(s.momentum, m[k], u[k]);
-        if (r + k < rows) s.m[first + (int64_t)(r + k) * g.ld] = m[k];
-        u[k] = s.nesterov ? fmaf(s.momentum, m[k], u[k]) : m[k];
+        float w[4] = {m[k].x, m[k].y, m[k].z, m[k].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          w[e] = fmaf(s.momentum, w[e], v[e]);
+          v[e] = s.nesterov ? fmaf(s.momentum, w[e], v[e]) : w[e];
+        }
+        *(float4*)(s.m + first + k * g.ld) = make_float4(w[0], w[1], w[2], w[3]);
       }
-      sum += (double)u[k] * u[k];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += (double)v[e] * v[e];
+    }
+  } else {
+    const int c = c0 + threadIdx.x, rows = c < g.cols ? min(NORM_ROWS, g.rows - r0) : 0;
+    const int64_t first = element(g, at.matrix, r0, c);
+    for (int r = 0; r < rows; r += 8) {        // eight rows on their way at a time
+      float u[8], m[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int64_t e = first + (int64_t)(r + k) * g.ld;
+        const bool on = r + k < rows;
+        u[k] = !on ? 0.f : s.in ? ld_f(s.in, (size_t)e, s.dt) : s.g[e];
+        m[k] = on && !s.in ? s.m[e] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (!s.in) {
+          m[k] = fmaf(s.momentum, m[k], u[k]);
+          if (r + k < rows) s.m[first + (int64_t)(r + k) * g.ld] = m[k];
+          u[k] = s.nesterov ? fmaf(s.momentum, m[k], u[k]) : m[k];
+        }
+        sum += (double)u[k] * u[k];
+      }
     }
   }
   __shared__ double sums[256];
@@ -172,6 +199,17 @@ __global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, c
   const int t = threadIdx.x, i0 = id / (g.np / 64) * 64, j0 = id % (g.np / 64) * 64;
   __shared__ double sums[256];
   __shared__ float tile[64][65];
+  const int r0 = g.tall ? j0 : i0, c0 = g.tall ? i0 : j0;                // in the caller's orientation: rows y of the tile
+  const bool whole = in_quads(g) && r0 + 64 <= g.rows && c0 + 64 <= g.cols && !(s.in && s.dt != F32);
+  float4 u[4], m[4];
+  if (whole) {                                                           // (on their way under the sum)
+    const int64_t first = element(g, at.matrix, r0 + t / 16, c0 + t % 16 * 4);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      u[k] = *(const float4*)((s.in ? (const float*)s.in : s.g) + first + k * 16 * g.ld);
+      if (!s.in) m[k] = *(const float4*)(s.m + first + k * 16 * g.ld);
+    }
+  }
   const double* part = (const double*)(ws + p.partials) + g.first_piece + at.matrix * g.pieces();
   double sum = 0;
   for (int k = t; k < g.pieces(); k += 256) sum += part[k];
@@ -183,12 +221,23 @@ __global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, c
   }
   const double norm = sqrt(sums[0]), inv = norm > 0 ? SCALE / norm : norm;      // NaN stays one
   if (id == 0 && t == 0) ((float*)(ws + p.shrink))[g.first + at.matrix] = (float)(norm / (norm + NORM_EPS));
-  for (int k = 0; k < 16; ++k) {
-    const int y = k * 4 + t / 64, x = t % 64;                  // in the caller's orientation: rows y
-    const int r = (g.tall ? j0 : i0) + y, c = (g.tall ? i0 : j0) + x;
-    const float v = r < g.rows && c < g.cols ? (float)(read_u(s, element(g, at.matrix, r, c)) * inv) : 0.f;
+  auto put = [&](int y, int x, float v) {
     if (g.tall) tile[x][y] = v;
     else tile[y][x] = v;
+  };
+  if (whole) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float v[4] = {u[k].x, u[k].y, u[k].z, u[k].w}, w[4] = {m[k].x, m[k].y, m[k].z, m[k].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        put(k * 16 + t / 16, t % 16 * 4 + e, (float)((s.in ? v[e] : s.nesterov ? fmaf(s.momentum, w[e], v[e]) : w[e]) * inv));
+    }
+  } else {
+    for (int k = 0; k < 16; ++k) {
+      const int y = k * 4 + t / 64, x = t % 64, r = r0 + y, c = c0 + x;
+      put(y, x, r < g.rows && c < g.cols ? (float)(read_u(s, element(g, at.matrix, r, c)) * inv) : 0.f);
+    }
   }
   __syncthreads();
   const int64_t plane = g.plane_x();
@@ -216,7 +265,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, c
 // Layouts in LDS, as in gemm_pipe.h: k contiguous (P, and Q of GRAM and POLY): rows of KT k, their 16-byte granules permuted; k rows (X of APPLY):
 // rows of TILE columns whose 64-byte windows are permuted, for the transposing read.
 template <int TILE> struct Tile {
-  static constexpr int KT = TILE == 128 ? 32 : 64, PLANE = TILE * KT * 2, STAGE = 4 * PLANE, LDS = 2 * STAGE;
+  static constexpr int KT = TILE == 128 ? 32 : 64, PLANE = TILE * KT * 2, STAGE = 4 * PLANE;
   static constexpr int PITCH = TILE * 2;                     // of a k row
   static constexpr int R32 = 32 * KT * 2;                    // 32 rows with k contiguous
 };
@@ -268,15 +317,23 @@ __device__ __forceinline__ void k_step(f32x16 (&hh)[2][2], f32x16 (&xx)[2][2], c
   }
 }
 
-template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_kernel(OrthoPlan p, XcdShares shares, Target t, char* ws, int step) {
+template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) void product_kernel(OrthoPlan p, OrthoProduct tiles, Target t, char* ws, int step) {
   using S = Tile<TILE>;
   constexpr bool TR = MODE >= APPLY;
-  extern __shared__ __align__(16) char stages[];
+  extern __shared__ __align__(256) char stages[];
+  PPLL_CODE_TO_L2(2);
+  // ---- which tile
   const int xcd = blockIdx.x & 7;
-  int id = shares.first[xcd] + (int)(blockIdx.x >> 3);
-  if (id >= shares.first[xcd + 1]) return;
-  const Place at = place_of(p, id, [](const OrthoGroup& g) { return tiles_of_matrix(g, TILE, MODE); });
-  const OrthoGroup& g = p.g[at.group];
+  int id = tiles.first[xcd] + (int)(blockIdx.x >> 3);
+  if (id >= tiles.first[xcd + 1]) return;
+  int group = 0, begin = 0;
+#pragma unroll
+  for (int k = 1; k < ORTHO_GROUPS; ++k)               // (all bounds are read at once)
+    if (id >= tiles.begin[k]) { group = k; begin = tiles.begin[k]; }
+  const OrthoGroup& g = p.g[group];
+  id -= begin;
+  const int matrix = quotient(id, tiles.each[group]);
+  id -= matrix * tiles.each[group];
   int bi, bj;
   if (MODE <= POLY) {
     bi = (int)((sqrtf(8.f * id + 1.f) - 1.f) * 0.5f);
@@ -285,13 +342,13 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
     bj = id - bi * (bi + 1) / 2;
   } else {
     const int down = (g.mp + TILE - 1) / TILE;         // tiles that read the same columns of X follow one another
-    bj = id / down; bi = id - bj * down;
+    bj = quotient(id, down); bi = id - bj * down;
   }
   const int64_t px = g.plane_x(), pa = g.plane_a();
   const int from = step & 1;
-  _Float16* X = (_Float16*)(ws + g.x[from]) + at.matrix * 2 * px;
-  _Float16* A = (_Float16*)(ws + g.a) + at.matrix * 2 * pa;
-  _Float16* B = (_Float16*)(ws + g.b) + at.matrix * 2 * pa;
+  _Float16* X = (_Float16*)(ws + g.x[from]) + matrix * 2 * px;
+  _Float16* A = (_Float16*)(ws + g.a) + matrix * 2 * pa;
+  _Float16* B = (_Float16*)(ws + g.b) + matrix * 2 * pa;
   const int K = MODE == GRAM ? g.np : g.mp, nk = K / S::KT;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -355,26 +412,26 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
   else wait_vm<0>();
   barrier();
   k_step<TILE, TR>(hh, xx, f1, f0, rp, rq);         // the first fragments: products with zeros under the reads
+  auto ready = [&](int i) {                         // stage i + 1 is in LDS, stage i is filled again; where stage i + 1 begins
+    wait_vm<0>();                                   // this wave's part
+    barrier();                                      // and everyone's; nobody reads stage i any more
+    issue(i + 2);
+    return (i + 1 & 1) * S::STAGE;
+  };
   if constexpr (TILE == 128) {
+    int st = 0;
     for (int i = 0; i < nk; ++i) {
-      const int st = (i & 1) * S::STAGE, nx = S::STAGE - st;
-      k_step<TILE, TR>(hh, xx, f0, f1, TILE == 128 ? (rp ^ 32) + st : 0, (TR ? rq + NEXT_Q : rq ^ 32) + st);
-      wait_vm<0>();         // this wave's part of stage i + 1 is in LDS
-      barrier();            // and everyone's; nobody reads stage i any more
-      issue(i + 2);
-      k_step<TILE, TR>(hh, xx, f1, f0, rp + nx, rq + nx);
+      k_step<TILE, TR>(hh, xx, f0, f1, (rp ^ 32) + st, (TR ? rq + NEXT_Q : rq ^ 32) + st);
+      st = ready(i);
+      k_step<TILE, TR>(hh, xx, f1, f0, rp + st, rq + st);
     }
   } else {
     for (int i = 0; i < nk; i += 2) {
-      wait_vm<0>();
-      barrier();
-      issue(i + 2);
-      k_step<TILE, TR>(hh, xx, f0, f1, rp + S::STAGE, rq + S::STAGE);
+      const int st = ready(i);
+      k_step<TILE, TR>(hh, xx, f0, f1, rp + st, rq + st);
       if (i + 1 >= nk) break;
-      wait_vm<0>();
-      barrier();
-      issue(i + 3);
-      k_step<TILE, TR>(hh, xx, f1, f0, rp, rq);
+      const int nx = ready(i + 1);
+      k_step<TILE, TR>(hh, xx, f1, f0, rp + nx, rq + nx);
     }
   }
   asm volatile("s_nop 15\n s_nop 3" ::: "memory");    // the last products are through before a vector instruction reads the accumulators
@@ -387,48 +444,96 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
 #pragma unroll
     for (int i = 0; i < 2; ++i) hh[j][i] += xx[j][i];
 
-  // ---- epilogue: through LDS, so that a wave reads and writes whole 16-byte pieces of whole cache lines
-  const Shrink shrink = shrink_of(((const float*)(ws + p.shrink))[g.first + at.matrix], step);
-  const float poly_b = NS_B * shrink.now * shrink.now, poly_c = NS_C * shrink.now * shrink.now * shrink.now * shrink.now;
+  // ---- epilogue: through LDS, so that a wave reads and writes whole 16-byte pieces of whole cache lines.  A wave finishes PASSES times ROWS rows
+  // of 64 columns: lane l pieces of eight at columns 8 (l % 8) of rows l / 8 + 8 n.  What lies past the padded size (a multiple of 64) is not stored.
   constexpr int PITCH = 68;                             // floats of a row of 64 and room: rows 4 banks apart
-  // rows r0 .. of `sums`, which holds the products of rows i0 .. and columns j0 .. j0 + 63: finished and stored; `again`: the finished values
-  // go back to `sums`, for the mirrored tile
-  auto store_rows = [&](float* sums, int rows, int i0, int j0, bool again) {
-    const int seg = (lane & 7) * 8;
+  constexpr int ROWS = TILE == 128 ? 32 : 16, PASSES = TILE == 128 ? 2 : 1, EACH = ROWS / 8;
+  const int i0 = TILE == 128 ? bi * 128 + wi * 64 : bi * 64 + wave * 16, j0 = TILE == 128 ? bj * 128 + wj * 64 : bj * 64;
+  const bool live = i0 < g.mp && j0 < (MODE <= POLY ? g.mp : g.np), mirrored = MODE <= POLY && bi != bj;
+  const int r8 = lane >> 3, seg = (lane & 7) * 8;
+  const int64_t ld = MODE >= APPLY ? g.np : g.mp, pl = MODE >= APPLY ? px : pa;
+  const bool quads = in_quads(g);
+  // all that the epilogue reads is on its way before the sums go through LDS: A or X, and of the last product the parameters (of tall matrices
+  // in the caller's orientation: eight of a row there, columns i of the tile, ROWS / 8 lanes a row)
+  f16x8 old_h[PASSES * EACH], old_l[PASSES * EACH];
+  constexpr int SEGS = ROWS / 8, TURNS = 64 * SEGS / 64;
+  float w[MODE == LAST && MUON ? PASSES * EACH : 1][8];
+  auto place = [&](int ps, int n, int& i, int& j) { i = i0 + ps * ROWS + r8 + 8 * n; j = j0 + seg; };
+  auto place_tall = [&](int ps, int n, int& i, int& j) { i = i0 + ps * ROWS + lane % SEGS * 8; j = j0 + lane / SEGS + n * (64 / SEGS); };
+  static_assert(TURNS == EACH, "");
+  if (live) {
 #pragma unroll
-    for (int r = lane >> 3; r < rows; r += 8) {
-      float* from_lds = sums + r * PITCH + seg;
+    for (int ps = 0; ps < PASSES; ++ps)
+#pragma unroll
+      for (int n = 0; n < EACH; ++n) {
+        int i, j;
+        if (MODE != GRAM) {
+          place(ps, n, i, j);
+          const _Float16* add = (MODE == POLY ? A : X) + i * ld + j;
+          old_h[ps * EACH + n] = *(const f16x8*)add;
+          old_l[ps * EACH + n] = *(const f16x8*)(add + pl);
+        }
+        if (MODE == LAST && MUON) {
+          if (!g.tall) {
+            place(ps, n, i, j);
+            load_eight(t, quads, element(g, matrix, i, j), i < g.m ? g.n - j : 0, w[ps * EACH + n]);
+          } else {
+            place_tall(ps, n, i, j);
+            load_eight(t, quads, element(g, matrix, j, i), j < g.n ? g.m - i : 0, w[ps * EACH + n]);
+          }
+        }
+      }
+  }
+  const Shrink shrink = shrink_of(((const float*)(ws + p.shrink))[g.first + matrix], step);
+  const float poly_b = NS_B * shrink.now * shrink.now, poly_c = NS_C * shrink.now * shrink.now * shrink.now * shrink.now * UNSCALE;
+  const float scale = MODE == LAST ? shrink.ratio * shrink.next * UNSCALE * (MUON ? 0.2f * t.lr * sqrtf((float)g.n) : 1.f) : shrink.ratio;
+  // rows r0 .. of `sums`, which holds the products
+  auto finish = [&](float* sums, int ps) {
+#pragma unroll
+    for (int n = 0; n < EACH; ++n) {
+      int i, j;
+      place(ps, n, i, j);
+      float* from_lds = sums + (r8 + 8 * n) * PITCH + seg;
       const float4 lo4 = *(const float4*)from_lds, hi4 = *(const float4*)(from_lds + 4);
       float v[8] = {lo4.x, lo4.y, lo4.z, lo4.w, hi4.x, hi4.y, hi4.z, hi4.w};
-      const int ld = MODE == APPLY ? g.np : g.mp;
-      const int64_t at_e = (int64_t)(i0 + r) * ld + j0 + seg, pl = MODE == APPLY ? px : pa;
-      if (MODE != GRAM) {
-        const _Float16* add = (MODE == POLY ? A : X) + at_e;
-        const f16x8 h = *(const f16x8*)add, l = *(const f16x8*)(add + pl);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float old = (float)h[k] + (float)l[k];
-          v[k] = MODE == POLY ? fmaf(poly_b, old, poly_c * (v[k] * UNSCALE)) : fmaf(NS_A, old, v[k] * UNSCALE) * shrink.ratio;
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= UNSCALE;
+      for (int k = 0; k < 8; ++k) {
+        const float old = MODE == GRAM ? 0.f : (float)old_h[ps * EACH + n][k] + (float)old_l[ps * EACH + n][k];
+        v[k] = MODE == GRAM ? v[k] * UNSCALE : MODE == POLY ? fmaf(poly_b, old, poly_c * v[k]) : fmaf(NS_A, old, v[k] * UNSCALE) * scale;
       }
-      if (again) {
+      if (mirrored || (MODE == LAST && g.tall)) {
         *(float4*)from_lds = make_float4(v[0], v[1], v[2], v[3]);
         *(float4*)(from_lds + 4) = make_float4(v[4], v[5], v[6], v[7]);
       }
-      const Terms<8> v2 = split_all<8>(v);
-      _Float16* to = (MODE == GRAM ? A : MODE == POLY ? B : (_Float16*)(ws + g.x[from ^ 1]) + at.matrix * 2 * px) + at_e;
-      *(f16x8*)to = v2.hi;
-      *(f16x8*)(to + pl) = v2.lo;
+      if (MODE != LAST) {
+        const Terms<8> v2 = split_all<8>(v);
+        _Float16* to = (MODE == GRAM ? A : MODE == POLY ? B : (_Float16*)(ws + g.x[from ^ 1]) + matrix * 2 * px) + i * ld + j;
+        *(f16x8*)to = v2.hi;
+        *(f16x8*)(to + pl) = v2.lo;
+      } else if (!g.tall && i < g.m && j < g.n) {
+        store_eight<MUON>(t, quads, element(g, matrix, i, j), g.n - j, v, w[MUON ? ps * EACH + n : 0]);
+      }
+    }
+  };
+  auto finish_tall = [&](const float* sums, int ps) {
+#pragma unroll
+    for (int n = 0; n < TURNS; ++n) {
+      int i, j;
+      place_tall(ps, n, i, j);
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = sums[(i - i0 - ps * ROWS + k) * PITCH + j - j0];
+      if (i < g.m && j < g.n) store_eight<MUON>(t, quads, element(g, matrix, j, i), g.m - i, v, w[MUON ? ps * EACH + n : 0]);
     }
   };
   // columns c0 .. c0 + cols - 1 of `rows` (a multiple of 8) finished rows, as rows of the mirrored tile
-  auto store_mirrored = [&](const float* sums, int rows, int i0, int c0, int cols, int j0) {
+  auto finish_mirrored = [&](const float* sums, int rows, int i0, int c0, int cols) {
     const int segs = rows / 8, seg = lane % segs * 8;
     _Float16* D = MODE == GRAM ? A : B;
-    for (int c = c0 + lane / segs; c < c0 + cols; c += 64 / segs) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int c = c0 + lane / segs + n * (64 / segs);
+      if (c >= c0 + cols) break;
       float v[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = sums[(seg + k) * PITCH + c];
@@ -436,36 +541,6 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
       _Float16* to = D + (int64_t)(j0 + c) * g.mp + i0 + seg;
       *(f16x8*)to = v2.hi;
       *(f16x8*)(to + pa) = v2.lo;
-    }
-  };
-  // the result: rows r0 .. of `sums`; where the matrix is tall the caller's rows are columns of `sums`
-  auto store_result = [&](float* sums, int r0, int rows, int i0, int j0) {
-    const float scale = UNSCALE * shrink.next * (t.out ? 1.f : 0.2f * t.lr * sqrtf((float)g.n));
-    const int seg = (lane & 7) * 8;
-    const bool quads = in_quads(g);
-    for (int r = r0 + (lane >> 3); r < r0 + rows; r += 8) {
-      float* from_lds = sums + r * PITCH + seg;
-      const float4 lo4 = *(const float4*)from_lds, hi4 = *(const float4*)(from_lds + 4);
-      float v[8] = {lo4.x, lo4.y, lo4.z, lo4.w, hi4.x, hi4.y, hi4.z, hi4.w};
-      const _Float16* add = X + (int64_t)(i0 + r) * g.np + j0 + seg;
-      const f16x8 h = *(const f16x8*)add, l = *(const f16x8*)(add + px);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = fmaf(NS_A, (float)h[k] + (float)l[k], v[k] * UNSCALE) * shrink.ratio * scale;
-      if (!g.tall) {
-        if (i0 + r < g.m && j0 + seg < g.n) store_eight(t, quads, element(g, at.matrix, i0 + r, j0 + seg), g.n - j0 - seg, v);
-      } else {
-        *(float4*)from_lds = make_float4(v[0], v[1], v[2], v[3]);
-        *(float4*)(from_lds + 4) = make_float4(v[4], v[5], v[6], v[7]);
-      }
-    }
-    if (!g.tall) return;
-    wave_sync();
-    const int segs = rows / 8, i = i0 + r0 + lane % segs * 8;
-    for (int c = lane / segs; c < 64; c += 64 / segs) {
-      float v[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = sums[(r0 + lane % segs * 8 + k) * PITCH + c];
-      if (i < g.m && j0 + c < g.n) store_eight(t, quads, element(g, at.matrix, j0 + c, i), g.m - i, v);
     }
   };
   // a 32 x 32 tile of sums: lane l holds row l % 32, columns 8 q + 4 (l / 32) + e in element 4 q + e
@@ -477,24 +552,23 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
   };
   barrier();                                            // nobody reads a stage any more
   if constexpr (TILE == 128) {
-    // 32 rows at a time, in a part of LDS of the wave's own; what lies past the padded size (a multiple of 64) is not stored
+    // 32 rows at a time, in a part of LDS of the wave's own
     float* sums = (float*)stages + wave * 32 * PITCH;
-    const int i0 = bi * 128 + wi * 64, j0 = bj * 128 + wj * 64;
-    if (i0 >= g.mp || j0 >= (MODE <= POLY ? g.mp : g.np)) return;
+    if (!live) return;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int ps = 0; ps < 2; ++ps) {
       wave_sync();
-      put(sums, hh[0][i], 0, 0);
-      put(sums, hh[1][i], 0, 32);
+      put(sums, hh[0][ps], 0, 0);
+      put(sums, hh[1][ps], 0, 32);
       wave_sync();
-      if (MODE == LAST) {
-        store_result(sums, 0, 32, i0 + 32 * i, j0);
-      } else {
-        store_rows(sums, 32, i0 + 32 * i, j0, MODE <= POLY && bi != bj);
-        if (MODE <= POLY && bi != bj) {
-          wave_sync();
-          store_mirrored(sums, 32, i0 + 32 * i, 0, 64, j0);
-        }
+      finish(sums, ps);
+      if (MODE == LAST && g.tall) {
+        wave_sync();
+        finish_tall(sums, ps);
+      }
+      if (mirrored) {
+        wave_sync();
+        finish_mirrored(sums, 32, i0 + 32 * ps, 0, 64);
       }
     }
   } else {
@@ -523,14 +597,14 @@ template <int TILE, int MODE> __global__ __launch_bounds__(256) void product_ker
     __syncthreads();
     put(sums, acc, (wave & 1) * 32, (wave >> 1) * 32);
     __syncthreads();
-    if (MODE == LAST) {
-      store_result(sums, wave * 16, 16, bi * 64, bj * 64);
-    } else {
-      store_rows(sums + wave * 16 * PITCH, 16, bi * 64 + wave * 16, bj * 64, MODE <= POLY && bi != bj);
-      if (MODE <= POLY && bi != bj) {
-        __syncthreads();
-        store_mirrored(sums, 64, bi * 64, wave * 16, 16, bj * 64);
-      }
+    finish(sums + wave * 16 * PITCH, 0);
+    if (MODE == LAST && g.tall) {
+      wave_sync();
+      finish_tall(sums + wave * 16 * PITCH, 0);
+    }
+    if (mirrored) {
+      __syncthreads();
+      finish_mirrored(sums, 64, bi * 64, wave * 16, 16);
     }
   }
 }
@@ -833,7 +907,11 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
       const float4 a = *(const float4*)(R + r * lx + c), b = *(const float4*)(R + r * lx + c + 4);
       v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
-    store_eight(t, quads, element(g, at.matrix, r, c), (g.tall ? g.m : g.n) - c, v);
+    const int64_t e = element(g, at.matrix, r, c);
+    const int count = (g.tall ? g.m : g.n) - c;
+    float w[8];
+    if (MUON) load_eight(t, quads, e, count, w);
+    store_eight<MUON>(t, quads, e, count, v, w);
   }
 }
 template <int NT, int NG> int launch_small(hipStream_t s, const OrthoPlan& p, const Source& src, const Target& dst, int steps, int matrices, int lds) {
@@ -849,16 +927,25 @@ template <int NT, int NG> int launch_small(hipStream_t s, const OrthoPlan& p, co
   return PPLL_OK;
 }
 
-template <int MODE> int launch_product(hipStream_t s, const OrthoPlan& p, const Target& t, char* ws, int step) {
-  const int phase = MODE < APPLY ? MODE : APPLY, tile = p.tile[phase];
-  const XcdShares& shares = p.shares[phase];
+template <int TILE, int MODE> int launch_tiles(hipStream_t s, const OrthoPlan& p, const Target& t, char* ws, int step) {
+  const OrthoProduct& tiles = p.product[MODE < APPLY ? MODE : APPLY];
   int longest = 0;
-  for (int x = 0; x < 8; ++x) longest = shares.first[x + 1] - shares.first[x] > longest ? shares.first[x + 1] - shares.first[x] : longest;
-  const dim3 grid(8 * (unsigned)longest);
-  if (tile == 128) hipLaunchKernelGGL((product_kernel<128, MODE>), grid, dim3(256), Tile<128>::LDS, s, p, shares, t, ws, step);
-  else hipLaunchKernelGGL((product_kernel<64, MODE>), grid, dim3(256), Tile<64>::LDS, s, p, shares, t, ws, step);
-  PPLL_HIP(hipGetLastError());
-  return PPLL_OK;
+  for (int x = 0; x < 8; ++x) longest = tiles.first[x + 1] - tiles.first[x] > longest ? tiles.first[x + 1] - tiles.first[x] : longest;
+  auto launch = [&](auto muon, OncePerDevice& once) -> int {
+    constexpr bool MUON = decltype(muon)::value;
+    const int lds = 2 * Tile<TILE>::STAGE;
+    PPLL_TRY(raise_lds((const void*)product_kernel<TILE, MODE, MUON>, lds, once));
+    hipLaunchKernelGGL((product_kernel<TILE, MODE, MUON>), dim3(8 * (unsigned)longest), dim3(256), lds, s, p, tiles, t, ws, step);
+    PPLL_HIP(hipGetLastError());
+    return PPLL_OK;
+  };
+  static OncePerDevice once, once_muon;
+  if constexpr (MODE == LAST)
+    if (!t.out) return launch(std::true_type(), once_muon);
+  return launch(std::false_type(), once);
+}
+template <int MODE> int launch_product(hipStream_t s, const OrthoPlan& p, const Target& t, char* ws, int step) {
+  return p.product[MODE < APPLY ? MODE : APPLY].tile == 128 ? launch_tiles<128, MODE>(s, p, t, ws, step) : launch_tiles<64, MODE>(s, p, t, ws, step);
 }
 
 int run(hipStream_t s, const OrthoPlan& p, const Source& src, const Target& dst, int steps, char* ws) {

@@ -35,40 +35,48 @@ bool overlap(const Run& a, const Run& b) {
   }
   return false;
 }
-// Tiles of one of the products, and how the XCDs share them.
-// A unit gets through 32 k of a 128 x 128 tile in about 0.4 us and of a 64 x 64 one in 0.17; the larger ones are ahead where there are enough of
-// them for the units, or where one is no longer than all of the smaller ones' turns.
+// Clocks that a workgroup spends on a tile, two of them on a unit: those that every tile costs (finding its place, the first copies' way, the
+// epilogue) and those of 64 k.
+double tile_clocks(const OrthoGroup& g, int tile, int phase) {
+  const int k = phase == ORTHO_GRAM ? g.np : g.mp;
+  return tile == 128 ? 10000 + k / 64 * 3200. : 7000 + k / 64 * 1150.;
+}
+// Tiles of one of the products, and how the XCDs share them.  The tile that takes less time: rounds of 512 workgroups, and none is shorter than its
+// longest tile.
 void plan_product(OrthoPlan* p, int phase) {
+  OrthoProduct& o = p->product[phase];
   double best = 0;
   for (int tile : {128, 64}) {
     double all = 0, longest = 0;
     for (int k = 0; k < p->n; ++k) {
-      const OrthoGroup& o = p->g[k];
-      if (o.small) continue;
-      const double len = (phase == ORTHO_GRAM ? o.np : o.mp) * (tile == 128 ? 0.4 : 0.17);
-      all += (double)o.count * tiles_of_matrix(o, tile, phase) * len;
-      if (len > longest) longest = len;
+      const OrthoGroup& g = p->g[k];
+      if (g.small) continue;
+      const double one = tile_clocks(g, tile, phase);
+      all += (double)g.count * tiles_of_matrix(g, tile, phase) * one;
+      longest = std::max(longest, one);
     }
-    const double time = std::max(all / 256, longest);
-    if (tile == 128 || time < best) { best = time; p->tile[phase] = tile; }
+    const double time = std::max(all / 512, longest);
+    if (tile == 128 || time < best) { best = time; o.tile = tile; }
   }
   // shares of equal work, in whole tiles
-  const int tile = p->tile[phase];
   double all = 0, before = 0;
   int32_t tiles = 0, x = 0;
-  auto len = [&](const OrthoGroup& o) { return (double)(phase == ORTHO_GRAM ? o.np : o.mp); };
-  for (int k = 0; k < p->n; ++k) all += (double)p->g[k].count * tiles_of_matrix(p->g[k], tile, phase) * len(p->g[k]);
-  int32_t* first = p->shares[phase].first;
-  first[0] = 0;
+  for (int k = 0; k < p->n; ++k) all += (double)p->g[k].count * tiles_of_matrix(p->g[k], o.tile, phase) * tile_clocks(p->g[k], o.tile, phase);
+  o.first[0] = 0;
   for (int k = 0; k < p->n; ++k) {
-    const int32_t n = p->g[k].count * tiles_of_matrix(p->g[k], tile, phase);
-    const double one = len(p->g[k]);
+    const OrthoGroup& g = p->g[k];
+    o.each[k] = tiles_of_matrix(g, o.tile, phase);
+    o.begin[k] = tiles;
+    const int32_t n = g.count * o.each[k];
+    const double one = tile_clocks(g, o.tile, phase);
     // the boundaries that fall into this group
-    while (x < 7 && before + n * one >= all * (x + 1) / 8) first[++x] = tiles + (int32_t)std::min<double>(n, std::ceil((all * (x + 1) / 8 - before) / one));
+    while (x < 7 && n > 0 && before + n * one >= all * (x + 1) / 8)
+      o.first[++x] = tiles + (int32_t)std::min<double>(n, std::ceil((all * (x + 1) / 8 - before) / one));
     before += n * one;
     tiles += n;
   }
-  while (x < 8) first[++x] = tiles;
+  for (int k = p->n; k <= ORTHO_GROUPS; ++k) o.begin[k] = tiles;
+  while (x < 8) o.first[++x] = tiles;
 }
 int64_t pad(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }

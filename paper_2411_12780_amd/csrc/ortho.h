@@ -49,14 +49,16 @@ __host__ __device__ inline int tiles_of_matrix(const OrthoGroup& g, int tile, in
   const int down = (g.mp + tile - 1) / tile, across = (g.np + tile - 1) / tile;
   return phase <= ORTHO_POLY ? down * (down + 1) / 2 : down * across;      // of a symmetric result those on and under the diagonal
 }
-// Workgroup w runs on XCD w % 8.  Each XCD has a run of the tiles, in the order of the groups, with an eighth of the work: tiles of one matrix,
-// which read the same rows at about the same time, meet in one L2.
-struct XcdShares { int32_t first[9]; };
+// The tiles of one product: `each` of a matrix, those of group k from begin[k] on.  Workgroup w runs on XCD w % 8.  Each XCD has a run of the
+// tiles, first[x] .. first[x + 1], with an eighth of the work: tiles of one matrix, which read the same rows at about the same time, meet in one L2.
+struct OrthoProduct {
+  int32_t tile;                        // 64 or 128
+  int32_t first[9], begin[ORTHO_GROUPS + 1], each[ORTHO_GROUPS];
+};
 struct OrthoPlan {
   OrthoGroup g[ORTHO_GROUPS];          // longest rows first: their tiles take the longest
   int32_t n;                           // groups with a matrix in them
-  int32_t tile[3];                     // 64 or 128, for each product
-  XcdShares shares[3];
+  OrthoProduct product[3];
   int64_t partials;                    // byte offset of the partial sums of squares, one double a piece
   int64_t shrink;                      // and of a float for each matrix (see k_ortho.hip)
   int64_t bytes;
