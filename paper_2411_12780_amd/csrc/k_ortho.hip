@@ -457,10 +457,24 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
   // in the caller's orientation: eight of a row there, columns i of the tile, ROWS / 8 lanes a row)
   f16x8 old_h[PASSES * EACH], old_l[PASSES * EACH];
   constexpr int SEGS = ROWS / 8, TURNS = 64 * SEGS / 64;
-  float w[MODE == LAST && MUON ? PASSES * EACH : 1][8];
+  float w[MODE == LAST && MUON ? EACH : 1][8];
   auto place = [&](int ps, int n, int& i, int& j) { i = i0 + ps * ROWS + r8 + 8 * n; j = j0 + seg; };
   auto place_tall = [&](int ps, int n, int& i, int& j) { i = i0 + ps * ROWS + lane % SEGS * 8; j = j0 + lane / SEGS + n * (64 / SEGS); };
   static_assert(TURNS == EACH, "");
+  auto parameters = [&](int ps) {
+    if (MODE != LAST || !MUON) return;
+#pragma unroll
+    for (int n = 0; n < EACH; ++n) {
+      int i, j;
+      if (!g.tall) {
+        place(ps, n, i, j);
+        load_eight(t, quads, element(g, matrix, i, j), i < g.m ? g.n - j : 0, w[n]);
+      } else {
+        place_tall(ps, n, i, j);
+        load_eight(t, quads, element(g, matrix, j, i), j < g.n ? g.m - i : 0, w[n]);
+      }
+    }
+  };
   if (live) {
 #pragma unroll
     for (int ps = 0; ps < PASSES; ++ps)
@@ -473,16 +487,8 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
           old_h[ps * EACH + n] = *(const f16x8*)add;
           old_l[ps * EACH + n] = *(const f16x8*)(add + pl);
         }
-        if (MODE == LAST && MUON) {
-          if (!g.tall) {
-            place(ps, n, i, j);
-            load_eight(t, quads, element(g, matrix, i, j), i < g.m ? g.n - j : 0, w[ps * EACH + n]);
-          } else {
-            place_tall(ps, n, i, j);
-            load_eight(t, quads, element(g, matrix, j, i), j < g.n ? g.m - i : 0, w[ps * EACH + n]);
-          }
-        }
       }
+    parameters(0);
   }
   const Shrink shrink = shrink_of(((const float*)(ws + p.shrink))[g.first + matrix], step);
   const float poly_b = NS_B * shrink.now * shrink.now, poly_c = NS_C * shrink.now * shrink.now * shrink.now * shrink.now * UNSCALE;
@@ -511,7 +517,7 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
         *(f16x8*)to = v2.hi;
         *(f16x8*)(to + pl) = v2.lo;
       } else if (!g.tall && i < g.m && j < g.n) {
-        store_eight<MUON>(t, quads, element(g, matrix, i, j), g.n - j, v, w[MUON ? ps * EACH + n : 0]);
+        store_eight<MUON>(t, quads, element(g, matrix, i, j), g.n - j, v, w[MUON ? n : 0]);
       }
     }
   };
@@ -523,7 +529,7 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
       float v[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k] = sums[(i - i0 - ps * ROWS + k) * PITCH + j - j0];
-      if (i < g.m && j < g.n) store_eight<MUON>(t, quads, element(g, matrix, j, i), g.m - i, v, w[MUON ? ps * EACH + n : 0]);
+      if (i < g.m && j < g.n) store_eight<MUON>(t, quads, element(g, matrix, j, i), g.m - i, v, w[MUON ? n : 0]);
     }
   };
   // columns c0 .. c0 + cols - 1 of `rows` (a multiple of 8) finished rows, as rows of the mirrored tile
@@ -557,6 +563,7 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
     if (!live) return;
 #pragma unroll
     for (int ps = 0; ps < 2; ++ps) {
+      if (ps) parameters(ps);
       wave_sync();
       put(sums, hh[0][ps], 0, 0);
       put(sums, hh[1][ps], 0, 32);
