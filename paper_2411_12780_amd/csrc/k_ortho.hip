@@ -16,6 +16,7 @@ using pipe::u32x2;
 using pipe::u32x4;
 using pipe::wait_vm;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
@@ -221,6 +222,7 @@ __global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, c
   }
   const double norm = sqrt(sums[0]), inv = norm > 0 ? SCALE / norm : norm;      // NaN stays one
   if (id == 0 && t == 0) ((float*)(ws + p.shrink))[g.first + at.matrix] = (float)(norm / (norm + NORM_EPS));
+  if (blockIdx.x * 256 + t < p.counters) ((int*)(ws + p.arrived))[blockIdx.x * 256 + t] = 0;     // (there are more threads than tiles)
   auto put = [&](int y, int x, float v) {
     if (g.tall) tile[x][y] = v;
     else tile[y][x] = v;
@@ -317,6 +319,47 @@ __device__ __forceinline__ void k_step(f32x16 (&hh)[2][2], f32x16 (&xx)[2][2], c
   }
 }
 
+// The sums of a tile whose k is in `pieces` pieces: each workgroup leaves its own in `sums`, and the one that finds all the others' there adds them up,
+// in the order of the pieces whichever it is.  Whether this is that one.  What goes from one workgroup to another passes the L2 caches (each XCD has its
+// own) both ways, as agent-wide atomic accesses do; a store has arrived when the counter of stores in flight says so.  No workgroup waits for another.
+template <int N> __device__ __forceinline__ bool join(f32x16 (&v)[N], char* sums, int piece, int pieces, int* arrived, int& before, bool live) {
+  constexpr int PAST_L2 = 16, BYTES = 256 * N * 64;
+  const __amdgpu_buffer_rsrc_t rs = pipe::make_rsrc(sums, (uint32_t)(pieces * BYTES));
+  const int at = (threadIdx.x >> 6) * N * 4096 + (threadIdx.x & 63) * 16;
+  if (live) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, (f32x4){v[n][4 * q], v[n][4 * q + 1], v[n][4 * q + 2], v[n][4 * q + 3]}), rs,
+                                               at + (4 * n + q) * 1024, piece * BYTES, PAST_L2);
+  }
+  wait_vm<0>();
+  __syncthreads();
+  if (threadIdx.x == 0) before = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (before != pieces - 1) return false;
+  if (threadIdx.x == 0) __hip_atomic_store(arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next product
+  if (live) {
+    for (int k = 0; k < pieces; ++k) {
+      u32x4 u[N][4];
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) u[n][q] = __builtin_amdgcn_raw_buffer_load_b128(rs, at + (4 * n + q) * 1024, k * BYTES, PAST_L2);
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 w = __builtin_bit_cast(f32x4, u[n][q]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[n][4 * q + e] = k ? v[n][4 * q + e] + w[e] : w[e];
+        }
+    }
+  }
+  return true;
+}
+
 template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) void product_kernel(OrthoPlan p, OrthoProduct tiles, Target t, char* ws, int step) {
   using S = Tile<TILE>;
   constexpr bool TR = MODE >= APPLY;
@@ -334,6 +377,11 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
   id -= begin;
   const int matrix = quotient(id, tiles.each[group]);
   id -= matrix * tiles.each[group];
+  constexpr bool PIECES = MODE <= POLY;
+  const int pieces = PIECES ? tiles.split[group] : 1, of_matrix = PIECES ? tiles_of_matrix(g, TILE, MODE) : 1;
+  const int piece = PIECES && pieces > 1 ? quotient(id, of_matrix) : 0;
+  if (PIECES) id -= piece * of_matrix;
+  const int tile_id = id;
   int bi, bj;
   if (MODE <= POLY) {
     bi = (int)((sqrtf(8.f * id + 1.f) - 1.f) * 0.5f);
@@ -349,7 +397,8 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
   _Float16* X = (_Float16*)(ws + g.x[from]) + matrix * 2 * px;
   _Float16* A = (_Float16*)(ws + g.a) + matrix * 2 * pa;
   _Float16* B = (_Float16*)(ws + g.b) + matrix * 2 * pa;
-  const int K = MODE == GRAM ? g.np : g.mp, nk = K / S::KT;
+  const int K = MODE == GRAM ? g.np : g.mp, stages_of_tile = K / S::KT;
+  const int first_stage = piece * stages_of_tile / pieces, nk = (piece + 1) * stages_of_tile / pieces - first_stage;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // ---- what this wave copies: plane `wave` of P hi, P lo, Q hi, Q lo
@@ -381,7 +430,7 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
     if (i >= nk) return;
     lds_char* to = lds + (i & 1) * S::STAGE + wave * S::PLANE;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) pipe::load_to_lds(rs, to + c * 1024, off[c & 1] + c * every + i * step_k);
+    for (int c = 0; c < 8; ++c) pipe::load_to_lds(rs, to + c * 1024, off[c & 1] + c * every + (i + first_stage) * step_k);
   };
 
   // ---- where this wave reads its fragments, in stage 0
@@ -475,7 +524,8 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
       }
     }
   };
-  if (live) {
+  auto load_old = [&]() {
+    if (!live) return;
 #pragma unroll
     for (int ps = 0; ps < PASSES; ++ps)
 #pragma unroll
@@ -489,7 +539,12 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
         }
       }
     parameters(0);
-  }
+  };
+  if (pieces == 1) load_old();
+  char* joint = nullptr;
+  int& before = *(int*)(stages + 2 * S::STAGE - 4);
+  int* arrived = (int*)(ws + p.arrived) + tiles.tile_of[group] + matrix * of_matrix + tile_id;
+  if (PIECES && pieces > 1) joint = ws + p.sums + tiles.sums_of[group] + ((int64_t)matrix * of_matrix + tile_id) * pieces * (TILE * TILE * 4);
   const Shrink shrink = shrink_of(((const float*)(ws + p.shrink))[g.first + matrix], step);
   const float poly_b = NS_B * shrink.now * shrink.now, poly_c = NS_C * shrink.now * shrink.now * shrink.now * shrink.now * UNSCALE;
   const float scale = MODE == LAST ? shrink.ratio * shrink.next * UNSCALE * (MUON ? 0.2f * t.lr * sqrtf((float)g.n) : 1.f) : shrink.ratio;
@@ -560,6 +615,13 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
   if constexpr (TILE == 128) {
     // 32 rows at a time, in a part of LDS of the wave's own
     float* sums = (float*)stages + wave * 32 * PITCH;
+    if (PIECES && pieces > 1) {
+      f32x16 v[4] = {hh[0][0], hh[0][1], hh[1][0], hh[1][1]};
+      if (!join<4>(v, joint, piece, pieces, arrived, before, live)) return;
+      load_old();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) hh[k >> 1][k & 1] = v[k];
+    }
     if (!live) return;
 #pragma unroll
     for (int ps = 0; ps < 2; ++ps) {
@@ -600,6 +662,12 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
         a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
       }
       acc[4 * q] = a.x; acc[4 * q + 1] = a.y; acc[4 * q + 2] = a.z; acc[4 * q + 3] = a.w;
+    }
+    if (PIECES && pieces > 1) {
+      f32x16 v[1] = {acc};
+      if (!join<1>(v, joint, piece, pieces, arrived, before, true)) return;
+      load_old();
+      acc = v[0];
     }
     __syncthreads();
     put(sums, acc, (wave & 1) * 32, (wave >> 1) * 32);

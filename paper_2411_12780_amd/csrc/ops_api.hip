@@ -35,40 +35,65 @@ bool overlap(const Run& a, const Run& b) {
   }
   return false;
 }
-// Clocks that a workgroup spends on a tile, two of them on a unit: those that every tile costs (finding its place, the first copies' way, the
-// epilogue) and those of 64 k.
-double tile_clocks(const OrthoGroup& g, int tile, int phase) {
-  const int k = phase == ORTHO_GRAM ? g.np : g.mp;
-  return tile == 128 ? 10000 + k / 64 * 3200. : 7000 + k / 64 * 1150.;
+// Clocks that a workgroup spends on its part of a tile, two of them on a unit: those that every part costs (finding its place, the first copies' way,
+// the epilogue), those of 64 k, and of a tile in pieces the way of its sums through memory.
+double part_clocks(const OrthoGroup& g, int tile, int phase, int pieces) {
+  const double stages = (phase == ORTHO_GRAM ? g.np : g.mp) / 64 / (double)pieces;
+  return tile == 128 ? 10000 + stages * 3200 + (pieces > 1 ? 8000 + 2000 * pieces : 0) : 7000 + stages * 1150 + (pieces > 1 ? 4500 + 700 * pieces : 0);
 }
-// Tiles of one of the products, and how the XCDs share them.  The tile that takes less time: rounds of 512 workgroups, and none is shorter than its
-// longest tile.
+int pieces_of(const OrthoGroup& g, int phase, int length) {
+  const int k = phase == ORTHO_GRAM ? g.np : g.mp;
+  return phase <= ORTHO_POLY ? std::max(1, (k + length / 2) / length) : 1;
+}
+// Tiles of one of the products, into how many pieces the k of each is split, and how the XCDs share them.  Taken is what fills rounds of 512 workgroups
+// (two on a unit) in the least time: whole rounds, the last one filled up with the shortest part, and none shorter than the longest.  Measured, five
+// steps: one matrix of 256 x 2048 (10 tiles of 64) 205 us whole, 145 in eight pieces; 512 x 512 160 and 168, so whole; two of 1536 x 6144 1893 in tiles
+// of 64 (600, little more than a round), 1685 in tiles of 128 in three pieces (468).
 void plan_product(OrthoPlan* p, int phase) {
   OrthoProduct& o = p->product[phase];
+  int longest_k = 0, length = 1 << 20;
+  for (int k = 0; k < p->n; ++k)
+    if (!p->g[k].small) longest_k = std::max(longest_k, phase == ORTHO_GRAM ? p->g[k].np : p->g[k].mp);
   double best = 0;
-  for (int tile : {128, 64}) {
-    double all = 0, longest = 0;
-    for (int k = 0; k < p->n; ++k) {
-      const OrthoGroup& g = p->g[k];
-      if (g.small) continue;
-      const double one = tile_clocks(g, tile, phase);
-      all += (double)g.count * tiles_of_matrix(g, tile, phase) * one;
-      longest = std::max(longest, one);
+  for (int tile : {128, 64})
+    for (int most : {1, 2, 3, 4, 6, 8}) {
+      if (most > 1 && (phase > ORTHO_POLY || longest_k < 128 * most)) break;
+      const int len = most == 1 ? 1 << 20 : longest_k / most;
+      double all = 0, longest = 0, parts = 0, last = 0;
+      for (int k = 0; k < p->n; ++k) {
+        const OrthoGroup& g = p->g[k];
+        if (g.small) continue;
+        const int pieces = pieces_of(g, phase, len);
+        const double one = part_clocks(g, tile, phase, pieces), n = (double)g.count * tiles_of_matrix(g, tile, phase) * pieces;
+        all += n * one;
+        parts += n;
+        longest = std::max(longest, one);
+        last = last > 0 ? std::min(last, one) : one;
+      }
+      const double time = std::max((all + (std::ceil(parts / 512) * 512 - parts) * last) / 512, longest);
+      if (best == 0 || time < best) { best = time; o.tile = tile; length = len; }
     }
-    const double time = std::max(all / 512, longest);
-    if (tile == 128 || time < best) { best = time; o.tile = tile; }
-  }
   // shares of equal work, in whole tiles
   double all = 0, before = 0;
   int32_t tiles = 0, x = 0;
-  for (int k = 0; k < p->n; ++k) all += (double)p->g[k].count * tiles_of_matrix(p->g[k], o.tile, phase) * tile_clocks(p->g[k], o.tile, phase);
+  int32_t split_tiles = 0; int64_t split_pieces = 0;
+  for (int k = 0; k < p->n; ++k) {
+    const int tl = tiles_of_matrix(p->g[k], o.tile, phase);
+    o.split[k] = pieces_of(p->g[k], phase, length);
+    o.tile_of[k] = split_tiles;
+    o.sums_of[k] = 4 * (int64_t)o.tile * o.tile * split_pieces;
+    if (o.split[k] > 1) { split_tiles += p->g[k].count * tl; split_pieces += (int64_t)p->g[k].count * tl * o.split[k]; }
+    all += (double)p->g[k].count * tl * o.split[k] * part_clocks(p->g[k], o.tile, phase, o.split[k]);
+  }
+  p->counters = std::max(p->counters, split_tiles);
+  p->sums = std::max<int64_t>(p->sums, 4 * (int64_t)o.tile * o.tile * split_pieces);
   o.first[0] = 0;
   for (int k = 0; k < p->n; ++k) {
     const OrthoGroup& g = p->g[k];
-    o.each[k] = tiles_of_matrix(g, o.tile, phase);
+    o.each[k] = tiles_of_matrix(g, o.tile, phase) * o.split[k];
     o.begin[k] = tiles;
     const int32_t n = g.count * o.each[k];
-    const double one = tile_clocks(g, o.tile, phase);
+    const double one = part_clocks(g, o.tile, phase, o.split[k]);
     // the boundaries that fall into this group
     while (x < 7 && n > 0 && before + n * one >= all * (x + 1) / 8)
       o.first[++x] = tiles + (int32_t)std::min<double>(n, std::ceil((all * (x + 1) / 8 - before) / one));
@@ -132,6 +157,8 @@ int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* pla
     if (pieces > MOST_ITEMS || 8 * squares > MOST_ITEMS) { set_error("too many matrices for one call"); return PPLL_ERR_SHAPE; }
   }
   for (int phase = 0; phase < 3; ++phase) plan_product(plan, phase);
+  plan->sums = take(plan->sums);
+  plan->arrived = take(plan->counters * (int64_t)sizeof(int32_t));
   plan->partials = take(pieces * (int64_t)sizeof(double));
   plan->shrink = take(matrices * (int64_t)sizeof(float));
   plan->bytes = at;

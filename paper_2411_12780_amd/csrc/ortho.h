@@ -54,6 +54,9 @@ __host__ __device__ inline int tiles_of_matrix(const OrthoGroup& g, int tile, in
 struct OrthoProduct {
   int32_t tile;                        // 64 or 128
   int32_t first[9], begin[ORTHO_GROUPS + 1], each[ORTHO_GROUPS];
+  int32_t split[ORTHO_GROUPS];         // pieces of the k of a tile, each a workgroup's
+  int32_t tile_of[ORTHO_GROUPS];       // the group's first tile among those in pieces
+  int64_t sums_of[ORTHO_GROUPS];       // and its first sums, in bytes
 };
 struct OrthoPlan {
   OrthoGroup g[ORTHO_GROUPS];          // longest rows first: their tiles take the longest
@@ -61,6 +64,8 @@ struct OrthoPlan {
   OrthoProduct product[3];
   int64_t partials;                    // byte offset of the partial sums of squares, one double a piece
   int64_t shrink;                      // and of a float for each matrix (see k_ortho.hip)
+  int64_t sums, arrived;               // of the tiles whose k is in pieces: sums of each piece, and how many of them are there (an int a tile)
+  int32_t counters;                    // such tiles, of the product that has the most
   int64_t bytes;
 };
 

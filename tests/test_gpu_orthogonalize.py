@@ -303,3 +303,36 @@ def test_sizes_on_both_sides_of_what_one_workgroup_holds(rows, cols):
         values = np.random.default_rng(rows + cols).standard_normal(blob_size(groups)).astype(np.float32)
         given, got = run(groups, values)
         check(groups, given, got)
+
+
+# few tiles and long rows: the k of a tile is in pieces, whose sums one of its workgroups adds up; with 1536 x 3000 in the larger tiles
+@pytest.mark.parametrize("rows,cols,count", [(256, 2048, 1), (130, 2001, 2), (4000, 65, 1), (520, 1990, 1), (1000, 1000, 1), (1536, 3000, 1)])
+def test_few_tiles_of_long_rows(rows, cols, count):
+    groups = [P.matrix_group(0, rows, cols, count=count)]
+    values = np.random.default_rng(rows + cols).standard_normal(count * rows * cols).astype(np.float32)
+    given, got = run(groups, values, steps=2)
+    check(groups, given, got, steps=2)
+    for _ in range(6):                                      # whichever piece comes last: the same bits
+        assert np.array_equal(run(groups, values, steps=2)[1], got)
+
+
+def test_pieces_replayed_with_calls_between():
+    groups = [P.matrix_group(0, 200, 2048), P.matrix_group(200 * 2048, 2048, 140)]
+    x = torch.randn(blob_size(groups), device=DEV)
+    out, eager = torch.empty_like(x), torch.empty_like(x)
+    ws = workspace(groups)
+    s = torch.cuda.Stream()
+    call = lambda dst: P.ppll_orthogonalize(groups, P.FP32, 5, x, dst, ws, ws.numel(), stream())  # noqa: E731
+    call(eager)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        call(out)
+    for _ in range(4):
+        x.copy_(torch.randn_like(x))
+        ws.fill_(255)                                       # nothing is kept in the workspace from call to call
+        graph.replay()
+        torch.cuda.synchronize()
+        call(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
