@@ -79,6 +79,7 @@ int validate_config(const ppll_block_config* c) {
       if (c->qk_norm && (!(c->qk_norm_eps > 0.f) || !std::isfinite(c->qk_norm_eps))) return bad("qk_norm_eps must be positive and finite");
     }
     if (c->optimizer == PPLL_MUON && c->mlp_dim > ORTHO_SIDE) return bad("mlp_dim above 8192 with the Muon optimizer");
+    if (c->optimizer == PPLL_MUON && (int64_t)c->depth + c->aux_depth > ORTHO_COUNT) return bad("more than 65535 layers with the Muon optimizer");
     // every limit a kernel of the step would otherwise hit at launch time, when earlier kernels are already enqueued
     const size_t dh = (size_t)(c->dim / c->heads), T = (size_t)c->tokens;
     if (c->precision != PPLL_BF16 || dh != 64) {   // the run-time-typed attention kernels keep K, V (or Q, dO) of one head in LDS
@@ -104,6 +105,7 @@ int validate_config(const ppll_block_config* c) {
     if (c->rotary || c->qk_norm) return bad("rotary positions and qk_norm belong to ViT blocks");
     if (c->optimizer == PPLL_MUON && (9 * c->channels > ORTHO_SIDE || c->aux_channels > ORTHO_SIDE))
       return bad("9 * channels or aux_channels above 8192 with the Muon optimizer");
+    if (c->optimizer == PPLL_MUON && c->n_basic_blocks > ORTHO_COUNT) return bad("more than 65535 basic blocks with the Muon optimizer");
     if (c->bn_eps <= 0.f || c->bn_momentum < 0.f || c->bn_momentum > 1.f) return bad("bn_eps > 0 and bn_momentum in [0,1] required");
     {
       const size_t m = c->transition_block > 0 ? 2 : 1, wide = c->channels > c->aux_channels ? c->channels : c->aux_channels;

@@ -267,7 +267,7 @@ int rows_wg(const RotaryPlan& p, bool bwd) {
 }
 int workgroups_of(const RotaryPlan& p, bool bwd) {
   const int each = rows_wg(p, bwd) > 0 ? rows_wg(p, bwd) : 1;
-  const int64_t blocks = ((int64_t)p.rows + each - 1) / each, most = bwd ? ROTARY_PARTIALS : (int64_t)1 << 30;
+  const int64_t blocks = ((int64_t)p.rows + each - 1) / each, most = bwd ? ROTARY_PARTIALS : (int64_t)1 << 23;      // (threads of a launch: under 2^32)
   return (int)(blocks < most ? blocks : most);
 }
 // Elements of a lane's piece: 16 bytes, or 8 where half a head or a buffer has no more in common with them; 0: no pieces.

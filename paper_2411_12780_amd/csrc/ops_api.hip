@@ -118,7 +118,7 @@ int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* pla
       set_error("group %d: %d x %d outside 1..%d", k, g.rows, g.cols, ORTHO_SIDE);
       return PPLL_ERR_SHAPE;
     }
-    if (g.count < 0 || g.count > 65535) { set_error("group %d: count %d outside 0..65535", k, g.count); return PPLL_ERR_SHAPE; }
+    if (g.count < 0 || g.count > ORTHO_COUNT) { set_error("group %d: count %d outside 0..%d", k, g.count, ORTHO_COUNT); return PPLL_ERR_SHAPE; }
     if (g.reserved) { set_error("group %d: reserved is not 0", k); return PPLL_ERR_SHAPE; }
     if (g.offset < 0 || g.stride < 0 || g.offset >= FAR || g.stride >= FAR || g.ld < g.cols || g.ld >= FAR >> 13) {
       set_error("group %d: offset, stride or ld out of range", k);
@@ -289,6 +289,10 @@ int ppll_muon_step(const ppll_matrix_group* groups, int32_t n_groups, int32_t st
   PPLL_TRY(check_blob(momentum_dev, "momentum_dev"));
   PPLL_TRY(check_blob(params_dev, "params_dev"));
   if (shadow_dev) PPLL_TRY(check_blob(shadow_dev, "shadow_dev"));
+  const void* blobs[] = {grads_dev, momentum_dev, params_dev, shadow_dev};
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < i; ++j)
+      if (blobs[i] == blobs[j]) { set_error("gradients, momentum, parameters and shadow need a blob each"); return PPLL_ERR_SHAPE; }
   PPLL_TRY(check_workspace(workspace_dev, workspace_bytes, (size_t)p.bytes));
   return launch_muon((hipStream_t)hip_stream, p, steps, grads_dev, momentum_dev, params_dev, (uint16_t*)shadow_dev, lr, momentum, nesterov != 0,
                      weight_decay, (char*)workspace_dev);

@@ -9,6 +9,7 @@ namespace ppll {
 
 constexpr int ORTHO_GROUPS = 16;       // groups of a call
 constexpr int ORTHO_SIDE = 8192;       // rows and columns of a matrix, at most
+constexpr int ORTHO_COUNT = 65535;     // matrices of a group, at most
 constexpr int ORTHO_STEPS = 16;        // Newton-Schulz steps, at most
 constexpr int NORM_ROWS = 32, NORM_COLS = 256;   // piece of a matrix whose squares one workgroup adds up
 

@@ -14,14 +14,14 @@ OLD = P.BlockConfig.rotary.offset       # size of a configuration before those f
 @pytest.mark.parametrize("bad", [dict(rotary=2), dict(qk_norm=-1), dict(grid_h=7), dict(grid_h=4, grid_w=16), dict(grid_h=0, grid_w=0), dict(rotary_base=0.0),
                                  dict(rotary_base=-1.0), dict(rotary_base=float("inf")), dict(rotary_base=float("nan")), dict(qk_norm_eps=0.0),
                                  dict(qk_norm_eps=float("nan")), dict(heads=128), dict(heads=1), dict(mlp_dim=8200),
-                                 dict(input_kind=synth.ACTIVATION, grid_h=65536, grid_w=65536), dict(optimizer=3)])
+                                 dict(input_kind=synth.ACTIVATION, grid_h=65536, grid_w=65536), dict(optimizer=3), dict(depth=65535, aux_depth=1)])
 def test_refused_vit_configurations(bad):
     with pytest.raises(P.PpllError) as e:
         P.ppll_block_workspace_bytes(P.make_config(dict(GOOD, **bad)))
     assert e.value.status == 2
 
 
-@pytest.mark.parametrize("bad", [dict(rotary=1), dict(qk_norm=1), dict(optimizer=synth.MUON, channels=912), dict(optimizer=synth.MUON, aux_channels=8200)])
+@pytest.mark.parametrize("bad", [dict(rotary=1), dict(qk_norm=1), dict(optimizer=synth.MUON, channels=912), dict(optimizer=synth.MUON, aux_channels=8200), dict(optimizer=synth.MUON, n_basic_blocks=65536)])
 def test_refused_resnet_configurations(bad):
     with pytest.raises(P.PpllError) as e:
         P.ppll_block_workspace_bytes(P.make_config(synth.workload("resnet_stage_bf16", batch=1, **bad)))

@@ -92,7 +92,7 @@ def test_muon_refusals():
     for status, bad in ((CONFIG, dict(steps=0)), (CONFIG, dict(lr=math.nan)), (CONFIG, dict(momentum=math.nan)), (CONFIG, dict(decay=math.nan)),
                         (NULL, dict(grads=None)), (NULL, dict(m=None)), (NULL, dict(p=None)), (NULL, dict(work=None)),
                         (WORKSPACE, dict(grads=8)), (WORKSPACE, dict(m=8)), (WORKSPACE, dict(p=8)), (WORKSPACE, dict(shadow=8)),
-                        (WORKSPACE, dict(nbytes=ws - 1))):
+                        (WORKSPACE, dict(nbytes=ws - 1)), (SHAPE, dict(grads=32)), (SHAPE, dict(m=48)), (SHAPE, dict(shadow=48)), (SHAPE, dict(shadow=16))):
         refused(status, lambda: call(**bad))
 
 
