@@ -72,20 +72,19 @@ __device__ __forceinline__ bool in_quads(const OrthoGroup& g) { return ((g.offse
 __device__ __forceinline__ int64_t element(const OrthoGroup& g, int matrix, int r, int c) {
   return g.offset + (int64_t)matrix * g.stride + (int64_t)r * g.ld + c;
 }
-// The matrix that work item `id` of a launch belongs to, `each(group)` items a matrix; id becomes the place within it.
-struct Place { int group, matrix; };
-template <class EACH> __device__ __forceinline__ Place place_of(const OrthoPlan& p, int& id, EACH each) {
-  for (int k = 0; k < p.n; ++k) {
-    const int e = each(p.g[k]), all = e * p.g[k].count;      // (none: no items of this kind)
-    if (id < all) {
-      const int i = id / e;
-      id -= i * e;
-      return {k, i};
-    }
-    id -= all;
-  }
-  return {-1, 0};
+// The group that work item `id` of a launch belongs to; id becomes the place within the group.  All bounds are read at once.
+__device__ __forceinline__ int group_of(const int32_t (&begin)[ORTHO_GROUPS], int& id) {
+  static_assert(ORTHO_GROUPS == 16, "");
+  asm volatile("" ::"s"(begin[1]), "s"(begin[2]), "s"(begin[3]), "s"(begin[4]), "s"(begin[5]), "s"(begin[6]), "s"(begin[7]), "s"(begin[8]),
+               "s"(begin[9]), "s"(begin[10]), "s"(begin[11]), "s"(begin[12]), "s"(begin[13]), "s"(begin[14]), "s"(begin[15]));
+  int group = 0, from = 0;
+#pragma unroll
+  for (int k = 1; k < ORTHO_GROUPS; ++k)
+    if (id >= begin[k]) { group = k; from = begin[k]; }
+  id -= from;
+  return group;
 }
+// Values that a kernel needs sooner or later, loaded here and now
 __device__ __forceinline__ float read_u(const Source& s, int64_t at) {
   if (s.in) return ld_f(s.in, (size_t)at, s.dt);
   const float m = s.m[at];
@@ -128,16 +127,28 @@ template <bool MUON> __device__ __forceinline__ void store_eight(const Target& t
   }
 }
 
-// The momentum, and the sums of squares of pieces of 32 x 256 (in 64 bits: gradients of 1e-25 or 1e25 have a norm as well).
+// The sum over a workgroup of four waves, in every thread
+__device__ __forceinline__ double sum_of_all(double v) {
+  __shared__ double waves[4];
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return waves[0] + waves[1] + waves[2] + waves[3];
+}
+
+// The momentum, and the sums of squares of pieces of 16 x 256 (in 64 bits: gradients of 1e-25 or 1e25 have a norm as well).
 __global__ __launch_bounds__(256) void squares_kernel(OrthoPlan p, Source s, char* ws) {
   int id = blockIdx.x;
-  const Place at = place_of(p, id, [](const OrthoGroup& g) { return g.small ? 0 : g.pieces(); });
-  const OrthoGroup& g = p.g[at.group];
-  const int across = (g.cols + NORM_COLS - 1) / NORM_COLS, r0 = id / across * NORM_ROWS, c0 = id % across * NORM_COLS;
+  const int group = group_of(p.pieces.begin, id);
+  const OrthoGroup& g = p.g[group];
+  asm volatile("" ::"s"(g.offset), "s"(g.stride), "s"(g.ld), "s"(g.rows), "s"(g.cols), "s"(g.first_piece));      // one batch of loads
+  const int each = p.pieces.each[group], matrix = quotient(id, each);
+  id -= matrix * each;
+  const int across = (g.cols + NORM_COLS - 1) / NORM_COLS, down = quotient(id, across), r0 = down * NORM_ROWS, c0 = (id - down * across) * NORM_COLS;
   double sum = 0;
   if (in_quads(g) && r0 + NORM_ROWS <= g.rows && c0 + NORM_COLS <= g.cols && !(s.in && s.dt != F32)) {
     // a wave's rows, 16 bytes a lane, all of them on their way at once
-    const int64_t first = element(g, at.matrix, r0 + (threadIdx.x >> 6) * (NORM_ROWS / 4), c0 + (threadIdx.x & 63) * 4);
+    const int64_t first = element(g, matrix, r0 + (threadIdx.x >> 6) * (NORM_ROWS / 4), c0 + (threadIdx.x & 63) * 4);
     float4 u[NORM_ROWS / 4], m[NORM_ROWS / 4];
 #pragma unroll
     for (int k = 0; k < NORM_ROWS / 4; ++k) {
@@ -161,89 +172,80 @@ __global__ __launch_bounds__(256) void squares_kernel(OrthoPlan p, Source s, cha
     }
   } else {
     const int c = c0 + threadIdx.x, rows = c < g.cols ? min(NORM_ROWS, g.rows - r0) : 0;
-    const int64_t first = element(g, at.matrix, r0, c);
-    for (int r = 0; r < rows; r += 8) {        // eight rows on their way at a time
-      float u[8], m[8];
+    const int64_t first = element(g, matrix, r0, c);
+    float u[NORM_ROWS], m[NORM_ROWS];          // all on their way at once
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int64_t e = first + (int64_t)(r + k) * g.ld;
-        const bool on = r + k < rows;
-        u[k] = !on ? 0.f : s.in ? ld_f(s.in, (size_t)e, s.dt) : s.g[e];
-        m[k] = on && !s.in ? s.m[e] : 0.f;
-      }
+    for (int k = 0; k < NORM_ROWS; ++k) {
+      const int64_t e = first + k * g.ld;
+      u[k] = k >= rows ? 0.f : s.in ? ld_f(s.in, (size_t)e, s.dt) : s.g[e];
+      m[k] = k < rows && !s.in ? s.m[e] : 0.f;
+    }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if (!s.in) {
-          m[k] = fmaf(s.momentum, m[k], u[k]);
-          if (r + k < rows) s.m[first + (int64_t)(r + k) * g.ld] = m[k];
-          u[k] = s.nesterov ? fmaf(s.momentum, m[k], u[k]) : m[k];
-        }
-        sum += (double)u[k] * u[k];
+    for (int k = 0; k < NORM_ROWS; ++k) {
+      if (!s.in) {
+        m[k] = fmaf(s.momentum, m[k], u[k]);
+        if (k < rows) s.m[first + k * g.ld] = m[k];
+        u[k] = s.nesterov ? fmaf(s.momentum, m[k], u[k]) : m[k];
       }
+      sum += (double)u[k] * u[k];
     }
   }
-  __shared__ double sums[256];
-  sums[threadIdx.x] = sum;
-  __syncthreads();
-  for (int w = 128; w > 0; w >>= 1) {
-    if (threadIdx.x < w) sums[threadIdx.x] += sums[threadIdx.x + w];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) ((double*)(ws + p.partials))[g.first_piece + at.matrix * g.pieces() + id] = sums[0];
+  sum = sum_of_all(sum);
+  if (threadIdx.x == 0) ((double*)(ws + p.partials))[g.first_piece + matrix * each + id] = sum;
 }
 
 // Y = u / |u|, in tiles of 64 x 64.
-__global__ __launch_bounds__(256) void normalise_kernel(OrthoPlan p, Source s, char* ws) {
+__global__ __launch_bounds__(256, 8) void normalise_kernel(OrthoPlan p, Source s, char* ws) {
   int id = blockIdx.x;
-  const Place at = place_of(p, id, [](const OrthoGroup& g) { return g.small ? 0 : (g.mp / 64) * (g.np / 64); });
-  const OrthoGroup& g = p.g[at.group];
-  const int t = threadIdx.x, i0 = id / (g.np / 64) * 64, j0 = id % (g.np / 64) * 64;
-  __shared__ double sums[256];
+  const int group = group_of(p.squares.begin, id);
+  const OrthoGroup& g = p.g[group];
+  asm volatile("" ::"s"(g.offset), "s"(g.stride), "s"(g.ld), "s"(g.rows), "s"(g.cols), "s"(g.mp), "s"(g.np), "s"(g.tall), "s"(g.first),
+               "s"(g.first_piece), "s"(g.x[0]));                                   // one batch of loads
+  const int each = p.squares.each[group], matrix = quotient(id, each);
+  id -= matrix * each;
+  const int t = threadIdx.x, across = g.np / 64, down = quotient(id, across), i0 = down * 64, j0 = (id - down * across) * 64;
   __shared__ float tile[64][65];
   const int r0 = g.tall ? j0 : i0, c0 = g.tall ? i0 : j0;                // in the caller's orientation: rows y of the tile
   const bool whole = in_quads(g) && r0 + 64 <= g.rows && c0 + 64 <= g.cols && !(s.in && s.dt != F32);
-  float4 u[4], m[4];
-  if (whole) {                                                           // (on their way under the sum)
-    const int64_t first = element(g, at.matrix, r0 + t / 16, c0 + t % 16 * 4);
+  float4 u[4], m[4];                                                     // (on their way under the sum)
+  if (whole) {
+    const int64_t first = element(g, matrix, r0 + t / 16, c0 + t % 16 * 4);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       u[k] = *(const float4*)((s.in ? (const float*)s.in : s.g) + first + k * 16 * g.ld);
       if (!s.in) m[k] = *(const float4*)(s.m + first + k * 16 * g.ld);
     }
+  } else {
+    const int64_t first = element(g, matrix, r0 + t / 64, c0 + t % 64);
+    const int rows = c0 + t % 64 < g.cols ? g.rows - r0 - t / 64 : 0;
+    auto at = [&](int k) { return 4 * k < rows ? read_u(s, first + k * 4 * g.ld) : 0.f; };
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = make_float4(at(4 * k), at(4 * k + 1), at(4 * k + 2), at(4 * k + 3));
   }
-  const double* part = (const double*)(ws + p.partials) + g.first_piece + at.matrix * g.pieces();
+  const int pieces = g.pieces();
+  const double* part = (const double*)(ws + p.partials) + g.first_piece + matrix * pieces;
   double sum = 0;
-  for (int k = t; k < g.pieces(); k += 256) sum += part[k];
-  sums[t] = sum;
-  __syncthreads();
-  for (int w = 128; w > 0; w >>= 1) {
-    if (t < w) sums[t] += sums[t + w];
-    __syncthreads();
-  }
-  const double norm = sqrt(sums[0]), inv = norm > 0 ? SCALE / norm : norm;      // NaN stays one
-  if (id == 0 && t == 0) ((float*)(ws + p.shrink))[g.first + at.matrix] = (float)(norm / (norm + NORM_EPS));
+  for (int k = t; k < pieces; k += 256) sum += part[k];
+  sum = sum_of_all(sum);
+  const double norm = sqrt(sum), inv = norm > 0 ? SCALE / norm : norm;      // NaN stays one
+  if (id == 0 && t == 0) ((float*)(ws + p.shrink))[g.first + matrix] = (float)(norm / (norm + NORM_EPS));
   if (blockIdx.x * 256 + t < p.counters) ((int*)(ws + p.arrived))[blockIdx.x * 256 + t] = 0;     // (there are more threads than tiles)
   auto put = [&](int y, int x, float v) {
     if (g.tall) tile[x][y] = v;
     else tile[y][x] = v;
   };
-  if (whole) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float v[4] = {u[k].x, u[k].y, u[k].z, u[k].w}, w[4] = {m[k].x, m[k].y, m[k].z, m[k].w};
+  for (int k = 0; k < 4; ++k) {
+    const float v[4] = {u[k].x, u[k].y, u[k].z, u[k].w}, w[4] = {m[k].x, m[k].y, m[k].z, m[k].w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        put(k * 16 + t / 16, t % 16 * 4 + e, (float)((s.in ? v[e] : s.nesterov ? fmaf(s.momentum, w[e], v[e]) : w[e]) * inv));
-    }
-  } else {
-    for (int k = 0; k < 16; ++k) {
-      const int y = k * 4 + t / 64, x = t % 64, r = r0 + y, c = c0 + x;
-      put(y, x, r < g.rows && c < g.cols ? (float)(read_u(s, element(g, at.matrix, r, c)) * inv) : 0.f);
+    for (int e = 0; e < 4; ++e) {
+      if (whole) put(k * 16 + t / 16, t % 16 * 4 + e, (float)((s.in ? v[e] : s.nesterov ? fmaf(s.momentum, w[e], v[e]) : w[e]) * inv));
+      else put((4 * k + e) * 4 + t / 64, t % 64, (float)(v[e] * inv));
     }
   }
   __syncthreads();
   const int64_t plane = g.plane_x();
-  _Float16* x = (_Float16*)(ws + g.x[0]) + at.matrix * 2 * plane;
+  _Float16* x = (_Float16*)(ws + g.x[0]) + matrix * 2 * plane;
   const int y = t / 4, q = t % 4 * 16;
   _Float16* to = x + (int64_t)(i0 + y) * g.np + j0 + q;
 #pragma unroll
@@ -360,28 +362,34 @@ template <int N> __device__ __forceinline__ bool join(f32x16 (&v)[N], char* sums
   return true;
 }
 
-template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) void product_kernel(OrthoPlan p, OrthoProduct tiles, Target t, char* ws, int step) {
+template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) void product_kernel(OrthoPlan p, Target t, char* ws, int step) {
   using S = Tile<TILE>;
   constexpr bool TR = MODE >= APPLY;
   extern __shared__ __align__(256) char stages[];
   PPLL_CODE_TO_L2(2);
   // ---- which tile
+  const OrthoProduct& all = p.product[MODE < APPLY ? MODE : APPLY];
   const int xcd = blockIdx.x & 7;
-  int id = tiles.first[xcd] + (int)(blockIdx.x >> 3);
-  if (id >= tiles.first[xcd + 1]) return;
-  int group = 0, begin = 0;
-#pragma unroll
-  for (int k = 1; k < ORTHO_GROUPS; ++k)               // (all bounds are read at once)
-    if (id >= tiles.begin[k]) { group = k; begin = tiles.begin[k]; }
+  int id = all.first[xcd] + (int)(blockIdx.x >> 3);
+  const int end = all.first[xcd + 1];
+  asm volatile("" ::"s"(id), "s"(end), "s"(ws), "s"(step), "s"(p.shrink));      // loaded with the bounds, before the branch
+  const bool none = id >= end;
+  int group = group_of(all.begin, id);
+  asm volatile("" : "+s"(group));
+  if (none) return;
   const OrthoGroup& g = p.g[group];
-  id -= begin;
-  const int matrix = quotient(id, tiles.each[group]);
-  id -= matrix * tiles.each[group];
+  const OrthoProduct::Group& part = all.group[group];
+  // and the next batch, of the group's
+  const int64_t x0 = g.x[0], x1 = g.x[1];
+  asm volatile("" ::"s"(g.m), "s"(g.n), "s"(g.mp), "s"(g.np), "s"(g.tall), "s"(g.first), "s"(x0), "s"(x1), "s"(g.a), "s"(g.b),
+               "s"(part.each), "s"(part.tiles), "s"(part.split), "s"(part.tile_of), "s"(part.sums_of));
+  const int matrix = quotient(id, part.each);
+  id -= matrix * part.each;
   constexpr bool PIECES = MODE <= POLY;
-  const int pieces = PIECES ? tiles.split[group] : 1, of_matrix = PIECES ? tiles_of_matrix(g, TILE, MODE) : 1;
-  const int piece = PIECES && pieces > 1 ? quotient(id, of_matrix) : 0;
-  if (PIECES) id -= piece * of_matrix;
-  const int tile_id = id;
+  const int pieces = PIECES ? part.split : 1;
+  const int piece = PIECES && pieces > 1 ? quotient(id, part.tiles) : 0;
+  if (PIECES) id -= piece * part.tiles;
+  const int tile_of_all = matrix * part.tiles + id;
   int bi, bj;
   if (MODE <= POLY) {
     bi = (int)((sqrtf(8.f * id + 1.f) - 1.f) * 0.5f);
@@ -394,7 +402,7 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
   }
   const int64_t px = g.plane_x(), pa = g.plane_a();
   const int from = step & 1;
-  _Float16* X = (_Float16*)(ws + g.x[from]) + matrix * 2 * px;
+  _Float16* X = (_Float16*)(ws + (from ? x1 : x0)) + matrix * 2 * px;
   _Float16* A = (_Float16*)(ws + g.a) + matrix * 2 * pa;
   _Float16* B = (_Float16*)(ws + g.b) + matrix * 2 * pa;
   const int K = MODE == GRAM ? g.np : g.mp, stages_of_tile = K / S::KT;
@@ -543,8 +551,8 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
   if (pieces == 1) load_old();
   char* joint = nullptr;
   int& before = *(int*)(stages + 2 * S::STAGE - 4);
-  int* arrived = (int*)(ws + p.arrived) + tiles.tile_of[group] + matrix * of_matrix + tile_id;
-  if (PIECES && pieces > 1) joint = ws + p.sums + tiles.sums_of[group] + ((int64_t)matrix * of_matrix + tile_id) * pieces * (TILE * TILE * 4);
+  int* arrived = (int*)(ws + p.arrived) + part.tile_of + tile_of_all;
+  if (PIECES && pieces > 1) joint = ws + p.sums + part.sums_of + (int64_t)tile_of_all * pieces * (TILE * TILE * 4);
   const Shrink shrink = shrink_of(((const float*)(ws + p.shrink))[g.first + matrix], step);
   const float poly_b = NS_B * shrink.now * shrink.now, poly_c = NS_C * shrink.now * shrink.now * shrink.now * shrink.now * UNSCALE;
   const float scale = MODE == LAST ? shrink.ratio * shrink.next * UNSCALE * (MUON ? 0.2f * t.lr * sqrtf((float)g.n) : 1.f) : shrink.ratio;
@@ -568,7 +576,7 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
       }
       if (MODE != LAST) {
         const Terms<8> v2 = split_all<8>(v);
-        _Float16* to = (MODE == GRAM ? A : MODE == POLY ? B : (_Float16*)(ws + g.x[from ^ 1]) + matrix * 2 * px) + i * ld + j;
+        _Float16* to = (MODE == GRAM ? A : MODE == POLY ? B : (_Float16*)(ws + (from ? x0 : x1)) + matrix * 2 * px) + i * ld + j;
         *(f16x8*)to = v2.hi;
         *(f16x8*)(to + pl) = v2.lo;
       } else if (!g.tall && i < g.m && j < g.n) {
@@ -706,9 +714,9 @@ constexpr int SMALL_TURNS = (ORTHO_SMALL_LDS / 4096 + SMALL_WAVES - 1) / SMALL_W
 template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS) void small_kernel(OrthoPlan p, Source src, Target t, int steps) {
   extern __shared__ __align__(16) char stages[];
   __shared__ double sums[SMALL_WAVES];
-  int id = blockIdx.x;
-  const Place at = place_of(p, id, [](const OrthoGroup& g) { return g.small ? 1 : 0; });
-  const OrthoGroup& g = p.g[at.group];
+  int matrix = blockIdx.x;
+  const OrthoGroup& g = p.g[group_of(p.small.begin, matrix)];
+  asm volatile("" ::"s"(g.offset), "s"(g.stride), "s"(g.ld), "s"(g.rows), "s"(g.cols), "s"(g.m), "s"(g.n), "s"(g.mp), "s"(g.np), "s"(g.tall));
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lx = g.np + 8, la = g.mp + 8, px = g.mp * lx, pa = g.mp * la;      // row lengths and planes, in halves
   const SmallRoom room = small_room(g);
@@ -733,7 +741,7 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
     int i, j;
     const bool on = piece_at(n, i, j) && i < g.m;
     const int count = on ? min(8, g.n - j) : 0;
-    const int64_t e = g.tall ? element(g, at.matrix, j, i) : element(g, at.matrix, i, j), one = g.tall ? g.ld : 1;
+    const int64_t e = g.tall ? element(g, matrix, j, i) : element(g, matrix, i, j), one = g.tall ? g.ld : 1;
     float m[8];
     auto get = [&](const float* from, float* v) {
       if (!g.tall && quads && count == 8) {
@@ -982,7 +990,7 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
       const float4 a = *(const float4*)(R + r * lx + c), b = *(const float4*)(R + r * lx + c + 4);
       v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
-    const int64_t e = element(g, at.matrix, r, c);
+    const int64_t e = element(g, matrix, r, c);
     const int count = (g.tall ? g.m : g.n) - c;
     float w[8];
     if (MUON) load_eight(t, quads, e, count, w);
@@ -1003,14 +1011,14 @@ template <int NT, int NG> int launch_small(hipStream_t s, const OrthoPlan& p, co
 }
 
 template <int TILE, int MODE> int launch_tiles(hipStream_t s, const OrthoPlan& p, const Target& t, char* ws, int step) {
-  const OrthoProduct& tiles = p.product[MODE < APPLY ? MODE : APPLY];
+  const OrthoProduct& all = p.product[MODE < APPLY ? MODE : APPLY];
   int longest = 0;
-  for (int x = 0; x < 8; ++x) longest = tiles.first[x + 1] - tiles.first[x] > longest ? tiles.first[x + 1] - tiles.first[x] : longest;
+  for (int x = 0; x < 8; ++x) longest = all.first[x + 1] - all.first[x] > longest ? all.first[x + 1] - all.first[x] : longest;
   auto launch = [&](auto muon, OncePerDevice& once) -> int {
     constexpr bool MUON = decltype(muon)::value;
     const int lds = 2 * Tile<TILE>::STAGE;
     PPLL_TRY(raise_lds((const void*)product_kernel<TILE, MODE, MUON>, lds, once));
-    hipLaunchKernelGGL((product_kernel<TILE, MODE, MUON>), dim3(8 * (unsigned)longest), dim3(256), lds, s, p, tiles, t, ws, step);
+    hipLaunchKernelGGL((product_kernel<TILE, MODE, MUON>), dim3(8 * (unsigned)longest), dim3(256), lds, s, p, t, ws, step);
     PPLL_HIP(hipGetLastError());
     return PPLL_OK;
   };

@@ -73,35 +73,44 @@ void plan_product(OrthoPlan* p, int phase) {
       const double time = std::max((all + (std::ceil(parts / 512) * 512 - parts) * last) / 512, longest);
       if (best == 0 || time < best) { best = time; o.tile = tile; length = len; }
     }
-  // shares of equal work, in whole tiles
+  // shares of equal work, in whole parts
   double all = 0, before = 0;
-  int32_t tiles = 0, x = 0;
-  int32_t split_tiles = 0; int64_t split_pieces = 0;
+  int32_t parts = 0, x = 0, split_tiles = 0;
+  int64_t split_parts = 0;
   for (int k = 0; k < p->n; ++k) {
-    const int tl = tiles_of_matrix(p->g[k], o.tile, phase);
-    o.split[k] = pieces_of(p->g[k], phase, length);
-    o.tile_of[k] = split_tiles;
-    o.sums_of[k] = 4 * (int64_t)o.tile * o.tile * split_pieces;
-    if (o.split[k] > 1) { split_tiles += p->g[k].count * tl; split_pieces += (int64_t)p->g[k].count * tl * o.split[k]; }
-    all += (double)p->g[k].count * tl * o.split[k] * part_clocks(p->g[k], o.tile, phase, o.split[k]);
+    OrthoProduct::Group& part = o.group[k];
+    part.tiles = tiles_of_matrix(p->g[k], o.tile, phase);
+    part.split = pieces_of(p->g[k], phase, length);
+    part.each = part.tiles * part.split;
+    part.tile_of = split_tiles;
+    part.sums_of = 4 * (int64_t)o.tile * o.tile * split_parts;
+    if (part.split > 1) { split_tiles += p->g[k].count * part.tiles; split_parts += (int64_t)p->g[k].count * part.each; }
+    all += (double)p->g[k].count * part.each * part_clocks(p->g[k], o.tile, phase, part.split);
   }
   p->counters = std::max(p->counters, split_tiles);
-  p->sums = std::max<int64_t>(p->sums, 4 * (int64_t)o.tile * o.tile * split_pieces);
+  p->sums = std::max<int64_t>(p->sums, 4 * (int64_t)o.tile * o.tile * split_parts);
   o.first[0] = 0;
   for (int k = 0; k < p->n; ++k) {
-    const OrthoGroup& g = p->g[k];
-    o.each[k] = tiles_of_matrix(g, o.tile, phase) * o.split[k];
-    o.begin[k] = tiles;
-    const int32_t n = g.count * o.each[k];
-    const double one = part_clocks(g, o.tile, phase, o.split[k]);
+    o.begin[k] = parts;
+    const int32_t n = p->g[k].count * o.group[k].each;
+    const double one = part_clocks(p->g[k], o.tile, phase, o.group[k].split);
     // the boundaries that fall into this group
     while (x < 7 && n > 0 && before + n * one >= all * (x + 1) / 8)
-      o.first[++x] = tiles + (int32_t)std::min<double>(n, std::ceil((all * (x + 1) / 8 - before) / one));
+      o.first[++x] = parts + (int32_t)std::min<double>(n, std::ceil((all * (x + 1) / 8 - before) / one));
     before += n * one;
-    tiles += n;
+    parts += n;
   }
-  for (int k = p->n; k <= ORTHO_GROUPS; ++k) o.begin[k] = tiles;
-  while (x < 8) o.first[++x] = tiles;
+  for (int k = p->n; k < ORTHO_GROUPS; ++k) o.begin[k] = parts;
+  while (x < 8) o.first[++x] = parts;
+}
+template <class EACH> void count_items(const OrthoPlan& p, OrthoItems* items, EACH each) {
+  int32_t at = 0;
+  for (int k = 0; k < ORTHO_GROUPS; ++k) {
+    items->begin[k] = at;
+    if (k >= p.n) continue;
+    items->each[k] = each(p.g[k]);
+    at += p.g[k].count * items->each[k];
+  }
 }
 int64_t pad(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -159,6 +168,9 @@ int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* pla
   for (int phase = 0; phase < 3; ++phase) plan_product(plan, phase);
   plan->sums = take(plan->sums);
   plan->arrived = take(plan->counters * (int64_t)sizeof(int32_t));
+  count_items(*plan, &plan->pieces, [](const OrthoGroup& g) { return g.small ? 0 : g.pieces(); });
+  count_items(*plan, &plan->squares, [](const OrthoGroup& g) { return g.small ? 0 : g.mp / 64 * (g.np / 64); });
+  count_items(*plan, &plan->small, [](const OrthoGroup& g) { return g.small ? 1 : 0; });
   plan->partials = take(pieces * (int64_t)sizeof(double));
   plan->shrink = take(matrices * (int64_t)sizeof(float));
   plan->bytes = at;

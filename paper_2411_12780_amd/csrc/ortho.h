@@ -11,7 +11,7 @@ constexpr int ORTHO_GROUPS = 16;       // groups of a call
 constexpr int ORTHO_SIDE = 8192;       // rows and columns of a matrix, at most
 constexpr int ORTHO_COUNT = 65535;     // matrices of a group, at most
 constexpr int ORTHO_STEPS = 16;        // Newton-Schulz steps, at most
-constexpr int NORM_ROWS = 32, NORM_COLS = 256;   // piece of a matrix whose squares one workgroup adds up
+constexpr int NORM_ROWS = 16, NORM_COLS = 256;   // piece of a matrix whose squares one workgroup adds up
 
 constexpr int ORTHO_SMALL_LDS = 160 * 1024 - 256;   // what a workgroup of the small kernel may have (256 bytes are its own)
 
@@ -50,25 +50,34 @@ __host__ __device__ inline int tiles_of_matrix(const OrthoGroup& g, int tile, in
   const int down = (g.mp + tile - 1) / tile, across = (g.np + tile - 1) / tile;
   return phase <= ORTHO_POLY ? down * (down + 1) / 2 : down * across;      // of a symmetric result those on and under the diagonal
 }
-// The tiles of one product: `each` of a matrix, those of group k from begin[k] on.  Workgroup w runs on XCD w % 8.  Each XCD has a run of the
-// tiles, first[x] .. first[x + 1], with an eighth of the work: tiles of one matrix, which read the same rows at about the same time, meet in one L2.
+// Work items of a launch, `each` of a matrix: those of group k from begin[k] on (a group that has none begins where the next one does).  A kernel
+// finds its group from one batch of loads, and what it needs of the group with the next: its arguments lie in memory, where a load takes half a
+// microsecond, and a search that reads group by group is a chain of them.
+struct OrthoItems { int32_t begin[ORTHO_GROUPS], each[ORTHO_GROUPS]; };
+// The tiles of one product.  Workgroup w runs on XCD w % 8.  Each XCD has a run of the tiles, first[x] .. first[x + 1], with an eighth of the work:
+// tiles of one matrix, which read the same rows at about the same time, meet in one L2.
 struct OrthoProduct {
   int32_t tile;                        // 64 or 128
-  int32_t first[9], begin[ORTHO_GROUPS + 1], each[ORTHO_GROUPS];
-  int32_t split[ORTHO_GROUPS];         // pieces of the k of a tile, each a workgroup's
-  int32_t tile_of[ORTHO_GROUPS];       // the group's first tile among those in pieces
-  int64_t sums_of[ORTHO_GROUPS];       // and its first sums, in bytes
+  int32_t first[9], begin[ORTHO_GROUPS];
+  struct Group {
+    int32_t each, tiles;               // parts and tiles of a matrix
+    int32_t split;                     // parts of a tile, each with a piece of the k and a workgroup of its own
+    int32_t tile_of;                   // the group's first tile among those in pieces
+    int64_t sums_of;                   // and its first sums, in bytes
+  } group[ORTHO_GROUPS];
 };
 struct OrthoPlan {
   OrthoGroup g[ORTHO_GROUPS];          // longest rows first: their tiles take the longest
   int32_t n;                           // groups with a matrix in them
   OrthoProduct product[3];
+  OrthoItems pieces, squares, small;   // of the sums of squares, of the normalisation, matrices of the small kernel
   int64_t partials;                    // byte offset of the partial sums of squares, one double a piece
   int64_t shrink;                      // and of a float for each matrix (see k_ortho.hip)
   int64_t sums, arrived;               // of the tiles whose k is in pieces: sums of each piece, and how many of them are there (an int a tile)
   int32_t counters;                    // such tiles, of the product that has the most
   int64_t bytes;
 };
+static_assert(sizeof(OrthoPlan) <= 3900, "a kernel takes 4 KB of arguments");
 
 // Checks the groups and lays the workspace out.  PPLL_OK, or an error with its text set.
 int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* plan);
