@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256, 8) void normalise_kernel(OrthoPlan p, Source s
     const int64_t first = element(g, matrix, r0 + t / 16, c0 + t % 16 * 4);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      u[k] = *(const float4*)((s.in ? (const float*)s.in : s.g) + first + k * 16 * g.ld);
+      u[k] = s.in || s.nesterov ? *(const float4*)((s.in ? (const float*)s.in : s.g) + first + k * 16 * g.ld) : make_float4(0.f, 0.f, 0.f, 0.f);
       if (!s.in) m[k] = *(const float4*)(s.m + first + k * 16 * g.ld);
     }
   } else {
