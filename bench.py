@@ -64,6 +64,9 @@ def step_flops(wl: dict, dense: bool = False) -> float:
     return total + 3.0 * aux + 3.0 * 2.0 * B * A * wl["num_classes"]
 
 
+OPTIMIZERS = ("sgd", "adamw", "muon")      # by the number in a configuration
+
+
 def kernel_source_sha() -> str:
     """Hash of the kernel sources the library is built from: a counter summary is only valid for the sources it
     was taken with."""
@@ -191,7 +194,7 @@ def bench_pipeline(args, torch, P, synth, dev) -> int:
         "warmup": max(args.warmup, 8), "ms_per_step": 1e3 * elapsed / args.steps, "higher_is_better": True,
         "scaling": "weak", "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
         "config": dict({"workload": args.workload, "batch": first["batch"], "blocks": len(cfgs), "queue_depth": depth,
-                        "streams": len(cfgs), "optimizer": "adamw" if first["optimizer"] == 1 else "sgd"},
+                        "streams": len(cfgs), "optimizer": OPTIMIZERS[first["optimizer"]]},
                        **({"layers_per_block": [w["depth"] for w in wls], "aux_depths": [w["aux_depth"] for w in wls]}
                           if vit else {"basic_blocks_per_module": [w["n_basic_blocks"] for w in wls],
                                        "channels": [w["channels"] for w in wls]})),
@@ -325,7 +328,7 @@ def main() -> int:
         "config": {"workload": args.workload, "batch": wl["batch"],
                    "shape": {k: wl[k] for k in ("tokens", "dim", "heads", "mlp_dim", "depth", "aux_depth",
                                                 "channels", "height", "width", "n_basic_blocks") if k in wl},
-                   "optimizer": "adamw" if wl["optimizer"] == synth.ADAMW else "sgd"},
+                   "optimizer": OPTIMIZERS[wl["optimizer"]]},
         "step_gflop": flops / 1e9,
         **({"step_gflop_note": "executed work: of the last auxiliary layer only the class-token row is computed behind K, V",
             "step_gflop_dense_definition": step_flops(wl, dense=True) / 1e9} if wl["arch"] == synth.VIT else {}),

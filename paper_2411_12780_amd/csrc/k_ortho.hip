@@ -72,7 +72,9 @@ __device__ __forceinline__ bool in_quads(const OrthoGroup& g) { return ((g.offse
 __device__ __forceinline__ int64_t element(const OrthoGroup& g, int matrix, int r, int c) {
   return g.offset + (int64_t)matrix * g.stride + (int64_t)r * g.ld + c;
 }
-// The group that work item `id` of a launch belongs to; id becomes the place within the group.  All bounds are read at once.
+// The group that work item `id` of a launch belongs to; id becomes the place within the group.  All bounds are read at once: arguments lie in
+// memory, and a search that reads them group by group made each launch of a small batch half a microsecond longer (five steps of five 201 x 333
+// matrices 136.7 us, 129.2 with two batches of loads, of the bounds and of the group).
 __device__ __forceinline__ int group_of(const int32_t (&begin)[ORTHO_GROUPS], int& id) {
   static_assert(ORTHO_GROUPS == 16, "");
   asm volatile("" ::"s"(begin[1]), "s"(begin[2]), "s"(begin[3]), "s"(begin[4]), "s"(begin[5]), "s"(begin[6]), "s"(begin[7]), "s"(begin[8]),
@@ -84,7 +86,6 @@ __device__ __forceinline__ int group_of(const int32_t (&begin)[ORTHO_GROUPS], in
   id -= from;
   return group;
 }
-// Values that a kernel needs sooner or later, loaded here and now
 __device__ __forceinline__ float read_u(const Source& s, int64_t at) {
   if (s.in) return ld_f(s.in, (size_t)at, s.dt);
   const float m = s.m[at];
@@ -136,7 +137,9 @@ __device__ __forceinline__ double sum_of_all(double v) {
   return waves[0] + waves[1] + waves[2] + waves[3];
 }
 
-// The momentum, and the sums of squares of pieces of 16 x 256 (in 64 bits: gradients of 1e-25 or 1e25 have a norm as well).
+// The momentum, and the sums of squares of pieces of 16 x 256 (in 64 bits: gradients of 1e-25 or 1e25 have a norm as well).  Bound by memory: 25 M
+// gradients and momenta in 55 us, 5.5 TB/s.  Longer pieces hold fewer threads' loads in flight (32 rows: 60 us, and 13 instead of 7 for five
+// matrices of 201 x 333, whose rows are no multiple of 16 bytes).
 __global__ __launch_bounds__(256) void squares_kernel(OrthoPlan p, Source s, char* ws) {
   int id = blockIdx.x;
   const int group = group_of(p.pieces.begin, id);
@@ -194,7 +197,8 @@ __global__ __launch_bounds__(256) void squares_kernel(OrthoPlan p, Source s, cha
   if (threadIdx.x == 0) ((double*)(ws + p.partials))[g.first_piece + matrix * each + id] = sum;
 }
 
-// Y = u / |u|, in tiles of 64 x 64.
+// Y = u / |u|, in tiles of 64 x 64.  Bound by memory: 25 M momenta in 47 us, 4.3 TB/s.  A tile's elements are on their way while the workgroup
+// adds up the pieces' sums; tall matrices are turned in LDS.
 __global__ __launch_bounds__(256, 8) void normalise_kernel(OrthoPlan p, Source s, char* ws) {
   int id = blockIdx.x;
   const int group = group_of(p.squares.begin, id);
@@ -266,6 +270,11 @@ __global__ __launch_bounds__(256, 8) void normalise_kernel(OrthoPlan p, Source s
 // LDS; there are two stages.  A wave multiplies 64 x 64: three products of 32 x 32 x 16 for each pair of fragments, 12 for eight fragments read.
 //  TILE 128: a wave has a quarter of the tile and all k.  TILE 64: it has all of the tile and a quarter of the k, and the four sums are added up
 //  at the end: fragments are read once for 12 products all the same, where quarters of 32 x 32 would read twice as much for each.
+// Bound, with many tiles, by the power that the matrix instructions draw: two of 1536 x 6144, five steps, X X' 120 us, b A + c A A 43, the
+// application 185, the last 190 us: 0.94 PFLOP/s of fp16 in the application, where a large library product of fp16 runs at 1.16 and clocks are 1.7
+// to 1.8 GHz.  With few, by the way of the first copies and the epilogue: 7 - 9 us a launch of 50 tiles with 4 to 6 stages.  Slower: four stages and
+// one workgroup a unit (application 170 -> 199 us over wide layers), eight waves that share the k of a tile of 128 (168 -> 193), the copies
+// between the products of a k step (five 201 x 333 matrices 125.6 -> 130.6).
 // Layouts in LDS, as in gemm_pipe.h: k contiguous (P, and Q of GRAM and POLY): rows of KT k, their 16-byte granules permuted; k rows (X of APPLY):
 // rows of TILE columns whose 64-byte windows are permuted, for the transposing read.
 template <int TILE> struct Tile {
@@ -698,8 +707,9 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
 
 // ------------------------------------------------------------------ small matrices
 // All steps of one matrix in one workgroup of 8 waves: X and the symmetric matrices stay in LDS as planes, rows 16 bytes longer than their
-// elements, so that pieces of neighbouring rows meet no bank twice.  Bound by LDS reads and the barriers between the products: with tiles of
-// 16 x 16 on 16 waves, which read each element twice as often, a step of 64 x 64 took 2.7 us and one of 128 x 128 15.3.
+// elements, so that pieces of neighbouring rows meet no bank twice.  Bound by the chain of LDS reads, products, conversions and barriers: a step of
+// 64 x 64 takes 2.8 us, of 288 x 32 4.4, of 128 x 128 10.0.  Tiles of 16 x 16 on 16 waves, which read each element twice as often: 2.7 and 15.3 (64
+// and 128).
 //  Gram and square: tiles of 32 x 32 on and under the diagonal, dealt out to the waves; where there are fewer (one, or three of long rows) the
 //  waves share the k and add up in LDS.
 //  The results of a product wait in registers until everyone has read what they replace, unless there is room for a second buffer.

@@ -30,7 +30,8 @@ __device__ __forceinline__ void fill_table(const RotaryArgs& a, int row0, int ro
   }
 }
 
-// Any head width, any alignment: a wave a head, element by element.
+// Any head width, any alignment: a wave a head, element by element.  What the kernel below does not take: heads that turn in part, widths and
+// strides with less in common than 8 bytes.
 template <bool BWD> __global__ __launch_bounds__(256) void rotary_plain_kernel(RotaryArgs a, int dt) {
   extern __shared__ float2 table[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, P = a.p.pairs, hd = a.p.hd;
@@ -138,7 +139,9 @@ __device__ __forceinline__ float head_sum(float v, int lanes) {
 
 // Heads that turn whole, V pairs a lane in two pieces of V elements (of either half of the head, or neighbours), the head's P / V lanes
 // rounded up to a power of two; queries and keys in workgroups of their own (blockIdx.y), which leaves registers for the sums of one side
-// and the next head's elements on their way.  Bound by memory: each element is read and written once, cos and sin come from LDS.
+// and the next head's elements on their way.  Bound by memory: each element is read and written once, cos and sin come from LDS.  664 MB of a
+// clip's queries and keys (64800 rows, 16 and 4 heads of 128, bf16) in 127 us, 5.2 TB/s, a copy's rate; the gradients of 25216 rows with 12 + 12
+// heads of 64 and the norm, 232 MB, in 53 us, 4.4 TB/s.  Small calls by the launch and the table: 8320 rows with 6 + 6 heads 10.8 us forward.
 template <class T, int V, bool NEXT, bool NORM, bool BWD> __global__ __launch_bounds__(256, 4) void rotary_kernel(RotaryArgs a) {
   extern __shared__ float2 table[];
   const int side = a.p.heads[0] ? blockIdx.y : 1;
@@ -231,7 +234,7 @@ template <class T, int V, bool NEXT, bool NORM, bool BWD> __global__ __launch_bo
   if (e < hd) a.partials[((int64_t)blockIdx.x * 2 + side) * hd + e] = part[0][e] + part[1][e] + part[2][e] + part[3][e];
 }
 
-// d scale from the workgroups' partial sums, 16 elements a workgroup; queries first, then keys
+// d scale from the workgroups' partial sums, 16 elements a workgroup; queries first, then keys.  A launch of no size: 4.4 us for 512 rows of sums.
 __global__ __launch_bounds__(1024) void rotary_scale_kernel(const float* partials, int chunks, int hd, float* dq, float* dk) {
   __shared__ float red[64][17];
   const int col = threadIdx.x & 15, grp = threadIdx.x >> 4, across = (hd + 15) / 16;
