@@ -46,21 +46,29 @@ struct Source { const void* in; int dt; const float* g; float* m; float momentum
 // Where the result goes: out (orthogonalize), or null: the parameters
 struct Target { void* out; int dt; float* p; uint16_t* shadow; float lr, decay; };
 
-// hi and lo of n values.  Each is pinned to its fp32 value first: the compiler may fold the arithmetic that gives it into one of the conversions
-// (a fused operation that rounds to fp16 once) and not into the other, and at a tie hi and what lo is counted from are then two neighbours (one
-// element in some 20000 was off by a whole step of hi, 2^-11 of it).  Two values are converted by one instruction; lo is one fused operation.
+// hi and lo of n values: two values to hi in one instruction, and each lo = value - hi, rounded once, in one mixed-precision instruction that reads hi as
+// it was stored.  (Left to the compiler, the arithmetic that gives a value may be folded into one of two conversions and not into the other, and at a tie
+// hi and what lo is counted from are two neighbours: one element in some 20000 was off by a whole step of hi, 2^-11 of it.)
 template <int N> struct Terms { _Float16 __attribute__((ext_vector_type(N))) hi, lo; };
 template <int N> __device__ __forceinline__ Terms<N> split_all(const float* v) {
-  Terms<N> r;
+  typedef __attribute__((ext_vector_type(N / 2))) uint32_t words;
+  words hi, lo;
 #pragma unroll
-  for (int k = 0; k < N; k += 2) {
-    float a = v[k], b = v[k + 1];
-    asm("" : "+v"(a), "+v"(b));
-    const _Float16 ha = (_Float16)a, hb = (_Float16)b;
-    r.hi[k] = ha; r.hi[k + 1] = hb;
-    r.lo[k] = (_Float16)fmaf((float)ha, -1.f, a); r.lo[k + 1] = (_Float16)fmaf((float)hb, -1.f, b);
+  for (int k = 0; k < N / 2; ++k) {
+    uint32_t h, l;
+    asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(h) : "v"(v[2 * k]), "v"(v[2 * k + 1]));
+    asm("v_fma_mixlo_f16 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(l) : "v"(h), "v"(v[2 * k]));
+    asm("v_fma_mixhi_f16 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(l) : "v"(h), "v"(v[2 * k + 1]));
+    hi[k] = h; lo[k] = l;
   }
-  return r;
+  return {__builtin_bit_cast(decltype(Terms<N>::hi), hi), __builtin_bit_cast(decltype(Terms<N>::lo), lo)};
+}
+// v[0] and v[1] plus `by` times the two values whose terms the words hold: two mixed-precision instructions a value
+__device__ __forceinline__ void add_two(float* v, uint32_t hi, uint32_t lo, float by) {
+  asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel_hi:[1,0,0]" : "+v"(v[0]) : "v"(lo), "v"(by));
+  asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(v[1]) : "v"(lo), "v"(by));
+  asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel_hi:[1,0,0]" : "+v"(v[0]) : "v"(hi), "v"(by));
+  asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(v[1]) : "v"(hi), "v"(by));
 }
 // a / b for a >= 0, b > 0 and a quotient under 2^21 (tiles of a side, matrices of a group): in fp32 it is off by less than one
 __device__ __forceinline__ int quotient(int a, int b) {
@@ -575,9 +583,11 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
       const float4 lo4 = *(const float4*)from_lds, hi4 = *(const float4*)(from_lds + 4);
       float v[8] = {lo4.x, lo4.y, lo4.z, lo4.w, hi4.x, hi4.y, hi4.z, hi4.w};
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float old = MODE == GRAM ? 0.f : (float)old_h[ps * EACH + n][k] + (float)old_l[ps * EACH + n][k];
-        v[k] = MODE == GRAM ? v[k] * UNSCALE : MODE == POLY ? fmaf(poly_b, old, poly_c * v[k]) : fmaf(NS_A, old, v[k] * UNSCALE) * scale;
+      for (int k = 0; k < 8; ++k) v[k] *= MODE == GRAM ? UNSCALE : MODE == POLY ? poly_c : UNSCALE * scale;
+      if (MODE != GRAM) {
+        const u32x4 h = __builtin_bit_cast(u32x4, old_h[ps * EACH + n]), l = __builtin_bit_cast(u32x4, old_l[ps * EACH + n]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) add_two(v + 2 * k, h[k], l[k], MODE == POLY ? poly_b : NS_A * scale);
       }
       if (mirrored || (MODE == LAST && g.tall)) {
         *(float4*)from_lds = make_float4(v[0], v[1], v[2], v[3]);
@@ -863,12 +873,17 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
     i0 = 32 * i; j0 = 32 * (n - i * (i + 1) / 2);
   };
   const int ts = whole ? ta * ta : ta * (ta + 1) / 2, col = 4 * (lane >> 5);
-  auto add_old = [&](const _Float16* from, int plane, f32x16 v, float old_by, float by, float ratio) {
+  auto add_old = [&](const _Float16* from, int plane, f32x16 v, float old_by, float by) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const f16x4 h = *(const f16x4*)(from + 8 * q), l = *(const f16x4*)(from + plane + 8 * q);
+      const u32x2 h = *(const u32x2*)(from + 8 * q), l = *(const u32x2*)(from + plane + 8 * q);
+      float four[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[4 * q + e] = fmaf(old_by, (float)h[e] + (float)l[e], by * (v[4 * q + e] * UNSCALE)) * ratio;
+      for (int e = 0; e < 4; ++e) four[e] = v[4 * q + e] * by;
+      add_two(four, h.x, l.x, old_by);
+      add_two(four + 2, h.y, l.y, old_by);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * q + e] = four[e];
     }
     return v;
   };
@@ -943,7 +958,7 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
       if (tile >= ts) break;
       int i0, j0;
       sym_tile(tile, i0, j0);
-      held[n] = add_old(A + (i0 + row) * la + j0 + col, pa, rows_product(A, la, pa, i0, j0, 0, g.mp), NS_B * t2, NS_C * t2 * t2, 1.f);
+      held[n] = add_old(A + (i0 + row) * la + j0 + col, pa, rows_product(A, la, pa, i0, j0, 0, g.mp), NS_B * t2, NS_C * t2 * t2 * UNSCALE);
     }
     if (!room.two_a) __syncthreads();
 #pragma unroll
@@ -960,7 +975,7 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
     for (int n = 0; n < NT; ++n) {
       const int tile = nth(n), i0 = tile / tx * 32, j0 = tile % tx * 32;
       if (tile >= ta * tx) break;
-      held[n] = add_old(X + (i0 + row) * lx + j0 + col, px, columns_product(X, i0, j0), NS_A, 1.f, shrink.ratio);
+      held[n] = add_old(X + (i0 + row) * lx + j0 + col, px, columns_product(X, i0, j0), NS_A * shrink.ratio, UNSCALE * shrink.ratio);
     }
     if (k + 1 == steps) break;
     if (!room.two_x) __syncthreads();
