@@ -827,22 +827,32 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
   // 64 k at a time, all fragments on their way before the first product: one wait for LDS instead of four.  32 where that many registers are taken.
   struct Pair { f16x8 ph, pl, qh, ql; };
   auto sum_up = [&](int from, int to, auto load) {
-    f32x16 hh = {}, xx = {};
-    auto piece = [&](int k, auto n) {
+    f32x16 hh, xx;
+    auto piece = [&](int k, auto n, auto first) {
       Pair f[decltype(n)::value];
 #pragma unroll
       for (int i = 0; i < decltype(n)::value; ++i) f[i] = load(k + 16 * i);
 #pragma unroll
       for (int i = 0; i < decltype(n)::value; ++i) {
-        hh = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i].qh, f[i].ph, hh, 0, 0, 0);
-        xx = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i].ql, f[i].ph, xx, 0, 0, 0);
+        const bool none = decltype(first)::value && i == 0;          // (the instruction takes a zero as it is)
+        hh = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i].qh, f[i].ph, none ? f32x16{} : hh, 0, 0, 0);
+        xx = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i].ql, f[i].ph, none ? f32x16{} : xx, 0, 0, 0);
         xx = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[i].qh, f[i].pl, xx, 0, 0, 0);
       }
     };
+    std::integral_constant<int, 4> four;
+    std::integral_constant<int, 2> two;
+    if (from >= to) return f32x16{};
     int k = from;
-    if (NT <= 2)
-      for (; k + 64 <= to; k += 64) piece(k, std::integral_constant<int, 4>());
-    for (; k < to; k += 32) piece(k, std::integral_constant<int, 2>());
+    if (NT <= 2 && k + 64 <= to) {
+      piece(k, four, std::true_type());
+      for (k += 64; k + 64 <= to; k += 64) piece(k, four, std::false_type());
+      if (k < to) piece(k, two, std::false_type());
+    } else {
+      piece(k, two, std::true_type());
+      if (NT > 2)
+        for (k += 32; k < to; k += 32) piece(k, two, std::false_type());
+    }
     return hh + xx;
   };
   auto rows_product = [&](const _Float16* P, int ld, int plane, int i0, int j0, int from, int to) {
