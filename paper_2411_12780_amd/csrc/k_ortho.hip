@@ -136,10 +136,29 @@ template <bool MUON> __device__ __forceinline__ void store_eight(const Target& t
   }
 }
 
+// The sum over a wave, in every lane: over 16 lanes by moves within the vector unit (a move through LDS takes ten times as long), then of four
+template <int MOVE> __device__ __forceinline__ double add_moved(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, MOVE, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), MOVE, 0xf, 0xf, true);
+  return v + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double sum_of_wave(double v) {
+  v = add_moved<0xb1>(v);                // neighbours
+  v = add_moved<0x4e>(v);                // pairs
+  v = add_moved<0x141>(v);               // mirrored in eight lanes
+  v = add_moved<0x140>(v);               // in sixteen
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  auto row = [&](int lane) {
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  };
+  return row(0) + row(16) + (row(32) + row(48));
+}
 // The sum over a workgroup of four waves, in every thread
 __device__ __forceinline__ double sum_of_all(double v) {
   __shared__ double waves[4];
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  v = sum_of_wave(v);
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
   __syncthreads();
   return waves[0] + waves[1] + waves[2] + waves[3];
@@ -718,8 +737,8 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
 // ------------------------------------------------------------------ small matrices
 // All steps of one matrix in one workgroup of 8 waves: X and the symmetric matrices stay in LDS as planes, rows 16 bytes longer than their
 // elements, so that pieces of neighbouring rows meet no bank twice.  Bound by the chain of LDS reads, products, conversions and barriers: a step of
-// 64 x 64 takes 2.8 us, of 288 x 32 4.4, of 128 x 128 10.0.  Tiles of 16 x 16 on 16 waves, which read each element twice as often: 2.7 and 15.3 (64
-// and 128).
+// 64 x 64 takes 2.4 us, of 288 x 32 3.8, of 128 x 128 9.0 (2.8, 4.4 and 10.0 with a conversion an instruction and sums that begin with zeros in
+// registers).  Tiles of 16 x 16 on 16 waves, which read each element twice as often, were level with that at 64 x 64 and took 15.3 at 128 x 128.
 //  Gram and square: tiles of 32 x 32 on and under the diagonal, dealt out to the waves; where there are fewer (one, or three of long rows) the
 //  waves share the k and add up in LDS.
 //  The results of a product wait in registers until everyone has read what they replace, unless there is room for a second buffer.
@@ -799,7 +818,7 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum += (double)u[n][k] * u[n][k];
   }
-  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  sum = sum_of_wave(sum);
   if (lane == 0) sums[wave] = sum;
   __syncthreads();
   sum = 0;
@@ -824,7 +843,8 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
 
   // ---- products of 32 x 32: lane l holds row l % 32, columns 8 q + 4 (l / 32) + e in element 4 q + e
   const int row = lane & 31, kpart = 8 * (lane >> 5);
-  // 64 k at a time, all fragments on their way before the first product: one wait for LDS instead of four.  32 where that many registers are taken.
+  // 64 k at a time, 32 where that many registers are taken.  (All sixteen fragments on their way before the first product, which the compiler does not
+  // do by itself: five steps of 64 x 64 19.7 -> 20.2 us.)
   struct Pair { f16x8 ph, pl, qh, ql; };
   auto sum_up = [&](int from, int to, auto load) {
     f32x16 hh, xx;
