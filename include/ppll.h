@@ -282,6 +282,7 @@ typedef struct {
  * with the groups' layout; out_dev may be in_dev; elements of out_dev outside the matrices are left as they are.  steps: 1..16.
  * All arithmetic is at fp32 precision whichever the type (operands of the products as two fp16 terms each).  A matrix of zeros gives
  * zeros; one with a NaN or an infinity gives NaN in all its elements and leaves the others alone.
+ * Calls with the same groups give the same bits; with other groups beside it a matrix may be summed up in another order.
  * Workspace: ppll_orthogonalize_workspace_bytes(the same groups) bytes, used by nothing else until the stream has passed the call; its
  * contents need not survive between calls, and calls that may run at the same time need one each.  Asynchronous on hip_stream; may be
  * captured into a graph.  n_groups = 0 and groups of count 0 are allowed. */
