@@ -401,7 +401,7 @@ template <int N> __device__ __forceinline__ bool join(f32x16 (&v)[N], char* sums
 template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) void product_kernel(OrthoPlan p, Target t, char* ws, int step) {
   using S = Tile<TILE>;
   constexpr bool TR = MODE >= APPLY;
-  extern __shared__ __align__(256) char stages[];
+  extern __shared__ __align__(256) char stages[];     // (behind the 256 bytes of the next line and nothing else: k_step turns bits of addresses below 256)
   PPLL_CODE_TO_L2(2);
   // ---- which tile
   const OrthoProduct& all = p.product[MODE < APPLY ? MODE : APPLY];
@@ -687,27 +687,29 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
       }
     }
   } else {
-    // the four waves' sums: each adds up the 32 x 32 tile of its number and finishes 16 rows of the whole
+    // the four waves' sums: each adds up the 32 x 32 tile of its number, which it holds a part of itself, and finishes 16 rows of the whole
     float4* quarters = (float4*)stages;                 // [wave][tile][q][lane]
     float* sums = (float*)stages;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x16& v = hh[k >> 1][k & 1];
-        quarters[((wave * 4 + k) * 4 + q) * 64 + lane] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-      }
-    __syncthreads();
     f32x16 acc;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      float4 a = quarters[(wave * 4 + q) * 64 + lane];
-#pragma unroll
-      for (int w = 1; w < 4; ++w) {
-        const float4 b = quarters[((w * 4 + wave) * 4 + q) * 64 + lane];
-        a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+    for (int k = 0; k < 4; ++k) {
+      const f32x16& v = hh[k >> 1][k & 1];
+      if (k == wave) {
+        acc = v;
+        continue;
       }
-      acc[4 * q] = a.x; acc[4 * q + 1] = a.y; acc[4 * q + 2] = a.z; acc[4 * q + 3] = a.w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) quarters[((wave * 4 + k) * 4 + q) * 64 + lane] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      const int other = wave ^ w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float4 b = quarters[((other * 4 + wave) * 4 + q) * 64 + lane];
+        acc[4 * q] += b.x; acc[4 * q + 1] += b.y; acc[4 * q + 2] += b.z; acc[4 * q + 3] += b.w;
+      }
     }
     if (PIECES && pieces > 1) {
       f32x16 v[1] = {acc};
