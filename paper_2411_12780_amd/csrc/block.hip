@@ -4,6 +4,7 @@
 #include "block.h"
 #include "plan.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -247,14 +248,12 @@ size_t Block::plan(char* base) {
     const std::vector<ppll_matrix_group> groups = muon_groups();
     (void)ortho_plan(groups.data(), (int)groups.size(), &ortho);   // sizes that it refuses, validate_config has refused
     ortho_ws = (char*)bump.take((size_t)ortho.bytes);
-    auto matrix = [&](size_t off) {
-      for (const ppll_matrix_group& g : groups)
-        for (int i = 0; i < g.count; ++i)
-          if ((int64_t)off == g.offset + i * g.stride) return true;
-      return false;
-    };
+    std::vector<int64_t> matrices;         // where they begin
+    for (const ppll_matrix_group& g : groups)
+      for (int i = 0; i < g.count; ++i) matrices.push_back(g.offset + i * g.stride);
+    std::sort(matrices.begin(), matrices.end());
     for (const TensorDesc& t : tensors) {
-      if (matrix(t.off)) continue;
+      if (std::binary_search(matrices.begin(), matrices.end(), (int64_t)t.off)) continue;
       if (!adam_ranges.empty() && adam_ranges.back().off + adam_ranges.back().n == t.off) adam_ranges.back().n += t.n;
       else adam_ranges.push_back({t.off, t.n});
     }
