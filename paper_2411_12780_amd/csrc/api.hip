@@ -181,7 +181,9 @@ int ppll_block_workspace_bytes(const ppll_block_config* cfg, size_t* bytes) {
   if (!bytes) { set_error("bytes is null"); return PPLL_ERR_NULL; }
   Block b;
   b.cfg = full;
-  *bytes = b.plan(nullptr);
+  const size_t need = b.plan(nullptr);
+  PPLL_TRY(b.plan_status);
+  *bytes = need;
   return PPLL_OK;
 }
 
@@ -192,6 +194,7 @@ int ppll_block_param_bytes(const ppll_block_config* cfg, size_t* bytes) {
   Block b;
   b.cfg = full;
   b.plan(nullptr);
+  PPLL_TRY(b.plan_status);
   *bytes = b.P * sizeof(float);
   return PPLL_OK;
 }
@@ -230,6 +233,11 @@ int ppll_block_init(const ppll_block_config* cfg, void* workspace_dev, size_t wo
   b.cfg = full;
   b.device = device;
   size_t need = b.plan((char*)workspace_dev);
+  if (b.plan_status != PPLL_OK) {
+    const int st = b.plan_status;
+    delete h;
+    return st;
+  }
   if (workspace_bytes < need) {
     set_error("workspace has %zu bytes, %zu needed", workspace_bytes, need);
     delete h;
@@ -477,7 +485,7 @@ int ppll_pipeline_workspace_bytes(const ppll_block_config* given, int32_t K, int
   ppll_block_in_bytes(&cfgs[0], &in_b);
   total += (size_t)depth * (align256(in_b) + lab);
   for (int j = 0; j < K; ++j) {
-    ppll_block_workspace_bytes(&cfgs[j], &ws);
+    PPLL_TRY(ppll_block_workspace_bytes(&cfgs[j], &ws));
     ppll_block_out_bytes(&cfgs[j], &out_b);
     total += align256(ws);
     total += j < K - 1 ? (size_t)depth * (align256(out_b) + lab) : align256(out_b);

@@ -101,6 +101,7 @@ struct Block {
   // What Muon updates (groups of equal matrices), and the ranges of the blob that are left to AdamW
   std::vector<ppll_matrix_group> muon_groups() const;
   OrthoPlan ortho{};
+  int plan_status = PPLL_OK;          // what plan() found beyond validate_config's reach
   char* ortho_ws = nullptr;
   std::vector<BlobRange> adam_ranges;
   size_t pe_w = 0, pe_b = 0, cls = 0, pos = 0, head_ln_g = 0, head_ln_b = 0, head_w = 0, head_b = 0;

@@ -242,11 +242,12 @@ size_t Block::plan(char* base) {
   mom2 = cfg.optimizer != PPLL_SGD ? bump.floats(P) : nullptr;
   shadow = dt == BF16 ? (uint16_t*)bump.take(P * sizeof(uint16_t)) : nullptr;
   adam_ranges.clear();
+  plan_status = PPLL_OK;
   ortho = OrthoPlan{};
   ortho_ws = nullptr;
   if (cfg.optimizer == PPLL_MUON) {
     const std::vector<ppll_matrix_group> groups = muon_groups();
-    (void)ortho_plan(groups.data(), (int)groups.size(), &ortho);   // sizes that it refuses, validate_config has refused
+    if (ortho_plan(groups.data(), (int)groups.size(), &ortho) != PPLL_OK) plan_status = PPLL_ERR_CONFIG;   // more matrices than a call takes
     ortho_ws = (char*)bump.take((size_t)ortho.bytes);
     std::vector<int64_t> matrices;         // where they begin
     for (const ppll_matrix_group& g : groups)
