@@ -269,7 +269,9 @@ int ppll_probe_copy(const void* src_dev, void* dst_dev, size_t bytes, void* hip_
  * matrix i is blob[offset + i * stride + r * ld + c].  The matrices of a group lie one behind the other (stride >= (rows - 1) * ld + cols)
  * or side by side (stride >= cols, (count - 1) * stride + cols <= ld: the query, key and value parts of a [dim, 3 dim] weight).  No element
  * belongs to two matrices of a call: groups whose extents overlap need one ld and different columns of it, else PPLL_ERR_SHAPE.
- * rows, cols: 1..8192; count: 0..65535; offset and stride >= 0. */
+ * rows, cols: 1..8192; count: 0..65535; offset and stride >= 0.  Those matrices of a call that need a workspace come to fewer than 2^24
+ * pieces of 16 x 256 elements and fewer than 2^24 tiles of 64 x 64 (a launch holds no more; over 100 GB of workspace: 32767 columns of 8192
+ * elements, say), else PPLL_ERR_SHAPE before anything is enqueued. */
 typedef struct {
   int64_t offset, stride, ld;
   int32_t rows, cols, count, reserved;   /* reserved: 0 */

@@ -1068,9 +1068,7 @@ template <int NT, int NG> int launch_small(hipStream_t s, const OrthoPlan& p, co
 }
 
 template <int TILE, int MODE> int launch_tiles(hipStream_t s, const OrthoPlan& p, const Target& t, char* ws, int step) {
-  const OrthoProduct& all = p.product[MODE < APPLY ? MODE : APPLY];
-  int longest = 0;
-  for (int x = 0; x < 8; ++x) longest = all.first[x + 1] - all.first[x] > longest ? all.first[x + 1] - all.first[x] : longest;
+  const int longest = p.product[MODE < APPLY ? MODE : APPLY].longest();
   auto launch = [&](auto muon, OncePerDevice& once) -> int {
     constexpr bool MUON = decltype(muon)::value;
     const int lds = 2 * Tile<TILE>::STAGE;

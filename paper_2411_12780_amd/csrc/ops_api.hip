@@ -11,7 +11,7 @@ namespace ppll {
 
 namespace {
 constexpr int64_t FAR = (int64_t)1 << 40;          // offsets and strides below it: no sum of them passes 64 bits
-constexpr int64_t MOST_ITEMS = 0x7fffffff;         // workgroups of a launch
+constexpr int64_t MOST_ITEMS = (1 << 24) - 1;      // workgroups of 256 threads that a launch takes: under 2^32 threads
 
 int64_t extent(const ppll_matrix_group& g) { return (int64_t)(g.rows - 1) * g.ld + g.cols; }
 // A group as matrices one behind the other; side by side they are one as wide as all of them.
@@ -163,9 +163,12 @@ int ortho_plan(const ppll_matrix_group* groups, int32_t n_groups, OrthoPlan* pla
     o.x[1] = take(o.count * 2 * 2 * o.plane_x());
     o.a = take(o.count * 2 * 2 * o.plane_a());
     o.b = take(o.count * 2 * 2 * o.plane_a());
-    if (pieces > MOST_ITEMS || 8 * squares > MOST_ITEMS) { set_error("too many matrices for one call"); return PPLL_ERR_SHAPE; }
+    if (pieces > MOST_ITEMS || squares > MOST_ITEMS) { set_error("too many matrices for one call"); return PPLL_ERR_SHAPE; }
   }
-  for (int phase = 0; phase < 3; ++phase) plan_product(plan, phase);
+  for (int phase = 0; phase < 3; ++phase) {
+    plan_product(plan, phase);
+    if (8 * (int64_t)plan->product[phase].longest() > MOST_ITEMS) { set_error("too many matrices for one call"); return PPLL_ERR_SHAPE; }
+  }
   plan->sums = take(plan->sums);
   plan->arrived = take(plan->counters * (int64_t)sizeof(int32_t));
   count_items(*plan, &plan->pieces, [](const OrthoGroup& g) { return g.small ? 0 : g.pieces(); });

@@ -65,6 +65,11 @@ struct OrthoProduct {
     int32_t tile_of;                   // the group's first tile among those in pieces
     int64_t sums_of;                   // and its first sums, in bytes
   } group[ORTHO_GROUPS];
+  int longest() const {                // run of an XCD: a launch has eight times as many workgroups
+    int most = 0;
+    for (int x = 0; x < 8; ++x) most = first[x + 1] - first[x] > most ? first[x + 1] - first[x] : most;
+    return most;
+  }
 };
 struct OrthoPlan {
   OrthoGroup g[ORTHO_GROUPS];          // longest rows first: their tiles take the longest

@@ -29,3 +29,20 @@ def test_a_block_whose_matrices_are_too_many_for_one_call_is_refused():
         with pytest.raises(P.PpllError) as e:
             call(cfg)
         assert e.value.status == CONFIG and "too many matrices" in P.ppll_last_error()
+
+
+def test_calls_that_no_launch_can_hold_are_refused_before_anything_is_enqueued():
+    # a matrix of 8192 x 1 has 512 pieces of 16 rows, a workgroup of 256 threads each: 2^32 threads from 32768 matrices on
+    size, columns = P.ppll_orthogonalize_workspace_bytes, lambda n, at=0: P.matrix_group(at, 8192, 1, count=n)
+    assert size([columns(32767)]) > 1 << 36
+    small = P.matrix_group(0, 8, 8)
+    for groups in ([columns(32768)], [columns(65535)], [columns(20000), columns(20000, 1 << 30)], [small, columns(32768, 64)],
+                   [P.matrix_group(0, 2048, 2048, count=16384)]):
+        with pytest.raises(P.PpllError) as e:
+            size(groups)
+        assert e.value.status == SHAPE
+        for call in (lambda: P.ppll_orthogonalize(groups, P.FP32, 5, 16, 32, 48, 1 << 60),
+                     lambda: P.ppll_muon_step(groups, 5, 16, 32, 48, None, 0.1, 0.9, True, 0.0, 64, 1 << 60)):
+            with pytest.raises(P.PpllError) as e:
+                call()
+            assert e.value.status == SHAPE
