@@ -14,22 +14,35 @@ constexpr int64_t FAR = (int64_t)1 << 40;          // offsets and strides below 
 constexpr int64_t MOST_ITEMS = (1 << 24) - 1;      // workgroups of 256 threads that a launch takes: under 2^32 threads
 
 int64_t extent(const ppll_matrix_group& g) { return (int64_t)(g.rows - 1) * g.ld + g.cols; }
-// A group as matrices one behind the other; side by side they are one as wide as all of them.
-struct Run { int64_t offset, stride, ld; int64_t rows, cols, count; };
+// A group as matrices one behind the other, each of `parts` blocks of columns `step` apart: matrices side by side are the blocks of one.
+struct Run { int64_t offset, stride, ld, rows, count, cols, step, parts; };
 Run run_of(const ppll_matrix_group& g) {
-  if (g.count > 1 && g.stride < extent(g)) return {g.offset, 0, g.ld, g.rows, (g.count - 1) * g.stride + g.cols, 1};
-  return {g.offset, g.stride, g.ld, g.rows, g.cols, g.count};
+  if (g.count > 1 && g.stride < extent(g)) return {g.offset, 0, g.ld, g.rows, 1, g.cols, g.stride, g.count};
+  return {g.offset, g.stride, g.ld, g.rows, g.count, g.cols, 0, 1};
+}
+// Whether one of a run's blocks of columns meets columns lo .. hi - 1
+bool meets(const Run& a, int64_t lo, int64_t hi) {
+  const int64_t i = a.parts > 1 && lo >= a.cols ? (lo - a.cols) / a.step + 1 : 0;      // the first block that ends behind lo
+  return i < a.parts && i * a.step < hi && i * a.step + a.cols > lo;
 }
 // Whether matrices of two runs may share an element: their extents meet, and they are not different columns of rows of one length.
 bool overlap(const Run& a, const Run& b) {
-  const int64_t ea = (a.rows - 1) * a.ld + a.cols, eb = (b.rows - 1) * b.ld + b.cols;
+  auto length = [](const Run& r) { return (r.rows - 1) * r.ld + (r.parts - 1) * r.step + r.cols; };
+  const int64_t ea = length(a), eb = length(b), apart = b.offset - a.offset;
+  auto share = [&](int64_t from) {         // matrices that begin `from` elements from one another
+    if (from >= ea || -from >= eb) return false;
+    if (a.ld != b.ld) return true;
+    const int64_t d = (from % a.ld + a.ld) % a.ld;
+    for (int64_t j = 0; j < b.parts; ++j) {
+      const int64_t lo = d + j * b.step, hi = lo + b.cols;
+      if (meets(a, lo, hi) || meets(a, lo - a.ld, hi - a.ld)) return true;
+    }
+    return false;
+  };
   int64_t i = 0, j = 0;
   while (i < a.count && j < b.count) {
-    const int64_t la = a.offset + i * a.stride, lb = b.offset + j * b.stride;
-    if (la + ea > lb && lb + eb > la) {
-      const int64_t d = a.ld == b.ld ? ((lb - la) % a.ld + a.ld) % a.ld : 0;
-      if (a.ld != b.ld || d < a.cols || d + b.cols > a.ld) return true;
-    }
+    const int64_t la = i * a.stride, lb = apart + j * b.stride;
+    if (share(lb - la)) return true;
     if (la + ea < lb + eb) ++i;
     else ++j;
   }

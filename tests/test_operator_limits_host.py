@@ -1,4 +1,5 @@
 """Many layers, many matrices, and what lies at the limits of the orthogonalised updates: host arithmetic only, no call here launches."""
+import random
 import time
 
 import pytest
@@ -46,3 +47,64 @@ def test_calls_that_no_launch_can_hold_are_refused_before_anything_is_enqueued()
             with pytest.raises(P.PpllError) as e:
                 call()
             assert e.value.status == SHAPE
+
+
+def elements(g):
+    """Of a group: for each of its matrices, all side by side being one, the first element, one past the last, columns from the first."""
+    if g.count > 1 and g.stride < (g.rows - 1) * g.ld + g.cols:
+        cols = [i * g.stride + c for i in range(g.count) for c in range(g.cols)]
+        return [(g.offset, g.offset + (g.rows - 1) * g.ld + cols[-1] + 1, cols)]
+    return [(g.offset + i * g.stride, g.offset + i * g.stride + (g.rows - 1) * g.ld + g.cols, list(range(g.cols))) for i in range(g.count)]
+
+
+def by_the_rule(x, y):
+    """Extents that overlap need one ld and different columns of it."""
+    for la, ha, ca in elements(x):
+        for lb, hb, cb in elements(y):
+            if la < hb and lb < ha and (x.ld != y.ld or {c % x.ld for c in ca} & {(lb - la + c) % x.ld for c in cb}):
+                return False
+    return True
+
+
+def touched(g):
+    at = [g.offset + i * g.stride + r * g.ld + c for i in range(g.count) for r in range(g.rows) for c in range(g.cols)]
+    assert len(set(at)) == len(at)
+    return set(at)
+
+
+def test_what_is_shared_is_refused_and_what_is_not_is_taken():
+    rng = random.Random(5)
+    taken = refused = beside = 0
+    for _ in range(6000):
+        ld = rng.randint(4, 14)
+        pair = []
+        for _ in range(2):
+            rows, cols = rng.randint(1, 4), rng.randint(1, 4)
+            mine = ld if rng.random() < 0.8 else rng.randint(4, 14)
+            extent = (rows - 1) * mine + cols
+            if rng.random() < 0.5:                           # side by side
+                stride = rng.randint(cols, cols + 4)
+                count = rng.randint(1, max(1, (mine - cols) // stride + 1))
+            else:
+                stride, count = extent + rng.choice([0, 1, rng.randint(0, 60)]), rng.randint(1, 6)
+            pair.append(P.matrix_group(rng.randint(0, 90), rows, cols, ld=mine, count=count, stride=stride))
+        want = by_the_rule(*pair)
+        try:
+            P.ppll_orthogonalize_workspace_bytes(pair)
+            got = True
+        except P.PpllError:
+            got = False
+        assert got == want, [[getattr(g, f) for f, _ in g._fields_] for g in pair]
+        if got:
+            assert not touched(pair[0]) & touched(pair[1])
+            taken += 1
+            beside += any(a < d and c < b for a, b, _ in elements(pair[0]) for c, d, _ in elements(pair[1]))
+        else:
+            refused += 1
+    assert taken > 1000 and refused > 1000 and beside > 50
+
+
+def test_groups_side_by_side_that_take_turns_are_taken():
+    # query and key parts of three heads in one weight, a head's query beside its key
+    group = lambda at: P.matrix_group(at, 8, 4, ld=24, count=3, stride=8)  # noqa: E731
+    assert P.ppll_orthogonalize_workspace_bytes([group(0), group(4)]) == 0
