@@ -29,6 +29,7 @@ bool meets(const Run& a, int64_t lo, int64_t hi) {
 bool overlap(const Run& a, const Run& b) {
   auto length = [](const Run& r) { return (r.rows - 1) * r.ld + (r.parts - 1) * r.step + r.cols; };
   const int64_t ea = length(a), eb = length(b), apart = b.offset - a.offset;
+  if (apart >= (a.count - 1) * a.stride + ea || -apart >= (b.count - 1) * b.stride + eb) return false;
   auto share = [&](int64_t from) {         // matrices that begin `from` elements from one another
     if (from >= ea || -from >= eb) return false;
     if (a.ld != b.ld) return true;
@@ -39,6 +40,14 @@ bool overlap(const Run& a, const Run& b) {
     }
     return false;
   };
+  if (a.count == 1 || b.count == 1 || a.stride == b.stride) {
+    // i-th and j-th begin apart + (j - i) stride from one another: j - i from where they first meet
+    const int64_t stride = b.count > 1 ? b.stride : a.stride;
+    int64_t k = a.count > 1 || b.count > 1 ? std::max<int64_t>(1 - a.count, (-eb - apart) / stride - 1) : 0;
+    for (; k < b.count && apart + k * stride < ea; ++k)
+      if (share(apart + k * stride)) return true;
+    return false;
+  }
   int64_t i = 0, j = 0;
   while (i < a.count && j < b.count) {
     const int64_t la = i * a.stride, lb = apart + j * b.stride;

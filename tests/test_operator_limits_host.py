@@ -108,3 +108,13 @@ def test_groups_side_by_side_that_take_turns_are_taken():
     # query and key parts of three heads in one weight, a head's query beside its key
     group = lambda at: P.matrix_group(at, 8, 4, ld=24, count=3, stride=8)  # noqa: E731
     assert P.ppll_orthogonalize_workspace_bytes([group(0), group(4)]) == 0
+
+
+def test_many_matrices_are_compared_in_microseconds():
+    # groups apart, parts of weights that take turns, and small matrices within one stride of one another
+    far = [P.matrix_group((i << 33), 30, 30, count=65535, stride=901) for i in range(16)]
+    parts = [P.matrix_group(i * 40, 40, 40, ld=640, count=65535, stride=25600) for i in range(16)]
+    between = [P.matrix_group(i * 16, 4, 4, count=65535, stride=4000) for i in range(16)]
+    for groups in (far, parts, between):
+        # a walk over all matrices of each of the 120 pairs takes 24 to 120 ms
+        assert min(seconds(P.ppll_orthogonalize_workspace_bytes, groups) for _ in range(5)) < 5e-3
