@@ -21,22 +21,29 @@ typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr double NORM_EPS = 1e-7;
-// Operands are stored as hi + lo, two fp16 of a value times 2^14: 22 bits, and the products hi hi + hi lo + lo hi miss 2^-22 of a product,
-// a rounding of fp32.  The scale keeps lo above fp16's denormals: entries are 1 / sqrt(m n) in the mean, 2^-13 for the largest matrices.
-// It cannot overflow: singular values are 1.2023 at most (the polynomial's maximum on [0, 1.2023]), so entries are 1.2023 at most for X,
-// 1.446 for A, and b A + c A A has eigenvalues from -2.81 to 0: 46000 times 1, of 65504.
+// Operands are stored as hi + lo / 2048, two fp16 of a value times 2^14: 22 bits, and the products hi hi + (hi lo + lo hi) / 2048 leave lo lo out, 2^-22
+// of a product at most.  Fewer bits than fp32's 24 at the worst, and chosen because fp16 products are eight times as fast: in the mean what is stored and
+// what is left out are each off by about a rounding of fp32 (errors beside those of fp32 products: 1.4 times for one step of a random matrix, level after
+// five).  lo is kept 2^11 times as large as what it stands for, as large as hi: both are then exact down to values of 2^-28 (beside a norm of 1), and below
+// those off by 2^-50.  (With lo as it is, a row of 1e-6 beside others of 1 came out with errors of 6e-4.)  It cannot overflow: singular values are 1.2023 at most (the polynomial's maximum on [0, 1.2023]), so entries are 1.2023 at most for X,
+// 1.446 for A, and b A + c A A has eigenvalues from -2.81 to 0: 46000 times 1, of 65504; lo is 2048 times half a unit of that hi's last place, 32768.
 constexpr double SCALE = 16384;
 constexpr float UNSCALE = 1.f / 16384.f;
+constexpr float LOW = 2048.f, UNLOW = 1.f / 2048.f;
 
 // The operands are scaled to a Frobenius norm of exactly 1 at the start, and what X is smaller by, t0 = |u| / (|u| + 1e-7), enters as a
 // factor: X = t Y with t = min(1, a^k t0) in step k, so Y' = t / t' (a Y + (b t^2 Y Y' + c t^4 (Y Y')^2) Y).  Unless a matrix is as small as
 // the constant this is t = 1; one of norm 1e-20, whose X is of norm 1e-13, would be lost in fp16 otherwise.
 struct Shrink { float now, next, ratio; };
+__device__ __forceinline__ Shrink shrink_from(float t) {
+  Shrink s{t, fminf(1.f, NS_A * t), 1.f};
+  if (t > 0.f && t < 1.f) s.ratio = t / s.next;
+  return s;
+}
 __device__ __forceinline__ Shrink shrink_of(float t0, int step) {
   float t = t0;
   for (int k = 0; k < step; ++k) t = fminf(1.f, NS_A * t);
-  const float next = fminf(1.f, NS_A * t);
-  return {t, next, t0 > 0.f ? t / next : 1.f};
+  return shrink_from(t);
 }
 
 constexpr int GRAM = ORTHO_GRAM, POLY = ORTHO_POLY, APPLY = ORTHO_APPLY, LAST = ORTHO_APPLY + 1;
@@ -46,7 +53,7 @@ struct Source { const void* in; int dt; const float* g; float* m; float momentum
 // Where the result goes: out (orthogonalize), or null: the parameters
 struct Target { void* out; int dt; float* p; uint16_t* shadow; float lr, decay; };
 
-// hi and lo of n values: two values to hi in one instruction, and each lo = value - hi, rounded once, in one mixed-precision instruction that reads hi as
+// hi and lo of n values: two values to hi in one instruction, and each lo = 2048 value - 2048 hi, rounded once, in one mixed-precision instruction that reads hi as
 // it was stored.  (Left to the compiler, the arithmetic that gives a value may be folded into one of two conversions and not into the other, and at a tie
 // hi and what lo is counted from are two neighbours: one element in some 20000 was off by a whole step of hi, 2^-11 of it.)
 template <int N> struct Terms { _Float16 __attribute__((ext_vector_type(N))) hi, lo; };
@@ -57,16 +64,16 @@ template <int N> __device__ __forceinline__ Terms<N> split_all(const float* v) {
   for (int k = 0; k < N / 2; ++k) {
     uint32_t h, l;
     asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(h) : "v"(v[2 * k]), "v"(v[2 * k + 1]));
-    asm("v_fma_mixlo_f16 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(l) : "v"(h), "v"(v[2 * k]));
-    asm("v_fma_mixhi_f16 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(l) : "v"(h), "v"(v[2 * k + 1]));
+    asm("v_fma_mixlo_f16 %0, %1, %3, %2 op_sel_hi:[1,0,0]" : "=v"(l) : "v"(h), "v"(v[2 * k] * LOW), "s"(-LOW));
+    asm("v_fma_mixhi_f16 %0, %1, %3, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(l) : "v"(h), "v"(v[2 * k + 1] * LOW), "s"(-LOW));
     hi[k] = h; lo[k] = l;
   }
   return {__builtin_bit_cast(decltype(Terms<N>::hi), hi), __builtin_bit_cast(decltype(Terms<N>::lo), lo)};
 }
 // v[0] and v[1] plus `by` times the two values whose terms the words hold: two mixed-precision instructions a value
 __device__ __forceinline__ void add_two(float* v, uint32_t hi, uint32_t lo, float by) {
-  asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel_hi:[1,0,0]" : "+v"(v[0]) : "v"(lo), "v"(by));
-  asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(v[1]) : "v"(lo), "v"(by));
+  asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel_hi:[1,0,0]" : "+v"(v[0]) : "v"(lo), "v"(by * UNLOW));
+  asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(v[1]) : "v"(lo), "v"(by * UNLOW));
   asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel_hi:[1,0,0]" : "+v"(v[0]) : "v"(hi), "v"(by));
   asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "+v"(v[1]) : "v"(hi), "v"(by));
 }
@@ -535,7 +542,7 @@ template <int TILE, int MODE, bool MUON> __global__ __launch_bounds__(256, 2) vo
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) hh[j][i] += xx[j][i];
+    for (int i = 0; i < 2; ++i) hh[j][i] += xx[j][i] * UNLOW;
 
   // ---- epilogue: through LDS, so that a wave reads and writes whole 16-byte pieces of whole cache lines.  A wave finishes PASSES times ROWS rows
   // of 64 columns: lane l pieces of eight at columns 8 (l % 8) of rows l / 8 + 8 n.  What lies past the padded size (a multiple of 64) is not stored.
@@ -827,7 +834,7 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
 #pragma unroll
   for (int w = 0; w < SMALL_WAVES; ++w) sum += sums[w];
   const double norm = sqrt(sum), inv = norm > 0 ? SCALE / norm : norm;
-  const float t0 = (float)(norm / (norm + NORM_EPS));
+  Shrink shrink = shrink_from(__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint((float)(norm / (norm + NORM_EPS))))));
   // (a norm whose reciprocal fp32 cannot hold takes the products in 64 bits)
   const float inv32 = (float)inv;
   const bool far = !(inv32 > 1e-30f && inv32 < 1e30f);
@@ -875,7 +882,7 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
       if (NT > 2)
         for (k += 32; k < to; k += 32) piece(k, two, std::false_type());
     }
-    return hh + xx;
+    return hh + xx * UNLOW;
   };
   auto rows_product = [&](const _Float16* P, int ld, int plane, int i0, int j0, int from, int to) {
     const _Float16 *pr = P + (i0 + row) * ld + kpart, *qr = P + (j0 + row) * ld + kpart;
@@ -948,7 +955,6 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
     return first + n * SMALL_WAVES;
   };
   for (int k = 0; k < steps; ++k) {
-    const Shrink shrink = shrink_of(t0, k);
     const float t2 = shrink.now * shrink.now;
     // X X'
     if (room.shares == 1) {
@@ -1010,6 +1016,7 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
       held[n] = add_old(X + (i0 + row) * lx + j0 + col, px, columns_product(X, i0, j0), NS_A * shrink.ratio, UNSCALE * shrink.ratio);
     }
     if (k + 1 == steps) break;
+    shrink = shrink_from(shrink.next);
     if (!room.two_x) __syncthreads();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -1023,7 +1030,7 @@ template <int NT, int NG, bool MUON> __global__ __launch_bounds__(SMALL_THREADS)
   }
   // ---- the result, from LDS in the same pieces
   float* R = (float*)XN;                               // rows of lx floats, as large as the planes
-  const float scale = UNSCALE * shrink_of(t0, steps - 1).next * (MUON ? 0.2f * t.lr * sqrtf((float)g.n) : 1.f);
+  const float scale = UNSCALE * shrink.next * (MUON ? 0.2f * t.lr * sqrtf((float)g.n) : 1.f);
   if (!room.two_x) __syncthreads();
 #pragma unroll
   for (int n = 0; n < NT; ++n) {

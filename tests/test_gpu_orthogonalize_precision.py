@@ -14,6 +14,7 @@ from paper_2411_12780_amd import binding as P
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 FP32 = 3
+FLOOR = 2.0 ** -50          # of a matrix of norm 1: half the last place of a low term
 
 
 def stream():
@@ -92,6 +93,28 @@ def test_errors_of_a_muon_step_are_those_of_fp32(rows, cols, count, nesterov):
         fp32 = iterate(start_of(update(m[k], g[k])).float(), 5).double() * scale
         worst = [max(worst[0], off(p[k], want)), max(worst[1], off(fp32, want))]
     assert worst[0] <= FP32 * worst[1], worst
+
+
+@pytest.mark.parametrize("across", [False, True])
+@pytest.mark.parametrize("rows,cols", [(64, 64), (96, 120), (256, 1024), (700, 300), (384, 384)])
+def test_rows_and_columns_far_under_the_others_keep_their_digits(rows, cols, across):
+    # every product is linear in a row (a column) of X, so fp32 arithmetic leaves a small one the digits that it leaves a large one.  A row of size s beside
+    # others of 1 has elements of s / sqrt(rows cols), and each is stored to FLOOR; a step makes it 3.4445 times as large, so what the first ones lost
+    # counts most: 1 + 1 / 3.4445 + .. = 1.41 times it, three times for the three products
+    rng = np.random.default_rng([rows, cols, 2])
+    small = {1e-2: range(4), 1e-4: range(4, 8), 1e-6: range(8, 12)}
+    values = rng.standard_normal((rows, cols))
+    for size, lines in small.items():
+        for k in lines:
+            (values.T if across else values)[k] *= size
+    x = torch.from_numpy(values.astype(np.float32)).to(DEV)
+    got = call([P.matrix_group(0, rows, cols)], x)
+    want, fp32 = both(x, 5)
+    for size, lines in small.items():
+        lines = list(lines)
+        part = (lambda t: t[:, lines].t()) if across else (lambda t: t[lines])  # noqa: E731
+        own, usual = off(part(got), part(want), 1), off(part(fp32), part(want), 1)
+        assert own <= FP32 * usual + 3 * 1.41 * FLOOR * (rows * cols) ** 0.5 / size, (size, own, usual)
 
 
 @pytest.mark.parametrize("steps", [1, 3, 5])

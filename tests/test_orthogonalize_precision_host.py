@@ -21,7 +21,7 @@ def product(p, q, low, left_out):
     return (p[0] @ q[0].T + cross / np.float32(low)) / np.float32(2 ** 28)
 
 
-def emulated(u, steps=5, low=1, left_out=0, low_terms=True):
+def emulated(u, steps=5, low=2048, left_out=0, low_terms=True):
     a, b, c = (np.float32(v) for v in O.NEWTON_SCHULZ)
     terms = lambda v: split(v, low) if low_terms else (split(v, low)[0], np.zeros(v.shape, np.float32))  # noqa: E731
     value = lambda t: (t[0] + t[1] / np.float32(low)) / np.float32(16384)  # noqa: E731
@@ -58,3 +58,15 @@ def test_a_missing_term_is_seen(rows, cols, steps):
     assert off(emulated(u, steps, left_out=1), want) > 2 * limit
     assert off(emulated(u, steps, left_out=2), want) > 2 * limit
     assert off(emulated(u, steps, low_terms=False), want) > 2 * limit
+
+
+def test_low_terms_at_the_scale_of_the_high_ones_lose_small_rows():
+    u = np.random.default_rng(3).standard_normal((96, 400))
+    u[:4] *= 1e-4
+    u[4:8] *= 1e-6
+    u = u.astype(np.float32).astype(np.float64)
+    want, fp32 = iterate(u, np.float64), iterate(u, np.float32)
+    for rows, size in ((slice(0, 4), 1e-4), (slice(4, 8), 1e-6)):
+        limit = ALLOWED * off(fp32[rows], want[rows], 1) + 3 * 1.41 * 2.0 ** -50 * (96 * 400) ** 0.5 / size
+        assert off(emulated(u)[rows], want[rows], 1) <= limit
+        assert off(emulated(u, low=1)[rows], want[rows], 1) > 2 * limit
