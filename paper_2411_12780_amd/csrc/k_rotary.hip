@@ -17,16 +17,20 @@ struct RotaryArgs {
 };
 
 // cos and sin of every pair of the rows from row0 on, once for all heads: the angle in turns and its nearest whole number in 64 bits (a
-// position of 2^31 leaves 22 bits of a turn's fraction in them, none in 32), the functions of what is left in 32.
+// position of 2^31 leaves 22 bits of a turn's fraction in them, none in 32), the functions of what is left in 32, and what the rounding of their
+// argument left out, up to 2^-25 half turns, by their derivatives: without it cos and sin are off by 3.3e-8 in the mean, over twice what rounding them
+// leaves.
 __device__ __forceinline__ void fill_table(const RotaryArgs& a, int row0, int rows, float2* table) {
   const int P = a.p.pairs;
   for (int e = threadIdx.x; e < rows * P; e += 256) {
     const int r = e / P, p = e - r * P, token = (row0 + r) % a.p.tokens;
     const int axis = p < a.p.end[0] ? 0 : p < a.p.end[1] ? 1 : 2;
     const double turns = a.p.turns[p] * a.positions[(int64_t)token * a.p.axes + axis];
+    const double half_turns = 2.0 * (turns - rint(turns));
+    const float near = (float)half_turns, rest = (float)(half_turns - near) * 3.14159265f;
     float s, c;
-    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-    table[e] = make_float2(c, s);
+    sincospif(near, &s, &c);
+    table[e] = make_float2(fmaf(-s, rest, c), fmaf(c, rest, s));
   }
 }
 
