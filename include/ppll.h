@@ -313,8 +313,10 @@ typedef struct {
 
 /* The rotation: `axes` axes of positions (1..3: a sequence; height, width; time, height, width), pairs[a] pairs of each head turn with axis a,
  * sum(pairs) <= head_dim / 2 (0: the norm alone).  Pair p of P = sum(pairs) is elements (p, P + p) of the head, or with `neighbours` (2p, 2p + 1);
- * elements from 2 P on do not turn.  Pair i of the n that belong to axis a turns by positions[token][a] * base^(-i / n) radians (the angle
- * is reduced in 64 bits, so far positions lose nothing).  Row r holds token r % tokens: a batch of sequences with the same positions, or
+ * elements from 2 P on do not turn.  Pair i of the n that belong to axis a turns by positions[token][a] * base^(-i / n) radians.  The angle
+ * is taken and reduced in 64 bits, off by (4 + 3 |log2 base^(-i / n)|) 2^-53 of itself at most: with base >= 1 under 1e-6 radians at any position and
+ * under a rounding of fp32 up to position 2^27; a base below 1 makes angles larger than positions, and the farthest lose their digits (at
+ * position 2^31: 6e-4 radians with base 0.01, all of them with 1e-6).  Row r holds token r % tokens: a batch of sequences with the same positions, or
  * with tokens = rows one row of positions each. */
 typedef struct {
   uint32_t struct_size;   /* = sizeof(ppll_rotary_config)                        */

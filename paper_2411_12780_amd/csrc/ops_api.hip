@@ -216,7 +216,7 @@ int rotary_plan(const ppll_rotary_config* c, RotaryPlan* p) {
   p->rows = c->rows; p->tokens = c->tokens; p->heads[0] = c->q_heads; p->heads[1] = c->k_heads;
   p->hd = c->head_dim; p->axes = c->axes; p->neighbours = c->neighbours != 0; p->eps = c->norm_eps;
   // (exp2 takes a third of pow's time, of the 0.7 us of a call with 32 pairs; the exponent's rounding is a relative 1e-16 for each octave,
-  // which a pair that turns less feels less)
+  // which a pair that turns less feels less; with a base below 1 pairs turn more, and far positions feel it)
   const double octaves = std::log2((double)c->base);
   int pairs = 0;
   for (int a = 0; a < 3; ++a) {

@@ -31,3 +31,16 @@ def test_cos_and_sin_are_off_by_their_own_roundings(pairs):
     cos, sin, angle = turned(rng.integers(-(1 << 20), 1 << 20, 30000), pairs, 3.0)
     for got, want in ((cos, np.cos(angle)), (sin, np.sin(angle))):
         assert np.sqrt(np.mean((got - want) ** 2)) <= 2.9e-8
+
+
+@pytest.mark.parametrize("base", [0.01, 0.5, 1.0, 100.0])
+@pytest.mark.parametrize("pairs", [16, 17])
+def test_far_positions_of_every_base(base, pairs):
+    # roundings of 2^-53 on the way to a turn, relative: exponent 3 of its |log2|, 2 to 4 of the power, the quotient by 2 pi and the product; in the oracle here
+    # one of the exponent's and 2 more.  Those of cos and sin themselves are 2^-23 at most.
+    positions = np.random.default_rng(2).integers(-(1 << 31), 1 << 31, 4000)
+    cos, sin, angle = turned(positions, pairs, base)
+    octaves = abs(np.log2(np.float64(np.float32(base)))) * np.arange(pairs) / pairs
+    limit = np.abs(angle) * (6 + 4 * octaves) * 2.0 ** -53 + 2.0 ** -23
+    for got, want in ((cos, np.cos(angle)), (sin, np.sin(angle))):
+        assert (np.abs(got - want) <= limit).all()
