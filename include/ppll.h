@@ -339,9 +339,10 @@ int ppll_qk_rotary_forward(const ppll_rotary_config* cfg, const int32_t* positio
                            const ppll_queries_keys* in, const ppll_queries_keys* out, const ppll_queries_keys* keep, void* hip_stream);
 
 /* Backward: from dy the gradient dx at the forward's input x, and with scales d_q_scale_dev / d_k_scale_dev, fp32 [head_dim], overwritten
- * (zeros where rows = 0).  x: the forward's input, needed with scales only (else null).  dx may be dy.  Without scales no workspace is
- * needed (null, 0), else ppll_qk_rotary_workspace_bytes(cfg) bytes that nothing else uses until the stream has passed the call.  The sums
- * over rows and heads run in a fixed order. */
+ * (zeros where rows = 0); they are two buffers, also where one scale serves both sides (its gradient is their sum).  x: the forward's input,
+ * needed with scales only (else null).  dx may be dy.  Without scales no workspace is needed (null, 0), else
+ * ppll_qk_rotary_workspace_bytes(cfg) bytes that nothing else uses until the stream has passed the call.  The sums over rows and heads run in
+ * a fixed order. */
 int ppll_qk_rotary_workspace_bytes(const ppll_rotary_config* cfg, size_t* bytes);
 int ppll_qk_rotary_backward(const ppll_rotary_config* cfg, const int32_t* positions_dev, const float* q_scale_dev, const float* k_scale_dev,
                             const ppll_queries_keys* x, const ppll_queries_keys* dy, const ppll_queries_keys* dx, float* d_q_scale_dev,

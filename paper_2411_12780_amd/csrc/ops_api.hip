@@ -384,6 +384,10 @@ int ppll_qk_rotary_backward(const ppll_rotary_config* cfg, const int32_t* positi
       PPLL_TRY(check_workspace(workspace_dev, workspace_bytes, rotary_partial_floats(p.hd) * sizeof(float)));
     }
   }
+  if (norm && p.heads[0] && p.heads[1]) {
+    const uintptr_t dq = (uintptr_t)d_q_scale_dev, dk = (uintptr_t)d_k_scale_dev, bytes = p.hd * sizeof(float);
+    if (dq < dk + bytes && dk < dq + bytes) { set_error("the gradients of the two scales share memory"); return PPLL_ERR_SHAPE; }
+  }
   int rows = 0;
   if (p.rows)
     PPLL_TRY(launch_rotary_bwd(s, p, dt, positions_dev, side_of(p, 0, norm ? x : nullptr, dy, dx, nullptr, norm ? q_scale_dev : nullptr),

@@ -118,3 +118,13 @@ def test_many_matrices_are_compared_in_microseconds():
     for groups in (far, parts, between):
         # a walk over all matrices of each of the 120 pairs takes 24 to 120 ms
         assert min(seconds(P.ppll_orthogonalize_workspace_bytes, groups) for _ in range(5)) < 5e-3
+
+
+@pytest.mark.parametrize("dk", [4096, 4096 + 28, 4096 - 28])
+def test_gradients_of_the_two_scales_that_share_memory_are_refused(dk):
+    for rows in (8, 0):
+        cfg = P.rotary_config(P.FP32, rows, 4, 2, 1, 8, [2, 2], 100.0)
+        qk = P.QueriesKeys(16, 32, 16, 8)
+        with pytest.raises(P.PpllError) as e:
+            P.ppll_qk_rotary_backward(cfg, 16, 16, 16, qk, qk, qk, 4096, dk, 64, P.ppll_qk_rotary_workspace_bytes(cfg))
+        assert e.value.status == SHAPE and "scales" in P.ppll_last_error()
