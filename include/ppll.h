@@ -280,11 +280,13 @@ typedef struct {
 /* Newton-Schulz orthogonalisation of every matrix G of up to 16 groups:
  *   X = G / (|G|_F + 1e-7);  `steps` times  A = X X^T,  X = a X + (b A + c A A) X,  (a, b, c) = (3.4445, -4.7750, 2.0315)
  * (X^T X on the other side where rows > cols, which is the same), the published polynomial of the Muon optimizer: after 5 steps the
- * singular values that are not tiny beside the largest lie around 1 (0.7 to 1.2).  in_dev and out_dev are blobs of `precision`'s type (PPLL_FP32, PPLL_BF16)
- * with the groups' layout; out_dev may be in_dev; elements of out_dev outside the matrices are left as they are.  steps: 1..16.
+ * singular values that are not tiny beside the largest lie around 1 (0.7 to 1.2).  in_dev and out_dev are blobs of `precision`'s type
+ * (PPLL_FP32, PPLL_BF16) with the groups' layout; out_dev may be in_dev; elements of out_dev outside the matrices are left as they are.
+ * steps: 1..16.
  * Precision, whichever the type: norms in 64 bits, sums in fp32, operands of the products as two fp16 terms, which hold 22 bits of an element
  * that is at least 2^-28 of its matrix's norm and are off by 2^-50 of the norm at most under that.  Errors of the result are like those of
- * fp32 products, also those of rows and columns that are 1e-6 of the others (of 1e-8: 3e-5 of themselves).  A matrix of zeros gives zeros; one with a NaN or an infinity gives NaN in all its elements and leaves the others alone.
+ * fp32 products, also those of rows and columns that are 1e-6 of the others (of 1e-8: 3e-5 of themselves).
+ * A matrix of zeros gives zeros; one with a NaN or an infinity gives NaN in all its elements and leaves the others alone.
  * Calls with the same groups give the same bits; with other groups beside it a matrix may be summed up in another order.
  * Workspace: ppll_orthogonalize_workspace_bytes(the same groups) bytes, used by nothing else until the stream has passed the call; its
  * contents need not survive between calls, and calls that may run at the same time need one each.  Asynchronous on hip_stream; may be

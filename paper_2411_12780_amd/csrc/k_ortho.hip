@@ -21,12 +21,14 @@ typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr double NORM_EPS = 1e-7;
-// Operands are stored as hi + lo / 2048, two fp16 of a value times 2^14: 22 bits, and the products hi hi + (hi lo + lo hi) / 2048 leave lo lo out, 2^-22
-// of a product at most.  Fewer bits than fp32's 24 at the worst, and chosen because fp16 products are eight times as fast: in the mean what is stored and
-// what is left out are each off by about a rounding of fp32 (errors beside those of fp32 products: 1.4 times for one step of a random matrix, level after
-// five).  lo is kept 2^11 times as large as what it stands for, as large as hi: both are then exact down to values of 2^-28 (beside a norm of 1), and below
-// those off by 2^-50.  (With lo as it is, a row of 1e-6 beside others of 1 came out with errors of 6e-4.)  It cannot overflow: singular values are 1.2023 at most (the polynomial's maximum on [0, 1.2023]), so entries are 1.2023 at most for X,
-// 1.446 for A, and b A + c A A has eigenvalues from -2.81 to 0: 46000 times 1, of 65504; lo is 2048 times half a unit of that hi's last place, 32768.
+// Operands are stored as hi + lo / 2048, two fp16 of a value times 2^14: 22 bits, and the products hi hi + (hi lo + lo hi) / 2048 leave lo lo out,
+// 2^-22 of a product at most.  Fewer bits than fp32's 24 at the worst, chosen because three fp16 products take 40 % of an fp32 one's time (1160 and 154
+// TFLOP/s in large library products): in the mean what is stored and what is left out are each off by about a rounding of fp32 (errors beside those of
+// fp32 products: 1.4 times for one step of a random matrix, level after five).  lo is kept 2^11 times as large as what it stands for, about as large as
+// hi, so a value beside a norm of 1 has its 22 bits down to 2^-28 and is off by 2^-50 under that.  (With lo as it is, a row of 1e-6 beside others of 1
+// came out with errors of 6e-4 of itself, now 4e-7.)  Neither can overflow: singular values are 1.2023 at most (the polynomial's maximum on [0, 1.2023]),
+// so entries are 1.2023 at most for X, 1.446 for A, and b A + c A A has eigenvalues from -2.81 to 0: 46000 times 1, of 65504; lo is 2048 times half a unit
+// of that hi's last place, 32768.
 constexpr double SCALE = 16384;
 constexpr float UNSCALE = 1.f / 16384.f;
 constexpr float LOW = 2048.f, UNLOW = 1.f / 2048.f;
@@ -53,9 +55,9 @@ struct Source { const void* in; int dt; const float* g; float* m; float momentum
 // Where the result goes: out (orthogonalize), or null: the parameters
 struct Target { void* out; int dt; float* p; uint16_t* shadow; float lr, decay; };
 
-// hi and lo of n values: two values to hi in one instruction, and each lo = 2048 value - 2048 hi, rounded once, in one mixed-precision instruction that reads hi as
-// it was stored.  (Left to the compiler, the arithmetic that gives a value may be folded into one of two conversions and not into the other, and at a tie
-// hi and what lo is counted from are two neighbours: one element in some 20000 was off by a whole step of hi, 2^-11 of it.)
+// hi and lo of n values: two values to hi in one instruction, and each lo = 2048 value - 2048 hi, rounded once, in one mixed-precision instruction that
+// reads hi as it was stored.  (Left to the compiler, the arithmetic that gives a value may be folded into one of two conversions and not into the other,
+// and at a tie hi and what lo is counted from are two neighbours: one element in some 20000 was off by a whole step of hi, 2^-11 of it.)
 template <int N> struct Terms { _Float16 __attribute__((ext_vector_type(N))) hi, lo; };
 template <int N> __device__ __forceinline__ Terms<N> split_all(const float* v) {
   typedef __attribute__((ext_vector_type(N / 2))) uint32_t words;
@@ -325,8 +327,8 @@ struct Planes { u32x4 p[2], pl[2], q[2], ql[2]; };           // fragments: hi an
                [b1] "v"(f.ql[1])
 #define NS_CROSS NS_MMA("x00", "b0", "p0") NS_MMA("x01", "b0", "p1") NS_MMA("x10", "b1", "p0") NS_MMA("x11", "b1", "p1") \
                  NS_MMA("x00", "q0", "a0") NS_MMA("x01", "q0", "a1") NS_MMA("x10", "q1", "a0") NS_MMA("x11", "q1", "a1")
-// The 12 products of the fragments at hand (into hh: hi hi, into xx the cross terms: small terms summed apart keep their digits, error of
-// 1536 x 6144 1.8e-6 instead of 3.2e-6), and under them the reads of the next ones, at rp and rq, which have arrived when the block ends.  One
+// The 12 products of the fragments at hand (into hh: hi hi, into xx the cross terms, 2048 times as large; summed apart they keep their
+// digits as well, error of 1536 x 6144 1.8e-6 instead of 3.2e-6), and under them the reads of the next ones, at rp and rq, which have arrived when the block ends.  One
 // assembly block, as in gemm_pipe.h: the compiler would wait for all copies into LDS before a read that it knows of.
 template <int TILE, bool TR>
 __device__ __forceinline__ void k_step(f32x16 (&hh)[2][2], f32x16 (&xx)[2][2], const Planes& f, Planes& n, int rp, int rq) {

@@ -16,8 +16,8 @@ struct RotaryArgs {
   int lanes;               // of a head, in rotary_kernel: a power of two
 };
 
-// cos and sin of every pair of the rows from row0 on, once for all heads: the angle in turns and its nearest whole number in 64 bits (with a
-// base from 1 on, position 2^31 leaves 22 bits of a turn's fraction in them, none in 32), the functions of what is left in 32, and what the rounding of their
+// cos and sin of every pair of the rows from row0 on, once for all heads: the angle in turns and its nearest whole number in 64 bits (with a base from
+// 1 on, position 2^31 leaves 22 bits of a turn's fraction in them, none in 32), the functions of what is left in 32, and what the rounding of their
 // argument left out, up to 2^-25 half turns, by their derivatives: without it cos and sin are off by 3.3e-8 in the mean, over twice what rounding them
 // leaves.
 __device__ __forceinline__ void fill_table(const RotaryArgs& a, int row0, int rows, float2* table) {
@@ -34,8 +34,8 @@ __device__ __forceinline__ void fill_table(const RotaryArgs& a, int row0, int ro
   }
 }
 
-// Any head width, any alignment: a wave a head, element by element.  What the kernel below does not take: heads that turn in part, widths and
-// strides with less in common than 8 bytes.
+// Any head width, any alignment: a wave a head, element by element.  What the kernel below does not take: heads that turn in part or not at all (the
+// norm alone), widths and strides with less in common than 8 bytes.
 template <bool BWD> __global__ __launch_bounds__(256) void rotary_plain_kernel(RotaryArgs a, int dt) {
   extern __shared__ float2 table[];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, P = a.p.pairs, hd = a.p.hd;
@@ -145,7 +145,9 @@ __device__ __forceinline__ float head_sum(float v, int lanes) {
 // rounded up to a power of two; queries and keys in workgroups of their own (blockIdx.y), which leaves registers for the sums of one side
 // and the next head's elements on their way.  Bound by memory: each element is read and written once, cos and sin come from LDS.  664 MB of a
 // clip's queries and keys (64800 rows, 16 and 4 heads of 128, bf16) in 127 us, 5.2 TB/s, a copy's rate; the gradients of 25216 rows with 12 + 12
-// heads of 64 and the norm, 232 MB, in 53 us, 4.4 TB/s.  Small calls by the launch and the table: 8320 rows with 6 + 6 heads 10.8 us forward.
+// heads of 64 and the norm, 232 MB, in 53 us, 4.4 TB/s.  Small calls by the launch and the table, those of an ordinary layer by registers: 8320
+// rows with 6 + 6 heads of 64 and the norm 10.9 us forward and 18 backward, where memory would allow 5.0 and 7.4.  Forward takes 98 registers, so four
+// workgroups to a unit and 2080 in 2.03 rounds; backward takes all 128 of four waves and keeps five more in scratch memory.
 template <class T, int V, bool NEXT, bool NORM, bool BWD> __global__ __launch_bounds__(256, 4) void rotary_kernel(RotaryArgs a) {
   extern __shared__ float2 table[];
   const int side = a.p.heads[0] ? blockIdx.y : 1;
@@ -258,9 +260,10 @@ __global__ __launch_bounds__(1024) void rotary_scale_kernel(const float* partial
   if (grp == 0 && e < hd) out[e] = red[0][col];
 }
 
-// Rows that a workgroup takes at a time.  Forward: enough for each thread to have two or three heads, whose reads then overlap, unless that
-// leaves the 256 units fewer than four workgroups.  Backward: the partial sums hold 512 workgroups a side, which share the rows evenly; the
-// table of a turn is 32 KB at most.
+// Rows that a workgroup takes at a time.  Forward: as many as leave 2048 workgroups over both sides, eight a unit, up to 10240 elements of a side, of
+// which each thread has two or three pieces whose reads overlap.  8320 rows with 6 + 6 heads of 64 and the norm get 8 rows (48 heads for 64 groups of
+// lanes, so none has a second one): 10.9 us; with 16 rows, four workgroups a unit, 11.0; with 4 rows 14.1.  Backward: the partial sums hold 512
+// workgroups a side, which share the rows evenly, also where there are no scales; the table of a turn is 32 KB at most.
 int rows_wg(const RotaryPlan& p, bool bwd) {
   const int most = p.pairs > 64 ? 32 : 64;
   if (bwd) {
