@@ -145,9 +145,9 @@ __device__ __forceinline__ float head_sum(float v, int lanes) {
 // rounded up to a power of two; queries and keys in workgroups of their own (blockIdx.y), which leaves registers for the sums of one side
 // and the next head's elements on their way.  Bound by memory: each element is read and written once, cos and sin come from LDS.  664 MB of a
 // clip's queries and keys (64800 rows, 16 and 4 heads of 128, bf16) in 127 us, 5.2 TB/s, a copy's rate; the gradients of 25216 rows with 12 + 12
-// heads of 64 and the norm, 232 MB, in 53 us, 4.4 TB/s.  Small calls by the launch and the table, those of an ordinary layer by registers: 8320
-// rows with 6 + 6 heads of 64 and the norm 10.9 us forward and 18 backward, where memory would allow 5.0 and 7.4.  Forward takes 98 registers, so four
-// workgroups to a unit and 2080 in 2.03 rounds; backward takes all 128 of four waves and keeps five more in scratch memory.
+// heads of 64 and the norm, 232 MB, in 49 to 53 us, 4.4 to 4.8 TB/s.  Small calls by the launch and the table, those of an ordinary layer by registers:
+// 8320 rows with 6 + 6 heads of 64 and the norm 10.9 us forward and 18 backward, where memory would allow 5.0 and 7.4.  Forward takes 98 registers, so
+// four workgroups to a unit and 2080 in 2.03 rounds; backward takes all 128 of four waves and keeps five more in scratch memory.
 template <class T, int V, bool NEXT, bool NORM, bool BWD> __global__ __launch_bounds__(256, 4) void rotary_kernel(RotaryArgs a) {
   extern __shared__ float2 table[];
   const int side = a.p.heads[0] ? blockIdx.y : 1;
