@@ -34,9 +34,11 @@ bool overlap(const Run& a, const Run& b) {
     if (from >= ea || -from >= eb) return false;
     if (a.ld != b.ld) return true;
     const int64_t d = (from % a.ld + a.ld) % a.ld;
-    for (int64_t j = 0; j < b.parts; ++j) {
-      const int64_t lo = d + j * b.step, hi = lo + b.cols;
-      if (meets(a, lo, hi) || meets(a, lo - a.ld, hi - a.ld)) return true;
+    // b's columns from d on, and a's from 0 and (the next row's) from ld on; block by block of the run that has fewer
+    const bool by_a = a.parts < b.parts;
+    for (int64_t j = 0; j < (by_a ? a.parts : b.parts); ++j) {
+      const int64_t lo = by_a ? j * a.step - d : d + j * b.step, hi = lo + (by_a ? a.cols : b.cols), row = by_a ? a.ld : -a.ld;
+      if (meets(by_a ? b : a, lo, hi) || meets(by_a ? b : a, lo + row, hi + row)) return true;
     }
     return false;
   };

@@ -128,3 +128,11 @@ def test_gradients_of_the_two_scales_that_share_memory_are_refused(dk):
         with pytest.raises(P.PpllError) as e:
             P.ppll_qk_rotary_backward(cfg, 16, 16, 16, qk, qk, qk, 4096, dk, 64, P.ppll_qk_rotary_workspace_bytes(cfg))
         assert e.value.status == SHAPE and "scales" in P.ppll_last_error()
+
+
+def test_many_matrices_between_many_columns_are_compared_as_quickly():
+    # 65535 columns side by side, and as many matrices of one element between them, whichever group comes first
+    columns = P.matrix_group(0, 2, 1, ld=1 << 20, count=65535, stride=16)
+    between = P.matrix_group(8, 1, 1, ld=1 << 20, count=65535, stride=16)
+    for groups in ([columns, between], [between, columns]):
+        assert min(seconds(P.ppll_orthogonalize_workspace_bytes, groups) for _ in range(2)) < 0.1
