@@ -297,10 +297,10 @@ def _run_plain(s):
 
 
 # ------------------------------------------------------------------ this library's calls
-def _new_rows8(P, rows, cols):
+def _new_byte_rows(P, rows, cols):
     q = torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.int8, device=DEV)
     e = torch.empty(rows, dtype=torch.int8, device=DEV)
-    return q, e, P.rows8(q, e)
+    return q, e, P.byte_rows(q, e)
 
 
 def _workspace(nbytes):
@@ -314,24 +314,24 @@ def _run_own(s):
     new = lambda *shape: torch.empty(shape, dtype=dtype, device=DEV)  # noqa: E731
     rows = lambda t: None if t is None else P.rows(t)  # noqa: E731
     if c["op"] == CHECKPOINT:
-        q, e, x8 = _new_rows8(P, c["rows"], c["cols"])
-        P.ppll_rows8_pack(precision, c["rows"], c["cols"], rows(s["x"]), x8, stream)
+        q, e, x8 = _new_byte_rows(P, c["rows"], c["cols"])
+        P.ppll_byte_rows_pack(precision, c["rows"], c["cols"], rows(s["x"]), x8, stream)
         out = new(c["rows"], c["cols"])
-        P.ppll_rows8_unpack(precision, c["rows"], c["cols"], x8, rows(out), stream)
+        P.ppll_byte_rows_unpack(precision, c["rows"], c["cols"], x8, rows(out), stream)
         return out
     if c["op"] in (FORWARD, BACKWARD):
         m, k, n = c["rows"], c["in"], c["out"]
-        cfg = P.linear8_config(precision=precision, rows=m, in_dim=k, out_dim=n, activation=P.ACT_GELU if c["gelu"] else P.ACT_NONE)
-        w8 = P.rows8(s["w"], s["w_exp"])
+        cfg = P.byte_linear_config(precision=precision, rows=m, in_dim=k, out_dim=n, activation=P.ACT_GELU if c["gelu"] else P.ACT_NONE)
+        w8 = P.byte_rows(s["w"], s["w_exp"])
         if c["op"] == FORWARD:
-            q, e, x8 = _new_rows8(P, m, k)
-            P.ppll_rows8_pack(precision, m, k, rows(s["x"]), x8, stream)
+            q, e, x8 = _new_byte_rows(P, m, k)
+            P.ppll_byte_rows_pack(precision, m, k, rows(s["x"]), x8, stream)
             y, slope = new(m, n), new(m, n) if c["gelu"] else None
-            P.ppll_linear8_forward(cfg, x8, w8, s["bias"], rows(s["residual"]), rows(y), rows(slope), stream)
+            P.ppll_byte_linear_forward(cfg, x8, w8, s["bias"], rows(s["residual"]), rows(y), rows(slope), stream)
             return {"y": y, "slope": slope} if c["gelu"] else {"y": y}
         dx, dw, db = new(m, k), torch.empty(k, n, device=DEV), torch.empty(n, device=DEV)
-        ws = _workspace(P.ppll_linear8_workspace_bytes(cfg))
-        P.ppll_linear8_backward(cfg, P.rows8(s["x"], s["x_exp"]), w8, rows(s["dy"]), rows(s["gate"]), rows(dx), dw, db, ws, ws.numel(), stream)
+        ws = _workspace(P.ppll_byte_linear_workspace_bytes(cfg))
+        P.ppll_byte_linear_backward(cfg, P.byte_rows(s["x"], s["x_exp"]), w8, rows(s["dy"]), rows(s["gate"]), rows(dx), dw, db, ws, ws.numel(), stream)
         return {"dx": dx, "dw": dw, "db": db}
     p, ch = _pixels(c), c["channels"]
     act = {"none": P.ACT_NONE, "relu": P.ACT_RELU, "silu": P.ACT_SILU, "gelu": P.ACT_GELU}[c["act"]]
@@ -340,16 +340,16 @@ def _run_own(s):
     ws = _workspace(P.ppll_group_norm_workspace_bytes(cfg))
     if c["op"] == NORM:
         y, stats = new(p, ch), torch.empty(c["images"], c["groups"], 2, device=DEV)
-        q, e, x8 = _new_rows8(P, p, ch) if c["kept"] else (None, None, None)
+        q, e, x8 = _new_byte_rows(P, p, ch) if c["kept"] else (None, None, None)
         P.ppll_group_norm_forward(cfg, rows(s["x"]), s["scale"], s["shift"], rows(s["residual"]), rows(y), stats, x8, ws, ws.numel(), stream)
         out = {"y": y, "stats": stats}
         if c["kept"]:
             out["kept"] = new(p, ch)
-            P.ppll_rows8_unpack(precision, p, ch, x8, rows(out["kept"]), stream)
+            P.ppll_byte_rows_unpack(precision, p, ch, x8, rows(out["kept"]), stream)
         return out
     dx, dres = new(p, ch), new(p, ch) if c["residual"] else None
     d_scale, d_shift = torch.empty(ch, device=DEV), torch.empty(ch, device=DEV)
-    x, x8 = (None, P.rows8(s["x"], s["x_exp"])) if c["kept"] else (rows(s["x"]), None)
+    x, x8 = (None, P.byte_rows(s["x"], s["x_exp"])) if c["kept"] else (rows(s["x"]), None)
     P.ppll_group_norm_backward(cfg, x, x8, s["stats"], s["scale"], s["shift"], rows(s["residual"]), rows(s["y"]), rows(s["dy"]), rows(dx),
                                rows(dres), d_scale, d_shift, ws, ws.numel(), stream)
     out = {"dx": dx, "d_scale": d_scale, "d_shift": d_shift}
@@ -361,7 +361,7 @@ def run(state):
 
 
 # ------------------------------------------------------------------ from the definitions, in 64 bits
-def _exact_rows8(x):
+def _exact_byte_rows(x):
     """The values that x's rows stand for in 8 bits."""
     x = x.double()
     most = x.abs().max(1).values
@@ -392,9 +392,9 @@ def _exact_act(name, z):
 def exact(case, seed):
     c, s = case, prepare(case, seed)
     if c["op"] == CHECKPOINT:
-        return _exact_rows8(s["x"])
+        return _exact_byte_rows(s["x"])
     if c["op"] == FORWARD:
-        h = torch.matmul(_exact_rows8(s["x"]), _exact_values(s, s["w"], s["w_exp"])[:, :c["in"]].t().contiguous()) + s["bias"].double()
+        h = torch.matmul(_exact_byte_rows(s["x"]), _exact_values(s, s["w"], s["w_exp"])[:, :c["in"]].t().contiguous()) + s["bias"].double()
         if c["extra"]:
             h += s["residual"].double()
         y, slope = _exact_act("gelu" if c["gelu"] else "none", h)
@@ -415,7 +415,7 @@ def exact(case, seed):
         z = (x - spread(mean)) * spread(r) * s["scale"].double() + s["shift"].double()
         z = z.view(-1, ch) if s["residual"] is None else z.view(-1, ch) + s["residual"].double()
         out = {"y": _exact_act(c["act"], z)[0], "stats": torch.stack([mean, r], 2)}
-        return {**out, "kept": _exact_rows8(s["x"])} if c["kept"] else out
+        return {**out, "kept": _exact_byte_rows(s["x"])} if c["kept"] else out
     x = (_exact_values(s, s["x"], s["x_exp"])[:, :ch] if c["kept"] else s["x"].double()).reshape(shape)
     mean, r = s["stats"].double().unbind(2)
     xhat, dz = (x - spread(mean)) * spread(r), s["dy"].double().view(shape)
