@@ -350,6 +350,99 @@ int ppll_qk_rotary_backward(const ppll_rotary_config* cfg, const int32_t* positi
                             const ppll_queries_keys* x, const ppll_queries_keys* dy, const ppll_queries_keys* dx, float* d_q_scale_dev,
                             float* d_k_scale_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
+/* ------------------------------------------------------------------ rows of 8 bits
+ * What layers hold in 8 bits: rows (a token's activations, a pixel's channels, the weights of one output channel) of int8 values q with one
+ * exponent e each; element c of row r stands for q[r * ld + c] * 2^e[r].  e is -126..121, or -128 for a row that stands for NaN.
+ * q is 16-byte aligned, ld a multiple of 16 (to 2^20) and at least the number of columns; the bytes between the last column and the next multiple of
+ * 16 hold 0.  The calls that write rows write those zeros, the products count on them; bytes behind are left as they are.
+ * The step of a row is a power of two, up to twice the step that its largest element needs, so that every value has at most 7 significant
+ * bits: it is exact in bf16, and so are the products in the gradients of a linear layer, whose sums the steps stand under. */
+typedef struct {
+  int8_t *q, *e;          /* device memory */
+  int64_t ld;
+} ppll_byte_rows;
+
+/* Rows of one element type, `ld` elements apart (ld >= columns, ld < 2^31): element c of row r is p[r * ld + c].  Aligned to the element. */
+typedef struct {
+  void* p;                /* device memory */
+  int64_t ld;
+} ppll_rows;
+
+/* Rows (0..2^30 of them, cols 1..65536) of `precision`'s type into 8 bits: e is the least exponent of -126..121 with max|x| <= 127 * 2^e, q is x * 2^-e
+ * rounded to the nearest whole number, ties to even, at most 127.  A row with a NaN or an infinity becomes a row of NaN (q = 0).  Elements
+ * under 2^-127 become 0. */
+int ppll_byte_rows_pack(int32_t precision, int32_t rows, int32_t cols, const ppll_rows* in, const ppll_byte_rows* out, void* hip_stream);
+
+/* The same of the columns of a [rows, cols] matrix (rows 1..65536, cols 0..65536), say a weight as layers have it, [in, out]: row c of `out` is column c of
+ * `in`, `rows` values. */
+int ppll_byte_rows_pack_columns(int32_t precision, int32_t rows, int32_t cols, const ppll_rows* in, const ppll_byte_rows* out, void* hip_stream);
+
+/* What rows of 8 bits stand for, in `precision`'s type: exact but where an fp32 or bf16 overflows (never for rows that pack made). */
+int ppll_byte_rows_unpack(int32_t precision, int32_t rows, int32_t cols, const ppll_byte_rows* in, const ppll_rows* out, void* hip_stream);
+
+/* ------------------------------------------------------------------ activations */
+enum { PPLL_ACT_NONE = 0, PPLL_ACT_RELU = 1, PPLL_ACT_SILU = 2, PPLL_ACT_GELU = 3 };   /* x, max(x, 0), x / (1 + e^-x), x Phi(x) with the normal CDF */
+
+/* ------------------------------------------------------------------ linear layer on rows of 8 bits
+ * X [rows, in_dim] tokens, W [out_dim, in_dim] a row for each output channel (ppll_byte_rows_pack_columns of an [in, out] weight). */
+typedef struct {
+  uint32_t struct_size;   /* = sizeof(ppll_byte_linear_config)                   */
+  int32_t precision;      /* element type of all that is not in 8 bits           */
+  int32_t rows;           /* 0..2^30                                             */
+  int32_t in_dim, out_dim;/* 1..65536                                            */
+  int32_t activation;     /* forward: PPLL_ACT_NONE or PPLL_ACT_GELU; ignored by the backward call */
+} ppll_byte_linear_config;
+
+/* Forward: h = X W^T + bias (+ residual), y = h or GELU(h); slope (nullable, with GELU only) receives GELU'(h), what a backward pass multiplies
+ * by.  The sums over in_dim are taken in 8-bit products and 32-bit whole numbers, exactly; the rest in fp32.  bias: fp32 [out_dim], nullable;
+ * residual: [rows, out_dim], nullable; it may be y (same pointer and stride); otherwise outputs overlap nothing. */
+int ppll_byte_linear_forward(const ppll_byte_linear_config* cfg, const ppll_byte_rows* x, const ppll_byte_rows* w, const float* bias_dev,
+                             const ppll_rows* residual, const ppll_rows* y, const ppll_rows* slope, void* hip_stream);
+
+/* Gradients of X W^T + bias at what the rows stand for, from dy [rows, out_dim]:
+ *   dx = dy W, times gate where given (an activation's slope at the place X came from; [rows, in_dim]);  dw = X^T dy, fp32 [in_dim, out_dim] row by row;
+ *   db = the column sums of dy, fp32 [out_dim].
+ * Each of dx, dw, db may be null (not wanted); w is needed for dx, x for dw.  dx may be gate; dw and db are overwritten (zeros where rows = 0).
+ * Sums in fp32 in a fixed order.  Workspace: ppll_byte_linear_workspace_bytes(cfg) bytes, 16-byte aligned, used by nothing else until the
+ * stream has passed the call; it holds what one operand at a time stands for. */
+int ppll_byte_linear_workspace_bytes(const ppll_byte_linear_config* cfg, size_t* bytes);
+int ppll_byte_linear_backward(const ppll_byte_linear_config* cfg, const ppll_byte_rows* x, const ppll_byte_rows* w, const ppll_rows* dy,
+                              const ppll_rows* gate, const ppll_rows* dx, float* dw_dev, float* db_dev, void* workspace_dev, size_t workspace_bytes,
+                              void* hip_stream);
+
+/* ------------------------------------------------------------------ group norm with an activation, channels last
+ * Maps of `images` x `pixels` rows of `channels` (NHWC; a row's stride in each ppll_rows).  A group is channels / groups neighbouring channels; mean and
+ * variance (biased) run over a group's channels at all pixels of one image:
+ *   z = (x - mean) / sqrt(var + eps) * scale[c] + shift[c] (+ residual),  y = activation(z). */
+typedef struct {
+  uint32_t struct_size;   /* = sizeof(ppll_group_norm_config)                    */
+  int32_t precision;      /* element type of maps and their gradients            */
+  int32_t images, pixels; /* images >= 0, pixels >= 1, images * pixels <= 2^30   */
+  int32_t channels;       /* 1..4096                                             */
+  int32_t groups;         /* >= 1, divides channels                              */
+  int32_t activation;     /* PPLL_ACT_...                                        */
+  float eps;              /* > 0 and finite                                      */
+} ppll_group_norm_config;
+
+/* Bytes of workspace that either call needs: 16-byte aligned, used by nothing else until the stream has passed the call.  May be 0. */
+int ppll_group_norm_workspace_bytes(const ppll_group_norm_config* cfg, size_t* bytes);
+
+/* Forward.  scale_dev, shift_dev: fp32 [channels]; residual nullable; stats_dev: fp32 [images][groups][2], mean and 1 / sqrt(var + eps), nullable;
+ * keep (nullable) receives x in 8 bits, a row for each pixel, for the backward call.  y may be x or residual (same pointer and
+ * stride), otherwise outputs overlap nothing. */
+int ppll_group_norm_forward(const ppll_group_norm_config* cfg, const ppll_rows* x, const float* scale_dev, const float* shift_dev, const ppll_rows* residual,
+                            const ppll_rows* y, float* stats_dev, const ppll_byte_rows* keep, void* workspace_dev, size_t workspace_bytes,
+                            void* hip_stream);
+
+/* Backward, with the forward's statistics.  x: the forward's input, or null where x_bytes, the same in 8 bits, is given.  dz = dy times the activation's
+ * slope at z: y is needed with ReLU (the slope is 1 where y > 0), residual with SiLU and GELU if the forward had one; both are ignored
+ * otherwise.  dx and d_residual (= dz, nullable) may be dy, one of them; d_scale_dev, d_shift_dev: fp32 [channels], overwritten (zeros where images = 0).  Sums
+ * in fp32 in a fixed order. */
+int ppll_group_norm_backward(const ppll_group_norm_config* cfg, const ppll_rows* x, const ppll_byte_rows* x_bytes, const float* stats_dev,
+                             const float* scale_dev, const float* shift_dev, const ppll_rows* residual, const ppll_rows* y, const ppll_rows* dy,
+                             const ppll_rows* dx, const ppll_rows* d_residual, float* d_scale_dev, float* d_shift_dev, void* workspace_dev,
+                             size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

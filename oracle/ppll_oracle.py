@@ -455,6 +455,60 @@ def rms_norm_bwd(dy, cache, g):
     return r * (dh - xhat * (dh * xhat).mean(axis=-1, keepdims=True)), (dy * xhat).sum(axis=tuple(range(dy.ndim - 1)))
 
 
+# ---------------------------------------------------------------- rows of 8 bits, group norm
+def byte_rows(x):
+    """Rows in 8 bits: whole numbers q and exponents e [rows] with row r about q[r] 2^e[r]; e the least of -126 .. 121 with max|x| <= 127 2^e."""
+    x = np.asarray(x, dtype=np.float64)
+    q, e = np.zeros(x.shape), np.full(x.shape[0], -126)
+    for r, row in enumerate(x):
+        if not np.isfinite(row).all():
+            e[r] = -128
+            continue
+        while e[r] < 121 and np.abs(row).max() > 127 * 2.0 ** e[r]:
+            e[r] += 1
+        q[r] = np.clip(np.rint(row / 2.0 ** e[r]), -127, 127)        # (rint: ties to even)
+    return q, e
+
+
+def byte_values(q, e):
+    """What rows of 8 bits stand for."""
+    step = np.where(e == -128, np.nan, 2.0 ** e.astype(np.float64))
+    return q.astype(np.float64) * step[:, None]
+
+
+def activation(name, z):
+    """An activation and its derivative."""
+    if name == "relu":
+        return np.maximum(z, 0), (z > 0).astype(np.float64)
+    if name == "silu":
+        s = 1 / (1 + np.exp(-z))
+        return z * s, s * (1 + z * (1 - s))
+    if name == "gelu":
+        return gelu_fwd(z), gelu_bwd(np.ones_like(z), z)
+    return z, np.ones_like(z)
+
+
+def group_norm_fwd(x, g, b, groups, eps, act="none", residual=None):
+    """x [images, pixels, channels] -> y, statistics [images, groups, 2] (mean, 1 / deviation), z in front of the activation."""
+    v = x.reshape(*x.shape[:2], groups, -1)
+    mean = v.mean(axis=(1, 3), keepdims=True)
+    r = 1 / np.sqrt(v.var(axis=(1, 3), keepdims=True) + eps)
+    z = ((v - mean) * r).reshape(x.shape) * g + b
+    if residual is not None:
+        z = z + residual
+    return activation(act, z)[0], np.stack([mean, r], -1).reshape(x.shape[0], groups, 2), z
+
+
+def group_norm_bwd(dz, x, stats, g):
+    """dz: gradient in front of the activation (the residual's too) -> dx, dg, db."""
+    groups = stats.shape[1]
+    split = lambda a: a.reshape(*x.shape[:2], groups, -1)
+    mean, r = (stats[..., i].reshape(x.shape[0], 1, groups, 1) for i in (0, 1))
+    xhat, d = (split(x) - mean) * r, split(dz * g)
+    dx = r * (d - d.mean(axis=(1, 3), keepdims=True) - xhat * (d * xhat).mean(axis=(1, 3), keepdims=True))
+    return dx.reshape(x.shape), (dz * xhat.reshape(x.shape)).sum(axis=(0, 1)), dz.sum(axis=(0, 1))
+
+
 # --------------------------------------------------------------------------
 # block = module M_j + auxiliary network A_j
 # --------------------------------------------------------------------------

@@ -17,6 +17,7 @@ PPLL_OK = 0
 ERR_NAMES = {1: "PPLL_ERR_NULL", 2: "PPLL_ERR_CONFIG", 3: "PPLL_ERR_SHAPE", 4: "PPLL_ERR_WORKSPACE",
              5: "PPLL_ERR_HIP", 6: "PPLL_ERR_LABEL", 7: "PPLL_ERR_STATE"}
 FP32, BF16 = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = range(4)
 T_PARAM, T_GRAD, T_MOMENT1, T_MOMENT2, T_BN_MEAN, T_BN_VAR = range(6)
 
 
@@ -104,6 +105,50 @@ def rotary_config(precision: int, rows: int, tokens: int, q_heads: int, k_heads:
                         (C.c_int32 * 3)(*pairs), 1 if neighbours else 0, base, norm_eps)
 
 
+class Rows(C.Structure):
+    """Mirror of ppll_rows."""
+    _fields_ = [("p", C.c_void_p), ("ld", C.c_int64)]
+
+
+def rows(t) -> Rows:
+    """A 2-d tensor whose last axis is contiguous."""
+    return Rows(*_rows(t))
+
+
+class ByteRows(C.Structure):
+    """Mirror of ppll_byte_rows."""
+    _fields_ = [("q", C.c_void_p), ("e", C.c_void_p), ("ld", C.c_int64)]
+
+
+def byte_rows(q, e) -> ByteRows:
+    """An int8 tensor [rows, ld or a part of it] whose last axis is contiguous, and the rows' exponents, int8 [rows]."""
+    if (q.element_size(), e.element_size()) != (1, 1) or e.dim() != 1 or (e.shape[0] > 1 and e.stride(0) != 1):
+        raise PpllError(3, "rows of 8 bits are an int8 tensor [rows, columns] and contiguous int8 exponents [rows]")
+    p, ld = _rows(q)
+    return ByteRows(p, e.data_ptr(), ld)
+
+
+class ByteLinearConfig(C.Structure):
+    """Mirror of ppll_byte_linear_config."""
+    _fields_ = [("struct_size", C.c_uint32), ("precision", C.c_int32), ("rows", C.c_int32), ("in_dim", C.c_int32), ("out_dim", C.c_int32),
+                ("activation", C.c_int32)]
+
+
+def byte_linear_config(precision: int, rows: int, in_dim: int, out_dim: int, activation: int = ACT_NONE) -> ByteLinearConfig:
+    return ByteLinearConfig(C.sizeof(ByteLinearConfig), precision, rows, in_dim, out_dim, activation)
+
+
+class GroupNormConfig(C.Structure):
+    """Mirror of ppll_group_norm_config."""
+    _fields_ = [("struct_size", C.c_uint32), ("precision", C.c_int32), ("images", C.c_int32), ("pixels", C.c_int32), ("channels", C.c_int32),
+                ("groups", C.c_int32), ("activation", C.c_int32), ("eps", C.c_float)]
+
+
+def group_norm_config(precision: int, images: int, pixels: int, channels: int, groups: int, activation: int = ACT_NONE,
+                      eps: float = 1e-5) -> GroupNormConfig:
+    return GroupNormConfig(C.sizeof(GroupNormConfig), precision, images, pixels, channels, groups, activation, eps)
+
+
 _lib = None
 _SIGS = {
     "ppll_last_error": (C.c_char_p, []),
@@ -150,6 +195,20 @@ _SIGS = {
     "ppll_qk_rotary_backward": (C.c_int, [C.POINTER(RotaryConfig), C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(QueriesKeys),
                                           C.POINTER(QueriesKeys), C.POINTER(QueriesKeys), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                                           C.c_void_p]),
+    "ppll_byte_rows_pack": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.POINTER(Rows), C.POINTER(ByteRows), C.c_void_p]),
+    "ppll_byte_rows_pack_columns": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.POINTER(Rows), C.POINTER(ByteRows), C.c_void_p]),
+    "ppll_byte_rows_unpack": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.POINTER(ByteRows), C.POINTER(Rows), C.c_void_p]),
+    "ppll_byte_linear_forward": (C.c_int, [C.POINTER(ByteLinearConfig), C.POINTER(ByteRows), C.POINTER(ByteRows), C.c_void_p, C.POINTER(Rows),
+                                           C.POINTER(Rows), C.POINTER(Rows), C.c_void_p]),
+    "ppll_byte_linear_workspace_bytes": (C.c_int, [C.POINTER(ByteLinearConfig), C.POINTER(C.c_size_t)]),
+    "ppll_byte_linear_backward": (C.c_int, [C.POINTER(ByteLinearConfig), C.POINTER(ByteRows), C.POINTER(ByteRows), C.POINTER(Rows), C.POINTER(Rows),
+                                            C.POINTER(Rows), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ppll_group_norm_workspace_bytes": (C.c_int, [C.POINTER(GroupNormConfig), C.POINTER(C.c_size_t)]),
+    "ppll_group_norm_forward": (C.c_int, [C.POINTER(GroupNormConfig), C.POINTER(Rows), C.c_void_p, C.c_void_p, C.POINTER(Rows), C.POINTER(Rows),
+                                          C.c_void_p, C.POINTER(ByteRows), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "ppll_group_norm_backward": (C.c_int, [C.POINTER(GroupNormConfig), C.POINTER(Rows), C.POINTER(ByteRows), C.c_void_p, C.c_void_p, C.c_void_p,
+                                           C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.c_void_p,
+                                           C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "ppll_block_profile_read_small": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
 }
 EXPORTS = tuple(_SIGS)
@@ -191,9 +250,9 @@ def ppll_last_error() -> str:
     return lib().ppll_last_error().decode()
 
 
-def _size_query(fn_name: str, cfg: BlockConfig) -> int:
+def _size_query(fn_name: str, cfg) -> int:
     out = C.c_size_t(0)
-    _check(getattr(lib(), fn_name)(C.byref(cfg), C.byref(out)))
+    _check(getattr(lib(), fn_name)(_ref(cfg), C.byref(out)))
     return out.value
 
 
@@ -402,3 +461,48 @@ def ppll_qk_rotary_backward(cfg: RotaryConfig, positions, q_scale, k_scale, x: O
                             d_q_scale=None, d_k_scale=None, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
     _check(lib().ppll_qk_rotary_backward(_ref(cfg), _ptr(positions), _ptr(q_scale), _ptr(k_scale), _ref(x), _ref(dy), _ref(dx), _ptr(d_q_scale),
                                          _ptr(d_k_scale), _ptr(workspace), workspace_bytes, _ptr(stream)))
+
+
+def ppll_byte_rows_pack(precision: int, n_rows: int, cols: int, x: Rows, out: ByteRows, stream=None) -> None:
+    _check(lib().ppll_byte_rows_pack(precision, n_rows, cols, _ref(x), _ref(out), _ptr(stream)))
+
+
+def ppll_byte_rows_pack_columns(precision: int, n_rows: int, cols: int, x: Rows, out: ByteRows, stream=None) -> None:
+    _check(lib().ppll_byte_rows_pack_columns(precision, n_rows, cols, _ref(x), _ref(out), _ptr(stream)))
+
+
+def ppll_byte_rows_unpack(precision: int, n_rows: int, cols: int, x: ByteRows, out: Rows, stream=None) -> None:
+    _check(lib().ppll_byte_rows_unpack(precision, n_rows, cols, _ref(x), _ref(out), _ptr(stream)))
+
+
+def ppll_byte_linear_forward(cfg: ByteLinearConfig, x: ByteRows, w: ByteRows, bias, residual: Optional[Rows], y: Rows, slope: Optional[Rows] = None,
+                             stream=None) -> None:
+    _check(lib().ppll_byte_linear_forward(_ref(cfg), _ref(x), _ref(w), _ptr(bias), _ref(residual), _ref(y), _ref(slope), _ptr(stream)))
+
+
+def ppll_byte_linear_workspace_bytes(cfg: ByteLinearConfig) -> int:
+    return _size_query("ppll_byte_linear_workspace_bytes", cfg)
+
+
+def ppll_byte_linear_backward(cfg: ByteLinearConfig, x: Optional[ByteRows], w: Optional[ByteRows], dy: Rows, gate: Optional[Rows], dx: Optional[Rows],
+                              dw, db, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().ppll_byte_linear_backward(_ref(cfg), _ref(x), _ref(w), _ref(dy), _ref(gate), _ref(dx), _ptr(dw), _ptr(db), _ptr(workspace),
+                                           workspace_bytes, _ptr(stream)))
+
+
+def ppll_group_norm_workspace_bytes(cfg: GroupNormConfig) -> int:
+    return _size_query("ppll_group_norm_workspace_bytes", cfg)
+
+
+def ppll_group_norm_forward(cfg: GroupNormConfig, x: Rows, scale, shift, residual: Optional[Rows], y: Rows, stats=None,
+                            keep: Optional[ByteRows] = None, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().ppll_group_norm_forward(_ref(cfg), _ref(x), _ptr(scale), _ptr(shift), _ref(residual), _ref(y), _ptr(stats), _ref(keep),
+                                         _ptr(workspace), workspace_bytes, _ptr(stream)))
+
+
+def ppll_group_norm_backward(cfg: GroupNormConfig, x: Optional[Rows], x_bytes: Optional[ByteRows], stats, scale, shift, residual: Optional[Rows],
+                             y: Optional[Rows], dy: Rows, dx: Rows, d_residual: Optional[Rows], d_scale, d_shift, workspace=None,
+                             workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().ppll_group_norm_backward(_ref(cfg), _ref(x), _ref(x_bytes), _ptr(stats), _ptr(scale), _ptr(shift), _ref(residual), _ref(y),
+                                          _ref(dy), _ref(dx), _ref(d_residual), _ptr(d_scale), _ptr(d_shift), _ptr(workspace), workspace_bytes,
+                                          _ptr(stream)))

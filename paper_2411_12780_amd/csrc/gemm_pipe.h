@@ -142,14 +142,36 @@ template <bool TR, int ROWS, int KT = KS> __device__ __forceinline__ int frag_ba
 // compiler would order LDS reads that it knows of behind all outstanding copies into LDS; the wait is inside, so every output
 // is there when the compiler thinks it is.  The s_nop covers a register of the products written by a vector instruction before.
 #define PPLL_MMA(J, I) "v_mfma_f32_32x32x16_bf16 %[c" #J #I "], %[q" #J "], %[p" #I "], %[c" #J #I "]\n"
+#define PPLL_MMA8(J, I) "v_mfma_i32_32x32x32_i8 %[c" #J #I "], %[q" #J "], %[p" #I "], %[c" #J #I "]\n"
 #define PPLL_ACC [c00] "+v"(acc[0][0]), [c01] "+v"(acc[0][1]), [c02] "+v"(acc[0][2]), [c03] "+v"(acc[0][3]), \
                  [c10] "+v"(acc[1][0]), [c11] "+v"(acc[1][1]), [c12] "+v"(acc[1][2]), [c13] "+v"(acc[1][3])
 #define PPLL_CUR [p0] "v"(a.get(0)), [p1] "v"(a.get(1)), [p2] "v"(a.get(2)), [p3] "v"(a.get(3)), [q0] "v"(b.get(0)), [q1] "v"(b.get(1))
 #define PPLL_ROWS [r1] "n"(R32), [r2] "n"(2 * R32), [r3] "n"(3 * R32), [r4] "n"(4 * R32)
-template <bool AT, bool BT, int ROWS_A, int ROWS_B, int KK, int IM, int KT = KS>
+// I8: whole numbers of 8 bits instead of bf16, both with k contiguous: a fragment is 16 consecutive k of a row, the same bytes; sums in whole
+// numbers of 32 bits, in the same registers.
+#define PPLL_STEP5(MMA) \
+    asm volatile("s_nop 1\n" MMA(0, 0) "ds_read_b128 %[y0], %[rb]\n ds_read_b128 %[x0], %[ra]\n" MMA(0, 1) \
+                 "ds_read_b128 %[x1], %[ra] offset:%[r1]\n ds_read_b128 %[x2], %[ra] offset:%[r2]\n" MMA(0, 2) \
+                 "ds_read_b128 %[x3], %[ra] offset:%[r3]\n ds_read_b128 %[x4], %[ra] offset:%[r4]\n" MMA(0, 3) \
+                 "ds_read_b128 %[y1], %[rb] offset:%[r1]\n" MMA(0, 4) \
+                 MMA(1, 0) MMA(1, 1) MMA(1, 2) MMA(1, 3) MMA(1, 4) "s_waitcnt lgkmcnt(0)" \
+                 : PPLL_ACC, [c04] "+v"(acc[0][4]), [c14] "+v"(acc[1][4]), [x0] "=&v"(na.v[0]), [x1] "=&v"(na.v[1]), [x2] "=&v"(na.v[2]), \
+                   [x3] "=&v"(na.v[3]), [x4] "=&v"(na.v[4]), [y0] "=&v"(nb.v[0]), [y1] "=&v"(nb.v[1]) \
+                 : PPLL_CUR, [p4] "v"(a.get(4)), [ra] "v"(KK ? addrA ^ (32 * KK) : addrA), [rb] "v"(KK ? addrB ^ (32 * KK) : addrB), PPLL_ROWS \
+                 : "memory")
+#define PPLL_STEP4(MMA) \
+    asm volatile("s_nop 1\n" MMA(0, 0) "ds_read_b128 %[y0], %[rb]\n ds_read_b128 %[x0], %[ra]\n" MMA(0, 1) \
+                 "ds_read_b128 %[x1], %[ra] offset:%[r1]\n ds_read_b128 %[x2], %[ra] offset:%[r2]\n" MMA(0, 2) \
+                 "ds_read_b128 %[x3], %[ra] offset:%[r3]\n ds_read_b128 %[y1], %[rb] offset:%[r1]\n" MMA(0, 3) \
+                 MMA(1, 0) MMA(1, 1) MMA(1, 2) MMA(1, 3) "s_waitcnt lgkmcnt(0)" \
+                 : PPLL_ACC, [x0] "=&v"(na.v[0]), [x1] "=&v"(na.v[1]), [x2] "=&v"(na.v[2]), [x3] "=&v"(na.v[3]), [y0] "=&v"(nb.v[0]), \
+                   [y1] "=&v"(nb.v[1]) \
+                 : PPLL_CUR, [ra] "v"(KK ? addrA ^ (32 * KK) : addrA), [rb] "v"(KK ? addrB ^ (32 * KK) : addrB), PPLL_ROWS \
+                 : "memory")
+template <bool AT, bool BT, int ROWS_A, int ROWS_B, int KK, int IM, int KT = KS, bool I8 = false>
 __device__ __forceinline__ void k_step(f32x16 (&acc)[2][IM], const Frags<AT, IM>& a, const Frags<BT, 2>& b, Frags<AT, IM>& na, Frags<BT, 2>& nb,
                                        int addrA, int addrB) {
-  static_assert(IM == 4 || (IM == 5 && !AT), "");
+  static_assert((IM == 4 || (IM == 5 && !AT)) && (!I8 || (!AT && !BT)), "");
   constexpr int PA = ROWS_A * 2, PB = ROWS_B * 2, R32 = 64 * KT;     // bytes of 32 rows with k contiguous
   if constexpr (IM == 5 && BT) {
     asm volatile("s_nop 1\n" PPLL_MMA(0, 0)
@@ -165,15 +187,7 @@ __device__ __forceinline__ void k_step(f32x16 (&acc)[2][IM], const Frags<AT, IM>
                    [ol] "n"(KK * 16 * PB), [oh] "n"(KK * 16 * PB + 4 * PB), PPLL_ROWS
                  : "memory");
   } else if constexpr (IM == 5) {
-    asm volatile("s_nop 1\n" PPLL_MMA(0, 0) "ds_read_b128 %[y0], %[rb]\n ds_read_b128 %[x0], %[ra]\n" PPLL_MMA(0, 1)
-                 "ds_read_b128 %[x1], %[ra] offset:%[r1]\n ds_read_b128 %[x2], %[ra] offset:%[r2]\n" PPLL_MMA(0, 2)
-                 "ds_read_b128 %[x3], %[ra] offset:%[r3]\n ds_read_b128 %[x4], %[ra] offset:%[r4]\n" PPLL_MMA(0, 3)
-                 "ds_read_b128 %[y1], %[rb] offset:%[r1]\n" PPLL_MMA(0, 4)
-                 PPLL_MMA(1, 0) PPLL_MMA(1, 1) PPLL_MMA(1, 2) PPLL_MMA(1, 3) PPLL_MMA(1, 4) "s_waitcnt lgkmcnt(0)"
-                 : PPLL_ACC, [c04] "+v"(acc[0][4]), [c14] "+v"(acc[1][4]), [x0] "=&v"(na.v[0]), [x1] "=&v"(na.v[1]), [x2] "=&v"(na.v[2]),
-                   [x3] "=&v"(na.v[3]), [x4] "=&v"(na.v[4]), [y0] "=&v"(nb.v[0]), [y1] "=&v"(nb.v[1])
-                 : PPLL_CUR, [p4] "v"(a.get(4)), [ra] "v"(KK ? addrA ^ (32 * KK) : addrA), [rb] "v"(KK ? addrB ^ (32 * KK) : addrB), PPLL_ROWS
-                 : "memory");
+    if constexpr (I8) { PPLL_STEP5(PPLL_MMA8); } else { PPLL_STEP5(PPLL_MMA); }
   } else if constexpr (!AT && BT) {
     asm volatile("s_nop 1\n" PPLL_MMA(0, 0)
                  "ds_read_b64_tr_b16 %[l0], %[rb0] offset:%[ol]\n ds_read_b64_tr_b16 %[h0], %[rb0] offset:%[oh]\n" PPLL_MMA(0, 1)
@@ -187,14 +201,7 @@ __device__ __forceinline__ void k_step(f32x16 (&acc)[2][IM], const Frags<AT, IM>
                    [oh] "n"(KK * 16 * PB + 4 * PB), PPLL_ROWS
                  : "memory");
   } else if constexpr (!AT && !BT) {
-    asm volatile("s_nop 1\n" PPLL_MMA(0, 0) "ds_read_b128 %[y0], %[rb]\n ds_read_b128 %[x0], %[ra]\n" PPLL_MMA(0, 1)
-                 "ds_read_b128 %[x1], %[ra] offset:%[r1]\n ds_read_b128 %[x2], %[ra] offset:%[r2]\n" PPLL_MMA(0, 2)
-                 "ds_read_b128 %[x3], %[ra] offset:%[r3]\n ds_read_b128 %[y1], %[rb] offset:%[r1]\n" PPLL_MMA(0, 3)
-                 PPLL_MMA(1, 0) PPLL_MMA(1, 1) PPLL_MMA(1, 2) PPLL_MMA(1, 3) "s_waitcnt lgkmcnt(0)"
-                 : PPLL_ACC, [x0] "=&v"(na.v[0]), [x1] "=&v"(na.v[1]), [x2] "=&v"(na.v[2]), [x3] "=&v"(na.v[3]), [y0] "=&v"(nb.v[0]),
-                   [y1] "=&v"(nb.v[1])
-                 : PPLL_CUR, [ra] "v"(KK ? addrA ^ (32 * KK) : addrA), [rb] "v"(KK ? addrB ^ (32 * KK) : addrB), PPLL_ROWS
-                 : "memory");
+    if constexpr (I8) { PPLL_STEP4(PPLL_MMA8); } else { PPLL_STEP4(PPLL_MMA); }
   } else {
     static_assert(AT && BT, "");
     asm volatile("s_nop 1\n" PPLL_MMA(0, 0)
@@ -214,7 +221,10 @@ __device__ __forceinline__ void k_step(f32x16 (&acc)[2][IM], const Frags<AT, IM>
                  : "memory");
   }
 }
+#undef PPLL_STEP4
+#undef PPLL_STEP5
 #undef PPLL_MMA
+#undef PPLL_MMA8
 #undef PPLL_ACC
 #undef PPLL_CUR
 #undef PPLL_ROWS
@@ -226,7 +236,36 @@ template <bool BT> struct StageFrags {
   Frags<false, 8> a;      // fragment 2 kk + i: k step kk, 32-row tile i
   Frags<BT, 8> b;
 };
-template <bool BT>
+#define PPLL_STAGE(MMA) \
+    asm volatile("ds_read_b128 %[x0], %[ra0]\n ds_read_b128 %[x1], %[ra0] offset:4096\n " \
+                 MMA " %[c00], %[q0], %[p0], %[c00]\n ds_read_b128 %[y0], %[rb0]\n " \
+                 "ds_read_b128 %[y1], %[rb0] offset:4096\n " MMA " %[c01], %[q0], %[p1], %[c01]\n " \
+                 "ds_read_b128 %[x2], %[ra1]\n ds_read_b128 %[x3], %[ra1] offset:4096\n " \
+                 MMA " %[c10], %[q1], %[p0], %[c10]\n ds_read_b128 %[y2], %[rb1]\n " \
+                 "ds_read_b128 %[y3], %[rb1] offset:4096\n " MMA " %[c11], %[q1], %[p1], %[c11]\n " \
+                 "ds_read_b128 %[x4], %[ra2]\n ds_read_b128 %[x5], %[ra2] offset:4096\n " \
+                 MMA " %[c00], %[q2], %[p2], %[c00]\n ds_read_b128 %[y4], %[rb2]\n " \
+                 "ds_read_b128 %[y5], %[rb2] offset:4096\n " MMA " %[c01], %[q2], %[p3], %[c01]\n " \
+                 "ds_read_b128 %[x6], %[ra3]\n ds_read_b128 %[x7], %[ra3] offset:4096\n " \
+                 MMA " %[c10], %[q3], %[p2], %[c10]\n ds_read_b128 %[y6], %[rb3]\n " \
+                 "ds_read_b128 %[y7], %[rb3] offset:4096\n " MMA " %[c11], %[q3], %[p3], %[c11]\n " \
+                 MMA " %[c00], %[q4], %[p4], %[c00]\n " MMA " %[c01], %[q4], %[p5], %[c01]\n " \
+                 MMA " %[c10], %[q5], %[p4], %[c10]\n " MMA " %[c11], %[q5], %[p5], %[c11]\n " \
+                 MMA " %[c00], %[q6], %[p6], %[c00]\n " MMA " %[c01], %[q6], %[p7], %[c01]\n " \
+                 MMA " %[c10], %[q7], %[p6], %[c10]\n " MMA " %[c11], %[q7], %[p7], %[c11]\n " \
+                 "s_waitcnt lgkmcnt(0)" \
+                 : [c00] "+v"(acc[0][0]), [c01] "+v"(acc[0][1]), [c10] "+v"(acc[1][0]), [c11] "+v"(acc[1][1]), [x0] "=&v"(n.a.v[0]), \
+                   [x1] "=&v"(n.a.v[1]), [x2] "=&v"(n.a.v[2]), [x3] "=&v"(n.a.v[3]), [x4] "=&v"(n.a.v[4]), [x5] "=&v"(n.a.v[5]), \
+                   [x6] "=&v"(n.a.v[6]), [x7] "=&v"(n.a.v[7]), [y0] "=&v"(n.b.v[0]), [y1] "=&v"(n.b.v[1]), [y2] "=&v"(n.b.v[2]), \
+                   [y3] "=&v"(n.b.v[3]), [y4] "=&v"(n.b.v[4]), [y5] "=&v"(n.b.v[5]), [y6] "=&v"(n.b.v[6]), [y7] "=&v"(n.b.v[7]) \
+                 : [p0] "v"(f.a.get(0)), [q0] "v"(f.b.get(0)), [p1] "v"(f.a.get(1)), [q1] "v"(f.b.get(1)), \
+                   [p2] "v"(f.a.get(2)), [q2] "v"(f.b.get(2)), [p3] "v"(f.a.get(3)), [q3] "v"(f.b.get(3)), \
+                   [p4] "v"(f.a.get(4)), [q4] "v"(f.b.get(4)), [p5] "v"(f.a.get(5)), [q5] "v"(f.b.get(5)), \
+                   [p6] "v"(f.a.get(6)), [q6] "v"(f.b.get(6)), [p7] "v"(f.a.get(7)), [q7] "v"(f.b.get(7)), [ra0] "v"(addrA), \
+                   [ra1] "v"(addrA ^ 32), [ra2] "v"(addrA ^ 64), [ra3] "v"(addrA ^ 96), [rb0] "v"(addrB), [rb1] "v"(addrB ^ 32), \
+                   [rb2] "v"(addrB ^ 64), [rb3] "v"(addrB ^ 96) \
+                 : "memory")
+template <bool BT, bool I8 = false>
 __device__ __forceinline__ void stage_step(f32x16 (&acc)[2][2], const StageFrags<BT>& f, StageFrags<BT>& n, int addrA, int addrB) {
   if constexpr (BT) {
     asm volatile("ds_read_b128 %[x0], %[ra0]\n ds_read_b128 %[x1], %[ra0] offset:4096\n ds_read_b64_tr_b16 %[l0], %[rb0] offset:0\n "
@@ -263,41 +302,17 @@ __device__ __forceinline__ void stage_step(f32x16 (&acc)[2][2], const StageFrags
                    [ra1] "v"(addrA ^ 32), [ra2] "v"(addrA ^ 64), [ra3] "v"(addrA ^ 96), [rb0] "v"(addrB), [rb1] "v"(addrB ^ 64)
                  : "memory");
   } else {
-    asm volatile("ds_read_b128 %[x0], %[ra0]\n ds_read_b128 %[x1], %[ra0] offset:4096\n "
-                 "v_mfma_f32_32x32x16_bf16 %[c00], %[q0], %[p0], %[c00]\n ds_read_b128 %[y0], %[rb0]\n "
-                 "ds_read_b128 %[y1], %[rb0] offset:4096\n v_mfma_f32_32x32x16_bf16 %[c01], %[q0], %[p1], %[c01]\n "
-                 "ds_read_b128 %[x2], %[ra1]\n ds_read_b128 %[x3], %[ra1] offset:4096\n "
-                 "v_mfma_f32_32x32x16_bf16 %[c10], %[q1], %[p0], %[c10]\n ds_read_b128 %[y2], %[rb1]\n "
-                 "ds_read_b128 %[y3], %[rb1] offset:4096\n v_mfma_f32_32x32x16_bf16 %[c11], %[q1], %[p1], %[c11]\n "
-                 "ds_read_b128 %[x4], %[ra2]\n ds_read_b128 %[x5], %[ra2] offset:4096\n "
-                 "v_mfma_f32_32x32x16_bf16 %[c00], %[q2], %[p2], %[c00]\n ds_read_b128 %[y4], %[rb2]\n "
-                 "ds_read_b128 %[y5], %[rb2] offset:4096\n v_mfma_f32_32x32x16_bf16 %[c01], %[q2], %[p3], %[c01]\n "
-                 "ds_read_b128 %[x6], %[ra3]\n ds_read_b128 %[x7], %[ra3] offset:4096\n "
-                 "v_mfma_f32_32x32x16_bf16 %[c10], %[q3], %[p2], %[c10]\n ds_read_b128 %[y6], %[rb3]\n "
-                 "ds_read_b128 %[y7], %[rb3] offset:4096\n v_mfma_f32_32x32x16_bf16 %[c11], %[q3], %[p3], %[c11]\n "
-                 "v_mfma_f32_32x32x16_bf16 %[c00], %[q4], %[p4], %[c00]\n v_mfma_f32_32x32x16_bf16 %[c01], %[q4], %[p5], %[c01]\n "
-                 "v_mfma_f32_32x32x16_bf16 %[c10], %[q5], %[p4], %[c10]\n v_mfma_f32_32x32x16_bf16 %[c11], %[q5], %[p5], %[c11]\n "
-                 "v_mfma_f32_32x32x16_bf16 %[c00], %[q6], %[p6], %[c00]\n v_mfma_f32_32x32x16_bf16 %[c01], %[q6], %[p7], %[c01]\n "
-                 "v_mfma_f32_32x32x16_bf16 %[c10], %[q7], %[p6], %[c10]\n v_mfma_f32_32x32x16_bf16 %[c11], %[q7], %[p7], %[c11]\n "
-                 "s_waitcnt lgkmcnt(0)"
-                 : [c00] "+v"(acc[0][0]), [c01] "+v"(acc[0][1]), [c10] "+v"(acc[1][0]), [c11] "+v"(acc[1][1]), [x0] "=&v"(n.a.v[0]),
-                   [x1] "=&v"(n.a.v[1]), [x2] "=&v"(n.a.v[2]), [x3] "=&v"(n.a.v[3]), [x4] "=&v"(n.a.v[4]), [x5] "=&v"(n.a.v[5]),
-                   [x6] "=&v"(n.a.v[6]), [x7] "=&v"(n.a.v[7]), [y0] "=&v"(n.b.v[0]), [y1] "=&v"(n.b.v[1]), [y2] "=&v"(n.b.v[2]),
-                   [y3] "=&v"(n.b.v[3]), [y4] "=&v"(n.b.v[4]), [y5] "=&v"(n.b.v[5]), [y6] "=&v"(n.b.v[6]), [y7] "=&v"(n.b.v[7])
-                 : [p0] "v"(f.a.get(0)), [q0] "v"(f.b.get(0)), [p1] "v"(f.a.get(1)), [q1] "v"(f.b.get(1)),
-                   [p2] "v"(f.a.get(2)), [q2] "v"(f.b.get(2)), [p3] "v"(f.a.get(3)), [q3] "v"(f.b.get(3)),
-                   [p4] "v"(f.a.get(4)), [q4] "v"(f.b.get(4)), [p5] "v"(f.a.get(5)), [q5] "v"(f.b.get(5)),
-                   [p6] "v"(f.a.get(6)), [q6] "v"(f.b.get(6)), [p7] "v"(f.a.get(7)), [q7] "v"(f.b.get(7)), [ra0] "v"(addrA),
-                   [ra1] "v"(addrA ^ 32), [ra2] "v"(addrA ^ 64), [ra3] "v"(addrA ^ 96), [rb0] "v"(addrB), [rb1] "v"(addrB ^ 32),
-                   [rb2] "v"(addrB ^ 64), [rb3] "v"(addrB ^ 96)
-                 : "memory");
+    static_assert(!I8 || !BT, "");
+    if constexpr (I8) { PPLL_STAGE("v_mfma_i32_32x32x32_i8"); } else { PPLL_STAGE("v_mfma_f32_32x32x16_bf16"); }
   }
 }
+#undef PPLL_STAGE
 
 // acc[jn][im] (of a wave that multiplies): C^T tiles (the B fragment goes first into the MFMA): lane l holds row im*32 + l%32, columns jn*32 + 8 q +
 // 4 (l/32) + e in element 4 q + e.  csum[jn] (COLSUM, wave-uniform do_colsum): this lane's share, k % 8 = e of its half of every
 // k step in element e, of the sum over k of B's row jn*32 + l%32.
-template <class S, bool AT, bool BT, bool COLSUM>
+// I8: lda, ldb, K in pairs of bytes, acc whole numbers of 32 bits.
+template <class S, bool AT, bool BT, bool COLSUM, bool I8 = false>
 __device__ __forceinline__ void multiply(const __amdgpu_buffer_rsrc_t rsA, const __amdgpu_buffer_rsrc_t rsB, long lda, long ldb,
                                          int m0, int n0, int M, int N, int K, lds_char* lds, f32x16 (&acc)[2][S::IM],
                                          float (&csum)[2][8], bool do_colsum) {
@@ -355,16 +370,16 @@ __device__ __forceinline__ void multiply(const __amdgpu_buffer_rsrc_t rsA, const
     for (int i = 0; i < IM; ++i) set_zero(a1, i);
 #pragma unroll
     for (int j = 0; j < 2; ++j) set_zero(b1, j);
-    k_step<AT, BT, S::BM, S::BN, 0, IM>(acc, a1, b1, a0, b0, fa0, fb0);
+    k_step<AT, BT, S::BM, S::BN, 0, IM, KS, I8>(acc, a1, b1, a0, b0, fa0, fb0);
     for (int i = 0; i < nk; ++i) {
       const int st = (i % NS) * S::STAGE, nx = ((i + 1) % NS) * S::STAGE;
       wait_vm<(NS - 3) * S::COPIES>();       // this wave's part of stage i + 1 is in LDS
       barrier();          // and everyone's; nobody reads stage i - 1 any more
       issue(i + NS - 1);
       column_sums(b0);
-      k_step<AT, BT, S::BM, S::BN, 1, IM>(acc, a0, b0, a1, b1, fa0 + st, fb0 + st);
+      k_step<AT, BT, S::BM, S::BN, 1, IM, KS, I8>(acc, a0, b0, a1, b1, fa0 + st, fb0 + st);
       column_sums(b1);
-      k_step<AT, BT, S::BM, S::BN, 0, IM>(acc, a1, b1, a0, b0, fa0 + nx, fb0 + nx);
+      k_step<AT, BT, S::BM, S::BN, 0, IM, KS, I8>(acc, a1, b1, a0, b0, fa0 + nx, fb0 + nx);
     }
   } else if constexpr (S::COPY_WAVES) {
     // All fragments of a stage are in registers before it is multiplied, so its place in LDS is filled again meanwhile: NS - 1 stages are on
@@ -388,7 +403,7 @@ __device__ __forceinline__ void multiply(const __amdgpu_buffer_rsrc_t rsA, const
 #pragma unroll
     for (int i = 0; i < 8; ++i) { set_zero(f1.a, i); set_zero(f1.b, i); }
     barrier();
-    stage_step<BT>(acc, f1, f0, fa0, fb0);   // the first fragments: products with zeros under the reads
+    stage_step<BT, I8>(acc, f1, f0, fa0, fb0);   // the first fragments: products with zeros under the reads
     int st = 0;
     auto next = [&] {
       barrier();
@@ -396,10 +411,10 @@ __device__ __forceinline__ void multiply(const __amdgpu_buffer_rsrc_t rsA, const
     };
     for (int i = 0; i < nk; i += 2) {
       next();
-      stage_step<BT>(acc, f0, f1, fa0 + st, fb0 + st);
+      stage_step<BT, I8>(acc, f0, f1, fa0 + st, fb0 + st);
       if (i + 1 >= nk) break;
       next();
-      stage_step<BT>(acc, f1, f0, fa0 + st, fb0 + st);
+      stage_step<BT, I8>(acc, f1, f0, fa0 + st, fb0 + st);
     }
   } else {
     // two stages of 64 k: one is filled from the moment that everyone has read it until the same point a stage later
@@ -411,16 +426,16 @@ __device__ __forceinline__ void multiply(const __amdgpu_buffer_rsrc_t rsA, const
     for (int i = 0; i < IM; ++i) set_zero(a1, i);
 #pragma unroll
     for (int j = 0; j < 2; ++j) set_zero(b1, j);
-    k_step<AT, BT, S::BM, S::BN, 0, IM, KT>(acc, a1, b1, a0, b0, fa0, fb0);
+    k_step<AT, BT, S::BM, S::BN, 0, IM, KT, I8>(acc, a1, b1, a0, b0, fa0, fb0);
     for (int i = 0; i < nk; ++i) {
       const int st = (i & 1) * S::STAGE, nx = S::STAGE - st;
-      k_step<AT, BT, S::BM, S::BN, 1, IM, KT>(acc, a0, b0, a1, b1, fa0 + st, fb0 + st);
-      k_step<AT, BT, S::BM, S::BN, 2, IM, KT>(acc, a1, b1, a0, b0, fa0 + st, fb0 + st);
-      k_step<AT, BT, S::BM, S::BN, 3, IM, KT>(acc, a0, b0, a1, b1, fa0 + st, fb0 + st);
+      k_step<AT, BT, S::BM, S::BN, 1, IM, KT, I8>(acc, a0, b0, a1, b1, fa0 + st, fb0 + st);
+      k_step<AT, BT, S::BM, S::BN, 2, IM, KT, I8>(acc, a1, b1, a0, b0, fa0 + st, fb0 + st);
+      k_step<AT, BT, S::BM, S::BN, 3, IM, KT, I8>(acc, a0, b0, a1, b1, fa0 + st, fb0 + st);
       wait_vm<0>();         // this wave's part of stage i + 1 is in LDS
       barrier();            // and everyone's; nobody reads stage i any more
       issue(i + 2);
-      k_step<AT, BT, S::BM, S::BN, 0, IM, KT>(acc, a1, b1, a0, b0, fa0 + nx, fb0 + nx);
+      k_step<AT, BT, S::BM, S::BN, 0, IM, KT, I8>(acc, a1, b1, a0, b0, fa0 + nx, fb0 + nx);
     }
   }
   // the last products are through before a vector instruction reads the accumulators

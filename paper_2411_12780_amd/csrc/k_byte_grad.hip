@@ -1,0 +1,416 @@
+// Gradients of the linear layer on rows of 8 bits: dX = dY W and dW = X^T dY, the operand in 8 bits on its way to LDS made the bf16 values that it
+// stands for (exactly: 7 significant bits and a power of two), then as a product in v_mfma_f32_32x32x16_bf16, fp32 sums.
+//
+// Both products run over the rows of the operand in 8 bits (output channels, tokens), whose other index is contiguous: it lies in LDS as in
+// memory, [k][row], and fragments come out of transposing reads; so does dY in dW, while in dX its k is contiguous.  128 x 128 tiles of four
+// waves, two stages of 64 k in LDS and two in registers.  dY in fp32 is three bf16 terms that add up to it exactly (8 bits each), three products,
+// stages of 32 k.  Operands of any alignment: 16-byte loads from where the elements lie; the last pieces of a ragged row are read ending at the
+// row's end and shifted.
+#include <algorithm>
+
+#include "bytes.h"
+
+namespace ppll {
+
+namespace {
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+constexpr int BM = 128, BN = 128, THREADS = 256, PITCH = 320;      // PITCH: bytes between k rows of a [k][row] tile (free of bank conflicts)
+constexpr int STAGE_LD = BN + 4;
+
+struct GradArgs {
+  const int8_t *q, *e; int64_t ldq; int qcols;       // operand in 8 bits: [K][qcols], qcols padded
+  const char* d; int64_t ldd; int dcols;             // dY, elements: [M][K] (dX) or [K][N]
+  char* out; int64_t ldo;                            // dX, or dW / its parts
+  const char* gate; int64_t ldg;
+  float* db;                                         // dW: column sums of dY (of a part), or null
+  int M, N, K, tiles_m, tiles_n, per_xcd, parts, part_k;
+  int64_t part_out;                                  // elements from part to part, and behind them of db
+};
+
+template <int DT> constexpr int terms() { return DT == F32 ? 3 : 1; }
+template <int DT> constexpr int step_k() { return DT == F32 ? 32 : 64; }
+// one term of the dY tile, the tile in 8 bits, a stage
+template <bool DX, int DT> constexpr int d_bytes() { return DX ? BM * step_k<DT>() * 2 : step_k<DT>() * PITCH; }
+template <int DT> constexpr int q_bytes() { return step_k<DT>() * PITCH; }
+template <bool DX, int DT> constexpr int stage_bytes() { return q_bytes<DT>() + terms<DT>() * d_bytes<DX, DT>(); }
+template <bool DX, int DT> constexpr int lds_bytes() { return std::max(2 * stage_bytes<DX, DT>(), BM * STAGE_LD * 4); }
+
+template <int BK> __device__ __forceinline__ int row_major(int row, int granule) {
+  return BK == 64 ? row * 128 + ((granule ^ ((row >> 1) & 7)) << 4) : row * 64 + ((granule ^ ((row >> 2) & 3)) << 4);
+}
+__device__ __forceinline__ uint2 lds_read_tr(const char* p) {
+  const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+  return __builtin_bit_cast(uint2, v);
+}
+// The three terms of eight values
+__device__ __forceinline__ void split(const Eight<F32>& x, uint4 (&t)[3]) {
+  float v[8];
+  x.get(v);
+  uint32_t w[3][4];
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[k][i] = f32x2_to_bf16x2(v[2 * i], v[2 * i + 1]);
+      v[2 * i] -= __uint_as_float(w[k][i] << 16);
+      v[2 * i + 1] -= __uint_as_float(w[k][i] & 0xffff0000u);
+    }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) t[k] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+}
+// Elements `by` .. 7 of eight to the front, zeros behind
+__device__ __forceinline__ void shift_down(Eight<BF16>& x, int by) {
+  const uint64_t lo = (uint64_t)x.w.x | (uint64_t)x.w.y << 32, hi = (uint64_t)x.w.z | (uint64_t)x.w.w << 32;
+  const int bits = 16 * by, b = bits & 63;
+  const uint64_t a = bits >= 64 ? hi : lo, c = bits >= 64 ? 0 : hi;
+  const uint64_t l = b ? a >> b | c << (64 - b) : a, h = c >> b;
+  x.w = make_uint4((uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32));
+}
+__device__ __forceinline__ void shift_down(Eight<F32>& x, int by) {
+  float v[8];
+  x.get(v);
+#pragma unroll
+  for (int s = 4; s >= 1; s >>= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = by & s ? (i + s < 8 ? v[i + s] : 0.f) : v[i];
+  x.set(v);
+}
+// Elements c .. c + 7 of a row of `cols`, zeros from `cols` on; c may be any
+template <int DT, bool RAGGED> __device__ __forceinline__ void load_eight(Eight<DT>& x, const char* row, int c, int cols) {
+  if (RAGGED && cols < 8) {
+    x.zero();
+    if (c < cols) x.load(row, c, cols);
+    return;
+  }
+  const int at = min(c, cols - 8);
+  __builtin_memcpy(&x, row + (int64_t)at * (DT == BF16 ? 2 : 4), sizeof x);
+  if (RAGGED) shift_down(x, min(c - at, 7));       // (c beyond the row: its last element may come, which no sum that is kept meets)
+}
+
+template <int DT> struct Regs {
+  static constexpr int NP = step_k<DT>() / 16;
+  uint2 q[NP];
+  int e[NP];
+  Eight<DT> d[NP];
+};
+
+template <bool DX, int DT, bool RAGGED>
+__global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
+  constexpr int T = terms<DT>(), BK = step_k<DT>(), NP = BK / 16, ESZ = DT == BF16 ? 2 : 4;
+  constexpr int QB = q_bytes<DT>(), DB = d_bytes<DX, DT>(), STAGE = stage_bytes<DX, DT>();
+  extern __shared__ __align__(16) char smem[];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, wm = wave >> 1, wn = wave & 1;
+  // XCD x (workgroup id % 8) takes a contiguous stretch: tiles of a row (of a part of k) share what they read in its L2
+  const int tiles = p.tiles_m * p.tiles_n, u = (blockIdx.x & 7) * p.per_xcd + (blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= p.per_xcd || u >= tiles * p.parts) return;
+  const int part = u / tiles, t = u - part * tiles, m0 = t / p.tiles_n * BM, n0 = t % p.tiles_n * BN;
+  const int kbeg = part * p.part_k, kend = min(p.K, kbeg + p.part_k), nk = (kend - kbeg + BK - 1) / BK;
+
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+
+  const int tk = tid >> 4, tc = (tid & 15) * 8;                                   // [k][row]: k rows tk + 16 j, columns tc ..
+  const int rk = (tid & (BK / 8 - 1)) * 8, rr = tid / (BK / 8);                   // [row][k]: rows rr + 2048 / BK j, k rk ..
+  constexpr int RSTEP = THREADS / (BK / 8);
+  const int qc = min((DX ? n0 : m0) + tc, p.qcols - 8);
+  const int8_t* qbase = p.q + qc;
+  auto gload = [&](int i, Regs<DT>& r) {
+    const int k0 = kbeg + i * BK;
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      const int k = min(k0 + tk + 16 * j, p.K - 1);
+      r.q[j] = *(const uint2*)(qbase + k * p.ldq);
+      r.e[j] = p.e[k];
+      if (DX) {
+        const int m = min(m0 + rr + RSTEP * j, p.M - 1);
+        load_eight<DT, RAGGED>(r.d[j], p.d + m * p.ldd * ESZ, k0 + rk, p.dcols);
+      } else {
+        load_eight<DT, RAGGED>(r.d[j], p.d + k * p.ldd * ESZ, n0 + tc, p.dcols);
+      }
+    }
+  };
+  // column sums of dY, by the workgroups of the first row of tiles, from the registers on their way
+  const bool do_db = !DX && p.db && m0 == 0;
+  float csum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  auto lstore = [&](int stage, int i, const Regs<DT>& r, int j) {
+    if (j >= NP) return;
+    char* st = smem + stage * STAGE;
+    const int k0 = kbeg + i * BK;
+    const bool in = k0 + tk + 16 * j < kend;
+    float f[8];
+    bytes_get(r.q[j], byte_step(r.e[j]), f);
+    Eight<BF16> x;
+    x.set(f);
+    if (!in) x.zero();
+    *(uint4*)(st + (tk + 16 * j) * PITCH + tc * 2) = x.w;
+    Eight<DT> d = r.d[j];
+    // dX: k from dcols on is beyond the row where the row is ragged, and zero; elsewhere a piece is in or out as a whole
+    if (DX ? k0 + rk >= kend : !in) d.zero();
+    if (do_db) {
+      float v[8];
+      d.get(v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) csum[e] += v[e];
+    }
+    char* to = st + QB + (DX ? row_major<BK>(rr + RSTEP * j, rk >> 3) : (tk + 16 * j) * PITCH + tc * 2);
+    if constexpr (DT == BF16) {
+      *(uint4*)to = d.w;
+    } else {
+      uint4 w[3];
+      split(d, w);
+#pragma unroll
+      for (int s = 0; s < 3; ++s) *(uint4*)(to + s * DB) = w[s];
+    }
+  };
+  const int tr_lane = (8 * (lane >> 5) + ((lane & 15) >> 2)) * PITCH + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+  auto frag_tr = [&](const char* tile, int row0, int kk) -> bf16x8 {
+    const char* a = tile + tr_lane + kk * 16 * PITCH + row0 * 2;
+    const uint2 lo = lds_read_tr(a), hi = lds_read_tr(a + 4 * PITCH);
+    return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+  };
+  auto frag_d = [&](const char* tile, int row0, int kk) -> bf16x8 {
+    if (DX) return *reinterpret_cast<const bf16x8*>(tile + row_major<BK>(row0 + (lane & 31), kk * 2 + (lane >> 5)));
+    return frag_tr(tile, row0, kk);
+  };
+  // wm: the wave's half of the rows of C, wn: of its columns
+  const int q0 = DX ? wn * 64 : wm * 64, d0 = DX ? wm * 64 : wn * 64;
+  bf16x8 fq[2][2], fd[2][2][T];
+  auto load_frags = [&](int stage, int kk, int set) {
+    const char* st = smem + stage * STAGE;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) fq[set][i] = frag_tr(st, q0 + 32 * i, kk);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int s = 0; s < T; ++s) fd[set][i][s] = frag_d(st + QB + s * DB, d0 + 32 * i, kk);
+  };
+  auto multiply = [&](int stage, int i, const Regs<DT>& next, bool stage_next) {
+#pragma unroll
+    for (int kk = 0; kk < BK / 16; ++kk) {
+      if (kk + 1 < BK / 16) load_frags(stage, kk + 1, (kk + 1) & 1);
+#pragma unroll
+      for (int s = T - 1; s >= 0; --s)       // the small terms first
+#pragma unroll
+        for (int jn = 0; jn < 2; ++jn)
+#pragma unroll
+          for (int im = 0; im < 2; ++im) {
+            const bf16x8 b = DX ? fq[kk & 1][jn] : fd[kk & 1][jn][s], a = DX ? fd[kk & 1][im][s] : fq[kk & 1][im];
+            acc[jn][im] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, acc[jn][im], 0, 0, 0);
+          }
+      if (stage_next) lstore(stage ^ 1, i + 1, next, kk);
+    }
+  };
+  Regs<DT> r[2];
+  gload(0, r[0]);
+  gload(1, r[1]);
+#pragma unroll
+  for (int j = 0; j < NP; ++j) lstore(0, 0, r[0], j);
+  __syncthreads();
+  gload(2, r[0]);
+  load_frags(0, 0, 0);
+  auto step = [&](int u, Regs<DT>& next, int i) {
+    multiply(u, i, next, true);
+    __syncthreads();
+    load_frags(u ^ 1, 0, 0);
+    gload(i + 3, next);
+  };
+  int i = 0;
+  for (; i + 2 < nk; i += 2) {
+    step(0, r[1], i);
+    step(1, r[0], i + 1);
+  }
+  if (nk - i == 2) {
+    step(0, r[1], i);
+    multiply(1, i + 1, r[0], false);
+  } else {
+    multiply(0, i, r[1], false);
+  }
+
+  // Epilogue through LDS: a thread takes 8 consecutive columns of a row
+  float* tile = reinterpret_cast<float*>(smem);
+  __syncthreads();
+#pragma unroll
+  for (int jn = 0; jn < 2; ++jn)
+#pragma unroll
+    for (int im = 0; im < 2; ++im)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(tile + (wm * 64 + im * 32 + (lane & 31)) * STAGE_LD + wn * 64 + jn * 32 + 8 * q + 4 * (lane >> 5)) =
+            make_float4(acc[jn][im][4 * q], acc[jn][im][4 * q + 1], acc[jn][im][4 * q + 2], acc[jn][im][4 * q + 3]);
+  __syncthreads();
+  const int n = n0 + tc;
+  if (n < p.N) {
+#pragma unroll
+    for (int j = 0; j < BM / 16; ++j) {
+      const int64_t m = m0 + tk + 16 * j;
+      if (m >= p.M) continue;
+      const float4 lo = *reinterpret_cast<const float4*>(tile + (tk + 16 * j) * STAGE_LD + tc), hi = *reinterpret_cast<const float4*>(tile + (tk + 16 * j) * STAGE_LD + tc + 4);
+      float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      if (DX) {
+        if (p.gate) {
+          Eight<DT> g;
+          float f[8];
+          g.load(p.gate + m * p.ldg * ESZ, n, p.N);
+          g.get(f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= f[e];
+        }
+        Eight<DT> o;
+        o.set(v);
+        o.store(p.out + m * p.ldo * ESZ, n, p.N);
+      } else {
+        Eight<F32> o;
+        o.set(v);
+        o.store(p.out + (part * p.part_out + m * p.ldo) * 4, n, p.N);
+      }
+    }
+  }
+  if (do_db) {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) tile[tk * STAGE_LD + tc + e] = csum[e];
+    __syncthreads();
+    if (tid < BN && n0 + tid < p.N) {
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s += tile[j * STAGE_LD + tid];
+      p.db[part * p.part_out + n0 + tid] = s;
+    }
+  }
+}
+
+// Sums of parts, in their order
+__global__ __launch_bounds__(256) void byte_grad_sum_kernel(const float* parts, int n_parts, int64_t part_out, float* dw, int64_t n_dw, float* db, int n_db) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  const int64_t n = n_dw + n_db;
+  if (i >= n) return;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int k = 0; k < n_parts; ++k) {       // (a part has room for whole pieces of four)
+    const float4 v = *(const float4*)(parts + k * part_out + i);
+    s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (i + e < n_dw) dw[i + e] = s[e];
+    else if (i + e < n) db[i + e - n_dw] = s[e];
+  }
+}
+
+// Column sums alone: each workgroup 64 columns of a stretch of rows
+constexpr int SUM_COLS = 64, SUM_ROWS = 512;
+template <int DT> __global__ __launch_bounds__(256) void byte_grad_columns_kernel(const char* d, int64_t ldd, int rows, int cols, float* out) {
+  __shared__ float sums[4][SUM_COLS];
+  const int c = blockIdx.x * SUM_COLS + (threadIdx.x & 63), w = threadIdx.x >> 6, r1 = min(rows, (int)(blockIdx.y + 1) * SUM_ROWS);
+  float s = 0.f;
+  if (c < cols)
+#pragma unroll 8
+    for (int r = blockIdx.y * SUM_ROWS + w; r < r1; r += 4) s += ld_f(d, r * ldd + c, DT);
+  sums[w][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (w == 0 && c < cols) out[(int64_t)blockIdx.y * cols + c] = sums[0][c - blockIdx.x * SUM_COLS] + sums[1][c - blockIdx.x * SUM_COLS] +
+                                                                sums[2][c - blockIdx.x * SUM_COLS] + sums[3][c - blockIdx.x * SUM_COLS];
+}
+__global__ __launch_bounds__(256) void byte_grad_zero_kernel(float* p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0.f;
+}
+
+template <bool DX, int DT> int launch(hipStream_t s, GradArgs& p) {
+  constexpr int LDS = lds_bytes<DX, DT>();
+  p.tiles_m = (p.M + BM - 1) / BM; p.tiles_n = (p.N + BN - 1) / BN;
+  p.per_xcd = (int)(((int64_t)p.tiles_m * p.tiles_n * p.parts + 7) / 8);
+  const dim3 grid(8 * p.per_xcd);
+  if (p.dcols & 7) {
+    static OncePerDevice once;
+    PPLL_TRY(raise_lds((const void*)byte_grad_kernel<DX, DT, true>, LDS, once));
+    hipLaunchKernelGGL((byte_grad_kernel<DX, DT, true>), grid, dim3(THREADS), LDS, s, p);
+  } else {
+    static OncePerDevice once;
+    PPLL_TRY(raise_lds((const void*)byte_grad_kernel<DX, DT, false>, LDS, once));
+    hipLaunchKernelGGL((byte_grad_kernel<DX, DT, false>), grid, dim3(THREADS), LDS, s, p);
+  }
+  PPLL_HIP(hipGetLastError());
+  return PPLL_OK;
+}
+
+// Into how many parts the reduction of dW goes: two workgroups a unit, none under four steps
+struct Parts { int n, k; int64_t out; };
+Parts parts_of(const ByteLinear& l) {
+  const int bk = l.dt == F32 ? step_k<F32>() : step_k<BF16>();
+  const int64_t tiles = (int64_t)((l.in + BM - 1) / BM) * ((l.out + BN - 1) / BN), steps = ((int64_t)l.rows + bk - 1) / bk;
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / 4));
+  const int64_t each = (steps + want - 1) / want;
+  Parts p;
+  p.n = (int)std::max<int64_t>(1, (steps + each - 1) / each);
+  p.k = (int)std::min<int64_t>(each * bk, 0x7fffffff);
+  p.out = ((int64_t)l.in * l.out + l.out + 3) / 4 * 4;
+  return p;
+}
+int sum_chunks(int rows) { return (int)(((int64_t)rows + SUM_ROWS - 1) / SUM_ROWS); }
+
+template <int DT> int backward(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
+                               const ppll_rows& dx, float* dw, float* db, float* ws) {
+  GradArgs p{};
+  p.d = (const char*)dy.p; p.ldd = dy.ld; p.dcols = l.out;
+  if (dx.p) {
+    p.q = w.q; p.e = w.e; p.ldq = w.ld; p.qcols = pad16(l.in);
+    p.out = (char*)dx.p; p.ldo = dx.ld; p.gate = (const char*)gate.p; p.ldg = gate.ld;
+    p.M = l.rows; p.N = l.in; p.K = l.out; p.parts = 1; p.part_k = l.out;
+    PPLL_TRY((launch<true, DT>(s, p)));
+  }
+  if (dw) {
+    const Parts parts = parts_of(l);
+    p.q = x.q; p.e = x.e; p.ldq = x.ld; p.qcols = pad16(l.in);
+    const bool whole = parts.n == 1;
+    p.out = (char*)(whole ? dw : ws); p.ldo = l.out; p.gate = nullptr;
+    p.db = !db ? nullptr : whole ? db : ws + (int64_t)l.in * l.out;
+    p.M = l.in; p.N = l.out; p.K = l.rows; p.parts = parts.n; p.part_k = parts.k; p.part_out = parts.out;
+    PPLL_TRY((launch<false, DT>(s, p)));
+    if (!whole) {
+      const int64_t n = (int64_t)l.in * l.out + (db ? l.out : 0);
+      hipLaunchKernelGGL(byte_grad_sum_kernel, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s, ws, parts.n, parts.out, dw, (int64_t)l.in * l.out, db,
+                         db ? l.out : 0);
+      PPLL_HIP(hipGetLastError());
+    }
+  } else if (db) {
+    const int chunks = sum_chunks(l.rows);
+    hipLaunchKernelGGL(byte_grad_columns_kernel<DT>, dim3((l.out + SUM_COLS - 1) / SUM_COLS, chunks), dim3(256), 0, s, p.d, p.ldd, l.rows, l.out,
+                       chunks == 1 ? db : ws);
+    PPLL_HIP(hipGetLastError());
+    if (chunks > 1) PPLL_TRY(reduce_partials(s, ws, chunks, l.out, l.out, 1.f, db));
+  }
+  return PPLL_OK;
+}
+int zero(hipStream_t s, float* p, int64_t n) {
+  if (!p) return PPLL_OK;
+  hipLaunchKernelGGL(byte_grad_zero_kernel, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 4096)), dim3(256), 0, s, p, n);
+  PPLL_HIP(hipGetLastError());
+  return PPLL_OK;
+}
+}  // namespace
+
+size_t byte_linear_workspace(const ByteLinear& l) {
+  if (l.rows <= 0) return 0;
+  const Parts p = parts_of(l);
+  const int64_t parts = p.n > 1 ? p.n * p.out : 0, sums = sum_chunks(l.rows) > 1 ? (int64_t)sum_chunks(l.rows) * l.out : 0;
+  return (size_t)std::max(parts, sums) * sizeof(float);
+}
+
+int launch_byte_linear_bwd(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
+                           const ppll_rows& dx, float* dw, float* db, char* ws) {
+  if (l.rows <= 0) {
+    PPLL_TRY(zero(s, dw, (int64_t)l.in * l.out));
+    return zero(s, db, l.out);
+  }
+  return l.dt == BF16 ? backward<BF16>(s, l, x, w, dy, gate, dx, dw, db, (float*)ws) : backward<F32>(s, l, x, w, dy, gate, dx, dw, db, (float*)ws);
+}
+
+}  // namespace ppll

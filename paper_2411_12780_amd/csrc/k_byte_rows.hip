@@ -1,0 +1,214 @@
+// Rows of 8 bits: into them, out of them, and out of the columns of a matrix.
+//
+// L neighbouring lanes hold a row in pieces of 8 elements, P each, read once; the largest magnitude goes round the lanes in registers and the
+// bytes leave 8 a lane.  What bounds it: memory (3 bytes an element from bf16).
+#include "bytes.h"
+
+namespace ppll {
+
+namespace {
+constexpr int THREADS = 256;
+constexpr unsigned MOST_BLOCKS = 1u << 20;
+
+template <int DT, int L, int P>
+__global__ __launch_bounds__(THREADS) void byte_rows_pack_kernel(const char* in, int64_t in_ld, int8_t* q, int8_t* e, int64_t q_ld, int rows, int cols) {
+  constexpr int R = THREADS / L, ESZ = DT == BF16 ? 2 : 4;
+  const int lane = threadIdx.x % L, pieces = (cols + 15) / 16 * 2;
+  for (int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / L; r < rows; r += (int64_t)gridDim.x * R) {
+    const char* row = in + r * in_ld * ESZ;
+    Eight<DT> v[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int c = (lane + i * L) * 8;
+      if (c < cols) v[i].load(row, c, cols);
+      else v[i].zero();
+    }
+    uint32_t most = 0;
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < P; ++i) { v[i].get(f); most = most_of(f, most); }
+    const int x = byte_exponent(lanes_most<L>(most));
+    const bool nan = x == BYTE_NAN;
+    const float inv = exp2_bits(nan ? 0 : -x);
+    if (lane == 0) e[r] = (int8_t)x;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int p = lane + i * L;
+      v[i].get(f);
+      if (p < pieces) *(uint2*)(q + r * q_ld + p * 8) = nan ? make_uint2(0, 0) : bytes_of(f, inv);
+    }
+  }
+}
+
+// Rows that the lanes do not hold: read twice, a wave each
+template <int DT>
+__global__ __launch_bounds__(THREADS) void byte_rows_pack_long_kernel(const char* in, int64_t in_ld, int8_t* q, int8_t* e, int64_t q_ld, int rows, int cols) {
+  constexpr int R = THREADS / 64, ESZ = DT == BF16 ? 2 : 4;
+  const int lane = threadIdx.x % 64, pieces = (cols + 15) / 16 * 2;
+  for (int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / 64; r < rows; r += (int64_t)gridDim.x * R) {
+    const char* row = in + r * in_ld * ESZ;
+    uint32_t most = 0;
+    float f[8];
+    for (int p = lane; p * 8 < cols; p += 64) {
+      Eight<DT> v;
+      v.load(row, p * 8, cols);
+      v.get(f);
+      most = most_of(f, most);
+    }
+    const int x = byte_exponent(lanes_most<64>(most));
+    const bool nan = x == BYTE_NAN;
+    const float inv = exp2_bits(nan ? 0 : -x);
+    if (lane == 0) e[r] = (int8_t)x;
+    for (int p = lane; p < pieces; p += 64) {
+      Eight<DT> v;
+      v.zero();
+      if (p * 8 < cols) v.load(row, p * 8, cols);
+      v.get(f);
+      *(uint2*)(q + r * q_ld + p * 8) = nan ? make_uint2(0, 0) : bytes_of(f, inv);
+    }
+  }
+}
+
+template <int DT, int L>
+__global__ __launch_bounds__(THREADS) void byte_rows_unpack_kernel(const int8_t* q, const int8_t* e, int64_t q_ld, char* out, int64_t out_ld, int rows, int cols) {
+  constexpr int R = THREADS / L, ESZ = DT == BF16 ? 2 : 4;
+  const int lane = threadIdx.x % L;
+  for (int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / L; r < rows; r += (int64_t)gridDim.x * R) {
+    const float step = byte_step(e[r]);
+    char* row = out + r * out_ld * ESZ;
+#pragma unroll 4
+    for (int c = lane * 8; c < cols; c += L * 8) {
+      const uint2 w = *(const uint2*)(q + r * q_ld + c);
+      float f[8];
+      bytes_get(w, step, f);
+      Eight<DT> v;
+      v.set(f);
+      v.store(row, c, cols);
+    }
+  }
+}
+
+// 32 columns a workgroup: their largest magnitudes over all rows, then the bytes, turned in LDS, 256 rows at a time
+constexpr int TC = 32, CT = 512, CHUNK = 256, CPITCH = CHUNK + 16;
+template <int DT>
+__global__ __launch_bounds__(CT) void byte_rows_pack_columns_kernel(const char* in, int64_t in_ld, int8_t* q, int8_t* e, int64_t q_ld, int rows, int cols) {
+  constexpr int ESZ = DT == BF16 ? 2 : 4, LANES = CT / 4;      // rows at a time: four threads a row
+  __shared__ uint32_t most[LANES][TC + 1];
+  __shared__ __align__(16) int8_t turned[TC][CPITCH];
+  __shared__ int exps[TC];
+  const int c0 = blockIdx.x * TC, mine = (threadIdx.x & 3) * 8, r0 = threadIdx.x >> 2, ncols = cols - c0;
+  const char* base = in + (int64_t)c0 * ESZ;
+  uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (mine < ncols) {
+#pragma unroll 4
+    for (int r = r0; r < rows; r += LANES) {
+      Eight<DT> v;
+      float f[8];
+      v.load(base + r * in_ld * ESZ, mine, ncols);
+      v.get(f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[i] = max(m[i], __float_as_uint(f[i]) & 0x7fffffffu);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most[r0][mine + i] = m[i];
+  __syncthreads();
+  for (int h = LANES / 2; h >= 16; h /= 2) {       // 16 threads a column at the end
+    for (int i = threadIdx.x; i < h * TC; i += CT) most[i / TC][i % TC] = max(most[i / TC][i % TC], most[i / TC + h][i % TC]);
+    __syncthreads();
+  }
+  if (threadIdx.x < TC) {
+    uint32_t a = 0;
+    for (int i = 0; i < 16; ++i) a = max(a, most[i][threadIdx.x]);
+    const int x = byte_exponent(a);
+    exps[threadIdx.x] = x;
+    if ((int)threadIdx.x < ncols) e[c0 + threadIdx.x] = (int8_t)x;
+  }
+  __syncthreads();
+  const int padded = (rows + 15) & ~15;
+  for (int k0 = 0; k0 < padded; k0 += CHUNK) {
+    for (int k = r0; k < CHUNK; k += LANES) {
+      const int r = k0 + k;
+      float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (r < rows && mine < ncols) {
+        Eight<DT> v;
+        v.load(base + r * in_ld * ESZ, mine, ncols);
+        v.get(f);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int x = exps[mine + i];
+        const uint32_t w = byte_pack4(f[i], 0.f, 0.f, 0.f, exp2_bits(x == BYTE_NAN ? 0 : -x));
+        turned[mine + i][k] = x == BYTE_NAN ? 0 : (int8_t)w;
+      }
+    }
+    __syncthreads();
+    {
+      const int c = threadIdx.x >> 4, k = (threadIdx.x & 15) * 16;
+      if (c < ncols && k0 + k < padded) *(uint4*)(q + (int64_t)(c0 + c) * q_ld + k0 + k) = *(const uint4*)&turned[c][k];
+    }
+    __syncthreads();
+  }
+}
+static_assert(TC * (CHUNK / 16) == CT, "");
+
+unsigned blocks_of(int rows, int per) {
+  const unsigned n = (unsigned)(((int64_t)rows + per - 1) / per);
+  return n < MOST_BLOCKS ? n : MOST_BLOCKS;
+}
+template <int DT, int L, int P> int pack(hipStream_t s, int rows, int cols, const ppll_rows& in, const ppll_byte_rows& out) {
+  hipLaunchKernelGGL((byte_rows_pack_kernel<DT, L, P>), dim3(blocks_of(rows, THREADS / L)), dim3(THREADS), 0, s, (const char*)in.p, in.ld, out.q, out.e, out.ld,
+                     rows, cols);
+  PPLL_HIP(hipGetLastError());
+  return PPLL_OK;
+}
+template <int DT> int pack_any(hipStream_t s, int rows, int cols, const ppll_rows& in, const ppll_byte_rows& out) {
+  const int pieces = (cols + 15) / 16 * 2;
+  if (pieces <= 4) return pack<DT, 1, 4>(s, rows, cols, in, out);
+  if (pieces <= 8) return pack<DT, 2, 4>(s, rows, cols, in, out);
+  if (pieces <= 16) return pack<DT, 4, 4>(s, rows, cols, in, out);
+  if (pieces <= 32) return pack<DT, 8, 4>(s, rows, cols, in, out);
+  if (pieces <= 64) return pack<DT, 16, 4>(s, rows, cols, in, out);
+  if (pieces <= 128) return pack<DT, 32, 4>(s, rows, cols, in, out);
+  if (pieces <= 256) return pack<DT, 64, 4>(s, rows, cols, in, out);
+  if (pieces <= 512) return pack<DT, 64, 8>(s, rows, cols, in, out);
+  if (pieces <= 1024) return pack<DT, 64, 16>(s, rows, cols, in, out);
+  hipLaunchKernelGGL((byte_rows_pack_long_kernel<DT>), dim3(blocks_of(rows, THREADS / 64)), dim3(THREADS), 0, s, (const char*)in.p, in.ld, out.q, out.e, out.ld,
+                     rows, cols);
+  PPLL_HIP(hipGetLastError());
+  return PPLL_OK;
+}
+template <int DT, int L> int unpack(hipStream_t s, int rows, int cols, const ppll_byte_rows& in, const ppll_rows& out) {
+  hipLaunchKernelGGL((byte_rows_unpack_kernel<DT, L>), dim3(blocks_of(rows, THREADS / L)), dim3(THREADS), 0, s, in.q, in.e, in.ld, (char*)out.p, out.ld, rows,
+                     cols);
+  PPLL_HIP(hipGetLastError());
+  return PPLL_OK;
+}
+template <int DT> int unpack_any(hipStream_t s, int rows, int cols, const ppll_byte_rows& in, const ppll_rows& out) {
+  if (cols <= 32) return unpack<DT, 1>(s, rows, cols, in, out);
+  if (cols <= 128) return unpack<DT, 4>(s, rows, cols, in, out);
+  if (cols <= 512) return unpack<DT, 16>(s, rows, cols, in, out);
+  return unpack<DT, 64>(s, rows, cols, in, out);
+}
+}  // namespace
+
+int launch_byte_rows_pack(hipStream_t s, int dt, int rows, int cols, const ppll_rows& in, const ppll_byte_rows& out) {
+  if (rows <= 0) return PPLL_OK;
+  return dt == BF16 ? pack_any<BF16>(s, rows, cols, in, out) : pack_any<F32>(s, rows, cols, in, out);
+}
+int launch_byte_rows_unpack(hipStream_t s, int dt, int rows, int cols, const ppll_byte_rows& in, const ppll_rows& out) {
+  if (rows <= 0) return PPLL_OK;
+  return dt == BF16 ? unpack_any<BF16>(s, rows, cols, in, out) : unpack_any<F32>(s, rows, cols, in, out);
+}
+int launch_byte_rows_pack_columns(hipStream_t s, int dt, int rows, int cols, const ppll_rows& in, const ppll_byte_rows& out) {
+  if (cols <= 0) return PPLL_OK;
+  const dim3 grid((cols + TC - 1) / TC);
+  if (dt == BF16)
+    hipLaunchKernelGGL(byte_rows_pack_columns_kernel<BF16>, grid, dim3(CT), 0, s, (const char*)in.p, in.ld, out.q, out.e, out.ld, rows, cols);
+  else
+    hipLaunchKernelGGL(byte_rows_pack_columns_kernel<F32>, grid, dim3(CT), 0, s, (const char*)in.p, in.ld, out.q, out.e, out.ld, rows, cols);
+  PPLL_HIP(hipGetLastError());
+  return PPLL_OK;
+}
+
+}  // namespace ppll
