@@ -384,7 +384,8 @@ int ppll_byte_rows_unpack(int32_t precision, int32_t rows, int32_t cols, const p
 enum { PPLL_ACT_NONE = 0, PPLL_ACT_RELU = 1, PPLL_ACT_SILU = 2, PPLL_ACT_GELU = 3 };   /* x, max(x, 0), x / (1 + e^-x), x Phi(x) with the normal CDF */
 
 /* ------------------------------------------------------------------ linear layer on rows of 8 bits
- * X [rows, in_dim] tokens, W [out_dim, in_dim] a row for each output channel (ppll_byte_rows_pack_columns of an [in, out] weight). */
+ * X [rows, in_dim] tokens, W [out_dim, in_dim] a row for each output channel (ppll_byte_rows_pack_columns of an [in, out] weight).  Row strides
+ * of the ppll_rows: 2^20 at most. */
 typedef struct {
   uint32_t struct_size;   /* = sizeof(ppll_byte_linear_config)                   */
   int32_t precision;      /* element type of all that is not in 8 bits           */
@@ -411,7 +412,7 @@ int ppll_byte_linear_backward(const ppll_byte_linear_config* cfg, const ppll_byt
                               void* hip_stream);
 
 /* ------------------------------------------------------------------ group norm with an activation, channels last
- * Maps of `images` x `pixels` rows of `channels` (NHWC; a row's stride in each ppll_rows).  A group is channels / groups neighbouring channels; mean and
+ * Maps of `images` x `pixels` rows of `channels` (NHWC; a row's stride in each ppll_rows, 2^20 at most).  A group is channels / groups neighbouring channels; mean and
  * variance (biased) run over a group's channels at all pixels of one image:
  *   z = (x - mean) / sqrt(var + eps) * scale[c] + shift[c] (+ residual),  y = activation(z). */
 typedef struct {

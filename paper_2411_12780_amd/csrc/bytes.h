@@ -10,7 +10,7 @@ constexpr int BYTE_NAN = -128;            // exponent of a row that stands for N
 constexpr int BYTE_LEAST = -126, BYTE_MOST = 121;
 constexpr int BYTE_COLS = 65536;          // columns at most: 127 * 127 * 65536 < 2^31
 constexpr int64_t BYTE_LD = 1 << 20;      // bytes between rows at most: the rows of a tile stay under 2^31 bytes
-constexpr int64_t ROW_LD = (int64_t)1 << 31;
+constexpr int64_t ROW_LD = (int64_t)1 << 31, MAP_LD = 1 << 20;      // elements between rows, and between those of a linear layer or a map
 
 inline int pad16(int v) { return (v + 15) & ~15; }
 
@@ -59,9 +59,9 @@ __device__ __forceinline__ uint32_t byte_pack4(float a, float b, float c, float 
   const uint32_t lo = __builtin_amdgcn_perm(q(b), q(a), 0x0c0c0400u), hi = __builtin_amdgcn_perm(q(d), q(c), 0x04000c0cu);
   return lo | hi;
 }
-__device__ __forceinline__ float byte_at(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
 
-// Eight neighbouring elements of a row, c .. c + 7, whatever their alignment; those at `cols` and behind read as 0
+// Eight neighbouring elements of a row, c .. c + 7, whatever their alignment; those at `cols` and behind read as 0.  (load_all, store_all: all
+// eight are there.)
 template <int DT> struct Eight;
 template <> struct Eight<F32> {
   float4 a, b;
@@ -82,6 +82,8 @@ template <> struct Eight<F32> {
   }
   __device__ __forceinline__ void set(const float (&v)[8]) { a = make_float4(v[0], v[1], v[2], v[3]); b = make_float4(v[4], v[5], v[6], v[7]); }
   __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void load_all(const char* p) { __builtin_memcpy(&a, p, 16); __builtin_memcpy(&b, p + 16, 16); }
+  __device__ __forceinline__ void store_all(char* p) const { __builtin_memcpy(p, &a, 16); __builtin_memcpy(p + 16, &b, 16); }
   __device__ __forceinline__ void store(void* row, int c, int cols) const {
     float* p = (float*)row + c;
     if (c + 8 <= cols) {
@@ -118,6 +120,8 @@ template <> struct Eight<BF16> {
     w = make_uint4(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7]));
   }
   __device__ __forceinline__ void zero() { w = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void load_all(const char* p) { __builtin_memcpy(&w, p, 16); }
+  __device__ __forceinline__ void store_all(char* p) const { __builtin_memcpy(p, &w, 16); }
   __device__ __forceinline__ void store(void* row, int c, int cols) const {
     uint16_t* p = (uint16_t*)row + c;
     if (c + 8 <= cols) {
@@ -130,10 +134,10 @@ template <> struct Eight<BF16> {
     }
   }
 };
-// Eight bytes of a row, c a multiple of 8 below the padded end
+// Eight bytes of a row times the row's step
 __device__ __forceinline__ void bytes_get(uint2 w, float step, float (&v)[8]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { v[i] = byte_at(w.x, i) * step; v[4 + i] = byte_at(w.y, i) * step; }
+  for (int i = 0; i < 4; ++i) { v[i] = (float)(int8_t)(w.x >> (8 * i)) * step; v[4 + i] = (float)(int8_t)(w.y >> (8 * i)) * step; }
 }
 __device__ __forceinline__ uint2 bytes_of(const float (&v)[8], float inv) {
   return make_uint2(byte_pack4(v[0], v[1], v[2], v[3], inv), byte_pack4(v[4], v[5], v[6], v[7], inv));

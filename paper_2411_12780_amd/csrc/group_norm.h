@@ -1,0 +1,211 @@
+// Group norm: what its forward and backward kernels share.
+#pragma once
+#include <algorithm>
+
+#include "bytes.h"
+
+namespace ppll {
+namespace norm {
+
+constexpr unsigned MOST_BLOCKS = 1u << 20;
+enum Mode : int { WHOLE = 0, PART = 1, APPLY = 2 };      // an image in one go; what a piece of it leaves; the result of a piece
+
+// How the threads of a workgroup lie over a slab: NPC piece columns (8 channels), RT pixels at a time
+struct NormArgs {
+  const char *x, *residual, *y_in, *dy;
+  const int8_t *q, *qe;
+  char *y, *dx, *dres;
+  int8_t *keep, *keep_e;
+  int64_t ldx, ldr, ldy, ldd, ldq, lddx, lddr, ldk;
+  const float *scale, *shift, *stats_in;
+  float *stats, *parts;            // parts: what PART leaves and APPLY joins
+  float* sums;                     // backward: channel sums of each image, [images][2][C]
+  int images, pixels, C, groups, cg, act;
+  int slab, slabs, npc, rt, pow2;  // channels of a slab; npc: piece columns, pow2: a power of two up to 64
+  int chunk, chunks;               // pixels of a piece, pieces of an image
+  int spg;                         // segments of a group
+  float eps;
+};
+
+template <bool EXACT> __device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + (EXACT ? expf(-z) : __expf(-z)));
+}
+// Activations and slopes as types, so that a loop over elements holds one of them
+struct Clamp {       // none (from = -infinity) and ReLU (0); a NaN stays one
+  float from;
+  __device__ __forceinline__ float operator()(float z) const { return z < from ? from : z; }
+};
+template <bool EXACT> struct Silu {
+  __device__ __forceinline__ float operator()(float z) const { return z * sigmoid<EXACT>(z); }
+  __device__ __forceinline__ float slope(float z) const {
+    const float s = sigmoid<EXACT>(z);
+    return s * (1.f + z * (1.f - s));
+  }
+};
+struct Gelu {
+  __device__ __forceinline__ float operator()(float z) const {
+    float cdf, pdf;
+    cdf_pdf(z, cdf, pdf);
+    return z * cdf;
+  }
+  __device__ __forceinline__ float slope(float z) const {
+    float cdf, pdf;
+    cdf_pdf(z, cdf, pdf);
+    return cdf + z * pdf;
+  }
+};
+template <bool EXACT, class F> __device__ __forceinline__ void with_activation(int act, F f) {
+  if (act == PPLL_ACT_SILU) f(Silu<EXACT>());
+  else if (act == PPLL_ACT_GELU) f(Gelu());
+  else f(Clamp{act == PPLL_ACT_RELU ? 0.f : -INFINITY});
+}
+
+// Sums of NV values over all threads of a piece column; every thread has its column's.  room: NV floats a thread
+template <int NV> __device__ __forceinline__ void column_sums(float (&v)[NV], const NormArgs& p, float* room) {
+  const int t = threadIdx.x, T = blockDim.x;
+  const bool live = t < p.rt * p.npc;
+  if (p.pow2) {       // lanes of one column lie npc apart
+    for (int s = p.npc; s < 64; s <<= 1)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) v[i] += __shfl_xor(v[i], s);
+    if (T > 64) {
+      const int lane = t & 63, width = p.npc * NV;
+      __syncthreads();
+      if (lane < p.npc)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) room[(t >> 6) * width + lane * NV + i] = v[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NV; ++i) v[i] = 0.f;
+      for (int w = 0; w < T / 64; ++w)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] += room[w * width + (lane & (p.npc - 1)) * NV + i];
+    }
+    return;
+  }
+  const int row = t / p.npc, at = t * NV;     // (thread t is row t / npc, column t % npc)
+  __syncthreads();
+  if (live)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) room[at + i] = v[i];
+  __syncthreads();
+  for (int n = p.rt; n > 1;) {
+    const int h = (n + 1) / 2;
+    if (live && row < n - h)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) room[at + i] += room[at + h * p.npc * NV + i];
+    __syncthreads();
+    n = h;
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) v[i] = live ? room[(t % p.npc) * NV + i] : 0.f;
+}
+// Of GV segments of a thread's piece (their column sums) the sums of their groups.  room: npc GV floats
+template <int GV> __device__ __forceinline__ void group_sums(float (&v)[GV], const NormArgs& p, float* room) {
+  if (p.spg == 1) return;
+  const int col = threadIdx.x % p.npc;
+  __syncthreads();
+  if ((int)threadIdx.x < p.npc)
+#pragma unroll
+    for (int i = 0; i < GV; ++i) room[col * GV + i] = v[i];
+  __syncthreads();
+  const int segments = p.slab / p.cg * p.spg;
+#pragma unroll
+  for (int i = 0; i < GV; ++i) {
+    const int seg = col * GV + i, g0 = seg / p.spg * p.spg;
+    float s = 0.f;
+    if (seg < segments)
+      for (int k = 0; k < p.spg; ++k) s += room[g0 + k];
+    v[i] = s;
+  }
+}
+
+// A unit of work: an image's slab, or its piece of pixels
+struct Unit { int image, slab, part, first, last; };
+__device__ __forceinline__ Unit unit_of(const NormArgs& p, int u) {
+  Unit w;
+  const int per = p.slabs * p.chunks;
+  w.image = u / per;
+  const int rest = u - w.image * per;
+  w.slab = rest / p.chunks;
+  w.part = rest - w.slab * p.chunks;
+  w.first = w.part * p.chunk;
+  w.last = min(p.pixels, w.first + p.chunk);
+  return w;
+}
+
+// A thread's pieces of a map: piece i is pixel `first` + row + i rt of an image.  The address is a uniform one and 32 bits a thread (rows lie
+// 2^20 elements apart at most, and a workgroup has 512 of them).  VEC: channels come in eights, so every piece is whole.
+template <int DT, bool VEC> struct Map {
+  static constexpr int ESZ = DT == BF16 ? 2 : 4;
+  char* base;
+  int64_t step;
+  uint32_t at;
+  int c, cols;
+  __device__ __forceinline__ void init(const void* p, int64_t ld, int64_t pixel, int c0, int row, int c_, int cols_, int rt) {
+    base = (char*)p + (pixel * ld + c0) * ESZ;
+    step = rt * ld * ESZ;
+    c = c_; cols = cols_;
+    at = ((uint32_t)row * (uint32_t)ld + (VEC ? c : 0)) * ESZ;
+  }
+  __device__ __forceinline__ void load(Eight<DT>& x, int i) const {
+    if (VEC) x.load_all(base + i * step + at);
+    else x.load(base + i * step + at, c, cols);
+  }
+  __device__ __forceinline__ void store(const Eight<DT>& x, int i) const {
+    if (VEC) x.store_all(base + i * step + at);
+    else x.store(base + i * step + at, c, cols);
+  }
+};
+
+// How the work is laid out: an image (slab) a workgroup where its pieces find room in the registers of one, else pieces of pixels: `chunk` of them
+// where they are held (the forward's statistics), `stretch` where they pass by
+struct Layout { int slab, threads, mi, chunk, stretch; bool whole; };
+constexpr int MOST_THREADS = 512;
+inline int most_mi(int dt) { return dt == BF16 ? 8 : 4; }
+inline int piece_columns(int channels) { return (channels + 7) / 8; }
+inline Layout layout_of(const GroupNorm& g) {
+  Layout l{};
+  const int size = g.dt == BF16 ? 2 : 4;
+  // slabs of whole groups whose rows of a pixel are whole pieces and 64 bytes or more; the widest that fits
+  for (int n = 1; n <= g.groups && !l.whole; ++n) {
+    if (g.groups % n) continue;
+    const int slab = g.channels / n;
+    if (n > 1 && (slab % 8 || slab * size < 64)) continue;
+    if (g.pixels <= (int64_t)(MOST_THREADS / piece_columns(slab)) * most_mi(g.dt)) { l.whole = true; l.slab = slab; }
+  }
+  if (!l.whole) l.slab = g.channels;
+  const int npc = piece_columns(l.slab);
+  const int64_t pieces = (int64_t)g.pixels * npc;
+  l.threads = 64;
+  if (l.whole) {
+    while (l.threads < MOST_THREADS && (l.threads < npc || 2 * pieces > most_mi(g.dt) * (int64_t)l.threads)) l.threads *= 2;
+    const int rt = l.threads / npc;
+    l.mi = (int)(((int64_t)g.pixels + rt - 1) / rt);
+    l.chunk = l.stretch = g.pixels;
+  } else {
+    l.threads = MOST_THREADS;
+    const int rt = l.threads / npc;
+    l.mi = most_mi(g.dt);
+    l.chunk = rt * l.mi;
+    // some 2048 workgroups, none under eight pieces a thread
+    const int64_t per_image = std::max<int64_t>(1, 2048 / g.images), even = ((int64_t)g.pixels + per_image - 1) / per_image;
+    l.stretch = (int)std::max<int64_t>((even + rt - 1) / rt, 8) * rt;
+  }
+  return l;
+}
+inline int chunks_of(const GroupNorm& g, int chunk) { return (int)(((int64_t)g.pixels + chunk - 1) / chunk); }
+
+inline NormArgs args_of(const GroupNorm& g, const Layout& l, int chunk) {
+  NormArgs p{};
+  p.images = g.images; p.pixels = g.pixels; p.C = g.channels; p.groups = g.groups; p.cg = g.channels / g.groups; p.act = g.activation; p.eps = g.eps;
+  p.slab = l.slab; p.slabs = g.channels / l.slab; p.npc = piece_columns(l.slab); p.rt = l.threads / p.npc;
+  p.pow2 = p.npc <= 64 && (p.npc & (p.npc - 1)) == 0;
+  p.chunk = chunk; p.chunks = chunks_of(g, chunk);
+  return p;
+}
+inline int segments_of(int cg) { return cg % 8 == 0 ? 1 : cg == 4 ? 2 : cg == 2 ? 4 : 8; }
+inline unsigned grid_of(const NormArgs& p) { return (unsigned)std::min<int64_t>((int64_t)p.images * p.slabs * p.chunks, MOST_BLOCKS); }
+
+}  // namespace norm
+}  // namespace ppll

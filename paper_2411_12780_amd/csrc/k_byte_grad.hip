@@ -16,6 +16,7 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr int BM = 128, BN = 128, THREADS = 256, PITCH = 320;      // PITCH: bytes between k rows of a [k][row] tile (free of bank conflicts)
 constexpr int STAGE_LD = BN + 4;
@@ -78,16 +79,10 @@ __device__ __forceinline__ void shift_down(Eight<F32>& x, int by) {
     for (int i = 0; i < 8; ++i) v[i] = by & s ? (i + s < 8 ? v[i + s] : 0.f) : v[i];
   x.set(v);
 }
-// Elements c .. c + 7 of a row of `cols`, zeros from `cols` on; c may be any
-template <int DT, bool RAGGED> __device__ __forceinline__ void load_eight(Eight<DT>& x, const char* row, int c, int cols) {
-  if (RAGGED && cols < 8) {
-    x.zero();
-    if (c < cols) x.load(row, c, cols);
-    return;
-  }
-  const int at = min(c, cols - 8);
-  __builtin_memcpy(&x, row + (int64_t)at * (DT == BF16 ? 2 : 4), sizeof x);
-  if (RAGGED) shift_down(x, min(c - at, 7));       // (c beyond the row: its last element may come, which no sum that is kept meets)
+// Elements c .. c + 7 of a row of fewer than 8
+template <int DT> __device__ __forceinline__ void load_few(Eight<DT>& x, const char* row, int c, int cols) {
+  x.zero();
+  if (c < cols) x.load(row, c, cols);
 }
 
 template <int DT> struct Regs {
@@ -121,19 +116,47 @@ __global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
   const int rk = (tid & (BK / 8 - 1)) * 8, rr = tid / (BK / 8);                   // [row][k]: rows rr + 2048 / BK j, k rk ..
   constexpr int RSTEP = THREADS / (BK / 8);
   const int qc = min((DX ? n0 : m0) + tc, p.qcols - 8);
-  const int8_t* qbase = p.q + qc;
+  const uint32_t q_at = (uint32_t)tk * (uint32_t)p.ldq + qc;
+  // Stage i: k from kbeg + i BK.  Where all of its k are there, addresses are a uniform one and the thread's 32 bits; else k rows stop at the last
+  // one (and its values are dropped on the way to LDS).
+  const int d_col = DX ? 0 : n0 + tc, d_from = RAGGED ? max(min(d_col, p.dcols - 8), 0) : min(d_col, p.dcols - 8);
+  const uint32_t d_at = DX ? 0 : ((uint32_t)tk * (uint32_t)p.ldd + d_from) * ESZ;
+  const char* d_base = DX ? p.d + (int64_t)m0 * p.ldd * ESZ : nullptr;
+  uint32_t d_row[NP];
+  if (DX) {
+#pragma unroll
+    for (int j = 0; j < NP; ++j) d_row[j] = (uint32_t)min(rr + RSTEP * j, p.M - 1 - m0) * (uint32_t)p.ldd * ESZ;
+  }
+  auto whole = [&](int i) { return kbeg + (i + 1) * BK <= kend; };
   auto gload = [&](int i, Regs<DT>& r) {
     const int k0 = kbeg + i * BK;
+    if (whole(i)) {
 #pragma unroll
-    for (int j = 0; j < NP; ++j) {
-      const int k = min(k0 + tk + 16 * j, p.K - 1);
-      r.q[j] = *(const uint2*)(qbase + k * p.ldq);
-      r.e[j] = p.e[k];
-      if (DX) {
-        const int m = min(m0 + rr + RSTEP * j, p.M - 1);
-        load_eight<DT, RAGGED>(r.d[j], p.d + m * p.ldd * ESZ, k0 + rk, p.dcols);
-      } else {
-        load_eight<DT, RAGGED>(r.d[j], p.d + k * p.ldd * ESZ, n0 + tc, p.dcols);
+      for (int j = 0; j < NP; ++j) {
+        r.q[j] = *(const uint2*)(p.q + (int64_t)(k0 + 16 * j) * p.ldq + q_at);
+        r.e[j] = (p.e + k0 + 16 * j)[(uint32_t)tk];
+        if (!DX) {
+          if (RAGGED && p.dcols < 8) load_few<DT>(r.d[j], p.d + (int64_t)(k0 + 16 * j + tk) * p.ldd * ESZ, d_col, p.dcols);
+          else r.d[j].load_all(p.d + (int64_t)(k0 + 16 * j) * p.ldd * ESZ + d_at);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        const int64_t k = min(k0 + tk + 16 * j, p.K - 1);
+        r.q[j] = *(const uint2*)(p.q + k * p.ldq + qc);
+        r.e[j] = p.e[k];
+        if (!DX) {
+          if (RAGGED && p.dcols < 8) load_few<DT>(r.d[j], p.d + k * p.ldd * ESZ, d_col, p.dcols);
+          else r.d[j].load_all(p.d + (k * p.ldd + d_from) * ESZ);
+        }
+      }
+    }
+    if (DX) {
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        if (RAGGED && p.dcols < 8) load_few<DT>(r.d[j], d_base + d_row[j], k0 + rk, p.dcols);
+        else r.d[j].load_all(d_base + (d_row[j] + (uint32_t)min(k0 + rk, p.dcols - 8) * ESZ));
       }
     }
   };
@@ -144,16 +167,23 @@ __global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
     if (j >= NP) return;
     char* st = smem + stage * STAGE;
     const int k0 = kbeg + i * BK;
-    const bool in = k0 + tk + 16 * j < kend;
+    const bool full = whole(i);
     float f[8];
     bytes_get(r.q[j], byte_step(r.e[j]), f);
     Eight<BF16> x;
     x.set(f);
-    if (!in) x.zero();
-    *(uint4*)(st + (tk + 16 * j) * PITCH + tc * 2) = x.w;
     Eight<DT> d = r.d[j];
-    // dX: k from dcols on is beyond the row where the row is ragged, and zero; elsewhere a piece is in or out as a whole
-    if (DX ? k0 + rk >= kend : !in) d.zero();
+    if (!full) {
+      if (k0 + tk + 16 * j >= kend) x.zero();
+      if (DX ? k0 + rk >= kend : k0 + tk + 16 * j >= kend) d.zero();
+    }
+    // a piece that goes over its row's end was read ending there.  (One beyond the end keeps its last element, which no sum that is kept meets; in dX
+    // it is zero already.)
+    if (RAGGED && p.dcols >= 8 && (DX ? !full : n0 + BN > p.dcols)) {
+      const int c = DX ? k0 + rk : d_col;
+      shift_down(d, min(c - min(c, p.dcols - 8), 7));
+    }
+    *(u32x4*)(st + (tk + 16 * j) * PITCH + tc * 2) = (u32x4){x.w.x, x.w.y, x.w.z, x.w.w};
     if (do_db) {
       float v[8];
       d.get(v);
@@ -162,12 +192,12 @@ __global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
     }
     char* to = st + QB + (DX ? row_major<BK>(rr + RSTEP * j, rk >> 3) : (tk + 16 * j) * PITCH + tc * 2);
     if constexpr (DT == BF16) {
-      *(uint4*)to = d.w;
+      *(u32x4*)to = (u32x4){d.w.x, d.w.y, d.w.z, d.w.w};
     } else {
       uint4 w[3];
       split(d, w);
 #pragma unroll
-      for (int s = 0; s < 3; ++s) *(uint4*)(to + s * DB) = w[s];
+      for (int s = 0; s < 3; ++s) *(u32x4*)(to + s * DB) = (u32x4){w[s].x, w[s].y, w[s].z, w[s].w};
     }
   };
   const int tr_lane = (8 * (lane >> 5) + ((lane & 15) >> 2)) * PITCH + (16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
@@ -234,8 +264,21 @@ __global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
     multiply(0, i, r[1], false);
   }
 
-  // Epilogue through LDS: a thread takes 8 consecutive columns of a row
+  // Epilogue through LDS: a thread takes 8 consecutive columns of a row; the gate is on its way meanwhile
   float* tile = reinterpret_cast<float*>(smem);
+  const int n = n0 + tc;
+  const bool vec = (p.N & 7) == 0;
+  Eight<DT> gate[DX ? BM / 16 : 1];
+  if (DX && p.gate) {
+#pragma unroll
+    for (int j = 0; j < BM / 16; ++j) {
+      const int64_t m = m0 + tk + 16 * j;
+      gate[j].zero();
+      if (m >= p.M || n >= p.N) continue;
+      if (vec) gate[j].load_all(p.gate + (m * p.ldg + n) * ESZ);
+      else gate[j].load(p.gate + m * p.ldg * ESZ, n, p.N);
+    }
+  }
   __syncthreads();
 #pragma unroll
   for (int jn = 0; jn < 2; ++jn)
@@ -246,31 +289,29 @@ __global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
         *reinterpret_cast<float4*>(tile + (wm * 64 + im * 32 + (lane & 31)) * STAGE_LD + wn * 64 + jn * 32 + 8 * q + 4 * (lane >> 5)) =
             make_float4(acc[jn][im][4 * q], acc[jn][im][4 * q + 1], acc[jn][im][4 * q + 2], acc[jn][im][4 * q + 3]);
   __syncthreads();
-  const int n = n0 + tc;
-  if (n < p.N) {
 #pragma unroll
-    for (int j = 0; j < BM / 16; ++j) {
-      const int64_t m = m0 + tk + 16 * j;
-      if (m >= p.M) continue;
-      const float4 lo = *reinterpret_cast<const float4*>(tile + (tk + 16 * j) * STAGE_LD + tc), hi = *reinterpret_cast<const float4*>(tile + (tk + 16 * j) * STAGE_LD + tc + 4);
-      float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-      if (DX) {
-        if (p.gate) {
-          Eight<DT> g;
-          float f[8];
-          g.load(p.gate + m * p.ldg * ESZ, n, p.N);
-          g.get(f);
+  for (int j = 0; j < BM / 16; ++j) {
+    const int64_t m = m0 + tk + 16 * j;
+    if (m >= p.M || n >= p.N) continue;
+    const float4 lo = *reinterpret_cast<const float4*>(tile + (tk + 16 * j) * STAGE_LD + tc), hi = *reinterpret_cast<const float4*>(tile + (tk + 16 * j) * STAGE_LD + tc + 4);
+    float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    if (DX) {
+      if (p.gate) {
+        float f[8];
+        gate[j].get(f);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] *= f[e];
-        }
-        Eight<DT> o;
-        o.set(v);
-        o.store(p.out + m * p.ldo * ESZ, n, p.N);
-      } else {
-        Eight<F32> o;
-        o.set(v);
-        o.store(p.out + (part * p.part_out + m * p.ldo) * 4, n, p.N);
+        for (int e = 0; e < 8; ++e) v[e] *= f[e];
       }
+      Eight<DT> o;
+      o.set(v);
+      if (vec) o.store_all(p.out + (m * p.ldo + n) * ESZ);
+      else o.store(p.out + m * p.ldo * ESZ, n, p.N);
+    } else {
+      Eight<F32> o;
+      o.set(v);
+      float* row = (float*)p.out + part * p.part_out + m * p.ldo;
+      if (vec) o.store_all((char*)(row + n));
+      else o.store(row, n, p.N);
     }
   }
   if (do_db) {
@@ -341,12 +382,12 @@ template <bool DX, int DT> int launch(hipStream_t s, GradArgs& p) {
   return PPLL_OK;
 }
 
-// Into how many parts the reduction of dW goes: two workgroups a unit, none under four steps
+// Into how many parts the reduction of dW goes: a workgroup a unit, none under four steps
 struct Parts { int n, k; int64_t out; };
 Parts parts_of(const ByteLinear& l) {
   const int bk = l.dt == F32 ? step_k<F32>() : step_k<BF16>();
   const int64_t tiles = (int64_t)((l.in + BM - 1) / BM) * ((l.out + BN - 1) / BN), steps = ((int64_t)l.rows + bk - 1) / bk;
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / 4));
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, steps / 4));
   const int64_t each = (steps + want - 1) / want;
   Parts p;
   p.n = (int)std::max<int64_t>(1, (steps + each - 1) / each);

@@ -20,40 +20,53 @@ struct ByteArgs {
   int64_t ldy, lds, ldr;            // elements
   const float* bias;
   int M, N, K;                      // K in pairs of bytes, padded
-  bool gelu;
+  bool gelu, vec;                   // vec: rows of y, slope and residual in pieces of 16 bytes
   TileMap map;
   int helpers;
 };
 
 // What eight sums of a row become, columns n .. n + 7
-template <int DT> __device__ __forceinline__ void byte_end(const ByteArgs& p, int64_t m, int n, int row_exp, const int (&col_exp)[8], const float (&bias)[8],
-                                                           const int (&sum)[8], const Eight<DT>& res) {
-  const bool nan = row_exp == BYTE_NAN;
-  float v[8], dg[8], r[8];
+template <int DT, bool VEC> __device__ __forceinline__ void byte_end(const ByteArgs& p, int64_t m, int n, int row_exp, const int (&col_exp)[8], const float (&bias)[8],
+                                                                     const int (&sum)[8], const Eight<DT>& res) {
+  constexpr int ESZ = DT == BF16 ? 2 : 4;
+  auto put = [&](char* to, int64_t ld, const float (&v)[8]) {
+    Eight<DT> o;
+    o.set(v);
+    char* row = to + m * ld * ESZ;
+    if (VEC) {
+      if constexpr (DT == BF16) {
+        store_through(row + n * ESZ, o.w);
+      } else {
+        store_through(row + n * ESZ, __builtin_bit_cast(uint4, o.a));
+        store_through(row + n * ESZ + 16, __builtin_bit_cast(uint4, o.b));
+      }
+    } else {
+      o.store(row, n, p.N);
+    }
+  };
+  float v[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = (nan ? __uint_as_float(0x7fc00000u) : ldexpf((float)sum[i], row_exp + col_exp[i])) + bias[i];
+  for (int i = 0; i < 8; ++i) v[i] = ldexpf((float)sum[i], row_exp + col_exp[i]) + bias[i];
+  if (row_exp == BYTE_NAN)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7fc00000u);
   if (p.residual) {
+    float r[8];
     res.get(r);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += r[i];
   }
-  constexpr int ESZ = DT == BF16 ? 2 : 4;
   if (p.gelu) {
+    float dg[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       float cdf, pdf;
       cdf_pdf(v[i], cdf, pdf);
       dg[i] = cdf + v[i] * pdf; v[i] *= cdf;
     }
-    if (p.slope) {
-      Eight<DT> o;
-      o.set(dg);
-      o.store(p.slope + m * p.lds * ESZ, n, p.N);
-    }
+    if (p.slope) put(p.slope, p.lds, dg);
   }
-  Eight<DT> o;
-  o.set(v);
-  o.store(p.y + m * p.ldy * ESZ, n, p.N);
+  put(p.y, p.ldy, v);
 }
 // Exponents and biases of columns n .. n + 7; a channel of NaN has a bias of NaN
 __device__ __forceinline__ void columns_of(const ByteArgs& p, int n, int (&exps)[8], float (&bias)[8]) {
@@ -66,7 +79,7 @@ __device__ __forceinline__ void columns_of(const ByteArgs& p, int n, int (&exps)
   }
 }
 
-template <int DT, int WGM, int WGN, int IM, int NS, int KT>
+template <int DT, bool VEC, int WGM, int WGN, int IM, int NS, int KT>
 __global__ __launch_bounds__((Shape<false, false, WGM, WGN, IM, NS, KT>::THREADS), 2) void byte_linear_kernel(ByteArgs p) {
   using S = Shape<false, false, WGM, WGN, IM, NS, KT>;
   constexpr int JN = 2, ESZ = DT == BF16 ? 2 : 4;
@@ -132,12 +145,15 @@ __global__ __launch_bounds__((Shape<false, false, WGM, WGN, IM, NS, KT>::THREADS
       const bool in = m < p.M && n < p.N;
       res[q].zero();
       ex[q] = in ? p.ex[m] : 0;
-      if (in && p.residual) res[q].load(p.residual + m * p.ldr * ESZ, n, p.N);
+      if (in && p.residual) {
+        if (VEC) res[q].load_all(p.residual + (m * p.ldr + n) * ESZ);
+        else res[q].load(p.residual + m * p.ldr * ESZ, n, p.N);
+      }
     }
 #pragma unroll
     for (int q = 0; q < NP; ++q) {
       const int64_t m = mw + im * 32 + q * RPP + r0;
-      if (m < p.M && n < p.N) byte_end<DT>(p, m, n, ex[q], exps, bias, sums[q], res[q]);
+      if (m < p.M && n < p.N) byte_end<DT, VEC>(p, m, n, ex[q], exps, bias, sums[q], res[q]);
     }
   }
 }
@@ -192,11 +208,11 @@ __global__ __launch_bounds__(64 * FW) void byte_linear_rows_kernel(ByteArgs p) {
     Eight<DT> res;
     res.zero();
     if (p.residual) res.load(p.residual + m * p.ldr * ESZ, n, p.N);
-    byte_end<DT>(p, m, n, p.ex[m], exps, bias, sum, res);
+    byte_end<DT, false>(p, m, n, p.ex[m], exps, bias, sum, res);
   }
 }
 
-template <int DT, int WGM, int WGN, int IM, int NS, int KT> int byte_launch(hipStream_t s, ByteArgs& p, int units) {
+template <int DT, bool VEC, int WGM, int WGN, int IM, int NS, int KT> int byte_launch_as(hipStream_t s, ByteArgs& p, int units) {
   using S = Shape<false, false, WGM, WGN, IM, NS, KT>;
   if (S::COPY_WAVES) {
     p.map = tile_map(p.M, p.N, S::BM, S::BN, units);
@@ -205,16 +221,32 @@ template <int DT, int WGM, int WGN, int IM, int NS, int KT> int byte_launch(hipS
     p.map = TileMap{tiles_m, tiles_n, (int)(((long)tiles_m * tiles_n + 7) / 8), 0, 0, 0, false};
   }
   static OncePerDevice once;
-  PPLL_TRY(raise_lds((const void*)byte_linear_kernel<DT, WGM, WGN, IM, NS, KT>, S::LDS, once));
-  hipLaunchKernelGGL((byte_linear_kernel<DT, WGM, WGN, IM, NS, KT>), dim3(8 * p.map.per_xcd), dim3(S::THREADS), S::LDS, s, p);
+  PPLL_TRY(raise_lds((const void*)byte_linear_kernel<DT, VEC, WGM, WGN, IM, NS, KT>, S::LDS, once));
+  hipLaunchKernelGGL((byte_linear_kernel<DT, VEC, WGM, WGN, IM, NS, KT>), dim3(8 * p.map.per_xcd), dim3(S::THREADS), S::LDS, s, p);
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }
 
+template <int DT, int WGM, int WGN, int IM, int NS, int KT> int byte_launch(hipStream_t s, ByteArgs& p, int units) {
+  return p.vec ? byte_launch_as<DT, true, WGM, WGN, IM, NS, KT>(s, p, units) : byte_launch_as<DT, false, WGM, WGN, IM, NS, KT>(s, p, units);
+}
+
 constexpr int FEW_ROWS = 64;
 
-template <int DT> int forward(hipStream_t s, ByteArgs& p) {
-  if (p.M <= FEW_ROWS) {
+// Which kernel a product goes to: 1 few rows, 3 tiles of 128 x 128 with copying waves, 4 / 8 / 10 tiles of 128 / 256 / 320 rows of 256 columns
+int choice(const ByteArgs& p, int units) {
+  if (p.M <= FEW_ROWS) return 1;
+  const ProductEnd end = p.gelu ? END_GELU : p.residual ? END_RESIDUAL : END_BIAS;
+  const long tiles = (long)((p.M + 127) / 128) * ((p.N + 127) / 128);
+  if (tiles <= units) return 3;
+  const int wide = wide_tile_rows(p.M, p.N, p.K, end, units), alone = unit_tile_rows(p.M, p.N, p.K, end, wide, units);
+  const int im = alone ? alone : wide;
+  return im == 5 ? 4 : im ? im : 3;
+}
+template <int DT> int forward(hipStream_t s, ByteArgs& p, int kernel) {
+  const int units = compute_units() > 0 ? compute_units() : 256;
+  if (!kernel) kernel = choice(p, units);
+  if (kernel == 1) {
     const int rt = p.M <= 16 ? 1 : 2;
     const dim3 grid((p.N + 15) / 16, (p.M + 16 * rt - 1) / (16 * rt));
     if (rt == 1) hipLaunchKernelGGL((byte_linear_rows_kernel<DT, 1>), grid, dim3(64 * FW), 0, s, p);
@@ -222,22 +254,13 @@ template <int DT> int forward(hipStream_t s, ByteArgs& p) {
     PPLL_HIP(hipGetLastError());
     return PPLL_OK;
   }
-  const int units = compute_units() > 0 ? compute_units() : 256;
-  const ProductEnd end = p.gelu ? END_GELU : p.residual ? END_RESIDUAL : END_BIAS;
-  const long tiles = (long)((p.M + 127) / 128) * ((p.N + 127) / 128);
-  if (tiles > units) {
-    const int wide = wide_tile_rows(p.M, p.N, p.K, end, units), alone = unit_tile_rows(p.M, p.N, p.K, end, wide, units);
-    const int im = alone ? alone : wide;
-    if (im == 4 || im == 5) return byte_launch<DT, 1, 4, 4, 3, 32>(s, p, units);
-    if (im == 8) return byte_launch<DT, 2, 4, 4, 2, 64>(s, p, units);
-    if (im == 10) return byte_launch<DT, 2, 4, 5, 2, 64>(s, p, units);
-  }
+  if (kernel == 4) return byte_launch<DT, 1, 4, 4, 3, 32>(s, p, units);
+  if (kernel == 8) return byte_launch<DT, 2, 4, 4, 2, 64>(s, p, units);
+  if (kernel == 10) return byte_launch<DT, 2, 4, 5, 2, 64>(s, p, units);
   return byte_launch<DT, 2, 2, 2, 4, 64>(s, p, units);
 }
-}  // namespace
-
-int launch_byte_linear_fwd(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const float* bias, const ppll_rows& residual,
-                           const ppll_rows& y, const ppll_rows& slope) {
+int product(hipStream_t s, int kernel, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const float* bias, const ppll_rows& residual,
+            const ppll_rows& y, const ppll_rows& slope) {
   if (l.rows <= 0) return PPLL_OK;
   ByteArgs p{};
   p.x = x.q; p.ex = x.e; p.ldx = x.ld; p.w = w.q; p.ew = w.e; p.ldw = w.ld;
@@ -245,6 +268,26 @@ int launch_byte_linear_fwd(hipStream_t s, const ByteLinear& l, const ppll_byte_r
   p.bias = bias;
   p.M = l.rows; p.N = l.out; p.K = pad16(l.in) / 2;
   p.gelu = l.activation == PPLL_ACT_GELU;
-  return l.dt == BF16 ? forward<BF16>(s, p) : forward<F32>(s, p);
+  const int each = l.dt == BF16 ? 8 : 4;
+  auto whole = [&](const ppll_rows& r) { return !r.p || (r.ld % each == 0 && ((uintptr_t)r.p & 15) == 0); };
+  p.vec = l.out % 8 == 0 && whole(y) && whole(slope) && whole(residual);
+  return l.dt == BF16 ? forward<BF16>(s, p, kernel) : forward<F32>(s, p, kernel);
 }
+}  // namespace
+
+int launch_byte_linear_fwd(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const float* bias, const ppll_rows& residual,
+                           const ppll_rows& y, const ppll_rows& slope) {
+  return product(s, 0, l, x, w, bias, residual, y, slope);
+}
+
 }  // namespace ppll
+
+// One product on one kernel (choice() above), for tests of a kernel against another (no part of the public interface)
+extern "C" int ppll_internal_byte_linear(int kernel, int precision, int rows, int in, int out, int gelu, const ppll_byte_rows* x, const ppll_byte_rows* w,
+                                         const float* bias, const ppll_rows* residual, const ppll_rows* y, const ppll_rows* slope, void* stream) {
+  using namespace ppll;
+  if (kernel != 1 && kernel != 3 && kernel != 4 && kernel != 8 && kernel != 10) { set_error("there is no kernel %d", kernel); return PPLL_ERR_CONFIG; }
+  const ppll_rows none{nullptr, 0};
+  return product((hipStream_t)stream, kernel, {precision == PPLL_BF16 ? BF16 : F32, rows, in, out, gelu ? PPLL_ACT_GELU : PPLL_ACT_NONE}, *x, *w, bias,
+                 residual ? *residual : none, *y, slope ? *slope : none);
+}

@@ -25,6 +25,13 @@ int check_rows(const ppll_rows* r, int cols, int32_t precision, const char* what
   return PPLL_OK;
 }
 int check_maybe(const ppll_rows* r, int cols, int32_t precision, const char* what) { return r ? check_rows(r, cols, precision, what) : PPLL_OK; }
+// rows of a linear layer, pixels of a map
+int check_map(const ppll_rows* r, int cols, int32_t precision, const char* what) {
+  PPLL_TRY(check_rows(r, cols, precision, what));
+  if (r->ld > MAP_LD) { set_error("rows of %s more than 2^20 elements apart", what); return PPLL_ERR_SHAPE; }
+  return PPLL_OK;
+}
+int check_maybe_map(const ppll_rows* r, int cols, int32_t precision, const char* what) { return r ? check_map(r, cols, precision, what) : PPLL_OK; }
 int check_bytes(const ppll_byte_rows* r, int cols, const char* what) {
   if (!r || !r->q || !r->e) { set_error("%s is null", what); return PPLL_ERR_NULL; }
   if (!aligned(r->q, 16)) { set_error("%s is not 16-byte aligned", what); return PPLL_ERR_SHAPE; }
@@ -121,9 +128,9 @@ int ppll_byte_linear_forward(const ppll_byte_linear_config* cfg, const ppll_byte
   PPLL_TRY(check_bytes(x, l.in, "x"));
   PPLL_TRY(check_bytes(w, l.in, "w"));
   if (bias_dev) PPLL_TRY(check_floats(bias_dev, "bias_dev"));
-  PPLL_TRY(check_maybe(residual, l.out, cfg->precision, "residual"));
-  PPLL_TRY(check_rows(y, l.out, cfg->precision, "y"));
-  PPLL_TRY(check_maybe(slope, l.out, cfg->precision, "slope"));
+  PPLL_TRY(check_maybe_map(residual, l.out, cfg->precision, "residual"));
+  PPLL_TRY(check_map(y, l.out, cfg->precision, "y"));
+  PPLL_TRY(check_maybe_map(slope, l.out, cfg->precision, "slope"));
   return launch_byte_linear_fwd((hipStream_t)hip_stream, l, *x, *w, bias_dev, given(residual), *y, given(slope));
 }
 
@@ -145,10 +152,10 @@ int ppll_byte_linear_backward(const ppll_byte_linear_config* cfg, const ppll_byt
   if (!dx && gate) { set_error("gate goes with dx"); return PPLL_ERR_NULL; }
   if (l.rows) {
     if (!dx && !dw_dev && !db_dev) return PPLL_OK;
-    PPLL_TRY(check_rows(dy, l.out, cfg->precision, "dy"));
+    PPLL_TRY(check_map(dy, l.out, cfg->precision, "dy"));
     if (dx) {
-      PPLL_TRY(check_rows(dx, l.in, cfg->precision, "dx"));
-      PPLL_TRY(check_maybe(gate, l.in, cfg->precision, "gate"));
+      PPLL_TRY(check_map(dx, l.in, cfg->precision, "dx"));
+      PPLL_TRY(check_maybe_map(gate, l.in, cfg->precision, "gate"));
       PPLL_TRY(check_bytes(w, l.in, "w"));
     }
     if (dw_dev) PPLL_TRY(check_bytes(x, l.in, "x"));
@@ -171,11 +178,11 @@ int ppll_group_norm_forward(const ppll_group_norm_config* cfg, const ppll_rows* 
   GroupNorm g;
   PPLL_TRY(norm_of(cfg, &g));
   if (!g.images) return PPLL_OK;
-  PPLL_TRY(check_rows(x, g.channels, cfg->precision, "x"));
+  PPLL_TRY(check_map(x, g.channels, cfg->precision, "x"));
   PPLL_TRY(check_floats(scale_dev, "scale_dev"));
   PPLL_TRY(check_floats(shift_dev, "shift_dev"));
-  PPLL_TRY(check_maybe(residual, g.channels, cfg->precision, "residual"));
-  PPLL_TRY(check_rows(y, g.channels, cfg->precision, "y"));
+  PPLL_TRY(check_maybe_map(residual, g.channels, cfg->precision, "residual"));
+  PPLL_TRY(check_map(y, g.channels, cfg->precision, "y"));
   if (stats_dev) PPLL_TRY(check_floats(stats_dev, "stats_dev"));
   if (keep) PPLL_TRY(check_bytes(keep, g.channels, "keep"));
   PPLL_TRY(check_workspace(workspace_dev, workspace_bytes, group_norm_workspace(g)));
@@ -194,15 +201,15 @@ int ppll_group_norm_backward(const ppll_group_norm_config* cfg, const ppll_rows*
   if (g.images) {
     if (x && x_bytes) { set_error("x is given twice"); return PPLL_ERR_SHAPE; }
     if (x_bytes) PPLL_TRY(check_bytes(x_bytes, g.channels, "x_bytes"));
-    else PPLL_TRY(check_rows(x, g.channels, cfg->precision, "x"));
+    else PPLL_TRY(check_map(x, g.channels, cfg->precision, "x"));
     PPLL_TRY(check_floats(stats_dev, "stats_dev"));
     PPLL_TRY(check_floats(scale_dev, "scale_dev"));
     PPLL_TRY(check_floats(shift_dev, "shift_dev"));
-    if (curved) PPLL_TRY(check_maybe(residual, g.channels, cfg->precision, "residual"));
-    if (relu) PPLL_TRY(check_rows(y, g.channels, cfg->precision, "y"));
-    PPLL_TRY(check_rows(dy, g.channels, cfg->precision, "dy"));
-    PPLL_TRY(check_rows(dx, g.channels, cfg->precision, "dx"));
-    PPLL_TRY(check_maybe(d_residual, g.channels, cfg->precision, "d_residual"));
+    if (curved) PPLL_TRY(check_maybe_map(residual, g.channels, cfg->precision, "residual"));
+    if (relu) PPLL_TRY(check_map(y, g.channels, cfg->precision, "y"));
+    PPLL_TRY(check_map(dy, g.channels, cfg->precision, "dy"));
+    PPLL_TRY(check_map(dx, g.channels, cfg->precision, "dx"));
+    PPLL_TRY(check_maybe_map(d_residual, g.channels, cfg->precision, "d_residual"));
     if (d_residual && d_residual->p == dx->p) { set_error("dx and d_residual are one buffer"); return PPLL_ERR_SHAPE; }
     PPLL_TRY(check_workspace(workspace_dev, workspace_bytes, group_norm_workspace(g)));
   }

@@ -3,6 +3,8 @@
 Tolerances.  Forward: the whole-number sum is exact, its conversion, bias and residual are a rounding each of fp32, GELU's normal CDF is within 1e-6
 (the rational approximation of erf within 1.5e-7, its exponential and reciprocal within a few 2^-22), the result a rounding of its type.  Backward:
 products of a bf16 (or its three terms) and a value of 7 bits are exact in fp32, sums of K of them are off by 2^-23 of the sum of magnitudes for each addition at most."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -53,10 +55,21 @@ def forward(l, gelu=False, residual=None, bias=True, slope=True):
     return y, s
 
 
-def check_forward(l, gelu=False, with_residual=False, bias=True):
+def forward_on(kernel, l, gelu, residual):
+    m, k, n = l.shape
+    y, s = l.empty(m, n), l.empty(m, n) if gelu else None
+    ref = lambda r: None if r is None else ctypes.byref(r)  # noqa: E731
+    status = P.lib().ppll_internal_byte_linear(kernel, P.BF16 if l.dtype == torch.bfloat16 else P.FP32, m, k, n, int(gelu), ref(l.bytes(l.x)),
+                                               ref(l.bytes(l.w)), ctypes.c_void_p(l.bias.data_ptr()), ref(rows(residual)), ref(rows(y)), ref(rows(s)),
+                                               ctypes.c_void_p(stream()))
+    assert status == 0, P.ppll_last_error()
+    return y, s
+
+
+def check_forward(l, gelu=False, with_residual=False, bias=True, kernel=None):
     m, _, n = l.shape
     residual = l.put(m, n) if with_residual else None
-    y, s = forward(l, gelu, residual, bias)
+    y, s = forward(l, gelu, residual, bias) if kernel is None else forward_on(kernel, l, gelu, residual)
     x, w = l.values()
     h = x @ w.T
     size = np.abs(h)
@@ -95,6 +108,15 @@ def test_forward(precision, dtype, size, gelu, residual):
 def test_forward_of_strided_rows(precision, dtype, size, place):
     check_forward(Layer(*size, dtype, seed=1, **place), True, True)
     check_forward(Layer(*size, dtype, seed=1, **place), False, False, bias=False)
+
+
+@pytest.mark.parametrize("precision,dtype", TYPES)
+@pytest.mark.parametrize("kernel", [1, 3, 4, 8, 10])
+@pytest.mark.parametrize("size,place", [((1, 16, 8), {}), ((130, 1, 9), dict(room=3)), ((321, 33, 264), {}), ((700, 200, 520), dict(room=8, shift=8)),
+                                        ((257, 513, 255), dict(room=1, shift=1)), ((640, 1000, 256), {})])
+def test_each_kernel(precision, dtype, kernel, size, place):
+    check_forward(Layer(*size, dtype, seed=2, **place), True, True, kernel=kernel)
+    check_forward(Layer(*size, dtype, seed=2, **place), kernel=kernel)
 
 
 @pytest.mark.parametrize("size", [(8320, 384, 1536), (20000, 200, 1536), (9000, 256, 264), (30000, 64, 768), (33000, 130, 512), (50000, 32, 256)])
