@@ -459,15 +459,11 @@ def rms_norm_bwd(dy, cache, g):
 def byte_rows(x):
     """Rows in 8 bits: whole numbers q and exponents e [rows] with row r about q[r] 2^e[r]; e the least of -126 .. 121 with max|x| <= 127 2^e."""
     x = np.asarray(x, dtype=np.float64)
-    q, e = np.zeros(x.shape), np.full(x.shape[0], -126)
-    for r, row in enumerate(x):
-        if not np.isfinite(row).all():
-            e[r] = -128
-            continue
-        while e[r] < 121 and np.abs(row).max() > 127 * 2.0 ** e[r]:
-            e[r] += 1
-        q[r] = np.clip(np.rint(row / 2.0 ** e[r]), -127, 127)        # (rint: ties to even)
-    return q, e
+    fine = np.isfinite(x).all(axis=1)
+    x = np.where(fine[:, None], x, 0)
+    e = np.searchsorted(127 * 2.0 ** np.arange(-126, 121), np.abs(x).max(axis=1)) - 126       # the first that is no smaller
+    q = np.clip(np.rint(x / 2.0 ** e[:, None].astype(np.float64)), -127, 127)                 # (rint: ties to even)
+    return q, np.where(fine, e, -128)
 
 
 def byte_values(q, e):

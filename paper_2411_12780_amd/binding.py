@@ -77,10 +77,10 @@ def _rows(t):
     """Address and row stride of a 2-d tensor whose last axis is contiguous."""
     if t is None:
         return None, 0
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+    stride = t.stride()
+    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1):
         raise PpllError(3, "queries and keys are 2-d tensors with a contiguous last axis")
-    return t.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], shape[1])
+    return t.data_ptr(), stride[0] if t.shape[0] > 1 else max(stride[0], t.shape[1])
 
 
 def queries_keys(q, k) -> QueriesKeys:
@@ -122,7 +122,8 @@ class ByteRows(C.Structure):
 
 def byte_rows(q, e) -> ByteRows:
     """An int8 tensor [rows, ld or a part of it] whose last axis is contiguous, and the rows' exponents, int8 [rows]."""
-    if (q.element_size(), e.element_size()) != (1, 1) or e.dim() != 1 or (e.shape[0] > 1 and e.stride(0) != 1):
+    step = e.stride()
+    if q.element_size() != 1 or e.element_size() != 1 or len(step) != 1 or (step[0] != 1 and e.shape[0] > 1):
         raise PpllError(3, "rows of 8 bits are an int8 tensor [rows, columns] and contiguous int8 exponents [rows]")
     p, ld = _rows(q)
     return ByteRows(p, e.data_ptr(), ld)
@@ -241,9 +242,10 @@ def _ptr(t) -> Optional[int]:
     """Device/host address of a torch tensor, numpy array, int or None."""
     if t is None or isinstance(t, int):
         return t
-    if isinstance(t, np.ndarray):
+    try:
+        return t.data_ptr()
+    except AttributeError:
         return t.ctypes.data
-    return t.data_ptr()
 
 
 def ppll_last_error() -> str:

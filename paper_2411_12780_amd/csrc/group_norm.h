@@ -62,43 +62,59 @@ template <bool EXACT, class F> __device__ __forceinline__ void with_activation(i
 
 // Sums of NV values over all threads of a piece column; every thread has its column's.  room: NV floats a thread
 template <int NV> __device__ __forceinline__ void column_sums(float (&v)[NV], const NormArgs& p, float* room) {
-  const int t = threadIdx.x, T = blockDim.x;
+  const int t = threadIdx.x, T = blockDim.x, width = p.npc * NV;
   const bool live = t < p.rt * p.npc;
-  if (p.pow2) {       // lanes of one column lie npc apart
-    for (int s = p.npc; s < 64; s <<= 1)
+  if (p.pow2) {
+    // lanes of one column lie npc apart; the far ones first, so that a rotation of 16 lanes brings what the lane across has (see lanes_reduce)
 #pragma unroll
-      for (int i = 0; i < NV; ++i) v[i] += __shfl_xor(v[i], s);
-    if (T > 64) {
-      const int lane = t & 63, width = p.npc * NV;
-      __syncthreads();
-      if (lane < p.npc)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) room[(t >> 6) * width + lane * NV + i] = v[i];
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < NV; ++i) v[i] = 0.f;
-      for (int w = 0; w < T / 64; ++w)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] += room[w * width + (lane & (p.npc - 1)) * NV + i];
+    for (int i = 0; i < NV; ++i) {
+      if (p.npc <= 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+      }
+      if (p.npc <= 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+      }
+      if (p.npc <= 8) v[i] += dpp_f<0x128>(v[i]);
+      if (p.npc <= 4) v[i] += dpp_f<0x124>(v[i]);
+      if (p.npc <= 2) v[i] += dpp_f<0x122>(v[i]);
+      if (p.npc <= 1) v[i] += dpp_f<0x121>(v[i]);
     }
+    if (T == 64) return;
+    const int lane = t & 63, col = lane & (p.npc - 1);
+    __syncthreads();
+    if (lane < p.npc)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) room[(t >> 6) * width + i * p.npc + lane] = v[i];
+    __syncthreads();
+    for (int j = t; j < width; j += T) {
+      float s = room[j];
+      for (int w = 1; w < T / 64; ++w) s += room[w * width + j];
+      room[j] = s;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = room[i * p.npc + col];
     return;
   }
-  const int row = t / p.npc, at = t * NV;     // (thread t is row t / npc, column t % npc)
+  const int row = t / p.npc, col = t % p.npc;
+  float* mine = room + row * width + col;
   __syncthreads();
   if (live)
 #pragma unroll
-    for (int i = 0; i < NV; ++i) room[at + i] = v[i];
+    for (int i = 0; i < NV; ++i) mine[i * p.npc] = v[i];
   __syncthreads();
   for (int n = p.rt; n > 1;) {
     const int h = (n + 1) / 2;
     if (live && row < n - h)
 #pragma unroll
-      for (int i = 0; i < NV; ++i) room[at + i] += room[at + h * p.npc * NV + i];
+      for (int i = 0; i < NV; ++i) mine[i * p.npc] += mine[h * width + i * p.npc];
     __syncthreads();
     n = h;
   }
 #pragma unroll
-  for (int i = 0; i < NV; ++i) v[i] = live ? room[(t % p.npc) * NV + i] : 0.f;
+  for (int i = 0; i < NV; ++i) v[i] = live ? room[i * p.npc + col] : 0.f;
 }
 // Of GV segments of a thread's piece (their column sums) the sums of their groups.  room: npc GV floats
 template <int GV> __device__ __forceinline__ void group_sums(float (&v)[GV], const NormArgs& p, float* room) {
@@ -162,6 +178,7 @@ template <int DT, bool VEC> struct Map {
 // where they are held (the forward's statistics), `stretch` where they pass by
 struct Layout { int slab, threads, mi, chunk, stretch; bool whole; };
 constexpr int MOST_THREADS = 512;
+constexpr int PART_MI = 4;       // 80 registers a thread: three workgroups a unit (8 pieces take 130 and leave one: 16 x 96 x 96 x 256 55 us)
 inline int most_mi(int dt) { return dt == BF16 ? 8 : 4; }
 inline int piece_columns(int channels) { return (channels + 7) / 8; }
 inline Layout layout_of(const GroupNorm& g) {
@@ -186,7 +203,7 @@ inline Layout layout_of(const GroupNorm& g) {
   } else {
     l.threads = MOST_THREADS;
     const int rt = l.threads / npc;
-    l.mi = most_mi(g.dt);
+    l.mi = PART_MI;
     l.chunk = rt * l.mi;
     // some 2048 workgroups, none under eight pieces a thread
     const int64_t per_image = std::max<int64_t>(1, 2048 / g.images), even = ((int64_t)g.pixels + per_image - 1) / per_image;

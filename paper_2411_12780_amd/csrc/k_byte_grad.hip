@@ -92,15 +92,15 @@ template <int DT> struct Regs {
   Eight<DT> d[NP];
 };
 
-template <bool DX, int DT, bool RAGGED>
-__global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
+// A tile (of a part of k): workgroup `group` of those of this product
+template <bool DX, int DT, bool RAGGED> __device__ __forceinline__ void grad_tile(const GradArgs& p, int group) {
   constexpr int T = terms<DT>(), BK = step_k<DT>(), NP = BK / 16, ESZ = DT == BF16 ? 2 : 4;
   constexpr int QB = q_bytes<DT>(), DB = d_bytes<DX, DT>(), STAGE = stage_bytes<DX, DT>();
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, wm = wave >> 1, wn = wave & 1;
   // XCD x (workgroup id % 8) takes a contiguous stretch: tiles of a row (of a part of k) share what they read in its L2
-  const int tiles = p.tiles_m * p.tiles_n, u = (blockIdx.x & 7) * p.per_xcd + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= p.per_xcd || u >= tiles * p.parts) return;
+  const int tiles = p.tiles_m * p.tiles_n, u = (group & 7) * p.per_xcd + (group >> 3);
+  if (u >= tiles * p.parts) return;
   const int part = u / tiles, t = u - part * tiles, m0 = t / p.tiles_n * BM, n0 = t % p.tiles_n * BN;
   const int kbeg = part * p.part_k, kend = min(p.K, kbeg + p.part_k), nk = (kend - kbeg + BK - 1) / BK;
 
@@ -116,47 +116,33 @@ __global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
   const int rk = (tid & (BK / 8 - 1)) * 8, rr = tid / (BK / 8);                   // [row][k]: rows rr + 2048 / BK j, k rk ..
   constexpr int RSTEP = THREADS / (BK / 8);
   const int qc = min((DX ? n0 : m0) + tc, p.qcols - 8);
-  const uint32_t q_at = (uint32_t)tk * (uint32_t)p.ldq + qc;
-  // Stage i: k from kbeg + i BK.  Where all of its k are there, addresses are a uniform one and the thread's 32 bits; else k rows stop at the last
-  // one (and its values are dropped on the way to LDS).
-  const int d_col = DX ? 0 : n0 + tc, d_from = RAGGED ? max(min(d_col, p.dcols - 8), 0) : min(d_col, p.dcols - 8);
-  const uint32_t d_at = DX ? 0 : ((uint32_t)tk * (uint32_t)p.ldd + d_from) * ESZ;
-  const char* d_base = DX ? p.d + (int64_t)m0 * p.ldd * ESZ : nullptr;
-  uint32_t d_row[NP];
+  // Stage i: k from kbeg + i BK (behind the last one: the last one again).  Addresses are a uniform one and 32 bits of the thread; in a last stage that
+  // is cut short k rows stop at the last one, whose values are dropped on the way to LDS.
+  const int last = nk - 1, left = kend - (kbeg + last * BK);
+  const int d_col = DX ? 0 : n0 + tc, d_from = max(min(d_col, p.dcols - 8), 0);
+  const bool few = RAGGED && p.dcols < 8;
+  const uint32_t ldq = (uint32_t)p.ldq, ldd = (uint32_t)p.ldd * ESZ;               // below 2^24
+  const char* d_base = DX ? p.d + (int64_t)m0 * p.ldd * ESZ : p.d;
+  uint32_t d_row[DX ? NP : 1];
   if (DX) {
 #pragma unroll
-    for (int j = 0; j < NP; ++j) d_row[j] = (uint32_t)min(rr + RSTEP * j, p.M - 1 - m0) * (uint32_t)p.ldd * ESZ;
+    for (int j = 0; j < NP; ++j) d_row[j] = (uint32_t)min(rr + RSTEP * j, p.M - 1 - m0) * ldd;
   }
-  auto whole = [&](int i) { return kbeg + (i + 1) * BK <= kend; };
   auto gload = [&](int i, Regs<DT>& r) {
-    const int k0 = kbeg + i * BK;
-    if (whole(i)) {
+    const int ic = min(i, last), k0 = kbeg + ic * BK, most = ic == last ? left - 1 : BK - 1;
+    const int8_t *qb = p.q + (int64_t)k0 * p.ldq, *eb = p.e + k0;
+    const char* db = p.d + (int64_t)k0 * p.ldd * ESZ;
+    const uint32_t dk = (uint32_t)max(min(k0 + rk, p.dcols - 8), 0) * ESZ;
 #pragma unroll
-      for (int j = 0; j < NP; ++j) {
-        r.q[j] = *(const uint2*)(p.q + (int64_t)(k0 + 16 * j) * p.ldq + q_at);
-        r.e[j] = (p.e + k0 + 16 * j)[(uint32_t)tk];
-        if (!DX) {
-          if (RAGGED && p.dcols < 8) load_few<DT>(r.d[j], p.d + (int64_t)(k0 + 16 * j + tk) * p.ldd * ESZ, d_col, p.dcols);
-          else r.d[j].load_all(p.d + (int64_t)(k0 + 16 * j) * p.ldd * ESZ + d_at);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NP; ++j) {
-        const int64_t k = min(k0 + tk + 16 * j, p.K - 1);
-        r.q[j] = *(const uint2*)(p.q + k * p.ldq + qc);
-        r.e[j] = p.e[k];
-        if (!DX) {
-          if (RAGGED && p.dcols < 8) load_few<DT>(r.d[j], p.d + k * p.ldd * ESZ, d_col, p.dcols);
-          else r.d[j].load_all(p.d + (k * p.ldd + d_from) * ESZ);
-        }
-      }
-    }
-    if (DX) {
-#pragma unroll
-      for (int j = 0; j < NP; ++j) {
-        if (RAGGED && p.dcols < 8) load_few<DT>(r.d[j], d_base + d_row[j], k0 + rk, p.dcols);
-        else r.d[j].load_all(d_base + (d_row[j] + (uint32_t)min(k0 + rk, p.dcols - 8) * ESZ));
+    for (int j = 0; j < NP; ++j) {
+      const uint32_t k = (uint32_t)min(tk + 16 * j, most);
+      r.q[j] = *(const uint2*)(qb + (__umul24(k, ldq) + qc));
+      r.e[j] = eb[k];
+      if (few) {
+        if (DX) load_few<DT>(r.d[j], d_base + d_row[DX ? j : 0], k0 + rk, p.dcols);
+        else load_few<DT>(r.d[j], db + __umul24(k, ldd), d_col, p.dcols);
+      } else {
+        r.d[j].load_all(DX ? d_base + (d_row[DX ? j : 0] + dk) : db + (__umul24(k, ldd) + d_from * ESZ));
       }
     }
   };
@@ -167,19 +153,19 @@ __global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
     if (j >= NP) return;
     char* st = smem + stage * STAGE;
     const int k0 = kbeg + i * BK;
-    const bool full = whole(i);
+    const bool cut = i == last && left < BK;
     float f[8];
     bytes_get(r.q[j], byte_step(r.e[j]), f);
     Eight<BF16> x;
     x.set(f);
     Eight<DT> d = r.d[j];
-    if (!full) {
+    if (cut) {
       if (k0 + tk + 16 * j >= kend) x.zero();
       if (DX ? k0 + rk >= kend : k0 + tk + 16 * j >= kend) d.zero();
     }
     // a piece that goes over its row's end was read ending there.  (One beyond the end keeps its last element, which no sum that is kept meets; in dX
     // it is zero already.)
-    if (RAGGED && p.dcols >= 8 && (DX ? !full : n0 + BN > p.dcols)) {
+    if (RAGGED && !few && (DX ? cut : n0 + BN > p.dcols)) {
       const int c = DX ? k0 + rk : d_col;
       shift_down(d, min(c - min(c, p.dcols - 8), 7));
     }
@@ -190,7 +176,7 @@ __global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) csum[e] += v[e];
     }
-    char* to = st + QB + (DX ? row_major<BK>(rr + RSTEP * j, rk >> 3) : (tk + 16 * j) * PITCH + tc * 2);
+    char* to = st + QB + (DX ? row_major<BK>(rr, rk >> 3) + j * RSTEP * BK * 2 : (tk + 16 * j) * PITCH + tc * 2);
     if constexpr (DT == BF16) {
       *(u32x4*)to = (u32x4){d.w.x, d.w.y, d.w.z, d.w.w};
     } else {
@@ -328,6 +314,13 @@ __global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs p) {
   }
 }
 
+// Both products in one launch, the longer ones of dW first: they need nothing of each other, and neither fills its last round of units by itself
+template <int DT, bool RAGGED> __global__ __launch_bounds__(THREADS, 2) void byte_grad_kernel(GradArgs dw, GradArgs dx) {
+  const int first = 8 * dw.per_xcd;
+  if ((int)blockIdx.x < first) grad_tile<false, DT, RAGGED>(dw, blockIdx.x);
+  else grad_tile<true, DT, RAGGED>(dx, blockIdx.x - first);
+}
+
 // Sums of parts, in their order
 __global__ __launch_bounds__(256) void byte_grad_sum_kernel(const float* parts, int n_parts, int64_t part_out, float* dw, int64_t n_dw, float* db, int n_db) {
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
@@ -364,19 +357,21 @@ __global__ __launch_bounds__(256) void byte_grad_zero_kernel(float* p, int64_t n
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0.f;
 }
 
-template <bool DX, int DT> int launch(hipStream_t s, GradArgs& p) {
-  constexpr int LDS = lds_bytes<DX, DT>();
-  p.tiles_m = (p.M + BM - 1) / BM; p.tiles_n = (p.N + BN - 1) / BN;
-  p.per_xcd = (int)(((int64_t)p.tiles_m * p.tiles_n * p.parts + 7) / 8);
-  const dim3 grid(8 * p.per_xcd);
-  if (p.dcols & 7) {
+template <int DT> int launch(hipStream_t s, GradArgs& dw, GradArgs& dx) {
+  constexpr int LDS = std::max(lds_bytes<true, DT>(), lds_bytes<false, DT>());
+  for (GradArgs* p : {&dw, &dx}) {
+    p->tiles_m = (p->M + BM - 1) / BM; p->tiles_n = (p->N + BN - 1) / BN;
+    p->per_xcd = (int)(((int64_t)p->tiles_m * p->tiles_n * p->parts + 7) / 8);
+  }
+  const dim3 grid(8 * (dw.per_xcd + dx.per_xcd));
+  if ((dw.parts ? dw.dcols : dx.dcols) & 7) {
     static OncePerDevice once;
-    PPLL_TRY(raise_lds((const void*)byte_grad_kernel<DX, DT, true>, LDS, once));
-    hipLaunchKernelGGL((byte_grad_kernel<DX, DT, true>), grid, dim3(THREADS), LDS, s, p);
+    PPLL_TRY(raise_lds((const void*)byte_grad_kernel<DT, true>, LDS, once));
+    hipLaunchKernelGGL((byte_grad_kernel<DT, true>), grid, dim3(THREADS), LDS, s, dw, dx);
   } else {
     static OncePerDevice once;
-    PPLL_TRY(raise_lds((const void*)byte_grad_kernel<DX, DT, false>, LDS, once));
-    hipLaunchKernelGGL((byte_grad_kernel<DX, DT, false>), grid, dim3(THREADS), LDS, s, p);
+    PPLL_TRY(raise_lds((const void*)byte_grad_kernel<DT, false>, LDS, once));
+    hipLaunchKernelGGL((byte_grad_kernel<DT, false>), grid, dim3(THREADS), LDS, s, dw, dx);
   }
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
@@ -399,22 +394,24 @@ int sum_chunks(int rows) { return (int)(((int64_t)rows + SUM_ROWS - 1) / SUM_ROW
 
 template <int DT> int backward(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
                                const ppll_rows& dx, float* dw, float* db, float* ws) {
-  GradArgs p{};
-  p.d = (const char*)dy.p; p.ldd = dy.ld; p.dcols = l.out;
+  GradArgs pw{}, px{};       // (no parts: not wanted)
+  const Parts parts = parts_of(l);
+  const bool whole = parts.n == 1;
   if (dx.p) {
-    p.q = w.q; p.e = w.e; p.ldq = w.ld; p.qcols = pad16(l.in);
-    p.out = (char*)dx.p; p.ldo = dx.ld; p.gate = (const char*)gate.p; p.ldg = gate.ld;
-    p.M = l.rows; p.N = l.in; p.K = l.out; p.parts = 1; p.part_k = l.out;
-    PPLL_TRY((launch<true, DT>(s, p)));
+    px.d = (const char*)dy.p; px.ldd = dy.ld; px.dcols = l.out;
+    px.q = w.q; px.e = w.e; px.ldq = w.ld; px.qcols = pad16(l.in);
+    px.out = (char*)dx.p; px.ldo = dx.ld; px.gate = (const char*)gate.p; px.ldg = gate.ld;
+    px.M = l.rows; px.N = l.in; px.K = l.out; px.parts = 1; px.part_k = l.out;
   }
   if (dw) {
-    const Parts parts = parts_of(l);
-    p.q = x.q; p.e = x.e; p.ldq = x.ld; p.qcols = pad16(l.in);
-    const bool whole = parts.n == 1;
-    p.out = (char*)(whole ? dw : ws); p.ldo = l.out; p.gate = nullptr;
-    p.db = !db ? nullptr : whole ? db : ws + (int64_t)l.in * l.out;
-    p.M = l.in; p.N = l.out; p.K = l.rows; p.parts = parts.n; p.part_k = parts.k; p.part_out = parts.out;
-    PPLL_TRY((launch<false, DT>(s, p)));
+    pw.d = (const char*)dy.p; pw.ldd = dy.ld; pw.dcols = l.out;
+    pw.q = x.q; pw.e = x.e; pw.ldq = x.ld; pw.qcols = pad16(l.in);
+    pw.out = (char*)(whole ? dw : ws); pw.ldo = l.out;
+    pw.db = !db ? nullptr : whole ? db : ws + (int64_t)l.in * l.out;
+    pw.M = l.in; pw.N = l.out; pw.K = l.rows; pw.parts = parts.n; pw.part_k = parts.k; pw.part_out = parts.out;
+  }
+  if (dx.p || dw) PPLL_TRY(launch<DT>(s, pw, px));
+  if (dw) {
     if (!whole) {
       const int64_t n = (int64_t)l.in * l.out + (db ? l.out : 0);
       hipLaunchKernelGGL(byte_grad_sum_kernel, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s, ws, parts.n, parts.out, dw, (int64_t)l.in * l.out, db,
@@ -423,7 +420,7 @@ template <int DT> int backward(hipStream_t s, const ByteLinear& l, const ppll_by
     }
   } else if (db) {
     const int chunks = sum_chunks(l.rows);
-    hipLaunchKernelGGL(byte_grad_columns_kernel<DT>, dim3((l.out + SUM_COLS - 1) / SUM_COLS, chunks), dim3(256), 0, s, p.d, p.ldd, l.rows, l.out,
+    hipLaunchKernelGGL(byte_grad_columns_kernel<DT>, dim3((l.out + SUM_COLS - 1) / SUM_COLS, chunks), dim3(256), 0, s, (const char*)dy.p, dy.ld, l.rows, l.out,
                        chunks == 1 ? db : ws);
     PPLL_HIP(hipGetLastError());
     if (chunks > 1) PPLL_TRY(reduce_partials(s, ws, chunks, l.out, l.out, 1.f, db));

@@ -223,8 +223,9 @@ template <int DT, int MODE, bool VEC, int GV> int fwd_launch(hipStream_t s, cons
   constexpr int MOST = DT == BF16 ? 8 : 4;
   const size_t lds = sizeof(float) * (size_t)(l.threads * GV);
   const dim3 grid(grid_of(p)), block(l.threads);
-  if (MODE == WHOLE && l.mi <= MOST / 2) hipLaunchKernelGGL((group_norm_fwd_kernel<DT, MODE, VEC, GV, MOST / 2>), grid, block, lds, s, p);
-  else hipLaunchKernelGGL((group_norm_fwd_kernel<DT, MODE, VEC, GV, MOST>), grid, block, lds, s, p);
+  if (MODE == PART) hipLaunchKernelGGL((group_norm_fwd_kernel<DT, MODE, VEC, GV, PART_MI>), grid, block, lds, s, p);
+  else if (l.mi <= MOST / 2) hipLaunchKernelGGL((group_norm_fwd_kernel<DT, WHOLE, VEC, GV, MOST / 2>), grid, block, lds, s, p);
+  else hipLaunchKernelGGL((group_norm_fwd_kernel<DT, WHOLE, VEC, GV, MOST>), grid, block, lds, s, p);
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }

@@ -7,7 +7,7 @@ namespace ppll {
 
 namespace {
 constexpr int MOST_ROWS = 1 << 30;
-constexpr int64_t MOST_TILES = (1 << 24) - 1;      // workgroups of 256 threads that a launch takes: under 2^32 threads
+constexpr int64_t MOST_TILES = 1 << 23;            // workgroups of 256 threads, two products in a launch: under 2^32 threads
 
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 int esz(int32_t precision) { return precision == PPLL_BF16 ? 2 : 4; }
