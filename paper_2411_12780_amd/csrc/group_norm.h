@@ -22,10 +22,14 @@ struct NormArgs {
   float* sums;                     // backward: channel sums of each image, [images][2][C]
   int images, pixels, C, groups, cg, act;
   int slab, slabs, npc, rt, pow2;  // channels of a slab; npc: piece columns, pow2: a power of two up to 64
-  int chunk, chunks;               // pixels of a piece, pieces of an image
+  int chunk, chunks, units;        // pixels of a piece, pieces of an image, workgroups' work
   int spg;                         // segments of a group
-  float eps;
+  float eps, over_cg, over_npc;    // 1 / cg, 1 / npc: see quotient()
 };
+
+// v / n for 0 <= v < 4096 and 1 <= n <= 4096, over = 1 / n: (v + 1/2) / n is at least 1 / (2 n) off every whole number, its value in fp32 less than 2^-12 of
+// that (two instructions; a division of whole numbers takes some thirty)
+__device__ __forceinline__ int quotient(int v, float over) { return (int)(((float)v + 0.5f) * over); }
 
 template <bool EXACT> __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.f + (EXACT ? expf(-z) : __expf(-z)));
@@ -98,7 +102,7 @@ template <int NV> __device__ __forceinline__ void column_sums(float (&v)[NV], co
     for (int i = 0; i < NV; ++i) v[i] = room[i * p.npc + col];
     return;
   }
-  const int row = t / p.npc, col = t % p.npc;
+  const int row = quotient(t, p.over_npc), col = t - row * p.npc;
   float* mine = room + row * width + col;
   __syncthreads();
   if (live)
@@ -119,7 +123,7 @@ template <int NV> __device__ __forceinline__ void column_sums(float (&v)[NV], co
 // Of GV segments of a thread's piece (their column sums) the sums of their groups.  room: npc GV floats
 template <int GV> __device__ __forceinline__ void group_sums(float (&v)[GV], const NormArgs& p, float* room) {
   if (p.spg == 1) return;
-  const int col = threadIdx.x % p.npc;
+  const int col = (int)threadIdx.x - quotient(threadIdx.x, p.over_npc) * p.npc;
   __syncthreads();
   if ((int)threadIdx.x < p.npc)
 #pragma unroll
@@ -140,11 +144,17 @@ template <int GV> __device__ __forceinline__ void group_sums(float (&v)[GV], con
 struct Unit { int image, slab, part, first, last; };
 __device__ __forceinline__ Unit unit_of(const NormArgs& p, int u) {
   Unit w;
-  const int per = p.slabs * p.chunks;
-  w.image = u / per;
-  const int rest = u - w.image * per;
-  w.slab = rest / p.chunks;
-  w.part = rest - w.slab * p.chunks;
+  if (p.slabs > 1) {       // an image's slabs share the lines of its pixels: to one XCD (workgroup id % 8).  (The last images may not be there.)
+    const int eight = u / (8 * p.slabs), rest = u - eight * 8 * p.slabs;
+    w.image = eight * 8 + (rest & 7);
+    w.slab = rest >> 3;
+    w.part = w.first = 0;
+    w.last = p.pixels;
+    return w;
+  }
+  w.slab = 0;
+  w.image = u / p.chunks;
+  w.part = u - w.image * p.chunks;
   w.first = w.part * p.chunk;
   w.last = min(p.pixels, w.first + p.chunk);
   return w;
@@ -181,28 +191,30 @@ constexpr int MOST_THREADS = 512;
 constexpr int PART_MI = 4;       // 80 registers a thread: three workgroups a unit (8 pieces take 130 and leave one: 16 x 96 x 96 x 256 55 us)
 inline int most_mi(int dt) { return dt == BF16 ? 8 : 4; }
 inline int piece_columns(int channels) { return (channels + 7) / 8; }
+inline void set_slab(const GroupNorm& g, Layout& l, int slab) {
+  const int npc = piece_columns(slab);
+  const int64_t pieces = (int64_t)g.pixels * npc;
+  l.slab = slab;
+  l.threads = 64;
+  while (l.threads < MOST_THREADS && (l.threads < npc || 2 * pieces > most_mi(g.dt) * (int64_t)l.threads)) l.threads *= 2;
+  const int rt = l.threads / npc;
+  l.mi = (int)(((int64_t)g.pixels + rt - 1) / rt);
+}
 inline Layout layout_of(const GroupNorm& g) {
   Layout l{};
   const int size = g.dt == BF16 ? 2 : 4;
+  l.chunk = l.stretch = g.pixels;
   // slabs of whole groups whose rows of a pixel are whole pieces and 64 bytes or more; the widest that fits
   for (int n = 1; n <= g.groups && !l.whole; ++n) {
     if (g.groups % n) continue;
     const int slab = g.channels / n;
     if (n > 1 && (slab % 8 || slab * size < 64)) continue;
-    if (g.pixels <= (int64_t)(MOST_THREADS / piece_columns(slab)) * most_mi(g.dt)) { l.whole = true; l.slab = slab; }
+    if (g.pixels <= (int64_t)(MOST_THREADS / piece_columns(slab)) * most_mi(g.dt)) { l.whole = true; set_slab(g, l, slab); }
   }
-  if (!l.whole) l.slab = g.channels;
-  const int npc = piece_columns(l.slab);
-  const int64_t pieces = (int64_t)g.pixels * npc;
-  l.threads = 64;
-  if (l.whole) {
-    while (l.threads < MOST_THREADS && (l.threads < npc || 2 * pieces > most_mi(g.dt) * (int64_t)l.threads)) l.threads *= 2;
-    const int rt = l.threads / npc;
-    l.mi = (int)(((int64_t)g.pixels + rt - 1) / rt);
-    l.chunk = l.stretch = g.pixels;
-  } else {
+  if (!l.whole) {
+    l.slab = g.channels;
     l.threads = MOST_THREADS;
-    const int rt = l.threads / npc;
+    const int rt = l.threads / piece_columns(l.slab);
     l.mi = PART_MI;
     l.chunk = rt * l.mi;
     // some 2048 workgroups, none under eight pieces a thread
@@ -213,16 +225,26 @@ inline Layout layout_of(const GroupNorm& g) {
 }
 inline int chunks_of(const GroupNorm& g, int chunk) { return (int)(((int64_t)g.pixels + chunk - 1) / chunk); }
 
+inline int units_of(const NormArgs& p) { return p.slabs > 1 ? (p.images + 7) / 8 * 8 * p.slabs : p.images * p.chunks; }
+// Few images: narrower slabs, down to a piece a pixel, until every unit has one
+inline void spread_over_units(const GroupNorm& g, Layout& l) {
+  if (!l.whole) return;
+  for (int n = g.channels / l.slab + 1; n <= g.groups && (int64_t)g.images * (g.channels / l.slab) < 256; ++n)
+    if (g.groups % n == 0 && g.channels / n % 8 == 0) set_slab(g, l, g.channels / n);
+}
+
 inline NormArgs args_of(const GroupNorm& g, const Layout& l, int chunk) {
   NormArgs p{};
   p.images = g.images; p.pixels = g.pixels; p.C = g.channels; p.groups = g.groups; p.cg = g.channels / g.groups; p.act = g.activation; p.eps = g.eps;
   p.slab = l.slab; p.slabs = g.channels / l.slab; p.npc = piece_columns(l.slab); p.rt = l.threads / p.npc;
   p.pow2 = p.npc <= 64 && (p.npc & (p.npc - 1)) == 0;
   p.chunk = chunk; p.chunks = chunks_of(g, chunk);
+  p.units = units_of(p);
+  p.over_cg = 1.f / (float)p.cg; p.over_npc = 1.f / (float)p.npc;
   return p;
 }
 inline int segments_of(int cg) { return cg % 8 == 0 ? 1 : cg == 4 ? 2 : cg == 2 ? 4 : 8; }
-inline unsigned grid_of(const NormArgs& p) { return (unsigned)std::min<int64_t>((int64_t)p.images * p.slabs * p.chunks, MOST_BLOCKS); }
+inline unsigned grid_of(const NormArgs& p) { return (unsigned)std::min(p.units, (int)MOST_BLOCKS); }
 
 }  // namespace norm
 }  // namespace ppll

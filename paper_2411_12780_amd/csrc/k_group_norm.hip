@@ -60,11 +60,12 @@ template <int DT, int MODE, bool VEC, int GV, int MI>
 __global__ __launch_bounds__(MOST_THREADS) void group_norm_fwd_kernel(NormArgs p) {
   constexpr int PER = 8 / GV;
   extern __shared__ float room[];
-  const int t = threadIdx.x, col = t % p.npc, row = t / p.npc;
+  const int t = threadIdx.x, row = quotient(t, p.over_npc), col = t - row * p.npc;
   const bool live = row < p.rt;
-  const int units = p.images * p.slabs * p.chunks;
+  const int units = p.units;
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
     const Unit w = unit_of(p, u);
+    if (w.image >= p.images) continue;
     const int c0 = w.slab * p.slab, c = col * 8, cols = p.slab, g0 = c0 / p.cg;
     const int64_t at = (int64_t)w.image * p.pixels + w.first;
     const int n = live ? w.last - w.first - row : 0;         // piece i is there where i rt < n
@@ -124,9 +125,9 @@ __global__ __launch_bounds__(MOST_THREADS) void group_norm_fwd_kernel(NormArgs p
       if (MODE == WHOLE) rstd[i] = rsqrtf(rstd[i] / count + p.eps);
       float* to = MODE == PART ? p.parts + ((int64_t)w.image * p.chunks + w.part) * p.groups * 2 : p.stats ? p.stats + (int64_t)w.image * p.groups * 2 : nullptr;
       // the first pixel's threads tell, of each group the one with its first channel
-      if (to && row == 0 && c + i * PER < cols && (c + i * PER) % p.cg == 0) {
-        to += 2 * (g0 + (c + i * PER) / p.cg);
-        to[0] = mean[i]; to[1] = rstd[i];
+      if (to && row == 0 && c + i * PER < cols) {
+        const int g = quotient(c + i * PER, p.over_cg);
+        if (g * p.cg == c + i * PER) { to[2 * (g0 + g)] = mean[i]; to[2 * (g0 + g) + 1] = rstd[i]; }
       }
     }
     if constexpr (MODE == WHOLE) {
@@ -177,43 +178,56 @@ __global__ __launch_bounds__(256) void group_norm_join_kernel(NormArgs p, float*
   }
 }
 
-// y of a piece of pixels, from the image's statistics
-constexpr int BATCH = 4;
-template <int DT, bool VEC> __global__ __launch_bounds__(MOST_THREADS, 4) void group_norm_apply_kernel(NormArgs p) {
-  const int t = threadIdx.x, col = t % p.npc, row = t / p.npc;
+// y of a piece of pixels, from the image's statistics.  Two batches of pieces in turn, one on its way while the other is worked on.
+template <int DT, bool VEC> struct Batch {
+  static constexpr int N = 2;
+  Eight<DT> x[N], res[N];
+  __device__ __forceinline__ void load(const NormArgs& p, int64_t at, int row, int c, int n) {
+    Map<DT, VEC> from, side;
+    from.init(p.x, p.ldx, at, 0, row, c, p.slab, p.rt);
+    side.init(p.residual, p.ldr, at, 0, row, c, p.slab, p.rt);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i].zero();
+      res[i].zero();
+      if (i * p.rt < n) {
+        from.load(x[i], i);
+        if (p.residual) side.load(res[i], i);
+      }
+    }
+  }
+};
+template <int DT, bool VEC> __global__ __launch_bounds__(MOST_THREADS, DT == BF16 ? 4 : 2) void group_norm_apply_kernel(NormArgs p) {
+  constexpr int N = Batch<DT, VEC>::N;
+  const int t = threadIdx.x, row = quotient(t, p.over_npc), col = t - row * p.npc;
   if (row >= p.rt) return;
-  const int units = p.images * p.chunks;
+  const int units = p.units;
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
     const Unit w = unit_of(p, u);
-    const int c = col * 8, cols = p.slab;
+    const int c = col * 8, cols = p.slab, step = N * p.rt;
+    const int64_t image = (int64_t)w.image * p.pixels;
+    Batch<DT, VEC> even, odd;
+    even.load(p, image + w.first, row, c, w.last - w.first - row);
     float mean[8], rstd[8], a[8], b[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float* st = p.stats_in + ((int64_t)w.image * p.groups + min(c + e, cols - 1) / p.cg) * 2;
+      const float* st = p.stats_in + ((int64_t)w.image * p.groups + quotient(min(c + e, cols - 1), p.over_cg)) * 2;
       mean[e] = st[0]; rstd[e] = st[1];
     }
     affine(p, 0, c, rstd, a, b);
     with_activation<DT == F32>(p.act, [&](auto act) {
-      for (int q = w.first; q < w.last; q += BATCH * p.rt) {
-        const int64_t at = (int64_t)w.image * p.pixels + q;
-        const int n = w.last - q - row;
-        Map<DT, VEC> from, side, to;
-        from.init(p.x, p.ldx, at, 0, row, c, cols, p.rt);
-        side.init(p.residual, p.ldr, at, 0, row, c, cols, p.rt);
-        to.init(p.y, p.ldy, at, 0, row, c, cols, p.rt);
-        Eight<DT> x[BATCH], res[BATCH];
+      auto finish_batch = [&](const Batch<DT, VEC>& d, int q) {
+        Map<DT, VEC> to;
+        to.init(p.y, p.ldy, image + q, 0, row, c, cols, p.rt);
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-          x[i].zero();
-          res[i].zero();
-          if (i * p.rt < n) {
-            from.load(x[i], i);
-            if (p.residual) side.load(res[i], i);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i)
-          if (i * p.rt < n) finish<DT, VEC>(act, mean, a, b, x[i], res[i], p.residual, to, i);
+        for (int i = 0; i < N; ++i)
+          if (i * p.rt < w.last - q - row) finish<DT, VEC>(act, mean, a, b, d.x[i], d.res[i], p.residual, to, i);
+      };
+      for (int q = w.first; q < w.last; q += 2 * step) {
+        odd.load(p, image + q + step, row, c, w.last - q - step - row);
+        finish_batch(even, q);
+        even.load(p, image + q + 2 * step, row, c, w.last - q - 2 * step - row);
+        finish_batch(odd, q + step);
       }
     });
   }
@@ -247,7 +261,7 @@ template <int DT> int fwd_all(hipStream_t s, const GroupNorm& g, NormArgs& p, co
   hipLaunchKernelGGL(group_norm_join_kernel, dim3((unsigned)std::min<int64_t>(((int64_t)p.images * p.groups + 3) / 4, MOST_BLOCKS)), dim3(256), 0, s, p, joined);
   PPLL_HIP(hipGetLastError());
   p.stats_in = joined;
-  p.chunk = l.stretch; p.chunks = chunks_of(g, l.stretch);
+  p.chunk = l.stretch; p.chunks = chunks_of(g, l.stretch); p.units = units_of(p);
   if (p.slab % 8 == 0) hipLaunchKernelGGL((group_norm_apply_kernel<DT, true>), dim3(grid_of(p)), dim3(l.threads), 0, s, p);
   else hipLaunchKernelGGL((group_norm_apply_kernel<DT, false>), dim3(grid_of(p)), dim3(l.threads), 0, s, p);
   PPLL_HIP(hipGetLastError());
@@ -266,7 +280,8 @@ size_t group_norm_workspace(const GroupNorm& g) {
 int launch_group_norm_fwd(hipStream_t s, const GroupNorm& g, const ppll_rows& x, const float* scale, const float* shift, const ppll_rows& residual,
                           const ppll_rows& y, float* stats, const ppll_byte_rows& keep, char* ws) {
   if (g.images <= 0) return PPLL_OK;
-  const Layout l = layout_of(g);
+  Layout l = layout_of(g);
+  if (!keep.q) spread_over_units(g, l);        // (a row in 8 bits needs all channels of a pixel)
   NormArgs p = args_of(g, l, l.chunk);
   p.x = (const char*)x.p; p.ldx = x.ld; p.residual = (const char*)residual.p; p.ldr = residual.ld; p.y = (char*)y.p; p.ldy = y.ld;
   p.scale = scale; p.shift = shift; p.stats = stats;

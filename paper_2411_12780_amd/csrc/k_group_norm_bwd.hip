@@ -56,13 +56,14 @@ template <int DT, bool VEC> struct XMap<DT, VEC, true> {
   }
 };
 
-// What a thread knows of its channels; GV: 1 where its eight are of one group
+// What a thread knows of its channels; GV: segments of its eight, each of one group
 template <int GV> struct Channels {
+  static constexpr int PER = 8 / GV;
   float mean[GV], rstd[GV], scale[8], shift[8];
   __device__ __forceinline__ void load(const NormArgs& p, int image, int c0, int c) {
 #pragma unroll
     for (int e = 0; e < GV; ++e) {
-      const float* st = p.stats_in + ((int64_t)image * p.groups + (c0 + min(c + e, p.slab - 1)) / p.cg) * 2;
+      const float* st = p.stats_in + ((int64_t)image * p.groups + quotient(c0 + min(c + e * PER, p.slab - 1), p.over_cg)) * 2;
       mean[e] = st[0]; rstd[e] = st[1];
     }
 #pragma unroll
@@ -75,23 +76,31 @@ template <int GV> struct Channels {
   template <class X> __device__ __forceinline__ void xhat(const X& x, float (&h)[8]) const {
     x.get(h);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = (h[e] - mean[e % GV]) * rstd[e % GV];
+    for (int e = 0; e < 8; ++e) h[e] = (h[e] - mean[e / PER]) * rstd[e / PER];
   }
   // dz; side: y (ReLU) or the residual (curved activations)
-  template <int DT> __device__ __forceinline__ void gradient(const Clamp& act, const Eight<DT>& dy, const Eight<DT>& side, const float (&)[8], float (&d)[8]) const {
-    float s[8];
+  template <int DT> __device__ __forceinline__ void gradient(const Clamp&, const Eight<DT>& dy, const Eight<DT>& side, bool has_side, const float (&)[8], float (&d)[8]) const {
     dy.get(d);
+    if (!has_side) return;       // no activation
+    float s[8];
     side.get(s);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d[e] = act.from < 0.f || s[e] > 0.f ? d[e] : 0.f;
+    for (int e = 0; e < 8; ++e) d[e] = s[e] > 0.f ? d[e] : 0.f;
   }
   template <int DT, class A>
-  __device__ __forceinline__ void gradient(const A& act, const Eight<DT>& dy, const Eight<DT>& side, const float (&h)[8], float (&d)[8]) const {
-    float s[8];
-    dy.get(d);
-    side.get(s);
+  __device__ __forceinline__ void gradient(const A& act, const Eight<DT>& dy, const Eight<DT>& side, bool has_side, const float (&h)[8], float (&d)[8]) const {
+    float z[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d[e] *= act.slope(h[e] * scale[e] + shift[e] + s[e]);
+    for (int e = 0; e < 8; ++e) z[e] = h[e] * scale[e] + shift[e];
+    if (has_side) {
+      float s[8];
+      side.get(s);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] += s[e];
+    }
+    dy.get(d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[e] *= act.slope(z[e]);
   }
   // d_residual and dx of a piece
   template <int DT, bool VEC>
@@ -103,7 +112,7 @@ template <int GV> struct Channels {
       dres.store(o, i);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d[e] = rstd[e % GV] * (d[e] * scale[e] - ga[e % GV] - h[e] * gb[e % GV]);
+    for (int e = 0; e < 8; ++e) d[e] = rstd[e / PER] * (d[e] * scale[e] - ga[e / PER] - h[e] * gb[e / PER]);
     o.set(d);
     dx.store(o, i);
   }
@@ -138,7 +147,7 @@ template <int GV> __device__ __forceinline__ void group_means(const NormArgs& p,
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < GV; ++e) {
-    const int g = min(c + e, cols - 1) / p.cg;
+    const int g = quotient(min(c + e * (8 / GV), cols - 1), p.over_cg);
     ga[e] = group[2 * g]; gb[e] = group[2 * g + 1];
   }
 }
@@ -147,11 +156,12 @@ template <int GV> __device__ __forceinline__ void group_means(const NormArgs& p,
 template <int DT, bool VEC, int GV, bool BYTES, int MI>
 __global__ __launch_bounds__(MOST_THREADS) void group_norm_bwd_kernel(NormArgs p) {
   extern __shared__ float room[];
-  const int t = threadIdx.x, col = t % p.npc, row = t / p.npc;
+  const int t = threadIdx.x, row = quotient(t, p.over_npc), col = t - row * p.npc;
   const bool live = row < p.rt;
-  const int units = p.images * p.slabs;
+  const int units = p.units;
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
     const Unit w = unit_of(p, u);
+    if (w.image >= p.images) continue;
     const int c0 = w.slab * p.slab, c = col * 8, cols = p.slab, n = live ? p.pixels - row : 0;
     Maps<DT, VEC, BYTES> m;
     m.init(p, (int64_t)w.image * p.pixels, c0, row, c);
@@ -159,10 +169,7 @@ __global__ __launch_bounds__(MOST_THREADS) void group_norm_bwd_kernel(NormArgs p
     Eight<DT> dy[MI], side[MI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      x[i].zero();
-      dy[i].zero();
-      side[i].zero();
-      if (i * p.rt < n) {
+      if (i * p.rt < n) {       // (a piece that is not there is not looked at)
         m.x.load(x[i], i);
         m.dy.load(dy[i], i);
         if (m.has_side) m.side.load(side[i], i);
@@ -178,7 +185,7 @@ __global__ __launch_bounds__(MOST_THREADS) void group_norm_bwd_kernel(NormArgs p
       for (int i = 0; i < MI; ++i) {
         if (i * p.rt >= n) continue;
         k.xhat(x[i], h);
-        k.gradient(act, dy[i], side[i], h, d);
+        k.gradient(act, dy[i], side[i], m.has_side, h, d);
 #pragma unroll
         for (int e = 0; e < 8; ++e) { sums[e] += d[e]; sums[8 + e] += d[e] * h[e]; }
       }
@@ -201,7 +208,7 @@ __global__ __launch_bounds__(MOST_THREADS) void group_norm_bwd_kernel(NormArgs p
       for (int i = 0; i < MI; ++i) {
         if (i * p.rt >= n) continue;
         k.xhat(x[i], h);
-        k.gradient(act, dy[i], side[i], h, d);
+        k.gradient(act, dy[i], side[i], m.has_side, h, d);
         k.out(m.dx, m.dres, p.dres, i, ga, gb, h, d);
       }
     });
@@ -209,17 +216,41 @@ __global__ __launch_bounds__(MOST_THREADS) void group_norm_bwd_kernel(NormArgs p
   }
 }
 
-// Pieces of pixels: PART leaves their channel sums, [images][chunks][2][C]; APPLY takes the gradient from those of the image, p.sums
+// Pieces of pixels: PART leaves their channel sums, [images][chunks][2][C]; APPLY takes the gradient from those of the image, p.sums.  Two batches of
+// pieces in turn, one on its way while the other is worked on.
+template <int DT, bool VEC, bool BYTES> struct Batch {
+  static constexpr int N = DT == BF16 ? 1 : 2;
+  typename XMap<DT, VEC, BYTES>::Piece x[N];
+  Eight<DT> dy[N], side[N];
+  __device__ __forceinline__ void load(const NormArgs& p, int64_t at, int row, int c, int n) {
+    Maps<DT, VEC, BYTES> m;
+    m.init(p, at, 0, row, c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i].zero();
+      dy[i].zero();
+      side[i].zero();
+      if (i * p.rt < n) {
+        m.x.load(x[i], i);
+        m.dy.load(dy[i], i);
+        if (m.has_side) m.side.load(side[i], i);
+      }
+    }
+  }
+};
 template <int DT, int MODE, bool VEC, int GV, bool BYTES>
-__global__ __launch_bounds__(MOST_THREADS, GV == 1 ? 4 : 2) void group_norm_bwd_piece_kernel(NormArgs p) {
+__global__ __launch_bounds__(MOST_THREADS, GV == 1 && DT == BF16 ? 4 : 2) void group_norm_bwd_piece_kernel(NormArgs p) {
   extern __shared__ float room[];
-  constexpr int N = 2;
-  const int t = threadIdx.x, col = t % p.npc, row = t / p.npc;
+  typedef Batch<DT, VEC, BYTES> B;
+  const int t = threadIdx.x, row = quotient(t, p.over_npc), col = t - row * p.npc;
   const bool live = row < p.rt;
-  const int units = p.images * p.chunks;
+  const int units = p.units;
   for (int u = blockIdx.x; u < units; u += gridDim.x) {
     const Unit w = unit_of(p, u);
-    const int c = col * 8, cols = p.slab;
+    const int c = col * 8, cols = p.slab, step = B::N * p.rt, end = live ? w.last - row : 0;      // pixel q + i rt + row is there where q + i rt < end
+    const int64_t image = (int64_t)w.image * p.pixels;
+    B even, odd;
+    even.load(p, image + w.first, row, c, end - w.first);
     Channels<GV> k;
     k.load(p, w.image, 0, c);
     float sums[16], ga[GV], gb[GV], h[8], d[8];
@@ -232,28 +263,14 @@ __global__ __launch_bounds__(MOST_THREADS, GV == 1 ? 4 : 2) void group_norm_bwd_
 #pragma unroll
     for (int e = 0; e < 16; ++e) sums[e] = 0.f;
     with_activation<DT == F32>(p.act, [&](auto act) {
-      for (int q = w.first; live && q < w.last; q += N * p.rt) {
+      auto work = [&](const B& b, int q) {
         Maps<DT, VEC, BYTES> m;
-        m.init(p, (int64_t)w.image * p.pixels + q, 0, row, c);
-        typename XMap<DT, VEC, BYTES>::Piece x[N];
-        Eight<DT> dy[N], side[N];
-        const int n = w.last - q - row;
+        m.init(p, image + q, 0, row, c);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          x[i].zero();
-          dy[i].zero();
-          side[i].zero();
-          if (i * p.rt < n) {
-            m.x.load(x[i], i);
-            m.dy.load(dy[i], i);
-            if (m.has_side) m.side.load(side[i], i);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          if (i * p.rt >= n) continue;
-          k.xhat(x[i], h);
-          k.gradient(act, dy[i], side[i], h, d);
+        for (int i = 0; i < B::N; ++i) {
+          if (q + i * p.rt >= end) continue;
+          k.xhat(b.x[i], h);
+          k.gradient(act, b.dy[i], b.side[i], m.has_side, h, d);
           if (MODE == PART) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) { sums[e] += d[e]; sums[8 + e] += d[e] * h[e]; }
@@ -261,6 +278,12 @@ __global__ __launch_bounds__(MOST_THREADS, GV == 1 ? 4 : 2) void group_norm_bwd_
             k.out(m.dx, m.dres, p.dres, i, ga, gb, h, d);
           }
         }
+      };
+      for (int q = w.first; q < w.last; q += 2 * step) {
+        odd.load(p, image + q + step, row, c, end - q - step);
+        work(even, q);
+        even.load(p, image + q + 2 * step, row, c, end - q - 2 * step);
+        work(odd, q + step);
       }
     });
     if (MODE == PART) {
@@ -333,7 +356,8 @@ template <int DT, bool VEC, int GV, bool BYTES> int launches(hipStream_t s, cons
 }
 template <int DT, bool BYTES> int bwd(hipStream_t s, const GroupNorm& g, NormArgs& p, const Layout& l, float* d_scale, float* d_shift, float* ws) {
   if (p.slab % 8) return launches<DT, false, 8, BYTES>(s, g, p, l, d_scale, d_shift, ws);
-  if (p.cg % 8) return launches<DT, true, 8, BYTES>(s, g, p, l, d_scale, d_shift, ws);
+  if (p.cg % 4) return launches<DT, true, 8, BYTES>(s, g, p, l, d_scale, d_shift, ws);
+  if (p.cg % 8) return launches<DT, true, 2, BYTES>(s, g, p, l, d_scale, d_shift, ws);
   return launches<DT, true, 1, BYTES>(s, g, p, l, d_scale, d_shift, ws);
 }
 }  // namespace
@@ -346,7 +370,8 @@ int launch_group_norm_bwd(hipStream_t s, const GroupNorm& g, const ppll_rows& x,
     PPLL_HIP(hipGetLastError());
     return PPLL_OK;
   }
-  const Layout l = layout_of(g);
+  Layout l = layout_of(g);
+  spread_over_units(g, l);
   NormArgs p = args_of(g, l, l.stretch);
   p.x = (const char*)x.p; p.ldx = x.ld; p.q = x8.q; p.qe = x8.e; p.ldq = x8.ld;
   p.residual = (const char*)residual.p; p.ldr = residual.ld; p.y_in = (const char*)y.p; p.ldy = y.ld; p.dy = (const char*)dy.p; p.ldd = dy.ld;
