@@ -405,7 +405,7 @@ int ppll_byte_linear_forward(const ppll_byte_linear_config* cfg, const ppll_byte
  *   db = the column sums of dy, fp32 [out_dim].
  * Each of dx, dw, db may be null (not wanted); w is needed for dx, x for dw.  dx may be gate; dw and db are overwritten (zeros where rows = 0).
  * Sums in fp32 in a fixed order.  Workspace: ppll_byte_linear_workspace_bytes(cfg) bytes, 16-byte aligned, used by nothing else until the
- * stream has passed the call; it holds what one operand at a time stands for. */
+ * stream has passed the call. */
 int ppll_byte_linear_workspace_bytes(const ppll_byte_linear_config* cfg, size_t* bytes);
 int ppll_byte_linear_backward(const ppll_byte_linear_config* cfg, const ppll_byte_rows* x, const ppll_byte_rows* w, const ppll_rows* dy,
                               const ppll_rows* gate, const ppll_rows* dx, float* dw_dev, float* db_dev, void* workspace_dev, size_t workspace_bytes,

@@ -17,6 +17,8 @@ inline int pad16(int v) { return (v + 15) & ~15; }
 int launch_byte_rows_pack(hipStream_t s, int dt, int rows, int cols, const ppll_rows& in, const ppll_byte_rows& out);
 int launch_byte_rows_unpack(hipStream_t s, int dt, int rows, int cols, const ppll_byte_rows& in, const ppll_rows& out);
 int launch_byte_rows_pack_columns(hipStream_t s, int dt, int rows, int cols, const ppll_rows& in, const ppll_byte_rows& out);
+// What rows a, and behind them rows b, stand for, in bf16, row by row; cols a multiple of 8, out 16-byte aligned
+int launch_byte_rows_values(hipStream_t s, int cols, const ppll_byte_rows& a, int a_rows, const ppll_byte_rows& b, int b_rows, uint16_t* out);
 
 // The linear layer.  residual, slope, bias may have null pointers.
 struct ByteLinear {

@@ -392,7 +392,56 @@ Parts parts_of(const ByteLinear& l) {
 }
 int sum_chunks(int rows) { return (int)(((int64_t)rows + SUM_ROWS - 1) / SUM_ROWS); }
 
-template <int DT> int backward(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
+// ---- The other way: operands written out in bf16, which is what they stand for, and the products on the kernels of bf16 operands.  Those reach 1100
+// TFLOP/s where the kernel above is held at 750 by LDS (64 x 64 of a wave: 192 KB through it for 64 k of four of them, and the conversion's own way
+// in), but X goes through memory twice more.
+bool values_fit(const ByteLinear& l) {
+  const int64_t most = (1 << 29) - 1;       // elements that the products address
+  return l.dt == BF16 && l.in % 8 == 0 && l.out % 8 == 0 && (int64_t)l.rows * std::max(l.in, l.out) <= most && (int64_t)l.in * l.out <= most;
+}
+bool lies_whole(const void* p, int64_t ld) { return !p || (ld % 8 == 0 && ((uintptr_t)p & 15) == 0); }
+// Microseconds, this kernel / values, both gradients, rows x in x out: 8320 x 1536 x 384 51 / 63, 25216 x 768 x 768 101 / 111, 4096 x 2048 x 2048 93 / 99,
+// 8320 x 1536 x 1536 143 / 116, 25216 x 768 x 2304 248 / 191, 8192 x 4096 x 4096 744 / 505, 512 x 6144 x 6144 156 / 138; with few output channels X's way
+// counts for more: 32768 x 4096 x 256 236 / 286.
+bool values_for_both(const ByteLinear& l) { return values_fit(l) && 4.0 * l.rows * l.in * l.out >= 7.5e10 && l.out >= 512; }
+// (dX alone: W alone is written out.  8320 x 1536 x 384 30 / 24, 25216 x 768 x 768 54 / 35, 640 x 768 x 768 14.7 / 8.6, 8320 x 384 x 384 10.5 / 11.6)
+GemmArgs dw_product(const ByteLinear& l, const uint16_t* xv, const ppll_rows& dy, float* dw, float* db) {
+  GemmArgs g{};
+  g.A = xv; g.a_dt = BF16; g.a_sm = 1; g.a_sk = l.in;
+  g.B = dy.p; g.b_dt = BF16; g.b_sk = dy.p ? dy.ld : l.out; g.b_sn = 1;
+  g.C = dw; g.c_dt = F32; g.ldc = l.out; g.M = l.in; g.N = l.out; g.K = l.rows;
+  g.colsum = db;
+  return g;
+}
+size_t dw_floats(const ByteLinear& l) {       // for the parts of its tiles
+  const GemmArgs g = dw_product(l, nullptr, {nullptr, 0}, nullptr, nullptr);
+  size_t floats = 0;
+  gemm_big_grads_choice(&g, 1, &floats);
+  return std::max(floats, gemm_mfma_balanced_floats());
+}
+int64_t values_bytes(const ByteLinear& l, bool x, bool w) { return (((x ? (int64_t)l.rows : 0) + (w ? l.out : 0)) * l.in * 2 + 255) / 256 * 256; }
+bool values_supported(const ByteLinear& l, const ppll_rows& dy, const ppll_rows& gate, const ppll_rows& dx, const float* dw) {
+  return values_fit(l) && lies_whole(dy.p, dy.ld) && lies_whole(gate.p, gate.ld) && lies_whole(dx.p, dx.ld) && lies_whole(dw, l.out);
+}
+int backward_values(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
+                    const ppll_rows& dx, float* dw, float* db, char* ws) {
+  uint16_t* xv = (uint16_t*)ws;
+  uint16_t* wv = xv + (dw ? (int64_t)l.rows * l.in : 0);
+  PPLL_TRY(launch_byte_rows_values(s, l.in, x, dw ? l.rows : 0, w, dx.p ? l.out : 0, xv));
+  if (dx.p) {
+    GemmArgs g{};
+    g.A = dy.p; g.a_dt = BF16; g.a_sm = dy.ld; g.a_sk = 1;
+    g.B = wv; g.b_dt = BF16; g.b_sk = l.in; g.b_sn = 1;
+    g.C = dx.p; g.c_dt = BF16; g.ldc = dx.ld; g.M = l.rows; g.N = l.in; g.K = l.out;
+    if (gate.p) { g.epilogue = EPI_DGELU; g.aux = gate.p; g.aux_dt = BF16; g.ldaux = gate.ld; }
+    PPLL_TRY(launch_gemm(s, g));
+  }
+  if (!dw) return PPLL_OK;
+  const GemmArgs g = dw_product(l, xv, dy, dw, db);
+  return launch_gemm_group(s, &g, 1, (float*)(ws + values_bytes(l, true, true)), dw_floats(l), true);
+}
+
+template <int DT> int backward_here(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
                                const ppll_rows& dx, float* dw, float* db, float* ws) {
   GradArgs pw{}, px{};       // (no parts: not wanted)
   const Parts parts = parts_of(l);
@@ -433,14 +482,26 @@ int zero(hipStream_t s, float* p, int64_t n) {
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }
-}  // namespace
-
-size_t byte_linear_workspace(const ByteLinear& l) {
+// way: 0 by the rules, 1 the kernel here, 2 values
+int backward(hipStream_t s, int way, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
+             const ppll_rows& dx, float* dw, float* db, char* ws) {
+  const bool values = (dx.p || dw) && (dw || !db) && values_supported(l, dy, gate, dx, dw) && (way ? way == 2 : dw ? dx.p && values_for_both(l) : true);
+  if (way == 2 && !values) { set_error("not as values"); return PPLL_ERR_CONFIG; }
+  if (values) return backward_values(s, l, x, w, dy, gate, dx, dw, db, ws);
+  return l.dt == BF16 ? backward_here<BF16>(s, l, x, w, dy, gate, dx, dw, db, (float*)ws) : backward_here<F32>(s, l, x, w, dy, gate, dx, dw, db, (float*)ws);
+}
+size_t workspace(const ByteLinear& l, bool any) {
   if (l.rows <= 0) return 0;
   const Parts p = parts_of(l);
   const int64_t parts = p.n > 1 ? p.n * p.out : 0, sums = sum_chunks(l.rows) > 1 ? (int64_t)sum_chunks(l.rows) * l.out : 0;
-  return (size_t)std::max(parts, sums) * sizeof(float);
+  int64_t bytes = std::max(parts, sums) * (int64_t)sizeof(float);
+  if (values_fit(l)) bytes = std::max(bytes, values_bytes(l, false, true));
+  if (any ? values_fit(l) : values_for_both(l)) bytes = std::max(bytes, values_bytes(l, true, true) + (int64_t)(dw_floats(l) * sizeof(float)));
+  return (size_t)bytes;
 }
+}  // namespace
+
+size_t byte_linear_workspace(const ByteLinear& l) { return workspace(l, false); }
 
 int launch_byte_linear_bwd(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
                            const ppll_rows& dx, float* dw, float* db, char* ws) {
@@ -448,7 +509,17 @@ int launch_byte_linear_bwd(hipStream_t s, const ByteLinear& l, const ppll_byte_r
     PPLL_TRY(zero(s, dw, (int64_t)l.in * l.out));
     return zero(s, db, l.out);
   }
-  return l.dt == BF16 ? backward<BF16>(s, l, x, w, dy, gate, dx, dw, db, (float*)ws) : backward<F32>(s, l, x, w, dy, gate, dx, dw, db, (float*)ws);
+  return backward(s, 0, l, x, w, dy, gate, dx, dw, db, ws);
 }
 
 }  // namespace ppll
+
+// Both gradients one way (backward() above), for tests of one against the other (no part of the public interface); ws null: its size to *bytes
+extern "C" int ppll_internal_byte_linear_backward(int way, int rows, int in, int out, const ppll_byte_rows* x, const ppll_byte_rows* w, const ppll_rows* dy,
+                                                  const ppll_rows* gate, const ppll_rows* dx, float* dw, float* db, char* ws, size_t* bytes, void* stream) {
+  using namespace ppll;
+  const ByteLinear l{BF16, rows, in, out, PPLL_ACT_NONE};
+  if (!ws) { *bytes = workspace(l, true); return PPLL_OK; }
+  const ppll_rows none{nullptr, 0};
+  return backward((hipStream_t)stream, way, l, *x, *w, *dy, gate ? *gate : none, dx ? *dx : none, dw, db, ws);
+}

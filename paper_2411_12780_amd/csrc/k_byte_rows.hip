@@ -2,6 +2,8 @@
 //
 // L neighbouring lanes hold a row in pieces of 8 elements, P each, read once; the largest magnitude goes round the lanes in registers and the
 // bytes leave 8 a lane.  What bounds it: memory (3 bytes an element from bf16).
+#include <algorithm>
+
 #include "bytes.h"
 
 namespace ppll {
@@ -84,6 +86,27 @@ __global__ __launch_bounds__(THREADS) void byte_rows_unpack_kernel(const int8_t*
       Eight<DT> v;
       v.set(f);
       v.store(row, c, cols);
+    }
+  }
+}
+
+// Two operands of as many columns, one behind the other, to bf16 rows without room between them
+template <int L>
+__global__ __launch_bounds__(THREADS) void byte_rows_values_kernel(ppll_byte_rows a, int a_rows, ppll_byte_rows b, int b_rows, uint16_t* out, int cols) {
+  constexpr int R = THREADS / L;
+  const int lane = threadIdx.x % L;
+  for (int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / L; r < (int64_t)a_rows + b_rows; r += (int64_t)gridDim.x * R) {
+    const bool first = r < a_rows;
+    const int64_t k = first ? r : r - a_rows;
+    const int8_t* q = first ? a.q + k * a.ld : b.q + k * b.ld;
+    const float step = byte_step(first ? a.e[k] : b.e[k]);
+#pragma unroll 4
+    for (int c = lane * 8; c < cols; c += L * 8) {
+      float f[8];
+      bytes_get(*(const uint2*)(q + c), step, f);
+      Eight<BF16> v;
+      v.set(f);
+      *(uint4*)(out + r * cols + c) = v.w;
     }
   }
 }
@@ -199,6 +222,14 @@ int launch_byte_rows_pack(hipStream_t s, int dt, int rows, int cols, const ppll_
 int launch_byte_rows_unpack(hipStream_t s, int dt, int rows, int cols, const ppll_byte_rows& in, const ppll_rows& out) {
   if (rows <= 0) return PPLL_OK;
   return dt == BF16 ? unpack_any<BF16>(s, rows, cols, in, out) : unpack_any<F32>(s, rows, cols, in, out);
+}
+int launch_byte_rows_values(hipStream_t s, int cols, const ppll_byte_rows& a, int a_rows, const ppll_byte_rows& b, int b_rows, uint16_t* out) {
+  const int64_t rows = (int64_t)a_rows + b_rows;
+  auto grid = [&](int per) { return dim3((unsigned)std::min<int64_t>((rows + per - 1) / per, MOST_BLOCKS)); };
+  if (cols <= 512) hipLaunchKernelGGL((byte_rows_values_kernel<16>), grid(THREADS / 16), dim3(THREADS), 0, s, a, a_rows, b, b_rows, out, cols);
+  else hipLaunchKernelGGL((byte_rows_values_kernel<64>), grid(THREADS / 64), dim3(THREADS), 0, s, a, a_rows, b, b_rows, out, cols);
+  PPLL_HIP(hipGetLastError());
+  return PPLL_OK;
 }
 int launch_byte_rows_pack_columns(hipStream_t s, int dt, int rows, int cols, const ppll_rows& in, const ppll_byte_rows& out) {
   if (cols <= 0) return PPLL_OK;

@@ -159,7 +159,7 @@ int ppll_byte_linear_backward(const ppll_byte_linear_config* cfg, const ppll_byt
       PPLL_TRY(check_bytes(w, l.in, "w"));
     }
     if (dw_dev) PPLL_TRY(check_bytes(x, l.in, "x"));
-    if (dw_dev || db_dev) PPLL_TRY(check_workspace(workspace_dev, workspace_bytes, byte_linear_workspace(l)));
+    PPLL_TRY(check_workspace(workspace_dev, workspace_bytes, byte_linear_workspace(l)));
   }
   return launch_byte_linear_bwd((hipStream_t)hip_stream, l, given(x), given(w), given(dy), given(gate), given(dx), dw_dev, db_dev, (char*)workspace_dev);
 }

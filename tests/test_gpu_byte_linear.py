@@ -174,15 +174,26 @@ def test_forward_in_place_of_the_residual():
     assert torch.equal(residual.view, y.view)
 
 
-def check_backward(l, gate=False, want=("dx", "dw", "db"), seed_scale=1e-3):
+def check_backward(l, gate=False, want=("dx", "dw", "db"), seed_scale=1e-3, way=None):
     m, k, n = l.shape
     dy, g = l.put(m, n, scale=seed_scale), l.put(m, k) if gate else None
     dx = l.empty(m, k) if "dx" in want else None
     dw = torch.full((k, n), 7.0, device=DEV) if "dw" in want else None
     db = torch.full((n,), 7.0, device=DEV) if "db" in want else None
-    size = P.ppll_byte_linear_workspace_bytes(l.cfg())
-    ws = torch.full((max(size, 16) + 64,), 0x77, dtype=torch.uint8, device=DEV)
-    P.ppll_byte_linear_backward(l.cfg(), l.bytes(l.x), l.bytes(l.w), rows(dy), rows(g), rows(dx), dw, db, ws, size, stream())
+    if way is None:
+        size = P.ppll_byte_linear_workspace_bytes(l.cfg())
+        ws = torch.full((max(size, 16) + 64,), 0x77, dtype=torch.uint8, device=DEV)
+        P.ppll_byte_linear_backward(l.cfg(), l.bytes(l.x), l.bytes(l.w), rows(dy), rows(g), rows(dx), dw, db, ws, size, stream())
+    else:
+        n_bytes = ctypes.c_size_t(0)
+        ref = lambda r: None if r is None else ctypes.byref(r)  # noqa: E731
+        ptr = lambda t: None if t is None else ctypes.c_void_p(t.data_ptr())  # noqa: E731
+        call = lambda ws_: P.lib().ppll_internal_byte_linear_backward(way, m, k, n, ref(l.bytes(l.x)), ref(l.bytes(l.w)), ref(rows(dy)), ref(rows(g)),  # noqa: E731
+                                                                      ref(rows(dx)), ptr(dw), ptr(db), ws_, ctypes.byref(n_bytes), ctypes.c_void_p(stream()))
+        assert call(None) == 0
+        size = n_bytes.value
+        ws = torch.full((max(size, 16) + 64,), 0x77, dtype=torch.uint8, device=DEV)
+        assert call(ptr(ws)) == 0, P.ppll_last_error()
     x, w = l.values()
     d, half = dy.host(), HALF[l.dtype]
     if dx is not None:
@@ -224,6 +235,34 @@ def test_backward_of_strided_rows(precision, dtype, size, place):
 def test_gradients_that_are_not_wanted(precision, dtype, want):
     for rows_ in (5, 700, 2000):
         check_backward(Layer(rows_, 72, 40, dtype), False, want)
+
+
+@pytest.mark.parametrize("way", [1, 2])
+@pytest.mark.parametrize("size", [(1, 16, 8), (70, 40, 24), (333, 136, 200), (1000, 520, 264), (2500, 24, 72)])
+@pytest.mark.parametrize("want", [("dx", "dw", "db"), ("dx",), ("dw",)])
+def test_each_way_backward(way, size, want):
+    check_backward(Layer(*size, torch.bfloat16, seed=3, room=8), "dx" in want, want, way=way)
+
+
+def test_backward_of_a_wide_layer():
+    # as values by the rules, both gradients and dX alone
+    l = Layer(4100, 1536, 3200, torch.bfloat16)
+    m, k, n = l.shape
+    x, w = (torch.from_numpy(v).to(DEV).float() for v in l.values())
+    dy = l.put(m, n)
+    d = dy.view.float()
+    dx, dw, db = l.empty(m, k), torch.empty(k, n, device=DEV), torch.empty(n, device=DEV)
+    size = P.ppll_byte_linear_workspace_bytes(l.cfg())
+    ws = torch.full((size + 64,), 0x77, dtype=torch.uint8, device=DEV)
+    P.ppll_byte_linear_backward(l.cfg(), l.bytes(l.x), l.bytes(l.w), rows(dy), None, rows(dx), dw, db, ws, size, stream())
+    both = dx.view.clone()
+    # against fp32 products, each side off by the roundings of its sums
+    for got, want, count in ((both.float(), d @ w, n), (dw, x.t().contiguous() @ d, m)):
+        size_of = (d.abs() @ w.abs()) if count == n else (x.abs().t().contiguous() @ d.abs())
+        assert bool(((got - want).abs() <= 4 * count * ULP * size_of + (2 ** -8 * want.abs() if count == n else 0)).all())
+    assert bool(((db.double() - d.double().sum(0)).abs() <= m * ULP * d.double().abs().sum(0)).all())
+    P.ppll_byte_linear_backward(l.cfg(), None, l.bytes(l.w), rows(dy), None, rows(dx), None, None, ws, size, stream())
+    assert torch.equal(dx.view, both) and bool((ws[size:] == 0x77).all())
 
 
 def test_backward_of_many_rows():
