@@ -1,8 +1,12 @@
 // Linear layer on rows of 8 bits.  Forward: y = X W^T in v_mfma_i32_*_i8, both operands with k contiguous, sums exact in 32-bit whole numbers; a
 // row's exponent and a channel's enter in the epilogue.
 //
-// The loop is that of the bf16 products (gemm_pipe.h): a fragment of 16 bytes holds 16 k instead of 8, an instruction takes the time of a
-// bf16 one, so a product costs what a bf16 one of half its k does, and the same rules choose the tiles.
+// The loop is that of the bf16 products (gemm_pipe.h): a fragment of 16 bytes holds 16 k instead of 8 and an instruction takes the time of a
+// bf16 one, so a product costs what a bf16 one of half its k does: 8192 x 8192 x 8192 476 us (2312 TOP/s), 25216 x 6144 x 1536 with a residual 222 us (2142).
+// What bounds it: LDS reads and products in the loop, the epilogue where k is short (8320 x 384 x 1536 with GELU and its slope 22 us, 14 without: 24
+// instructions' time for an element's two results).
+#include <algorithm>
+
 #include "bytes.h"
 #include "gemm_pipe.h"
 #include "plan.h"
@@ -25,9 +29,25 @@ struct ByteArgs {
   int helpers;
 };
 
+// Steps and biases of columns n .. n + 7; a channel of NaN has a bias of NaN
+struct Columns {
+  int most;               // the largest exponent
+  float step[8], bias[8];
+  __device__ __forceinline__ void load(const ByteArgs& p, int n) {
+    most = -256;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int at = min(n + i, p.N - 1), e = p.ew[at];
+      const float b = p.bias ? p.bias[at] : 0.f;
+      bias[i] = e == BYTE_NAN ? __uint_as_float(0x7fc00000u) : b;
+      step[i] = exp2_bits(e == BYTE_NAN ? 0 : e);
+      most = max(most, e == BYTE_NAN ? 0 : e);
+    }
+  }
+};
 // What eight sums of a row become, columns n .. n + 7
-template <int DT, bool VEC> __device__ __forceinline__ void byte_end(const ByteArgs& p, int64_t m, int n, int row_exp, const int (&col_exp)[8], const float (&bias)[8],
-                                                                     const int (&sum)[8], const Eight<DT>& res) {
+template <int DT, bool VEC> __device__ __forceinline__ void byte_end(const ByteArgs& p, int64_t m, int n, int row_exp, const Columns& c, const int (&sum)[8],
+                                                                     const Eight<DT>& res) {
   constexpr int ESZ = DT == BF16 ? 2 : 4;
   auto put = [&](char* to, int64_t ld, const float (&v)[8]) {
     Eight<DT> o;
@@ -45,11 +65,14 @@ template <int DT, bool VEC> __device__ __forceinline__ void byte_end(const ByteA
     }
   };
   float v[8];
+  // the product of two steps is a power of two, exact (also as a subnormal one) below 2^128; from there on only a sum of 0 is none too large
+  const bool rare = row_exp == BYTE_NAN || row_exp + c.most > 127;
+  const float step = exp2_bits(rare ? 0 : row_exp);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = ldexpf((float)sum[i], row_exp + col_exp[i]) + bias[i];
-  if (row_exp == BYTE_NAN)
+  for (int i = 0; i < 8; ++i) v[i] = fmaf((float)sum[i], c.step[i] * step, c.bias[i]);
+  if (rare)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7fc00000u);
+    for (int i = 0; i < 8; ++i) v[i] = row_exp == BYTE_NAN ? __uint_as_float(0x7fc00000u) : ldexpf((float)sum[i], row_exp + (int)(__float_as_uint(c.step[i]) >> 23) - 127) + c.bias[i];
   if (p.residual) {
     float r[8];
     res.get(r);
@@ -68,19 +91,10 @@ template <int DT, bool VEC> __device__ __forceinline__ void byte_end(const ByteA
   }
   put(p.y, p.ldy, v);
 }
-// Exponents and biases of columns n .. n + 7; a channel of NaN has a bias of NaN
-__device__ __forceinline__ void columns_of(const ByteArgs& p, int n, int (&exps)[8], float (&bias)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const bool in = n + i < p.N;
-    const int e = in ? p.ew[n + i] : 0;
-    bias[i] = e == BYTE_NAN ? __uint_as_float(0x7fc00000u) : in && p.bias ? p.bias[n + i] : 0.f;
-    exps[i] = e == BYTE_NAN ? 0 : e;
-  }
-}
 
 template <int DT, bool VEC, int WGM, int WGN, int IM, int NS, int KT>
 __global__ __launch_bounds__((Shape<false, false, WGM, WGN, IM, NS, KT>::THREADS), 2) void byte_linear_kernel(ByteArgs p) {
+  PPLL_CODE_TO_L2(4);
   using S = Shape<false, false, WGM, WGN, IM, NS, KT>;
   constexpr int JN = 2, ESZ = DT == BF16 ? 2 : 4;
   extern __shared__ __align__(1024) char smem[];
@@ -116,11 +130,34 @@ __global__ __launch_bounds__((Shape<false, false, WGM, WGN, IM, NS, KT>::THREADS
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int* st = reinterpret_cast<int*>(smem) + wave * 32 * PITCH;
   const int mw = m0 + wave / WGN * IM * 32, c8 = lane % LPR * 8, n = n0 + wave % WGN * COLS + c8, r0 = lane / LPR;
-  int exps[8];
-  float bias[8];
-  columns_of(p, n, exps, bias);
+  // exponents of all its rows and columns at once (asked for 32 rows at a time, each time took a way to memory: a tile of 256 x 256 by itself 14.9 us,
+  // so 10.7; 25216 x 768 x 2304 85 and 68)
+  Columns columns;
+  columns.load(p, n);
+  static_assert(NP == 4, "");
+  uint32_t ex[IM];
 #pragma unroll
   for (int im = 0; im < IM; ++im) {
+    uint32_t e[NP];
+#pragma unroll
+    for (int q = 0; q < NP; ++q) e[q] = (uint8_t)p.ex[min(mw + im * 32 + q * RPP + r0, p.M - 1)];
+    ex[im] = e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24;
+  }
+  constexpr int AHEAD = DT == BF16 ? 2 : 1;      // residuals of 32 rows on their way (fp32: no registers for more)
+  Eight<DT> res[AHEAD][NP];
+  auto ask = [&](int im) {
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+      const int64_t m = mw + im * 32 + q * RPP + r0;
+      if (m >= p.M || n >= p.N) continue;
+      if (VEC) res[im % AHEAD][q].load_all(p.residual + (m * p.ldr + n) * ESZ);
+      else res[im % AHEAD][q].load(p.residual + m * p.ldr * ESZ, n, p.N);
+    }
+  };
+  if (p.residual && AHEAD == 2) ask(0);
+#pragma unroll
+  for (int im = 0; im < IM; ++im) {
+    if (p.residual && im + AHEAD - 1 < IM) ask(im + AHEAD - 1);
 #pragma unroll
     for (int jn = 0; jn < JN; ++jn)
 #pragma unroll
@@ -129,32 +166,15 @@ __global__ __launch_bounds__((Shape<false, false, WGM, WGN, IM, NS, KT>::THREADS
             make_float4(acc[jn][im][4 * q], acc[jn][im][4 * q + 1], acc[jn][im][4 * q + 2], acc[jn][im][4 * q + 3]);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
-    int sums[NP][8];
 #pragma unroll
     for (int q = 0; q < NP; ++q) {
       const int4 lo = *reinterpret_cast<const int4*>(st + (q * RPP + r0) * PITCH + c8), hi = *reinterpret_cast<const int4*>(st + (q * RPP + r0) * PITCH + c8 + 4);
-      sums[q][0] = lo.x; sums[q][1] = lo.y; sums[q][2] = lo.z; sums[q][3] = lo.w; sums[q][4] = hi.x; sums[q][5] = hi.y; sums[q][6] = hi.z; sums[q][7] = hi.w;
+      const int sums[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      const int64_t m = mw + im * 32 + q * RPP + r0;
+      if (m < p.M && n < p.N) byte_end<DT, VEC>(p, m, n, (int8_t)(ex[im] >> (8 * q)), columns, sums, res[im % AHEAD][q]);
     }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
-    Eight<DT> res[NP];
-    int ex[NP];
-#pragma unroll
-    for (int q = 0; q < NP; ++q) {
-      const int64_t m = mw + im * 32 + q * RPP + r0;
-      const bool in = m < p.M && n < p.N;
-      res[q].zero();
-      ex[q] = in ? p.ex[m] : 0;
-      if (in && p.residual) {
-        if (VEC) res[q].load_all(p.residual + (m * p.ldr + n) * ESZ);
-        else res[q].load(p.residual + m * p.ldr * ESZ, n, p.N);
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < NP; ++q) {
-      const int64_t m = mw + im * 32 + q * RPP + r0;
-      if (m < p.M && n < p.N) byte_end<DT, VEC>(p, m, n, ex[q], exps, bias, sums[q], res[q]);
-    }
   }
 }
 
@@ -196,19 +216,19 @@ __global__ __launch_bounds__(64 * FW) void byte_linear_rows_kernel(ByteArgs p) {
     const int row = i >> 1, n = n0 + (i & 1) * 8;
     const int64_t m = m0 + row;
     if (m >= p.M || n >= p.N) continue;
-    int sum[8], exps[8];
-    float bias[8];
+    int sum[8];
+    Columns columns;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       sum[e] = 0;
 #pragma unroll
       for (int w = 0; w < FW; ++w) sum[e] += part[w][row >> 4][row & 15][(i & 1) * 8 + e];
     }
-    columns_of(p, n, exps, bias);
+    columns.load(p, n);
     Eight<DT> res;
     res.zero();
     if (p.residual) res.load(p.residual + m * p.ldr * ESZ, n, p.N);
-    byte_end<DT, false>(p, m, n, p.ex[m], exps, bias, sum, res);
+    byte_end<DT, false>(p, m, n, p.ex[m], columns, sum, res);
   }
 }
 
@@ -233,15 +253,27 @@ template <int DT, int WGM, int WGN, int IM, int NS, int KT> int byte_launch(hipS
 
 constexpr int FEW_ROWS = 64;
 
-// Which kernel a product goes to: 1 few rows, 3 tiles of 128 x 128 with copying waves, 4 / 8 / 10 tiles of 128 / 256 / 320 rows of 256 columns
+// Which kernel a product goes to: 1 few rows, 3 tiles of 128 x 128 with copying waves, 4 / 8 / 10 tiles of 128 / 256 / 320 rows of 256 columns.
+// Microseconds of a round of workgroups (a unit each, two of kernel 4): per k, and with the epilogue (plain, residual, GELU and its slope); a last round that
+// fills the share f of the units counts as last + (1 - last) f.  Fits to products of 4096 to 32768 rows, 512 to 1536 channels, k of 128 to 4096, within
+// 13 %; 16384 x 1024, k = 1024: 46, 26, 23, 28 us, k = 128 with GELU: 35, 19.3, 19.4, 27; 8192 x 1024, k = 4096: 43, 54, 54, 63; 20480 x 1024, k = 4096:
+// 116, 130, 115, 84.
 int choice(const ByteArgs& p, int units) {
   if (p.M <= FEW_ROWS) return 1;
-  const ProductEnd end = p.gelu ? END_GELU : p.residual ? END_RESIDUAL : END_BIAS;
-  const long tiles = (long)((p.M + 127) / 128) * ((p.N + 127) / 128);
-  if (tiles <= units) return 3;
-  const int wide = wide_tile_rows(p.M, p.N, p.K, end, units), alone = unit_tile_rows(p.M, p.N, p.K, end, wide, units);
-  const int im = alone ? alone : wide;
-  return im == 5 ? 4 : im ? im : 3;
+  struct Cost { int kernel, rows, cols, places; double last, k, end[3]; };
+  static const Cost costs[] = {{3, 128, 128, 1, 0.66, 0.0036, {6.6, 8.8, 9.0}},
+                               {4, 128, 256, 2, 0.70, 0.0178, {7.4, 12.2, 16.9}},
+                               {8, 256, 256, 1, 0.70, 0.0133, {9.1, 14.7, 18.9}},
+                               {10, 320, 256, 1, 0.70, 0.0176, {12.0, 18.3, 22.9}}};
+  int best = 0;
+  double least = 0;
+  for (const Cost& c : costs) {
+    const int64_t tiles = ((int64_t)p.M + c.rows - 1) / c.rows * (((int64_t)p.N + c.cols - 1) / c.cols), places = (int64_t)c.places * units;
+    const double share = std::min(1.0, (double)(tiles % places) / units), last = tiles % places == 0 ? 0 : tiles % places > units ? 1 : c.last + (c.places == 1 ? (1 - c.last) * share : 0);
+    const double time = ((double)(tiles / places) + last) * (c.k * 2 * p.K + c.end[p.gelu ? 2 : p.residual ? 1 : 0]);
+    if (!best || time < least) { best = c.kernel; least = time; }
+  }
+  return best;
 }
 template <int DT> int forward(hipStream_t s, ByteArgs& p, int kernel) {
   const int units = compute_units() > 0 ? compute_units() : 256;
@@ -286,7 +318,7 @@ int launch_byte_linear_fwd(hipStream_t s, const ByteLinear& l, const ppll_byte_r
 extern "C" int ppll_internal_byte_linear(int kernel, int precision, int rows, int in, int out, int gelu, const ppll_byte_rows* x, const ppll_byte_rows* w,
                                          const float* bias, const ppll_rows* residual, const ppll_rows* y, const ppll_rows* slope, void* stream) {
   using namespace ppll;
-  if (kernel != 1 && kernel != 3 && kernel != 4 && kernel != 8 && kernel != 10) { set_error("there is no kernel %d", kernel); return PPLL_ERR_CONFIG; }
+  if (kernel != 0 && kernel != 1 && kernel != 3 && kernel != 4 && kernel != 8 && kernel != 10) { set_error("there is no kernel %d", kernel); return PPLL_ERR_CONFIG; }
   const ppll_rows none{nullptr, 0};
   return product((hipStream_t)stream, kernel, {precision == PPLL_BF16 ? BF16 : F32, rows, in, out, gelu ? PPLL_ACT_GELU : PPLL_ACT_NONE}, *x, *w, bias,
                  residual ? *residual : none, *y, slope ? *slope : none);
