@@ -74,7 +74,7 @@ enum { PPLL_T_PARAM = 0, PPLL_T_GRAD = 1, PPLL_T_MOMENT1 = 2, PPLL_T_MOMENT2 = 3
  * zero channels, the blocks before it work on [2*height, 2*width, channels/2]
  * and that is also the shape of x_in (of the stem's output with a stem). */
 typedef struct {
-  uint32_t struct_size;   /* = sizeof(ppll_block_config), or of its part that ends with `seed`: the fields behind are then 0 */
+  uint32_t struct_size;   /* = sizeof(ppll_block_config), or of its part that ends with `seed` or with `qk_norm_eps`: the fields behind are then 0 */
   int32_t arch;           /* PPLL_VIT | PPLL_RESNET                              */
   int32_t precision;      /* PPLL_FP32 | PPLL_BF16 (fp32 master weights always)  */
   int32_t input_kind;     /* PPLL_IN_IMAGE (ViT patches, ResNet stem) | PPLL_IN_ACTIVATION */
@@ -100,6 +100,16 @@ typedef struct {
   float rotary_base;                /* > 0                                       */
   int32_t qk_norm;
   float qk_norm_eps;                /* > 0                                       */
+  /* ResNet: group_norm = G > 0 puts group norms of G groups (ppll_group_norm_forward with a ReLU) in the place of all BatchNorms; scales, shifts and
+   * eps (bn_eps) keep their names, there are no running statistics, training and evaluation normalise alike.  G divides all channels.
+   * byte_checkpoints: those norms keep their inputs in 8 bits for the backward pass, which reads them; the maps themselves share one buffer. */
+  int32_t group_norm;
+  int32_t byte_checkpoints;         /* 0 or 1 (with group_norm)                  */
+  /* ViT: the four linear products of every encoder layer on rows of 8 bits (ppll_byte_linear_forward): tokens and weights are brought into 8 bits in
+   * every step, the tokens stay so for the weight gradients, and gradients are those at the values in 8 bits, the weight's taken over by the fp32
+   * master weights. */
+  int32_t byte_products;            /* 0 or 1                                    */
+  int32_t reserved;                 /* 0                                         */
 } ppll_block_config;
 
 typedef struct ppll_block ppll_block_t;

@@ -98,6 +98,9 @@ class BlockConfig:
     rotary_base: float = 100.0
     qk_norm: int = 0
     qk_norm_eps: float = 1e-6
+    # ResNet: group norms of so many groups in the place of the BatchNorms; their inputs kept in 8 bits for the backward pass
+    group_norm: int = 0
+    byte_checkpoints: int = 0
 
 
 # --------------------------------------------------------------------------
@@ -169,7 +172,7 @@ def param_spec(cfg: BlockConfig) -> List[Tuple[str, Tuple[int, ...]]]:
 
 def bn_stat_spec(cfg: BlockConfig) -> List[Tuple[str, int]]:
     """BatchNorm layers carrying running statistics, in forward order."""
-    if cfg.arch != ARCH_RESNET:
+    if cfg.arch != ARCH_RESNET or cfg.group_norm:
         return []
     out = []
     if cfg.input_kind == IN_IMAGE:
@@ -684,6 +687,29 @@ def _bn_track(st: BlockState, name, cache, n):
     st.bn_var[name] = (1 - m) * st.bn_var[name] + m * var * (n / (n - 1.0))
 
 
+def _norm_fwd(st: BlockState, x, name, track=True):
+    """BatchNorm on the batch's statistics, or the group norm in its place: values in front of the ReLU, and what the backward pass reads."""
+    cfg, p = st.cfg, st.params
+    if cfg.group_norm:
+        v = x.reshape(x.shape[0], -1, x.shape[-1])
+        z, stats, _ = group_norm_fwd(v, p[name + ".g"], p[name + ".b"], cfg.group_norm, cfg.bn_eps)
+        if cfg.byte_checkpoints:
+            v = byte_values(*byte_rows(v.reshape(-1, v.shape[-1]))).reshape(v.shape).astype(x.dtype)
+        return z.reshape(x.shape).astype(x.dtype), (v, stats)
+    y, cache = batchnorm_fwd(x, p[name + ".g"], p[name + ".b"], cfg.bn_eps)
+    if track:
+        _bn_track(st, name, cache, x.size // x.shape[-1])
+    return y, cache
+
+
+def _norm_bwd(st: BlockState, dy, cache, name):
+    if not st.cfg.group_norm:
+        return batchnorm_bwd(dy, cache, st.params[name + ".g"])
+    x, stats = cache
+    dx, dg, db = group_norm_bwd(dy.reshape(x.shape), x, stats, st.params[name + ".g"])
+    return dx.reshape(dy.shape).astype(dy.dtype), dg, db
+
+
 def resnet_forward(st: BlockState, x_in, track=True):
     """[stem conv3x3 -> BN -> ReLU when the input is the image] -> n basic blocks
     relu(shortcut(x) + bn2(conv2(relu(bn1(conv1(x)))))) -> x_out, then the auxiliary head
@@ -693,30 +719,22 @@ def resnet_forward(st: BlockState, x_in, track=True):
     caches = {}
     if cfg.input_kind == IN_IMAGE:
         c0 = S(conv3x3_fwd(x, W(p["stem.conv.w"]), 1))
-        b0, cb0 = batchnorm_fwd(c0, p["stem.bn.g"], p["stem.bn.b"], cfg.bn_eps)
-        if track:
-            _bn_track(st, "stem.bn", cb0, c0.size // c0.shape[-1])
+        b0, cb0 = _norm_fwd(st, c0, "stem.bn", track)
         caches["stem"] = (x, cb0, b0)
         x = S(np.maximum(b0, 0))
     for i, (_, co, stride) in enumerate(resnet_layout(cfg)):
         pre = f"rb{i}"
         c1 = S(conv3x3_fwd(x, W(p[pre + ".conv1.w"]), stride))
-        b1, cb1 = batchnorm_fwd(c1, p[pre + ".bn1.g"], p[pre + ".bn1.b"], cfg.bn_eps)
+        b1, cb1 = _norm_fwd(st, c1, pre + ".bn1", track)
         y1 = S(np.maximum(b1, 0))
         c2 = S(conv3x3_fwd(y1, W(p[pre + ".conv2.w"]), 1))
-        b2, cb2 = batchnorm_fwd(c2, p[pre + ".bn2.g"], p[pre + ".bn2.b"], cfg.bn_eps)
+        b2, cb2 = _norm_fwd(st, c2, pre + ".bn2", track)
         s = shortcut_fwd(x, co, stride) + b2
         caches[pre] = (x, cb1, b1, y1, cb2, s)
-        if track:
-            n = c1.size // c1.shape[-1]
-            _bn_track(st, pre + ".bn1", cb1, n)
-            _bn_track(st, pre + ".bn2", cb2, n)
         x = S(np.maximum(s, 0))
     x_out = x
     ca = S(conv3x3_fwd(x_out, W(p["aux.conv.w"]), 2))
-    ba, cba = batchnorm_fwd(ca, p["aux.bn.g"], p["aux.bn.b"], cfg.bn_eps)
-    if track:
-        _bn_track(st, "aux.bn", cba, ca.size // ca.shape[-1])
+    ba, cba = _norm_fwd(st, ca, "aux.bn", track)
     ya = S(np.maximum(ba, 0))
     pooled = S(ya.mean(axis=(1, 2)))
     logits = linear_fwd(pooled, p["head.w"], p["head.b"])
@@ -733,7 +751,7 @@ def resnet_backward(st: BlockState, dlogits, caches):
     hw = ya.shape[1] * ya.shape[2]
     dya = S(np.broadcast_to(dpool[:, None, None, :] / hw, ya.shape))
     dba = dya * (ba > 0)
-    dca, g["aux.bn.g"], g["aux.bn.b"] = batchnorm_bwd(dba, cba, p["aux.bn.g"])
+    dca, g["aux.bn.g"], g["aux.bn.b"] = _norm_bwd(st, dba, cba, "aux.bn")
     dca = S(dca)
     g["aux.conv.w"] = conv3x3_bwd_weight(dca, x_out, 2)
     dx = S(conv3x3_bwd_input(dca, st.wmat(p["aux.conv.w"]), 2, x_out.shape))
@@ -744,12 +762,12 @@ def resnet_backward(st: BlockState, dlogits, caches):
         stride = layout[i][2]
         x, cb1, b1, y1, cb2, s = caches[pre]
         ds = dx * (s > 0)
-        dc2, g[pre + ".bn2.g"], g[pre + ".bn2.b"] = batchnorm_bwd(ds, cb2, p[pre + ".bn2.g"])
+        dc2, g[pre + ".bn2.g"], g[pre + ".bn2.b"] = _norm_bwd(st, ds, cb2, pre + ".bn2")
         dc2 = S(dc2)
         g[pre + ".conv2.w"] = conv3x3_bwd_weight(dc2, y1, 1)
         dy1 = S(conv3x3_bwd_input(dc2, st.wmat(p[pre + ".conv2.w"]), 1, y1.shape))
         db1 = dy1 * (b1 > 0)
-        dc1, g[pre + ".bn1.g"], g[pre + ".bn1.b"] = batchnorm_bwd(db1, cb1, p[pre + ".bn1.g"])
+        dc1, g[pre + ".bn1.g"], g[pre + ".bn1.b"] = _norm_bwd(st, db1, cb1, pre + ".bn1")
         dc1 = S(dc1)
         g[pre + ".conv1.w"] = conv3x3_bwd_weight(dc1, x, stride)
         if i > 0 or stem:   # without a stem the first block's input is the detached x_{j-1}
@@ -757,7 +775,7 @@ def resnet_backward(st: BlockState, dlogits, caches):
     if stem:
         img, cb0, b0 = caches["stem"]
         db0 = dx * (b0 > 0)
-        dc0, g["stem.bn.g"], g["stem.bn.b"] = batchnorm_bwd(db0, cb0, p["stem.bn.g"])
+        dc0, g["stem.bn.g"], g["stem.bn.b"] = _norm_bwd(st, db0, cb0, "stem.bn")
         dc0 = S(dc0)
         g["stem.conv.w"] = conv3x3_bwd_weight(dc0, img, 1)
     return g
@@ -779,6 +797,8 @@ def block_forward_eval(st: BlockState, x_in):
     x = np.asarray(x_in, dtype=st.dtype)
 
     def bn(t, name):
+        if cfg.group_norm:       # the same in both modes
+            return _norm_fwd(st, t, name)[0]
         return batchnorm_eval(t, p[name + ".g"], p[name + ".b"], st.bn_mean[name], st.bn_var[name], cfg.bn_eps)
 
     if cfg.input_kind == IN_IMAGE:

@@ -41,7 +41,8 @@ class BlockConfig(C.Structure):
                 ("adam_eps", C.c_float), ("ln_eps", C.c_float), ("bn_eps", C.c_float),
                 ("bn_momentum", C.c_float), ("seed", C.c_uint64),
                 ("rotary", C.c_int32), ("grid_h", C.c_int32), ("grid_w", C.c_int32), ("rotary_base", C.c_float),
-                ("qk_norm", C.c_int32), ("qk_norm_eps", C.c_float)]
+                ("qk_norm", C.c_int32), ("qk_norm_eps", C.c_float),
+                ("group_norm", C.c_int32), ("byte_checkpoints", C.c_int32), ("byte_products", C.c_int32), ("reserved", C.c_int32)]
 
 
 def make_config(wl: dict) -> BlockConfig:

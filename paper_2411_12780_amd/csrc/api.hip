@@ -142,12 +142,12 @@ int scratch_lookup(void** ptr_out, int* dev_out) {
 }
 
 // A caller's configuration in full: one built before a field existed says so by its struct_size, and the field is 0.
-constexpr size_t CONFIG_TO_SEED = offsetof(ppll_block_config, rotary);
+constexpr size_t CONFIG_TO_SEED = offsetof(ppll_block_config, rotary), CONFIG_TO_QK_NORM = offsetof(ppll_block_config, group_norm);
 int read_config(const ppll_block_config* c, ppll_block_config* full) {
   if (!c) { set_error("config is null"); return PPLL_ERR_NULL; }
   memset(full, 0, sizeof *full);
-  if (c->struct_size == CONFIG_TO_SEED) {
-    memcpy(full, c, CONFIG_TO_SEED);
+  if (c->struct_size == CONFIG_TO_SEED || c->struct_size == CONFIG_TO_QK_NORM) {
+    memcpy(full, c, c->struct_size);
     full->struct_size = sizeof *full;
   } else if (c->struct_size == sizeof *full) {
     *full = *c;

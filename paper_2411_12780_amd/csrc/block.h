@@ -6,6 +6,7 @@
 #include <string>
 #include <vector>
 
+#include "bytes.h"
 #include "common.h"
 #include "ortho.h"
 #include "rotary.h"
@@ -60,7 +61,10 @@ struct EvalBuffers {
   void *stem_c = nullptr, *stem_y = nullptr, *stem_xp = nullptr, *stem_wp = nullptr;   // ResNet
   void *shortcut = nullptr, *aux_c = nullptr, *aux_y = nullptr, *pooled = nullptr;
   float *stem_mean = nullptr, *stem_rstd = nullptr, *aux_mean = nullptr, *aux_rstd = nullptr;
+  char* norm_ws = nullptr;     // of the group norms
 };
+// What a group norm keeps for its backward pass: statistics, and its input in 8 bits where that is asked for (else q is null)
+struct KeptNorm { float* stats; ppll_byte_rows bytes; };
 
 struct Block {
   ppll_block_config cfg{};
@@ -161,6 +165,19 @@ struct Block {
   // Whether the backward pass forms the weight gradient of a basic block's second convolution with its input gradient, and whether it goes
   // on through the first one in the same way (the block input has a gradient, over an identity shortcut)
   bool second_filter_from_bn(int i) const;
+  // Whether a convolution of equal channels runs with the BatchNorms around it
+  bool fused_bn(int H, int W, int C) const { return !cfg.group_norm && conv_bn_ok(dt, cfg.batch, H, W, C); }
+  // Group norms in the place of all BatchNorms (cfg.group_norm of them), each with its ReLU; in the order of the BatchNorms
+  std::vector<KeptNorm> norms;
+  char* norm_ws = nullptr;
+  void* norm_x = nullptr;                // one buffer for the inputs of all norms, where they are kept in 8 bits
+  template <class F> void each_norm(F f) const;
+  template <class BUMP> void plan_norms(BUMP& bump);
+  size_t norm_workspace() const;
+  GroupNorm group_norm_of(int pixels, int channels, int act) const;
+  int norm_fwd(int index, const void* x, int pixels, int channels, size_t g_off, size_t b_off, const void* res, void* y, hipStream_t s);
+  int norm_bwd(int index, const void* x, const void* y, const void* dy, int pixels, int channels, size_t g_off, size_t b_off, void* dx, hipStream_t s);
+  int norm_eval(const void* x, int pixels, int channels, size_t g_off, size_t b_off, const void* res, void* y, char* room, hipStream_t s) const;
   bool whole_chain(int i) const;
   int in_h = 0, in_w = 0, in_c = 0;      // activation the first basic block reads
   bool stem = false;                     // conv3x3 (img_c -> in_c) - BN - ReLU on the image in front of the blocks

@@ -49,6 +49,7 @@ int validate_config(const ppll_block_config* c) {
     return PPLL_ERR_CONFIG;
   }
   auto bad = [](const char* what) { set_error("config: %s", what); return PPLL_ERR_CONFIG; };
+  if (c->reserved) return bad("reserved is not 0");
   if (c->precision != PPLL_FP32 && c->precision != PPLL_BF16) return bad("precision must be PPLL_FP32 or PPLL_BF16");
   if (c->optimizer != PPLL_SGD && c->optimizer != PPLL_ADAMW && c->optimizer != PPLL_MUON) return bad("optimizer must be PPLL_SGD, PPLL_ADAMW or PPLL_MUON");
   if (c->batch < 1 || c->batch > 65536) return bad("batch outside 1..65536");
@@ -67,6 +68,8 @@ int validate_config(const ppll_block_config* c) {
         return bad("tokens must equal (img_h/patch)*(img_w/patch) + 1");
     }
     if ((c->rotary | c->qk_norm) & ~1) return bad("rotary and qk_norm must be 0 or 1");
+    if (c->group_norm || c->byte_checkpoints) return bad("group norm belongs to ResNet blocks");
+    if (c->byte_products & ~1) return bad("byte_products must be 0 or 1");
     if (c->rotary || c->qk_norm) {
       const int dh = c->dim / c->heads;
       if (dh % 2 || dh > 2 * ROTARY_PAIRS) return bad("rotary positions and qk_norm need an even head width of 256 at most");
@@ -107,6 +110,16 @@ int validate_config(const ppll_block_config* c) {
     if (c->optimizer == PPLL_MUON && (9 * c->channels > ORTHO_SIDE || c->aux_channels > ORTHO_SIDE))
       return bad("9 * channels or aux_channels above 8192 with the Muon optimizer");
     if (c->optimizer == PPLL_MUON && c->n_basic_blocks > ORTHO_COUNT) return bad("more than 65535 basic blocks with the Muon optimizer");
+    if (c->byte_products) return bad("products in 8 bits belong to ViT blocks");
+    if (c->group_norm < 0 || (c->byte_checkpoints & ~1) || (c->byte_checkpoints && !c->group_norm))
+      return bad("group_norm >= 0 and byte_checkpoints 0, or 1 with a group norm, required");
+    if (c->group_norm) {
+      const int m = c->transition_block > 0 ? 2 : 1;
+      if (c->channels % (m * c->group_norm) || c->aux_channels % c->group_norm || c->aux_channels > 4096)
+        return bad("the groups of a group norm must divide all channels, of which there are 4096 at most");
+      if ((int64_t)c->batch * (m * c->height) * (m * c->width) > (1 << 30)) return bad("batch x map above 2^30 pixels with a group norm");
+      if (!(c->bn_eps > 0.f) || !std::isfinite(c->bn_eps)) return bad("bn_eps must be positive and finite");
+    }
     if (c->bn_eps <= 0.f || c->bn_momentum < 0.f || c->bn_momentum > 1.f) return bad("bn_eps > 0 and bn_momentum in [0,1] required");
     {
       const size_t m = c->transition_block > 0 ? 2 : 1, wide = c->channels > c->aux_channels ? c->channels : c->aux_channels;
@@ -213,9 +226,12 @@ size_t Block::plan(char* base) {
     in_h = m * cfg.height; in_w = m * cfg.width; in_c = Ch / m;
     stem = cfg.input_kind == PPLL_IN_IMAGE;
     bn_base = stem ? 1 : 0;
+    auto add_bn = [&](const std::string& name, int c) {        // (a group norm keeps no running statistics)
+      if (!cfg.group_norm) { bn_names.push_back(name); bn_channels.push_back(c); }
+    };
     if (stem) {
       stem_w = add("stem.conv.w", 9 * cfg.img_c, in_c); stem_g = add("stem.bn.g", 1, in_c); stem_b = add("stem.bn.b", 1, in_c);
-      bn_names.push_back("stem.bn"); bn_channels.push_back(in_c);
+      add_bn("stem.bn", in_c);
     }
     for (int i = 0; i < cfg.n_basic_blocks; ++i) {
       std::string p = "rb" + std::to_string(i);
@@ -228,11 +244,11 @@ size_t Block::plan(char* base) {
       r.conv1_w = add(p + ".conv1.w", 9 * d.Ci, d.Co); r.bn1_g = add(p + ".bn1.g", 1, d.Co); r.bn1_b = add(p + ".bn1.b", 1, d.Co);
       r.conv2_w = add(p + ".conv2.w", 9 * d.Co, d.Co); r.bn2_g = add(p + ".bn2.g", 1, d.Co); r.bn2_b = add(p + ".bn2.b", 1, d.Co);
       rb_p.push_back(r);
-      bn_names.push_back(p + ".bn1"); bn_channels.push_back(d.Co);
-      bn_names.push_back(p + ".bn2"); bn_channels.push_back(d.Co);
+      add_bn(p + ".bn1", d.Co);
+      add_bn(p + ".bn2", d.Co);
     }
     aux_conv_w = add("aux.conv.w", 9 * Ch, A); aux_bn_g = add("aux.bn.g", 1, A); aux_bn_b = add("aux.bn.b", 1, A);
-    bn_names.push_back("aux.bn"); bn_channels.push_back(A);
+    add_bn("aux.bn", A);
     head_w = add("head.w", A, C); head_b = add("head.b", 1, C);
   }
   P = off;
@@ -344,9 +360,12 @@ size_t Block::plan(char* base) {
     size_t widest = (size_t)B * in_h * in_w * in_c;   // largest activation a gradient buffer has to hold
     auto grow = [&](size_t v) { if (v > partial_floats) partial_floats = v; };
     partial_floats = 0;
+    plan_norms(bump);
+    // what a norm reads: buffers of the layers' own, or one of all where the 8 bits that the norms leave are kept
+    auto norm_in = [&](size_t elems) { return cfg.byte_checkpoints ? norm_x : bump.take(elems * esz); };
     if (stem) {
-      stem_c = bump.take(widest * esz); stem_y = bump.take(widest * esz);
-      stem_mask = conv_bn_ok(dt, B, in_h, in_w, in_c) ? (uint8_t*)bump.take(widest / 8) : nullptr;
+      stem_c = norm_in(widest); stem_y = bump.take(widest * esz);
+      stem_mask = fused_bn(in_h, in_w, in_c) ? (uint8_t*)bump.take(widest / 8) : nullptr;
       stem_mean = bump.floats(in_c); stem_rstd = bump.floats(in_c);
       stem_xp = stem_wp = nullptr;
       stem_pad = dt == BF16 && cfg.img_c < 16 && in_c % 16 == 0 && in_c <= 64;
@@ -363,11 +382,11 @@ size_t Block::plan(char* base) {
       const size_t act = (size_t)B * d.Ho * d.Wo * d.Co;
       if (act > widest) widest = act;
       BasicBlockActs a;
-      a.c1 = bump.take(act * esz); a.y1 = bump.take(act * esz); a.c2 = bump.take(act * esz); a.out = bump.take(act * esz);
+      a.c1 = norm_in(act); a.y1 = bump.take(act * esz); a.c2 = norm_in(act); a.out = bump.take(act * esz);
       // not where the launch that forms them leaves the weight gradient instead (y1 an evaluation needs all the same)
       a.d1 = second_filter_from_bn(i) && whole_chain(i) ? nullptr : bump.take(act * esz);
       a.d2 = second_filter_from_bn(i) ? nullptr : bump.take(act * esz);
-      const bool masks = conv_bn_ok(dt, B, d.Ho, d.Wo, d.Co);
+      const bool masks = fused_bn(d.Ho, d.Wo, d.Co);
       a.mask1 = masks ? (uint8_t*)bump.take(act / 8) : nullptr; a.mask2 = masks ? (uint8_t*)bump.take(act / 8) : nullptr;
       a.mean1 = bump.floats(d.Co); a.rstd1 = bump.floats(d.Co); a.mean2 = bump.floats(d.Co); a.rstd2 = bump.floats(d.Co);
       rb_a.push_back(a);
@@ -376,7 +395,7 @@ size_t Block::plan(char* base) {
       grow((size_t)conv3x3_wgrad_partial_floats(B, d.Ho, d.Wo, d.Co, d.Co, 1));
       grow((size_t)bn_partial_floats(B * d.Ho * d.Wo, d.Co));
     }
-    aux_c = bump.take(aact * esz); aux_y = bump.take(aact * esz); d_aux = bump.take(aact * esz);
+    aux_c = norm_in(aact); aux_y = bump.take(aact * esz); d_aux = bump.take(aact * esz);
     pooled = bump.take((size_t)B * A * esz); dpooled = bump.take((size_t)B * A * esz);
     aux_mean = bump.floats(A); aux_rstd = bump.floats(A);
     r_gA = bump.take(widest * esz); r_gB = bump.take(widest * esz); r_t1 = bump.take(widest * esz);
@@ -388,7 +407,7 @@ size_t Block::plan(char* base) {
   if (o > partial_floats) partial_floats = o;
   if (cfg.arch == PPLL_RESNET && dt == BF16)   // rows of sums that the fused convolutions leave
     for (const BasicBlockDims& d : rb_d)
-      if (conv_bn_ok(dt, B, d.Ho, d.Wo, d.Co)) {
+      if (fused_bn(d.Ho, d.Wo, d.Co)) {
         const size_t f = (size_t)conv_bn_stat_blocks(B, d.Ho, d.Wo, d.Co) * 2 * d.Co;
         if (f > partial_floats) partial_floats = f;
       }
@@ -419,7 +438,7 @@ size_t Block::plan(char* base) {
     arena_floats = (size_t)conv3x3_wgrad_partial_floats(cfg.batch, Hh, W, Ch, A, 2) + 64 +
                    vit_head_partial_floats(cfg.batch, A, cfg.num_classes) + 256;
     for (const BasicBlockDims& d : rb_d) {
-      const size_t here = conv_bn_ok(dt, cfg.batch, d.Ho, d.Wo, d.Co) ? conv_bn_filter_floats(cfg.batch, d.Ho, d.Wo, d.Co) : 0;
+      const size_t here = fused_bn(d.Ho, d.Wo, d.Co) ? conv_bn_filter_floats(cfg.batch, d.Ho, d.Wo, d.Co) : 0;
       arena_floats += std::max((size_t)conv3x3_wgrad_partial_floats(cfg.batch, d.Hin, d.Win, d.Ci, d.Co, d.stride), here) +
                       std::max((size_t)conv3x3_wgrad_partial_floats(cfg.batch, d.Ho, d.Wo, d.Co, d.Co, 1), here) + 128;
     }
@@ -428,6 +447,62 @@ size_t Block::plan(char* base) {
   rq.arena = arena_floats ? bump.floats(arena_floats) : nullptr;
   rq.arena_floats = arena_floats;
   return (bump.off + 255) & ~(size_t)255;
+}
+
+// ------------------------------------------------------------------ group norms of a ResNet block, in BatchNorm's order: stem, two of each basic
+// block, auxiliary
+template <class F> void Block::each_norm(F f) const {
+  if (stem) f(in_h * in_w, in_c);
+  for (const BasicBlockDims& d : rb_d)
+    for (int k = 0; k < 2; ++k) f(d.Ho * d.Wo, d.Co);
+  f(((cfg.height - 1) / 2 + 1) * ((cfg.width - 1) / 2 + 1), cfg.aux_channels);
+}
+GroupNorm Block::group_norm_of(int pixels, int channels, int act) const {
+  return GroupNorm{dt, cfg.batch, pixels, channels, cfg.group_norm, act, cfg.bn_eps};
+}
+size_t Block::norm_workspace() const {
+  size_t most = 0;
+  each_norm([&](int pixels, int channels) { most = std::max(most, group_norm_workspace(group_norm_of(pixels, channels, PPLL_ACT_RELU))); });
+  return most;
+}
+template <class BUMP> void Block::plan_norms(BUMP& bump) {
+  norms.clear();
+  norm_ws = nullptr;
+  norm_x = nullptr;
+  if (!cfg.group_norm) return;
+  size_t widest = 0;
+  each_norm([&](int pixels, int channels) {
+    const size_t rows = (size_t)cfg.batch * pixels;
+    KeptNorm n{};
+    n.stats = bump.floats((size_t)cfg.batch * cfg.group_norm * 2);
+    if (cfg.byte_checkpoints) {
+      n.bytes.ld = pad16(channels);
+      n.bytes.q = (int8_t*)bump.take(rows * n.bytes.ld);
+      n.bytes.e = (int8_t*)bump.take(rows);
+    }
+    norms.push_back(n);
+    widest = std::max(widest, rows * channels);
+  });
+  norm_ws = (char*)bump.take(norm_workspace());
+  if (cfg.byte_checkpoints) norm_x = bump.take(widest * esz);
+}
+// y = ReLU(norm(x) + res) of the `index`-th norm
+int Block::norm_fwd(int index, const void* x, int pixels, int channels, size_t g_off, size_t b_off, const void* res, void* y, hipStream_t s) {
+  const KeptNorm& n = norms[index];
+  auto rows = [&](const void* p) { return ppll_rows{(void*)p, channels}; };
+  return launch_group_norm_fwd(s, group_norm_of(pixels, channels, PPLL_ACT_RELU), rows(x), params + g_off, params + b_off, rows(res), rows(y), n.stats,
+                               n.bytes, norm_ws);
+}
+int Block::norm_eval(const void* x, int pixels, int channels, size_t g_off, size_t b_off, const void* res, void* y, char* room, hipStream_t s) const {
+  auto rows = [&](const void* p) { return ppll_rows{(void*)p, channels}; };
+  return launch_group_norm_fwd(s, group_norm_of(pixels, channels, PPLL_ACT_RELU), rows(x), params + g_off, params + b_off, rows(res), rows(y), nullptr,
+                               ppll_byte_rows{}, room);
+}
+int Block::norm_bwd(int index, const void* x, const void* y, const void* dy, int pixels, int channels, size_t g_off, size_t b_off, void* dx, hipStream_t s) {
+  const KeptNorm& n = norms[index];
+  auto rows = [&](const void* p) { return ppll_rows{(void*)p, channels}; };
+  return launch_group_norm_bwd(s, group_norm_of(pixels, channels, PPLL_ACT_RELU), n.bytes.q ? ppll_rows{} : rows(x), n.bytes, n.stats, params + g_off,
+                               params + b_off, ppll_rows{}, rows(y), rows(dy), rows(dx), ppll_rows{}, grads + g_off, grads + b_off, norm_ws);
 }
 
 // ------------------------------------------------------------------ ViT
@@ -831,7 +906,7 @@ int Block::stem_conv_fwd(const void* x_in, void* xp, void* wp, void* out, hipStr
 
 bool Block::second_filter_from_bn(int i) const {
   const BasicBlockDims& d = rb_d[i];
-  return conv_bn_ok(dt, cfg.batch, d.Ho, d.Wo, d.Co) && conv_bn_filter_floats(cfg.batch, d.Ho, d.Wo, d.Co, units) > 0;
+  return fused_bn(d.Ho, d.Wo, d.Co) && conv_bn_filter_floats(cfg.batch, d.Ho, d.Wo, d.Co, units) > 0;
 }
 bool Block::whole_chain(int i) const { return rb_d[i].stride == 1 && rb_d[i].Ci == rb_d[i].Co && (i > 0 || stem); }
 
@@ -867,7 +942,7 @@ int Block::resnet_step(const void* x_in, const int32_t* labels, void* x_out, hip
   };
   auto conv = [&](const void* in, const void* w, int Hi, int Wi, int Ci, int Co, int stride, void* out, int* ready) -> int {
     *ready = 0;
-    if (stride == 1 && Ci == Co && conv_bn_ok(dt, B, Hi, Wi, Ci)) {
+    if (stride == 1 && Ci == Co && fused_bn(Hi, Wi, Ci)) {
       if (waiting && bn.blocks == 0) PPLL_TRY(launch_bn_sums_fwd_bf16(s, bn.x, bn_rows, bn_c, area, &bn.blocks));
       const bool take = waiting;
       waiting = false;
@@ -878,7 +953,11 @@ int Block::resnet_step(const void* x_in, const int32_t* labels, void* x_out, hip
     PPLL_TRY(apply_bn());
     return launch_conv3x3_fwd(s, in, w, wdt(), dt, B, Hi, Wi, Ci, Co, stride, out, area, ready);
   };
-  if (stem) {
+  if (stem && cfg.group_norm) {
+    PPLL_TRY(stem_conv_fwd(x_in, stem_xp, stem_wp, stem_c, s));
+    PPLL_TRY(norm_fwd(0, stem_c, in_h * in_w, in_c, stem_g, stem_b, nullptr, stem_y, s));
+    x = stem_y;
+  } else if (stem) {
     const int rows0 = B * in_h * in_w;
     int ready = 0;   // partial rows of the BatchNorm sums that the convolution has written itself
     PPLL_TRY(stem_conv_fwd(x_in, stem_xp, stem_wp, stem_c, s, area, &ready));
@@ -892,6 +971,19 @@ int Block::resnet_step(const void* x_in, const int32_t* labels, void* x_out, hip
     const int rows = B * d.Ho * d.Wo, b1 = bn_base + 2 * i, b2 = b1 + 1;
     block_in[i] = x;
     block_out[i] = i == n - 1 ? x_out : a.out;
+    if (cfg.group_norm) {
+      PPLL_TRY(launch_conv3x3_fwd(s, x, wptr(p.conv1_w), wdt(), dt, B, d.Hin, d.Win, d.Ci, d.Co, d.stride, a.c1));
+      PPLL_TRY(norm_fwd(b1, a.c1, d.Ho * d.Wo, d.Co, p.bn1_g, p.bn1_b, nullptr, a.y1, s));
+      PPLL_TRY(launch_conv3x3_fwd(s, a.y1, wptr(p.conv2_w), wdt(), dt, B, d.Ho, d.Wo, d.Co, d.Co, 1, a.c2));
+      const void* skip = x;
+      if (d.stride != 1 || d.Ci != d.Co) {
+        PPLL_TRY(launch_shortcut_fwd(s, x, dt, B, d.Hin, d.Win, d.Ci, d.Co, d.stride, shortcut));
+        skip = shortcut;
+      }
+      PPLL_TRY(norm_fwd(b2, a.c2, d.Ho * d.Wo, d.Co, p.bn2_g, p.bn2_b, skip, block_out[i], s));
+      x = block_out[i];
+      continue;
+    }
     int ready = 0;
     PPLL_TRY(conv(x, wptr(p.conv1_w), d.Hin, d.Win, d.Ci, d.Co, d.stride, a.c1, &ready));
     // y1 is stored where something but the second convolution reads it
@@ -912,9 +1004,14 @@ int Block::resnet_step(const void* x_in, const int32_t* labels, void* x_out, hip
   // ---- auxiliary forward
   const int ba = bn_base + 2 * n;
   int aux_ready = 0;
-  PPLL_TRY(launch_conv3x3_fwd(s, x, wptr(aux_conv_w), wdt(), dt, B, H, W, Ch, A, 2, aux_c, partials, &aux_ready));
-  PPLL_TRY(launch_bn_train_fwd(s, aux_c, dt, arows, A, eps, mom, partials, aux_mean, aux_rstd, run_mean(ba), run_var(ba),
-                               params + aux_bn_g, params + aux_bn_b, nullptr, aux_y, aux_ready));
+  if (cfg.group_norm) {
+    PPLL_TRY(launch_conv3x3_fwd(s, x, wptr(aux_conv_w), wdt(), dt, B, H, W, Ch, A, 2, aux_c));
+    PPLL_TRY(norm_fwd(ba, aux_c, Ho * Wo, A, aux_bn_g, aux_bn_b, nullptr, aux_y, s));
+  } else {
+    PPLL_TRY(launch_conv3x3_fwd(s, x, wptr(aux_conv_w), wdt(), dt, B, H, W, Ch, A, 2, aux_c, partials, &aux_ready));
+    PPLL_TRY(launch_bn_train_fwd(s, aux_c, dt, arows, A, eps, mom, partials, aux_mean, aux_rstd, run_mean(ba), run_var(ba),
+                                 params + aux_bn_g, params + aux_bn_b, nullptr, aux_y, aux_ready));
+  }
   PPLL_TRY(launch_gap_fwd(s, aux_y, dt, B, Ho * Wo, A, pooled));
   if (vit_head_fused_ok(A, C)) {
     // ---- Linear head, local loss and the head's backward in one launch (the fused head without a LayerNorm)
@@ -943,8 +1040,9 @@ int Block::resnet_step(const void* x_in, const int32_t* labels, void* x_out, hip
   }
   // ---- backward: auxiliary net
   PPLL_TRY(launch_gap_bwd(s, dpooled, dt, B, Ho * Wo, A, d_aux));
-  PPLL_TRY(launch_bn_bwd(s, d_aux, aux_y, aux_c, dt, arows, A, aux_mean, aux_rstd, params + aux_bn_g, partials,
-                         grads + aux_bn_g, grads + aux_bn_b, d_aux));
+  if (cfg.group_norm) PPLL_TRY(norm_bwd(ba, aux_c, aux_y, d_aux, Ho * Wo, A, aux_bn_g, aux_bn_b, d_aux, s));
+  else PPLL_TRY(launch_bn_bwd(s, d_aux, aux_y, aux_c, dt, arows, A, aux_mean, aux_rstd, params + aux_bn_g, partials,
+                              grads + aux_bn_g, grads + aux_bn_b, d_aux));
   PPLL_TRY(launch_conv3x3_wgrad(s, x, d_aux, dt, B, H, W, Ch, A, 2, rq, grads + aux_conv_w));
   void *gcur = r_gA, *gnext = r_gB;   // gradient with respect to the output of the block in hand / of the one before it
   PPLL_TRY(launch_conv3x3_dgrad(s, d_aux, wptr(aux_conv_w), wdt(), dt, B, H, W, Ch, A, 2, nullptr, nullptr, gcur));
@@ -981,7 +1079,24 @@ int Block::resnet_step(const void* x_in, const int32_t* labels, void* x_out, hip
     const BasicBlockDims& d = rb_d[i];
     BasicBlockActs& a = rb_a[i];
     const int rows = B * d.Ho * d.Wo;
-    const bool fused = conv_bn_ok(dt, B, d.Ho, d.Wo, d.Co), identity = d.stride == 1 && d.Ci == d.Co;
+    const bool fused = fused_bn(d.Ho, d.Wo, d.Co), identity = d.stride == 1 && d.Ci == d.Co;
+    if (cfg.group_norm) {
+      const int b1 = bn_base + 2 * i;
+      PPLL_TRY(norm_bwd(b1 + 1, a.c2, block_out[i], gcur, d.Ho * d.Wo, d.Co, p.bn2_g, p.bn2_b, a.d2, s));
+      defer(a.y1, a.d2, grads + p.conv2_w, d.Ho, d.Wo, d.Co, d.Co, 1);
+      PPLL_TRY(launch_conv3x3_dgrad(s, a.d2, wptr(p.conv2_w), wdt(), dt, B, d.Ho, d.Wo, d.Co, d.Co, 1, nullptr, nullptr, r_t1));
+      PPLL_TRY(norm_bwd(b1, a.c1, a.y1, r_t1, d.Ho * d.Wo, d.Co, p.bn1_g, p.bn1_b, a.d1, s));
+      defer(block_in[i], a.d1, grads + p.conv1_w, d.Hin, d.Win, d.Ci, d.Co, d.stride);
+      if (i == 0 && !stem) break;   // the block input is the detached x_{j-1}
+      if (identity) {
+        PPLL_TRY(launch_conv3x3_dgrad(s, a.d1, wptr(p.conv1_w), wdt(), dt, B, d.Hin, d.Win, d.Ci, d.Co, 1, gcur, block_out[i], gcur));
+      } else {
+        PPLL_TRY(launch_conv3x3_dgrad(s, a.d1, wptr(p.conv1_w), wdt(), dt, B, d.Hin, d.Win, d.Ci, d.Co, d.stride, nullptr, nullptr, gnext));
+        PPLL_TRY(launch_shortcut_bwd(s, gcur, block_out[i], dt, B, d.Hin, d.Win, d.Ci, d.Co, d.stride, gnext));
+        std::swap(gcur, gnext);
+      }
+      continue;
+    }
     const bool filters = second_filter_from_bn(i);
     if (!filters) defer(a.y1, a.d2, grads + p.conv2_w, d.Ho, d.Wo, d.Co, d.Co, 1);
     if (fused) {
@@ -1027,8 +1142,9 @@ int Block::resnet_step(const void* x_in, const int32_t* labels, void* x_out, hip
                                         shapes[k].Ci, shapes[k].Co, shapes[k].stride, rq));
   if (stem) {
     const int rows0 = B * in_h * in_w;
-    PPLL_TRY(launch_bn_bwd(s, gcur, stem_y, stem_c, dt, rows0, in_c, stem_mean, stem_rstd, params + stem_g, area,
-                           grads + stem_g, grads + stem_b, r_t1, ready));
+    if (cfg.group_norm) PPLL_TRY(norm_bwd(0, stem_c, stem_y, gcur, in_h * in_w, in_c, stem_g, stem_b, r_t1, s));
+    else PPLL_TRY(launch_bn_bwd(s, gcur, stem_y, stem_c, dt, rows0, in_c, stem_mean, stem_rstd, params + stem_g, area,
+                                grads + stem_g, grads + stem_b, r_t1, ready));
     if (stem_pad)   // the padded image is still in place from the forward pass
       PPLL_TRY(launch_conv3x3_wgrad(s, stem_xp, r_t1, dt, B, in_h, in_w, 16, in_c, 1, rq, grads + stem_w, cfg.img_c));
     else
@@ -1058,6 +1174,7 @@ int Block::forward_eval(const void* x_in, void* x_out, float* logits_out, hipStr
   e.patches = patches; e.embed_tmp = embed_tmp; e.x0 = x0; e.z = z; e.head_mean = head_mean; e.head_rstd = head_rstd;
   e.stem_c = stem_c; e.stem_y = stem_y; e.stem_xp = stem_xp; e.stem_wp = stem_wp; e.shortcut = shortcut;
   e.aux_c = aux_c; e.aux_y = aux_y; e.pooled = pooled;
+  e.norm_ws = norm_ws;
   e.stem_mean = stem_mean; e.stem_rstd = stem_rstd; e.aux_mean = aux_mean; e.aux_rstd = aux_rstd;
   return forward_eval_with(e, x_in, x_out, logits_out, s);
 }
@@ -1112,6 +1229,7 @@ size_t Block::plan_eval_scratch(char* base, EvalBuffers* e) const {
     e->aux_c = bump.take(B * Ho * Wo * A * esz); e->aux_y = bump.take(B * Ho * Wo * A * esz);
     e->pooled = bump.take(B * A * esz);
     e->aux_mean = bump.floats(A); e->aux_rstd = bump.floats(A);
+    e->norm_ws = cfg.group_norm ? (char*)bump.take(norm_workspace()) : nullptr;
   }
   return (bump.off + 255) & ~(size_t)255;
 }
@@ -1187,9 +1305,10 @@ int Block::forward_eval_with(const EvalBuffers& e, const void* x_in, void* x_out
   const void* x = x_in;
   if (stem) {
     PPLL_TRY(stem_conv_fwd(x_in, e.stem_xp, e.stem_wp, e.stem_c, s));
-    PPLL_TRY(launch_bn_running_stats(s, bn_mean_run + bn_off[0], bn_var_run + bn_off[0], in_c, eps, e.stem_mean, e.stem_rstd));
-    PPLL_TRY(launch_bn_apply(s, e.stem_c, dt, B * in_h * in_w, in_c, e.stem_mean, e.stem_rstd, params + stem_g, params + stem_b,
-                             nullptr, e.stem_y, units));
+    if (cfg.group_norm) PPLL_TRY(norm_eval(e.stem_c, in_h * in_w, in_c, stem_g, stem_b, nullptr, e.stem_y, e.norm_ws, s));
+    else PPLL_TRY(launch_bn_running_stats(s, bn_mean_run + bn_off[0], bn_var_run + bn_off[0], in_c, eps, e.stem_mean, e.stem_rstd));
+    if (!cfg.group_norm) PPLL_TRY(launch_bn_apply(s, e.stem_c, dt, B * in_h * in_w, in_c, e.stem_mean, e.stem_rstd, params + stem_g, params + stem_b,
+                                                  nullptr, e.stem_y, units));
     x = e.stem_y;
   }
   for (int i = 0; i < n; ++i) {
@@ -1199,24 +1318,33 @@ int Block::forward_eval_with(const EvalBuffers& e, const void* x_in, void* x_out
     const int rows = B * d.Ho * d.Wo, b1 = bn_base + 2 * i, b2 = b1 + 1;
     void* out = i == n - 1 ? x_out : a.out;
     PPLL_TRY(launch_conv3x3_fwd(s, x, wptr(p.conv1_w), wdt(), dt, B, d.Hin, d.Win, d.Ci, d.Co, d.stride, a.c1));
-    PPLL_TRY(launch_bn_running_stats(s, bn_mean_run + bn_off[b1], bn_var_run + bn_off[b1], d.Co, eps, a.mean1, a.rstd1));
-    PPLL_TRY(launch_bn_apply(s, a.c1, dt, rows, d.Co, a.mean1, a.rstd1, params + p.bn1_g, params + p.bn1_b, nullptr, a.y1, units));
+    if (cfg.group_norm) {
+      PPLL_TRY(norm_eval(a.c1, d.Ho * d.Wo, d.Co, p.bn1_g, p.bn1_b, nullptr, a.y1, e.norm_ws, s));
+    } else {
+      PPLL_TRY(launch_bn_running_stats(s, bn_mean_run + bn_off[b1], bn_var_run + bn_off[b1], d.Co, eps, a.mean1, a.rstd1));
+      PPLL_TRY(launch_bn_apply(s, a.c1, dt, rows, d.Co, a.mean1, a.rstd1, params + p.bn1_g, params + p.bn1_b, nullptr, a.y1, units));
+    }
     PPLL_TRY(launch_conv3x3_fwd(s, a.y1, wptr(p.conv2_w), wdt(), dt, B, d.Ho, d.Wo, d.Co, d.Co, 1, a.c2));
-    PPLL_TRY(launch_bn_running_stats(s, bn_mean_run + bn_off[b2], bn_var_run + bn_off[b2], d.Co, eps, a.mean2, a.rstd2));
+    if (!cfg.group_norm) PPLL_TRY(launch_bn_running_stats(s, bn_mean_run + bn_off[b2], bn_var_run + bn_off[b2], d.Co, eps, a.mean2, a.rstd2));
     const void* skip = x;
     if (d.stride != 1 || d.Ci != d.Co) {
       PPLL_TRY(launch_shortcut_fwd(s, x, dt, B, d.Hin, d.Win, d.Ci, d.Co, d.stride, e.shortcut));
       skip = e.shortcut;
     }
-    PPLL_TRY(launch_bn_apply(s, a.c2, dt, rows, d.Co, a.mean2, a.rstd2, params + p.bn2_g, params + p.bn2_b, skip, out, units));
+    if (cfg.group_norm) PPLL_TRY(norm_eval(a.c2, d.Ho * d.Wo, d.Co, p.bn2_g, p.bn2_b, skip, out, e.norm_ws, s));
+    else PPLL_TRY(launch_bn_apply(s, a.c2, dt, rows, d.Co, a.mean2, a.rstd2, params + p.bn2_g, params + p.bn2_b, skip, out, units));
     x = out;
   }
   if (!logits_out) return PPLL_OK;
   PPLL_TRY(launch_conv3x3_fwd(s, x, wptr(aux_conv_w), wdt(), dt, B, H, W, Ch, A, 2, e.aux_c));
-  PPLL_TRY(launch_bn_running_stats(s, bn_mean_run + bn_off[bn_base + 2 * n], bn_var_run + bn_off[bn_base + 2 * n], A, eps,
-                                   e.aux_mean, e.aux_rstd));
-  PPLL_TRY(launch_bn_apply(s, e.aux_c, dt, arows, A, e.aux_mean, e.aux_rstd, params + aux_bn_g, params + aux_bn_b, nullptr,
-                           e.aux_y, units));
+  if (cfg.group_norm) {
+    PPLL_TRY(norm_eval(e.aux_c, Ho * Wo, A, aux_bn_g, aux_bn_b, nullptr, e.aux_y, e.norm_ws, s));
+  } else {
+    PPLL_TRY(launch_bn_running_stats(s, bn_mean_run + bn_off[bn_base + 2 * n], bn_var_run + bn_off[bn_base + 2 * n], A, eps,
+                                     e.aux_mean, e.aux_rstd));
+    PPLL_TRY(launch_bn_apply(s, e.aux_c, dt, arows, A, e.aux_mean, e.aux_rstd, params + aux_bn_g, params + aux_bn_b, nullptr,
+                             e.aux_y, units));
+  }
   PPLL_TRY(launch_gap_fwd(s, e.aux_y, dt, B, Ho * Wo, A, e.pooled));
   g.A = e.pooled; g.a_dt = dt; g.a_sm = A; g.a_sk = 1;
   g.B = params + head_w; g.b_dt = F32; g.b_sk = C; g.b_sn = 1;
