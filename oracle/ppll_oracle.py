@@ -101,6 +101,8 @@ class BlockConfig:
     # ResNet: group norms of so many groups in the place of the BatchNorms; their inputs kept in 8 bits for the backward pass
     group_norm: int = 0
     byte_checkpoints: int = 0
+    # ViT: the linear products of the encoder layers on rows of 8 bits, tokens and output channels a row each; gradients at those values
+    byte_products: int = 0
 
 
 # --------------------------------------------------------------------------
@@ -607,30 +609,42 @@ def _qk_bwd(dqkv, cache, p, pre, grads, cfg):
     return out
 
 
+def _in_bytes(x, p, name, st):
+    """Input and weight of a linear product as it reads them: rounded to rows of 8 bits with byte_products."""
+    w = p[name]
+    if not st.cfg.byte_products:
+        return x, w
+    rounded = lambda a: byte_values(*byte_rows(a)).astype(a.dtype)
+    return rounded(x.reshape(-1, x.shape[-1])).reshape(x.shape), rounded(w.T).T
+
+
 def _encoder_fwd(x, p, pre, st):
     cfg = st.cfg
     u, c_ln1 = layernorm_fwd(x, p[pre + ".ln1.g"], p[pre + ".ln1.b"], cfg.ln_eps)
-    qkv = linear_fwd(u, p[pre + ".qkv.w"], p[pre + ".qkv.b"])
+    u, w_qkv = _in_bytes(u, p, pre + ".qkv.w", st)
+    qkv = linear_fwd(u, w_qkv, p[pre + ".qkv.b"])
     qkv, c_qk = _qk_fwd(qkv, p, pre, cfg)
     o, c_att = attention_fwd(qkv, cfg.heads)
-    x1 = x + linear_fwd(o, p[pre + ".proj.w"], p[pre + ".proj.b"])
+    o, w_proj = _in_bytes(o, p, pre + ".proj.w", st)
+    x1 = x + linear_fwd(o, w_proj, p[pre + ".proj.b"])
     u2, c_ln2 = layernorm_fwd(x1, p[pre + ".ln2.g"], p[pre + ".ln2.b"], cfg.ln_eps)
-    h = linear_fwd(u2, p[pre + ".fc1.w"], p[pre + ".fc1.b"])
-    gl = gelu_fwd(h)
-    x2 = x1 + linear_fwd(gl, p[pre + ".fc2.w"], p[pre + ".fc2.b"])
-    return x2, (c_ln1, u, c_qk, c_att, o, c_ln2, u2, h, gl)
+    u2, w_fc1 = _in_bytes(u2, p, pre + ".fc1.w", st)
+    h = linear_fwd(u2, w_fc1, p[pre + ".fc1.b"])
+    gl, w_fc2 = _in_bytes(gelu_fwd(h), p, pre + ".fc2.w", st)
+    x2 = x1 + linear_fwd(gl, w_fc2, p[pre + ".fc2.b"])
+    return x2, (c_ln1, u, c_qk, c_att, o, c_ln2, u2, h, gl, w_qkv, w_proj, w_fc1, w_fc2)
 
 
 def _encoder_bwd(dx2, cache, p, pre, grads, st):
-    c_ln1, u, c_qk, c_att, o, c_ln2, u2, h, gl = cache
-    dgl, grads[pre + ".fc2.w"], grads[pre + ".fc2.b"] = linear_bwd(dx2, gl, p[pre + ".fc2.w"])
+    c_ln1, u, c_qk, c_att, o, c_ln2, u2, h, gl, w_qkv, w_proj, w_fc1, w_fc2 = cache
+    dgl, grads[pre + ".fc2.w"], grads[pre + ".fc2.b"] = linear_bwd(dx2, gl, w_fc2)
     dh = gelu_bwd(dgl, h)
-    du2, grads[pre + ".fc1.w"], grads[pre + ".fc1.b"] = linear_bwd(dh, u2, p[pre + ".fc1.w"])
+    du2, grads[pre + ".fc1.w"], grads[pre + ".fc1.b"] = linear_bwd(dh, u2, w_fc1)
     d, grads[pre + ".ln2.g"], grads[pre + ".ln2.b"] = layernorm_bwd(du2, c_ln2, p[pre + ".ln2.g"])
     dx1 = dx2 + d
-    do, grads[pre + ".proj.w"], grads[pre + ".proj.b"] = linear_bwd(dx1, o, p[pre + ".proj.w"])
+    do, grads[pre + ".proj.w"], grads[pre + ".proj.b"] = linear_bwd(dx1, o, w_proj)
     dqkv = _qk_bwd(attention_bwd(do, c_att), c_qk, p, pre, grads, st.cfg)
-    du, grads[pre + ".qkv.w"], grads[pre + ".qkv.b"] = linear_bwd(dqkv, u, p[pre + ".qkv.w"])
+    du, grads[pre + ".qkv.w"], grads[pre + ".qkv.b"] = linear_bwd(dqkv, u, w_qkv)
     d, grads[pre + ".ln1.g"], grads[pre + ".ln1.b"] = layernorm_bwd(du, c_ln1, p[pre + ".ln1.g"])
     return dx1 + d
 

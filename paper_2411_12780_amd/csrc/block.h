@@ -27,6 +27,8 @@ struct EncoderActs {     // saved by the forward for the backward (h: gelu' at t
   void *u1, *qkv, *att, *x1, *u2, *h, *gl, *x2;
   void* qk = nullptr;      // queries and keys as projected [M, 2D], where they are normalised; null: nothing is kept
   float *mean1, *rstd1, *mean2, *rstd2, *lse;
+  // with byte_products: what the four products read, tokens and weights, in 8 bits
+  ppll_byte_rows u1_8{}, att_8{}, u2_8{}, gl_8{}, qkv_8{}, proj_8{}, fc1_8{}, fc2_8{};
 };
 // Compact buffers of the last auxiliary encoder layer, of which only the class-token row is computed behind the
 // key / value projection ([B, .] instead of [B*T, .]; see Block::encoder_fwd_cls).
@@ -239,6 +241,11 @@ struct Block {
   // two are launches of their own
   int encoder_fwd(int l, const EncoderActs& a, const void* x, void* x2_out, const EncoderActs* next, hipStream_t s,
                   const std::function<int()>& stored = nullptr);
+  char* byte_ws = nullptr;      // of the backward products on rows of 8 bits
+  ByteLinear byte_linear(int in, int out, int act = PPLL_ACT_NONE) const;
+  template <class BUMP> void plan_byte_acts(BUMP& bump, EncoderActs* a) const;
+  int encoder_fwd_bytes(int l, const EncoderActs& a, const void* x, void* x2_out, const EncoderActs* next, hipStream_t s, const std::function<int()>& stored);
+  int encoder_bwd_bytes(int l, const void* x, const void* g_in, void* g_tmp, void* g_out, bool need_dx, hipStream_t s);
   int first_norm(int l, const EncoderActs& a, const void* x, hipStream_t s);
   NormOut first_norm_out(int l, const EncoderActs& a) const;
   int forward_eval_with(const EvalBuffers& e, const void* x_in, void* x_out, float* logits_out, hipStream_t s);

@@ -70,6 +70,7 @@ int validate_config(const ppll_block_config* c) {
     if ((c->rotary | c->qk_norm) & ~1) return bad("rotary and qk_norm must be 0 or 1");
     if (c->group_norm || c->byte_checkpoints) return bad("group norm belongs to ResNet blocks");
     if (c->byte_products & ~1) return bad("byte_products must be 0 or 1");
+    if (c->byte_products && (c->dim > BYTE_COLS / 3 || c->mlp_dim > BYTE_COLS)) return bad("3 dim or mlp_dim above 65536 with products in 8 bits");
     if (c->rotary || c->qk_norm) {
       const int dh = c->dim / c->heads;
       if (dh % 2 || dh > 2 * ROTARY_PAIRS) return bad("rotary positions and qk_norm need an even head width of 256 at most");
@@ -292,11 +293,16 @@ size_t Block::plan(char* base) {
       embed_tmp = bump.take((size_t)B * (T - 1) * D * esz);
       x0 = bump.take(M * D * esz);
     }
+    byte_ws = nullptr;
     for (int l = 0; l < cfg.depth + cfg.aux_depth; ++l) {
       EncoderActs a;
-      a.u1 = bump.take(M * D * esz); a.qkv = bump.take(M * 3 * D * esz); a.att = bump.take(M * D * esz);
-      a.x1 = bump.take(M * D * esz); a.u2 = bump.take(M * D * esz);
-      a.h = bump.take(M * F * esz); a.gl = bump.take(M * F * esz);
+      // what a product on rows of 8 bits reads stays in those alone: one buffer of each width for all layers
+      const bool first = !cfg.byte_products || l == 0;
+      auto product_in = [&](void* of_all, size_t elems) { return first ? bump.take(elems * esz) : of_all; };
+      a.u1 = product_in(l ? enc_a[0].u1 : nullptr, M * D); a.qkv = bump.take(M * 3 * D * esz); a.att = bump.take(M * D * esz);
+      a.x1 = bump.take(M * D * esz); a.u2 = cfg.byte_products ? a.u1 : bump.take(M * D * esz);
+      a.h = bump.take(M * F * esz); a.gl = product_in(l ? enc_a[0].gl : nullptr, M * F);
+      if (cfg.byte_products) plan_byte_acts(bump, &a);
       a.x2 = bump.take(M * D * esz);
       a.mean1 = bump.floats(M); a.rstd1 = bump.floats(M); a.mean2 = bump.floats(M); a.rstd2 = bump.floats(M);
       a.lse = bump.floats((size_t)B * H * T);
@@ -317,7 +323,7 @@ size_t Block::plan(char* base) {
       rope_pos = (int32_t*)bump.take((size_t)T * 2 * sizeof(int32_t));
     }
     z = bump.take((size_t)B * D * esz); dz = bump.take((size_t)B * D * esz); dcls = bump.take((size_t)B * D * esz);
-    prune_cls = cfg.aux_depth >= 1 && attention_cls_lds_bytes(T, D / H) <= 160 * 1024;
+    prune_cls = cfg.aux_depth >= 1 && !cfg.byte_products && attention_cls_lds_bytes(T, D / H) <= 160 * 1024;
     if (prune_cls) {
       ClsActs& c = cls_a;
       const size_t bd = (size_t)B * D * esz, bf = (size_t)B * F * esz;
@@ -333,13 +339,23 @@ size_t Block::plan(char* base) {
     const int layers = cfg.depth + cfg.aux_depth;
     for (int l = 0; l <= layers; ++l) g_res.push_back(bump.take(M * D * esz));
     for (int l = 0; l < layers; ++l) {
+      if (l && cfg.byte_products) {     // whose weight gradients are formed at once
+        g_mid.push_back(g_mid[0]); d_h.push_back(d_h[0]); d_qkv.push_back(d_qkv[0]);
+        continue;
+      }
       g_mid.push_back(bump.take(M * D * esz));
       d_h.push_back(bump.take(M * F * esz));
       d_qkv.push_back(bump.take(M * 3 * D * esz));
     }
+    if (cfg.byte_products) {
+      size_t most = 0;
+      for (const ByteLinear& b : {byte_linear((int)D, (int)(3 * D)), byte_linear((int)D, (int)D), byte_linear((int)D, (int)F), byte_linear((int)F, (int)D)})
+        most = std::max(most, byte_linear_workspace(b));
+      byte_ws = (char*)bump.take(most);
+    }
     if (dt == BF16) {   // parts of divided tiles of the weight-gradient launch at the end of the backward pass
       const std::vector<GemmArgs> set = weight_grads();
-      wgrad_big = wgrad_any_order() && gemm_big_grads_choice(set.data(), (int)set.size(), &wgrad_ws_floats);
+      wgrad_big = !set.empty() && wgrad_any_order() && gemm_big_grads_choice(set.data(), (int)set.size(), &wgrad_ws_floats);
       if (!wgrad_big) wgrad_ws_floats = gemm_mfma_balanced_floats();
       wgrad_ws = wgrad_ws_floats ? bump.floats(wgrad_ws_floats) : nullptr;
     }
@@ -549,6 +565,7 @@ int Block::qk_bwd(int l, void* dq, long q_ld, int q_rows, int q_tokens, const vo
 
 int Block::encoder_fwd(int l, const EncoderActs& a, const void* x, void* x2_out, const EncoderActs* next, hipStream_t s,
                        const std::function<int()>& stored) {
+  if (cfg.byte_products) return encoder_fwd_bytes(l, a, x, x2_out, next, s, stored);
   const int D = cfg.dim, F = cfg.mlp_dim, T = cfg.tokens, H = cfg.heads, M = cfg.batch * T;
   const EncoderParams& p = enc_p[l];
   GemmArgs g = gemm_args();
@@ -586,6 +603,7 @@ int Block::encoder_fwd(int l, const EncoderActs& a, const void* x, void* x2_out,
 // g_in: gradient w.r.t. the layer output; g_tmp receives the gradient at the
 // mid-layer residual; g_out the gradient w.r.t. the layer input.
 int Block::encoder_bwd(int l, const void* x, const void* g_in, void* g_tmp, void* g_out, bool need_dx, hipStream_t s) {
+  if (cfg.byte_products) return encoder_bwd_bytes(l, x, g_in, g_tmp, g_out, need_dx, s);
   const int D = cfg.dim, F = cfg.mlp_dim, T = cfg.tokens, H = cfg.heads, M = cfg.batch * T;
   const EncoderParams& p = enc_p[l];
   EncoderActs& a = enc_a[l];
@@ -627,6 +645,70 @@ int Block::encoder_bwd(int l, const void* x, const void* g_in, void* g_tmp, void
   return wgrad(a.u1, D, d_qkv, 3 * D, p.qkv_w, p.qkv_b);
 }
 
+// ---- the encoder layer with its products on rows of 8 bits
+ByteLinear Block::byte_linear(int in, int out, int act) const { return ByteLinear{dt, cfg.batch * cfg.tokens, in, out, act}; }
+template <class BUMP> void Block::plan_byte_acts(BUMP& bump, EncoderActs* a) const {
+  const size_t M = (size_t)cfg.batch * cfg.tokens;
+  const int D = cfg.dim, F = cfg.mlp_dim;
+  auto rows = [&](size_t n, int cols) {
+    ppll_byte_rows r;
+    r.ld = pad16(cols);
+    r.q = (int8_t*)bump.take(n * r.ld);
+    r.e = (int8_t*)bump.take(n);
+    return r;
+  };
+  a->u1_8 = rows(M, D); a->att_8 = rows(M, D); a->u2_8 = rows(M, D); a->gl_8 = rows(M, F);
+  a->qkv_8 = rows(3 * D, D); a->proj_8 = rows(D, D); a->fc1_8 = rows(F, D); a->fc2_8 = rows(D, F);
+}
+// The weights are brought into 8 bits here and not by the optimizer: 12 of a step's bytes per weight beside the 20 and more that the update moves, and
+// tensors that a caller writes, and evaluations, need nothing of their own.
+int Block::encoder_fwd_bytes(int l, const EncoderActs& a, const void* x, void* x2_out, const EncoderActs* next, hipStream_t s,
+                             const std::function<int()>& stored) {
+  const int D = cfg.dim, F = cfg.mlp_dim, T = cfg.tokens, H = cfg.heads, M = cfg.batch * T;
+  const EncoderParams& p = enc_p[l];
+  auto rows = [](const void* v, int64_t ld) { return ppll_rows{(void*)v, ld}; };
+  auto product = [&](const void* in, const ppll_byte_rows& in8, size_t w, const ppll_byte_rows& w8, size_t b, int from, int to, const ppll_rows& residual, void* out,
+                     int act = PPLL_ACT_NONE, void* slope = nullptr) -> int {
+    PPLL_TRY(launch_byte_rows_pack(s, dt, M, from, rows(in, from), in8));
+    PPLL_TRY(launch_byte_rows_pack_columns(s, F32, from, to, rows(params + w, to), w8));
+    return launch_byte_linear_fwd(s, byte_linear(from, to, act), in8, w8, params + b, residual, rows(out, to), slope ? rows(slope, to) : ppll_rows{});
+  };
+  PPLL_TRY(product(a.u1, a.u1_8, p.qkv_w, a.qkv_8, p.qkv_b, D, 3 * D, ppll_rows{}, a.qkv));
+  if (qk_prepared()) {
+    char *q = (char*)a.qkv, *keep = (char*)a.qk;
+    PPLL_TRY(qk_fwd(l, q, 3 * D, M, T, keep, 2 * D, q + D * esz, 3 * D, keep ? keep + D * esz : nullptr, 2 * D, s));
+  }
+  PPLL_TRY(launch_attention_fwd(s, a.qkv, dt, cfg.batch, T, H, D / H, a.att, a.lse));
+  PPLL_TRY(product(a.att, a.att_8, p.proj_w, a.proj_8, p.proj_b, D, D, rows(x, D), a.x1));
+  PPLL_TRY(launch_layernorm_fwd(s, a.x1, dt, D, M, D, params + p.ln2_g, params + p.ln2_b, cfg.ln_eps, a.u2, a.mean2, a.rstd2));
+  PPLL_TRY(product(a.u2, a.u2_8, p.fc1_w, a.fc1_8, p.fc1_b, D, F, ppll_rows{}, a.gl, PPLL_ACT_GELU, a.h));
+  PPLL_TRY(product(a.gl, a.gl_8, p.fc2_w, a.fc2_8, p.fc2_b, F, D, rows(a.x1, D), x2_out));
+  if (stored) PPLL_TRY(stored());
+  return next ? first_norm(l + 1, *next, x2_out, s) : PPLL_OK;
+}
+int Block::encoder_bwd_bytes(int l, const void* x, const void* g_in, void* g_tmp, void* g_out, bool need_dx, hipStream_t s) {
+  const int D = cfg.dim, F = cfg.mlp_dim, T = cfg.tokens, H = cfg.heads, M = cfg.batch * T;
+  const EncoderParams& p = enc_p[l];
+  EncoderActs& a = enc_a[l];
+  void *d_h = this->d_h[l], *d_qkv = this->d_qkv[l];
+  auto rows = [](const void* v, int64_t ld) { return ppll_rows{(void*)v, ld}; };
+  auto product = [&](const void* dy, int from, int to, const ppll_byte_rows& in8, const ppll_byte_rows& w8, const ppll_rows& gate, void* dx, size_t w, size_t b) {
+    return launch_byte_linear_bwd(s, byte_linear(from, to), in8, w8, rows(dy, to), gate, rows(dx, from), grads + w, grads + b, byte_ws);
+  };
+  PPLL_TRY(product(g_in, F, D, a.gl_8, a.fc2_8, rows(a.h, F), d_h, p.fc2_w, p.fc2_b));
+  PPLL_TRY(product(d_h, D, F, a.u2_8, a.fc1_8, ppll_rows{}, d_u, p.fc1_w, p.fc1_b));
+  PPLL_TRY(launch_layernorm_bwd(s, d_u, a.x1, dt, D, M, D, params + p.ln2_g, a.mean2, a.rstd2, g_in, 1, g_tmp, rq, grads + p.ln2_g, grads + p.ln2_b));
+  PPLL_TRY(product(g_tmp, D, D, a.att_8, a.proj_8, ppll_rows{}, d_u, p.proj_w, p.proj_b));
+  PPLL_TRY(launch_attention_bwd(s, a.qkv, a.att, d_u, a.lse, dt, cfg.batch, T, H, D / H, d_qkv));
+  if (qk_prepared()) {
+    char *d = (char*)d_qkv, *raw = (char*)a.qk;
+    PPLL_TRY(qk_bwd(l, d, 3 * D, M, T, raw, 2 * D, d + D * esz, 3 * D, raw ? raw + D * esz : nullptr, 2 * D, s));
+  }
+  PPLL_TRY(product(d_qkv, D, 3 * D, a.u1_8, a.qkv_8, ppll_rows{}, d_u, p.qkv_w, p.qkv_b));
+  return launch_layernorm_bwd(s, d_u, x, dt, D, M, D, params + p.ln1_g, a.mean1, a.rstd1, g_tmp, 1, need_dx ? g_out : nullptr, rq, grads + p.ln1_g,
+                              grads + p.ln1_b);
+}
+
 GemmArgs Block::wgrad_args(const void* xin, long x_ld, int in_dim, const void* dy, long dy_ld, int out_dim, int K, float* dW, long ldw,
                            float* db) const {
   GemmArgs g = gemm_args();
@@ -647,7 +729,7 @@ std::vector<GemmArgs> Block::weight_grads() const {
     const GemmArgs g = wgrad_args(xin, x_ld, in_dim, dy, dy_ld, out_dim, K, grad(w_off), ldw, grad(b_off));
     if (gemm_weight_grad_groupable(g)) set.push_back(g);
   };
-  for (int l = cfg.depth + cfg.aux_depth - 1; l >= 0; --l) {
+  for (int l = cfg.byte_products ? -1 : cfg.depth + cfg.aux_depth - 1; l >= 0; --l) {
     const EncoderParams& p = enc_p[l];
     const EncoderActs& a = enc_a[l];
     if (prune_cls && l == cfg.depth + cfg.aux_depth - 1) {
@@ -1196,6 +1278,7 @@ size_t Block::plan_eval_scratch(char* base, EvalBuffers* e) const {
     a.h = bump.take(M * F * esz); a.gl = bump.take(M * F * esz);
     a.mean1 = bump.floats(M); a.rstd1 = bump.floats(M); a.mean2 = bump.floats(M); a.rstd2 = bump.floats(M);
     a.lse = bump.floats(B * H * T);
+    if (cfg.byte_products) plan_byte_acts(bump, &a);
     e->shared_enc[0] = a; e->shared_enc[1] = a;      // (qk null: an evaluation keeps no queries and keys)
     e->shared_enc[0].x2 = bump.take(M * D * esz);
     e->shared_enc[1].x2 = bump.take(M * D * esz);

@@ -25,7 +25,8 @@ def test_refused_resnet_configurations(bad):
     assert e.value.status == 2
 
 
-@pytest.mark.parametrize("bad", [dict(group_norm=8), dict(byte_checkpoints=1), dict(reserved=1)])
+@pytest.mark.parametrize("bad", [dict(group_norm=8), dict(byte_checkpoints=1), dict(reserved=1), dict(byte_products=2), dict(byte_products=-1),
+                                 dict(byte_products=1, mlp_dim=65537), dict(byte_products=1, dim=21848, heads=8)])
 def test_refused_vit_configurations(bad):
     with pytest.raises(P.PpllError) as e:
         size(synth.workload("vit_tiny_fp32", **bad))
@@ -55,6 +56,16 @@ def test_inputs_kept_in_bytes_take_less_memory():
     maps = 10 * 128 * 16 * 16 * 32                # elements that the norms of five basic blocks read
     # in the place of 2 bytes an element: 1 byte and 1/32 for the exponent; one map of full width for the next product's output
     assert size(wl) - size(dict(wl, byte_checkpoints=1)) >= maps * (2 - 1 - 1 / 32) - 2 * maps / 10 - (1 << 20)
+
+
+def test_products_in_bytes_take_less_memory():
+    wl = synth.workload("vit_stage_act_bf16")
+    M, D, F, layers = wl["batch"] * wl["tokens"], wl["dim"], wl["mlp_dim"], wl["depth"] + wl["aux_depth"]
+    # for all layers but one, what the products read, in 2 bytes an element: the norms' outputs (2 D wide) and the MLP's middle (F); and gradients of 4 D + F
+    # that wait for a launch at the end.  In their place a byte, and one of attention's output (D), that attention's backward keeps as it is too
+    saved = (layers - 1) * M * (2 * (2 * D + F) + 2 * (4 * D + F) - (3 * D + F))
+    weights = layers * (4 * D * D + 2 * D * F)
+    assert size(wl) - size(dict(wl, byte_products=1)) >= 0.5 * saved - weights > 0
 
 
 def test_there_are_no_running_statistics():
