@@ -105,9 +105,10 @@ typedef struct {
    * byte_checkpoints: those norms keep their inputs in 8 bits for the backward pass, which reads them; the maps themselves share one buffer. */
   int32_t group_norm;
   int32_t byte_checkpoints;         /* 0 or 1 (with group_norm)                  */
-  /* ViT: the four linear products of every encoder layer on rows of 8 bits (ppll_byte_linear_forward): tokens and weights are brought into 8 bits in
+  /* ViT: the four linear products of the encoder layers on rows of 8 bits (ppll_byte_linear_forward): tokens and weights are brought into 8 bits in
    * every step, the tokens stay so for the weight gradients, and gradients are those at the values in 8 bits, the weight's taken over by the fp32
-   * master weights. */
+   * master weights.  The last layer of an auxiliary network, of which only the class token's row goes on, stays in `precision`.  mlp_dim and 3 * dim
+   * are 65536 at most. */
   int32_t byte_products;            /* 0 or 1                                    */
   int32_t reserved;                 /* 0                                         */
 } ppll_block_config;

@@ -101,7 +101,8 @@ class BlockConfig:
     # ResNet: group norms of so many groups in the place of the BatchNorms; their inputs kept in 8 bits for the backward pass
     group_norm: int = 0
     byte_checkpoints: int = 0
-    # ViT: the linear products of the encoder layers on rows of 8 bits, tokens and output channels a row each; gradients at those values
+    # ViT: the linear products of the encoder layers on rows of 8 bits, tokens and output channels a row each; gradients at those values.  Not of
+    # the auxiliary network's last layer
     byte_products: int = 0
 
 
@@ -612,7 +613,7 @@ def _qk_bwd(dqkv, cache, p, pre, grads, cfg):
 def _in_bytes(x, p, name, st):
     """Input and weight of a linear product as it reads them: rounded to rows of 8 bits with byte_products."""
     w = p[name]
-    if not st.cfg.byte_products:
+    if not st.cfg.byte_products or name.startswith(f"aux{st.cfg.aux_depth - 1}."):
         return x, w
     rounded = lambda a: byte_values(*byte_rows(a)).astype(a.dtype)
     return rounded(x.reshape(-1, x.shape[-1])).reshape(x.shape), rounded(w.T).T

@@ -242,6 +242,8 @@ struct Block {
   int encoder_fwd(int l, const EncoderActs& a, const void* x, void* x2_out, const EncoderActs* next, hipStream_t s,
                   const std::function<int()>& stored = nullptr);
   char* byte_ws = nullptr;      // of the backward products on rows of 8 bits
+  // Whether a layer's products are: all but the last one of an auxiliary network, of which only the class token's row is used
+  bool byte_layer(int l) const { return cfg.byte_products && !(cfg.aux_depth >= 1 && l == cfg.depth + cfg.aux_depth - 1); }
   ByteLinear byte_linear(int in, int out, int act = PPLL_ACT_NONE) const;
   template <class BUMP> void plan_byte_acts(BUMP& bump, EncoderActs* a) const;
   int encoder_fwd_bytes(int l, const EncoderActs& a, const void* x, void* x2_out, const EncoderActs* next, hipStream_t s, const std::function<int()>& stored);

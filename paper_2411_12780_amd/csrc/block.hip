@@ -297,12 +297,12 @@ size_t Block::plan(char* base) {
     for (int l = 0; l < cfg.depth + cfg.aux_depth; ++l) {
       EncoderActs a;
       // what a product on rows of 8 bits reads stays in those alone: one buffer of each width for all layers
-      const bool first = !cfg.byte_products || l == 0;
-      auto product_in = [&](void* of_all, size_t elems) { return first ? bump.take(elems * esz) : of_all; };
+      const bool bytes = byte_layer(l), shared = bytes && l > 0;
+      auto product_in = [&](void* of_all, size_t elems) { return shared ? of_all : bump.take(elems * esz); };
       a.u1 = product_in(l ? enc_a[0].u1 : nullptr, M * D); a.qkv = bump.take(M * 3 * D * esz); a.att = bump.take(M * D * esz);
-      a.x1 = bump.take(M * D * esz); a.u2 = cfg.byte_products ? a.u1 : bump.take(M * D * esz);
+      a.x1 = bump.take(M * D * esz); a.u2 = bytes ? a.u1 : bump.take(M * D * esz);
       a.h = bump.take(M * F * esz); a.gl = product_in(l ? enc_a[0].gl : nullptr, M * F);
-      if (cfg.byte_products) plan_byte_acts(bump, &a);
+      if (bytes) plan_byte_acts(bump, &a);
       a.x2 = bump.take(M * D * esz);
       a.mean1 = bump.floats(M); a.rstd1 = bump.floats(M); a.mean2 = bump.floats(M); a.rstd2 = bump.floats(M);
       a.lse = bump.floats((size_t)B * H * T);
@@ -323,7 +323,7 @@ size_t Block::plan(char* base) {
       rope_pos = (int32_t*)bump.take((size_t)T * 2 * sizeof(int32_t));
     }
     z = bump.take((size_t)B * D * esz); dz = bump.take((size_t)B * D * esz); dcls = bump.take((size_t)B * D * esz);
-    prune_cls = cfg.aux_depth >= 1 && !cfg.byte_products && attention_cls_lds_bytes(T, D / H) <= 160 * 1024;
+    prune_cls = cfg.aux_depth >= 1 && attention_cls_lds_bytes(T, D / H) <= 160 * 1024;
     if (prune_cls) {
       ClsActs& c = cls_a;
       const size_t bd = (size_t)B * D * esz, bf = (size_t)B * F * esz;
@@ -339,7 +339,7 @@ size_t Block::plan(char* base) {
     const int layers = cfg.depth + cfg.aux_depth;
     for (int l = 0; l <= layers; ++l) g_res.push_back(bump.take(M * D * esz));
     for (int l = 0; l < layers; ++l) {
-      if (l && cfg.byte_products) {     // whose weight gradients are formed at once
+      if (l && byte_layer(l)) {     // whose weight gradients are formed at once
         g_mid.push_back(g_mid[0]); d_h.push_back(d_h[0]); d_qkv.push_back(d_qkv[0]);
         continue;
       }
@@ -565,7 +565,7 @@ int Block::qk_bwd(int l, void* dq, long q_ld, int q_rows, int q_tokens, const vo
 
 int Block::encoder_fwd(int l, const EncoderActs& a, const void* x, void* x2_out, const EncoderActs* next, hipStream_t s,
                        const std::function<int()>& stored) {
-  if (cfg.byte_products) return encoder_fwd_bytes(l, a, x, x2_out, next, s, stored);
+  if (byte_layer(l)) return encoder_fwd_bytes(l, a, x, x2_out, next, s, stored);
   const int D = cfg.dim, F = cfg.mlp_dim, T = cfg.tokens, H = cfg.heads, M = cfg.batch * T;
   const EncoderParams& p = enc_p[l];
   GemmArgs g = gemm_args();
@@ -603,7 +603,7 @@ int Block::encoder_fwd(int l, const EncoderActs& a, const void* x, void* x2_out,
 // g_in: gradient w.r.t. the layer output; g_tmp receives the gradient at the
 // mid-layer residual; g_out the gradient w.r.t. the layer input.
 int Block::encoder_bwd(int l, const void* x, const void* g_in, void* g_tmp, void* g_out, bool need_dx, hipStream_t s) {
-  if (cfg.byte_products) return encoder_bwd_bytes(l, x, g_in, g_tmp, g_out, need_dx, s);
+  if (byte_layer(l)) return encoder_bwd_bytes(l, x, g_in, g_tmp, g_out, need_dx, s);
   const int D = cfg.dim, F = cfg.mlp_dim, T = cfg.tokens, H = cfg.heads, M = cfg.batch * T;
   const EncoderParams& p = enc_p[l];
   EncoderActs& a = enc_a[l];
@@ -729,7 +729,8 @@ std::vector<GemmArgs> Block::weight_grads() const {
     const GemmArgs g = wgrad_args(xin, x_ld, in_dim, dy, dy_ld, out_dim, K, grad(w_off), ldw, grad(b_off));
     if (gemm_weight_grad_groupable(g)) set.push_back(g);
   };
-  for (int l = cfg.byte_products ? -1 : cfg.depth + cfg.aux_depth - 1; l >= 0; --l) {
+  for (int l = cfg.depth + cfg.aux_depth - 1; l >= 0; --l) {
+    if (byte_layer(l)) break;      // and those below
     const EncoderParams& p = enc_p[l];
     const EncoderActs& a = enc_a[l];
     if (prune_cls && l == cfg.depth + cfg.aux_depth - 1) {

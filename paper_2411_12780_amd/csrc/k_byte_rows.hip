@@ -111,69 +111,82 @@ __global__ __launch_bounds__(THREADS) void byte_rows_values_kernel(ppll_byte_row
   }
 }
 
-// 32 columns a workgroup: their largest magnitudes over all rows, then the bytes, turned in LDS, 256 rows at a time
-constexpr int TC = 32, CT = 512, CHUNK = 256, CPITCH = CHUNK + 16;
+// 8 columns a workgroup: their largest magnitudes over all rows, then the bytes, turned in LDS.  A thread has 4 rows, one behind the other, so that
+// four bytes of a column are a word; the first 4096 rows stay in registers between the two passes.  A weight is small beside the chip, so what bounds
+// this is how few loads wait on each other: 32 columns a workgroup of 512, 128 rows at a time and all rows loaded twice, took 20 us a weight on average
+// over 768 x 2304, 768 x 768, 768 x 4 x 768 and its transpose (fp32), where this takes 7.  The 32-byte pieces of a line belong to neighbouring
+// workgroups: those of one XCD (workgroup id % 8) are neighbours.
+constexpr int TC = 8, CT = 512, UNITS = 2, CHUNK = CT * 4 * UNITS, CPITCH = CHUNK + 16;
 template <int DT>
-__global__ __launch_bounds__(CT) void byte_rows_pack_columns_kernel(const char* in, int64_t in_ld, int8_t* q, int8_t* e, int64_t q_ld, int rows, int cols) {
-  constexpr int ESZ = DT == BF16 ? 2 : 4, LANES = CT / 4;      // rows at a time: four threads a row
-  __shared__ uint32_t most[LANES][TC + 1];
-  __shared__ __align__(16) int8_t turned[TC][CPITCH];
-  __shared__ int exps[TC];
-  const int c0 = blockIdx.x * TC, mine = (threadIdx.x & 3) * 8, r0 = threadIdx.x >> 2, ncols = cols - c0;
+__global__ __launch_bounds__(CT) void byte_rows_pack_columns_kernel(const char* in, int64_t in_ld, int8_t* q, int8_t* e, int64_t q_ld, int rows, int cols,
+                                                                    int groups) {
+  constexpr int ESZ = DT == BF16 ? 2 : 4;
+  __shared__ uint32_t most[CT / 64][TC];
+  __shared__ __align__(16) uint32_t turned[TC][CPITCH / 4];
+  const int group = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  if (group >= groups) return;
+  const int c0 = group * TC, ncols = cols - c0, padded = (rows + 15) & ~15;
   const char* base = in + (int64_t)c0 * ESZ;
+  Eight<DT> kept[UNITS][4];
   uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (mine < ncols) {
-#pragma unroll 4
-    for (int r = r0; r < rows; r += LANES) {
-      Eight<DT> v;
-      float f[8];
-      v.load(base + r * in_ld * ESZ, mine, ncols);
-      v.get(f);
+  auto load = [&](int k0) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m[i] = max(m[i], __float_as_uint(f[i]) & 0x7fffffffu);
-    }
+    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = k0 + (u * CT + (int)threadIdx.x) * 4 + j;
+        if (r < rows) kept[u][j].load(base + r * in_ld * ESZ, 0, ncols);
+        else kept[u][j].zero();
+      }
+  };
+  for (int k0 = (rows - 1) / CHUNK * CHUNK; k0 >= 0; k0 -= CHUNK) {     // the first rows last: they are kept
+    load(k0);
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float f[8];
+        kept[u][j].get(f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[i] = max(m[i], __float_as_uint(f[i]) & 0x7fffffffu);
+      }
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) most[r0][mine + i] = m[i];
-  __syncthreads();
-  for (int h = LANES / 2; h >= 16; h /= 2) {       // 16 threads a column at the end
-    for (int i = threadIdx.x; i < h * TC; i += CT) most[i / TC][i % TC] = max(most[i / TC][i % TC], most[i / TC + h][i % TC]);
-    __syncthreads();
-  }
-  if (threadIdx.x < TC) {
-    uint32_t a = 0;
-    for (int i = 0; i < 16; ++i) a = max(a, most[i][threadIdx.x]);
-    const int x = byte_exponent(a);
-    exps[threadIdx.x] = x;
-    if ((int)threadIdx.x < ncols) e[c0 + threadIdx.x] = (int8_t)x;
+  for (int i = 0; i < 8; ++i) {
+    m[i] = lanes_most<64>(m[i]);
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6][i] = m[i];
   }
   __syncthreads();
-  const int padded = (rows + 15) & ~15;
+  float inv[8];
+  uint32_t fine[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    uint32_t v = most[0][i];
+#pragma unroll
+    for (int w = 1; w < CT / 64; ++w) v = max(v, most[w][i]);
+    const int x = byte_exponent(v);
+    if (threadIdx.x == i && i < ncols) e[c0 + i] = (int8_t)x;
+    inv[i] = exp2_bits(x == BYTE_NAN ? 0 : -x);
+    fine[i] = x == BYTE_NAN ? 0u : ~0u;
+  }
   for (int k0 = 0; k0 < padded; k0 += CHUNK) {
-    for (int k = r0; k < CHUNK; k += LANES) {
-      const int r = k0 + k;
-      float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (r < rows && mine < ncols) {
-        Eight<DT> v;
-        v.load(base + r * in_ld * ESZ, mine, ncols);
-        v.get(f);
-      }
+    if (k0) load(k0);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int x = exps[mine + i];
-        const uint32_t w = byte_pack4(f[i], 0.f, 0.f, 0.f, exp2_bits(x == BYTE_NAN ? 0 : -x));
-        turned[mine + i][k] = x == BYTE_NAN ? 0 : (int8_t)w;
-      }
+    for (int u = 0; u < UNITS; ++u) {
+      float f[4][8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kept[u][j].get(f[j]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) turned[i][u * CT + threadIdx.x] = byte_pack4(f[0][i], f[1][i], f[2][i], f[3][i], inv[i]) & fine[i];
     }
     __syncthreads();
-    {
-      const int c = threadIdx.x >> 4, k = (threadIdx.x & 15) * 16;
-      if (c < ncols && k0 + k < padded) *(uint4*)(q + (int64_t)(c0 + c) * q_ld + k0 + k) = *(const uint4*)&turned[c][k];
-    }
+    const int chunk = min(CHUNK, padded - k0), c = threadIdx.x >> 6;      // a wave a column
+    if (c < ncols)
+      for (int k = (threadIdx.x & 63) * 16; k < chunk; k += 64 * 16) *(uint4*)(q + (int64_t)(c0 + c) * q_ld + k0 + k) = *(const uint4*)&turned[c][k / 4];
     __syncthreads();
   }
 }
-static_assert(TC * (CHUNK / 16) == CT, "");
+static_assert(TC == CT / 64 && CPITCH % 16 == 0, "");
 
 unsigned blocks_of(int rows, int per) {
   const unsigned n = (unsigned)(((int64_t)rows + per - 1) / per);
@@ -233,11 +246,12 @@ int launch_byte_rows_values(hipStream_t s, int cols, const ppll_byte_rows& a, in
 }
 int launch_byte_rows_pack_columns(hipStream_t s, int dt, int rows, int cols, const ppll_rows& in, const ppll_byte_rows& out) {
   if (cols <= 0) return PPLL_OK;
-  const dim3 grid((cols + TC - 1) / TC);
+  const int groups = (cols + TC - 1) / TC;
+  const dim3 grid((groups + 7) / 8 * 8);
   if (dt == BF16)
-    hipLaunchKernelGGL(byte_rows_pack_columns_kernel<BF16>, grid, dim3(CT), 0, s, (const char*)in.p, in.ld, out.q, out.e, out.ld, rows, cols);
+    hipLaunchKernelGGL(byte_rows_pack_columns_kernel<BF16>, grid, dim3(CT), 0, s, (const char*)in.p, in.ld, out.q, out.e, out.ld, rows, cols, groups);
   else
-    hipLaunchKernelGGL(byte_rows_pack_columns_kernel<F32>, grid, dim3(CT), 0, s, (const char*)in.p, in.ld, out.q, out.e, out.ld, rows, cols);
+    hipLaunchKernelGGL(byte_rows_pack_columns_kernel<F32>, grid, dim3(CT), 0, s, (const char*)in.p, in.ld, out.q, out.e, out.ld, rows, cols, groups);
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }

@@ -88,6 +88,18 @@ def test_pack_columns(precision, dtype, rows, cols, room, shift):
     assert np.array_equal(out.e(), e) and np.array_equal(out.q(), q) and out.padding_is_zero_and_the_rest_untouched()
 
 
+@pytest.mark.parametrize("precision,dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(2048, 64), (2049, 65), (4096, 9), (4097, 20), (8192, 7), (9001, 130), (65536, 3)])
+def test_pack_columns_of_many_rows(precision, dtype, rows, cols):
+    """More rows than stay in registers, a last piece of one row, columns whose largest value is in the last or the first row."""
+    x = rows_of(cols, rows, dtype, seed=4).t().contiguous()
+    x[rows - 1, 0], x[0, 1] = 1e9, -1e9
+    src, out = Placed(x, dtype), PlacedBytes(cols, rows, room=16)
+    P.ppll_byte_rows_pack_columns(precision, rows, cols, P.rows(src.view), P.byte_rows(out.store, out.exps), stream())
+    q, e = O.byte_rows(x.double().numpy().T)
+    assert np.array_equal(out.e(), e) and np.array_equal(out.q(), q) and out.padding_is_zero_and_the_rest_untouched()
+
+
 def test_rows_beyond_32_bits():
     # 70000 rows 32768 elements apart, columns of the last rows beyond 2^31 elements
     rows, cols, ld = 70000, 24, 32768
