@@ -381,7 +381,7 @@ typedef struct {
 
 /* Rows (0..2^30 of them, cols 1..65536) of `precision`'s type into 8 bits: e is the least exponent of -126..121 with max|x| <= 127 * 2^e, q is x * 2^-e
  * rounded to the nearest whole number, ties to even, at most 127.  A row with a NaN or an infinity becomes a row of NaN (q = 0).  Elements
- * under 2^-127 become 0. */
+ * under 2^-127 become 0.  Here and below, outputs overlap no input and each other in nothing but what a call names. */
 int ppll_byte_rows_pack(int32_t precision, int32_t rows, int32_t cols, const ppll_rows* in, const ppll_byte_rows* out, void* hip_stream);
 
 /* The same of the columns of a [rows, cols] matrix (rows 1..65536, cols 0..65536), say a weight as layers have it, [in, out]: row c of `out` is column c of
@@ -414,7 +414,7 @@ int ppll_byte_linear_forward(const ppll_byte_linear_config* cfg, const ppll_byte
 /* Gradients of X W^T + bias at what the rows stand for, from dy [rows, out_dim]:
  *   dx = dy W, times gate where given (an activation's slope at the place X came from; [rows, in_dim]);  dw = X^T dy, fp32 [in_dim, out_dim] row by row;
  *   db = the column sums of dy, fp32 [out_dim].
- * Each of dx, dw, db may be null (not wanted); w is needed for dx, x for dw.  dx may be gate; dw and db are overwritten (zeros where rows = 0).
+ * Each of dx, dw, db may be null (not wanted); w is needed for dx, x for dw.  dx may be gate (same pointer and stride), not dy; dw and db are overwritten (zeros where rows = 0).
  * Sums in fp32 in a fixed order.  Workspace: ppll_byte_linear_workspace_bytes(cfg) bytes, 16-byte aligned, used by nothing else until the
  * stream has passed the call. */
 int ppll_byte_linear_workspace_bytes(const ppll_byte_linear_config* cfg, size_t* bytes);

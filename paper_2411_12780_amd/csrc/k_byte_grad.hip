@@ -339,15 +339,16 @@ __global__ __launch_bounds__(256) void byte_grad_sum_kernel(const float* parts, 
   }
 }
 
-// Column sums alone: each workgroup 64 columns of a stretch of rows
-constexpr int SUM_COLS = 64, SUM_ROWS = 512;
+// Column sums alone: each workgroup 64 columns of a stretch of rows, 512 of them or what leaves 32768 stretches (a grid has no more)
+constexpr int SUM_COLS = 64;
+__host__ __device__ constexpr int sum_rows(int rows) { return rows <= 512 << 15 ? 512 : (rows + 32767) >> 15; }
 template <int DT> __global__ __launch_bounds__(256) void byte_grad_columns_kernel(const char* d, int64_t ldd, int rows, int cols, float* out) {
   __shared__ float sums[4][SUM_COLS];
-  const int c = blockIdx.x * SUM_COLS + (threadIdx.x & 63), w = threadIdx.x >> 6, r1 = min(rows, (int)(blockIdx.y + 1) * SUM_ROWS);
+  const int c = blockIdx.x * SUM_COLS + (threadIdx.x & 63), w = threadIdx.x >> 6, each = sum_rows(rows), r1 = min(rows, (int)(blockIdx.y + 1) * each);
   float s = 0.f;
   if (c < cols)
 #pragma unroll 8
-    for (int r = blockIdx.y * SUM_ROWS + w; r < r1; r += 4) s += ld_f(d, r * ldd + c, DT);
+    for (int r = blockIdx.y * each + w; r < r1; r += 4) s += ld_f(d, r * ldd + c, DT);
   sums[w][threadIdx.x & 63] = s;
   __syncthreads();
   if (w == 0 && c < cols) out[(int64_t)blockIdx.y * cols + c] = sums[0][c - blockIdx.x * SUM_COLS] + sums[1][c - blockIdx.x * SUM_COLS] +
@@ -390,7 +391,7 @@ Parts parts_of(const ByteLinear& l) {
   p.out = ((int64_t)l.in * l.out + l.out + 3) / 4 * 4;
   return p;
 }
-int sum_chunks(int rows) { return (int)(((int64_t)rows + SUM_ROWS - 1) / SUM_ROWS); }
+int sum_chunks(int rows) { return (int)(((int64_t)rows + sum_rows(rows) - 1) / sum_rows(rows)); }
 
 // ---- The other way: operands written out in bf16, which is what they stand for, and the products on the kernels of bf16 operands.  Those reach 1100
 // TFLOP/s where the kernel above is held at 750 by LDS (64 x 64 of a wave: 192 KB through it for 64 k of four of them, and the conversion's own way
@@ -400,6 +401,7 @@ bool values_fit(const ByteLinear& l) {
   return l.dt == BF16 && l.in % 8 == 0 && l.out % 8 == 0 && (int64_t)l.rows * std::max(l.in, l.out) <= most && (int64_t)l.in * l.out <= most;
 }
 bool lies_whole(const void* p, int64_t ld) { return !p || (ld % 8 == 0 && ((uintptr_t)p & 15) == 0); }
+bool lies_near(const ByteLinear& l, const ppll_rows& r) { return !r.p || l.rows * r.ld < 1 << 29; }       // (elements, as in values_fit)
 // Microseconds, this kernel / values, both gradients, rows x in x out: 8320 x 1536 x 384 51 / 63, 25216 x 768 x 768 101 / 111, 4096 x 2048 x 2048 93 / 99,
 // 8320 x 1536 x 1536 143 / 116, 25216 x 768 x 2304 248 / 191, 8192 x 4096 x 4096 744 / 505, 512 x 6144 x 6144 156 / 138; with few output channels X's way
 // counts for more: 32768 x 4096 x 256 236 / 286.
@@ -421,7 +423,7 @@ size_t dw_floats(const ByteLinear& l) {       // for the parts of its tiles
 }
 int64_t values_bytes(const ByteLinear& l, bool x, bool w) { return (((x ? (int64_t)l.rows : 0) + (w ? l.out : 0)) * l.in * 2 + 255) / 256 * 256; }
 bool values_supported(const ByteLinear& l, const ppll_rows& dy, const ppll_rows& gate, const ppll_rows& dx, const float* dw) {
-  return values_fit(l) && lies_whole(dy.p, dy.ld) && lies_whole(gate.p, gate.ld) && lies_whole(dx.p, dx.ld) && lies_whole(dw, l.out);
+  return values_fit(l) && lies_near(l, dy) && lies_near(l, gate) && lies_near(l, dx) && lies_whole(dy.p, dy.ld) && lies_whole(gate.p, gate.ld) && lies_whole(dx.p, dx.ld) && lies_whole(dw, l.out);
 }
 int backward_values(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
                     const ppll_rows& dx, float* dw, float* db, char* ws) {

@@ -31,10 +31,11 @@ struct ByteArgs {
 
 // Steps and biases of columns n .. n + 7; a channel of NaN has a bias of NaN
 struct Columns {
-  int most;               // the largest exponent
+  int most, least;        // the largest and smallest exponent
   float step[8], bias[8];
   __device__ __forceinline__ void load(const ByteArgs& p, int n) {
     most = -256;
+    least = 256;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int at = min(n + i, p.N - 1), e = p.ew[at];
@@ -42,6 +43,7 @@ struct Columns {
       bias[i] = e == BYTE_NAN ? __uint_as_float(0x7fc00000u) : b;
       step[i] = exp2_bits(e == BYTE_NAN ? 0 : e);
       most = max(most, e == BYTE_NAN ? 0 : e);
+      least = min(least, e == BYTE_NAN ? 0 : e);
     }
   }
 };
@@ -65,8 +67,8 @@ template <int DT, bool VEC> __device__ __forceinline__ void byte_end(const ByteA
     }
   };
   float v[8];
-  // the product of two steps is a power of two, exact (also as a subnormal one) below 2^128; from there on only a sum of 0 is none too large
-  const bool rare = row_exp == BYTE_NAN || row_exp + c.most > 127;
+  // the product of two steps is a power of two, exact from 2^-149 (a subnormal one) to 2^127; outside a sum of many may be in range where the step is not
+  const bool rare = row_exp == BYTE_NAN || row_exp + c.most > 127 || row_exp + c.least < -149;
   const float step = exp2_bits(rare ? 0 : row_exp);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = fmaf((float)sum[i], c.step[i] * step, c.bias[i]);

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(THREADS) void byte_rows_values_kernel(ppll_byte_row
 // 8 columns a workgroup: their largest magnitudes over all rows, then the bytes, turned in LDS.  A thread has 4 rows, one behind the other, so that
 // four bytes of a column are a word; the first 4096 rows stay in registers between the two passes.  A weight is small beside the chip, so what bounds
 // this is how few loads wait on each other: 32 columns a workgroup of 512, 128 rows at a time and all rows loaded twice, took 20 us a weight on average
-// over 768 x 2304, 768 x 768, 768 x 4 x 768 and its transpose (fp32), where this takes 7.  The 32-byte pieces of a line belong to neighbouring
+// over the four weights of an encoder layer of width 768 (fp32), where this takes 7.  The 32-byte pieces of a line belong to neighbouring
 // workgroups: those of one XCD (workgroup id % 8) are neighbours.
 constexpr int TC = 8, CT = 512, UNITS = 2, CHUNK = CT * 4 * UNITS, CPITCH = CHUNK + 16;
 template <int DT>

@@ -25,6 +25,12 @@ int check_rows(const ppll_rows* r, int cols, int32_t precision, const char* what
   return PPLL_OK;
 }
 int check_maybe(const ppll_rows* r, int cols, int32_t precision, const char* what) { return r ? check_rows(r, cols, precision, what) : PPLL_OK; }
+// Buffers from one place, but where they may be one and the same
+int check_apart(const ppll_rows* a, const ppll_rows* b, bool may_be_one, const char* what) {
+  if (!a || !b || a->p != b->p || (may_be_one && a->ld == b->ld)) return PPLL_OK;
+  set_error("%s share memory", what);
+  return PPLL_ERR_SHAPE;
+}
 // rows of a linear layer, pixels of a map
 int check_map(const ppll_rows* r, int cols, int32_t precision, const char* what) {
   PPLL_TRY(check_rows(r, cols, precision, what));
@@ -131,6 +137,9 @@ int ppll_byte_linear_forward(const ppll_byte_linear_config* cfg, const ppll_byte
   PPLL_TRY(check_maybe_map(residual, l.out, cfg->precision, "residual"));
   PPLL_TRY(check_map(y, l.out, cfg->precision, "y"));
   PPLL_TRY(check_maybe_map(slope, l.out, cfg->precision, "slope"));
+  PPLL_TRY(check_apart(y, residual, true, "y and residual of other strides"));
+  PPLL_TRY(check_apart(y, slope, false, "y and slope"));
+  PPLL_TRY(check_apart(slope, residual, false, "slope and residual"));
   return launch_byte_linear_fwd((hipStream_t)hip_stream, l, *x, *w, bias_dev, given(residual), *y, given(slope));
 }
 
@@ -160,6 +169,8 @@ int ppll_byte_linear_backward(const ppll_byte_linear_config* cfg, const ppll_byt
     }
     if (dw_dev) PPLL_TRY(check_bytes(x, l.in, "x"));
     PPLL_TRY(check_workspace(workspace_dev, workspace_bytes, byte_linear_workspace(l)));
+    PPLL_TRY(check_apart(dx, gate, true, "dx and gate of other strides"));
+    PPLL_TRY(check_apart(dx, dy, false, "dx and dy"));
   }
   return launch_byte_linear_bwd((hipStream_t)hip_stream, l, given(x), given(w), given(dy), given(gate), given(dx), dw_dev, db_dev, (char*)workspace_dev);
 }
@@ -185,6 +196,8 @@ int ppll_group_norm_forward(const ppll_group_norm_config* cfg, const ppll_rows* 
   PPLL_TRY(check_map(y, g.channels, cfg->precision, "y"));
   if (stats_dev) PPLL_TRY(check_floats(stats_dev, "stats_dev"));
   if (keep) PPLL_TRY(check_bytes(keep, g.channels, "keep"));
+  PPLL_TRY(check_apart(y, x, true, "y and x of other strides"));
+  PPLL_TRY(check_apart(y, residual, true, "y and residual of other strides"));
   PPLL_TRY(check_workspace(workspace_dev, workspace_bytes, group_norm_workspace(g)));
   return launch_group_norm_fwd((hipStream_t)hip_stream, g, *x, scale_dev, shift_dev, given(residual), *y, stats_dev, given(keep), (char*)workspace_dev);
 }
@@ -210,7 +223,11 @@ int ppll_group_norm_backward(const ppll_group_norm_config* cfg, const ppll_rows*
     PPLL_TRY(check_map(dy, g.channels, cfg->precision, "dy"));
     PPLL_TRY(check_map(dx, g.channels, cfg->precision, "dx"));
     PPLL_TRY(check_maybe_map(d_residual, g.channels, cfg->precision, "d_residual"));
-    if (d_residual && d_residual->p == dx->p) { set_error("dx and d_residual are one buffer"); return PPLL_ERR_SHAPE; }
+    PPLL_TRY(check_apart(dx, d_residual, false, "dx and d_residual"));
+    PPLL_TRY(check_apart(dx, dy, true, "dx and dy of other strides"));
+    PPLL_TRY(check_apart(d_residual, dy, true, "d_residual and dy of other strides"));
+    if (!x_bytes) PPLL_TRY(check_apart(dx, x, false, "dx and x"));
+    if (!x_bytes) PPLL_TRY(check_apart(d_residual, x, false, "d_residual and x"));
     PPLL_TRY(check_workspace(workspace_dev, workspace_bytes, group_norm_workspace(g)));
   }
   const uintptr_t a = (uintptr_t)d_scale_dev, b = (uintptr_t)d_shift_dev, bytes = g.channels * sizeof(float);

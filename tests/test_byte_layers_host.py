@@ -120,6 +120,25 @@ def test_norm_refusals():
     refused(NULL, lambda: back(c=none, dg=None))
 
 
+def test_outputs_that_are_inputs():
+    gelu = P.byte_linear_config(**GOOD, activation=P.ACT_GELU)
+    forward = lambda **k: P.ppll_byte_linear_forward(gelu, B(), B(), 16, k.get("res"), R(4096), k.get("slope"))  # noqa: E731
+    refused(SHAPE, lambda: forward(res=R(4096, 72)))
+    refused(SHAPE, lambda: forward(slope=R(4096)))
+    refused(SHAPE, lambda: forward(res=R(8192), slope=R(8192)))
+    cfg = P.byte_linear_config(**GOOD)
+    need = P.ppll_byte_linear_workspace_bytes(cfg)
+    refused(SHAPE, lambda: P.ppll_byte_linear_backward(cfg, B(), B(), R(4096), None, R(4096), 64, 64, 64, need))
+    refused(SHAPE, lambda: P.ppll_byte_linear_backward(cfg, B(), B(), R(4096), R(8192, 72), R(8192), 64, 64, 64, need))
+    cfg = P.group_norm_config(**NORM)
+    need = P.ppll_group_norm_workspace_bytes(cfg)
+    refused(SHAPE, lambda: P.ppll_group_norm_forward(cfg, R(4096, 72), 64, 64, None, R(4096), None, None, 64, need))
+    refused(SHAPE, lambda: P.ppll_group_norm_forward(cfg, R(8192), 64, 64, R(4096, 72), R(4096), None, None, 64, need))
+    back = lambda x=R(4096), dy=R(8192), dx=R(16384), dr=None: P.ppll_group_norm_backward(cfg, x, None, 64, 64, 64, None, None, dy, dx, dr, 1024, 2048, 64, need)  # noqa: E731
+    for bad in (dict(dx=R(4096)), dict(dx=R(8192, 72)), dict(dr=R(8192, 72)), dict(dr=R(4096)), dict(dr=R(16384))):
+        refused(SHAPE, lambda: back(**bad))
+
+
 def test_tensors_of_rows():
     refused(SHAPE, P.rows, torch.zeros(2, 3, 4))
     refused(SHAPE, P.rows, torch.zeros(4, 3).t())

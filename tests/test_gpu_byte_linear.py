@@ -166,6 +166,24 @@ def test_forward_of_the_largest_sums():
     assert np.array_equal(y.host(), want)
 
 
+@pytest.mark.parametrize("precision,dtype", TYPES)
+@pytest.mark.parametrize("rows_", [3, 100, 400])
+def test_forward_of_steps_below_the_types_range(precision, dtype, rows_):
+    """A step of 2^-160 is none in fp32, 2^26 of them are a number (a subnormal one)."""
+    l = Layer(rows_, 4096, 20, dtype)
+    l.x.exps[:rows_], l.w.exps[:20] = -100, -60
+    l.x.exps[1] = -90
+    l.x.store[:], l.w.store[:] = 127, 127
+    l.w.store[3] = -127
+    y, _ = forward(l, bias=False)
+    want = np.full((rows_, 20), 4096 * 127 * 127 * 2.0 ** -160)
+    want[1] *= 2.0 ** 10
+    want[:, 3] *= -1
+    smallest = 2.0 ** (-149 if dtype == torch.float32 else -133)
+    assert (np.abs(y.host() - want) <= HALF[dtype] * np.abs(want) + smallest / 2).all()
+    assert (y.host()[1] != 0).all()
+
+
 def test_forward_in_place_of_the_residual():
     l = Layer(70, 64, 48, torch.bfloat16)
     residual = l.put(70, 48)
@@ -269,6 +287,57 @@ def test_backward_of_many_rows():
     check_backward(Layer(8320, 384, 128, torch.bfloat16), True)
     check_backward(Layer(20000, 40, 24, torch.bfloat16))
     check_backward(Layer(9000, 24, 40, torch.float32))
+
+
+def test_column_sums_of_more_rows_than_a_grid_has_stretches_of():
+    m = (1 << 24) + 700
+    for dtype, precision in ((torch.bfloat16, P.BF16), (torch.float32, P.FP32)):
+        dy = torch.randint(-1, 2, (m, 2), device=DEV).to(dtype)      # whole sums, exact in fp32
+        cfg, db = P.byte_linear_config(precision, m, 1, 2), torch.empty(2, device=DEV)
+        ws = torch.empty(P.ppll_byte_linear_workspace_bytes(cfg), dtype=torch.uint8, device=DEV)
+        P.ppll_byte_linear_backward(cfg, None, None, P.rows(dy), None, None, None, db, ws, ws.numel(), stream())
+        assert torch.equal(db.double(), dy.double().sum(0))
+
+
+def test_backward_of_rows_far_apart():
+    # 2^20 elements between rows of dy, dx and gate in turn: more than 32 bits of bytes over all of them
+    m, k, n = 1100, 64, 64
+    l = Layer(m, k, n, torch.bfloat16)
+    near = {name: torch.randn(m, 64, device=DEV).bfloat16() for name in ("dy", "gate", "dx")}
+    store = torch.zeros(m << 20, dtype=torch.bfloat16, device=DEV).view(m, 1 << 20)
+    ws = torch.empty(P.ppll_byte_linear_workspace_bytes(l.cfg()), dtype=torch.uint8, device=DEV)
+
+    def run(dw, **other):
+        t = {**near, **other}
+        P.ppll_byte_linear_backward(l.cfg(), l.bytes(l.x), l.bytes(l.w), P.rows(t["dy"]), P.rows(t["gate"]), P.rows(t["dx"]), dw, None, ws, ws.numel(), stream())
+        return t["dx"].double().cpu()
+    x, w = l.values()
+    d, g = near["dy"].double().cpu().numpy(), near["gate"].double().cpu().numpy()
+    want = (d @ w) * g
+    allowed = ((n + 2) * 2 * ULP * (np.abs(d) @ np.abs(w)) + ULP * np.abs(d @ w)) * np.abs(g)
+    for name in ("dy", "gate", "dx"):
+        far = store[:, -64:]
+        far.copy_(near[name])
+        for dw in (None, torch.empty(k, n, device=DEV)):
+            got = run(dw, **{name: far}).numpy()
+            assert (np.abs(got - want) <= allowed + HALF[torch.bfloat16] * (np.abs(want) + allowed)).all()
+            if dw is not None:
+                assert (np.abs(dw.double().cpu().numpy() - x.T @ d) <= (m + 2) * 2 * ULP * (np.abs(x).T @ np.abs(d))).all()
+        store.zero_()
+
+
+@pytest.mark.parametrize("precision,dtype", TYPES)
+@pytest.mark.parametrize("size,dw", [((300, 70, 40), True), ((700, 128, 64), False), ((700, 128, 64), True), ((8192, 1536, 1536), True)])
+def test_dx_in_place_of_the_gate(precision, dtype, size, dw):
+    m, k, n = size
+    l = Layer(*size, dtype)
+    dy, gate, dx = l.put(m, n), l.put(m, k), l.empty(m, k)
+    ws = torch.empty(max(P.ppll_byte_linear_workspace_bytes(l.cfg()), 16), dtype=torch.uint8, device=DEV)
+    go = lambda to: P.ppll_byte_linear_backward(l.cfg(), l.bytes(l.x), l.bytes(l.w), rows(dy), rows(gate), rows(to),  # noqa: E731
+                                                torch.empty(k, n, device=DEV) if dw else None, None, ws, ws.numel(), stream())
+    go(dx)
+    go(gate)
+    assert torch.equal(dx.view, gate.view)
 
 
 def test_the_sums_have_a_fixed_order_and_need_nothing_of_the_workspace():
