@@ -58,9 +58,10 @@ struct Gelu {
     return cdf + z * pdf;
   }
 };
-template <bool EXACT, class F> __device__ __forceinline__ void with_activation(int act, F f) {
-  if (act == PPLL_ACT_SILU) f(Silu<EXACT>());
-  else if (act == PPLL_ACT_GELU) f(Gelu());
+// KIND: 0 straight ones (none, ReLU), 1 curved ones (SiLU, GELU), -1 any
+template <bool EXACT, int KIND, class F> __device__ __forceinline__ void with_activation(int act, F f) {
+  if (KIND != 0 && act == PPLL_ACT_SILU) f(Silu<EXACT>());
+  else if (KIND != 0 && (KIND == 1 || act == PPLL_ACT_GELU)) f(Gelu());
   else f(Clamp{act == PPLL_ACT_RELU ? 0.f : -INFINITY});
 }
 

@@ -55,9 +55,10 @@ template <int DT> __device__ __forceinline__ void keep_piece(const NormArgs& p, 
 }
 
 // An image's slab in registers (WHOLE), or a piece of an image, of which its statistics are left (PART).  GV: segments of a piece of 8 channels, each of
-// one group; MI: pieces a thread holds.
+// one group; MI: pieces a thread holds.  Up to 4 of them within 128 registers, so that a unit has two workgroups of 512, one's memory busy during the
+// other's sums (1024 x 32 x 32 x 16, groups of 2, 25 us; 33 with the 129 registers that the compiler took by itself).
 template <int DT, int MODE, bool VEC, int GV, int MI>
-__global__ __launch_bounds__(MOST_THREADS) void group_norm_fwd_kernel(NormArgs p) {
+__global__ __launch_bounds__(MOST_THREADS, MI * (DT == BF16 ? 1 : 2) <= 4 && GV <= 4 ? 4 : 2) void group_norm_fwd_kernel(NormArgs p) {
   constexpr int PER = 8 / GV;
   extern __shared__ float room[];
   const int t = threadIdx.x, row = quotient(t, p.over_npc), col = t - row * p.npc;
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(MOST_THREADS) void group_norm_fwd_kernel(NormArgs p
       affine(p, c0, c, r, a, b);
       Map<DT, VEC> to;
       to.init(p.y, p.ldy, at, c0, row, c, cols, p.rt);
-      with_activation<DT == F32>(p.act, [&](auto act) {
+      with_activation<DT == F32, -1>(p.act, [&](auto act) {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
           if (i * p.rt < n) finish<DT, VEC>(act, m, a, b, x[i], res[i], p.residual, to, i);
@@ -215,7 +216,7 @@ template <int DT, bool VEC> __global__ __launch_bounds__(MOST_THREADS, DT == BF1
       mean[e] = st[0]; rstd[e] = st[1];
     }
     affine(p, 0, c, rstd, a, b);
-    with_activation<DT == F32>(p.act, [&](auto act) {
+    with_activation<DT == F32, -1>(p.act, [&](auto act) {
       auto finish_batch = [&](const Batch<DT, VEC>& d, int q) {
         Map<DT, VEC> to;
         to.init(p.y, p.ldy, image + q, 0, row, c, cols, p.rt);

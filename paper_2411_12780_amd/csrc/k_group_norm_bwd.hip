@@ -152,9 +152,10 @@ template <int GV> __device__ __forceinline__ void group_means(const NormArgs& p,
   }
 }
 
-// An image's slab in registers: channel sums, which are left in p.sums, and the gradient
-template <int DT, bool VEC, int GV, bool BYTES, int MI>
-__global__ __launch_bounds__(MOST_THREADS) void group_norm_bwd_kernel(NormArgs p) {
+// An image's slab in registers: channel sums, which are left in p.sums, and the gradient.  Straight and curved activations are kernels of their own: the
+// former take 40 to 50 registers less, which gives a unit two workgroups of 512 (1024 x 32 x 32 x 16, one group of 8, ReLU, 39 us; 54 in one kernel).
+template <int DT, bool VEC, int GV, bool BYTES, bool CURVED, int MI>
+__global__ __launch_bounds__(MOST_THREADS, !CURVED && GV <= 4 && MI * (DT == BF16 ? 1 : 2) <= 4 ? 4 : 2) void group_norm_bwd_kernel(NormArgs p) {
   extern __shared__ float room[];
   const int t = threadIdx.x, row = quotient(t, p.over_npc), col = t - row * p.npc;
   const bool live = row < p.rt;
@@ -177,8 +178,10 @@ __global__ __launch_bounds__(MOST_THREADS) void group_norm_bwd_kernel(NormArgs p
     }
     Channels<GV> k;
     k.load(p, w.image, c0, c);
-    with_activation<DT == F32>(p.act, [&](auto act) {
-      float sums[16], h[8], d[8];
+    // slopes of curved activations are worked out once, where there is room for what comes of them (1024 x 32 x 32 x 16 with GELU 52 us, 61 twice)
+    constexpr bool HELD = CURVED && MI * (DT == BF16 ? 1 : 2) <= 4;
+    with_activation<DT == F32, CURVED>(p.act, [&](auto act) {
+      float sums[16], h[8], d[8], held[HELD ? MI : 1][8];
 #pragma unroll
       for (int e = 0; e < 16; ++e) sums[e] = 0.f;
 #pragma unroll
@@ -187,7 +190,10 @@ __global__ __launch_bounds__(MOST_THREADS) void group_norm_bwd_kernel(NormArgs p
         k.xhat(x[i], h);
         k.gradient(act, dy[i], side[i], m.has_side, h, d);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { sums[e] += d[e]; sums[8 + e] += d[e] * h[e]; }
+        for (int e = 0; e < 8; ++e) {
+          sums[e] += d[e]; sums[8 + e] += d[e] * h[e];
+          if (HELD) held[HELD ? i : 0][e] = d[e];
+        }
       }
       column_sums<16>(sums, p, room);
       __syncthreads();
@@ -203,12 +209,17 @@ __global__ __launch_bounds__(MOST_THREADS) void group_norm_bwd_kernel(NormArgs p
       float ga[GV], gb[GV];
       group_means<GV>(p, room, room + 2 * cols, c, ga, gb);
 #pragma unroll
-      for (int i = 0; i < MI; ++i) { again(x[i]); again(dy[i]); }
+      for (int i = 0; i < MI; ++i) { again(x[i]); if (!HELD) again(dy[i]); }
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         if (i * p.rt >= n) continue;
         k.xhat(x[i], h);
-        k.gradient(act, dy[i], side[i], m.has_side, h, d);
+        if (HELD) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) d[e] = held[HELD ? i : 0][e];
+        } else {
+          k.gradient(act, dy[i], side[i], m.has_side, h, d);
+        }
         k.out(m.dx, m.dres, p.dres, i, ga, gb, h, d);
       }
     });
@@ -238,8 +249,8 @@ template <int DT, bool VEC, bool BYTES> struct Batch {
     }
   }
 };
-template <int DT, int MODE, bool VEC, int GV, bool BYTES>
-__global__ __launch_bounds__(MOST_THREADS, GV == 1 && DT == BF16 ? 4 : 2) void group_norm_bwd_piece_kernel(NormArgs p) {
+template <int DT, int MODE, bool VEC, int GV, bool BYTES, bool CURVED>
+__global__ __launch_bounds__(MOST_THREADS, DT == BF16 && (GV == 1 || (!CURVED && (GV < 8 || MODE == PART))) ? 4 : 2) void group_norm_bwd_piece_kernel(NormArgs p) {
   extern __shared__ float room[];
   typedef Batch<DT, VEC, BYTES> B;
   const int t = threadIdx.x, row = quotient(t, p.over_npc), col = t - row * p.npc;
@@ -262,7 +273,7 @@ __global__ __launch_bounds__(MOST_THREADS, GV == 1 && DT == BF16 ? 4 : 2) void g
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) sums[e] = 0.f;
-    with_activation<DT == F32>(p.act, [&](auto act) {
+    with_activation<DT == F32, CURVED>(p.act, [&](auto act) {
       auto work = [&](const B& b, int q) {
         Maps<DT, VEC, BYTES> m;
         m.init(p, image + q, 0, row, c);
@@ -328,7 +339,7 @@ __global__ __launch_bounds__(256) void group_norm_zero_kernel(float* a, float* b
 }
 
 static_assert(4 * 4096 * sizeof(float) <= 64 * 1024, "what a launch has without asking");
-template <int DT, bool VEC, int GV, bool BYTES> int launches(hipStream_t s, const GroupNorm& g, NormArgs& p, const Layout& l, float* d_scale, float* d_shift, float* ws) {
+template <int DT, bool VEC, int GV, bool BYTES, bool CURVED> int launches(hipStream_t s, const GroupNorm& g, NormArgs& p, const Layout& l, float* d_scale, float* d_shift, float* ws) {
   constexpr int MOST = DT == BF16 ? 8 : 4;
   const int C = g.channels;
   // sums of the columns, or channel sums and those of their groups
@@ -336,29 +347,34 @@ template <int DT, bool VEC, int GV, bool BYTES> int launches(hipStream_t s, cons
   const dim3 grid(grid_of(p)), block(l.threads), columns((2 * C + 15) / 16);
   p.sums = ws;
   if (l.whole) {
-    if (l.mi <= MOST / 2) hipLaunchKernelGGL((group_norm_bwd_kernel<DT, VEC, GV, BYTES, MOST / 2>), grid, block, lds, s, p);
-    else hipLaunchKernelGGL((group_norm_bwd_kernel<DT, VEC, GV, BYTES, MOST>), grid, block, lds, s, p);
+    if (l.mi <= MOST / 2) hipLaunchKernelGGL((group_norm_bwd_kernel<DT, VEC, GV, BYTES, CURVED, MOST / 2>), grid, block, lds, s, p);
+    else hipLaunchKernelGGL((group_norm_bwd_kernel<DT, VEC, GV, BYTES, CURVED, MOST>), grid, block, lds, s, p);
     PPLL_HIP(hipGetLastError());
   } else {
     p.parts = ws + (int64_t)g.images * 2 * C;
-    hipLaunchKernelGGL((group_norm_bwd_piece_kernel<DT, PART, VEC, GV, BYTES>), grid, block, lds, s, p);
+    hipLaunchKernelGGL((group_norm_bwd_piece_kernel<DT, PART, VEC, GV, BYTES, CURVED>), grid, block, lds, s, p);
     PPLL_HIP(hipGetLastError());
     // pieces into images
     hipLaunchKernelGGL(group_norm_sum_kernel, dim3(columns.x, std::min(g.images, 65535)), dim3(1024), 0, s, p.parts, p.chunks, (int64_t)p.chunks * 2 * C, g.images, C,
                        p.sums, (float*)nullptr, (float*)nullptr);
     PPLL_HIP(hipGetLastError());
-    hipLaunchKernelGGL((group_norm_bwd_piece_kernel<DT, APPLY, VEC, GV, BYTES>), grid, block, lds, s, p);
+    hipLaunchKernelGGL((group_norm_bwd_piece_kernel<DT, APPLY, VEC, GV, BYTES, CURVED>), grid, block, lds, s, p);
     PPLL_HIP(hipGetLastError());
   }
   hipLaunchKernelGGL(group_norm_sum_kernel, columns, dim3(1024), 0, s, p.sums, g.images, (int64_t)0, 1, C, (float*)nullptr, d_scale, d_shift);
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }
+template <int DT, bool BYTES, bool CURVED> int bwd_as(hipStream_t s, const GroupNorm& g, NormArgs& p, const Layout& l, float* d_scale, float* d_shift, float* ws) {
+  if (p.slab % 8) return launches<DT, false, 8, BYTES, CURVED>(s, g, p, l, d_scale, d_shift, ws);
+  if (p.cg % 2) return launches<DT, true, 8, BYTES, CURVED>(s, g, p, l, d_scale, d_shift, ws);
+  if (p.cg % 4) return launches<DT, true, 4, BYTES, CURVED>(s, g, p, l, d_scale, d_shift, ws);
+  if (p.cg % 8) return launches<DT, true, 2, BYTES, CURVED>(s, g, p, l, d_scale, d_shift, ws);
+  return launches<DT, true, 1, BYTES, CURVED>(s, g, p, l, d_scale, d_shift, ws);
+}
 template <int DT, bool BYTES> int bwd(hipStream_t s, const GroupNorm& g, NormArgs& p, const Layout& l, float* d_scale, float* d_shift, float* ws) {
-  if (p.slab % 8) return launches<DT, false, 8, BYTES>(s, g, p, l, d_scale, d_shift, ws);
-  if (p.cg % 4) return launches<DT, true, 8, BYTES>(s, g, p, l, d_scale, d_shift, ws);
-  if (p.cg % 8) return launches<DT, true, 2, BYTES>(s, g, p, l, d_scale, d_shift, ws);
-  return launches<DT, true, 1, BYTES>(s, g, p, l, d_scale, d_shift, ws);
+  if (p.act == PPLL_ACT_SILU || p.act == PPLL_ACT_GELU) return bwd_as<DT, BYTES, true>(s, g, p, l, d_scale, d_shift, ws);
+  return bwd_as<DT, BYTES, false>(s, g, p, l, d_scale, d_shift, ws);
 }
 }  // namespace
 
