@@ -7,6 +7,7 @@
 // stages of 32 k.  Operands of any alignment: 16-byte loads from where the elements lie; the last pieces of a ragged row are read ending at the
 // row's end and shifted.
 #include <algorithm>
+#include <cmath>
 
 #include "bytes.h"
 
@@ -404,8 +405,21 @@ bool lies_whole(const void* p, int64_t ld) { return !p || (ld % 8 == 0 && ((uint
 bool lies_near(const ByteLinear& l, const ppll_rows& r) { return !r.p || l.rows * r.ld < 1 << 29; }       // (elements, as in values_fit)
 // Microseconds, this kernel / values, both gradients, rows x in x out: 8320 x 1536 x 384 51 / 63, 25216 x 768 x 768 101 / 111, 4096 x 2048 x 2048 93 / 99,
 // 8320 x 1536 x 1536 143 / 116, 25216 x 768 x 2304 248 / 191, 8192 x 4096 x 4096 744 / 505, 512 x 6144 x 6144 156 / 138; with few output channels X's way
-// counts for more: 32768 x 4096 x 256 236 / 286.
-bool values_for_both(const ByteLinear& l) { return values_fit(l) && 4.0 * l.rows * l.in * l.out >= 7.5e10 && l.out >= 512; }
+// counts for more: 32768 x 4096 x 256 236 / 286.  So far the large ones.  With few rows the workgroups of dX, one after the other through all output
+// channels, leave units idle (128 x 1024 x 4096 61 / 26, 640 x 768 x 2304 42 / 30, 128 x 4096 x 1024 23 / 25, 640 x 768 x 768 20 / 22): there the times of
+// both are estimated, steps of the longest workgroup and steps of a unit's share against operations and elements.  Fitted to 114 products of 17 to
+// 20124 rows and 64 to 5680 channels each way; taken together they run 0.8 % longer than with the better one at each, the worst of them 37 %.
+bool values_for_both(const ByteLinear& l) {
+  if (!values_fit(l)) return false;
+  const double m = l.rows, in = l.in, out = l.out;
+  if (4 * m * in * out >= 7.5e10) return out >= 512;
+  const Parts p = parts_of(l);
+  auto pieces = [](double a, double of) { return std::ceil(a / of); };
+  const double k_dx = pieces(out, 64), k_dw = pieces(m, 64), columns = pieces(in, BN);
+  const double share = (pieces(m, BM) * columns * k_dx + columns * pieces(out, BN) * k_dw) / 256;
+  const double here = 4.4 + 0.8 * std::max(k_dx, p.k / 64.0) + 0.5 * share + (p.n > 1 ? 4.2 : 0);
+  return 14.1 + 1.3 * 4e-9 * m * in * out + 1.6e-6 * (m + out) * in + 1.2e-3 * m < here;
+}
 // (dX alone: W alone is written out.  8320 x 1536 x 384 30 / 24, 25216 x 768 x 768 54 / 35, 640 x 768 x 768 14.7 / 8.6, 8320 x 384 x 384 10.5 / 11.6)
 GemmArgs dw_product(const ByteLinear& l, const uint16_t* xv, const ppll_rows& dy, float* dw, float* db) {
   GemmArgs g{};

@@ -283,6 +283,13 @@ def test_backward_of_a_wide_layer():
     assert torch.equal(dx.view, both) and bool((ws[size:] == 0x77).all())
 
 
+@pytest.mark.parametrize("size", [(1, 16, 4096), (20, 88, 1344), (60, 224, 2432), (128, 1024, 4096), (499, 1632, 3352), (640, 768, 2304)])
+def test_backward_of_few_rows_and_many_channels(size):
+    # as values by the rules; with rows that do not lie whole the same gradients on the other way
+    check_backward(Layer(*size, torch.bfloat16, seed=5), True)
+    check_backward(Layer(*size, torch.bfloat16, seed=5, room=1), True)
+
+
 def test_backward_of_many_rows():
     check_backward(Layer(8320, 384, 128, torch.bfloat16), True)
     check_backward(Layer(20000, 40, 24, torch.bfloat16))
