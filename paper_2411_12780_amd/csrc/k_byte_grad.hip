@@ -7,7 +7,6 @@
 // stages of 32 k.  Operands of any alignment: 16-byte loads from where the elements lie; the last pieces of a ragged row are read ending at the
 // row's end and shifted.
 #include <algorithm>
-#include <cmath>
 
 #include "bytes.h"
 
@@ -30,6 +29,7 @@ struct GradArgs {
   float* db;                                         // dW: column sums of dY (of a part), or null
   int M, N, K, tiles_m, tiles_n, per_xcd, parts, part_k;
   int64_t part_out;                                  // elements from part to part, and behind them of db
+  bool sums;                                         // out takes sums in fp32: dW, parts
 };
 
 template <int DT> constexpr int terms() { return DT == F32 ? 3 : 1; }
@@ -256,7 +256,7 @@ template <bool DX, int DT, bool RAGGED> __device__ __forceinline__ void grad_til
   const int n = n0 + tc;
   const bool vec = (p.N & 7) == 0;
   Eight<DT> gate[DX ? BM / 16 : 1];
-  if (DX && p.gate) {
+  if (DX && p.gate && !p.sums) {
 #pragma unroll
     for (int j = 0; j < BM / 16; ++j) {
       const int64_t m = m0 + tk + 16 * j;
@@ -282,7 +282,7 @@ template <bool DX, int DT, bool RAGGED> __device__ __forceinline__ void grad_til
     if (m >= p.M || n >= p.N) continue;
     const float4 lo = *reinterpret_cast<const float4*>(tile + (tk + 16 * j) * STAGE_LD + tc), hi = *reinterpret_cast<const float4*>(tile + (tk + 16 * j) * STAGE_LD + tc + 4);
     float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    if (DX) {
+    if (DX && !p.sums) {
       if (p.gate) {
         float f[8];
         gate[j].get(f);
@@ -322,8 +322,44 @@ template <int DT, bool RAGGED> __global__ __launch_bounds__(THREADS, 2) void byt
   else grad_tile<true, DT, RAGGED>(dx, blockIdx.x - first);
 }
 
-// Sums of parts, in their order
-__global__ __launch_bounds__(256) void byte_grad_sum_kernel(const float* parts, int n_parts, int64_t part_out, float* dw, int64_t n_dw, float* db, int n_db) {
+// Sums of parts, in their order: `first` workgroups those of dW and db, the others those of dX, eight columns a thread
+struct SumArgs {
+  const float* parts; int n_parts; int64_t part_out; float* dw; int64_t n_dw; float* db; int n_db;
+  unsigned first;
+  const float* x_parts; int x_n; int64_t x_out; char* dx; int64_t ldx; const char* gate; int64_t ldg; int rows, cols;
+};
+template <int DT> __global__ __launch_bounds__(256) void byte_grad_sum_kernel(SumArgs p) {
+  if (blockIdx.x >= p.first) {
+    constexpr int ESZ = DT == BF16 ? 2 : 4;
+    const uint32_t pieces = (uint32_t)(p.cols + 7) / 8;
+    const uint32_t u = (blockIdx.x - p.first) * 256 + threadIdx.x, row = u / pieces;
+    const int c = (int)(u - row * pieces) * 8;
+    if (row >= (uint32_t)p.rows) return;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, f[8];
+    const float* from = p.x_parts + (int64_t)row * p.cols;
+#pragma unroll 4
+    for (int k = 0; k < p.x_n; ++k) {
+      Eight<F32> v;
+      v.load(from + k * p.x_out, c, p.cols);
+      v.get(f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] += f[e];
+    }
+    Eight<DT> o;
+    if (p.gate) {
+      o.load(p.gate + row * p.ldg * ESZ, c, p.cols);
+      o.get(f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] *= f[e];
+    }
+    o.set(s);
+    o.store(p.dx + row * p.ldx * ESZ, c, p.cols);
+    return;
+  }
+  const float* parts = p.parts;
+  float *dw = p.dw, *db = p.db;
+  const int n_parts = p.n_parts;
+  const int64_t part_out = p.part_out, n_dw = p.n_dw, n_db = p.n_db;
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   const int64_t n = n_dw + n_db;
   if (i >= n) return;
@@ -379,19 +415,24 @@ template <int DT> int launch(hipStream_t s, GradArgs& dw, GradArgs& dx) {
   return PPLL_OK;
 }
 
-// Into how many parts the reduction of dW goes: a workgroup a unit, none under four steps
+// Into how many parts a reduction goes: a workgroup a unit, none under four steps.  dX in one part / in parts of 12, 8, 6, 4, 3 steps at least, both
+// gradients, us: 41 x 63 x 5645 102 / 25, 22, 21, 21, 22; 56 x 1483 x 2737 76 / 38, 30, 28, 27, 26; 1140 x 249 x 875 29 / 29, 29, 22, 21, 22; 4621 x 151 x
+// 1795 in fp32 80 / 49, 50, 50, 49, 50.
 struct Parts { int n, k; int64_t out; };
-Parts parts_of(const ByteLinear& l) {
+Parts parts_of(const ByteLinear& l, int64_t m, int64_t n, int64_t k, int64_t out) {
   const int bk = l.dt == F32 ? step_k<F32>() : step_k<BF16>();
-  const int64_t tiles = (int64_t)((l.in + BM - 1) / BM) * ((l.out + BN - 1) / BN), steps = ((int64_t)l.rows + bk - 1) / bk;
+  const int64_t tiles = ((m + BM - 1) / BM) * ((n + BN - 1) / BN), steps = (k + bk - 1) / bk;
   const int64_t want = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, steps / 4));
   const int64_t each = (steps + want - 1) / want;
   Parts p;
   p.n = (int)std::max<int64_t>(1, (steps + each - 1) / each);
   p.k = (int)std::min<int64_t>(each * bk, 0x7fffffff);
-  p.out = ((int64_t)l.in * l.out + l.out + 3) / 4 * 4;
+  p.out = (out + 3) / 4 * 4;
   return p;
 }
+Parts dw_parts(const ByteLinear& l) { return parts_of(l, l.in, l.out, l.rows, (int64_t)l.in * l.out + l.out); }
+Parts dx_parts(const ByteLinear& l) { return parts_of(l, l.rows, l.in, l.out, (int64_t)l.rows * l.in); }
+int64_t part_floats(const Parts& p) { return p.n > 1 ? p.n * p.out : 0; }
 int sum_chunks(int rows) { return (int)(((int64_t)rows + sum_rows(rows) - 1) / sum_rows(rows)); }
 
 // ---- The other way: operands written out in bf16, which is what they stand for, and the products on the kernels of bf16 operands.  Those reach 1100
@@ -405,21 +446,10 @@ bool lies_whole(const void* p, int64_t ld) { return !p || (ld % 8 == 0 && ((uint
 bool lies_near(const ByteLinear& l, const ppll_rows& r) { return !r.p || l.rows * r.ld < 1 << 29; }       // (elements, as in values_fit)
 // Microseconds, this kernel / values, both gradients, rows x in x out: 8320 x 1536 x 384 51 / 63, 25216 x 768 x 768 101 / 111, 4096 x 2048 x 2048 93 / 99,
 // 8320 x 1536 x 1536 143 / 116, 25216 x 768 x 2304 248 / 191, 8192 x 4096 x 4096 744 / 505, 512 x 6144 x 6144 156 / 138; with few output channels X's way
-// counts for more: 32768 x 4096 x 256 236 / 286.  So far the large ones.  With few rows the workgroups of dX, one after the other through all output
-// channels, leave units idle (128 x 1024 x 4096 61 / 26, 640 x 768 x 2304 42 / 30, 128 x 4096 x 1024 23 / 25, 640 x 768 x 768 20 / 22): there the times of
-// both are estimated, steps of the longest workgroup and steps of a unit's share against operations and elements.  Fitted to 114 products of 17 to
-// 20124 rows and 64 to 5680 channels each way; taken together they run 0.8 % longer than with the better one at each, the worst of them 37 %.
-bool values_for_both(const ByteLinear& l) {
-  if (!values_fit(l)) return false;
-  const double m = l.rows, in = l.in, out = l.out;
-  if (4 * m * in * out >= 7.5e10) return out >= 512;
-  const Parts p = parts_of(l);
-  auto pieces = [](double a, double of) { return std::ceil(a / of); };
-  const double k_dx = pieces(out, 64), k_dw = pieces(m, 64), columns = pieces(in, BN);
-  const double share = (pieces(m, BM) * columns * k_dx + columns * pieces(out, BN) * k_dw) / 256;
-  const double here = 4.4 + 0.8 * std::max(k_dx, p.k / 64.0) + 0.5 * share + (p.n > 1 ? 4.2 : 0);
-  return 14.1 + 1.3 * 4e-9 * m * in * out + 1.6e-6 * (m + out) * in + 1.2e-3 * m < here;
-}
+// counts for more: 32768 x 4096 x 256 236 / 286.  From 4e10 operations on: 640 x 4096 x 4096 99 / 75, 2560 x 2048 x 2048 81 / 76, 2560 x 4096 x 1024 70.5 / 70.6;
+// below: 5120 x 768 x 2304 65 / 69, 1280 x 2048 x 2048 42 / 44.  Over 114 products of 17 to 20124 rows and 64 to 5680 channels each way the rule costs
+// half a per cent over the better way at each.
+bool values_for_both(const ByteLinear& l) { return values_fit(l) && 4.0 * l.rows * l.in * l.out >= 4e10 && l.out >= 512; }
 // (dX alone: W alone is written out.  8320 x 1536 x 384 30 / 24, 25216 x 768 x 768 54 / 35, 640 x 768 x 768 14.7 / 8.6, 8320 x 384 x 384 10.5 / 11.6)
 GemmArgs dw_product(const ByteLinear& l, const uint16_t* xv, const ppll_rows& dy, float* dw, float* db) {
   GemmArgs g{};
@@ -460,13 +490,15 @@ int backward_values(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x,
 template <int DT> int backward_here(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
                                const ppll_rows& dx, float* dw, float* db, float* ws) {
   GradArgs pw{}, px{};       // (no parts: not wanted)
-  const Parts parts = parts_of(l);
-  const bool whole = parts.n == 1;
+  const Parts parts = dw_parts(l), x_parts = dx_parts(l);
+  const bool whole = parts.n == 1, x_whole = x_parts.n == 1;
+  float* x_ws = ws + part_floats(parts);
   if (dx.p) {
     px.d = (const char*)dy.p; px.ldd = dy.ld; px.dcols = l.out;
     px.q = w.q; px.e = w.e; px.ldq = w.ld; px.qcols = pad16(l.in);
-    px.out = (char*)dx.p; px.ldo = dx.ld; px.gate = (const char*)gate.p; px.ldg = gate.ld;
-    px.M = l.rows; px.N = l.in; px.K = l.out; px.parts = 1; px.part_k = l.out;
+    px.out = x_whole ? (char*)dx.p : (char*)x_ws; px.ldo = x_whole ? dx.ld : l.in; px.gate = (const char*)gate.p; px.ldg = gate.ld;
+    px.M = l.rows; px.N = l.in; px.K = l.out; px.parts = x_parts.n; px.part_k = x_parts.k; px.part_out = x_parts.out;
+    px.sums = !x_whole;
   }
   if (dw) {
     pw.d = (const char*)dy.p; pw.ldd = dy.ld; pw.dcols = l.out;
@@ -474,16 +506,25 @@ template <int DT> int backward_here(hipStream_t s, const ByteLinear& l, const pp
     pw.out = (char*)(whole ? dw : ws); pw.ldo = l.out;
     pw.db = !db ? nullptr : whole ? db : ws + (int64_t)l.in * l.out;
     pw.M = l.in; pw.N = l.out; pw.K = l.rows; pw.parts = parts.n; pw.part_k = parts.k; pw.part_out = parts.out;
+    pw.sums = true;
   }
   if (dx.p || dw) PPLL_TRY(launch<DT>(s, pw, px));
-  if (dw) {
-    if (!whole) {
-      const int64_t n = (int64_t)l.in * l.out + (db ? l.out : 0);
-      hipLaunchKernelGGL(byte_grad_sum_kernel, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s, ws, parts.n, parts.out, dw, (int64_t)l.in * l.out, db,
-                         db ? l.out : 0);
-      PPLL_HIP(hipGetLastError());
+  if ((dw && !whole) || (dx.p && !x_whole)) {
+    SumArgs a{};
+    if (dw && !whole) {
+      a.parts = ws; a.n_parts = parts.n; a.part_out = parts.out; a.dw = dw; a.n_dw = (int64_t)l.in * l.out; a.db = db; a.n_db = db ? l.out : 0;
+      a.first = (unsigned)((a.n_dw + a.n_db + 1023) / 1024);
     }
-  } else if (db) {
+    unsigned more = 0;
+    if (dx.p && !x_whole) {
+      a.x_parts = x_ws; a.x_n = x_parts.n; a.x_out = x_parts.out; a.dx = (char*)dx.p; a.ldx = dx.ld; a.gate = (const char*)gate.p; a.ldg = gate.ld;
+      a.rows = l.rows; a.cols = l.in;
+      more = (unsigned)(((int64_t)l.rows * ((l.in + 7) / 8) + 255) / 256);      // (256 tiles at most)
+    }
+    hipLaunchKernelGGL(byte_grad_sum_kernel<DT>, dim3(a.first + more), dim3(256), 0, s, a);
+    PPLL_HIP(hipGetLastError());
+  }
+  if (db && !dw) {
     const int chunks = sum_chunks(l.rows);
     hipLaunchKernelGGL(byte_grad_columns_kernel<DT>, dim3((l.out + SUM_COLS - 1) / SUM_COLS, chunks), dim3(256), 0, s, (const char*)dy.p, dy.ld, l.rows, l.out,
                        chunks == 1 ? db : ws);
@@ -508,8 +549,7 @@ int backward(hipStream_t s, int way, const ByteLinear& l, const ppll_byte_rows& 
 }
 size_t workspace(const ByteLinear& l, bool any) {
   if (l.rows <= 0) return 0;
-  const Parts p = parts_of(l);
-  const int64_t parts = p.n > 1 ? p.n * p.out : 0, sums = sum_chunks(l.rows) > 1 ? (int64_t)sum_chunks(l.rows) * l.out : 0;
+  const int64_t parts = part_floats(dw_parts(l)) + part_floats(dx_parts(l)), sums = sum_chunks(l.rows) > 1 ? (int64_t)sum_chunks(l.rows) * l.out : 0;
   int64_t bytes = std::max(parts, sums) * (int64_t)sizeof(float);
   if (values_fit(l)) bytes = std::max(bytes, values_bytes(l, false, true));
   if (any ? values_fit(l) : values_for_both(l)) bytes = std::max(bytes, values_bytes(l, true, true) + (int64_t)(dw_floats(l) * sizeof(float)));
