@@ -24,10 +24,10 @@ struct NormArgs {
   int slab, slabs, npc, rt, pow2;  // channels of a slab; npc: piece columns, pow2: a power of two up to 64
   int chunk, chunks, units;        // pixels of a piece, pieces of an image, workgroups' work
   int spg;                         // segments of a group
-  float eps, over_cg, over_npc;    // 1 / cg, 1 / npc: see quotient()
+  float eps, over_cg, over_npc, over_spg;    // 1 / cg, 1 / npc, 1 / spg: see quotient()
 };
 
-// v / n for 0 <= v < 4096 and 1 <= n <= 4096, over = 1 / n: (v + 1/2) / n is at least 1 / (2 n) off every whole number, its value in fp32 less than 2^-12 of
+// v / n for 0 <= v <= 4096 and 1 <= n <= 4096, over = 1 / n: (v + 1/2) / n is at least 1 / (2 n) off every whole number, its value in fp32 less than 2^-12 of
 // that (two instructions; a division of whole numbers takes some thirty)
 __device__ __forceinline__ int quotient(int v, float over) { return (int)(((float)v + 0.5f) * over); }
 
@@ -121,24 +121,35 @@ template <int NV> __device__ __forceinline__ void column_sums(float (&v)[NV], co
 #pragma unroll
   for (int i = 0; i < NV; ++i) v[i] = live ? room[i * p.npc + col] : 0.f;
 }
-// Of GV segments of a thread's piece (their column sums) the sums of their groups.  room: npc GV floats
+// Sums of `sets` runs of n neighbouring floats in LDS: at(k) the first of run k, put(k, sum) by one lane.  A lane a short run, 16 one of
+// some length, 64 a long one.
+template <class AT, class PUT> __device__ __forceinline__ void runs_sums(int sets, int n, AT at, PUT put) {
+  const int log = n <= 4 ? 0 : n <= 64 ? 4 : 6, lane = threadIdx.x & ((1 << log) - 1);
+#pragma unroll 1
+  for (int k = threadIdx.x >> log; k < sets; k += blockDim.x >> log) {
+    const float* from = at(k);
+    float s = 0.f;
+#pragma unroll 1
+    for (int i = lane; i < n; i += 1 << log) s += from[i];
+    if (log) s = log == 4 ? lanes_sum<16>(s) : lanes_sum<64>(s);
+    if (lane == 0) put(k, s);
+  }
+}
+// Of GV segments of a thread's piece (their column sums) the sums of their groups.  room: npc GV floats and one a group.  (A thread by itself, going
+// through all segments of its groups, took two thirds of the time of wide groups: 20 x 165 x 317, one group, 67 us, so 29; 28 x 96 x 496, four groups, 51 and 15.)
 template <int GV> __device__ __forceinline__ void group_sums(float (&v)[GV], const NormArgs& p, float* room) {
   if (p.spg == 1) return;
-  const int col = (int)threadIdx.x - quotient(threadIdx.x, p.over_npc) * p.npc;
+  const int col = (int)threadIdx.x - quotient(threadIdx.x, p.over_npc) * p.npc, groups = quotient(p.slab, p.over_cg);
+  float* sums = room + p.npc * GV;
   __syncthreads();
   if ((int)threadIdx.x < p.npc)
 #pragma unroll
     for (int i = 0; i < GV; ++i) room[col * GV + i] = v[i];
   __syncthreads();
-  const int segments = p.slab / p.cg * p.spg;
+  runs_sums(groups, p.spg, [&](int g) { return room + g * p.spg; }, [&](int g, float s) { sums[g] = s; });
+  __syncthreads();
 #pragma unroll
-  for (int i = 0; i < GV; ++i) {
-    const int seg = col * GV + i, g0 = seg / p.spg * p.spg;
-    float s = 0.f;
-    if (seg < segments)
-      for (int k = 0; k < p.spg; ++k) s += room[g0 + k];
-    v[i] = s;
-  }
+  for (int i = 0; i < GV; ++i) v[i] = sums[min(quotient(col * GV + i, p.over_spg), groups - 1)];      // (behind the last channel: any)
 }
 
 // A unit of work: an image's slab, or its piece of pixels
@@ -205,11 +216,13 @@ inline Layout layout_of(const GroupNorm& g) {
   Layout l{};
   const int size = g.dt == BF16 ? 2 : 4;
   l.chunk = l.stretch = g.pixels;
-  // slabs of whole groups whose rows of a pixel are whole pieces and 64 bytes or more; the widest that fits
+  // slabs of whole groups whose rows of a pixel are whole pieces and 64 bytes or more, 32 in a map that stays in the L2s; the widest that fits
+  // (bf16, forward and backward, in slabs of 32 bytes / in pieces of pixels: 10 x 756 x 384 16, 22 / 25, 38 us; 128 x 1600 x 256 100, 167 / 80, 173)
+  const int least = (int64_t)g.images * g.pixels * g.channels * size <= 16 << 20 ? 32 : 64;
   for (int n = 1; n <= g.groups && !l.whole; ++n) {
     if (g.groups % n) continue;
     const int slab = g.channels / n;
-    if (n > 1 && (slab % 8 || slab * size < 64)) continue;
+    if (n > 1 && (slab % 8 || slab * size < least)) continue;
     if (g.pixels <= (int64_t)(MOST_THREADS / piece_columns(slab)) * most_mi(g.dt)) { l.whole = true; set_slab(g, l, slab); }
   }
   if (!l.whole) {
@@ -244,7 +257,7 @@ inline NormArgs args_of(const GroupNorm& g, const Layout& l, int chunk) {
   p.over_cg = 1.f / (float)p.cg; p.over_npc = 1.f / (float)p.npc;
   return p;
 }
-inline int segments_of(int cg) { return cg % 8 == 0 ? 1 : cg == 4 ? 2 : cg == 2 ? 4 : 8; }
+inline int segments_of(int cg) { return cg % 8 == 0 ? 1 : cg % 4 == 0 ? 2 : cg % 2 == 0 ? 4 : 8; }
 inline unsigned grid_of(const NormArgs& p) { return (unsigned)std::min(p.units, (int)MOST_BLOCKS); }
 
 }  // namespace norm

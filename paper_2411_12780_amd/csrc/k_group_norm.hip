@@ -58,7 +58,7 @@ template <int DT> __device__ __forceinline__ void keep_piece(const NormArgs& p, 
 // one group; MI: pieces a thread holds.  Up to 4 of them within 128 registers, so that a unit has two workgroups of 512, one's memory busy during the
 // other's sums (1024 x 32 x 32 x 16, groups of 2, 25 us; 33 with the 129 registers that the compiler took by itself).
 template <int DT, int MODE, bool VEC, int GV, int MI>
-__global__ __launch_bounds__(MOST_THREADS, MI * (DT == BF16 ? 1 : 2) <= 4 && GV <= 4 ? 4 : 2) void group_norm_fwd_kernel(NormArgs p) {
+__global__ __launch_bounds__(MOST_THREADS, MODE == PART || (MI * (DT == BF16 ? 1 : 2) <= 4 && GV <= 4) || (DT == F32 && GV == 1) ? 4 : 2) void group_norm_fwd_kernel(NormArgs p) {
   constexpr int PER = 8 / GV;
   extern __shared__ float room[];
   const int t = threadIdx.x, row = quotient(t, p.over_npc), col = t - row * p.npc;
@@ -198,7 +198,7 @@ template <int DT, bool VEC> struct Batch {
     }
   }
 };
-template <int DT, bool VEC> __global__ __launch_bounds__(MOST_THREADS, DT == BF16 ? 4 : 2) void group_norm_apply_kernel(NormArgs p) {
+template <int DT, bool VEC, bool CURVED> __global__ __launch_bounds__(MOST_THREADS, DT == BF16 ? 4 : 2) void group_norm_apply_kernel(NormArgs p) {
   constexpr int N = Batch<DT, VEC>::N;
   const int t = threadIdx.x, row = quotient(t, p.over_npc), col = t - row * p.npc;
   if (row >= p.rt) return;
@@ -216,7 +216,7 @@ template <int DT, bool VEC> __global__ __launch_bounds__(MOST_THREADS, DT == BF1
       mean[e] = st[0]; rstd[e] = st[1];
     }
     affine(p, 0, c, rstd, a, b);
-    with_activation<DT == F32, -1>(p.act, [&](auto act) {
+    with_activation<DT == F32, CURVED>(p.act, [&](auto act) {
       auto finish_batch = [&](const Batch<DT, VEC>& d, int q) {
         Map<DT, VEC> to;
         to.init(p.y, p.ldy, image + q, 0, row, c, cols, p.rt);
@@ -236,7 +236,7 @@ template <int DT, bool VEC> __global__ __launch_bounds__(MOST_THREADS, DT == BF1
 
 template <int DT, int MODE, bool VEC, int GV> int fwd_launch(hipStream_t s, const NormArgs& p, const Layout& l) {
   constexpr int MOST = DT == BF16 ? 8 : 4;
-  const size_t lds = sizeof(float) * (size_t)(l.threads * GV);
+  const size_t lds = sizeof(float) * (size_t)(l.threads * GV + p.slab / p.cg);
   const dim3 grid(grid_of(p)), block(l.threads);
   if (MODE == PART) hipLaunchKernelGGL((group_norm_fwd_kernel<DT, MODE, VEC, GV, PART_MI>), grid, block, lds, s, p);
   else if (l.mi <= MOST / 2) hipLaunchKernelGGL((group_norm_fwd_kernel<DT, WHOLE, VEC, GV, MOST / 2>), grid, block, lds, s, p);
@@ -248,11 +248,19 @@ template <int DT, int MODE> int fwd(hipStream_t s, NormArgs& p, const Layout& l)
   const bool vec = p.slab % 8 == 0;
   const int gv = vec ? segments_of(p.cg) : 8;
   p.spg = p.cg * gv / 8;
+  p.over_spg = 1.f / (float)p.spg;
   if (!vec) return fwd_launch<DT, MODE, false, 8>(s, p, l);
   if (gv == 1) return fwd_launch<DT, MODE, true, 1>(s, p, l);
   if (gv == 2) return fwd_launch<DT, MODE, true, 2>(s, p, l);
   if (gv == 4) return fwd_launch<DT, MODE, true, 4>(s, p, l);
   return fwd_launch<DT, MODE, true, 8>(s, p, l);
+}
+template <int DT, bool VEC> int apply(hipStream_t s, const NormArgs& p, const Layout& l) {
+  const dim3 grid(grid_of(p)), block(l.threads);
+  if (p.act == PPLL_ACT_SILU || p.act == PPLL_ACT_GELU) hipLaunchKernelGGL((group_norm_apply_kernel<DT, VEC, true>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((group_norm_apply_kernel<DT, VEC, false>), grid, block, 0, s, p);
+  PPLL_HIP(hipGetLastError());
+  return PPLL_OK;
 }
 template <int DT> int fwd_all(hipStream_t s, const GroupNorm& g, NormArgs& p, const Layout& l, float* ws) {
   if (l.whole) return fwd<DT, WHOLE>(s, p, l);
@@ -263,10 +271,7 @@ template <int DT> int fwd_all(hipStream_t s, const GroupNorm& g, NormArgs& p, co
   PPLL_HIP(hipGetLastError());
   p.stats_in = joined;
   p.chunk = l.stretch; p.chunks = chunks_of(g, l.stretch); p.units = units_of(p);
-  if (p.slab % 8 == 0) hipLaunchKernelGGL((group_norm_apply_kernel<DT, true>), dim3(grid_of(p)), dim3(l.threads), 0, s, p);
-  else hipLaunchKernelGGL((group_norm_apply_kernel<DT, false>), dim3(grid_of(p)), dim3(l.threads), 0, s, p);
-  PPLL_HIP(hipGetLastError());
-  return PPLL_OK;
+  return p.slab % 8 == 0 ? apply<DT, true>(s, p, l) : apply<DT, false>(s, p, l);
 }
 }  // namespace
 

@@ -138,12 +138,8 @@ template <int GV> __device__ __forceinline__ void group_means(const NormArgs& p,
   const int cols = p.slab;
   const float over = 1.f / (float)((int64_t)p.pixels * p.cg);
   __syncthreads();
-  for (int k = threadIdx.x; k < 2 * (cols / p.cg); k += blockDim.x) {
-    float s = 0.f;
-    const float* from = chan + (k & 1) * cols + (k >> 1) * p.cg;
-    for (int j = 0; j < p.cg; ++j) s += from[j];
-    group[k] = s * over;
-  }
+  runs_sums(2 * quotient(cols, p.over_cg), p.cg, [&](int k) { return chan + (k & 1) * cols + (k >> 1) * p.cg; },
+            [&](int k, float s) { group[k] = s * over; });
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < GV; ++e) {
@@ -153,7 +149,7 @@ template <int GV> __device__ __forceinline__ void group_means(const NormArgs& p,
 }
 
 // An image's slab in registers: channel sums, which are left in p.sums, and the gradient.  Straight and curved activations are kernels of their own: the
-// former take 40 to 50 registers less, which gives a unit two workgroups of 512 (1024 x 32 x 32 x 16, one group of 8, ReLU, 39 us; 54 in one kernel).
+// former take 40 to 50 registers less, which gives a unit two workgroups of 512 (1024 x 32 x 32 x 16, two groups, ReLU, 41 us; 54 in one kernel).
 template <int DT, bool VEC, int GV, bool BYTES, bool CURVED, int MI>
 __global__ __launch_bounds__(MOST_THREADS, !CURVED && GV <= 4 && MI * (DT == BF16 ? 1 : 2) <= 4 ? 4 : 2) void group_norm_bwd_kernel(NormArgs p) {
   extern __shared__ float room[];
@@ -178,7 +174,7 @@ __global__ __launch_bounds__(MOST_THREADS, !CURVED && GV <= 4 && MI * (DT == BF1
     }
     Channels<GV> k;
     k.load(p, w.image, c0, c);
-    // slopes of curved activations are worked out once, where there is room for what comes of them (1024 x 32 x 32 x 16 with GELU 52 us, 61 twice)
+    // slopes of curved activations are worked out once, where there is room for what comes of them (1024 x 32 x 32 x 16 with GELU 51 us, 61 twice)
     constexpr bool HELD = CURVED && MI * (DT == BF16 ? 1 : 2) <= 4;
     with_activation<DT == F32, CURVED>(p.act, [&](auto act) {
       float sums[16], h[8], d[8], held[HELD ? MI : 1][8];
