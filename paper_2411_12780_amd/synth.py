@@ -72,6 +72,12 @@ WORKLOADS = {
     # the ViT stage trained by Muon, with rotary positions of the 8 x 8 patches and normalised queries and keys
     "vit_stage_muon_bf16": dict(_VIT_STAGE, optimizer=MUON, momentum=0.95, nesterov=1, rotary=1, grid_h=8, grid_w=8, rotary_base=100.0,
                                 qk_norm=1, qk_norm_eps=1e-6),
+    # the ResNet stage with group norms, whose inputs are kept in 8 bits
+    "resnet_stage_group_norm_bf16": dict(arch=RESNET, precision=BF16, input_kind=ACTIVATION, batch=128, num_classes=10, channels=32, height=16, width=16,
+                                         n_basic_blocks=5, aux_channels=64, optimizer=SGD, momentum=0.9, nesterov=1, weight_decay=1e-4, bn_eps=1e-5,
+                                         bn_momentum=0.1, lr=0.01, group_norm=8, byte_checkpoints=1),
+    # the ViT stage with its linear products on rows of 8 bits
+    "vit_stage_bytes_bf16": dict(_VIT_STAGE, byte_products=1),
     # STL-10-shaped ViT stage (96 x 96 images)
     "vit_large_image_bf16": dict(_VIT_STAGE, batch=64, img_h=96, img_w=96, patch=8, tokens=145),
 }
