@@ -144,24 +144,25 @@ __device__ __forceinline__ void bytes_get(uint2 w, float step, float (&v)[8]) {
 __device__ __forceinline__ uint2 bytes_of(const float (&v)[8], float inv) {
   return make_uint2(byte_pack4(v[0], v[1], v[2], v[3], inv), byte_pack4(v[4], v[5], v[6], v[7], inv));
 }
-// The largest of a value over LANES neighbouring lanes (a power of two, 1 to 64), every lane receiving it.  Within 8 lanes by exchanges of
+// The largest of a value over `lanes` neighbouring lanes (a power of two, 1 to 64), every lane receiving it.  Within 8 lanes by exchanges of
 // pairs, of pairs of pairs and the mirror of 8; above as lanes_reduce.
-template <int LANES> __device__ __forceinline__ uint32_t lanes_most(uint32_t v) {
+__device__ __forceinline__ uint32_t lanes_most_of(uint32_t v, int lanes) {
   auto dpp = [](uint32_t x, auto ctrl) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xf, 0xf, true); };
-  if (LANES >= 2) v = max(v, dpp(v, std::integral_constant<int, 0xb1>()));     // quad_perm 1 0 3 2
-  if (LANES >= 4) v = max(v, dpp(v, std::integral_constant<int, 0x4e>()));     // quad_perm 2 3 0 1
-  if (LANES >= 8) v = max(v, dpp(v, std::integral_constant<int, 0x141>()));    // mirror of 8 lanes
-  if (LANES >= 16) v = max(v, dpp(v, std::integral_constant<int, 0x128>()));   // rotation of 16 by 8
-  if (LANES >= 32) {
+  if (lanes >= 2) v = max(v, dpp(v, std::integral_constant<int, 0xb1>()));     // quad_perm 1 0 3 2
+  if (lanes >= 4) v = max(v, dpp(v, std::integral_constant<int, 0x4e>()));     // quad_perm 2 3 0 1
+  if (lanes >= 8) v = max(v, dpp(v, std::integral_constant<int, 0x141>()));    // mirror of 8 lanes
+  if (lanes >= 16) v = max(v, dpp(v, std::integral_constant<int, 0x128>()));   // rotation of 16 by 8
+  if (lanes >= 32) {
     const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
     v = max((uint32_t)r[0], (uint32_t)r[1]);
   }
-  if (LANES >= 64) {
+  if (lanes >= 64) {
     const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
     v = max((uint32_t)r[0], (uint32_t)r[1]);
   }
   return v;
 }
+template <int LANES> __device__ __forceinline__ uint32_t lanes_most(uint32_t v) { return lanes_most_of(v, LANES); }
 __device__ __forceinline__ uint32_t most_of(const float (&v)[8], uint32_t m) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);

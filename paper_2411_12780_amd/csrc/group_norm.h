@@ -20,6 +20,8 @@ struct NormArgs {
   const float *scale, *shift, *stats_in;
   float *stats, *parts;            // parts: what PART leaves and APPLY joins
   float* sums;                     // backward: channel sums of each image, [images][2][C]
+  float *d_scale, *d_shift;        // backward, pieces of pixels: added up by the last `sum_blocks` workgroups of the launch
+  int sum_blocks;
   int images, pixels, C, groups, cg, act;
   int slab, slabs, npc, rt, pow2;  // channels of a slab; npc: piece columns, pow2: a power of two up to 64
   int chunk, chunks, units;        // pixels of a piece, pieces of an image, workgroups' work

@@ -43,8 +43,7 @@ __device__ __forceinline__ void affine(const NormArgs& p, int c0, int c, const f
 template <int DT> __device__ __forceinline__ void keep_piece(const NormArgs& p, const Eight<DT>& x, int64_t pixel, int col, bool in) {
   float v[8];
   x.get(v);
-  uint32_t most = most_of(v, 0);
-  for (int s = 1; s < p.npc; s <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, s));
+  const uint32_t most = lanes_most_of(most_of(v, 0), p.npc);
   const int e = byte_exponent(most);
   if (!in) return;
   const bool nan = e == BYTE_NAN;

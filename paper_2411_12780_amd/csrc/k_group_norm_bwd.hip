@@ -223,8 +223,29 @@ __global__ __launch_bounds__(MOST_THREADS, !CURVED && GV <= 4 && MI * (DT == BF1
   }
 }
 
+// Sums over the first axis of [n][2 C], in its order: a workgroup 16 columns, ROWS rows (a sixteenth of its threads) at a time.  To out [2 C], or (null) the
+// halves to d_shift and d_scale.  part: 17 floats a row.
+template <int ROWS> __device__ __forceinline__ void axis_sums(float* part, int block, const float* in, int n, int C, float* out, float* d_scale, float* d_shift) {
+  const int i = threadIdx.x & 15, c = block * 16 + i, r = threadIdx.x >> 4;
+  float s = 0.f;
+  if (c < 2 * C)
+#pragma unroll 4
+    for (int64_t k = r; k < n; k += ROWS) s += in[k * 2 * C + c];
+  __syncthreads();
+  part[r * 17 + i] = s;
+  __syncthreads();
+  if (r == 0 && c < 2 * C) {
+    s = 0.f;
+    for (int k = 0; k < ROWS; ++k) s += part[k * 17 + i];
+    if (out) out[c] = s;
+    else if (c < C) d_shift[c] = s;
+    else d_scale[c - C] = s;
+  }
+}
+constexpr int SUM_THREADS = 1024;
+
 // Pieces of pixels: PART leaves their channel sums, [images][chunks][2][C]; APPLY takes the gradient from those of the image, p.sums.  Two batches of
-// pieces in turn, one on its way while the other is worked on.
+// pieces in turn, one on its way while the other is worked on.  Beside APPLY the last workgroups add up the images' sums (a launch of its own took 5 us).
 template <int DT, bool VEC, bool BYTES> struct Batch {
   static constexpr int N = DT == BF16 ? 1 : 2;
   typename XMap<DT, VEC, BYTES>::Piece x[N];
@@ -251,8 +272,12 @@ __global__ __launch_bounds__(MOST_THREADS, DT == BF16 && (GV == 1 || (!CURVED &&
   typedef Batch<DT, VEC, BYTES> B;
   const int t = threadIdx.x, row = quotient(t, p.over_npc), col = t - row * p.npc;
   const bool live = row < p.rt;
-  const int units = p.units;
-  for (int u = blockIdx.x; u < units; u += gridDim.x) {
+  const int units = p.units, workers = gridDim.x - (MODE == APPLY ? p.sum_blocks : 0);
+  if (MODE == APPLY && (int)blockIdx.x >= workers) {
+    axis_sums<MOST_THREADS / 16>(room, blockIdx.x - workers, p.sums, p.images, p.C, nullptr, p.d_scale, p.d_shift);
+    return;
+  }
+  for (int u = blockIdx.x; u < units; u += workers) {
     const Unit w = unit_of(p, u);
     const int c = col * 8, cols = p.slab, step = B::N * p.rt, end = live ? w.last - row : 0;      // pixel q + i rt + row is there where q + i rt < end
     const int64_t image = (int64_t)w.image * p.pixels;
@@ -305,29 +330,11 @@ __global__ __launch_bounds__(MOST_THREADS, DT == BF16 && (GV == 1 || (!CURVED &&
   }
 }
 
-// Sums over the first axis of [n][2 C], in its order, of `sets` of them `set_stride` apart: a workgroup 16 columns of a set, 64 rows at a time.  To
-// out [sets][2 C], or (one set) the halves to d_shift and d_scale.
-__global__ __launch_bounds__(1024) void group_norm_sum_kernel(const float* in, int n, int64_t set_stride, int sets, int C, float* out, float* d_scale,
-                                                              float* d_shift) {
-  __shared__ float part[64][17];
-  const int c = blockIdx.x * 16 + (threadIdx.x & 15), r = threadIdx.x >> 4;
-  for (int set = blockIdx.y; set < sets; set += gridDim.y) {
-    const float* from = in + set * set_stride + c;
-    float s = 0.f;
-    if (c < 2 * C)
-#pragma unroll 4
-      for (int64_t k = r; k < n; k += 64) s += from[k * 2 * C];
-    __syncthreads();
-    part[r][threadIdx.x & 15] = s;
-    __syncthreads();
-    if (r == 0 && c < 2 * C) {
-      s = 0.f;
-      for (int k = 0; k < 64; ++k) s += part[k][threadIdx.x];
-      if (out) out[(int64_t)set * 2 * C + c] = s;
-      else if (c < C) d_shift[c] = s;
-      else d_scale[c - C] = s;
-    }
-  }
+__global__ __launch_bounds__(SUM_THREADS) void group_norm_sum_kernel(const float* in, int n, int64_t set_stride, int sets, int C, float* out, float* d_scale,
+                                                                     float* d_shift) {
+  __shared__ float part[SUM_THREADS + SUM_THREADS / 16];
+  for (int set = blockIdx.y; set < sets; set += gridDim.y)
+    axis_sums<SUM_THREADS / 16>(part, blockIdx.x, in + set * set_stride, n, C, out ? out + (int64_t)set * 2 * C : nullptr, d_scale, d_shift);
 }
 __global__ __launch_bounds__(256) void group_norm_zero_kernel(float* a, float* b, int n) {
   const int i = blockIdx.x * 256 + threadIdx.x;
@@ -351,13 +358,15 @@ template <int DT, bool VEC, int GV, bool BYTES, bool CURVED> int launches(hipStr
     hipLaunchKernelGGL((group_norm_bwd_piece_kernel<DT, PART, VEC, GV, BYTES, CURVED>), grid, block, lds, s, p);
     PPLL_HIP(hipGetLastError());
     // pieces into images
-    hipLaunchKernelGGL(group_norm_sum_kernel, dim3(columns.x, std::min(g.images, 65535)), dim3(1024), 0, s, p.parts, p.chunks, (int64_t)p.chunks * 2 * C, g.images, C,
+    hipLaunchKernelGGL(group_norm_sum_kernel, dim3(columns.x, std::min(g.images, 65535)), dim3(SUM_THREADS), 0, s, p.parts, p.chunks, (int64_t)p.chunks * 2 * C, g.images, C,
                        p.sums, (float*)nullptr, (float*)nullptr);
     PPLL_HIP(hipGetLastError());
-    hipLaunchKernelGGL((group_norm_bwd_piece_kernel<DT, APPLY, VEC, GV, BYTES, CURVED>), grid, block, lds, s, p);
+    p.sum_blocks = columns.x; p.d_scale = d_scale; p.d_shift = d_shift;
+    hipLaunchKernelGGL((group_norm_bwd_piece_kernel<DT, APPLY, VEC, GV, BYTES, CURVED>), dim3(grid.x + columns.x), block, lds, s, p);
     PPLL_HIP(hipGetLastError());
+    return PPLL_OK;
   }
-  hipLaunchKernelGGL(group_norm_sum_kernel, columns, dim3(1024), 0, s, p.sums, g.images, (int64_t)0, 1, C, (float*)nullptr, d_scale, d_shift);
+  hipLaunchKernelGGL(group_norm_sum_kernel, columns, dim3(SUM_THREADS), 0, s, p.sums, g.images, (int64_t)0, 1, C, (float*)nullptr, d_scale, d_shift);
   PPLL_HIP(hipGetLastError());
   return PPLL_OK;
 }
