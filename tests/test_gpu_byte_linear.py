@@ -290,6 +290,13 @@ def test_backward_of_few_rows_and_many_channels(size):
     check_backward(Layer(*size, torch.bfloat16, seed=5, room=1), True)
 
 
+@pytest.mark.parametrize("precision,dtype", TYPES)
+@pytest.mark.parametrize("size", [(1, 1, 2000), (5, 203, 1111), (41, 63, 1645), (130, 19, 777), (129, 300, 1030), (260, 131, 2051), (2, 8, 65536)])
+@pytest.mark.parametrize("want", [("dx", "dw", "db"), ("dx",), ("dx", "db")])
+def test_dx_in_parts_of_its_channels(precision, dtype, size, want):
+    check_backward(Layer(*size, dtype, seed=8, room=3), True, want)
+
+
 def test_backward_of_many_rows():
     check_backward(Layer(8320, 384, 128, torch.bfloat16), True)
     check_backward(Layer(20000, 40, 24, torch.bfloat16))
@@ -348,17 +355,52 @@ def test_dx_in_place_of_the_gate(precision, dtype, size, dw):
 
 
 def test_the_sums_have_a_fixed_order_and_need_nothing_of_the_workspace():
-    l = Layer(3000, 130, 70, torch.bfloat16)
-    dy = l.put(3000, 70)
-    got = []
-    size = P.ppll_byte_linear_workspace_bytes(l.cfg())
-    for fill in (0, 0xff, 0x3c):
-        dx, dw, db = l.empty(3000, 130), torch.empty(130, 70, device=DEV), torch.empty(70, device=DEV)
-        ws = torch.full((size,), fill, dtype=torch.uint8, device=DEV)
-        P.ppll_byte_linear_backward(l.cfg(), l.bytes(l.x), l.bytes(l.w), rows(dy), None, rows(dx), dw, db, ws, size, stream())
-        got.append((dx.view, dw, db))
-    for other in got[1:]:
-        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+    for m, k, n in ((3000, 130, 70), (90, 72, 1500), (1000, 64, 1100)):
+        l = Layer(m, k, n, torch.bfloat16)
+        dy = l.put(m, n)
+        got = []
+        size = P.ppll_byte_linear_workspace_bytes(l.cfg())
+        for fill in (0, 0xff, 0x3c):
+            dx, dw, db = l.empty(m, k), torch.empty(k, n, device=DEV), torch.empty(n, device=DEV)
+            ws = torch.full((size,), fill, dtype=torch.uint8, device=DEV)
+            P.ppll_byte_linear_backward(l.cfg(), l.bytes(l.x), l.bytes(l.w), rows(dy), None, rows(dx), dw, db, ws, size, stream())
+            got.append((dx.view, dw, db))
+        for other in got[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
+def test_calls_on_two_streams_at_once():
+    """Layers and norms with workspaces of their own, in flight together; results as one behind the other."""
+    def make(seed):
+        l = Layer(2500, 200, 600, torch.bfloat16, seed=seed)
+        dy, n = l.put(2500, 600), P.ppll_byte_linear_workspace_bytes(l.cfg())
+        norm = P.group_norm_config(P.BF16, 25, 100, 200, 8, P.ACT_SILU, 1e-5)
+        k = P.ppll_group_norm_workspace_bytes(norm)
+        scale = torch.linspace(0.5, 2, 200, device=DEV)
+
+        def go():
+            ws, ws2 = (torch.empty(max(b, 16), dtype=torch.uint8, device=DEV) for b in (n, k))
+            y, dx, dw, db = l.empty(2500, 600), l.empty(2500, 200), torch.empty(200, 600, device=DEV), torch.empty(600, device=DEV)
+            dn, stats, dg, dh = l.empty(2500, 200), torch.empty(25, 8, 2, device=DEV), torch.empty(200, device=DEV), torch.empty(200, device=DEV)
+            s = torch.cuda.current_stream().cuda_stream
+            for _ in range(5):
+                P.ppll_byte_linear_forward(l.cfg(), l.bytes(l.x), l.bytes(l.w), l.bias, None, rows(y), None, s)
+                P.ppll_byte_linear_backward(l.cfg(), l.bytes(l.x), l.bytes(l.w), rows(dy), None, rows(dx), dw, db, ws, n, s)
+                P.ppll_group_norm_forward(norm, rows(dx), scale, scale, None, rows(dn), stats, None, ws2, k, s)
+                P.ppll_group_norm_backward(norm, rows(dx), None, stats, scale, scale, None, None, rows(dn), rows(dn), None, dg, dh, ws2, k, s)
+            return [y.view, dx.view, dw, db, dn.view, stats, dg, dh], (ws, ws2)
+        return go
+    calls = [make(seed) for seed in (1, 2)]
+    want = [go()[0] for go in calls]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in calls], []
+    for _ in range(3):
+        for go, s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                got.append(go())
+    torch.cuda.synchronize()
+    for i, (g, _) in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(g, want[i % 2]))
 
 
 def test_no_rows():

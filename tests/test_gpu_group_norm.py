@@ -191,6 +191,20 @@ def test_backward(precision, dtype, shape):
     check_backward(Case(*shape, dtype, act="relu", residual=True))
 
 
+# groups of many channels, in pieces of 8 that hold one, two, four or eight segments of them; narrow slabs; more images than workgroups
+WIDE = [(4, 165, 317, 1), (3, 96, 496, 4), (2, 200, 124, 1), (3, 46, 354, 3), (3, 756, 384, 32), (2, 1218, 16, 16), (1, 30, 4096, 1), (1, 900, 4000, 2), (300, 3, 34, 17),
+        (600, 50, 12, 6), (2, 60, 6, 3)]
+
+
+@pytest.mark.parametrize("precision,dtype", TYPES)
+@pytest.mark.parametrize("shape", WIDE)
+@pytest.mark.parametrize("act", ["relu", "gelu"])
+def test_wide_groups_both_ways(precision, dtype, shape, act):
+    check_forward(Case(*shape, dtype, act=act, residual=True, seed=6), kept=True)
+    for from_bytes in (False, True):
+        check_backward(Case(*shape, dtype, act=act, residual=from_bytes, seed=7), from_bytes, d_residual=from_bytes)
+
+
 @pytest.mark.parametrize("precision,dtype", TYPES)
 @pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
 @pytest.mark.parametrize("place", [dict(), dict(room=1), dict(room=5, shift=3), dict(room=8, shift=8)])
