@@ -180,7 +180,7 @@ __global__ __launch_bounds__((Shape<false, false, WGM, WGN, IM, NS, KT>::THREADS
   }
 }
 
-// Few rows (tokens one by one): bound by the weight's bytes and by latency.  A workgroup has 16 channels and 16 RT rows; its eight waves take
+// Few rows (tokens one by one) or few channels: bound by the weight's or the tokens' bytes and by latency.  A workgroup has 16 channels and 16 RT rows; its eight waves take
 // every eighth step of 64 k straight from memory into fragments (k of a fragment: 16 lane / 16 of both operands) and add up in LDS.
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 constexpr int FW = 8;
@@ -188,7 +188,7 @@ template <int DT, int RT>
 __global__ __launch_bounds__(64 * FW) void byte_linear_rows_kernel(ByteArgs p) {
   constexpr int ESZ = DT == BF16 ? 2 : 4;
   __shared__ int part[FW][RT][16][16 + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * RT;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n0 = blockIdx.y * 16, m0 = blockIdx.x * 16 * RT;
   const int r = lane & 15, kl = (lane >> 4) * 16, bytes = 2 * p.K;
   const int8_t* wr = p.w + min(n0 + r, p.N - 1) * p.ldw;      // (rows that are not there: any, their sums are dropped)
   const int8_t* xr[RT];
@@ -253,13 +253,16 @@ template <int DT, int WGM, int WGN, int IM, int NS, int KT> int byte_launch(hipS
   return p.vec ? byte_launch_as<DT, true, WGM, WGN, IM, NS, KT>(s, p, units) : byte_launch_as<DT, false, WGM, WGN, IM, NS, KT>(s, p, units);
 }
 
-constexpr int FEW_ROWS = 64;
+constexpr int FEW_ROWS = 16;
 
 // Which kernel a product goes to: 1 few rows, 3 tiles of 128 x 128 with copying waves, 4 / 8 / 10 tiles of 128 / 256 / 320 rows of 256 columns.
 // Microseconds of a round of workgroups (a unit each, two of kernel 4): per k, and with the epilogue (plain, residual, GELU and its slope); a last round that
 // fills the share f of the units counts as last + (1 - last) f.  Fits to products of 4096 to 32768 rows, 512 to 1536 channels, k of 128 to 4096, within
 // 13 %; 16384 x 1024, k = 1024: 46, 26, 23, 28 us, k = 128 with GELU: 35, 19.3, 19.4, 27; 8192 x 1024, k = 4096: 43, 54, 54, 63; 20480 x 1024, k = 4096:
 // 116, 130, 115, 84.
+// Kernel 1 by its way through k, or by its workgroups of 16 channels and 32 rows where they are many; a tile by itself takes some 1.5 us more than the fits say.
+// Few rows or channels, us, kernel 1 and the best of the tiles: 128 x 768, k = 2560: 6.3, 12.1; 400 x 300, k = 1024: 4.5, 9.0; 1000 x 64, k = 6144: 12.8, 20.2;
+// 256 x 2304, k = 256: 6.5, 7.1; 200 x 2304, k = 1024: 9.1, 8.9; 400 x 768, k = 2560: 13.8, 13.4; 1000 x 768, k = 1024: 12.7, 9.0.
 int choice(const ByteArgs& p, int units) {
   if (p.M <= FEW_ROWS) return 1;
   struct Cost { int kernel, rows, cols, places; double last, k, end[3]; };
@@ -275,14 +278,16 @@ int choice(const ByteArgs& p, int units) {
     const double time = ((double)(tiles / places) + last) * (c.k * 2 * p.K + c.end[p.gelu ? 2 : p.residual ? 1 : 0]);
     if (!best || time < least) { best = c.kernel; least = time; }
   }
-  return best;
+  const double k = 2.0 * p.K, groups = (((int64_t)p.M + 31) / 32) * (((int64_t)p.N + 15) / 16);
+  if (groups > 1 << 20) return best;       // (what a launch holds)
+  return 2.6 + std::max(0.0013 * k, groups * (0.0023 + 4.7e-6 * k)) < least + 1.5 ? 1 : best;
 }
 template <int DT> int forward(hipStream_t s, ByteArgs& p, int kernel) {
   const int units = compute_units() > 0 ? compute_units() : 256;
   if (!kernel) kernel = choice(p, units);
   if (kernel == 1) {
     const int rt = p.M <= 16 ? 1 : 2;
-    const dim3 grid((p.N + 15) / 16, (p.M + 16 * rt - 1) / (16 * rt));
+    const dim3 grid((unsigned)(((int64_t)p.M + 16 * rt - 1) / (16 * rt)), (p.N + 15) / 16);
     if (rt == 1) hipLaunchKernelGGL((byte_linear_rows_kernel<DT, 1>), grid, dim3(64 * FW), 0, s, p);
     else hipLaunchKernelGGL((byte_linear_rows_kernel<DT, 2>), grid, dim3(64 * FW), 0, s, p);
     PPLL_HIP(hipGetLastError());

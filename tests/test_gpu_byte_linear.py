@@ -119,7 +119,7 @@ def test_each_kernel(precision, dtype, kernel, size, place):
     check_forward(Layer(*size, dtype, seed=2, **place), kernel=kernel)
 
 
-@pytest.mark.parametrize("size", [(8320, 384, 1536), (20000, 200, 1536), (9000, 256, 264), (30000, 64, 768), (33000, 130, 512), (50000, 32, 256)])
+@pytest.mark.parametrize("size", [(8320, 384, 1536), (20000, 200, 1536), (9000, 256, 264), (30000, 64, 768), (33000, 130, 512), (50000, 32, 256), (100001, 40, 20), (3000, 100, 33), (40, 300, 6100)])
 def test_forward_of_many_rows(size):
     # every kind of tile that the rules choose among
     m, k, n = size
