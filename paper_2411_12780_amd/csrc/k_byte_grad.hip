@@ -438,18 +438,27 @@ int sum_chunks(int rows) { return (int)(((int64_t)rows + sum_rows(rows) - 1) / s
 // ---- The other way: operands written out in bf16, which is what they stand for, and the products on the kernels of bf16 operands.  Those reach 1100
 // TFLOP/s where the kernel above is held at 750 by LDS (64 x 64 of a wave: 192 KB through it for 64 k of four of them, and the conversion's own way
 // in), but X goes through memory twice more.
-bool values_fit(const ByteLinear& l) {
-  const int64_t most = (1 << 29) - 1;       // elements that the products address
-  return l.dt == BF16 && l.in % 8 == 0 && l.out % 8 == 0 && (int64_t)l.rows * std::max(l.in, l.out) <= most && (int64_t)l.in * l.out <= most;
+constexpr int64_t PRODUCT_BYTES = (1 << 30) - 64;      // that those kernels address of an operand, and of C at 4 bytes an element whatever its type
+bool weight_fits(const ByteLinear& l) { return l.dt == BF16 && l.in % 8 == 0 && l.out % 8 == 0 && (int64_t)l.in * l.out * 2 <= PRODUCT_BYTES; }
+bool both_fit(const ByteLinear& l) {
+  return weight_fits(l) && (int64_t)l.rows * std::max(l.in, l.out) * 2 <= PRODUCT_BYTES && (int64_t)l.in * l.out * 4 <= PRODUCT_BYTES;
 }
-bool lies_whole(const void* p, int64_t ld) { return !p || (ld % 8 == 0 && ((uintptr_t)p & 15) == 0); }
-bool lies_near(const ByteLinear& l, const ppll_rows& r) { return !r.p || l.rows * r.ld < 1 << 29; }       // (elements, as in values_fit)
+// Rows of dX that one product takes: all, or stretches of about as many each (x 4096 from 4096 channels: 65535 rows 1727 us, 65536 in two stretches 1766).
+// 0: rows that lie so far apart that a stretch would be short, which the kernel above takes as they are.
+constexpr int64_t LEAST_STRETCH = 4096;
+int stretch_of(const ByteLinear& l, const ppll_rows& dy, const ppll_rows& gate, const ppll_rows& dx) {
+  const int64_t widest = std::max(dx.ld, (std::max(dy.ld, gate.p ? gate.ld : 0) + 1) / 2), most = PRODUCT_BYTES / 4 / widest;
+  if (l.rows <= most) return l.rows;
+  if (most < LEAST_STRETCH) return 0;
+  const int64_t n = (l.rows + most / 256 * 256 - 1) / (most / 256 * 256);
+  return (int)(((l.rows + n - 1) / n + 255) / 256 * 256);
+}
 // Microseconds, this kernel / values, both gradients, rows x in x out: 8320 x 1536 x 384 51 / 63, 25216 x 768 x 768 101 / 111, 4096 x 2048 x 2048 93 / 99,
 // 8320 x 1536 x 1536 143 / 116, 25216 x 768 x 2304 248 / 191, 8192 x 4096 x 4096 744 / 505, 512 x 6144 x 6144 156 / 138; with few output channels X's way
 // counts for more: 32768 x 4096 x 256 236 / 286.  From 4e10 operations on: 640 x 4096 x 4096 99 / 75, 2560 x 2048 x 2048 81 / 76, 2560 x 4096 x 1024 70.5 / 70.6;
 // below: 5120 x 768 x 2304 65 / 69, 1280 x 2048 x 2048 42 / 44.  Over 114 products of 17 to 20124 rows and 64 to 5680 channels each way the rule costs
 // half a per cent over the better way at each.
-bool values_for_both(const ByteLinear& l) { return values_fit(l) && 4.0 * l.rows * l.in * l.out >= 4e10 && l.out >= 512; }
+bool values_for_both(const ByteLinear& l) { return both_fit(l) && 4.0 * l.rows * l.in * l.out >= 4e10 && l.out >= 512; }
 // (dX alone: W alone is written out.  8320 x 1536 x 384 30 / 24, 25216 x 768 x 768 54 / 35, 640 x 768 x 768 14.7 / 8.6, 8320 x 384 x 384 10.5 / 11.6)
 GemmArgs dw_product(const ByteLinear& l, const uint16_t* xv, const ppll_rows& dy, float* dw, float* db) {
   GemmArgs g{};
@@ -466,22 +475,29 @@ size_t dw_floats(const ByteLinear& l) {       // for the parts of its tiles
   return std::max(floats, gemm_mfma_balanced_floats());
 }
 int64_t values_bytes(const ByteLinear& l, bool x, bool w) { return (((x ? (int64_t)l.rows : 0) + (w ? l.out : 0)) * l.in * 2 + 255) / 256 * 256; }
-bool values_supported(const ByteLinear& l, const ppll_rows& dy, const ppll_rows& gate, const ppll_rows& dx, const float* dw) {
-  return values_fit(l) && lies_near(l, dy) && lies_near(l, gate) && lies_near(l, dx) && lies_whole(dy.p, dy.ld) && lies_whole(gate.p, gate.ld) && lies_whole(dx.p, dx.ld) && lies_whole(dw, l.out);
+GemmArgs dx_product(const ByteLinear& l, const uint16_t* wv, const ppll_rows& dy, const ppll_rows& gate, const ppll_rows& dx, int64_t first, int rows) {
+  GemmArgs g{};
+  g.A = (const uint16_t*)dy.p + first * dy.ld; g.a_dt = BF16; g.a_sm = dy.ld; g.a_sk = 1;
+  g.B = wv; g.b_dt = BF16; g.b_sk = l.in; g.b_sn = 1;
+  g.C = (uint16_t*)dx.p + first * dx.ld; g.c_dt = BF16; g.ldc = dx.ld; g.M = rows; g.N = l.in; g.K = l.out;
+  if (gate.p) { g.epilogue = EPI_DGELU; g.aux = (const uint16_t*)gate.p + first * gate.ld; g.aux_dt = BF16; g.ldaux = gate.ld; }
+  return g;
+}
+// Whether the kernels of bf16 operands take what is wanted; ws: room that begins with the values of X and W
+uint16_t* w_values(const ByteLinear& l, const float* dw, char* ws) { return (uint16_t*)ws + (dw ? (int64_t)l.rows * l.in : 0); }
+bool values_supported(const ByteLinear& l, const ppll_rows& dy, const ppll_rows& gate, const ppll_rows& dx, float* dw, float* db, char* ws) {
+  if (!weight_fits(l) || (dw && (!both_fit(l) || !gemm_mfma_groupable(dw_product(l, (const uint16_t*)ws, dy, dw, db))))) return false;
+  if (!dx.p) return true;
+  const int rows = stretch_of(l, dy, gate, dx);
+  return rows > 0 && gemm_mfma_supported(dx_product(l, w_values(l, dw, ws), dy, gate, dx, 0, rows));
 }
 int backward_values(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
                     const ppll_rows& dx, float* dw, float* db, char* ws) {
-  uint16_t* xv = (uint16_t*)ws;
-  uint16_t* wv = xv + (dw ? (int64_t)l.rows * l.in : 0);
+  uint16_t *xv = (uint16_t*)ws, *wv = w_values(l, dw, ws);
   PPLL_TRY(launch_byte_rows_values(s, l.in, x, dw ? l.rows : 0, w, dx.p ? l.out : 0, xv));
-  if (dx.p) {
-    GemmArgs g{};
-    g.A = dy.p; g.a_dt = BF16; g.a_sm = dy.ld; g.a_sk = 1;
-    g.B = wv; g.b_dt = BF16; g.b_sk = l.in; g.b_sn = 1;
-    g.C = dx.p; g.c_dt = BF16; g.ldc = dx.ld; g.M = l.rows; g.N = l.in; g.K = l.out;
-    if (gate.p) { g.epilogue = EPI_DGELU; g.aux = gate.p; g.aux_dt = BF16; g.ldaux = gate.ld; }
-    PPLL_TRY(launch_gemm(s, g));
-  }
+  const int stretch = dx.p ? stretch_of(l, dy, gate, dx) : 0;
+  for (int64_t first = 0; dx.p && first < l.rows; first += stretch)
+    PPLL_TRY(launch_gemm(s, dx_product(l, wv, dy, gate, dx, first, (int)std::min<int64_t>(stretch, l.rows - first))));
   if (!dw) return PPLL_OK;
   const GemmArgs g = dw_product(l, xv, dy, dw, db);
   return launch_gemm_group(s, &g, 1, (float*)(ws + values_bytes(l, true, true)), dw_floats(l), true);
@@ -542,7 +558,7 @@ int zero(hipStream_t s, float* p, int64_t n) {
 // way: 0 by the rules, 1 the kernel here, 2 values
 int backward(hipStream_t s, int way, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
              const ppll_rows& dx, float* dw, float* db, char* ws) {
-  const bool values = (dx.p || dw) && (dw || !db) && values_supported(l, dy, gate, dx, dw) && (way ? way == 2 : dw ? dx.p && values_for_both(l) : true);
+  const bool values = (dx.p || dw) && (dw || !db) && values_supported(l, dy, gate, dx, dw, db, ws) && (way ? way == 2 : dw ? dx.p && values_for_both(l) : true);
   if (way == 2 && !values) { set_error("not as values"); return PPLL_ERR_CONFIG; }
   if (values) return backward_values(s, l, x, w, dy, gate, dx, dw, db, ws);
   return l.dt == BF16 ? backward_here<BF16>(s, l, x, w, dy, gate, dx, dw, db, (float*)ws) : backward_here<F32>(s, l, x, w, dy, gate, dx, dw, db, (float*)ws);
@@ -551,8 +567,8 @@ size_t workspace(const ByteLinear& l, bool any) {
   if (l.rows <= 0) return 0;
   const int64_t parts = part_floats(dw_parts(l)) + part_floats(dx_parts(l)), sums = sum_chunks(l.rows) > 1 ? (int64_t)sum_chunks(l.rows) * l.out : 0;
   int64_t bytes = std::max(parts, sums) * (int64_t)sizeof(float);
-  if (values_fit(l)) bytes = std::max(bytes, values_bytes(l, false, true));
-  if (any ? values_fit(l) : values_for_both(l)) bytes = std::max(bytes, values_bytes(l, true, true) + (int64_t)(dw_floats(l) * sizeof(float)));
+  if (weight_fits(l)) bytes = std::max(bytes, values_bytes(l, false, true));
+  if (any ? both_fit(l) : values_for_both(l)) bytes = std::max(bytes, values_bytes(l, true, true) + (int64_t)(dw_floats(l) * sizeof(float)));
   return (size_t)bytes;
 }
 }  // namespace

@@ -1,0 +1,85 @@
+"""Which kernels the gradients of linear layers on rows of 8 bits go to, on the CPU: the launches that a call asks a stand-in for the HIP runtime for
+(host_hip.py).  Addresses stand for buffers of any size and are never read."""
+import os
+import subprocess
+
+import pytest
+
+from host_hip import LIB, SOURCE
+
+MAIN = r"""
+struct Rows { void* p; int64_t ld; };
+struct ByteRows { void *q, *e; int64_t ld; };
+struct Config { uint32_t size; int32_t precision, rows, in, out, activation; };
+int main(int, char** argv) {
+  lib = dlopen(argv[1], RTLD_NOW | RTLD_LOCAL);
+  if (!lib) { std::fprintf(stderr, "%s\n", dlerror()); return 2; }
+  Config c{sizeof(Config), 0, 0, 0, 0, 0};
+  long ldy, ldx, ldg;
+  int dx, dw;
+  while (std::cin >> c.precision >> c.rows >> c.in >> c.out >> ldy >> ldx >> ldg >> dx >> dw) {
+    auto at = [](long i) { return (void*)(intptr_t)(i << 44); };
+    const int64_t ld8 = (c.in + 15) / 16 * 16;
+    ByteRows x{at(1), at(2), ld8}, w{at(3), at(4), ld8};
+    Rows gy{at(5), ldy}, gx{at(6), ldx}, gate{at(7), ldg};
+    size_t need = 0;
+    ok(call("ppll_byte_linear_workspace_bytes", &c, &need), "size");
+    std::printf("== %zu\n", need);
+    logging = true;
+    ok(call("ppll_byte_linear_backward", &c, dw ? &x : (ByteRows*)nullptr, dx ? &w : (ByteRows*)nullptr, &gy, dx && ldg ? &gate : (Rows*)nullptr,
+            dx ? &gx : (Rows*)nullptr, dw ? at(8) : nullptr, dw ? at(9) : nullptr, at(10), need, (void*)nullptr), "backward");
+    logging = false;
+  }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def backward(tmp_path_factory):
+    directory = str(tmp_path_factory.mktemp("backward"))
+    src, exe = os.path.join(directory, "b.cpp"), os.path.join(directory, "b")
+    with open(src, "w") as f:
+        f.write(SOURCE.split("int main(")[0] + MAIN)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Wno-unused-function", "-rdynamic", src, "-o", exe, "-ldl"], check=True)
+
+    def run(rows, n_in, n_out, room_y=0, room_x=0, gate=False, dx=True, dw=True, precision=1):
+        line = (precision, rows, n_in, n_out, n_out + room_y, n_in + room_x, n_in if gate else 0, int(dx), int(dw))
+        r = subprocess.run([exe, LIB], input=" ".join(map(str, line)), capture_output=True, text=True, timeout=60)
+        assert r.returncode == 0, r.stderr
+        launches = [(tuple(map(int, f[2:5])), f[7]) for f in (line.split() for line in r.stdout.splitlines()) if f[0] == "launch"]
+        for grid, name in launches:
+            assert grid[1] < 65536 and grid[2] < 65536, (grid, name)       # what a launch holds
+        return launches
+    return run
+
+
+def kernels(launches):
+    return [name for _, name in launches]
+
+
+# both sides of 2^28 elements of dX (where the bf16 kernels end), by columns, by rows' distance, by rows alone
+FAR = [dict(rows=65535, n_in=4096, n_out=4096), dict(rows=65536, n_in=4096, n_out=4096), dict(rows=65536, n_in=6144, n_out=1536),
+       dict(rows=100864, n_in=2816, n_out=768), dict(rows=131071, n_in=2048, n_out=512), dict(rows=200000, n_in=2048, n_out=512),
+       dict(rows=5000000, n_in=64, n_out=64), dict(rows=8192, n_in=1536, n_out=1536, room_x=64000), dict(rows=512, n_in=2048, n_out=2048, room_x=(1 << 19) + 8),
+       dict(rows=512, n_in=8192, n_out=8192, room_x=(1 << 19) + 8), dict(rows=600, n_in=18000, n_out=20000), dict(rows=1024, n_in=4096, n_out=4096, room_y=(1 << 19) + 8)]
+
+
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("dw", [False, True])
+@pytest.mark.parametrize("size", FAR, ids=str)
+def test_no_gradient_is_left_to_the_kernel_without_matrix_instructions(backward, size, dw, gate):
+    names = kernels(backward(**size, dw=dw, gate=gate))
+    assert names and not any("gemm_generic" in n or "gemm_f32" in n for n in names), names
+
+
+def test_dx_of_many_elements_in_stretches_of_rows(backward):
+    # as one product at 65535 x 4096, as two at 65536, on the kernel that reads the bytes where a stretch would be of few rows
+    products = lambda **k: [n for n in kernels(backward(**k, dw=False)) if "gemm" in n]  # noqa: E731
+    assert len(products(rows=65535, n_in=4096, n_out=4096)) == 1
+    assert len(products(rows=65536, n_in=4096, n_out=4096)) == 2
+    one, two = (products(rows=r, n_in=4096, n_out=4096) for r in (32768, 65536))
+    assert two == 2 * one
+    for far in (dict(room_x=(1 << 19) + 8), dict(room_y=(1 << 20) - 2048)):
+        names = kernels(backward(rows=512 + 2048 * ("room_y" in far), n_in=2048, n_out=2048, dw=False, **far))
+        assert names and all("byte_grad" in n for n in names), names
+    assert any("byte_grad_kernel" in n for n in kernels(backward(rows=600, n_in=18000, n_out=20000)))      # dW of 2^28 elements and more
