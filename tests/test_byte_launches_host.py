@@ -1,11 +1,12 @@
-"""Which kernels the gradients of linear layers on rows of 8 bits go to, on the CPU: the launches that a call asks a stand-in for the HIP runtime for
-(host_hip.py).  Addresses stand for buffers of any size and are never read."""
+"""Which kernels the gradients of linear layers on rows of 8 bits, and blocks that multiply such rows, go to, on the CPU: the launches that a call
+asks a stand-in for the HIP runtime for (host_hip.py).  Addresses stand for buffers of any size and are never read."""
 import os
 import subprocess
 
 import pytest
 
-from host_hip import LIB, SOURCE
+from host_hip import LIB, SOURCE, calls, compile_runtime
+from paper_2411_12780_amd import synth
 
 MAIN = r"""
 struct Rows { void* p; int64_t ld; };
@@ -53,6 +54,12 @@ def backward(tmp_path_factory):
     return run
 
 
+@pytest.fixture(scope="module")
+def runtime(tmp_path_factory):
+    exe = compile_runtime(str(tmp_path_factory.mktemp("runtime")))
+    return lambda workloads, *what: calls(exe, workloads, *what)
+
+
 def kernels(launches):
     return [name for _, name in launches]
 
@@ -83,3 +90,22 @@ def test_dx_of_many_elements_in_stretches_of_rows(backward):
         names = kernels(backward(rows=512 + 2048 * ("room_y" in far), n_in=2048, n_out=2048, dw=False, **far))
         assert names and all("byte_grad" in n for n in names), names
     assert any("byte_grad_kernel" in n for n in kernels(backward(rows=600, n_in=18000, n_out=20000)))      # dW of 2^28 elements and more
+
+
+def vit(byte_products, depth, aux_depth, batch=16, dim=128, precision=synth.BF16, **more):
+    return synth.workload("vit_stage_act_bf16", tokens=17, dim=dim, heads=dim // 64, mlp_dim=4 * dim, batch=batch, precision=precision, depth=depth, aux_depth=aux_depth,
+                          byte_products=byte_products, **more)
+
+
+@pytest.mark.parametrize("precision", [synth.FP32, synth.BF16])
+@pytest.mark.parametrize("depth,aux_depth,layers", [(1, 0, 1), (1, 1, 1), (2, 1, 2), (1, 2, 2), (3, 3, 5)])
+def test_every_layer_but_the_pruned_one_multiplies_bytes(runtime, precision, depth, aux_depth, layers):
+    made = lambda bytes_: [[c[5] for c in call if c[0] == "launch"] for call in runtime([vit(bytes_, depth, aux_depth, precision=precision)], "step", "eval", "eval_noalloc")]  # noqa: E731
+    count = lambda names, *parts: sum(any(p in n for p in parts) for n in names)  # noqa: E731
+    for i, names in enumerate(made(1)):
+        assert count(names, "byte_linear") == 4 * layers
+        assert count(names, "byte_rows_pack_columns") == 4 * layers
+        assert count(names, "byte_rows_pack_kernel", "byte_rows_pack_long") == 4 * layers
+        assert count(names, "byte_grad_kernel", "byte_rows_values") == (4 * layers if i == 0 else 0)
+    for names in made(0):
+        assert not count(names, "byte_")
