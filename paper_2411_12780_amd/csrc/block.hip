@@ -646,7 +646,7 @@ int Block::encoder_bwd(int l, const void* x, const void* g_in, void* g_tmp, void
 }
 
 // ---- the encoder layer with its products on rows of 8 bits
-ByteLinear Block::byte_linear(int in, int out, int act) const { return ByteLinear{dt, cfg.batch * cfg.tokens, in, out, act}; }
+ByteLinear Block::byte_linear(int in, int out, int act) const { return ByteLinear{dt, cfg.batch * cfg.tokens, in, out, act, !alone, units}; }
 template <class BUMP> void Block::plan_byte_acts(BUMP& bump, EncoderActs* a) const {
   const size_t M = (size_t)cfg.batch * cfg.tokens;
   const int D = cfg.dim, F = cfg.mlp_dim;

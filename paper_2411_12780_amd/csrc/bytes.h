@@ -23,6 +23,8 @@ int launch_byte_rows_values(hipStream_t s, int cols, const ppll_byte_rows& a, in
 // The linear layer.  residual, slope, bias may have null pointers.
 struct ByteLinear {
   int dt, rows, in, out, activation;
+  bool shared = false;      // as in GemmArgs
+  int units = 0;
 };
 int launch_byte_linear_fwd(hipStream_t s, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const float* bias, const ppll_rows& residual,
                            const ppll_rows& y, const ppll_rows& slope);

@@ -487,6 +487,7 @@ GemmArgs dx_product(const ByteLinear& l, const uint16_t* wv, const ppll_rows& dy
   g.B = wv; g.b_dt = BF16; g.b_sk = l.in; g.b_sn = 1;
   g.C = (uint16_t*)dx.p + first * dx.ld; g.c_dt = BF16; g.ldc = dx.ld; g.M = rows; g.N = l.in; g.K = l.out;
   if (gate.p) { g.epilogue = EPI_DGELU; g.aux = (const uint16_t*)gate.p + first * gate.ld; g.aux_dt = BF16; g.ldaux = gate.ld; }
+  g.shared = l.shared; g.units = l.units;
   return g;
 }
 // Whether the kernels of bf16 operands take what is wanted; ws: room that begins with the values of X and W

@@ -282,8 +282,9 @@ int choice(const ByteArgs& p, int units) {
   if (groups > 1 << 20) return best;       // (what a launch holds)
   return 2.6 + std::max(0.0013 * k, groups * (0.0023 + 4.7e-6 * k)) < least + 1.5 ? 1 : best;
 }
-template <int DT> int forward(hipStream_t s, ByteArgs& p, int kernel) {
-  const int units = compute_units() > 0 ? compute_units() : 256;
+template <int DT> int forward(hipStream_t s, ByteArgs& p, int kernel, int units) {
+  if (!units) units = compute_units();
+  if (units <= 0) units = 256;
   if (!kernel) kernel = choice(p, units);
   if (kernel == 1) {
     const int rt = p.M <= 16 ? 1 : 2;
@@ -310,7 +311,7 @@ int product(hipStream_t s, int kernel, const ByteLinear& l, const ppll_byte_rows
   const int each = l.dt == BF16 ? 8 : 4;
   auto whole = [&](const ppll_rows& r) { return !r.p || (r.ld % each == 0 && ((uintptr_t)r.p & 15) == 0); };
   p.vec = l.out % 8 == 0 && whole(y) && whole(slope) && whole(residual);
-  return l.dt == BF16 ? forward<BF16>(s, p, kernel) : forward<F32>(s, p, kernel);
+  return l.dt == BF16 ? forward<BF16>(s, p, kernel, l.units) : forward<F32>(s, p, kernel, l.units);
 }
 }  // namespace
 

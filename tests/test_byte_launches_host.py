@@ -109,3 +109,21 @@ def test_every_layer_but_the_pruned_one_multiplies_bytes(runtime, precision, dep
         assert count(names, "byte_grad_kernel", "byte_rows_values") == (4 * layers if i == 0 else 0)
     for names in made(0):
         assert not count(names, "byte_")
+
+
+@pytest.mark.parametrize("batch,call", [(50, "step"), (50, "batch"), (4, "batch"), (4, "eval")])
+def test_a_launch_asks_for_the_device_less_than_once(runtime, batch, call):
+    wl = dict(vit(1, 1, 1, batch=batch, dim=1024), tokens=65)
+    (made,) = runtime([wl] * (2 if call == "batch" else 1), call)
+    asked, launches = (sum(c[0] == kind for c in made) for kind in ("device", "launch"))
+    assert asked < launches, (asked, launches)
+
+
+def test_products_of_a_pipeline_leave_the_units_to_each_other(runtime):
+    # dX of the first MLP layer, 3250 rows of 1024 from 4096 channels, in values: alone on 208 tiles with copying waves, one a unit (512 threads, four stages
+    # of 64 k); in a pipeline on what it would be without rows of 8 bits
+    copying = lambda made: [c for c in made if c[0] == "launch" and "gemm_pipe" in c[5] and "ELi2ELi2ELi2ELi4ELi64E" in c[5]]  # noqa: E731
+    wl = dict(vit(1, 1, 0, batch=50, dim=1024), tokens=65)
+    alone, batch = runtime([wl], "step")[0], runtime([wl, wl], "batch")[0]
+    assert any("byte_rows_values" in c[5] for c in alone if c[0] == "launch")
+    assert copying(alone) and not copying(batch)
