@@ -274,6 +274,7 @@ int choice(const ByteArgs& p, int units) {
   double least = 0;
   for (const Cost& c : costs) {
     const int64_t tiles = ((int64_t)p.M + c.rows - 1) / c.rows * (((int64_t)p.N + c.cols - 1) / c.cols), places = (int64_t)c.places * units;
+    if (tiles * (c.kernel == 4 ? 256 : 512) > (int64_t)1 << 31) continue;       // a launch has under 2^32 threads; of kernel 4 there are never more than these
     const double share = std::min(1.0, (double)(tiles % places) / units), last = tiles % places == 0 ? 0 : tiles % places > units ? 1 : c.last + (c.places == 1 ? (1 - c.last) * share : 0);
     const double time = ((double)(tiles / places) + last) * (c.k * 2 * p.K + c.end[p.gelu ? 2 : p.residual ? 1 : 0]);
     if (!best || time < least) { best = c.kernel; least = time; }

@@ -7,7 +7,9 @@ namespace ppll {
 
 namespace {
 constexpr int MOST_ROWS = 1 << 30;
-constexpr int64_t MOST_TILES = 1 << 23;            // workgroups of 256 threads, two products in a launch: under 2^32 threads
+// Tiles of 128 x 128 of a product.  A launch has under 2^32 threads: both gradients have 256 a tile, the forward pass leaves the kernel with 512 out where
+// they are too many.
+constexpr int64_t MOST_TILES = 1 << 23;
 
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 int esz(int32_t precision) { return precision == PPLL_BF16 ? 2 : 4; }

@@ -17,8 +17,8 @@ int main(int, char** argv) {
   if (!lib) { std::fprintf(stderr, "%s\n", dlerror()); return 2; }
   Config c{sizeof(Config), 0, 0, 0, 0, 0};
   long ldy, ldx, ldg;
-  int dx, dw;
-  while (std::cin >> c.precision >> c.rows >> c.in >> c.out >> ldy >> ldx >> ldg >> dx >> dw) {
+  int dx, dw, forward;
+  while (std::cin >> forward >> c.precision >> c.rows >> c.in >> c.out >> ldy >> ldx >> ldg >> dx >> dw) {
     auto at = [](long i) { return (void*)(intptr_t)(i << 44); };
     const int64_t ld8 = (c.in + 15) / 16 * 16;
     ByteRows x{at(1), at(2), ld8}, w{at(3), at(4), ld8};
@@ -27,6 +27,12 @@ int main(int, char** argv) {
     ok(call("ppll_byte_linear_workspace_bytes", &c, &need), "size");
     std::printf("== %zu\n", need);
     logging = true;
+    if (forward) {       // with GELU and its slope, or with a residual (gate), or neither
+      c.activation = forward == 2 ? 3 : 0;
+      ok(call("ppll_byte_linear_forward", &c, &x, &w, at(9), ldg ? &gate : (Rows*)nullptr, &gy, forward == 2 ? &gx : (Rows*)nullptr, (void*)nullptr), "forward");
+      logging = false;
+      continue;
+    }
     ok(call("ppll_byte_linear_backward", &c, dw ? &x : (ByteRows*)nullptr, dx ? &w : (ByteRows*)nullptr, &gy, dx && ldg ? &gate : (Rows*)nullptr,
             dx ? &gx : (Rows*)nullptr, dw ? at(8) : nullptr, dw ? at(9) : nullptr, at(10), need, (void*)nullptr), "backward");
     logging = false;
@@ -36,21 +42,34 @@ int main(int, char** argv) {
 
 
 @pytest.fixture(scope="module")
-def backward(tmp_path_factory):
-    directory = str(tmp_path_factory.mktemp("backward"))
+def program(tmp_path_factory):
+    directory = str(tmp_path_factory.mktemp("linear"))
     src, exe = os.path.join(directory, "b.cpp"), os.path.join(directory, "b")
     with open(src, "w") as f:
         f.write(SOURCE.split("int main(")[0] + MAIN)
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Wno-unused-function", "-rdynamic", src, "-o", exe, "-ldl"], check=True)
 
-    def run(rows, n_in, n_out, room_y=0, room_x=0, gate=False, dx=True, dw=True, precision=1):
-        line = (precision, rows, n_in, n_out, n_out + room_y, n_in + room_x, n_in if gate else 0, int(dx), int(dw))
+    def run(*line):
         r = subprocess.run([exe, LIB], input=" ".join(map(str, line)), capture_output=True, text=True, timeout=60)
         assert r.returncode == 0, r.stderr
-        launches = [(tuple(map(int, f[2:5])), f[7]) for f in (line.split() for line in r.stdout.splitlines()) if f[0] == "launch"]
-        for grid, name in launches:
-            assert grid[1] < 65536 and grid[2] < 65536, (grid, name)       # what a launch holds
-        return launches
+        launches = [(tuple(map(int, f[2:5])), int(f[5]), f[7]) for f in (line.split() for line in r.stdout.splitlines()) if f[0] == "launch"]
+        for grid, threads, name in launches:       # what a launch holds
+            assert grid[1] < 65536 and grid[2] < 65536 and grid[0] * threads < 1 << 32, (grid, threads, name)
+        return [name for _, _, name in launches]
+    return run
+
+
+@pytest.fixture(scope="module")
+def backward(program):
+    def run(rows, n_in, n_out, room_y=0, room_x=0, gate=False, dx=True, dw=True, precision=1):
+        return program(0, precision, rows, n_in, n_out, n_out + room_y, n_in + room_x, n_in if gate else 0, int(dx), int(dw))
+    return run
+
+
+@pytest.fixture(scope="module")
+def forward(program):
+    def run(rows, n_in, n_out, gelu=False, residual=False, precision=1):
+        return program(2 if gelu else 1, precision, rows, n_in, n_out, n_out, n_out, n_out if residual else 0, 0, 0)
     return run
 
 
@@ -60,8 +79,14 @@ def runtime(tmp_path_factory):
     return lambda workloads, *what: calls(exe, workloads, *what)
 
 
-def kernels(launches):
-    return [name for _, name in launches]
+@pytest.mark.parametrize("precision", [0, 1])
+@pytest.mark.parametrize("rows,n_in", [(1 << 30, 16), (1 << 30, 112), ((1 << 30) - 1000, 128), (1 << 29, 256), (1 << 28, 512)])
+@pytest.mark.parametrize("end", [dict(), dict(gelu=True), dict(residual=True)], ids=str)
+def test_a_product_of_very_many_rows_fits_a_launch(forward, precision, rows, n_in, end):
+    # up to 2^23 tiles of 128 x 128, on which a workgroup of the kernel with copying waves has 512 threads
+    for n_out in (8, 128):
+        names = forward(rows, n_in, n_out, precision=precision, **end)
+        assert len(names) == 1 and "byte_linear" in names[0]
 
 
 # both sides of 2^28 elements of dX (where the bf16 kernels end), by columns, by rows' distance, by rows alone
@@ -75,21 +100,21 @@ FAR = [dict(rows=65535, n_in=4096, n_out=4096), dict(rows=65536, n_in=4096, n_ou
 @pytest.mark.parametrize("dw", [False, True])
 @pytest.mark.parametrize("size", FAR, ids=str)
 def test_no_gradient_is_left_to_the_kernel_without_matrix_instructions(backward, size, dw, gate):
-    names = kernels(backward(**size, dw=dw, gate=gate))
+    names = backward(**size, dw=dw, gate=gate)
     assert names and not any("gemm_generic" in n or "gemm_f32" in n for n in names), names
 
 
 def test_dx_of_many_elements_in_stretches_of_rows(backward):
     # as one product at 65535 x 4096, as two at 65536, on the kernel that reads the bytes where a stretch would be of few rows
-    products = lambda **k: [n for n in kernels(backward(**k, dw=False)) if "gemm" in n]  # noqa: E731
+    products = lambda **k: [n for n in backward(**k, dw=False) if "gemm" in n]  # noqa: E731
     assert len(products(rows=65535, n_in=4096, n_out=4096)) == 1
     assert len(products(rows=65536, n_in=4096, n_out=4096)) == 2
     one, two = (products(rows=r, n_in=4096, n_out=4096) for r in (32768, 65536))
     assert two == 2 * one
     for far in (dict(room_x=(1 << 19) + 8), dict(room_y=(1 << 20) - 2048)):
-        names = kernels(backward(rows=512 + 2048 * ("room_y" in far), n_in=2048, n_out=2048, dw=False, **far))
+        names = backward(rows=512 + 2048 * ("room_y" in far), n_in=2048, n_out=2048, dw=False, **far)
         assert names and all("byte_grad" in n for n in names), names
-    assert any("byte_grad_kernel" in n for n in kernels(backward(rows=600, n_in=18000, n_out=20000)))      # dW of 2^28 elements and more
+    assert any("byte_grad_kernel" in n for n in backward(rows=600, n_in=18000, n_out=20000))      # dW of 2^28 elements and more
 
 
 def vit(byte_products, depth, aux_depth, batch=16, dim=128, precision=synth.BF16, **more):
