@@ -74,19 +74,19 @@ class QueriesKeys(C.Structure):
     _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("q_ld", C.c_int64), ("k_ld", C.c_int64)]
 
 
-def _rows(t):
+def _rows(t, what: str):
     """Address and row stride of a 2-d tensor whose last axis is contiguous."""
     if t is None:
         return None, 0
     stride = t.stride()
     if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1):
-        raise PpllError(3, "queries and keys are 2-d tensors with a contiguous last axis")
+        raise PpllError(3, what + " are 2-d tensors with a contiguous last axis")
     return t.data_ptr(), stride[0] if t.shape[0] > 1 else max(stride[0], t.shape[1])
 
 
 def queries_keys(q, k) -> QueriesKeys:
     """2-d tensors [rows, heads * head_dim] whose last axis is contiguous, or None."""
-    (qp, ql), (kp, kl) = _rows(q), _rows(k)
+    (qp, ql), (kp, kl) = (_rows(t, "queries and keys") for t in (q, k))
     return QueriesKeys(qp, kp, ql, kl)
 
 
@@ -113,7 +113,7 @@ class Rows(C.Structure):
 
 def rows(t) -> Rows:
     """A 2-d tensor whose last axis is contiguous."""
-    return Rows(*_rows(t))
+    return Rows(*_rows(t, "rows"))
 
 
 class ByteRows(C.Structure):
@@ -126,7 +126,7 @@ def byte_rows(q, e) -> ByteRows:
     step = e.stride()
     if q.element_size() != 1 or e.element_size() != 1 or len(step) != 1 or (step[0] != 1 and e.shape[0] > 1):
         raise PpllError(3, "rows of 8 bits are an int8 tensor [rows, columns] and contiguous int8 exponents [rows]")
-    p, ld = _rows(q)
+    p, ld = _rows(q, "rows of 8 bits")
     return ByteRows(p, e.data_ptr(), ld)
 
 
