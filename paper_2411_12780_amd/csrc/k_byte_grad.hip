@@ -4,8 +4,12 @@
 // Both products run over the rows of the operand in 8 bits (output channels, tokens), whose other index is contiguous: it lies in LDS as in
 // memory, [k][row], and fragments come out of transposing reads; so does dY in dW, while in dX its k is contiguous.  128 x 128 tiles of four
 // waves, two stages of 64 k in LDS and two in registers.  dY in fp32 is three bf16 terms that add up to it exactly (8 bits each; under 2^-110 off by
-// 2^-134 at most, half of bf16's least step), three products, stages of 32 k.  Operands of any alignment: 16-byte loads from where the elements lie; the last pieces of a ragged row are read ending at the
-// row's end and shifted.  What bounds it: LDS (8320 x 1536 x 384 44 us, 446 TFLOP/s, MFMAs busy for 22 %).
+// 2^-134 at most, half of bf16's least step), three products, stages of 32 k.  Operands of any alignment: 16-byte loads from where the elements lie;
+// the last pieces of a ragged row are read ending at the row's end and shifted.
+//
+// What bounds it: no unit of the chip (8320 x 1536 x 384, both gradients and the sum of their parts 46 us, 426 TFLOP/s: matrix instructions run in 22 % of
+// the kernel's clocks, LDS is at work in 26 %, without conflicts, vector instructions are issued in 36 %; a wave waits for data and barriers in 29 % of its time,
+// for its turn in 32 %), but the order of a stage, load, conversion, LDS, barrier, fragments, products, with two waves a SIMD.
 #include <algorithm>
 
 #include "bytes.h"
@@ -442,8 +446,7 @@ int64_t part_floats(const Parts& p) { return p.n > 1 ? p.n * p.out : 0; }
 int sum_chunks(int rows) { return (int)(((int64_t)rows + sum_rows(rows) - 1) / sum_rows(rows)); }
 
 // ---- The other way: operands written out in bf16, which is what they stand for, and the products on the kernels of bf16 operands.  Those reach 1100
-// TFLOP/s where the kernel above is held at 750 by LDS (64 x 64 of a wave: 192 KB through it for 64 k of four of them, and the conversion's own way
-// in), but X goes through memory twice more.
+// TFLOP/s where the kernel above reaches 750, but X goes through memory twice more.
 constexpr int64_t PRODUCT_BYTES = (1 << 30) - 64;      // that those kernels address of an operand, and of C at 4 bytes an element whatever its type
 bool weight_fits(const ByteLinear& l) { return l.dt == BF16 && l.in % 8 == 0 && l.out % 8 == 0 && (int64_t)l.in * l.out * 2 <= PRODUCT_BYTES; }
 bool both_fit(const ByteLinear& l) {
@@ -459,13 +462,15 @@ int stretch_of(const ByteLinear& l, const ppll_rows& dy, const ppll_rows& gate, 
   const int64_t n = (l.rows + most / 256 * 256 - 1) / (most / 256 * 256);
   return (int)(((l.rows + n - 1) / n + 255) / 256 * 256);
 }
-// Microseconds, this kernel / values, both gradients, rows x in x out: 8320 x 1536 x 384 51 / 63, 25216 x 768 x 768 101 / 111, 4096 x 2048 x 2048 93 / 99,
-// 8320 x 1536 x 1536 143 / 116, 25216 x 768 x 2304 248 / 191, 8192 x 4096 x 4096 744 / 505, 512 x 6144 x 6144 156 / 138; with few output channels X's way
-// counts for more: 32768 x 4096 x 256 236 / 286.  From 4e10 operations on: 640 x 4096 x 4096 99 / 75, 2560 x 2048 x 2048 81 / 76, 2560 x 4096 x 1024 70.5 / 70.6;
-// below: 5120 x 768 x 2304 65 / 69, 1280 x 2048 x 2048 42 / 44.  Over 114 products of 17 to 20124 rows and 64 to 5680 channels each way the rule costs
+// Microseconds with the sum of parts, this kernel / values, both gradients, rows x in x out: 8320 x 1536 x 384 46 / 49, 25216 x 768 x 768 94 / 97,
+// 4096 x 2048 x 2048 94 / 95, 8320 x 1536 x 1536 143 / 106, 25216 x 768 x 2304 243 / 193, 8192 x 4096 x 4096 730 / 517, 512 x 6144 x 6144 153 / 129; with few
+// output channels X's way counts for more: 32768 x 4096 x 256 239 / 284.  From 4e10 operations on: 640 x 4096 x 4096 94 / 67, 2560 x 2048 x 2048 80 / 74, 2560 x
+// 4096 x 1024 67.5 / 67.5; below: 5120 x 768 x 2304 60 / 66, 1280 x 2048 x 2048 40 / 42.  Over 114 products of 17 to 20124 rows and 64 to 5680 channels each way the rule costs
 // half a per cent over the better way at each.
 bool values_for_both(const ByteLinear& l) { return both_fit(l) && 4.0 * l.rows * l.in * l.out >= 4e10 && l.out >= 512; }
-// (dX alone: W alone is written out.  8320 x 1536 x 384 30 / 24, 25216 x 768 x 768 54 / 35, 640 x 768 x 768 14.7 / 8.6, 8320 x 384 x 384 10.5 / 11.6)
+// dX alone: W alone is written out.  8320 x 1536 x 384 24 / 19, 25216 x 768 x 768 48 / 35, 8320 x 384 x 384 10.8 / 10.1, 640 x 768 x 768 13.8 / 8.2, 128 x 1536 x 384
+// 9.7 / 6.9, 64 x 768 x 2304 11.9 / 10.2; behind where few rows meet a large weight, 256 x 4096 x 4096 26 / 41, 1 x 4096 x 4096 14 / 28, which no rule looks at yet.
+// dW alone stays on this kernel, ahead at 8320 x 1536 x 384, 31 / 33, behind at 25216 x 768 x 768, 73 / 65, and 8192 x 4096 x 4096, 386 / 276.
 GemmArgs dw_product(const ByteLinear& l, const uint16_t* xv, const ppll_rows& dy, float* dw, float* db) {
   GemmArgs g{};
   g.A = xv; g.a_dt = BF16; g.a_sm = 1; g.a_sk = l.in;

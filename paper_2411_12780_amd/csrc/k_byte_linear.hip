@@ -180,8 +180,8 @@ __global__ __launch_bounds__((Shape<false, false, WGM, WGN, IM, NS, KT>::THREADS
   }
 }
 
-// Few rows (tokens one by one) or few channels: bound by the weight's or the tokens' bytes and by latency (one token 384 -> 1536 4.0 us; 6144 k 10.5, four steps
-// asked for at once or one).  A workgroup has 16 channels and 16 RT rows; its eight waves take every eighth step of 64 k straight from memory into
+// Few rows (tokens one by one) or few channels: bound by latency, of a step of k for each 512 (one token 384 -> 1536 4.0 us, one step; 6144 -> 1536 10.5, twelve,
+// which wait one for the other with four written out at once or one; its bytes alone 1.8).  A workgroup has 16 channels and 16 RT rows; its eight waves take every eighth step of 64 k straight from memory into
 // fragments (k of a fragment: 16 lane / 16 of both operands) and add up in LDS.
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 constexpr int FW = 8;
