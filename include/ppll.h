@@ -244,10 +244,11 @@ int ppll_pipeline_output(ppll_pipeline_t* pipe, const void** x_out_dev, size_t* 
 int ppll_pipeline_destroy(ppll_pipeline_t* pipe);
 
 /* Measurement aid (no part of the method), per block.  While it is on for a block, every launch of the bf16
- * matrix-core GEMM kernel (gemm_mfma_kernel, all variants) and of the bf16 matrix-core convolution kernel that the
- * block's steps make is bracketed by a pair of HIP events on its own stream (a split-K reduce that may follow is
- * outside the bracket), and the block keeps every launch on the step's own stream (no side stream for weight
- * gradients), so that each bracket holds one kernel running alone.  Other blocks are not affected.
+ * matrix-core GEMM kernel (gemm_mfma_kernel, all variants), of the products on rows of 8 bits (in both types, the
+ * sum of a gradient's parts counted in) and of the bf16 matrix-core convolution kernel that the block's steps make
+ * is bracketed by a pair of HIP events on its own stream (a split-K reduce that may follow is outside the bracket),
+ * and the block keeps every launch on the step's own stream (no side stream for weight gradients), so that each
+ * bracket holds one kernel running alone.  Other blocks are not affected.
  * ppll_block_profile_read waits for those events and returns, since the previous read: the summed duration of the
  * GEMM launches in milliseconds, their algorithmic flops 2*M*N*K, and their count (each pointer nullable);
  * products with fewer than 256 output rows (the class-token products of a pruned last auxiliary layer, Section

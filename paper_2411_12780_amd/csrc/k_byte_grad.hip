@@ -536,7 +536,11 @@ template <int DT> int backward_here(hipStream_t s, const ByteLinear& l, const pp
     pw.M = l.in; pw.N = l.out; pw.K = l.rows; pw.parts = parts.n; pw.part_k = parts.k; pw.part_out = parts.out;
     pw.sums = true;
   }
-  if (dx.p || dw) PPLL_TRY(launch<DT>(s, pw, px));
+  void* prof = nullptr;
+  if (dx.p || dw) {
+    PPLL_TRY(profile_begin(s, 2.0 * ((dx.p ? 1 : 0) + (dw ? 1 : 0)) * l.rows * l.in * l.out, &prof, l.rows < 256 ? 2 : 0));
+    PPLL_TRY(launch<DT>(s, pw, px));
+  }
   if ((dw && !whole) || (dx.p && !x_whole)) {
     SumArgs a{};
     if (dw && !whole) {
@@ -552,6 +556,7 @@ template <int DT> int backward_here(hipStream_t s, const ByteLinear& l, const pp
     hipLaunchKernelGGL(byte_grad_sum_kernel<DT>, dim3(a.first + more), dim3(256), 0, s, a);
     PPLL_HIP(hipGetLastError());
   }
+  PPLL_TRY(profile_end(s, prof));
   if (db && !dw) {
     const int chunks = sum_chunks(l.rows);
     hipLaunchKernelGGL(byte_grad_columns_kernel<DT>, dim3((l.out + SUM_COLS - 1) / SUM_COLS, chunks), dim3(256), 0, s, (const char*)dy.p, dy.ld, l.rows, l.out,

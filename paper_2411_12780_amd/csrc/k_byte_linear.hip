@@ -312,7 +312,10 @@ int product(hipStream_t s, int kernel, const ByteLinear& l, const ppll_byte_rows
   const int each = l.dt == BF16 ? 8 : 4;
   auto whole = [&](const ppll_rows& r) { return !r.p || (r.ld % each == 0 && ((uintptr_t)r.p & 15) == 0); };
   p.vec = l.out % 8 == 0 && whole(y) && whole(slope) && whole(residual);
-  return l.dt == BF16 ? forward<BF16>(s, p, kernel, l.units) : forward<F32>(s, p, kernel, l.units);
+  void* prof = nullptr;
+  PPLL_TRY(profile_begin(s, 2.0 * p.M * l.out * l.in, &prof, p.M < 256 ? 2 : 0));
+  PPLL_TRY(l.dt == BF16 ? forward<BF16>(s, p, kernel, l.units) : forward<F32>(s, p, kernel, l.units));
+  return profile_end(s, prof);
 }
 }  // namespace
 

@@ -101,3 +101,29 @@ def test_muon_updates(precision):
                       for part in np.split(u, 3 if name.endswith(".qkv.w") else 1, axis=1)) ** 0.5
             most += wl["lr"] * off / np.linalg.norm(own.params[name])
         assert rel_l2(params[name], own.params[name]) <= most, name
+
+
+@pytest.mark.parametrize("precision", [synth.FP32, synth.BF16])
+@pytest.mark.parametrize("size", [dict(dim=128, heads=2, depth=2, aux=0, batch=24), dict(dim=66, heads=3, grid=(5, 7), mlp_dim=37, depth=1, aux=0, batch=24),
+                                  dict(dim=768, heads=12, depth=1, aux=0, grid=(15, 16), batch=64, mlp_dim=2304)])
+def test_launch_brackets_count_the_products_of_bytes(precision, size):
+    """Forward, input and weight gradient of the four products of each layer, 2 M N K each, and the same results with the brackets as without."""
+    from gpu_harness import GpuBlock
+    wl = block(precision, **size)
+    flat = synth.make_params(O.param_spec(oracle_cfg(wl)), seed=34, jitter=True)
+    x, y = synth.make_batch(wl, seed=34)
+    losses = []
+    for on in (False, True):
+        gb = GpuBlock(wl, flat)
+        P.ppll_block_profile_enable(gb.h, on)
+        losses.append(gb.step(x, y, 0.01)[1])
+        ms, flops, n = P.ppll_block_profile_read(gb.h)
+        P.ppll_block_profile_enable(gb.h, False)
+        gb.close()
+        M, D, F = wl["batch"] * wl["tokens"], wl["dim"], wl["mlp_dim"]
+        forward = wl["depth"] * 2.0 * M * (D * 3 * D + D * D + 2 * D * F)
+        if on:
+            assert n >= 8 * wl["depth"] and ms > 0 and abs(flops - 3 * forward) <= 1e-6 * flops, (n, ms, flops, 3 * forward)
+        else:
+            assert n == 0
+    assert losses[0] == losses[1]
