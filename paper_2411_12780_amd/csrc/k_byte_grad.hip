@@ -465,8 +465,8 @@ int stretch_of(const ByteLinear& l, const ppll_rows& dy, const ppll_rows& gate, 
 // Microseconds with the sum of parts, this kernel / values, both gradients, rows x in x out: 8320 x 1536 x 384 46 / 49, 25216 x 768 x 768 94 / 97,
 // 4096 x 2048 x 2048 94 / 95, 8320 x 1536 x 1536 143 / 106, 25216 x 768 x 2304 243 / 193, 8192 x 4096 x 4096 730 / 517, 512 x 6144 x 6144 153 / 129; with few
 // output channels X's way counts for more: 32768 x 4096 x 256 239 / 284.  From 4e10 operations on: 640 x 4096 x 4096 94 / 67, 2560 x 2048 x 2048 80 / 74, 2560 x
-// 4096 x 1024 67.5 / 67.5; below: 5120 x 768 x 2304 60 / 66, 1280 x 2048 x 2048 40 / 42.  Over 114 products of 17 to 20124 rows and 64 to 5680 channels each way the rule costs
-// half a per cent over the better way at each.
+// 4096 x 1024 67.5 / 67.5; below: 5120 x 768 x 2304 60 / 66, 1280 x 2048 x 2048 40 / 42.  Over 114 products of 17 to 20124 rows and 64 to 5680 channels each
+// way the rule costs half a per cent over the better way at each.
 bool values_for_both(const ByteLinear& l) { return both_fit(l) && 4.0 * l.rows * l.in * l.out >= 4e10 && l.out >= 512; }
 // dX alone: W alone is written out.  8320 x 1536 x 384 24 / 19, 25216 x 768 x 768 48 / 35, 8320 x 384 x 384 10.8 / 10.1, 640 x 768 x 768 13.8 / 8.2, 128 x 1536 x 384
 // 9.7 / 6.9, 64 x 768 x 2304 11.9 / 10.2; behind where few rows meet a large weight, 256 x 4096 x 4096 26 / 41, 1 x 4096 x 4096 14 / 28, which no rule looks at yet.
@@ -575,7 +575,7 @@ int zero(hipStream_t s, float* p, int64_t n) {
 // way: 0 by the rules, 1 the kernel here, 2 values
 int backward(hipStream_t s, int way, const ByteLinear& l, const ppll_byte_rows& x, const ppll_byte_rows& w, const ppll_rows& dy, const ppll_rows& gate,
              const ppll_rows& dx, float* dw, float* db, char* ws) {
-  const bool values = (dx.p || dw) && (dw || !db) && values_supported(l, dy, gate, dx, dw, db, ws) && (way ? way == 2 : dw ? dx.p && values_for_both(l) : true);
+  const bool values = (dx.p || dw) && (dw || !db) && (way ? way == 2 : dw ? dx.p && values_for_both(l) : true) && values_supported(l, dy, gate, dx, dw, db, ws);
   if (way == 2 && !values) { set_error("not as values"); return PPLL_ERR_CONFIG; }
   if (values) return backward_values(s, l, x, w, dy, gate, dx, dw, db, ws);
   return l.dt == BF16 ? backward_here<BF16>(s, l, x, w, dy, gate, dx, dw, db, (float*)ws) : backward_here<F32>(s, l, x, w, dy, gate, dx, dw, db, (float*)ws);
