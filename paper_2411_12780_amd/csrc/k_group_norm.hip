@@ -3,8 +3,9 @@
 // A thread holds pieces of 8 channels of every RT-th pixel in registers, so that an image (or a slab of its channels, whole groups) that fits the
 // registers of a workgroup is read once and written once: mean, then the squares about it, then the result.  A larger image goes in pieces of pixels:
 // statistics of each piece, joined exactly, then the result, the map read a second time, from the last-level cache where it fits.  What bounds it:
-// the latency of loads, of which more would have to be on their way (16 x 96 x 96 x 256 bf16 in pieces, kept in 8 bits, 34 + 5 + 36 us: 3.3 and 4.2 TB/s, a copy
-// 5.2; waves wait in 52 to 67 % of their time; 1024 x 32 x 32 x 16 in one go 24 us, 2.8 TB/s: load, two sums over a workgroup and store one behind the other).
+// loads that wait and vector instructions, neither alone (16 x 96 x 96 x 256 bf16 in pieces, kept in 8 bits, 34 + 5 + 36 us: 3.3 and 4.2 TB/s, a copy 5.2; waves
+// wait in 58 and 66 % of their time, vector instructions are issued in 62 and 49 % of the clocks; 1024 x 32 x 32 x 16 in one go 24 us, 2.8 TB/s: load, two sums
+// over a workgroup and store one behind the other).
 #include "group_norm.h"
 
 namespace ppll {

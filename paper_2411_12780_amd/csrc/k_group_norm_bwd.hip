@@ -3,9 +3,10 @@
 // the means over a group of one image.  Both come from the sums of dz and dz xhat of each channel over an image.
 //
 // An image (or a slab of its channels, whole groups) that fits the registers of a workgroup is read once; a larger one goes in pieces of pixels, once
-// for the channel sums and once for the gradient.  Channel sums of the images are added in a launch behind, in their order.  What bounds it: the
-// latency of loads, with SiLU and GELU also the slopes' instructions (16 x 96 x 96 x 256 bf16 with SiLU in pieces 46 + 5 + 44 us, 3.3 and 5.2 TB/s, a copy's rate in
-// the second reading; waves wait in 59 % of their time in the first; 1024 x 32 x 32 x 16 with ReLU in one go 42 us, 3.2 TB/s).
+// for the channel sums and once for the gradient.  Channel sums of the images are added in a launch behind, in their order.  What bounds it: loads
+// that wait, with SiLU and GELU also the slopes' instructions (16 x 96 x 96 x 256 bf16 with SiLU in pieces 46 + 5 + 44 us, 3.3 and 5.2 TB/s, a copy's rate in the
+// second reading; waves wait in 59 % of their time in the first, vector instructions are issued in 53 % of its clocks; 1024 x 32 x 32 x 16 with ReLU in one go
+// 42 us, 3.2 TB/s).
 #include "group_norm.h"
 
 namespace ppll {
